@@ -18,10 +18,13 @@ TARGETS = {
                         ["pong_rules.cuh", "pong_kernels.cuh", os.path.join(INCLUDE, "pong.h")]),
     "libcartpole_b200.so": (["cartpole.cu"], [os.path.join(INCLUDE, "cartpole.h")]),
     "libgru_policy_b200.so": (["gru_policy.cu"], [os.path.join(INCLUDE, "gru_policy.h")]),
+    "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],
+                       ["ssm_common.cuh", "ssm_kernels.cuh", os.path.join(INCLUDE, "ssm.h")]),
 }
 LIB = os.path.join(HERE, "libpong_b200.so")
 CARTPOLE_LIB = os.path.join(HERE, "libcartpole_b200.so")
 GRU_POLICY_LIB = os.path.join(HERE, "libgru_policy_b200.so")
+SSM_LIB = os.path.join(HERE, "libssm_b200.so")
 
 
 def _nvcc() -> str:
@@ -51,7 +54,7 @@ def build_one(name: str, force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale(name):
         return lib
     tmp = lib + ".tmp.%d" % os.getpid()
-    cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", tmp] + src
+    cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["--threads", "0", "-o", tmp] + src
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose:
         sys.stderr.write(res.stderr)
@@ -74,3 +77,4 @@ if __name__ == "__main__":
     print(LIB)
     print(CARTPOLE_LIB)
     print(GRU_POLICY_LIB)
+    print(SSM_LIB)

@@ -1,0 +1,634 @@
+// ssm_scan_backward.cu -- gradients of the selective scan.
+//
+//     dh_t   = g_t c_t + E_t,    E_{t-1} = a_t dh_t  (zero where t starts an episode),   a_t = exp(delta_t A)
+//     dc_t   = sum_d g h_t       db_t = sum_d dh_t delta x
+//     pull   = sum_n dh_t b      S    = sum_n A dh_t a_t h_{t-1}
+//     dx     = D g + delta pull  d delta = S + x pull   dA += delta dh_t a_t h_{t-1}
+// with g = dy z sigmoid(z).  The recurrence of E runs backwards and needs h_t, which the forward
+// pass saved at the start of every chunk of steps.
+//
+// A thread owns 4 channels x 4 states, a warp 32 channels x 16 states: sums over channels (db,
+// dc) and over states (pull, S, y) are each formed over four values in registers first, and
+// both then take eight or four lanes.  Halving exchanges leave every lane with one total: of
+// the lane's own channel for the sums over states, of one (b or c, state) for the sums over
+// channels, so that the per-channel arithmetic is spread over the warp without repetition.
+//
+// Per chunk the warp runs the recurrence forward once, keeping h at every fourth step in
+// shared memory; then it takes the groups of four steps from the last to the first, recomputes
+// a_t and a_t h_{t-1} of the four steps into registers and walks them backwards.  Beyond 16
+// states the blocks of 16 states follow one another within the chunk.
+//
+// db and dc of a block's 128 channels are added in shared memory, those of different blocks by
+// k_scan_dbc; dA, dD and d dt_bias stay with the block over all its rows and are added by
+// k_scan_params: fixed orders, no atomics.
+#include "ssm_kernels.cuh"
+
+namespace ssm_k {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kGroup = 4;      // steps walked backwards out of registers
+
+__device__ __forceinline__ Pair zero_pair() { return Pair{0ull}; }
+
+// v[0..3] over the four lanes that share lane >> 2: lane gets the total of v[lane & 3].
+__device__ __forceinline__ float spread4(const float (&v)[4], int lane)
+{
+    const bool b1 = lane & 2, b0 = lane & 1;
+    const float s0 = b1 ? v[0] : v[2], s1 = b1 ? v[1] : v[3];
+    const float k0 = (b1 ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
+    const float k1 = (b1 ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, s1, 2);
+    return (b0 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? k0 : k1, 1);
+}
+
+// v[0..7] over the eight lanes that share lane & 3: lane gets the total of
+// v[4 * bit 4 + 2 * bit 3 + bit 2 of lane].
+__device__ __forceinline__ float spread8(const float (&v)[8], int lane)
+{
+    const bool b4 = lane & 16, b3 = lane & 8, b2 = lane & 4;
+    float k[4], m[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k[i] = (b4 ? v[4 + i] : v[i]) + __shfl_xor_sync(0xFFFFFFFFu, b4 ? v[i] : v[4 + i], 16);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) m[i] = (b3 ? k[2 + i] : k[i]) + __shfl_xor_sync(0xFFFFFFFFu, b3 ? k[i] : k[2 + i], 8);
+    return (b2 ? m[1] : m[0]) + __shfl_xor_sync(0xFFFFFFFFu, b2 ? m[0] : m[1], 4);
+}
+
+__device__ __forceinline__ void load4(Pair (&dst)[2], const float *src)   // 16-byte aligned
+{
+    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(src);
+    dst[0].v = v.x;
+    dst[1].v = v.y;
+}
+
+__device__ __forceinline__ void store4(float *dst, const Pair (&src)[2])
+{
+    *reinterpret_cast<ulonglong2 *>(dst) = make_ulonglong2(src[0].v, src[1].v);
+}
+
+template <int CH, int SB>
+struct Smem {
+    static constexpr int kStates = 16 * SB;
+    static constexpr int kBc = CH * 2 * kStates * 2;                    // floats: every value twice
+    static constexpr int kCheck = (CH / kGroup) * 16 * 32;              // per warp: h at every fourth step
+    static constexpr int kScal = CH * 2 * 32;                           // per warp: delta, delta x
+    static constexpr int kG = kGroup * 32;                              // per warp: g of the group's steps
+    static constexpr int kAcc = SB > 1 ? CH * 3 * 32 : 0;               // per warp: y, pull, S of earlier state blocks
+    static constexpr int kCarry = SB > 1 ? SB * 16 * 32 : 0;            // per warp: E; as many again: dA
+    static constexpr int kWarp = kCheck + kScal + kG + kAcc + 2 * kCarry;
+    static constexpr int kBytes = (kBc + kWarps * kWarp) * 4;
+};
+
+template <typename T, int CH, int SB>
+__global__ void __launch_bounds__(kThreads, 2)
+k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
+{
+    using S = Smem<CH, SB>;
+    constexpr int NS = S::kStates;
+    extern __shared__ __align__(16) float smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    float *s_bc = smem;                               // [CH][b|c][NS][2]
+    float *s_check = smem + S::kBc + warp * S::kWarp;   // [CH/4][4 states][32 lanes][4 channels]
+    float *s_scal = s_check + S::kCheck;              // [CH][delta|delta x][32]
+    float *s_g = s_scal + S::kScal;                   // [4][32]
+    float *s_acc = s_g + S::kG;                       // [CH][y|pull|S][32]
+    float *s_e = s_acc + S::kAcc;                     // [SB][4 states][32 lanes][4 channels]
+    float *s_da = s_e + S::kCarry;
+
+    const int tile = static_cast<int>(blockIdx.x % (tiles * s.groups));
+    const int slot = static_cast<int>(blockIdx.x / (tiles * s.groups));
+    const int g = tile / tiles;
+    const int tile_in_group = tile - g * tiles;
+    const int local0 = tile_in_group * kThreads + warp * 32;
+    const int d0 = g * s.group_channels + local0;     // the warp's first channel
+    const bool warp_live = local0 < s.group_channels;
+    const bool live = local0 + lane < s.group_channels;   // the lane's own channel
+    const int own = live ? d0 + lane : 0;
+    const int ch = 4 * (lane >> 2);                   // the thread's first channel within the warp
+    const int quad = lane & 3;                        // the thread's states within a block of 16
+    const int live4 = min(4, s.group_channels - (local0 + ch));   // how many of its channels exist (may be <= 0)
+    const float bias = p.dt_bias != nullptr && live ? p.dt_bias[own] : 0.0f;
+    const float skip = p.d != nullptr && live ? p.d[own] : 0.0f;
+    const bool gated = q.z.ptr != nullptr;
+    float dd = 0.0f, ddt_bias = 0.0f;
+    // E and dA of the state block at hand: with a single block they stay here, else in shared memory between chunks
+    Pair e[4][2], da[4][2];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) da[n][0] = da[n][1] = zero_pair();
+    if (SB > 1)
+        for (int i = 0; i < 4 * SB; ++i) store4(s_da + (i * 32 + lane) * 4, da[0]);
+
+    for (int64_t unit = slot; unit < s.batch * s.segments; unit += s.slots) {
+        const int64_t b = unit / s.segments;
+        const int seg = static_cast<int>(unit - b * s.segments);
+        const int c_first = seg * (s.segment_steps / CH);
+        const int c_last = min(s.chunks, c_first + s.segment_steps / CH) - 1;
+
+        // gradient that arrives from the steps after the segment
+        for (int sb = 0; sb < SB; ++sb) {
+            float in[4][4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int state = sb * 16 + 4 * quad + n;
+                    in[n][c] = 0.0f;
+                    if (c >= live4 || state >= s.states) continue;
+                    if (seg < s.segments - 1)
+                        in[n][c] = p.carry[(((b * s.segments + seg) * s.quads + sb * 4 + quad) * s.channels + d0 + ch + c) * 4 + n];
+                    else if (p.dstate_out != nullptr)
+                        in[n][c] = p.dstate_out[(b * s.channels + d0 + ch + c) * s.states + state];
+                }
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                e[n][0] = pair(in[n][0], in[n][1]);
+                e[n][1] = pair(in[n][2], in[n][3]);
+                if (SB > 1) store4(s_e + ((sb * 4 + n) * 32 + lane) * 4, e[n]);
+            }
+        }
+
+        for (int chunk = c_last; chunk >= c_first; --chunk) {
+            const int tc = chunk * CH;
+            const int steps = min(CH, s.time - tc);
+            const int groups = (steps + kGroup - 1) / kGroup;
+            for (int i = tid; i < CH * 2 * NS; i += kThreads) {
+                const int k = i / (2 * NS), n = i % NS;
+                const Seq<const T> &src = (i / NS) & 1 ? q.c : q.b;
+                const float v = k < steps && n < s.states ? to_f32(src.row(b, tc + k)[g * s.states + n]) : 0.0f;
+                *reinterpret_cast<float2 *>(s_bc + 2 * i) = make_float2(v, v);
+            }
+            uint32_t resets = 0;
+            if (q.reset.ptr != nullptr)
+                resets = __ballot_sync(0xFFFFFFFFu, lane < steps && *q.reset.row(b, tc + min(lane, steps - 1)) != 0);
+            if (warp_live) {
+#pragma unroll 8
+                for (int k = 0; k < CH; ++k) {
+                    const bool in = live && k < steps;
+                    const float x = in ? to_f32(q.x.row(b, tc + k)[own]) : 0.0f;
+                    const float delta = in ? softplus(to_f32(q.dt.row(b, tc + k)[own]) + bias) : 0.0f;
+                    s_scal[(2 * k) * 32 + lane] = delta;
+                    s_scal[(2 * k + 1) * 32 + lane] = delta * x;
+                }
+            }
+            __syncthreads();
+
+            for (int sb = 0; sb < SB; ++sb) {
+                if (warp_live) {
+                    Pair a2[4][2], h[4][2];
+                    {
+                        float av[4][4], hv[4][4];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const bool in = c < live4;
+                            const int64_t row = d0 + ch + (in ? c : 0);
+                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            if (in && sb * 4 + quad < s.quads)
+                                v = reinterpret_cast<const float4 *>(p.saved)[((b * s.chunks + chunk) * s.quads + sb * 4 + quad) * s.channels + row];
+                            hv[0][c] = v.x;
+                            hv[1][c] = v.y;
+                            hv[2][c] = v.z;
+                            hv[3][c] = v.w;
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                const int state = sb * 16 + 4 * quad + n;
+                                av[n][c] = in && state < s.states ? p.a[row * s.states + state] * kLog2e : 0.0f;
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                a2[n][c] = pair(av[n][2 * c], av[n][2 * c + 1]);
+                                h[n][c] = pair(hv[n][2 * c], hv[n][2 * c + 1]);
+                            }
+                    }
+                    const float *bc = s_bc + (sb * 16 + 4 * quad) * 2;
+
+                    // forward over the chunk: h before every group of steps
+                    for (int grp = 0; grp < groups; ++grp) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) store4(s_check + ((grp * 4 + n) * 32 + lane) * 4, h[n]);
+                        if (grp == groups - 1) break;
+#pragma unroll
+                        for (int j = 0; j < kGroup; ++j) {
+                            const int k = grp * kGroup + j;
+                            Pair delta[2], dtx[2];
+                            load4(delta, s_scal + (2 * k) * 32 + ch);
+                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
+                            if ((resets >> k) & 1u) {
+#pragma unroll
+                                for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
+                            }
+                            Pair bb[4];
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    h[n][c] = fma(ex2(mul(a2[n][c], delta[c])), h[n][c], mul(dtx[c], bb[n]));
+                        }
+                    }
+                    if (SB > 1) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            load4(e[n], s_e + ((sb * 4 + n) * 32 + lane) * 4);
+                            load4(da[n], s_da + ((sb * 4 + n) * 32 + lane) * 4);
+                        }
+                    }
+
+                    for (int grp = groups - 1; grp >= 0; --grp) {
+                        // the lane's own channel
+                        float x[kGroup], raw[kGroup], z[kGroup], dy[kGroup], gr[kGroup], sz[kGroup], yp[kGroup];
+#pragma unroll
+                        for (int j = 0; j < kGroup; ++j) {
+                            const int k = grp * kGroup + j;
+                            const bool in = live && k < steps;
+                            x[j] = in ? to_f32(q.x.row(b, tc + k)[own]) : 0.0f;
+                            raw[j] = in ? to_f32(q.dt.row(b, tc + k)[own]) + bias : 0.0f;
+                            dy[j] = in ? to_f32(q.dy.row(b, tc + k)[own]) : 0.0f;
+                            z[j] = in && gated ? to_f32(q.z.row(b, tc + k)[own]) : 0.0f;
+                        }
+#pragma unroll
+                        for (int j = 0; j < kGroup; ++j) {
+                            sz[j] = sigmoid(z[j]);
+                            gr[j] = gated ? dy[j] * z[j] * sz[j] : dy[j];
+                            s_g[j * 32 + lane] = gr[j];
+                        }
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) load4(h[n], s_check + ((grp * 4 + n) * 32 + lane) * 4);
+                        __syncwarp();
+
+                        Pair at[kGroup][4][2], ah[kGroup][4][2];
+#pragma unroll
+                        for (int j = 0; j < kGroup; ++j) {
+                            const int k = grp * kGroup + j;
+                            Pair delta[2], dtx[2], bb[4], cc[4];
+                            load4(delta, s_scal + (2 * k) * 32 + ch);
+                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[0]), bc + (2 * k + 1) * NS * 2);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[2]), bc + (2 * k + 1) * NS * 2 + 4);
+                            if ((resets >> k) & 1u) {
+#pragma unroll
+                                for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
+                            }
+                            Pair y2[2] = {zero_pair(), zero_pair()};
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) {
+                                    at[j][n][c] = ex2(mul(a2[n][c], delta[c]));
+                                    ah[j][n][c] = mul(at[j][n][c], h[n][c]);
+                                    h[n][c] = fma(dtx[c], bb[n], ah[j][n][c]);
+                                    y2[c] = fma(cc[n], h[n][c], y2[c]);
+                                }
+                            const float yv[4] = {lo(y2[0]), hi(y2[0]), lo(y2[1]), hi(y2[1])};
+                            yp[j] = spread4(yv, lane);
+                        }
+#pragma unroll
+                        for (int j = kGroup - 1; j >= 0; --j) {
+                            const int k = grp * kGroup + j;
+                            Pair delta[2], dtx[2], gg[2], bb[4], cc[4];
+                            load4(delta, s_scal + (2 * k) * 32 + ch);
+                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
+                            load4(gg, s_g + j * 32 + ch);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[0]), bc + (2 * k + 1) * NS * 2);
+                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[2]), bc + (2 * k + 1) * NS * 2 + 4);
+                            Pair pull[2] = {zero_pair(), zero_pair()}, sa[2] = {zero_pair(), zero_pair()};
+                            float dbc[8];
+                            const bool first = (resets >> k) & 1u;
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                Pair db2 = zero_pair(), dc2 = zero_pair();
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) {
+                                    const Pair ht = fma(dtx[c], bb[n], ah[j][n][c]);
+                                    dc2 = fma(gg[c], ht, dc2);
+                                    const Pair dh = fma(gg[c], cc[n], e[n][c]);
+                                    db2 = fma(dtx[c], dh, db2);
+                                    pull[c] = fma(bb[n], dh, pull[c]);
+                                    const Pair qq = mul(dh, ah[j][n][c]);
+                                    sa[c] = fma(a2[n][c], qq, sa[c]);
+                                    da[n][c] = fma(delta[c], qq, da[n][c]);
+                                    e[n][c] = first ? zero_pair() : mul(at[j][n][c], dh);
+                                }
+                                dbc[n] = lo(db2) + hi(db2);
+                                dbc[4 + n] = lo(dc2) + hi(dc2);
+                            }
+                            const float total = spread8(dbc, lane);
+                            const float pv[4] = {lo(pull[0]), hi(pull[0]), lo(pull[1]), hi(pull[1])};
+                            const float sv[4] = {lo(sa[0]), hi(sa[0]), lo(sa[1]), hi(sa[1])};
+                            float own_pull = spread4(pv, lane), own_s = spread4(sv, lane), own_y = yp[j];
+                            // the group's place in s_check has been read: its first words take the sums over channels
+                            s_check[grp * 4 * 128 + j * 32 + (lane & 16) + 4 * quad + ((lane >> 2) & 3)] = total;
+                            if (SB > 1) {
+                                float *acc = s_acc + (3 * k) * 32 + lane;
+                                if (sb > 0) {
+                                    own_y += acc[0];
+                                    own_pull += acc[32];
+                                    own_s += acc[64];
+                                }
+                                acc[0] = own_y;
+                                acc[32] = own_pull;
+                                acc[64] = own_s;
+                            }
+                            if (sb == SB - 1 && live && k < steps) {
+                                const float own_delta = s_scal[(2 * k) * 32 + lane];
+                                const float ypre = fmaf(skip, x[j], own_y);
+                                if (gated)
+                                    q.dz.row(b, tc + k)[own] =
+                                        from_f32<T>(dy[j] * ypre * fmaf(z[j] * sz[j], 1.0f - sz[j], sz[j]));
+                                q.dx.row(b, tc + k)[own] = from_f32<T>(fmaf(own_delta, own_pull, skip * gr[j]));
+                                const float ddt = fmaf(x[j], own_pull, kLn2 * own_s) * sigmoid(raw[j]);
+                                q.ddt.row(b, tc + k)[own] = from_f32<T>(ddt);
+                                ddt_bias += ddt;
+                                dd = fmaf(gr[j], x[j], dd);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (SB > 1) {
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            store4(s_e + ((sb * 4 + n) * 32 + lane) * 4, e[n]);
+                            store4(s_da + ((sb * 4 + n) * 32 + lane) * 4, da[n]);
+                        }
+                    }
+                }
+                __syncthreads();
+                // the block's channels together: warp w takes every fourth step
+                const int warps = min(kWarps, (s.group_channels - tile_in_group * kThreads + 31) / 32);
+                for (int k = warp; k < steps; k += kWarps) {
+                    float sum = 0.0f;
+                    for (int w = 0; w < warps; ++w)
+                        sum += smem[S::kBc + w * S::kWarp + (k / kGroup) * 4 * 128 + (k % kGroup) * 32 + lane];
+                    const int64_t row = (static_cast<int64_t>(tile_in_group) * s.batch + b) * s.time + tc + k;
+                    p.dbc_part[((row * s.groups + g) * 2 + (lane >> 4)) * NS + sb * 16 + (lane & 15)] = sum;
+                }
+                __syncthreads();
+            }
+        }
+
+        if (seg == 0 && p.dstate != nullptr && warp_live) {
+            for (int sb = 0; sb < SB; ++sb) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int state = sb * 16 + 4 * quad + n;
+                    if (SB > 1) load4(e[n], s_e + ((sb * 4 + n) * 32 + lane) * 4);
+                    const float out[4] = {lo(e[n][0]), hi(e[n][0]), lo(e[n][1]), hi(e[n][1])};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (c < live4 && state < s.states)
+                            p.dstate[(b * s.channels + d0 + ch + c) * s.states + state] = out[c];
+                }
+            }
+        }
+    }
+
+    if (!warp_live) return;
+    for (int sb = 0; sb < SB; ++sb) {
+        const int q4 = sb * 4 + quad;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            if (SB > 1) load4(da[n], s_da + ((sb * 4 + n) * 32 + lane) * 4);
+            const float out[4] = {lo(da[n][0]), hi(da[n][0]), lo(da[n][1]), hi(da[n][1])};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (c < live4 && q4 < s.quads)
+                    p.da_part[((static_cast<int64_t>(slot) * s.quads + q4) * s.channels + d0 + ch + c) * 4 + n] = out[c];
+        }
+    }
+    if (live) {
+        p.dd_part[(static_cast<int64_t>(slot) * 2) * s.channels + own] = dd;
+        p.dd_part[(static_cast<int64_t>(slot) * 2 + 1) * s.channels + own] = ddt_bias;
+    }
+}
+
+// The recurrence of E over a segment from a zero end, a channel (or a 16-state part) per thread
+// as in the forward kernel.
+template <typename T, int NP, int LN>
+__global__ void __launch_bounds__(128)
+k_scan_back_summary(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
+{
+    constexpr int NS = NP * LN, kTile = 8;
+    __shared__ __align__(16) float s_c[kTile][NS];
+    __shared__ uint8_t s_reset[kTile];
+    const int tid = threadIdx.x;
+    int64_t unit = blockIdx.x;
+    const int tile = static_cast<int>(unit % (tiles * s.groups));
+    unit /= tiles * s.groups;
+    const int seg = static_cast<int>(unit % s.segments);
+    const int64_t b = unit / s.segments;
+    if (seg == 0) return;                             // nothing lies before the first segment
+    const int g = tile / tiles;
+    const int part = tid % LN;
+    const int local = (tile - g * tiles) * (128 / LN) + tid / LN;
+    const bool live = local < s.group_channels;
+    const int d = g * s.group_channels + (live ? local : 0);
+    const int t0 = seg * s.segment_steps;
+    const int t1 = min(s.time, t0 + s.segment_steps);
+    Pair a2[NP / 2], e[NP / 2];
+#pragma unroll
+    for (int i = 0; i < NP; i += 2) {
+        const int n = part * NP + i;
+        const float *row = p.a + static_cast<int64_t>(d) * s.states;
+        a2[i / 2] = pair(live && n < s.states ? row[n] * kLog2e : 0.0f,
+                         live && n + 1 < s.states ? row[n + 1] * kLog2e : 0.0f);
+        e[i / 2] = zero_pair();
+    }
+    const float bias = p.dt_bias != nullptr && live ? p.dt_bias[d] : 0.0f;
+    const bool gated = q.z.ptr != nullptr;
+    float span = 0.0f;
+    bool cut = false;
+    for (int t = t0 + (t1 - 1 - t0) / kTile * kTile; t >= t0; t -= kTile) {
+        float dt[kTile], gr[kTile];
+#pragma unroll
+        for (int k = 0; k < kTile; ++k) {
+            const bool in = live && t + k < t1;
+            dt[k] = in ? to_f32(q.dt.row(b, t + k)[d]) : 0.0f;
+            gr[k] = in ? to_f32(q.dy.row(b, t + k)[d]) : 0.0f;
+            if (gated) {
+                const float z = in ? to_f32(q.z.row(b, t + k)[d]) : 0.0f;
+                gr[k] *= z * sigmoid(z);
+            }
+        }
+        __syncthreads();
+        for (int i = tid; i < kTile * NS; i += 128) {
+            const int k = i / NS, n = i % NS;
+            s_c[k][n] = t + k < t1 && n < s.states ? to_f32(q.c.row(b, t + k)[g * s.states + n]) : 0.0f;
+        }
+        if (tid < kTile) s_reset[tid] = q.reset.ptr != nullptr && t + tid < t1 ? *q.reset.row(b, t + tid) : 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = kTile - 1; k >= 0; --k) {
+            if (t + k >= t1) continue;
+            const float delta = softplus(dt[k] + bias);
+            const Pair dd = pair(delta, delta), gg = pair(gr[k], gr[k]);
+            const bool first = s_reset[k] != 0;
+            cut |= first;
+            span += delta;
+#pragma unroll
+            for (int i = 0; i < NP / 2; ++i) {
+                Pair c;
+                c.v = *reinterpret_cast<const unsigned long long *>(&s_c[k][part * NP + 2 * i]);
+                e[i] = first ? zero_pair() : mul(ex2(mul(a2[i], dd)), fma(gg, c, e[i]));
+            }
+        }
+    }
+    if (!live) return;
+#pragma unroll
+    for (int i = 0; i < NP / 4; ++i) {
+        const int64_t at = ((b * s.segments + seg) * s.quads + part * (NP / 4) + i) * s.channels + d;
+        reinterpret_cast<float4 *>(p.carry)[at] = make_float4(lo(e[2 * i]), hi(e[2 * i]), lo(e[2 * i + 1]), hi(e[2 * i + 1]));
+    }
+    if (part == 0) p.span[(b * s.segments + seg) * s.channels + d] = cut ? -1.0f : span;
+}
+
+// Turns what leaves each segment at its start (from a zero end) into what arrives at its end, in place.
+__global__ void __launch_bounds__(256)
+k_scan_back_carry(const ScanShape s, const ScanParams p)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int64_t per_row = static_cast<int64_t>(s.quads) * s.channels;
+    if (i >= s.batch * per_row) return;
+    const int64_t b = i / per_row;
+    const int quad = static_cast<int>((i - b * per_row) / s.channels);
+    const int d = static_cast<int>(i % s.channels);
+    float a[4], e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int n = 4 * quad + k;
+        const bool in = n < s.states;
+        a[k] = in ? p.a[static_cast<int64_t>(d) * s.states + n] * kLog2e : 0.0f;
+        e[k] = in && p.dstate_out != nullptr ? p.dstate_out[(b * s.channels + d) * s.states + n] : 0.0f;
+    }
+    for (int seg = s.segments - 1; seg >= 0; --seg) {
+        float4 *slot = reinterpret_cast<float4 *>(p.carry) + ((b * s.segments + seg) * s.quads + quad) * s.channels + d;
+        const float4 out = seg > 0 ? *slot : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float span = seg > 0 ? p.span[(b * s.segments + seg) * s.channels + d] : 0.0f;
+        *slot = make_float4(e[0], e[1], e[2], e[3]);
+        const float outs[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = span < 0.0f ? outs[k] : fmaf(ex2(a[k] * span), e[k], outs[k]);
+    }
+}
+
+// db and dc: the sum over the blocks of a group's channels, in block order.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_scan_dbc(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles, const int padded)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int64_t rows = s.batch * s.time * s.groups;
+    const int n = static_cast<int>(i % padded);
+    const int64_t which_row = i / padded;             // (row, b | c)
+    if (which_row >= 2 * rows || n >= s.states) return;
+    float sum = 0.0f;
+    for (int k = 0; k < tiles; ++k) sum += p.dbc_part[(k * 2 * rows + which_row) * padded + n];
+    const int64_t row = which_row >> 1;
+    const int g = static_cast<int>(row % s.groups);
+    const int64_t bt = row / s.groups;
+    const int64_t b = bt / s.time;
+    const Seq<T> &dst = which_row & 1 ? q.dc : q.db;
+    dst.row(b, bt - b * s.time)[g * s.states + n] = from_f32<T>(sum);
+}
+
+// dA, dD, d dt_bias: the sum over the slots.  32 neighbouring channels per warp, every eighth
+// slot per warp, the eight sums added in order.  blockIdx.y: a quad of states, or the last: dD and d dt_bias.
+__global__ void __launch_bounds__(256)
+k_scan_params(const ScanShape s, const ScanParams p)
+{
+    __shared__ float4 part[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int d = blockIdx.x * 32 + lane;
+    const int quad = blockIdx.y;
+    const bool rates = quad < s.quads;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (d < s.channels) {
+#pragma unroll 4
+        for (int k = warp; k < s.slots; k += 8) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (rates) {
+                v = reinterpret_cast<const float4 *>(p.da_part)[(static_cast<int64_t>(k) * s.quads + quad) * s.channels + d];
+            } else {
+                v.x = p.dd_part[(static_cast<int64_t>(k) * 2) * s.channels + d];
+                v.y = p.dd_part[(static_cast<int64_t>(k) * 2 + 1) * s.channels + d];
+            }
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+    }
+    part[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || d >= s.channels) return;
+    for (int w = 1; w < 8; ++w) {
+        const float4 v = part[w][lane];
+        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+    if (rates) {
+        const float out[4] = {sum.x, sum.y, sum.z, sum.w};
+        for (int n = 0; n < 4; ++n)
+            if (4 * quad + n < s.states) p.da[static_cast<int64_t>(d) * s.states + 4 * quad + n] = out[n];
+    } else {
+        if (p.dd != nullptr) p.dd[d] = sum.x;
+        if (p.ddt_bias != nullptr) p.ddt_bias[d] = sum.y;
+    }
+}
+
+template <typename T, int NP, int LN>
+void launch_summary(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
+{
+    const int tiles = (s.group_channels + 128 / LN - 1) / (128 / LN);
+    const unsigned blocks = static_cast<unsigned>(s.batch * s.segments * s.groups * tiles);
+    k_scan_back_summary<T, NP, LN><<<blocks, 128, 0, stream>>>(s, p, q, tiles);
+}
+
+template <typename T, int CH, int SB>
+int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
+{
+    using S = Smem<CH, SB>;
+    static_assert(S::kBytes <= 227 * 1024, "one block's shared memory");
+    const int tiles = (s.group_channels + kThreads - 1) / kThreads;
+    int launched = 3;
+    if (cudaFuncSetAttribute(k_scan_backward<T, CH, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) !=
+        cudaSuccess)
+        return -1;
+    if (s.segments > 1) {
+        if (s.states <= 4)
+            launch_summary<T, 4, 1>(s, p, q, stream);
+        else if (s.states <= 8)
+            launch_summary<T, 8, 1>(s, p, q, stream);
+        else
+            launch_summary<T, 16, SB>(s, p, q, stream);
+        const int64_t threads = s.batch * s.quads * s.channels;
+        k_scan_back_carry<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, stream>>>(s, p);
+        launched += 2;
+    }
+    k_scan_backward<T, CH, SB><<<static_cast<unsigned>(tiles * s.groups) * s.slots, kThreads, S::kBytes, stream>>>(s, p, q, tiles);
+    const int64_t values = s.batch * s.time * s.groups * 2 * S::kStates;
+    k_scan_dbc<T><<<static_cast<unsigned>((values + 255) / 256), 256, 0, stream>>>(s, p, q, tiles, S::kStates);
+    const dim3 grid(static_cast<unsigned>((s.channels + 31) / 32), static_cast<unsigned>(s.quads + 1));
+    k_scan_params<<<grid, 256, 0, stream>>>(s, p);
+    return cudaGetLastError() == cudaSuccess ? launched : -1;
+}
+
+}  // namespace
+
+template <typename T>
+int launch_scan_backward(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
+{
+    if (s.states <= 16) return launch<T, 32, 1>(s, p, q, stream);
+    if (s.states <= 32) return launch<T, 16, 2>(s, p, q, stream);
+    return launch<T, 16, 4>(s, p, q, stream);
+}
+
+template int launch_scan_backward<float>(const ScanShape &, const ScanParams &, const ScanSeqs<float> &, cudaStream_t);
+template int launch_scan_backward<__nv_bfloat16>(const ScanShape &, const ScanParams &, const ScanSeqs<__nv_bfloat16> &,
+                                                 cudaStream_t);
+template int launch_scan_backward<__half>(const ScanShape &, const ScanParams &, const ScanSeqs<__half> &, cudaStream_t);
+
+}  // namespace ssm_k

@@ -1,0 +1,389 @@
+// ssm_scan_forward.cu -- the selective scan over a sequence and its single-token form.
+//
+// k_scan_forward: a thread owns one channel (or, beyond 16 states, a 16-state part of one) and
+// walks the time axis with the recurrent state in registers:
+//     e = 2^(delta a log2 e),  h = e h + (delta x) b,  y += c h        per state
+// on packed pairs of states.  A warp's 32 channels are neighbours, so every access to x, dt, z
+// and y is one contiguous piece per step at any alignment; b and c, which all channels of a
+// group share, are staged as binary32 in shared memory, eight steps at a time, the next eight
+// steps' loads in flight meanwhile.
+//
+// Few rows: the time axis is cut into segments that run side by side.  k_scan_summary forms
+// each segment's end state from a zero start; since the decay over a whole segment is
+// exp(a * sum delta), k_scan_carry joins the segments with one exponential per state and
+// segment, and k_scan_forward then runs every segment from its true start.
+#include "ssm_kernels.cuh"
+
+namespace ssm_k {
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kTile = 8;     // steps whose loads are in flight together
+
+template <int NP>
+__device__ __forceinline__ void load_pairs(Pair (&dst)[NP / 2], const float *src)   // 16-byte aligned
+{
+#pragma unroll
+    for (int i = 0; i < NP / 4; ++i) {
+        const ulonglong2 v = reinterpret_cast<const ulonglong2 *>(src)[i];
+        dst[2 * i].v = v.x;
+        dst[2 * i + 1].v = v.y;
+    }
+}
+
+template <typename T, int NP, int LN, bool kSummary>
+__global__ void __launch_bounds__(kThreads)
+k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
+{
+    constexpr int NS = NP * LN;
+    constexpr int kWidth = (kSummary ? 1 : 2) * NS;               // staged values per step: b (and c)
+    constexpr int kStage = (kTile * kWidth + kThreads - 1) / kThreads;
+    __shared__ __align__(16) float s_bc[2][kTile][kWidth];
+    __shared__ uint8_t s_reset[2][kTile];
+
+    const int tid = threadIdx.x;
+    int64_t unit = blockIdx.x;
+    const int tile = static_cast<int>(unit % (tiles * s.groups));
+    unit /= tiles * s.groups;
+    const int seg = static_cast<int>(unit % s.segments);
+    const int64_t b = unit / s.segments;
+    if (kSummary && seg == s.segments - 1) return;                // nobody asks for the last segment's end
+    const int g = tile / tiles;
+    const int part = tid % LN;
+    const int local = (tile - g * tiles) * (kThreads / LN) + tid / LN;
+    const bool live = local < s.group_channels;
+    const bool warp_live = (tile - g * tiles) * (kThreads / LN) + (tid & ~31) / LN < s.group_channels;
+    const int d = g * s.group_channels + (live ? local : 0);
+    const int t0 = seg * s.segment_steps;
+    const int t1 = min(s.time, t0 + s.segment_steps);
+
+    Pair a2[NP / 2], h[NP / 2];
+#pragma unroll
+    for (int i = 0; i < NP; i += 2) {
+        const int n = part * NP + i;
+        const float *row = p.a + static_cast<int64_t>(d) * s.states;
+        a2[i / 2] = pair(live && n < s.states ? row[n] * kLog2e : 0.0f,
+                         live && n + 1 < s.states ? row[n + 1] * kLog2e : 0.0f);
+        h[i / 2] = pair(0.0f, 0.0f);
+    }
+    if (!kSummary && live) {
+        if (s.segments > 1) {
+#pragma unroll
+            for (int i = 0; i < NP / 4; ++i) {
+                const int64_t at = ((b * s.segments + seg) * s.quads + part * (NP / 4) + i) * s.channels + d;
+                const float4 v = reinterpret_cast<const float4 *>(p.carry)[at];
+                h[2 * i] = pair(v.x, v.y);
+                h[2 * i + 1] = pair(v.z, v.w);
+            }
+        } else if (p.state != nullptr) {
+            const float *row = p.state + (b * s.channels + d) * s.states;
+#pragma unroll
+            for (int i = 0; i < NP; i += 2) {
+                const int n = part * NP + i;
+                h[i / 2] = pair(n < s.states ? row[n] : 0.0f, n + 1 < s.states ? row[n + 1] : 0.0f);
+            }
+        }
+    }
+    const float bias = p.dt_bias != nullptr && live ? p.dt_bias[d] : 0.0f;
+    const float skip = p.d != nullptr && live ? p.d[d] : 0.0f;
+    const bool gated = !kSummary && q.z.ptr != nullptr;
+
+    // the next tile's values, in flight while the current one is worked on
+    T nx[kTile], ndt[kTile], nz[kTile], nbc[kStage];
+    uint8_t nreset = 0;
+    auto fetch = [&](int t) {
+        if (warp_live) {
+#pragma unroll
+            for (int k = 0; k < kTile; ++k) {
+                const bool in = live && t + k < t1;
+                nx[k] = in ? q.x.row(b, t + k)[d] : from_f32<T>(0.0f);
+                ndt[k] = in ? q.dt.row(b, t + k)[d] : from_f32<T>(0.0f);
+                if (!kSummary) nz[k] = in && gated ? q.z.row(b, t + k)[d] : from_f32<T>(0.0f);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kStage; ++k) {
+            const int i = k * kThreads + tid;
+            const int step = i / kWidth, n = i % NS;
+            const bool in = i < kTile * kWidth && t + step < t1 && n < s.states;
+            const Seq<const T> &src = (i / NS) % (kWidth / NS) == 0 ? q.b : q.c;
+            nbc[k] = in ? src.row(b, t + step)[g * s.states + n] : from_f32<T>(0.0f);
+        }
+        if (tid < kTile) nreset = q.reset.ptr != nullptr && t + tid < t1 ? *q.reset.row(b, t + tid) : 0;
+    };
+    fetch(t0);
+
+    float span = 0.0f;
+    bool cut = false;
+    int buf = 0;
+    for (int t = t0; t < t1; t += kTile, buf ^= 1) {
+        T cx[kTile], cdt[kTile], cz[kTile];
+#pragma unroll
+        for (int k = 0; k < kTile; ++k) {
+            cx[k] = nx[k];
+            cdt[k] = ndt[k];
+            cz[k] = nz[k];
+        }
+#pragma unroll
+        for (int k = 0; k < kStage; ++k) {
+            const int i = k * kThreads + tid;
+            if (i < kTile * kWidth) (&s_bc[buf][0][0])[i] = to_f32(nbc[k]);
+        }
+        if (tid < kTile) s_reset[buf][tid] = nreset;
+        __syncthreads();
+        if (t + kTile < t1) fetch(t + kTile);
+        if (!warp_live) continue;
+        if (!kSummary && p.saved != nullptr && t % s.chunk == 0 && live) {
+#pragma unroll
+            for (int i = 0; i < NP / 4; ++i) {
+                const int64_t at = ((b * s.chunks + t / s.chunk) * s.quads + part * (NP / 4) + i) * s.channels + d;
+                reinterpret_cast<float4 *>(p.saved)[at] =
+                    make_float4(lo(h[2 * i]), hi(h[2 * i]), lo(h[2 * i + 1]), hi(h[2 * i + 1]));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kTile; ++k) {
+            if (t + k >= t1) break;
+            const float x = to_f32(cx[k]);
+            const float delta = softplus(to_f32(cdt[k]) + bias);
+            if (s_reset[buf][k]) {
+                cut = true;
+#pragma unroll
+                for (int i = 0; i < NP / 2; ++i) h[i] = pair(0.0f, 0.0f);
+            }
+            span += delta;
+            const Pair dd = pair(delta, delta), dx = pair(delta * x, delta * x);
+            Pair bb[NP / 2], cc[NP / 2];
+            load_pairs<NP>(bb, &s_bc[buf][k][part * NP]);
+            if (!kSummary) load_pairs<NP>(cc, &s_bc[buf][k][NS * (kWidth / NS - 1) + part * NP]);
+            Pair acc[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+#pragma unroll
+            for (int i = 0; i < NP / 2; ++i) {
+                h[i] = fma(ex2(mul(a2[i], dd)), h[i], mul(dx, bb[i]));
+                if (!kSummary) acc[i & 1] = fma(cc[i], h[i], acc[i & 1]);
+            }
+            if (!kSummary) {
+                const Pair sum = add(acc[0], acc[1]);
+                float y = lo(sum) + hi(sum);
+#pragma unroll
+                for (int m = 1; m < LN; m *= 2) y += __shfl_xor_sync(0xFFFFFFFFu, y, m);
+                y = fmaf(skip, x, y);
+                if (gated) {
+                    const float z = to_f32(cz[k]);
+                    y *= z * sigmoid(z);
+                }
+                if (live && part == 0) q.y.row(b, t + k)[d] = from_f32<T>(y);
+            }
+        }
+    }
+    if (!live) return;
+    if (kSummary) {
+#pragma unroll
+        for (int i = 0; i < NP / 4; ++i) {
+            const int64_t at = ((b * s.segments + seg) * s.quads + part * (NP / 4) + i) * s.channels + d;
+            reinterpret_cast<float4 *>(p.carry)[at] =
+                make_float4(lo(h[2 * i]), hi(h[2 * i]), lo(h[2 * i + 1]), hi(h[2 * i + 1]));
+        }
+        if (part == 0) p.span[(b * s.segments + seg) * s.channels + d] = cut ? -1.0f : span;
+    } else if (t1 == s.time && p.state_out != nullptr) {
+        float *row = p.state_out + (b * s.channels + d) * s.states;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int n = part * NP + i;
+            if (n < s.states) row[n] = i & 1 ? hi(h[i / 2]) : lo(h[i / 2]);
+        }
+    }
+}
+
+// Turns the segments' ends (from a zero start) into their starts, in place.
+__global__ void __launch_bounds__(256)
+k_scan_carry(const ScanShape s, const ScanParams p)
+{
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int64_t per_row = static_cast<int64_t>(s.quads) * s.channels;
+    if (i >= s.batch * per_row) return;
+    const int64_t b = i / per_row;
+    const int quad = static_cast<int>((i - b * per_row) / s.channels);
+    const int d = static_cast<int>(i % s.channels);
+    float a[4], h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int n = 4 * quad + e;
+        const bool in = n < s.states;
+        a[e] = in ? p.a[static_cast<int64_t>(d) * s.states + n] * kLog2e : 0.0f;
+        h[e] = in && p.state != nullptr ? p.state[(b * s.channels + d) * s.states + n] : 0.0f;
+    }
+    for (int seg = 0; seg < s.segments; ++seg) {
+        const int64_t at = ((b * s.segments + seg) * s.quads + quad) * s.channels + d;
+        float4 *slot = reinterpret_cast<float4 *>(p.carry) + at;
+        const bool last = seg == s.segments - 1;
+        const float4 end = last ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *slot;
+        const float span = last ? 0.0f : p.span[(b * s.segments + seg) * s.channels + d];
+        *slot = make_float4(h[0], h[1], h[2], h[3]);
+        const float ends[4] = {end.x, end.y, end.z, end.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = span < 0.0f ? ends[e] : fmaf(ex2(a[e] * span), h[e], ends[e]);
+    }
+}
+
+template <typename T, int NP, int LN>
+int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
+{
+    const int per_block = kThreads / LN;
+    const int tiles = (s.group_channels + per_block - 1) / per_block;
+    const unsigned blocks = static_cast<unsigned>(s.batch * s.segments * s.groups * tiles);
+    int launched = 1;
+    if (s.segments > 1) {
+        k_scan_forward<T, NP, LN, true><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
+        const int64_t threads = s.batch * s.quads * s.channels;
+        k_scan_carry<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, stream>>>(s, p);
+        launched += 2;
+    }
+    k_scan_forward<T, NP, LN, false><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
+    return cudaGetLastError() == cudaSuccess ? launched : -1;
+}
+
+// ---- one token
+//
+// The state passes through memory once; 4 states make one 16-byte access and neighbouring lanes
+// hold neighbouring quads, so a warp's accesses to the state are contiguous.  A block keeps its
+// channels' parameters and walks rows.
+
+constexpr int kStepThreads = 256;
+constexpr int kStepRows = 4;    // rows whose states are in flight together
+
+template <typename T, int LPC, bool kAligned>
+__global__ void __launch_bounds__(kStepThreads)
+k_scan_step(const StepParams p, const T *__restrict__ x, const T *__restrict__ dt, const T *__restrict__ z,
+            const T *__restrict__ bv, const T *__restrict__ cv, T *__restrict__ y, const int rows_per_block)
+{
+    constexpr int kChannels = kStepThreads / LPC;
+    const int part = threadIdx.x % LPC;
+    const int c0 = blockIdx.x * kChannels + threadIdx.x / LPC;
+    const bool live = c0 < p.channels;
+    const int d = live ? c0 : p.channels - 1;
+    const int g = d / p.group_channels;
+    const int n0 = 4 * part;
+    float a2[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        a2[e] = n0 + e < p.states ? p.a[static_cast<int64_t>(d) * p.states + n0 + e] * kLog2e : 0.0f;
+    const float bias = p.dt_bias != nullptr ? p.dt_bias[d] : 0.0f;
+    const float skip = p.d != nullptr ? p.d[d] : 0.0f;
+    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * rows_per_block;
+    const int64_t r1 = r0 + rows_per_block < p.n ? r0 + rows_per_block : p.n;
+    for (int64_t r = r0; r < r1; r += kStepRows) {
+        float h[kStepRows][4];
+        float xv[kStepRows], dv[kStepRows], zv[kStepRows], bb[kStepRows][4], cc[kStepRows][4];
+#pragma unroll
+        for (int k = 0; k < kStepRows; ++k) {
+            const int64_t row = r + k < r1 ? r + k : r1 - 1;
+            const float *src = p.state + (row * p.channels + d) * p.states + n0;
+            const bool clear = p.done != nullptr && p.done[row * p.done_stride] != 0;
+            if (kAligned) {
+                const float4 v = n0 < p.states ? *reinterpret_cast<const float4 *>(src) : make_float4(0, 0, 0, 0);
+                h[k][0] = v.x;
+                h[k][1] = v.y;
+                h[k][2] = v.z;
+                h[k][3] = v.w;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[k][e] = n0 + e < p.states ? src[e] : 0.0f;
+            }
+            if (clear) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[k][e] = 0.0f;
+            }
+            xv[k] = to_f32(x[row * p.x_stride + d]);
+            dv[k] = to_f32(dt[row * p.dt_stride + d]);
+            zv[k] = z != nullptr ? to_f32(z[row * p.z_stride + d]) : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = n0 + e < p.states;
+                bb[k][e] = in ? to_f32(bv[row * p.b_stride + g * p.states + n0 + e]) : 0.0f;
+                cc[k][e] = in ? to_f32(cv[row * p.c_stride + g * p.states + n0 + e]) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kStepRows; ++k) {
+            const float delta = softplus(dv[k] + bias);
+            const float dx = delta * xv[k];
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                h[k][e] = fmaf(ex2(delta * a2[e]), h[k][e], dx * bb[k][e]);
+                sum = fmaf(cc[k][e], h[k][e], sum);
+            }
+#pragma unroll
+            for (int m = 1; m < LPC; m *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
+            sum = fmaf(skip, xv[k], sum);
+            if (z != nullptr) sum *= zv[k] * sigmoid(zv[k]);
+            if (live && r + k < r1) {
+                const int64_t row = r + k;
+                float *dst = p.state_out + (row * p.channels + d) * p.states + n0;
+                if (kAligned) {
+                    if (n0 < p.states) *reinterpret_cast<float4 *>(dst) = make_float4(h[k][0], h[k][1], h[k][2], h[k][3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (n0 + e < p.states) dst[e] = h[k][e];
+                }
+                if (part == 0) y[row * p.y_stride + d] = from_f32<T>(sum);
+            }
+        }
+    }
+}
+
+template <typename T, int LPC>
+int launch_step(const StepParams &p, const T *x, const T *dt, const T *z, const T *b, const T *c, T *y,
+                cudaStream_t stream)
+{
+    const int per_block = kStepThreads / LPC;
+    const unsigned tiles = static_cast<unsigned>((p.channels + per_block - 1) / per_block);
+    // rows per block: enough blocks for eight per SM, then longer walks that reuse the parameters
+    int64_t chunks = (static_cast<int64_t>(8) * p.sms + tiles - 1) / tiles;
+    if (chunks < (p.n + 63) / 64) chunks = (p.n + 63) / 64;
+    if (chunks > (p.n + kStepRows - 1) / kStepRows) chunks = (p.n + kStepRows - 1) / kStepRows;
+    if (chunks > 65535) chunks = 65535;
+    const int64_t rows = (p.n + chunks - 1) / chunks;
+    const dim3 grid(tiles, static_cast<unsigned>((p.n + rows - 1) / rows));
+    if (p.states % 4 == 0)
+        k_scan_step<T, LPC, true><<<grid, kStepThreads, 0, stream>>>(p, x, dt, z, b, c, y, static_cast<int>(rows));
+    else
+        k_scan_step<T, LPC, false><<<grid, kStepThreads, 0, stream>>>(p, x, dt, z, b, c, y, static_cast<int>(rows));
+    return cudaGetLastError() == cudaSuccess ? 1 : -1;
+}
+
+}  // namespace
+
+template <typename T>
+int launch_scan_forward(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
+{
+    if (s.states <= 4) return launch<T, 4, 1>(s, p, q, stream);
+    if (s.states <= 8) return launch<T, 8, 1>(s, p, q, stream);
+    if (s.states <= 16) return launch<T, 16, 1>(s, p, q, stream);
+    if (s.states <= 32) return launch<T, 16, 2>(s, p, q, stream);
+    return launch<T, 16, 4>(s, p, q, stream);
+}
+
+template <typename T>
+int launch_scan_step(const StepParams &p, const T *x, const T *dt, const T *z, const T *b, const T *c, T *y,
+                     cudaStream_t stream)
+{
+    if (p.states <= 4) return launch_step<T, 1>(p, x, dt, z, b, c, y, stream);
+    if (p.states <= 8) return launch_step<T, 2>(p, x, dt, z, b, c, y, stream);
+    if (p.states <= 16) return launch_step<T, 4>(p, x, dt, z, b, c, y, stream);
+    if (p.states <= 32) return launch_step<T, 8>(p, x, dt, z, b, c, y, stream);
+    return launch_step<T, 16>(p, x, dt, z, b, c, y, stream);
+}
+
+#define SSM_INSTANTIATE(T)                                                                                     \
+    template int launch_scan_forward<T>(const ScanShape &, const ScanParams &, const ScanSeqs<T> &,            \
+                                        cudaStream_t);                                                         \
+    template int launch_scan_step<T>(const StepParams &, const T *, const T *, const T *, const T *,           \
+                                     const T *, T *, cudaStream_t);
+SSM_INSTANTIATE(float)
+SSM_INSTANTIATE(__nv_bfloat16)
+SSM_INSTANTIATE(__half)
+
+}  // namespace ssm_k

@@ -98,3 +98,24 @@ def test_gru_policy_library_exports_every_declared_symbol():
     assert L.gru_policy_create(ctypes.byref(h), 64, 6, 3, *([None] * 8)) == -2
     assert L.gru_policy_destroy(None) == -2 and L.gru_policy_status(None) == -2
     assert L.gru_policy_cell(None, None, None, None, 1) == -2
+
+
+def test_ssm_library_exports_every_declared_symbol():
+    from paper_2603_12145_b200 import ssm
+    lib = ctypes.CDLL(build.build_one("libssm_b200.so"))
+    names = declared_symbols("ssm.h", "ssm")
+    assert len(names) >= 14
+    for name in names:
+        assert hasattr(lib, name), name
+    assert set(names) == set(ssm.EXPORTS)
+    L = ssm.load(build_if_missing=True)
+    assert ssm.strerror(0) == "ok" and ssm.strerror(-99) == "unknown error"
+    h = ctypes.c_void_p()
+    # argument checks that run before any CUDA call
+    assert L.ssm_create(None, 64, 16, 1, 4, 1) == -2
+    for bad in ((0, 16, 1, 4, 1), (64, 0, 1, 4, 1), (64, 65, 1, 4, 1), (64, 16, 3, 4, 1), (64, 16, 1, 5, 1),
+                (64, 16, 1, 1, 1), (64, 16, 1, 4, 3), (65537, 16, 1, 4, 1)):
+        assert L.ssm_create(ctypes.byref(h), *bad) == -1
+    assert L.ssm_destroy(None) == -2 and L.ssm_set_stream(None, None) == -2
+    assert L.ssm_scan_forward(None, None) == -2 and L.ssm_conv_backward(None, None) == -2
+    assert L.ssm_scan_saved_bytes(None, 1, 1) == 0
