@@ -1,0 +1,952 @@
+// gated_ffn.cu -- the gated feed-forward block (forward, backward) as sm_100a kernels behind the
+// C ABI of gated_ffn.h.
+//
+// k_product is one matrix product D = A B^T on CTA pairs (tcgen05, cta_group::2) with three
+// epilogues.  A pair's tile is 256 rows of A by 256 (or 192, 128) rows of B; each block of the pair
+// stages 128 rows of A and half of the rows of B per 64 reduction elements, the leader issues
+// M = 256 instructions into one of two 256-column accumulator buffers, and eight epilogue warps
+// per block empty the other one meanwhile.
+//
+//   kGated    forward: the leader stages 128 gate rows of W_in as its half of B, its peer the
+//             128 rows of the other projection, so that columns c and 128 + c of every
+//             accumulator row are g and u of one hidden unit: act(g) u is formed in registers.
+//   kSlope    backward: D = dy W_out; the epilogue reads g and u and writes dg and du.
+//   kStore    the remaining products.
+//
+// Operands lie in memory as they are: where the reduction runs along rows (W_in in dx, W_out in
+// dhidden, both operands of a weight gradient) TMA brings boxes of 64 elements of the row by 64
+// reduction rows and the instruction reads them MN-major; nothing is transposed.
+//
+// Work of kStore: whole rounds of tiles, one tile per pair, and then the tiles of the last one to
+// two rounds as one stretch of 64-element steps cut evenly over the pairs, so that all pairs
+// finish together whatever the number of tiles; a tile that a cut divides goes to scratch in
+// binary32 and k_join adds its pieces in order.
+//
+// k_rows: up to 32 rows of x, bound by reading the weights.  A block owns 16 rows of the weights
+// (of each projection), its warps split the reduction, and each lane's 16-byte loads of the
+// weights go straight into the operands of warp-wide matrix instructions: a dot product does not
+// care in which order its terms come, so a lane's eight consecutive elements serve as the
+// fragment positions of two instructions, for the weights and for x alike.
+#include <cstring>
+#include <new>
+
+#include <cuda_fp16.h>
+
+#include "../../include/gated_ffn.h"
+#include "sm100.cuh"
+
+namespace {
+
+constexpr int kBK = 64;                          // reduction elements per stage
+constexpr int kRowsPerBlock = 128;               // rows of A per block; a pair's tile has twice as many
+constexpr int kTileM = 2 * kRowsPerBlock;
+constexpr int kStages = 6;
+constexpr int kABytes = kRowsPerBlock * kBK * 2;
+constexpr int kBBytes = 128 * kBK * 2;           // at most 128 rows of B per block
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kAccCols = 256;
+constexpr int kTmemCols = 2 * kAccCols;
+constexpr int kEpilogueWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kSmemBytes = kStages * kStageBytes + 256 + 1024;
+constexpr int kMinSteps = 4;                     // a piece of a divided tile is at least this long
+
+enum Mode { kStore, kGated, kSlope };
+
+template <typename T>
+struct Type;
+template <>
+struct Type<__nv_bfloat16> {
+    static constexpr uint32_t kFormat = 1;       // operand format field of the instruction descriptor
+    static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16(a, b); }
+    static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
+};
+template <>
+struct Type<__half> {
+    static constexpr uint32_t kFormat = 0;
+    static constexpr CUtensorMapDataType kMap = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    static __device__ __forceinline__ uint32_t pack(float a, float b)
+    {
+        const __half2 v = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+};
+
+// ---- activation: act(v) = v sigmoid(s(v)), s(v) = v (silu) or 2 c (v + k v^3) (gelu, since
+// (1 + tanh w) / 2 = sigmoid(2 w)); act'(v) = sg + v sg (1 - sg) s'(v)
+
+constexpr float kGelu2C = 1.5957691216057308f;   // 2 sqrt(2 / pi)
+constexpr float kGeluK = 0.044715f;
+
+__device__ __forceinline__ float act_sigmoid(float v, int gelu)
+{
+    const float s = gelu ? kGelu2C * fmaf(kGeluK * v * v, v, v) : v;
+    return rcp_approx(1.0f + ex2_approx(-kLog2e * s));
+}
+
+__device__ __forceinline__ float act_slope(float v, float sg, int gelu)
+{
+    const float ds = gelu ? kGelu2C * fmaf(3.0f * kGeluK * v, v, 1.0f) : 1.0f;
+    return fmaf(v * sg * (1.0f - sg), ds, sg);
+}
+
+// ---- the product
+
+struct Product {
+    int64_t m;              // rows of A and D
+    int n;                  // rows of B, columns of D (kGated: hidden units)
+    int64_t k;              // reduction length
+    int a_rows, b_rows;     // 1: the operand is stored [k][rows] (MN-major), 0: [rows][k]
+    int tile_n;             // columns of D per tile: 256, 192 or 128 (kGated: 128 hidden units)
+    int m_tiles, n_tiles;
+    int m_first;            // 1: consecutive tiles run down the rows, 0: along the columns
+    int steps;              // ceil(k / 64)
+    int rounds;             // whole rounds of tiles
+    int cuts;               // pairs that share the rest (0: none)
+    void *out;              // kStore: D; kGated: hidden; kSlope: [dg | du]
+    int64_t out_stride;
+    void *pre;              // kGated: [g | u] or nullptr; kSlope: [g | u], read
+    float *pieces;          // [cuts][2][256][256]
+    int gelu;
+    int *err;
+};
+
+// The stretches of reduction steps a pair works through, in order.  Every role of the block runs its own copy.
+struct Walk {
+    const Product &p;
+    int pair, pairs, tiles;
+    int round = 0;
+    int64_t at, end, begin;      // steps of the shared rest
+    int tile, k0, k1, piece;     // the current stretch; piece: -1 whole tile, else which of the pair's two slots
+
+    __device__ Walk(const Product &q, int pair_, int pairs_) : p(q), pair(pair_), pairs(pairs_), tiles(q.m_tiles * q.n_tiles)
+    {
+        const int64_t rest = static_cast<int64_t>(tiles - p.rounds * pairs) * p.steps;
+        begin = at = pair < p.cuts ? rest * pair / p.cuts : 0;
+        end = pair < p.cuts ? rest * (pair + 1) / p.cuts : 0;
+    }
+    __device__ bool next()
+    {
+        if (round < p.rounds) {
+            tile = round * pairs + pair;
+            ++round;
+            k0 = 0;
+            k1 = p.steps;
+            piece = -1;
+            return tile < tiles;
+        }
+        if (at >= end) return false;
+        const int64_t t = at / p.steps;
+        tile = p.rounds * pairs + static_cast<int>(t);
+        k0 = static_cast<int>(at - t * p.steps);
+        const int64_t left = end - at;
+        k1 = left < p.steps - k0 ? k0 + static_cast<int>(left) : p.steps;
+        piece = k0 == 0 && k1 == p.steps ? -1 : (at == begin ? 0 : 1);
+        at += k1 - k0;
+        return true;
+    }
+    __device__ int row_tile() const { return p.m_first ? tile % p.m_tiles : tile / p.n_tiles; }
+    __device__ int col_tile() const { return p.m_first ? tile / p.m_tiles : tile % p.n_tiles; }
+};
+
+// MN-major operand tile with the 128-byte swizzle: boxes of 64 elements (128 bytes) by 64 reduction
+// rows; the next 64 elements are a box (8192 bytes, leading offset) further, the next 8
+// reduction rows 1024 bytes (stride offset).
+__device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr)
+{
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (512ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// Columns [c, c + 16) of a row of `width` columns (a multiple of 8).
+__device__ __forceinline__ void store16(void *row, int c, int width, const uint32_t (&w)[8])
+{
+    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(row) + c);
+    if (c < width) dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    if (c + 8 < width) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
+__device__ __forceinline__ void load16(const void *row, int c, int width, uint32_t (&w)[8])
+{
+    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
+    const uint4 a = c < width ? __ldg(src) : make_uint4(0, 0, 0, 0);
+    const uint4 b = c + 8 < width ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
+    w[0] = a.x;
+    w[1] = a.y;
+    w[2] = a.z;
+    w[3] = a.w;
+    w[4] = b.x;
+    w[5] = b.y;
+    w[6] = b.z;
+    w[7] = b.w;
+}
+
+template <typename T, int kMode>
+__global__ void __launch_bounds__(kThreads, 1)
+k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
+          const __grid_constant__ Product p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t tiles = (raw + 1023u) & ~1023u;
+    const uint32_t bars = tiles + kStages * kStageBytes;
+    uint8_t *bars_ptr = smem_raw + (bars - raw);
+    const uint32_t full0 = bars, empty0 = bars + 8 * kStages;
+    const uint32_t acc_full0 = bars + 16 * kStages, acc_empty0 = acc_full0 + 16;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars_ptr + 16 * kStages + 32);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(bars_ptr + 16 * kStages + 40);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_cta_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int tile_n = kMode == kGated ? 256 : p.tile_n;     // accumulator columns
+    const int b_half = tile_n / 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full0 + 8 * s, 1);
+            mbar_init(empty0 + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full0 + 8 * b, 1);
+            mbar_init(acc_empty0 + 8 * b, 2 * kEpilogueWarps);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
+    tc_fence_before_sync();
+    cluster_sync_all();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t s = 0, ph = 0;
+            bool ok = true;
+            const int b_boxes = (b_half + 63) / 64;
+            const uint32_t bytes = kABytes + (p.b_rows ? b_boxes * 64 * kBK * 2 : b_half * kBK * 2);
+            Walk w(p, pair, pairs);
+            while (ok && w.next()) {
+                const int a0 = w.row_tile() * kTileM + static_cast<int>(rank) * kRowsPerBlock;
+                const int b0 = kMode == kGated ? w.col_tile() * 128 + static_cast<int>(rank) * p.n
+                                               : w.col_tile() * tile_n + static_cast<int>(rank) * b_half;
+                for (int kc = w.k0; kc < w.k1; ++kc) {
+                    if (!mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t dst = tiles + s * kStageBytes;
+                    const uint32_t full = map_to_rank(full0 + 8 * s, 0);
+                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * bytes);
+                    if (p.a_rows) {
+                        tma_load_2d(dst, &tm_a, a0, kc * kBK, full);
+                        tma_load_2d(dst + kABytes / 2, &tm_a, a0 + 64, kc * kBK, full);
+                    } else {
+                        tma_load_2d(dst, &tm_a, kc * kBK, a0, full);
+                    }
+                    if (p.b_rows) {
+                        for (int i = 0; i < b_boxes; ++i)
+                            tma_load_2d(dst + kABytes + i * 64 * kBK * 2, &tm_b, b0 + 64 * i, kc * kBK, full);
+                    } else {
+                        tma_load_2d(dst + kABytes, &tm_b, kc * kBK, b0, full);
+                    }
+                    if (++s == kStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+            }
+            // do not leave while the leader's instructions may still read this block's stages
+            for (int i = 0; i < kStages && ok; ++i) {
+                ok = mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag);
+                if (++s == kStages) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = (1u << 4) | (Type<T>::kFormat << 7) | (Type<T>::kFormat << 10) |
+                                   (static_cast<uint32_t>(p.a_rows) << 15) | (static_cast<uint32_t>(p.b_rows) << 16) |
+                                   (static_cast<uint32_t>(tile_n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
+            // 16 reduction elements: 32 bytes along a K-major row, 16 rows of 128 bytes MN-major
+            const uint32_t a_step = p.a_rows ? 2048 >> 4 : 32 >> 4, b_step = p.b_rows ? 2048 >> 4 : 32 >> 4;
+            uint32_t s = 0, ph = 0;
+            bool ok = true;
+            int it = 0;
+            for (Walk w(p, pair, pairs); ok && w.next(); ++it) {
+                const uint32_t buf = it & 1, use = (it >> 1) & 1;
+                if (!mbar_wait(acc_empty0 + 8 * buf, use ^ 1u, abort_flag)) break;
+                tc_fence_after_sync();
+                const uint32_t d = tmem_base + buf * kAccCols;
+                for (int kc = w.k0; kc < w.k1; ++kc) {
+                    if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                    const uint32_t addr = tiles + s * kStageBytes;
+                    const uint64_t ad = p.a_rows ? smem_desc_rows(addr) : smem_desc(addr);
+                    const uint64_t bd = p.b_rows ? smem_desc_rows(addr + kABytes) : smem_desc(addr + kABytes);
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)
+                        umma_bf16(d, ad + a_step * k, bd + b_step * k, idesc, kc > w.k0 || k > 0);
+                    umma_commit_pair(empty0 + 8 * s);
+                    if (++s == kStages) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                if (ok) umma_commit_pair(acc_full0 + 8 * buf);
+            }
+        }
+    } else {
+        const int q = warp & 3;
+        const int half = (warp - 2) >> 2;                // which half of the columns
+        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+        int it = 0;
+        for (Walk w(p, pair, pairs); w.next(); ++it) {
+            const uint32_t buf = it & 1, use = (it >> 1) & 1;
+            const bool ready = mbar_wait(acc_full0 + 8 * buf, use, abort_flag);
+            if (!__all_sync(0xFFFFFFFFu, ready)) break;
+            tc_fence_after_sync();
+            const int row_in_block = q * 32 + lane;
+            const int64_t row = static_cast<int64_t>(w.row_tile()) * kTileM + static_cast<int>(rank) * kRowsPerBlock + row_in_block;
+            const bool live = row < p.m;
+            const uint32_t t0 = lane_base + buf * kAccCols;
+            if (kMode == kGated) {
+                const int f0 = w.col_tile() * 128;
+                uint16_t *hrow = static_cast<uint16_t *>(p.out) + (live ? row : 0) * p.out_stride;
+                uint16_t *prow = static_cast<uint16_t *>(p.pre) + (live ? row : 0) * 2 * p.n;
+#pragma unroll 1
+                for (int c = half * 64; c < half * 64 + 64; c += 16) {
+                    uint32_t g[16], u[16];
+                    tmem_ld16(t0 + c, g);
+                    tmem_ld16(t0 + 128 + c, u);
+                    tmem_wait_ld();
+                    uint32_t hw[8], gw[8], uw[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float g0 = __uint_as_float(g[2 * i]), g1 = __uint_as_float(g[2 * i + 1]);
+                        const float u0 = __uint_as_float(u[2 * i]), u1 = __uint_as_float(u[2 * i + 1]);
+                        hw[i] = Type<T>::pack(g0 * act_sigmoid(g0, p.gelu) * u0, g1 * act_sigmoid(g1, p.gelu) * u1);
+                        gw[i] = Type<T>::pack(g0, g1);
+                        uw[i] = Type<T>::pack(u0, u1);
+                    }
+                    if (live) {
+                        store16(hrow, f0 + c, p.n, hw);
+                        if (p.pre != nullptr) {
+                            store16(prow, f0 + c, p.n, gw);
+                            store16(prow + p.n, f0 + c, p.n, uw);
+                        }
+                    }
+                }
+            } else if (kMode == kSlope) {
+                const int f0 = w.col_tile() * tile_n;
+                const uint16_t *prow = static_cast<const uint16_t *>(p.pre) + (live ? row : 0) * 2 * p.n;
+                uint16_t *orow = static_cast<uint16_t *>(p.out) + (live ? row : 0) * p.out_stride;
+#pragma unroll 1
+                for (int c = half * (tile_n / 2); c < (half + 1) * (tile_n / 2); c += 16) {
+                    uint32_t d[16], gw[8], uw[8];
+                    tmem_ld16(t0 + c, d);
+                    load16(prow, live ? f0 + c : p.n, p.n, gw);
+                    load16(prow + p.n, live ? f0 + c : p.n, p.n, uw);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 g = Type<T>::unpack(gw[i]), u = Type<T>::unpack(uw[i]);
+                        const float d0 = __uint_as_float(d[2 * i]), d1 = __uint_as_float(d[2 * i + 1]);
+                        const float s0 = act_sigmoid(g.x, p.gelu), s1 = act_sigmoid(g.y, p.gelu);
+                        gw[i] = Type<T>::pack(d0 * u.x * act_slope(g.x, s0, p.gelu), d1 * u.y * act_slope(g.y, s1, p.gelu));
+                        uw[i] = Type<T>::pack(d0 * g.x * s0, d1 * g.y * s1);
+                    }
+                    if (live) {
+                        store16(orow, f0 + c, p.n, gw);
+                        store16(orow + p.n, f0 + c, p.n, uw);
+                    }
+                }
+            } else if (w.piece >= 0) {
+                float *dst = p.pieces + ((static_cast<int64_t>(pair) * 2 + w.piece) * kTileM + rank * kRowsPerBlock + row_in_block) * kAccCols;
+#pragma unroll 1
+                for (int c = half * (tile_n / 2); c < (half + 1) * (tile_n / 2); c += 16) {
+                    uint32_t d[16];
+                    tmem_ld16(t0 + c, d);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        reinterpret_cast<uint4 *>(dst + c)[i] = make_uint4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]);
+                }
+            } else {
+                const int c0 = w.col_tile() * tile_n;
+                uint16_t *orow = static_cast<uint16_t *>(p.out) + (live ? row : 0) * p.out_stride;
+#pragma unroll 1
+                for (int c = half * (tile_n / 2); c < (half + 1) * (tile_n / 2); c += 16) {
+                    uint32_t d[16], o[8];
+                    tmem_ld16(t0 + c, d);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        o[i] = Type<T>::pack(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]));
+                    if (live) store16(orow, c0 + c, p.n, o);
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_rank(acc_empty0 + 8 * buf, 0));
+        }
+    }
+
+    tc_fence_before_sync();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicExch(p.err, 1);
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < kDrainNs) __nanosleep(1000);
+    }
+    cluster_sync_all();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after_sync();
+        tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+// Adds the pieces of the tiles that were divided: 4 rows of a tile per block, 64 threads per row.
+template <typename T>
+__global__ void __launch_bounds__(256)
+k_join(const Product p, const int pairs)
+{
+    const int index = blockIdx.y;                        // tile of the shared rest
+    const int tile = p.rounds * pairs + index;
+    const int64_t rest = static_cast<int64_t>(p.m_tiles * p.n_tiles - p.rounds * pairs) * p.steps;
+    const int64_t lo = static_cast<int64_t>(index) * p.steps, hi = lo + p.steps;
+    // the pairs whose stretch meets [lo, hi): pair i has [rest i / cuts, rest (i + 1) / cuts)
+    int first = static_cast<int>(lo * p.cuts / rest);
+    while (rest * (first + 1) / p.cuts <= lo) ++first;
+    while (first > 0 && rest * first / p.cuts > lo) --first;
+    if (rest * first / p.cuts <= lo && rest * (first + 1) / p.cuts >= hi) return;   // one pair did all of it
+    const int row_in_tile = blockIdx.x * 4 + threadIdx.x / 64;
+    const int c = 4 * (threadIdx.x % 64);
+    const int64_t row = static_cast<int64_t>(p.m_first ? tile % p.m_tiles : tile / p.n_tiles) * kTileM + row_in_tile;
+    const int col = (p.m_first ? tile / p.m_tiles : tile % p.n_tiles) * p.tile_n + c;
+    if (row >= p.m || c >= p.tile_n || col >= p.n) return;
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = first; i < p.cuts && rest * i / p.cuts < hi; ++i) {
+        // the slot of its first stretch if that lies in this tile, else of its last
+        const int slot = rest * i / p.cuts / p.steps == index ? 0 : 1;
+        const float4 v = *reinterpret_cast<const float4 *>(
+            p.pieces + ((static_cast<int64_t>(i) * 2 + slot) * kTileM + row_in_tile) * kAccCols + c);
+        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+    uint32_t out[2] = {Type<T>::pack(sum.x, sum.y), Type<T>::pack(sum.z, sum.w)};
+    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * p.out_stride + col) = make_uint2(out[0], out[1]);
+}
+
+// ---- few rows
+
+constexpr int kRowsThreads = 256;
+constexpr int kRowsWarps = kRowsThreads / 32;
+constexpr int kRowsMax = 32;                     // rows of x
+
+template <typename T>
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                            uint32_t b0, uint32_t b1)
+{
+    if constexpr (Type<T>::kFormat == 1)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+            "{%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+            "{%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+struct Rows {
+    const void *x;
+    int64_t x_stride;
+    const void *w;              // kGated: [2 * width][k]; else [width][k]
+    void *out, *pre;
+    int64_t out_stride;
+    int n, width, k;            // rows of x, rows of w (one projection), reduction length
+    int gelu;
+};
+
+// NT: groups of 8 rows of x.
+template <typename T, bool kGatedRows, int NT>
+__global__ void __launch_bounds__(kRowsThreads)
+k_rows(const Rows p)
+{
+    constexpr int P = kGatedRows ? 2 : 1;
+    constexpr int kDepth = NT <= 2 ? 4 : 2;      // chunks of 32 reduction elements in flight
+    __shared__ float s_sum[kRowsWarps][P][16][NT * 8 + 1];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int g = lane >> 2, t = lane & 3;
+    const int f0 = blockIdx.x * 16;
+    const uint16_t *w = static_cast<const uint16_t *>(p.w);
+    const uint16_t *x = static_cast<const uint16_t *>(p.x);
+    float acc[P][NT][4];
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+    const int chunks = (p.k + 31) / 32;
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    for (int c0 = warp; c0 < chunks; c0 += kRowsWarps * kDepth) {
+        uint4 wv[kDepth][P][2], xv[kDepth][NT];
+#pragma unroll
+        for (int s = 0; s < kDepth; ++s) {
+            const int k = (c0 + s * kRowsWarps) * 32 + 8 * t;
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int f = f0 + g + 8 * h;
+                    wv[s][i][h] = k < p.k && f < p.width
+                                      ? __ldg(reinterpret_cast<const uint4 *>(w + (static_cast<int64_t>(i) * p.width + f) * p.k + k))
+                                      : none;
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int r = 8 * j + g;
+                xv[s][j] = k < p.k && r < p.n ? __ldg(reinterpret_cast<const uint4 *>(x + r * p.x_stride + k)) : none;
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < kDepth; ++s)
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    mma_16x8x16<T>(acc[i][j], wv[s][i][0].x, wv[s][i][1].x, wv[s][i][0].y, wv[s][i][1].y, xv[s][j].x, xv[s][j].y);
+                    mma_16x8x16<T>(acc[i][j], wv[s][i][0].z, wv[s][i][1].z, wv[s][i][0].w, wv[s][i][1].w, xv[s][j].z, xv[s][j].w);
+                }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_sum[warp][i][g + 8 * (e >> 1)][8 * j + 2 * t + (e & 1)] = acc[i][j][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * NT * 8; i += kRowsThreads) {
+        const int f = i % 16, r = i / 16;
+        if (r >= p.n || f0 + f >= p.width) continue;
+        float v[P];
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            v[e] = 0.0f;
+            for (int k = 0; k < kRowsWarps; ++k) v[e] += s_sum[k][e][f][r];
+        }
+        T *out = static_cast<T *>(p.out) + r * p.out_stride + f0 + f;
+        if constexpr (kGatedRows) {
+            *out = static_cast<T>(v[0] * act_sigmoid(v[0], p.gelu) * v[1]);
+            if (p.pre != nullptr) {
+                T *pre = static_cast<T *>(p.pre) + static_cast<int64_t>(r) * 2 * p.width + f0 + f;
+                pre[0] = static_cast<T>(v[0]);
+                pre[p.width] = static_cast<T>(v[1]);
+            }
+        } else {
+            *out = static_cast<T>(v[0]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+// An operand in the type T: rows x cols (cols contiguous), boxes of 64 columns by box_rows rows.
+bool encode(CUtensorMapDataType type, CUtensorMap *m, const void *base, int64_t rows, int64_t cols, int64_t stride,
+            uint32_t box_rows)
+{
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride) * 2};
+    const cuuint32_t box[2] = {kBK, box_rows};
+    const cuuint32_t elem_strides[2] = {1, 1};
+    return tensor_map_encoder()(m, type, 2, const_cast<void *>(base), dims, strides, box, elem_strides,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+struct gated_ffn {
+    int model = 0, hidden = 0, activation = 0, type = 0;
+    int device = 0, sms = 0, pairs = 0;
+    cudaStream_t stream = nullptr;
+    int64_t launches = 0;
+    int *err = nullptr;
+};
+
+namespace {
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Operand {
+    const void *ptr;
+    int64_t stride;   // elements between stored rows
+    int by_rows;      // 1: stored [k][rows]
+};
+
+// Sizes and the cut of D[m][n] = A B^T.
+Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
+{
+    Product q = {};
+    q.m = m;
+    q.n = n;
+    q.k = k;
+    // the narrowest total width wins, the widest tile among equals
+    q.tile_n = 256;
+    if (mode == kGated) {
+        q.tile_n = 128;
+    } else {
+        const int widths[2] = {192, 128};
+        for (int w : widths)
+            if (div_up(n, w) * w < div_up(n, q.tile_n) * q.tile_n) q.tile_n = w;
+    }
+    q.m_tiles = static_cast<int>(div_up(m, kTileM));
+    q.n_tiles = static_cast<int>(div_up(n, q.tile_n));
+    // Neighbouring tiles, worked on at the same time, share the operand of the longer side; the
+    // shorter side's operand is the smaller one and stays in L2.
+    q.m_first = q.m_tiles <= q.n_tiles;
+    q.steps = static_cast<int>(div_up(k, kBK));
+    const int64_t tiles = static_cast<int64_t>(q.m_tiles) * q.n_tiles;
+    if (mode != kStore) {
+        q.rounds = static_cast<int>(div_up(tiles, p->pairs));
+    } else {
+        q.rounds = static_cast<int>(tiles / p->pairs);
+        if (tiles % p->pairs != 0) {
+            if (q.rounds > 0) --q.rounds;
+            const int64_t rest = tiles - static_cast<int64_t>(q.rounds) * p->pairs;
+            int64_t cuts = rest * q.steps / kMinSteps;
+            if (cuts < rest) cuts = rest;
+            q.cuts = static_cast<int>(cuts < p->pairs ? cuts : p->pairs);
+        }
+    }
+    q.gelu = p->activation == GATED_FFN_GELU;
+    q.err = p->err;
+    return q;
+}
+
+size_t pieces_bytes(const Product &q) { return static_cast<size_t>(q.cuts) * 2 * kTileM * kAccCols * sizeof(float); }
+
+template <typename T, int kMode>
+int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b)
+{
+    CUtensorMap tm_a, tm_b;
+    const CUtensorMapDataType type = Type<T>::kMap;
+    const int64_t b_total = kMode == kGated ? 2 * static_cast<int64_t>(q.n) : q.n;
+    const uint32_t b_box = kMode == kGated ? 128 : q.tile_n / 2;
+    q.a_rows = a.by_rows;
+    q.b_rows = b.by_rows;
+    const bool ok = (a.by_rows ? encode(type, &tm_a, a.ptr, q.k, q.m, a.stride, kBK)
+                               : encode(type, &tm_a, a.ptr, q.m, q.k, a.stride, kRowsPerBlock)) &&
+                    (b.by_rows ? encode(type, &tm_b, b.ptr, q.k, b_total, b.stride, kBK)
+                               : encode(type, &tm_b, b.ptr, b_total, q.k, b.stride, b_box));
+    if (!ok) return GATED_FFN_ECUDA;
+    const int64_t tiles = static_cast<int64_t>(q.m_tiles) * q.n_tiles;
+    // a full grid, unless there is less than one round (then the walk's rounds count that grid's pairs)
+    int pairs = p->pairs;
+    if (q.rounds == 0) pairs = q.cuts;
+    else if (q.cuts == 0 && tiles < pairs) pairs = static_cast<int>(tiles);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.stream = p->stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, k_product<T, kMode>, tm_a, tm_b, q) != cudaSuccess) {
+        cudaGetLastError();
+        return GATED_FFN_ECUDA;
+    }
+    p->launches += 1;
+    if (q.cuts > 1) {
+        const dim3 grid(kTileM / 4, static_cast<unsigned>(tiles - static_cast<int64_t>(q.rounds) * pairs));
+        k_join<T><<<grid, 256, 0, p->stream>>>(q, pairs);
+        if (cudaGetLastError() != cudaSuccess) return GATED_FFN_ECUDA;
+        p->launches += 1;
+    }
+    return GATED_FFN_OK;
+}
+
+template <typename T, bool kGatedRows>
+int launch_rows(gated_ffn *p, const Rows &r)
+{
+    const unsigned blocks = static_cast<unsigned>(div_up(r.width, 16));
+    if (r.n <= 8)
+        k_rows<T, kGatedRows, 1><<<blocks, kRowsThreads, 0, p->stream>>>(r);
+    else if (r.n <= 16)
+        k_rows<T, kGatedRows, 2><<<blocks, kRowsThreads, 0, p->stream>>>(r);
+    else
+        k_rows<T, kGatedRows, 4><<<blocks, kRowsThreads, 0, p->stream>>>(r);
+    if (cudaGetLastError() != cudaSuccess) return GATED_FFN_ECUDA;
+    p->launches += 1;
+    return GATED_FFN_OK;
+}
+
+template <typename T>
+int run_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *pre,
+                void *hidden, void *y, int64_t y_stride, float *scratch, int64_t n)
+{
+    if (n <= kRowsMax) {
+        Rows r = {x, x_stride, w_in, hidden, pre, p->hidden, static_cast<int>(n), p->hidden, p->model,
+                  p->activation == GATED_FFN_GELU};
+        const int rc = launch_rows<T, true>(p, r);
+        if (rc != GATED_FFN_OK) return rc;
+        Rows s = {hidden, p->hidden, w_out, y, nullptr, y_stride, static_cast<int>(n), p->model, p->hidden, 0};
+        return launch_rows<T, false>(p, s);
+    }
+    Product q = plan(p, kGated, n, p->hidden, p->model);
+    q.out = hidden;
+    q.out_stride = p->hidden;
+    q.pre = pre;
+    const int rc = launch_product<T, kGated>(p, q, {x, x_stride, 0}, {w_in, p->model, 0});
+    if (rc != GATED_FFN_OK) return rc;
+    Product r = plan(p, kStore, n, p->model, p->hidden);
+    r.out = y;
+    r.out_stride = y_stride;
+    r.pieces = scratch;
+    return launch_product<T, kStore>(p, r, {hidden, p->hidden, 0}, {w_out, p->hidden, 0});
+}
+
+struct BackwardPlan {
+    Product slope, dx, dw_in, dw_out;
+    size_t dpre, pieces, total;
+};
+
+BackwardPlan plan_backward(const gated_ffn *p, int64_t n)
+{
+    BackwardPlan b;
+    b.slope = plan(p, kSlope, n, p->hidden, p->model);
+    b.dx = plan(p, kStore, n, p->model, 2 * static_cast<int64_t>(p->hidden));
+    b.dw_in = plan(p, kStore, 2 * static_cast<int64_t>(p->hidden), p->model, n);
+    b.dw_out = plan(p, kStore, p->model, p->hidden, n);
+    b.dpre = 0;
+    b.pieces = (static_cast<size_t>(n) * 2 * p->hidden * 2 + 255) & ~static_cast<size_t>(255);
+    // the products follow one another on the stream: one set of pieces serves all
+    size_t most = pieces_bytes(b.dx);
+    if (pieces_bytes(b.dw_in) > most) most = pieces_bytes(b.dw_in);
+    if (pieces_bytes(b.dw_out) > most) most = pieces_bytes(b.dw_out);
+    b.total = b.pieces + most;
+    return b;
+}
+
+template <typename T>
+int run_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride, const void *w_in,
+                 const void *w_out, const void *pre, const void *hidden, void *dx, int64_t dx_stride, void *dw_in,
+                 void *dw_out, uint8_t *scratch, int64_t n)
+{
+    BackwardPlan b = plan_backward(p, n);
+    void *dpre = scratch + b.dpre;
+    float *pieces = reinterpret_cast<float *>(scratch + b.pieces);
+    const int64_t f = p->hidden, d = p->model;
+    b.slope.out = dpre;
+    b.slope.out_stride = 2 * f;
+    b.slope.pre = const_cast<void *>(pre);
+    int rc = launch_product<T, kSlope>(p, b.slope, {dy, dy_stride, 0}, {w_out, f, 1});
+    if (rc != GATED_FFN_OK) return rc;
+    b.dx.pieces = b.dw_in.pieces = b.dw_out.pieces = pieces;
+    if (dx != nullptr) {
+        b.dx.out = dx;
+        b.dx.out_stride = dx_stride;
+        rc = launch_product<T, kStore>(p, b.dx, {dpre, 2 * f, 0}, {w_in, d, 1});
+        if (rc != GATED_FFN_OK) return rc;
+    }
+    b.dw_in.out = dw_in;
+    b.dw_in.out_stride = d;
+    rc = launch_product<T, kStore>(p, b.dw_in, {dpre, 2 * f, 1}, {x, x_stride, 1});
+    if (rc != GATED_FFN_OK) return rc;
+    b.dw_out.out = dw_out;
+    b.dw_out.out_stride = f;
+    return launch_product<T, kStore>(p, b.dw_out, {dy, dy_stride, 1}, {hidden, f, 1});
+}
+
+bool aligned16(const void *v) { return reinterpret_cast<uintptr_t>(v) % 16 == 0; }
+
+bool rows_ok(const gated_ffn *p, int64_t n)
+{
+    // rows and tile counts are 32-bit in the kernels
+    return n >= 1 && n <= 0x7FFFFF00 &&
+           div_up(n, kTileM) * div_up(2 * static_cast<int64_t>(p->hidden > p->model ? p->hidden : p->model), 128) < 0x7FFFFFFF;
+}
+
+bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride % 8 == 0; }
+
+template <typename T>
+bool prepare_kernels(int *pairs, int sms)
+{
+    const void *kernels[3] = {reinterpret_cast<const void *>(k_product<T, kStore>),
+                              reinterpret_cast<const void *>(k_product<T, kGated>),
+                              reinterpret_cast<const void *>(k_product<T, kSlope>)};
+    for (const void *k : kernels)
+        if (!raise_dynamic_smem(k, kSmemBytes)) return false;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(sms & ~1));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, k_product<T, kStore>, &cfg) != cudaSuccess || clusters < 1) return false;
+    *pairs = clusters < sms / 2 ? clusters : sms / 2;
+    return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gated_ffn_create(gated_ffn **out, int model, int hidden, int activation, int type)
+{
+    if (out == nullptr) return GATED_FFN_ENULL;
+    *out = nullptr;
+    if (model < 8 || model > GATED_FFN_MAX_WIDTH || model % 8 != 0) return GATED_FFN_EINVAL;
+    if (hidden < 8 || hidden > GATED_FFN_MAX_WIDTH || hidden % 8 != 0) return GATED_FFN_EINVAL;
+    if (activation != GATED_FFN_SILU && activation != GATED_FFN_GELU) return GATED_FFN_EINVAL;
+    if (type != GATED_FFN_BF16 && type != GATED_FFN_F16) return GATED_FFN_EINVAL;
+    if (tensor_map_encoder() == nullptr) return GATED_FFN_ECUDA;
+    gated_ffn *p = new (std::nothrow) gated_ffn;
+    if (p == nullptr) return GATED_FFN_ENOMEM;
+    p->model = model;
+    p->hidden = hidden;
+    p->activation = activation;
+    p->type = type;
+    bool ok = cudaGetDevice(&p->device) == cudaSuccess &&
+              cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) == cudaSuccess;
+    ok = ok && (type == GATED_FFN_BF16 ? prepare_kernels<__nv_bfloat16>(&p->pairs, p->sms)
+                                       : prepare_kernels<__half>(&p->pairs, p->sms));
+    if (!ok) {
+        cudaGetLastError();
+        delete p;
+        return GATED_FFN_ECUDA;
+    }
+    if (cudaMalloc(reinterpret_cast<void **>(&p->err), sizeof(int)) != cudaSuccess) {
+        cudaGetLastError();
+        delete p;
+        return GATED_FFN_ENOMEM;
+    }
+    if (cudaMemset(p->err, 0, sizeof(int)) != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(p->err);
+        delete p;
+        return GATED_FFN_ECUDA;
+    }
+    *out = p;
+    return GATED_FFN_OK;
+}
+
+int gated_ffn_destroy(gated_ffn *p)
+{
+    if (p == nullptr) return GATED_FFN_ENULL;
+    cudaStreamSynchronize(p->stream);
+    cudaFree(p->err);
+    delete p;
+    return GATED_FFN_OK;
+}
+
+int gated_ffn_set_stream(gated_ffn *p, void *cuda_stream)
+{
+    if (p == nullptr) return GATED_FFN_ENULL;
+    p->stream = static_cast<cudaStream_t>(cuda_stream);
+    return GATED_FFN_OK;
+}
+
+size_t gated_ffn_workspace_bytes(const gated_ffn *p, int64_t n, int backward)
+{
+    if (p == nullptr || !rows_ok(p, n)) return 0;
+    if (backward) return plan_backward(p, n).total;
+    return n <= kRowsMax ? 0 : pieces_bytes(plan(p, kStore, n, p->model, p->hidden));
+}
+
+int gated_ffn_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *pre,
+                      void *hidden, void *y, int64_t y_stride, void *workspace, size_t workspace_bytes, int64_t n)
+{
+    if (p == nullptr) return GATED_FFN_ENULL;
+    if (!rows_ok(p, n)) return GATED_FFN_EINVAL;      // first: an empty batch comes without pointers
+    if (x == nullptr || w_in == nullptr || w_out == nullptr || hidden == nullptr || y == nullptr) return GATED_FFN_ENULL;
+    if (!stride_ok(x_stride, p->model) || !stride_ok(y_stride, p->model)) return GATED_FFN_EINVAL;
+    for (const void *v : {x, w_in, w_out, static_cast<const void *>(pre), static_cast<const void *>(hidden),
+                          static_cast<const void *>(y), static_cast<const void *>(workspace)})
+        if (!aligned16(v)) return GATED_FFN_EALIGN;
+    const size_t need = gated_ffn_workspace_bytes(p, n, 0);
+    if (need > 0 && workspace == nullptr) return GATED_FFN_ENULL;
+    if (need > workspace_bytes) return GATED_FFN_ENOMEM;
+    float *scratch = static_cast<float *>(workspace);
+    return p->type == GATED_FFN_BF16
+               ? run_forward<__nv_bfloat16>(p, x, x_stride, w_in, w_out, pre, hidden, y, y_stride, scratch, n)
+               : run_forward<__half>(p, x, x_stride, w_in, w_out, pre, hidden, y, y_stride, scratch, n);
+}
+
+int gated_ffn_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                       const void *w_in, const void *w_out, const void *pre, const void *hidden, void *dx,
+                       int64_t dx_stride, void *dw_in, void *dw_out, void *workspace, size_t workspace_bytes,
+                       int64_t n)
+{
+    if (p == nullptr) return GATED_FFN_ENULL;
+    if (!rows_ok(p, n)) return GATED_FFN_EINVAL;
+    if (dy == nullptr || x == nullptr || w_in == nullptr || w_out == nullptr || pre == nullptr || hidden == nullptr ||
+        dw_in == nullptr || dw_out == nullptr || workspace == nullptr)
+        return GATED_FFN_ENULL;
+    if (!stride_ok(dy_stride, p->model) || !stride_ok(x_stride, p->model) ||
+        (dx != nullptr && !stride_ok(dx_stride, p->model)))
+        return GATED_FFN_EINVAL;
+    for (const void *v : {dy, x, w_in, w_out, pre, hidden, static_cast<const void *>(dx),
+                          static_cast<const void *>(dw_in), static_cast<const void *>(dw_out),
+                          static_cast<const void *>(workspace)})
+        if (!aligned16(v)) return GATED_FFN_EALIGN;
+    if (gated_ffn_workspace_bytes(p, n, 1) > workspace_bytes) return GATED_FFN_ENOMEM;
+    uint8_t *scratch = static_cast<uint8_t *>(workspace);
+    return p->type == GATED_FFN_BF16 ? run_backward<__nv_bfloat16>(p, dy, dy_stride, x, x_stride, w_in, w_out, pre,
+                                                                   hidden, dx, dx_stride, dw_in, dw_out, scratch, n)
+                                     : run_backward<__half>(p, dy, dy_stride, x, x_stride, w_in, w_out, pre, hidden,
+                                                            dx, dx_stride, dw_in, dw_out, scratch, n);
+}
+
+int gated_ffn_status(gated_ffn *p)
+{
+    if (p == nullptr) return GATED_FFN_ENULL;
+    if (cudaStreamSynchronize(p->stream) != cudaSuccess) return GATED_FFN_ECUDA;
+    int flag = 0;
+    if (cudaMemcpy(&flag, p->err, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return GATED_FFN_ECUDA;
+    if (flag != 0) {
+        cudaMemset(p->err, 0, sizeof(int));
+        return GATED_FFN_ETIMEOUT;
+    }
+    return GATED_FFN_OK;
+}
+
+int64_t gated_ffn_launch_count(const gated_ffn *p) { return p ? p->launches : 0; }
+
+const char *gated_ffn_strerror(int code)
+{
+    switch (code) {
+    case GATED_FFN_OK: return "ok";
+    case GATED_FFN_EINVAL: return "invalid size, stride, type or activation";
+    case GATED_FFN_ENULL: return "required pointer is NULL";
+    case GATED_FFN_EALIGN: return "pointer not 16-byte aligned";
+    case GATED_FFN_ECUDA: return "CUDA call or launch failed";
+    case GATED_FFN_ENOMEM: return "allocation failed, or the workspace is too small";
+    case GATED_FFN_ETIMEOUT: return "a kernel gave up a bounded wait; its output is invalid";
+    default: return "unknown error";
+    }
+}
+
+}  // extern "C"

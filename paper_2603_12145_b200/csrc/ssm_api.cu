@@ -370,9 +370,10 @@ int ssm_conv_backward(ssm *p, const ssm_conv_args *a) { return conv(p, a, true);
 int ssm_conv_step(ssm *p, const void *x, int64_t x_stride, const uint8_t *done, int64_t done_stride, const float *w,
                   const float *bias, const void *history, void *history_out, void *y, int64_t y_stride, int64_t n)
 {
-    if (p == nullptr || x == nullptr || w == nullptr || history == nullptr || history_out == nullptr || y == nullptr)
-        return SSM_ENULL;
-    if (n < 1 || n > kMaxBlocks * 128 / p->channels || x_stride < 0 || done_stride < 0) return SSM_EINVAL;
+    if (p == nullptr) return SSM_ENULL;
+    if (n < 1) return SSM_EINVAL;                     // first: an empty batch comes without pointers
+    if (x == nullptr || w == nullptr || history == nullptr || history_out == nullptr || y == nullptr) return SSM_ENULL;
+    if (n > kMaxBlocks * 128 / p->channels || x_stride < 0 || done_stride < 0) return SSM_EINVAL;
     if (n > 1 && y_stride < p->channels) return SSM_EINVAL;
     const size_t e = element_bytes(p);
     if (!aligned(x, e) || !aligned(y, e) || !aligned(history, e) || !aligned(history_out, e) || !aligned(w, 4) ||
@@ -424,10 +425,12 @@ int ssm_scan_step(ssm *p, const void *x, int64_t x_stride, const void *dt, int64
                   const uint8_t *done, int64_t done_stride, const float *a, const float *d, const float *dt_bias,
                   const float *state, float *state_out, void *y, int64_t y_stride, int64_t n)
 {
-    if (p == nullptr || x == nullptr || dt == nullptr || b == nullptr || c == nullptr || a == nullptr ||
-        state == nullptr || state_out == nullptr || y == nullptr)
+    if (p == nullptr) return SSM_ENULL;
+    if (n < 1) return SSM_EINVAL;
+    if (x == nullptr || dt == nullptr || b == nullptr || c == nullptr || a == nullptr || state == nullptr ||
+        state_out == nullptr || y == nullptr)
         return SSM_ENULL;
-    if (n < 1 || n > kMaxBlocks || x_stride < 0 || dt_stride < 0 || z_stride < 0 || b_stride < 0 || c_stride < 0 ||
+    if (n > kMaxBlocks || x_stride < 0 || dt_stride < 0 || z_stride < 0 || b_stride < 0 || c_stride < 0 ||
         done_stride < 0 || (n > 1 && y_stride < p->channels))
         return SSM_EINVAL;
     const size_t e = element_bytes(p);

@@ -119,3 +119,21 @@ def test_ssm_library_exports_every_declared_symbol():
     assert L.ssm_destroy(None) == -2 and L.ssm_set_stream(None, None) == -2
     assert L.ssm_scan_forward(None, None) == -2 and L.ssm_conv_backward(None, None) == -2
     assert L.ssm_scan_saved_bytes(None, 1, 1) == 0
+
+
+def test_gated_ffn_library_exports_every_declared_symbol():
+    from paper_2603_12145_b200 import gated_ffn
+    lib = ctypes.CDLL(build.build_one("libgated_ffn_b200.so"))
+    names = declared_symbols("gated_ffn.h", "gated_ffn")
+    assert len(names) >= 9
+    for name in names:
+        assert hasattr(lib, name), name
+    assert set(names) == set(gated_ffn.EXPORTS)
+    L = gated_ffn.load(build_if_missing=True)
+    assert gated_ffn.strerror(0) == "ok" and gated_ffn.strerror(-99) == "unknown error"
+    h = ctypes.c_void_p()
+    assert L.gated_ffn_create(None, 64, 64, 0, 0) == -2
+    for bad in ((60, 64, 0, 0), (64, 0, 0, 0), (64, 65544, 0, 0), (64, 64, 2, 0), (64, 64, 0, 2)):
+        assert L.gated_ffn_create(ctypes.byref(h), *bad) == -1
+    assert L.gated_ffn_destroy(None) == -2 and L.gated_ffn_status(None) == -2
+    assert L.gated_ffn_workspace_bytes(None, 1, 1) == 0
