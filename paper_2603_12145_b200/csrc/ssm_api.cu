@@ -45,13 +45,13 @@ bool sizes_ok(int64_t batch, int64_t time)
 void cut_time(ScanShape &s, int64_t blocks_per_segment, int64_t fill)
 {
     s.segments = 1;
-    s.segment_steps = s.chunks * s.chunk;
+    s.segment_steps = s.chunks * kScanChunk;
     if (2 * blocks_per_segment > fill || s.chunks < 2) return;
     const int64_t wanted = div_up(2 * fill, blocks_per_segment);
     const int64_t segments = wanted < s.chunks ? wanted : s.chunks;
     const int per = static_cast<int>(div_up(s.chunks, segments));
     s.segments = static_cast<int>(div_up(s.chunks, per));
-    s.segment_steps = per * s.chunk;
+    s.segment_steps = per * kScanChunk;
 }
 
 ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
@@ -64,8 +64,7 @@ ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
     s.groups = p->groups;
     s.group_channels = p->channels / p->groups;
     s.quads = quads_of(p->states);
-    s.chunk = scan_chunk(p->states);
-    s.chunks = static_cast<int>(div_up(time, s.chunk));
+    s.chunks = static_cast<int>(div_up(time, kScanChunk));
     const int64_t per_block = backward ? 128 : 128 / lanes_of(p->states);
     const int64_t tiles = div_up(s.group_channels, per_block) * s.groups;
     cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * (backward ? 2 : 3));
@@ -407,7 +406,7 @@ int ssm_conv_step(ssm *p, const void *x, int64_t x_stride, const uint8_t *done, 
 size_t ssm_scan_saved_bytes(const ssm *p, int64_t batch, int64_t time)
 {
     if (p == nullptr || !sizes_ok(batch, time)) return 0;
-    return static_cast<size_t>(batch) * div_up(time, scan_chunk(p->states)) * quads_of(p->states) * p->channels * 16;
+    return static_cast<size_t>(batch) * div_up(time, kScanChunk) * quads_of(p->states) * p->channels * 16;
 }
 
 size_t ssm_scan_workspace_bytes(const ssm *p, int64_t batch, int64_t time, int backward)

@@ -12,15 +12,15 @@ struct ScanShape {
     int channels, states, groups;
     int group_channels;        // channels / groups
     int quads;                 // recurrent states of a channel in groups of four, as `saved` holds them
-    int chunk;                 // steps between two saved states
-    int chunks;                // ceil(time / chunk)
+    int chunks;                // ceil(time / kScanChunk)
     int segments;              // pieces of the time axis worked on side by side
-    int segment_steps;         // multiple of chunk
+    int segment_steps;         // multiple of kScanChunk
     int slots;                 // blocks along the rows (backward): each takes several and keeps its sums
 };
 
-// steps between saved states: the backward kernel keeps a chunk's intermediate states on the SM
-inline int scan_chunk(int states) { return states <= 16 ? 32 : 16; }
+// Steps between saved states: the backward kernel keeps a chunk's intermediate states on the SM.
+// With 16 states and a 16-bit type the saved states are as much memory as two of the sequences.
+constexpr int kScanChunk = 16;
 
 struct ScanParams {
     const float *a, *d, *dt_bias;

@@ -13,10 +13,11 @@
 // the lane's own channel for the sums over states, of one (b or c, state) for the sums over
 // channels, so that the per-channel arithmetic is spread over the warp without repetition.
 //
-// Per chunk the warp runs the recurrence forward once, keeping h at every fourth step in
-// shared memory; then it takes the groups of four steps from the last to the first, recomputes
-// a_t and a_t h_{t-1} of the four steps into registers and walks them backwards.  Beyond 16
-// states the blocks of 16 states follow one another within the chunk.
+// Per chunk of 16 steps the warp first brings its channels' x, dt, z and dy, all loads in flight
+// together, and leaves what the steps need of them in shared memory.  It runs the recurrence
+// forward once, keeping h at every fourth step; then it takes the groups of four steps from the
+// last to the first, recomputes a_t and a_t h_{t-1} of the four steps into registers and walks
+// them backwards.  Beyond 16 states the blocks of 16 states follow one another within the chunk.
 //
 // db and dc of a block's 128 channels are added in shared memory, those of different blocks by
 // k_scan_dbc; dA, dD and d dt_bias stay with the block over all its rows and are added by
@@ -29,6 +30,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kGroup = 4;      // steps walked backwards out of registers
+constexpr int kChunk = kScanChunk;
 
 __device__ __forceinline__ Pair zero_pair() { return Pair{0ull}; }
 
@@ -67,33 +69,50 @@ __device__ __forceinline__ void store4(float *dst, const Pair (&src)[2])
     *reinterpret_cast<ulonglong2 *>(dst) = make_ulonglong2(src[0].v, src[1].v);
 }
 
-template <int CH, int SB>
+// What a step needs of the lane's own channel, binary32 [step][32] each.
+enum Scalar { kDelta, kDeltaX, kG, kX, kSig, kW, kScalars };   // kSig: sigmoid(dt + bias), kW: dy (z sigmoid(z))'
+
+template <int SB>
 struct Smem {
     static constexpr int kStates = 16 * SB;
-    static constexpr int kBc = CH * 2 * kStates * 2;                    // floats: every value twice
-    static constexpr int kCheck = (CH / kGroup) * 16 * 32;              // per warp: h at every fourth step
-    static constexpr int kScal = CH * 2 * 32;                           // per warp: delta, delta x
-    static constexpr int kG = kGroup * 32;                              // per warp: g of the group's steps
-    static constexpr int kAcc = SB > 1 ? CH * 3 * 32 : 0;               // per warp: y, pull, S of earlier state blocks
+    static constexpr int kBc = kChunk * 2 * kStates * 2;                // floats: every value twice
+    static constexpr int kCheck = (kChunk / kGroup) * 16 * 32;          // per warp: h at every fourth step
+    static constexpr int kScal = kScalars * kChunk * 32;                // per warp
+    static constexpr int kAcc = SB > 1 ? kChunk * 3 * 32 : 0;           // per warp: y, pull, S of earlier state blocks
     static constexpr int kCarry = SB > 1 ? SB * 16 * 32 : 0;            // per warp: E; as many again: dA
-    static constexpr int kWarp = kCheck + kScal + kG + kAcc + 2 * kCarry;
+    static constexpr int kWarp = kCheck + kScal + kAcc + 2 * kCarry;
     static constexpr int kBytes = (kBc + kWarps * kWarp) * 4;
 };
 
-template <typename T, int CH, int SB>
+__device__ __forceinline__ void load_bc(Pair (&dst)[4], const float *src)   // four states' values, each twice
+{
+    const ulonglong2 v = reinterpret_cast<const ulonglong2 *>(src)[0], w = reinterpret_cast<const ulonglong2 *>(src)[1];
+    dst[0].v = v.x;
+    dst[1].v = v.y;
+    dst[2].v = w.x;
+    dst[3].v = w.y;
+}
+
+__device__ __forceinline__ void clear(Pair (&h)[4][2])
+{
+#pragma unroll
+    for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
+}
+
+template <typename T, int SB>
 __global__ void __launch_bounds__(kThreads, 2)
 k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
 {
-    using S = Smem<CH, SB>;
+    using S = Smem<SB>;
     constexpr int NS = S::kStates;
+    constexpr int kStage = kChunk * 2 * NS / kThreads;   // values of b and c per thread and chunk
     extern __shared__ __align__(16) float smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    float *s_bc = smem;                               // [CH][b|c][NS][2]
-    float *s_check = smem + S::kBc + warp * S::kWarp;   // [CH/4][4 states][32 lanes][4 channels]
-    float *s_scal = s_check + S::kCheck;              // [CH][delta|delta x][32]
-    float *s_g = s_scal + S::kScal;                   // [4][32]
-    float *s_acc = s_g + S::kG;                       // [CH][y|pull|S][32]
-    float *s_e = s_acc + S::kAcc;                     // [SB][4 states][32 lanes][4 channels]
+    float *s_bc = smem;                                  // [step][b|c][NS][2]
+    float *s_check = smem + S::kBc + warp * S::kWarp;    // [step / 4][4 states][32 lanes][4 channels]
+    float *s_scal = s_check + S::kCheck;                 // [Scalar][step][32]
+    float *s_acc = s_scal + S::kScal;                    // [step][y|pull|S][32]
+    float *s_e = s_acc + S::kAcc;                        // [SB][4 states][32 lanes][4 channels]
     float *s_da = s_e + S::kCarry;
 
     const int tile = static_cast<int>(blockIdx.x % (tiles * s.groups));
@@ -101,29 +120,30 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
     const int g = tile / tiles;
     const int tile_in_group = tile - g * tiles;
     const int local0 = tile_in_group * kThreads + warp * 32;
-    const int d0 = g * s.group_channels + local0;     // the warp's first channel
+    const int d0 = g * s.group_channels + local0;        // the warp's first channel
     const bool warp_live = local0 < s.group_channels;
-    const bool live = local0 + lane < s.group_channels;   // the lane's own channel
+    const int warps = min(kWarps, (s.group_channels - tile_in_group * kThreads + 31) / 32);
+    const bool live = local0 + lane < s.group_channels;  // the lane's own channel
     const int own = live ? d0 + lane : 0;
-    const int ch = 4 * (lane >> 2);                   // the thread's first channel within the warp
-    const int quad = lane & 3;                        // the thread's states within a block of 16
+    const int ch = 4 * (lane >> 2);                      // the thread's first channel within the warp
+    const int quad = lane & 3;                           // the thread's states within a block of 16
     const int live4 = min(4, s.group_channels - (local0 + ch));   // how many of its channels exist (may be <= 0)
     const float bias = p.dt_bias != nullptr && live ? p.dt_bias[own] : 0.0f;
     const float skip = p.d != nullptr && live ? p.d[own] : 0.0f;
     const bool gated = q.z.ptr != nullptr;
+    const int total_at = (lane & 16) + 4 * quad + ((lane >> 2) & 3);   // which sum over channels spread8 leaves here
     float dd = 0.0f, ddt_bias = 0.0f;
     // E and dA of the state block at hand: with a single block they stay here, else in shared memory between chunks
     Pair e[4][2], da[4][2];
-#pragma unroll
-    for (int n = 0; n < 4; ++n) da[n][0] = da[n][1] = zero_pair();
+    clear(da);
     if (SB > 1)
         for (int i = 0; i < 4 * SB; ++i) store4(s_da + (i * 32 + lane) * 4, da[0]);
 
     for (int64_t unit = slot; unit < s.batch * s.segments; unit += s.slots) {
         const int64_t b = unit / s.segments;
         const int seg = static_cast<int>(unit - b * s.segments);
-        const int c_first = seg * (s.segment_steps / CH);
-        const int c_last = min(s.chunks, c_first + s.segment_steps / CH) - 1;
+        const int c_first = seg * (s.segment_steps / kChunk);
+        const int c_last = min(s.chunks, c_first + s.segment_steps / kChunk) - 1;
 
         // gradient that arrives from the steps after the segment
         for (int sb = 0; sb < SB; ++sb) {
@@ -149,27 +169,62 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
         }
 
         for (int chunk = c_last; chunk >= c_first; --chunk) {
-            const int tc = chunk * CH;
-            const int steps = min(CH, s.time - tc);
+            const int tc = chunk * kChunk;
+            const int steps = min(kChunk, s.time - tc);
             const int groups = (steps + kGroup - 1) / kGroup;
-            for (int i = tid; i < CH * 2 * NS; i += kThreads) {
-                const int k = i / (2 * NS), n = i % NS;
-                const Seq<const T> &src = (i / NS) & 1 ? q.c : q.b;
-                const float v = k < steps && n < s.states ? to_f32(src.row(b, tc + k)[g * s.states + n]) : 0.0f;
-                *reinterpret_cast<float2 *>(s_bc + 2 * i) = make_float2(v, v);
+            T bc[kStage];
+#pragma unroll
+            for (int i = 0; i < kStage; ++i) {
+                const int at = i * kThreads + tid;
+                const int k = at / (2 * NS), n = at % NS;
+                const Seq<const T> &src = (at / NS) & 1 ? q.c : q.b;
+                bc[i] = k < steps && n < s.states ? src.row(b, tc + k)[g * s.states + n] : from_f32<T>(0.0f);
             }
             uint32_t resets = 0;
             if (q.reset.ptr != nullptr)
                 resets = __ballot_sync(0xFFFFFFFFu, lane < steps && *q.reset.row(b, tc + min(lane, steps - 1)) != 0);
             if (warp_live) {
-#pragma unroll 8
-                for (int k = 0; k < CH; ++k) {
-                    const bool in = live && k < steps;
-                    const float x = in ? to_f32(q.x.row(b, tc + k)[own]) : 0.0f;
-                    const float delta = in ? softplus(to_f32(q.dt.row(b, tc + k)[own]) + bias) : 0.0f;
-                    s_scal[(2 * k) * 32 + lane] = delta;
-                    s_scal[(2 * k + 1) * 32 + lane] = delta * x;
+                const T *px = q.x.row(b, tc) + own, *pdt = q.dt.row(b, tc) + own, *pdy = q.dy.row(b, tc) + own;
+                const T *pz = gated ? q.z.row(b, tc) + own : nullptr;
+#pragma unroll
+                for (int k0 = 0; k0 < kChunk; k0 += 8) {
+                    T x[8], dt[8], dy[8], z[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const bool in = live && k0 + k < steps;
+                        x[k] = in ? *px : from_f32<T>(0.0f);
+                        dt[k] = in ? *pdt : from_f32<T>(0.0f);
+                        dy[k] = in ? *pdy : from_f32<T>(0.0f);
+                        z[k] = in && gated ? *pz : from_f32<T>(0.0f);
+                        px += q.x.st;
+                        pdt += q.dt.st;
+                        pdy += q.dy.st;
+                        pz += q.z.st;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const bool in = live && k0 + k < steps;
+                        float *dst = s_scal + (k0 + k) * 32 + lane;
+                        const float xv = to_f32(x[k]), raw = to_f32(dt[k]) + bias, dyv = to_f32(dy[k]);
+                        const float delta = in ? softplus(raw) : 0.0f;
+                        dst[kDelta * kChunk * 32] = delta;
+                        dst[kDeltaX * kChunk * 32] = delta * xv;
+                        dst[kX * kChunk * 32] = xv;
+                        dst[kSig * kChunk * 32] = sigmoid(raw);
+                        if (gated) {
+                            const float zv = to_f32(z[k]), sz = sigmoid(zv);
+                            dst[kG * kChunk * 32] = dyv * zv * sz;
+                            dst[kW * kChunk * 32] = dyv * fmaf(zv * sz, 1.0f - sz, sz);
+                        } else {
+                            dst[kG * kChunk * 32] = dyv;
+                        }
+                    }
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < kStage; ++i) {
+                const float v = to_f32(bc[i]);
+                *reinterpret_cast<float2 *>(s_bc + 2 * (i * kThreads + tid)) = make_float2(v, v);
             }
             __syncthreads();
 
@@ -203,31 +258,28 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                                 h[n][c] = pair(hv[n][2 * c], hv[n][2 * c + 1]);
                             }
                     }
-                    const float *bc = s_bc + (sb * 16 + 4 * quad) * 2;
+                    const float *bc4 = s_bc + (sb * 16 + 4 * quad) * 2;   // the thread's states of b; c is 2 NS further
+                    const float *sc4 = s_scal + ch;                       // its channels' scalars
 
                     // forward over the chunk: h before every group of steps
-                    for (int grp = 0; grp < groups; ++grp) {
+#pragma unroll 1
+                    for (int grp = 0;; ++grp) {
 #pragma unroll
                         for (int n = 0; n < 4; ++n) store4(s_check + ((grp * 4 + n) * 32 + lane) * 4, h[n]);
                         if (grp == groups - 1) break;
 #pragma unroll
                         for (int j = 0; j < kGroup; ++j) {
                             const int k = grp * kGroup + j;
-                            Pair delta[2], dtx[2];
-                            load4(delta, s_scal + (2 * k) * 32 + ch);
-                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
-                            if ((resets >> k) & 1u) {
-#pragma unroll
-                                for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
-                            }
-                            Pair bb[4];
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
+                            Pair delta[2], dtx[2], bb[4];
+                            load4(delta, sc4 + (kDelta * kChunk + k) * 32);
+                            load4(dtx, sc4 + (kDeltaX * kChunk + k) * 32);
+                            load_bc(bb, bc4 + (2 * k) * NS * 2);
+                            if ((resets >> k) & 1u) clear(h);
 #pragma unroll
                             for (int n = 0; n < 4; ++n)
 #pragma unroll
                                 for (int c = 0; c < 2; ++c)
-                                    h[n][c] = fma(ex2(mul(a2[n][c], delta[c])), h[n][c], mul(dtx[c], bb[n]));
+                                    h[n][c] = fma(decay(a2[n][c], delta[c]), h[n][c], mul(dtx[c], bb[n]));
                         }
                     }
                     if (SB > 1) {
@@ -238,49 +290,30 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                         }
                     }
 
+                    T *pdx = q.dx.row(b, tc + groups * kGroup) + own, *pddt = q.ddt.row(b, tc + groups * kGroup) + own;
+                    T *pdz = gated ? q.dz.row(b, tc + groups * kGroup) + own : nullptr;
+#pragma unroll 1
                     for (int grp = groups - 1; grp >= 0; --grp) {
-                        // the lane's own channel
-                        float x[kGroup], raw[kGroup], z[kGroup], dy[kGroup], gr[kGroup], sz[kGroup], yp[kGroup];
-#pragma unroll
-                        for (int j = 0; j < kGroup; ++j) {
-                            const int k = grp * kGroup + j;
-                            const bool in = live && k < steps;
-                            x[j] = in ? to_f32(q.x.row(b, tc + k)[own]) : 0.0f;
-                            raw[j] = in ? to_f32(q.dt.row(b, tc + k)[own]) + bias : 0.0f;
-                            dy[j] = in ? to_f32(q.dy.row(b, tc + k)[own]) : 0.0f;
-                            z[j] = in && gated ? to_f32(q.z.row(b, tc + k)[own]) : 0.0f;
-                        }
-#pragma unroll
-                        for (int j = 0; j < kGroup; ++j) {
-                            sz[j] = sigmoid(z[j]);
-                            gr[j] = gated ? dy[j] * z[j] * sz[j] : dy[j];
-                            s_g[j * 32 + lane] = gr[j];
-                        }
 #pragma unroll
                         for (int n = 0; n < 4; ++n) load4(h[n], s_check + ((grp * 4 + n) * 32 + lane) * 4);
                         __syncwarp();
-
                         Pair at[kGroup][4][2], ah[kGroup][4][2];
+                        float yp[kGroup];
 #pragma unroll
                         for (int j = 0; j < kGroup; ++j) {
                             const int k = grp * kGroup + j;
                             Pair delta[2], dtx[2], bb[4], cc[4];
-                            load4(delta, s_scal + (2 * k) * 32 + ch);
-                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[0]), bc + (2 * k + 1) * NS * 2);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[2]), bc + (2 * k + 1) * NS * 2 + 4);
-                            if ((resets >> k) & 1u) {
-#pragma unroll
-                                for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
-                            }
+                            load4(delta, sc4 + (kDelta * kChunk + k) * 32);
+                            load4(dtx, sc4 + (kDeltaX * kChunk + k) * 32);
+                            load_bc(bb, bc4 + (2 * k) * NS * 2);
+                            load_bc(cc, bc4 + (2 * k + 1) * NS * 2);
+                            if ((resets >> k) & 1u) clear(h);
                             Pair y2[2] = {zero_pair(), zero_pair()};
 #pragma unroll
                             for (int n = 0; n < 4; ++n)
 #pragma unroll
                                 for (int c = 0; c < 2; ++c) {
-                                    at[j][n][c] = ex2(mul(a2[n][c], delta[c]));
+                                    at[j][n][c] = decay(a2[n][c], delta[c]);
                                     ah[j][n][c] = mul(at[j][n][c], h[n][c]);
                                     h[n][c] = fma(dtx[c], bb[n], ah[j][n][c]);
                                     y2[c] = fma(cc[n], h[n][c], y2[c]);
@@ -292,40 +325,38 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                         for (int j = kGroup - 1; j >= 0; --j) {
                             const int k = grp * kGroup + j;
                             Pair delta[2], dtx[2], gg[2], bb[4], cc[4];
-                            load4(delta, s_scal + (2 * k) * 32 + ch);
-                            load4(dtx, s_scal + (2 * k + 1) * 32 + ch);
-                            load4(gg, s_g + j * 32 + ch);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[0]), bc + (2 * k) * NS * 2);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&bb[2]), bc + (2 * k) * NS * 2 + 4);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[0]), bc + (2 * k + 1) * NS * 2);
-                            load4(*reinterpret_cast<Pair(*)[2]>(&cc[2]), bc + (2 * k + 1) * NS * 2 + 4);
+                            load4(delta, sc4 + (kDelta * kChunk + k) * 32);
+                            load4(dtx, sc4 + (kDeltaX * kChunk + k) * 32);
+                            load4(gg, sc4 + (kG * kChunk + k) * 32);
+                            load_bc(bb, bc4 + (2 * k) * NS * 2);
+                            load_bc(cc, bc4 + (2 * k + 1) * NS * 2);
                             Pair pull[2] = {zero_pair(), zero_pair()}, sa[2] = {zero_pair(), zero_pair()};
                             float dbc[8];
-                            const bool first = (resets >> k) & 1u;
 #pragma unroll
                             for (int n = 0; n < 4; ++n) {
                                 Pair db2 = zero_pair(), dc2 = zero_pair();
 #pragma unroll
                                 for (int c = 0; c < 2; ++c) {
                                     const Pair ht = fma(dtx[c], bb[n], ah[j][n][c]);
-                                    dc2 = fma(gg[c], ht, dc2);
+                                    dc2 = c == 0 ? mul(gg[c], ht) : fma(gg[c], ht, dc2);
                                     const Pair dh = fma(gg[c], cc[n], e[n][c]);
-                                    db2 = fma(dtx[c], dh, db2);
-                                    pull[c] = fma(bb[n], dh, pull[c]);
+                                    db2 = c == 0 ? mul(dtx[c], dh) : fma(dtx[c], dh, db2);
+                                    pull[c] = n == 0 ? mul(bb[n], dh) : fma(bb[n], dh, pull[c]);
                                     const Pair qq = mul(dh, ah[j][n][c]);
-                                    sa[c] = fma(a2[n][c], qq, sa[c]);
+                                    sa[c] = n == 0 ? mul(a2[n][c], qq) : fma(a2[n][c], qq, sa[c]);
                                     da[n][c] = fma(delta[c], qq, da[n][c]);
-                                    e[n][c] = first ? zero_pair() : mul(at[j][n][c], dh);
+                                    e[n][c] = mul(at[j][n][c], dh);
                                 }
                                 dbc[n] = lo(db2) + hi(db2);
                                 dbc[4 + n] = lo(dc2) + hi(dc2);
                             }
+                            if ((resets >> k) & 1u) clear(e);
                             const float total = spread8(dbc, lane);
                             const float pv[4] = {lo(pull[0]), hi(pull[0]), lo(pull[1]), hi(pull[1])};
                             const float sv[4] = {lo(sa[0]), hi(sa[0]), lo(sa[1]), hi(sa[1])};
                             float own_pull = spread4(pv, lane), own_s = spread4(sv, lane), own_y = yp[j];
                             // the group's place in s_check has been read: its first words take the sums over channels
-                            s_check[grp * 4 * 128 + j * 32 + (lane & 16) + 4 * quad + ((lane >> 2) & 3)] = total;
+                            s_check[grp * 512 + j * 32 + total_at] = total;
                             if (SB > 1) {
                                 float *acc = s_acc + (3 * k) * 32 + lane;
                                 if (sb > 0) {
@@ -337,20 +368,21 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                                 acc[32] = own_pull;
                                 acc[64] = own_s;
                             }
+                            pdx -= q.dx.st;
+                            pddt -= q.ddt.st;
+                            pdz -= q.dz.st;
                             if (sb == SB - 1 && live && k < steps) {
-                                const float own_delta = s_scal[(2 * k) * 32 + lane];
-                                const float ypre = fmaf(skip, x[j], own_y);
-                                if (gated)
-                                    q.dz.row(b, tc + k)[own] =
-                                        from_f32<T>(dy[j] * ypre * fmaf(z[j] * sz[j], 1.0f - sz[j], sz[j]));
-                                q.dx.row(b, tc + k)[own] = from_f32<T>(fmaf(own_delta, own_pull, skip * gr[j]));
-                                const float ddt = fmaf(x[j], own_pull, kLn2 * own_s) * sigmoid(raw[j]);
-                                q.ddt.row(b, tc + k)[own] = from_f32<T>(ddt);
+                                const float *own_scal = s_scal + k * 32 + lane;
+                                const float x = own_scal[kX * kChunk * 32], gr = own_scal[kG * kChunk * 32];
+                                const float dx = fmaf(own_scal[kDelta * kChunk * 32], own_pull, skip * gr);
+                                const float ddt = fmaf(x, own_pull, kLn2 * own_s) * own_scal[kSig * kChunk * 32];
+                                *pdx = from_f32<T>(dx);
+                                *pddt = from_f32<T>(ddt);
+                                if (gated) *pdz = from_f32<T>(own_scal[kW * kChunk * 32] * fmaf(skip, x, own_y));
                                 ddt_bias += ddt;
-                                dd = fmaf(gr[j], x[j], dd);
+                                dd = fmaf(gr, x, dd);
                             }
                         }
-                        __syncwarp();
                     }
                     if (SB > 1) {
 #pragma unroll
@@ -362,11 +394,10 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                 }
                 __syncthreads();
                 // the block's channels together: warp w takes every fourth step
-                const int warps = min(kWarps, (s.group_channels - tile_in_group * kThreads + 31) / 32);
                 for (int k = warp; k < steps; k += kWarps) {
                     float sum = 0.0f;
                     for (int w = 0; w < warps; ++w)
-                        sum += smem[S::kBc + w * S::kWarp + (k / kGroup) * 4 * 128 + (k % kGroup) * 32 + lane];
+                        sum += smem[S::kBc + w * S::kWarp + (k / kGroup) * 512 + (k % kGroup) * 32 + lane];
                     const int64_t row = (static_cast<int64_t>(tile_in_group) * s.batch + b) * s.time + tc + k;
                     p.dbc_part[((row * s.groups + g) * 2 + (lane >> 4)) * NS + sb * 16 + (lane & 15)] = sum;
                 }
@@ -476,7 +507,7 @@ k_scan_back_summary(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, 
             for (int i = 0; i < NP / 2; ++i) {
                 Pair c;
                 c.v = *reinterpret_cast<const unsigned long long *>(&s_c[k][part * NP + 2 * i]);
-                e[i] = first ? zero_pair() : mul(ex2(mul(a2[i], dd)), fma(gg, c, e[i]));
+                e[i] = first ? zero_pair() : mul(decay(a2[i], dd), fma(gg, c, e[i]));
             }
         }
     }
@@ -587,14 +618,14 @@ void launch_summary(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &
     k_scan_back_summary<T, NP, LN><<<blocks, 128, 0, stream>>>(s, p, q, tiles);
 }
 
-template <typename T, int CH, int SB>
+template <typename T, int SB>
 int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
 {
-    using S = Smem<CH, SB>;
+    using S = Smem<SB>;
     static_assert(S::kBytes <= 227 * 1024, "one block's shared memory");
     const int tiles = (s.group_channels + kThreads - 1) / kThreads;
     int launched = 3;
-    if (cudaFuncSetAttribute(k_scan_backward<T, CH, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) !=
+    if (cudaFuncSetAttribute(k_scan_backward<T, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) !=
         cudaSuccess)
         return -1;
     if (s.segments > 1) {
@@ -608,7 +639,7 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
         k_scan_back_carry<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, stream>>>(s, p);
         launched += 2;
     }
-    k_scan_backward<T, CH, SB><<<static_cast<unsigned>(tiles * s.groups) * s.slots, kThreads, S::kBytes, stream>>>(s, p, q, tiles);
+    k_scan_backward<T, SB><<<static_cast<unsigned>(tiles * s.groups) * s.slots, kThreads, S::kBytes, stream>>>(s, p, q, tiles);
     const int64_t values = s.batch * s.time * s.groups * 2 * S::kStates;
     k_scan_dbc<T><<<static_cast<unsigned>((values + 255) / 256), 256, 0, stream>>>(s, p, q, tiles, S::kStates);
     const dim3 grid(static_cast<unsigned>((s.channels + 31) / 32), static_cast<unsigned>(s.quads + 1));
@@ -621,9 +652,9 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
 template <typename T>
 int launch_scan_backward(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaStream_t stream)
 {
-    if (s.states <= 16) return launch<T, 32, 1>(s, p, q, stream);
-    if (s.states <= 32) return launch<T, 16, 2>(s, p, q, stream);
-    return launch<T, 16, 4>(s, p, q, stream);
+    if (s.states <= 16) return launch<T, 1>(s, p, q, stream);
+    if (s.states <= 32) return launch<T, 2>(s, p, q, stream);
+    return launch<T, 4>(s, p, q, stream);
 }
 
 template int launch_scan_backward<float>(const ScanShape &, const ScanParams &, const ScanSeqs<float> &, cudaStream_t);

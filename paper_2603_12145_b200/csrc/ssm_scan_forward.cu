@@ -32,7 +32,7 @@ __device__ __forceinline__ void load_pairs(Pair (&dst)[NP / 2], const float *src
 }
 
 template <typename T, int NP, int LN, bool kSummary>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, NP == 16 ? 3 : 4)
 k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
 {
     constexpr int NS = NP * LN;
@@ -91,23 +91,36 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     // the next tile's values, in flight while the current one is worked on
     T nx[kTile], ndt[kTile], nz[kTile], nbc[kStage];
     uint8_t nreset = 0;
+    const T *px = q.x.row(b, t0) + d, *pdt = q.dt.row(b, t0) + d, *pz = gated ? q.z.row(b, t0) + d : nullptr;
+    T *py = kSummary ? nullptr : q.y.row(b, t0) + d;
+    const T *pbc[kStage];
+#pragma unroll
+    for (int k = 0; k < kStage; ++k) {
+        const int i = k * kThreads + tid;
+        const Seq<const T> &src = (i / NS) % (kWidth / NS) == 0 ? q.b : q.c;
+        pbc[k] = i < kTile * kWidth && i % NS < s.states ? src.row(b, t0 + i / kWidth) + g * s.states + i % NS : nullptr;
+    }
     auto fetch = [&](int t) {
         if (warp_live) {
 #pragma unroll
             for (int k = 0; k < kTile; ++k) {
                 const bool in = live && t + k < t1;
-                nx[k] = in ? q.x.row(b, t + k)[d] : from_f32<T>(0.0f);
-                ndt[k] = in ? q.dt.row(b, t + k)[d] : from_f32<T>(0.0f);
-                if (!kSummary) nz[k] = in && gated ? q.z.row(b, t + k)[d] : from_f32<T>(0.0f);
+                nx[k] = in ? *px : from_f32<T>(0.0f);
+                ndt[k] = in ? *pdt : from_f32<T>(0.0f);
+                px += q.x.st;
+                pdt += q.dt.st;
+                if (!kSummary) {
+                    nz[k] = in && gated ? *pz : from_f32<T>(0.0f);
+                    pz += q.z.st;
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < kStage; ++k) {
             const int i = k * kThreads + tid;
-            const int step = i / kWidth, n = i % NS;
-            const bool in = i < kTile * kWidth && t + step < t1 && n < s.states;
-            const Seq<const T> &src = (i / NS) % (kWidth / NS) == 0 ? q.b : q.c;
-            nbc[k] = in ? src.row(b, t + step)[g * s.states + n] : from_f32<T>(0.0f);
+            const int64_t st = (i / NS) % (kWidth / NS) == 0 ? q.b.st : q.c.st;
+            nbc[k] = pbc[k] != nullptr && t + i / kWidth < t1 ? *pbc[k] : from_f32<T>(0.0f);
+            if (pbc[k] != nullptr) pbc[k] += kTile * st;
         }
         if (tid < kTile) nreset = q.reset.ptr != nullptr && t + tid < t1 ? *q.reset.row(b, t + tid) : 0;
     };
@@ -117,12 +130,17 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     bool cut = false;
     int buf = 0;
     for (int t = t0; t < t1; t += kTile, buf ^= 1) {
-        T cx[kTile], cdt[kTile], cz[kTile];
+        // everything that does not wait for the recurrence, for all steps of the tile side by side
+        float delta[kTile], xv[kTile], gate[kTile];
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            cx[k] = nx[k];
-            cdt[k] = ndt[k];
-            cz[k] = nz[k];
+            // past the end: delta = 0 leaves the state as it is
+            delta[k] = t + k < t1 ? softplus(to_f32(ndt[k]) + bias) : 0.0f;
+            xv[k] = to_f32(nx[k]);
+            if (!kSummary) {
+                const float z = to_f32(nz[k]);
+                gate[k] = gated ? z * sigmoid(z) : 1.0f;
+            }
         }
 #pragma unroll
         for (int k = 0; k < kStage; ++k) {
@@ -133,46 +151,41 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
         __syncthreads();
         if (t + kTile < t1) fetch(t + kTile);
         if (!warp_live) continue;
-        if (!kSummary && p.saved != nullptr && t % s.chunk == 0 && live) {
+        if (!kSummary && p.saved != nullptr && t % kScanChunk == 0 && live) {
 #pragma unroll
             for (int i = 0; i < NP / 4; ++i) {
-                const int64_t at = ((b * s.chunks + t / s.chunk) * s.quads + part * (NP / 4) + i) * s.channels + d;
+                const int64_t at = ((b * s.chunks + t / kScanChunk) * s.quads + part * (NP / 4) + i) * s.channels + d;
                 reinterpret_cast<float4 *>(p.saved)[at] =
                     make_float4(lo(h[2 * i]), hi(h[2 * i]), lo(h[2 * i + 1]), hi(h[2 * i + 1]));
             }
         }
+        const bool stores = live && part == 0;
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            if (t + k >= t1) break;
-            const float x = to_f32(cx[k]);
-            const float delta = softplus(to_f32(cdt[k]) + bias);
             if (s_reset[buf][k]) {
                 cut = true;
 #pragma unroll
                 for (int i = 0; i < NP / 2; ++i) h[i] = pair(0.0f, 0.0f);
             }
-            span += delta;
-            const Pair dd = pair(delta, delta), dx = pair(delta * x, delta * x);
+            span += delta[k];
+            const Pair dd = pair(delta[k], delta[k]), dx = pair(delta[k] * xv[k], delta[k] * xv[k]);
             Pair bb[NP / 2], cc[NP / 2];
             load_pairs<NP>(bb, &s_bc[buf][k][part * NP]);
             if (!kSummary) load_pairs<NP>(cc, &s_bc[buf][k][NS * (kWidth / NS - 1) + part * NP]);
-            Pair acc[2] = {pair(0.0f, 0.0f), pair(0.0f, 0.0f)};
+            Pair acc[2];
 #pragma unroll
             for (int i = 0; i < NP / 2; ++i) {
-                h[i] = fma(ex2(mul(a2[i], dd)), h[i], mul(dx, bb[i]));
-                if (!kSummary) acc[i & 1] = fma(cc[i], h[i], acc[i & 1]);
+                h[i] = fma(decay(a2[i], dd), h[i], mul(dx, bb[i]));
+                if (!kSummary) acc[i & 1] = i < 2 ? mul(cc[i], h[i]) : fma(cc[i], h[i], acc[i & 1]);
             }
             if (!kSummary) {
                 const Pair sum = add(acc[0], acc[1]);
                 float y = lo(sum) + hi(sum);
 #pragma unroll
                 for (int m = 1; m < LN; m *= 2) y += __shfl_xor_sync(0xFFFFFFFFu, y, m);
-                y = fmaf(skip, x, y);
-                if (gated) {
-                    const float z = to_f32(cz[k]);
-                    y *= z * sigmoid(z);
-                }
-                if (live && part == 0) q.y.row(b, t + k)[d] = from_f32<T>(y);
+                y = fmaf(skip, xv[k], y) * gate[k];
+                if (stores && t + k < t1) *py = from_f32<T>(y);
+                py += q.y.st;
             }
         }
     }
