@@ -99,6 +99,46 @@ __device__ __forceinline__ void clear(Pair (&h)[4][2])
     for (int n = 0; n < 4; ++n) h[n][0] = h[n][1] = zero_pair();
 }
 
+// A log2 e of the thread's 4 channels and 4 states, zero where one does not exist.
+__device__ __forceinline__ void load_rates(Pair (&a2)[4][2], const ScanParams &p, const ScanShape &s, int channel, int channels,
+                                           int state)
+{
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        float v[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            v[c] = c < channels && state + n < s.states
+                       ? p.a[static_cast<int64_t>(channel + c) * s.states + state + n] * kLog2e : 0.0f;
+        a2[n][0] = pair(v[0], v[1]);
+        a2[n][1] = pair(v[2], v[3]);
+    }
+}
+
+__device__ __forceinline__ void load_saved(float4 (&h)[4], const ScanParams &p, const ScanShape &s, int64_t b, int chunk, int quad,
+                                           int channel, int channels)
+{
+    const float4 *src = reinterpret_cast<const float4 *>(p.saved) + ((b * s.chunks + chunk) * s.quads + quad) * s.channels + channel;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        h[c] = c < channels && quad < s.quads ? src[c] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+}
+
+// Four states per channel to four channels per state.
+__device__ __forceinline__ void turn(Pair (&h)[4][2], const float4 (&v)[4])
+{
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        h[0][c] = pair(v[2 * c].x, v[2 * c + 1].x);
+        h[1][c] = pair(v[2 * c].y, v[2 * c + 1].y);
+        h[2][c] = pair(v[2 * c].z, v[2 * c + 1].z);
+        h[3][c] = pair(v[2 * c].w, v[2 * c + 1].w);
+    }
+}
+
+// Asks for a line that will be needed soon.
+__device__ __forceinline__ void prefetch(const void *ptr) { asm volatile("prefetch.global.L2 [%0];" ::"l"(ptr)); }
+
 template <typename T, int SB>
 __global__ void __launch_bounds__(kThreads, 2)
 k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
@@ -133,8 +173,10 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
     const bool gated = q.z.ptr != nullptr;
     const int total_at = (lane & 16) + 4 * quad + ((lane >> 2) & 3);   // which sum over channels spread8 leaves here
     float dd = 0.0f, ddt_bias = 0.0f;
-    // E and dA of the state block at hand: with a single block they stay here, else in shared memory between chunks
-    Pair e[4][2], da[4][2];
+    // Rates, E and dA of the state block at hand: with a single block they stay here, else E and dA are in
+    // shared memory between chunks
+    Pair a2[4][2], e[4][2], da[4][2];
+    if (SB == 1) load_rates(a2, p, s, d0 + ch, live4, 4 * quad);
     clear(da);
     if (SB > 1)
         for (int i = 0; i < 4 * SB; ++i) store4(s_da + (i * 32 + lane) * 4, da[0]);
@@ -172,6 +214,8 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
             const int tc = chunk * kChunk;
             const int steps = min(kChunk, s.time - tc);
             const int groups = (steps + kGroup - 1) / kGroup;
+            float4 hv[4];
+            if (SB == 1) load_saved(hv, p, s, b, chunk, quad, d0 + ch, live4);
             T bc[kStage];
 #pragma unroll
             for (int i = 0; i < kStage; ++i) {
@@ -183,6 +227,11 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
             uint32_t resets = 0;
             if (q.reset.ptr != nullptr)
                 resets = __ballot_sync(0xFFFFFFFFu, lane < steps && *q.reset.row(b, tc + min(lane, steps - 1)) != 0);
+            if (chunk > c_first && live) {      // the chunk that follows: a lane asks for its row of two sequences
+                const int t = tc - kChunk + (lane & 15);
+                prefetch((lane < 16 ? q.x : q.dt).row(b, t) + d0);
+                prefetch((lane < 16 || !gated ? q.dy : q.z).row(b, t) + d0);
+            }
             if (warp_live) {
                 const T *px = q.x.row(b, tc) + own, *pdt = q.dt.row(b, tc) + own, *pdy = q.dy.row(b, tc) + own;
                 const T *pz = gated ? q.z.row(b, tc) + own : nullptr;
@@ -230,34 +279,12 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
 
             for (int sb = 0; sb < SB; ++sb) {
                 if (warp_live) {
-                    Pair a2[4][2], h[4][2];
-                    {
-                        float av[4][4], hv[4][4];
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const bool in = c < live4;
-                            const int64_t row = d0 + ch + (in ? c : 0);
-                            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            if (in && sb * 4 + quad < s.quads)
-                                v = reinterpret_cast<const float4 *>(p.saved)[((b * s.chunks + chunk) * s.quads + sb * 4 + quad) * s.channels + row];
-                            hv[0][c] = v.x;
-                            hv[1][c] = v.y;
-                            hv[2][c] = v.z;
-                            hv[3][c] = v.w;
-#pragma unroll
-                            for (int n = 0; n < 4; ++n) {
-                                const int state = sb * 16 + 4 * quad + n;
-                                av[n][c] = in && state < s.states ? p.a[row * s.states + state] * kLog2e : 0.0f;
-                            }
-                        }
-#pragma unroll
-                        for (int n = 0; n < 4; ++n)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                a2[n][c] = pair(av[n][2 * c], av[n][2 * c + 1]);
-                                h[n][c] = pair(hv[n][2 * c], hv[n][2 * c + 1]);
-                            }
+                    if (SB > 1) {
+                        load_rates(a2, p, s, d0 + ch, live4, sb * 16 + 4 * quad);
+                        load_saved(hv, p, s, b, chunk, sb * 4 + quad, d0 + ch, live4);
                     }
+                    Pair h[4][2];
+                    turn(h, hv);
                     const float *bc4 = s_bc + (sb * 16 + 4 * quad) * 2;   // the thread's states of b; c is 2 NS further
                     const float *sc4 = s_scal + ch;                       // its channels' scalars
 

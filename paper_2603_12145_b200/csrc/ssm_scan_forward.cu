@@ -18,7 +18,7 @@ namespace ssm_k {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kTile = 8;     // steps whose loads are in flight together
+constexpr int kTile = 4;     // steps whose loads are in flight together
 
 template <int NP>
 __device__ __forceinline__ void load_pairs(Pair (&dst)[NP / 2], const float *src)   // 16-byte aligned
@@ -32,7 +32,7 @@ __device__ __forceinline__ void load_pairs(Pair (&dst)[NP / 2], const float *src
 }
 
 template <typename T, int NP, int LN, bool kSummary>
-__global__ void __launch_bounds__(kThreads, NP == 16 ? 3 : 4)
+__global__ void __launch_bounds__(kThreads, LN > 1 ? 3 : 4)
 k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
 {
     constexpr int NS = NP * LN;
