@@ -237,7 +237,7 @@ ConvShape conv_shape(const ssm *p, int64_t batch, int64_t time)
     s.sms = p->sms;
     s.run = 32;
     const int64_t threads = static_cast<int64_t>(p->sms) * 512;
-    const int64_t vecs = div_up(p->channels, 8 / element_bytes(p));
+    const int64_t vecs = div_up(p->channels, 4);
     while (s.run > 8 && batch * div_up(time, s.run) * vecs < threads) s.run /= 2;
     s.runs = static_cast<int>(div_up(time, s.run));
     const int64_t units = batch * s.runs;
@@ -278,7 +278,7 @@ template <typename T>
 int run_conv(ssm *p, const ssm_conv_args *a, bool backward)
 {
     const ConvShape s = conv_shape(p, a->batch, a->time);
-    if (s.batch * s.runs > kMaxBlocks * 128 / s.channels) return SSM_EINVAL;
+    if (s.batch * s.runs > kMaxBlocks * 128 / (s.channels + 31)) return SSM_EINVAL;   // threads, rows of whole warps
     ConvParams k = {a->w, a->bias, a->dw, a->dbias, static_cast<float *>(a->workspace)};
     ConvSeqs<T> q = {};
     q.x = seq_of<const T>(a->x);

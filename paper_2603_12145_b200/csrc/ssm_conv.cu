@@ -1,9 +1,11 @@
 // ssm_conv.cu -- the short causal convolution: sequence, gradients, single token.
 //
-// All three are bound by memory: a thread takes V neighbouring channels (one 8- or 16-byte
-// access where sizes, strides and pointers allow, else one element) and walks a run of steps
+// All three should be bound by memory: a thread takes V = 4 neighbouring channels (one 8- or
+// 16-byte access, where sizes, strides and pointers allow; else V = 1) and walks a run of steps
 // with the last width - 1 inputs in registers, so that each input is read once plus width - 1
-// steps per run; the loads of the next steps are in flight while a step is computed.
+// steps per run; the next tile's loads are in flight while a tile is computed.  Arithmetic is on
+// pairs of channels.  The lanes of a warp share a sequence, so that a ballot gives them the
+// resets of a tile; a tile without one, the common case, takes a path that does not look at them.
 // A reset clears the window, which drops every tap from before the episode.
 //
 // The backward kernel walks forward too: step t gives dpre_t, which goes into the pending
@@ -11,6 +13,8 @@
 // then complete.  Its thread keeps its channels through all its runs, so dw and dbias stay in
 // registers until the end; each thread's sums go to a row of their own and a second kernel adds
 // the rows in a fixed order.
+#include <type_traits>
+
 #include "ssm_kernels.cuh"
 
 namespace ssm_k {
@@ -38,10 +42,57 @@ __device__ __forceinline__ Vec<T, V> zero_vec()
     return v;
 }
 
+// V channels as pairs (a single channel leaves the upper half at zero).
+template <typename T, int V>
+__device__ __forceinline__ void widen(Pair (&dst)[(V + 1) / 2], const Vec<T, V> &v)
+{
+#pragma unroll
+    for (int e = 0; e < V; e += 2) dst[e / 2] = pair(to_f32(v.e[e]), e + 1 < V ? to_f32(v.e[e + 1 < V ? e + 1 : e]) : 0.0f);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ Vec<T, V> narrow(const Pair (&src)[(V + 1) / 2])
+{
+    Vec<T, V> v;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.e[e] = from_f32<T>(e & 1 ? hi(src[e / 2]) : lo(src[e / 2]));
+    return v;
+}
+
+// The activation's sigmoid: for a 16-bit result the exponent's rounding (|u| 2^-24 relative) is far below the result's.
+template <typename T>
+__device__ __forceinline__ Pair sigmoid_for(Pair u)
+{
+    if (sizeof(T) == 4) return pair(sigmoid(lo(u)), sigmoid(hi(u)));
+    const Pair v = mul(u, pair(-kLog2e, -kLog2e));
+    const Pair w = add(pair(ex2(lo(v)), ex2(hi(v))), pair(1.0f, 1.0f));
+    return pair(rcp(lo(w)), rcp(hi(w)));
+}
+
+// The lane's part of a run of steps.
+template <typename T>
+struct Run {
+    int64_t b;
+    int t0, t1;
+    __device__ Run(const ConvShape &s, int64_t unit)
+    {
+        b = unit / s.runs;
+        t0 = static_cast<int>(unit - b * s.runs) * s.run;
+        t1 = min(s.time, t0 + s.run);
+    }
+    // bit k: step t + k < end starts an episode.  All lanes of the warp take part.
+    static __device__ uint32_t resets(const ConvSeqs<T> &q, int64_t b, int t, int count, int end)
+    {
+        if (q.reset.ptr == nullptr) return 0;
+        const int lane = threadIdx.x & 31;
+        return __ballot_sync(0xFFFFFFFFu, lane < count && t + lane < end && *q.reset.row(b, t + min(lane, end - 1 - t)) != 0);
+    }
+};
+
 // The window before step t0: win[j] = x[t0 - 1 - j], from the history before the sequence, zero
 // where an episode starts between it and t0 - 1.
 template <typename T, int V, int W>
-__device__ __forceinline__ void load_window(float (&win)[W - 1][V], const ConvShape &s, const ConvSeqs<T> &q,
+__device__ __forceinline__ void load_window(Pair (&win)[W - 1][(V + 1) / 2], const ConvShape &s, const ConvSeqs<T> &q,
                                             int64_t b, int t0, int c)
 {
     bool seen = true;
@@ -56,167 +107,212 @@ __device__ __forceinline__ void load_window(float (&win)[W - 1][V], const ConvSh
                 v = load_vec<T, V>(q.history + (b * (W - 1) + (W - 1 + t)) * s.channels + c);
             if (q.reset.ptr != nullptr && t >= 0 && *q.reset.row(b, t) != 0) seen = false;
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) win[j][e] = to_f32(v.e[e]);
+        widen<T, V>(win[j], v);
     }
+}
+
+template <int V>
+__device__ __forceinline__ void load_params(Pair (&dst)[(V + 1) / 2], const float *src, int stride)
+{
+#pragma unroll
+    for (int e = 0; e < V; e += 2)
+        dst[e / 2] = src == nullptr ? Pair{0ull} : pair(src[e * stride], e + 1 < V ? src[(e + 1) * stride] : 0.0f);
 }
 
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(kThreads)
 k_conv_forward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 {
-    constexpr int kTile = 8;
-    const int vecs = s.channels / V;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int64_t unit = i / vecs;
+    constexpr int kTile = 8, P = (V + 1) / 2;
+    const int vecs = s.channels / V, tiles = (vecs + 31) / 32;
+    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / 32;
+    const int64_t unit = warp / tiles;
     if (unit >= s.batch * s.runs) return;
-    const int c = static_cast<int>(i - unit * vecs) * V;
-    const int64_t b = unit / s.runs;
-    const int t0 = static_cast<int>(unit - b * s.runs) * s.run;
-    const int t1 = min(s.time, t0 + s.run);
-    float w[W][V], bias[V], win[W - 1][V];
+    const int vec = static_cast<int>(warp - unit * tiles) * 32 + (threadIdx.x & 31);
+    const bool live = vec < vecs;
+    const int c = (live ? vec : 0) * V;
+    const Run<T> r(s, unit);
+    Pair w[W][P], bias[P], win[W - 1][P];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-#pragma unroll
-        for (int k = 0; k < W; ++k) w[k][e] = p.w[static_cast<int64_t>(c + e) * W + k];
-        bias[e] = p.bias != nullptr ? p.bias[c + e] : 0.0f;
-    }
-    load_window<T, V, W>(win, s, q, b, t0, c);
-    for (int t = t0; t < t1; t += kTile) {
-        Vec<T, V> x[kTile];
-        uint8_t reset[kTile];
+    for (int k = 0; k < W; ++k) load_params<V>(w[k], p.w + static_cast<int64_t>(c) * W + k, W);
+    load_params<V>(bias, p.bias != nullptr ? p.bias + c : nullptr, 1);
+    load_window<T, V, W>(win, s, q, r.b, r.t0, c);
+    const T *px = q.x.row(r.b, r.t0) + c;
+    T *py = q.y.row(r.b, r.t0) + c;
+    Vec<T, V> next[kTile];
+    auto fetch = [&](int t) {
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            const bool in = t + k < t1;
-            x[k] = in ? load_vec<T, V>(q.x.row(b, t + k) + c) : zero_vec<T, V>();
-            reset[k] = in && q.reset.ptr != nullptr ? *q.reset.row(b, t + k) : 0;
+            next[k] = live && t + k < r.t1 ? load_vec<T, V>(px) : zero_vec<T, V>();
+            px += q.x.st;
+        }
+    };
+    fetch(r.t0);
+    uint32_t next_resets = Run<T>::resets(q, r.b, r.t0, kTile, r.t1);
+    for (int t = r.t0; t < r.t1; t += kTile) {
+        Vec<T, V> x[kTile];
+#pragma unroll
+        for (int k = 0; k < kTile; ++k) x[k] = next[k];
+        const uint32_t resets = next_resets;
+        if (t + kTile < r.t1) {
+            fetch(t + kTile);
+            next_resets = Run<T>::resets(q, r.b, t + kTile, kTile, r.t1);
         }
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            if (t + k >= t1) break;
-            if (reset[k]) {
+            if (t + k >= r.t1) break;
+            if ((resets >> k) & 1u) {
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) win[j][e] = 0.0f;
+                    for (int i = 0; i < P; ++i) win[j][i] = Pair{0ull};
             }
-            Vec<T, V> out;
+            Pair xv[P], out[P];
+            widen<T, V>(xv, x[k]);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float xv = to_f32(x[k].e[e]);
-                float u = bias[e];
+            for (int i = 0; i < P; ++i) {
+                Pair u = bias[i];
 #pragma unroll
-                for (int j = W - 2; j >= 0; --j) u = fmaf(w[W - 2 - j][e], win[j][e], u);
-                u = fmaf(w[W - 1][e], xv, u);
-                out.e[e] = from_f32<T>(u * sigmoid(u));
+                for (int j = W - 2; j >= 0; --j) u = fma(w[W - 2 - j][i], win[j][i], u);
+                u = fma(w[W - 1][i], xv[i], u);
+                out[i] = mul(u, sigmoid_for<T>(u));
 #pragma unroll
-                for (int j = W - 2; j > 0; --j) win[j][e] = win[j - 1][e];
-                win[0][e] = xv;
+                for (int j = W - 2; j > 0; --j) win[j][i] = win[j - 1][i];
+                win[0][i] = xv[i];
             }
-            *reinterpret_cast<Vec<T, V> *>(q.y.row(b, t + k) + c) = out;
+            if (live) *reinterpret_cast<Vec<T, V> *>(py) = narrow<T, V>(out);
+            py += q.y.st;
         }
     }
-    if (t1 == s.time && q.history_out != nullptr) {
+    if (r.t1 == s.time && q.history_out != nullptr && live) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) {
-            Vec<T, V> out;
-#pragma unroll
-            for (int e = 0; e < V; ++e) out.e[e] = from_f32<T>(win[j][e]);
-            *reinterpret_cast<Vec<T, V> *>(q.history_out + (b * (W - 1) + (W - 2 - j)) * s.channels + c) = out;
-        }
+        for (int j = 0; j < W - 1; ++j)
+            *reinterpret_cast<Vec<T, V> *>(q.history_out + (r.b * (W - 1) + (W - 2 - j)) * s.channels + c) = narrow<T, V>(win[j]);
     }
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 {
-    constexpr int kTile = 8;
-    const int vecs = s.channels / V;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    const int slot = static_cast<int>(i / vecs);
+    constexpr int kTile = 4, P = (V + 1) / 2;
+    const int vecs = s.channels / V, tiles = (vecs + 31) / 32;
+    const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / 32;
+    const int slot = static_cast<int>(warp / tiles);
     if (slot >= s.slots) return;
-    const int c = static_cast<int>(i - static_cast<int64_t>(slot) * vecs) * V;
-    float w[W][V], bias[V], dw[W][V], dbias[V];
+    const int vec = static_cast<int>(warp - static_cast<int64_t>(slot) * tiles) * 32 + (threadIdx.x & 31);
+    const bool live = vec < vecs;
+    const int c = (live ? vec : 0) * V;
+    const Pair zero = Pair{0ull}, one = pair(1.0f, 1.0f);
+    Pair w[W][P], bias[P], dw[W][P], dbias[P];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
+    for (int k = 0; k < W; ++k) load_params<V>(w[k], p.w + static_cast<int64_t>(c) * W + k, W);
+    load_params<V>(bias, p.bias != nullptr ? p.bias + c : nullptr, 1);
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-            w[k][e] = p.w[static_cast<int64_t>(c + e) * W + k];
-            dw[k][e] = 0.0f;
-        }
-        bias[e] = p.bias != nullptr ? p.bias[c + e] : 0.0f;
-        dbias[e] = 0.0f;
+    for (int i = 0; i < P; ++i) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) dw[k][i] = zero;
+        dbias[i] = zero;
     }
     for (int64_t unit = slot; unit < s.batch * s.runs; unit += s.slots) {
-        const int64_t b = unit / s.runs;
-        const int t0 = static_cast<int>(unit - b * s.runs) * s.run;
-        const int t1 = min(s.time, t0 + s.run);
-        const int t2 = t1 + W - 1;        // the gradients of the run's last inputs come from the steps up to here
-        float win[W - 1][V], pend[W][V];
-        load_window<T, V, W>(win, s, q, b, t0, c);
+        const Run<T> r(s, unit);
+        const int t2 = r.t1 + W - 1;        // the gradients of the run's last inputs come from the steps up to here
+        const int t3 = min(t2, s.time);     // steps that exist
+        Pair win[W - 1][P], pend[W][P];
+        load_window<T, V, W>(win, s, q, r.b, r.t0, c);
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int e = 0; e < V; ++e) pend[j][e] = 0.0f;
+            for (int i = 0; i < P; ++i) pend[j][i] = zero;
         int age = W;                      // steps since the episode began, as far as the run's own inputs go
-        for (int t = t0; t < t2; t += kTile) {
+        const T *px = q.x.row(r.b, r.t0) + c, *pdy = q.dy.row(r.b, r.t0) + c;
+        T *pdx = q.dx.row(r.b, r.t0) + c;
+        Vec<T, V> nx[kTile], ndy[kTile];
+        auto fetch = [&](int t) {
+#pragma unroll
+            for (int k = 0; k < kTile; ++k) {
+                const bool in = live && t + k < t3;
+                nx[k] = in ? load_vec<T, V>(px) : zero_vec<T, V>();
+                ndy[k] = in ? load_vec<T, V>(pdy) : zero_vec<T, V>();
+                px += q.x.st;
+                pdy += q.dy.st;
+            }
+        };
+        fetch(r.t0);
+        uint32_t next_resets = Run<T>::resets(q, r.b, r.t0, kTile, t3);
+        for (int t = r.t0; t < t2; t += kTile) {
             Vec<T, V> x[kTile], dy[kTile];
-            uint8_t reset[kTile];
 #pragma unroll
             for (int k = 0; k < kTile; ++k) {
-                const bool in = t + k < t2 && t + k < s.time;
-                x[k] = in ? load_vec<T, V>(q.x.row(b, t + k) + c) : zero_vec<T, V>();
-                dy[k] = in ? load_vec<T, V>(q.dy.row(b, t + k) + c) : zero_vec<T, V>();
-                reset[k] = in && q.reset.ptr != nullptr ? *q.reset.row(b, t + k) : 0;
+                x[k] = nx[k];
+                dy[k] = ndy[k];
             }
+            const uint32_t resets = next_resets;
+            if (t + kTile < t2) {
+                fetch(t + kTile);
+                next_resets = t + kTile < t3 ? Run<T>::resets(q, r.b, t + kTile, kTile, t3) : 0;
+            }
+            // kPlain: every step of the tile is the run's own, in one episode with its taps, and completes a gradient
+            auto walk = [&](auto plain) {
+                constexpr bool kPlain = decltype(plain)::value;
 #pragma unroll
-            for (int k = 0; k < kTile; ++k) {
-                if (t + k >= t2) break;
-                age = reset[k] ? 0 : age + 1;
-                const bool own = t + k < t1;
-                const bool inside = t + k < s.time;
-                Vec<T, V> out;
+                for (int k = 0; k < kTile; ++k) {
+                    if (!kPlain) {
+                        if (t + k >= t2) break;
+                        age = (resets >> k) & 1u ? 0 : age + 1;
+                        if (age == 0) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (reset[k]) {
+                            for (int j = 0; j < W - 1; ++j)
 #pragma unroll
-                        for (int j = 0; j < W - 1; ++j) win[j][e] = 0.0f;
+                                for (int i = 0; i < P; ++i) win[j][i] = zero;
+                        }
                     }
-                    const float xv = to_f32(x[k].e[e]);
-                    float u = bias[e];
+                    Pair xv[P], dyv[P];
+                    widen<T, V>(xv, x[k]);
+                    widen<T, V>(dyv, dy[k]);
 #pragma unroll
-                    for (int j = W - 2; j >= 0; --j) u = fmaf(w[W - 2 - j][e], win[j][e], u);
-                    u = fmaf(w[W - 1][e], xv, u);
-                    const float sg = sigmoid(u);
-                    // past the end of the sequence there is no step: not 0 * slope, which a NaN would survive
-                    const float dpre = inside ? to_f32(dy[k].e[e]) * fmaf(u * sg, 1.0f - sg, sg) : 0.0f;
-                    if (own) {
-                        dbias[e] += dpre;
-                        dw[W - 1][e] = fmaf(dpre, xv, dw[W - 1][e]);
+                    for (int i = 0; i < P; ++i) {
+                        Pair u = bias[i];
 #pragma unroll
-                        for (int j = 0; j < W - 1; ++j) dw[W - 2 - j][e] = fmaf(dpre, win[j][e], dw[W - 2 - j][e]);
+                        for (int j = W - 2; j >= 0; --j) u = fma(w[W - 2 - j][i], win[j][i], u);
+                        u = fma(w[W - 1][i], xv[i], u);
+                        const Pair sg = sigmoid_for<T>(u);
+                        // (u sigmoid(u))' = sg + u sg (1 - sg) = sg + (u sg) - (u sg) sg
+                        const Pair us = mul(u, sg);
+                        Pair dpre = mul(dyv[i], fma(us, fma(sg, pair(-1.0f, -1.0f), one), sg));
+                        // past the end of the sequence there is no step: not 0 * slope, which a NaN would survive
+                        if (!kPlain && t + k >= s.time) dpre = zero;
+                        if (kPlain || t + k < r.t1) {
+                            dbias[i] = add(dbias[i], dpre);
+                            dw[W - 1][i] = fma(dpre, xv[i], dw[W - 1][i]);
+#pragma unroll
+                            for (int j = 0; j < W - 1; ++j) dw[W - 2 - j][i] = fma(dpre, win[j][i], dw[W - 2 - j][i]);
+                        }
+#pragma unroll
+                        for (int j = W - 1; j > 0; --j)
+                            pend[j][i] = kPlain || age >= j ? fma(dpre, w[W - 1 - j][i], pend[j - 1][i]) : pend[j - 1][i];
+                        pend[0][i] = mul(dpre, w[W - 1][i]);
+#pragma unroll
+                        for (int j = W - 2; j > 0; --j) win[j][i] = win[j - 1][i];
+                        win[0][i] = xv[i];
                     }
-#pragma unroll
-                    for (int j = W - 1; j > 0; --j)
-                        pend[j][e] = age >= j ? fmaf(dpre, w[W - 1 - j][e], pend[j - 1][e]) : pend[j - 1][e];
-                    pend[0][e] = dpre * w[W - 1][e];
-                    out.e[e] = from_f32<T>(pend[W - 1][e]);
-#pragma unroll
-                    for (int j = W - 2; j > 0; --j) win[j][e] = win[j - 1][e];
-                    win[0][e] = xv;
+                    if (kPlain || t + k - (W - 1) >= r.t0) {
+                        if (live) *reinterpret_cast<Vec<T, V> *>(pdx) = narrow<T, V>(pend[W - 1]);
+                        pdx += q.dx.st;
+                    }
                 }
-                if (t + k - (W - 1) >= t0) *reinterpret_cast<Vec<T, V> *>(q.dx.row(b, t + k - (W - 1)) + c) = out;
-            }
+            };
+            if (resets == 0 && age >= W - 1 && t >= r.t0 + W - 1 && t + kTile <= r.t1)
+                walk(std::true_type());
+            else
+                walk(std::false_type());
         }
     }
+    if (!live) return;
 #pragma unroll
-    for (int k = 0; k <= W; ++k) {
-        Vec<float, V> out;
-#pragma unroll
-        for (int e = 0; e < V; ++e) out.e[e] = k < W ? dw[k < W ? k : 0][e] : dbias[e];
-        *reinterpret_cast<Vec<float, V> *>(p.part + (static_cast<int64_t>(slot) * (W + 1) + k) * s.channels + c) = out;
-    }
+    for (int k = 0; k <= W; ++k)
+        *reinterpret_cast<Vec<float, V> *>(p.part + (static_cast<int64_t>(slot) * (W + 1) + k) * s.channels + c) =
+            narrow<float, V>(k < W ? dw[k < W ? k : 0] : dbias);
 }
 
 // Adds the slots' rows of one (tap, channel): a warp takes 32 neighbouring channels at a time,
@@ -284,6 +380,9 @@ k_conv_step(const ConvShape s, const ConvParams p, const T *__restrict__ x, cons
 
 unsigned blocks_for(int64_t threads) { return static_cast<unsigned>((threads + kThreads - 1) / kThreads); }
 
+// rows of `vecs` vectors, a whole number of warps each
+int64_t warp_threads(int64_t rows, int vecs) { return rows * ((vecs + 31) / 32) * 32; }
+
 template <typename T>
 bool fits(const Seq<T> &q, int v)
 {
@@ -307,12 +406,13 @@ bool fits(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>(pt
 template <typename T>
 int launch_conv_forward(const ConvShape &s, const ConvParams &p, const ConvSeqs<T> &q, cudaStream_t stream)
 {
-    constexpr int V = 8 / sizeof(T);
-    if (s.channels % V == 0 && fits(q.x, V) && fits(q.y, V) && fits(q.history, 8) && fits(q.history_out, 8)) {
-        const unsigned blocks = blocks_for(s.batch * s.runs * (s.channels / V));
+    constexpr int V = 4;
+    if (s.channels % V == 0 && fits(q.x, V) && fits(q.y, V) && fits(q.history, V * sizeof(T)) &&
+        fits(q.history_out, V * sizeof(T))) {
+        const unsigned blocks = blocks_for(warp_threads(s.batch * s.runs, s.channels / V));
         SSM_BY_WIDTH(k_conv_forward, T, V, blocks, s, p, q);
     } else {
-        const unsigned blocks = blocks_for(s.batch * s.runs * s.channels);
+        const unsigned blocks = blocks_for(warp_threads(s.batch * s.runs, s.channels));
         SSM_BY_WIDTH(k_conv_forward, T, 1, blocks, s, p, q);
     }
     return cudaGetLastError() == cudaSuccess ? 1 : -1;
@@ -321,12 +421,12 @@ int launch_conv_forward(const ConvShape &s, const ConvParams &p, const ConvSeqs<
 template <typename T>
 int launch_conv_backward(const ConvShape &s, const ConvParams &p, const ConvSeqs<T> &q, cudaStream_t stream)
 {
-    constexpr int V = 8 / sizeof(T);
-    if (s.channels % V == 0 && fits(q.x, V) && fits(q.dy, V) && fits(q.dx, V) && fits(q.history, 8)) {
-        const unsigned blocks = blocks_for(static_cast<int64_t>(s.slots) * (s.channels / V));
+    constexpr int V = 4;
+    if (s.channels % V == 0 && fits(q.x, V) && fits(q.dy, V) && fits(q.dx, V) && fits(q.history, V * sizeof(T))) {
+        const unsigned blocks = blocks_for(warp_threads(s.slots, s.channels / V));
         SSM_BY_WIDTH(k_conv_backward, T, V, blocks, s, p, q);
     } else {
-        const unsigned blocks = blocks_for(static_cast<int64_t>(s.slots) * s.channels);
+        const unsigned blocks = blocks_for(warp_threads(s.slots, s.channels));
         SSM_BY_WIDTH(k_conv_backward, T, 1, blocks, s, p, q);
     }
     const dim3 grid(static_cast<unsigned>((s.channels + 31) / 32), static_cast<unsigned>(s.width + 1));
