@@ -225,8 +225,9 @@ int scan(ssm *p, const ssm_scan_args *a, bool backward)
     return p->type == SSM_BF16 ? run_scan<__nv_bfloat16>(p, a, backward) : run_scan<__half>(p, a, backward);
 }
 
-// Units of work of the convolution: runs of steps.  A run re-reads width - 1 steps, so it is as
-// long as the device stays full, 32 steps at most.
+// Units of work of the convolution: runs of steps, a warp for every 128 channels of each.  A run
+// re-reads width - 1 steps and starts with nothing in flight, so it is as long as the device
+// stays full, 128 steps at most.
 ConvShape conv_shape(const ssm *p, int64_t batch, int64_t time)
 {
     ConvShape s = {};
@@ -235,13 +236,13 @@ ConvShape conv_shape(const ssm *p, int64_t batch, int64_t time)
     s.channels = p->channels;
     s.width = p->width;
     s.sms = p->sms;
-    s.run = 32;
-    const int64_t threads = static_cast<int64_t>(p->sms) * 512;
-    const int64_t vecs = div_up(p->channels, 4);
-    while (s.run > 8 && batch * div_up(time, s.run) * vecs < threads) s.run /= 2;
+    const int64_t warps = div_up(p->channels, 128);          // of a run, where vectors can be used
+    const int64_t resident = static_cast<int64_t>(p->sms) * 16;
+    s.run = 128;
+    while (s.run > 8 && batch * div_up(time, s.run) * warps < 2 * resident) s.run /= 2;
     s.runs = static_cast<int>(div_up(time, s.run));
     const int64_t units = batch * s.runs;
-    int64_t slots = div_up(threads, vecs);
+    int64_t slots = div_up(resident, warps);
     if (slots > units) slots = units;
     s.slots = static_cast<int>(div_up(units, div_up(units, slots)));
     return s;

@@ -13,6 +13,7 @@
 // then complete.  Its thread keeps its channels through all its runs, so dw and dbias stay in
 // registers until the end; each thread's sums go to a row of their own and a second kernel adds
 // the rows in a fixed order.
+#include <cstring>
 #include <type_traits>
 
 #include "ssm_kernels.cuh"
@@ -22,40 +23,68 @@ namespace {
 
 constexpr int kThreads = 128;
 
+// V neighbouring elements as they lie in memory: one access, and nothing is taken apart before it is needed (an
+// extraction right behind a load would wait for it).
+template <int Bytes>
+struct Words;
+template <>
+struct Words<2> {
+    using type = uint16_t;
+};
+template <>
+struct Words<4> {
+    using type = uint32_t;
+};
+template <>
+struct Words<8> {
+    using type = uint2;
+};
+template <>
+struct Words<16> {
+    using type = uint4;
+};
+
 template <typename T, int V>
-struct alignas(sizeof(T) * V) Vec {
-    T e[V];
+struct Vec {
+    typename Words<sizeof(T) * V>::type w;
 };
 
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
 {
-    return *reinterpret_cast<const Vec<T, V> *>(p);
+    return Vec<T, V>{*reinterpret_cast<const decltype(Vec<T, V>::w) *>(p)};
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void store_vec(T *p, const Vec<T, V> &v)
+{
+    *reinterpret_cast<decltype(Vec<T, V>::w) *>(p) = v.w;
 }
 
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> zero_vec()
 {
-    Vec<T, V> v;
-#pragma unroll
-    for (int e = 0; e < V; ++e) v.e[e] = from_f32<T>(0.0f);
-    return v;
+    return Vec<T, V>{};
 }
 
 // V channels as pairs (a single channel leaves the upper half at zero).
 template <typename T, int V>
 __device__ __forceinline__ void widen(Pair (&dst)[(V + 1) / 2], const Vec<T, V> &v)
 {
+    T e[V];
+    memcpy(e, &v.w, sizeof(e));
 #pragma unroll
-    for (int e = 0; e < V; e += 2) dst[e / 2] = pair(to_f32(v.e[e]), e + 1 < V ? to_f32(v.e[e + 1 < V ? e + 1 : e]) : 0.0f);
+    for (int i = 0; i < V; i += 2) dst[i / 2] = pair(to_f32(e[i]), i + 1 < V ? to_f32(e[i + 1 < V ? i + 1 : i]) : 0.0f);
 }
 
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> narrow(const Pair (&src)[(V + 1) / 2])
 {
-    Vec<T, V> v;
+    T e[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v.e[e] = from_f32<T>(e & 1 ? hi(src[e / 2]) : lo(src[e / 2]));
+    for (int i = 0; i < V; ++i) e[i] = from_f32<T>(i & 1 ? hi(src[i / 2]) : lo(src[i / 2]));
+    Vec<T, V> v;
+    memcpy(&v.w, e, sizeof(e));
     return v;
 }
 
@@ -80,34 +109,38 @@ struct Run {
         t0 = static_cast<int>(unit - b * s.runs) * s.run;
         t1 = min(s.time, t0 + s.run);
     }
-    // bit k: step t + k < end starts an episode.  All lanes of the warp take part.
-    static __device__ uint32_t resets(const ConvSeqs<T> &q, int64_t b, int t, int count, int end)
+    // Lane k < count: does step t + k < end start an episode?  A ballot over the lanes, taken when the
+    // tile is worked on, gives all of them the tile's resets.
+    static __device__ uint8_t reset_of_lane(const ConvSeqs<T> &q, int64_t b, int t, int count, int end)
     {
-        if (q.reset.ptr == nullptr) return 0;
         const int lane = threadIdx.x & 31;
-        return __ballot_sync(0xFFFFFFFFu, lane < count && t + lane < end && *q.reset.row(b, t + min(lane, end - 1 - t)) != 0);
+        return q.reset.ptr != nullptr && lane < count && t + lane < end ? *q.reset.row(b, t + lane) : 0;
     }
 };
 
 // The window before step t0: win[j] = x[t0 - 1 - j], from the history before the sequence, zero
-// where an episode starts between it and t0 - 1.
+// where an episode starts between it and t0 - 1.  All loads are in flight together.
 template <typename T, int V, int W>
 __device__ __forceinline__ void load_window(Pair (&win)[W - 1][(V + 1) / 2], const ConvShape &s, const ConvSeqs<T> &q,
                                             int64_t b, int t0, int c)
 {
-    bool seen = true;
+    Vec<T, V> v[W - 1];
+    bool starts[W - 1];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int t = t0 - 1 - j;
-        Vec<T, V> v = zero_vec<T, V>();
-        if (seen) {
-            if (t >= 0)
-                v = load_vec<T, V>(q.x.row(b, t) + c);
-            else if (q.history != nullptr)
-                v = load_vec<T, V>(q.history + (b * (W - 1) + (W - 1 + t)) * s.channels + c);
-            if (q.reset.ptr != nullptr && t >= 0 && *q.reset.row(b, t) != 0) seen = false;
-        }
-        widen<T, V>(win[j], v);
+        v[j] = zero_vec<T, V>();
+        if (t >= 0)
+            v[j] = load_vec<T, V>(q.x.row(b, t) + c);
+        else if (q.history != nullptr)
+            v[j] = load_vec<T, V>(q.history + (b * (W - 1) + (W - 1 + t)) * s.channels + c);
+        starts[j] = q.reset.ptr != nullptr && t >= 0 && *q.reset.row(b, t) != 0;
+    }
+    bool seen = true;
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+        widen<T, V>(win[j], seen ? v[j] : zero_vec<T, V>());
+        seen = seen && !starts[j];
     }
 }
 
@@ -136,7 +169,6 @@ k_conv_forward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 #pragma unroll
     for (int k = 0; k < W; ++k) load_params<V>(w[k], p.w + static_cast<int64_t>(c) * W + k, W);
     load_params<V>(bias, p.bias != nullptr ? p.bias + c : nullptr, 1);
-    load_window<T, V, W>(win, s, q, r.b, r.t0, c);
     const T *px = q.x.row(r.b, r.t0) + c;
     T *py = q.y.row(r.b, r.t0) + c;
     Vec<T, V> next[kTile];
@@ -148,15 +180,16 @@ k_conv_forward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
         }
     };
     fetch(r.t0);
-    uint32_t next_resets = Run<T>::resets(q, r.b, r.t0, kTile, r.t1);
+    load_window<T, V, W>(win, s, q, r.b, r.t0, c);
+    uint8_t next_reset = Run<T>::reset_of_lane(q, r.b, r.t0, kTile, r.t1);
     for (int t = r.t0; t < r.t1; t += kTile) {
         Vec<T, V> x[kTile];
 #pragma unroll
         for (int k = 0; k < kTile; ++k) x[k] = next[k];
-        const uint32_t resets = next_resets;
+        const uint32_t resets = __ballot_sync(0xFFFFFFFFu, next_reset != 0);
         if (t + kTile < r.t1) {
             fetch(t + kTile);
-            next_resets = Run<T>::resets(q, r.b, t + kTile, kTile, r.t1);
+            next_reset = Run<T>::reset_of_lane(q, r.b, t + kTile, kTile, r.t1);
         }
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
@@ -180,19 +213,19 @@ k_conv_forward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
                 for (int j = W - 2; j > 0; --j) win[j][i] = win[j - 1][i];
                 win[0][i] = xv[i];
             }
-            if (live) *reinterpret_cast<Vec<T, V> *>(py) = narrow<T, V>(out);
+            if (live) store_vec<T, V>(py, narrow<T, V>(out));
             py += q.y.st;
         }
     }
     if (r.t1 == s.time && q.history_out != nullptr && live) {
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
-            *reinterpret_cast<Vec<T, V> *>(q.history_out + (r.b * (W - 1) + (W - 2 - j)) * s.channels + c) = narrow<T, V>(win[j]);
+            store_vec<T, V>(q.history_out + (r.b * (W - 1) + (W - 2 - j)) * s.channels + c, narrow<T, V>(win[j]));
     }
 }
 
 template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, 4)
 k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 {
     constexpr int kTile = 4, P = (V + 1) / 2;
@@ -219,7 +252,6 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
         const int t2 = r.t1 + W - 1;        // the gradients of the run's last inputs come from the steps up to here
         const int t3 = min(t2, s.time);     // steps that exist
         Pair win[W - 1][P], pend[W][P];
-        load_window<T, V, W>(win, s, q, r.b, r.t0, c);
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
@@ -239,7 +271,8 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
             }
         };
         fetch(r.t0);
-        uint32_t next_resets = Run<T>::resets(q, r.b, r.t0, kTile, t3);
+        load_window<T, V, W>(win, s, q, r.b, r.t0, c);
+        uint8_t next_reset = Run<T>::reset_of_lane(q, r.b, r.t0, kTile, t3);
         for (int t = r.t0; t < t2; t += kTile) {
             Vec<T, V> x[kTile], dy[kTile];
 #pragma unroll
@@ -247,10 +280,10 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
                 x[k] = nx[k];
                 dy[k] = ndy[k];
             }
-            const uint32_t resets = next_resets;
+            const uint32_t resets = __ballot_sync(0xFFFFFFFFu, next_reset != 0);
             if (t + kTile < t2) {
                 fetch(t + kTile);
-                next_resets = t + kTile < t3 ? Run<T>::resets(q, r.b, t + kTile, kTile, t3) : 0;
+                next_reset = Run<T>::reset_of_lane(q, r.b, t + kTile, kTile, t3);
             }
             // kPlain: every step of the tile is the run's own, in one episode with its taps, and completes a gradient
             auto walk = [&](auto plain) {
@@ -297,7 +330,7 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
                         win[0][i] = xv[i];
                     }
                     if (kPlain || t + k - (W - 1) >= r.t0) {
-                        if (live) *reinterpret_cast<Vec<T, V> *>(pdx) = narrow<T, V>(pend[W - 1]);
+                        if (live) store_vec<T, V>(pdx, narrow<T, V>(pend[W - 1]));
                         pdx += q.dx.st;
                     }
                 }
@@ -311,8 +344,8 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
     if (!live) return;
 #pragma unroll
     for (int k = 0; k <= W; ++k)
-        *reinterpret_cast<Vec<float, V> *>(p.part + (static_cast<int64_t>(slot) * (W + 1) + k) * s.channels + c) =
-            narrow<float, V>(k < W ? dw[k < W ? k : 0] : dbias);
+        store_vec<float, V>(p.part + (static_cast<int64_t>(slot) * (W + 1) + k) * s.channels + c,
+                            narrow<float, V>(k < W ? dw[k < W ? k : 0] : dbias));
 }
 
 // Adds the slots' rows of one (tap, channel): a warp takes 32 neighbouring channels at a time,
@@ -349,6 +382,7 @@ k_conv_step(const ConvShape s, const ConvParams p, const T *__restrict__ x, cons
             const uint8_t *__restrict__ done, const int64_t done_stride, const T *history, T *history_out,
             T *__restrict__ y, const int64_t y_stride)
 {
+    constexpr int P = (V + 1) / 2;
     const int vecs = s.channels / V;
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     const int64_t row = i / vecs;
@@ -365,17 +399,22 @@ k_conv_step(const ConvShape s, const ConvParams p, const T *__restrict__ x, cons
 #pragma unroll
         for (int k = 0; k < W - 1; ++k) taps[k] = zero_vec<T, V>();
     }
-    Vec<T, V> out;
+    Pair x4[W][P], out[P];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        float u = p.bias != nullptr ? p.bias[c + e] : 0.0f;
+    for (int k = 0; k < W; ++k) widen<T, V>(x4[k], taps[k]);
+    load_params<V>(out, p.bias != nullptr ? p.bias + c : nullptr, 1);
 #pragma unroll
-        for (int k = 0; k < W; ++k) u = fmaf(p.w[static_cast<int64_t>(c + e) * W + k], to_f32(taps[k].e[e]), u);
-        out.e[e] = from_f32<T>(u * sigmoid(u));
+    for (int k = 0; k < W; ++k) {
+        Pair w[P];
+        load_params<V>(w, p.w + static_cast<int64_t>(c) * W + k, W);
+#pragma unroll
+        for (int i = 0; i < P; ++i) out[i] = fma(w[i], x4[k][i], out[i]);
     }
-    *reinterpret_cast<Vec<T, V> *>(y + row * y_stride + c) = out;
 #pragma unroll
-    for (int k = 0; k < W - 1; ++k) *reinterpret_cast<Vec<T, V> *>(dst + k * s.channels) = taps[k + 1];
+    for (int i = 0; i < P; ++i) out[i] = mul(out[i], sigmoid_for<T>(out[i]));
+    store_vec<T, V>(y + row * y_stride + c, narrow<T, V>(out));
+#pragma unroll
+    for (int k = 0; k < W - 1; ++k) store_vec<T, V>(dst + k * s.channels, taps[k + 1]);
 }
 
 unsigned blocks_for(int64_t threads) { return static_cast<unsigned>((threads + kThreads - 1) / kThreads); }
@@ -439,9 +478,10 @@ int launch_conv_step(const ConvShape &s, const ConvParams &p, const T *x, int64_
                      int64_t done_stride, const T *history, T *history_out, T *y, int64_t y_stride,
                      cudaStream_t stream)
 {
-    constexpr int V = 8 / sizeof(T);
-    if (s.channels % V == 0 && x_stride % V == 0 && y_stride % V == 0 && fits(x, 8) && fits(y, 8) &&
-        fits(history, 8) && fits(history_out, 8)) {
+    constexpr int V = 4;
+    constexpr size_t kBytes = V * sizeof(T);
+    if (s.channels % V == 0 && x_stride % V == 0 && y_stride % V == 0 && fits(x, kBytes) && fits(y, kBytes) &&
+        fits(history, kBytes) && fits(history_out, kBytes)) {
         const unsigned blocks = blocks_for(s.batch * (s.channels / V));
         SSM_BY_WIDTH(k_conv_step, T, V, blocks, s, p, x, x_stride, done, done_stride, history, history_out, y, y_stride);
     } else {
