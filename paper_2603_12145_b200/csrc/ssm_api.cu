@@ -39,17 +39,16 @@ bool sizes_ok(int64_t batch, int64_t time)
     return batch >= 1 && time >= 1 && batch <= kMaxBlocks && time <= kMaxBlocks / 2;
 }
 
-// The cut of the time axis.  One segment costs one pass over its steps; several cost two passes,
-// the first of them shorter (no output), so the cut pays where the rows alone leave more than half of the
-// device idle.  `fill` blocks keep it busy.
-void cut_time(ScanShape &s, int64_t blocks_per_segment, int64_t fill)
+// The cut of the time axis.  One segment costs one pass over its steps, several cost two, so the cut pays
+// where the rows alone occupy less than half of the `resident` blocks that the device holds; the
+// segments are then as many as fit at once, since a block more would double the time.
+void cut_time(ScanShape &s, int64_t blocks_per_segment, int64_t resident)
 {
     s.segments = 1;
     s.segment_steps = s.chunks * kScanChunk;
-    if (2 * blocks_per_segment > fill || s.chunks < 2) return;
-    const int64_t wanted = div_up(2 * fill, blocks_per_segment);
-    const int64_t segments = wanted < s.chunks ? wanted : s.chunks;
-    const int per = static_cast<int>(div_up(s.chunks, segments));
+    const int64_t most = resident / blocks_per_segment;
+    if (most < 2 || s.chunks < 2) return;
+    const int per = static_cast<int>(div_up(s.chunks, most < s.chunks ? most : s.chunks));
     s.segments = static_cast<int>(div_up(s.chunks, per));
     s.segment_steps = per * kScanChunk;
 }
@@ -67,7 +66,8 @@ ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
     s.chunks = static_cast<int>(div_up(time, kScanChunk));
     const int64_t per_block = backward ? 128 : 128 / lanes_of(p->states);
     const int64_t tiles = div_up(s.group_channels, per_block) * s.groups;
-    cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * (backward ? 2 : 3));
+    // blocks per SM by registers (see the kernels' launch bounds)
+    cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * (backward ? 2 : lanes_of(p->states) == 1 ? 4 : 3));
     s.slots = 1;
     if (backward) {
         // about four rounds of resident blocks, each with the same number of rows

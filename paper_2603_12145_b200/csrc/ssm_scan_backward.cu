@@ -216,13 +216,13 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
             const int groups = (steps + kGroup - 1) / kGroup;
             float4 hv[4];
             if (SB == 1) load_saved(hv, p, s, b, chunk, quad, d0 + ch, live4);
-            T bc[kStage];
+            uint32_t bc[kStage];
 #pragma unroll
             for (int i = 0; i < kStage; ++i) {
                 const int at = i * kThreads + tid;
                 const int k = at / (2 * NS), n = at % NS;
                 const Seq<const T> &src = (at / NS) & 1 ? q.c : q.b;
-                bc[i] = k < steps && n < s.states ? src.row(b, tc + k)[g * s.states + n] : from_f32<T>(0.0f);
+                bc[i] = k < steps && n < s.states ? load_bits(src.row(b, tc + k) + g * s.states + n) : 0;
             }
             uint32_t resets = 0;
             if (q.reset.ptr != nullptr)
@@ -230,49 +230,56 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
             if (chunk > c_first && live) {      // the chunk that follows: a lane asks for its row of two sequences
                 const int t = tc - kChunk + (lane & 15);
                 prefetch((lane < 16 ? q.x : q.dt).row(b, t) + d0);
+                if (lane < 16)      // and the first block of saved states: a line holds eight channels of a quad
+                    prefetch(reinterpret_cast<const float4 *>(p.saved) +
+                             ((b * s.chunks + chunk - 1) * s.quads + min(lane >> 2, s.quads - 1)) * s.channels + d0 +
+                             min(8 * (lane & 3), s.group_channels - local0 - 1));
                 prefetch((lane < 16 || !gated ? q.dy : q.z).row(b, t) + d0);
             }
             if (warp_live) {
+                // All of the chunk's loads first, none of them conditional (a value that may also be a constant
+                // would be waited for where the two meet): beyond the end the last step is read again, a lane without a channel
+                // reads the first one, and without a gate x stands in for z.
+                uint32_t x[kChunk], dt[kChunk], dy[kChunk], z[kChunk];
+                const Seq<const T> &sz = gated ? q.z : q.x;
                 const T *px = q.x.row(b, tc) + own, *pdt = q.dt.row(b, tc) + own, *pdy = q.dy.row(b, tc) + own;
-                const T *pz = gated ? q.z.row(b, tc) + own : nullptr;
+                const T *pz = sz.row(b, tc) + own;
 #pragma unroll
-                for (int k0 = 0; k0 < kChunk; k0 += 8) {
-                    T x[8], dt[8], dy[8], z[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const bool in = live && k0 + k < steps;
-                        x[k] = in ? *px : from_f32<T>(0.0f);
-                        dt[k] = in ? *pdt : from_f32<T>(0.0f);
-                        dy[k] = in ? *pdy : from_f32<T>(0.0f);
-                        z[k] = in && gated ? *pz : from_f32<T>(0.0f);
+                for (int k = 0; k < kChunk; ++k) {
+                    x[k] = load_bits(px);
+                    dt[k] = load_bits(pdt);
+                    dy[k] = load_bits(pdy);
+                    z[k] = load_bits(pz);
+                    if (k + 1 < steps) {
                         px += q.x.st;
                         pdt += q.dt.st;
                         pdy += q.dy.st;
-                        pz += q.z.st;
+                        pz += sz.st;
                     }
+                }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const bool in = live && k0 + k < steps;
-                        float *dst = s_scal + (k0 + k) * 32 + lane;
-                        const float xv = to_f32(x[k]), raw = to_f32(dt[k]) + bias, dyv = to_f32(dy[k]);
-                        const float delta = in ? softplus(raw) : 0.0f;
-                        dst[kDelta * kChunk * 32] = delta;
-                        dst[kDeltaX * kChunk * 32] = delta * xv;
-                        dst[kX * kChunk * 32] = xv;
-                        dst[kSig * kChunk * 32] = sigmoid(raw);
-                        if (gated) {
-                            const float zv = to_f32(z[k]), sz = sigmoid(zv);
-                            dst[kG * kChunk * 32] = dyv * zv * sz;
-                            dst[kW * kChunk * 32] = dyv * fmaf(zv * sz, 1.0f - sz, sz);
-                        } else {
-                            dst[kG * kChunk * 32] = dyv;
-                        }
+                for (int k = 0; k < kChunk; ++k) {
+                    float *dst = s_scal + k * 32 + lane;
+                    const bool in = live && k < steps;
+                    const float xv = in ? from_bits<T>(x[k]) : 0.0f, dyv = in ? from_bits<T>(dy[k]) : 0.0f;
+                    const float raw = from_bits<T>(dt[k]) + bias;
+                    const float delta = in ? softplus(raw) : 0.0f;
+                    dst[kDelta * kChunk * 32] = delta;
+                    dst[kDeltaX * kChunk * 32] = delta * xv;
+                    dst[kX * kChunk * 32] = xv;
+                    dst[kSig * kChunk * 32] = sigmoid(raw);
+                    if (gated) {
+                        const float zv = in ? from_bits<T>(z[k]) : 0.0f, sg = sigmoid(zv);
+                        dst[kG * kChunk * 32] = dyv * zv * sg;
+                        dst[kW * kChunk * 32] = dyv * fmaf(zv * sg, 1.0f - sg, sg);
+                    } else {
+                        dst[kG * kChunk * 32] = dyv;
                     }
                 }
             }
 #pragma unroll
             for (int i = 0; i < kStage; ++i) {
-                const float v = to_f32(bc[i]);
+                const float v = from_bits<T>(bc[i]);
                 *reinterpret_cast<float2 *>(s_bc + 2 * (i * kThreads + tid)) = make_float2(v, v);
             }
             __syncthreads();

@@ -89,7 +89,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     const bool gated = !kSummary && q.z.ptr != nullptr;
 
     // the next tile's values, in flight while the current one is worked on
-    T nx[kTile], ndt[kTile], nz[kTile], nbc[kStage];
+    uint32_t nx[kTile], ndt[kTile], nz[kTile], nbc[kStage];
     uint8_t nreset = 0;
     const T *px = q.x.row(b, t0) + d, *pdt = q.dt.row(b, t0) + d, *pz = gated ? q.z.row(b, t0) + d : nullptr;
     T *py = kSummary ? nullptr : q.y.row(b, t0) + d;
@@ -105,12 +105,12 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
 #pragma unroll
             for (int k = 0; k < kTile; ++k) {
                 const bool in = live && t + k < t1;
-                nx[k] = in ? *px : from_f32<T>(0.0f);
-                ndt[k] = in ? *pdt : from_f32<T>(0.0f);
+                nx[k] = in ? load_bits(px) : 0;
+                ndt[k] = in ? load_bits(pdt) : 0;
                 px += q.x.st;
                 pdt += q.dt.st;
                 if (!kSummary) {
-                    nz[k] = in && gated ? *pz : from_f32<T>(0.0f);
+                    nz[k] = in && gated ? load_bits(pz) : 0;
                     pz += q.z.st;
                 }
             }
@@ -119,7 +119,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
         for (int k = 0; k < kStage; ++k) {
             const int i = k * kThreads + tid;
             const int64_t st = (i / NS) % (kWidth / NS) == 0 ? q.b.st : q.c.st;
-            nbc[k] = pbc[k] != nullptr && t + i / kWidth < t1 ? *pbc[k] : from_f32<T>(0.0f);
+            nbc[k] = pbc[k] != nullptr && t + i / kWidth < t1 ? load_bits(pbc[k]) : 0;
             if (pbc[k] != nullptr) pbc[k] += kTile * st;
         }
         if (tid < kTile) nreset = q.reset.ptr != nullptr && t + tid < t1 ? *q.reset.row(b, t + tid) : 0;
@@ -135,17 +135,17 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
             // past the end: delta = 0 leaves the state as it is
-            delta[k] = t + k < t1 ? softplus(to_f32(ndt[k]) + bias) : 0.0f;
-            xv[k] = to_f32(nx[k]);
+            delta[k] = t + k < t1 ? softplus(from_bits<T>(ndt[k]) + bias) : 0.0f;
+            xv[k] = from_bits<T>(nx[k]);
             if (!kSummary) {
-                const float z = to_f32(nz[k]);
+                const float z = from_bits<T>(nz[k]);
                 gate[k] = gated ? z * sigmoid(z) : 1.0f;
             }
         }
 #pragma unroll
         for (int k = 0; k < kStage; ++k) {
             const int i = k * kThreads + tid;
-            if (i < kTile * kWidth) (&s_bc[buf][0][0])[i] = to_f32(nbc[k]);
+            if (i < kTile * kWidth) (&s_bc[buf][0][0])[i] = from_bits<T>(nbc[k]);
         }
         if (tid < kTile) s_reset[buf][tid] = nreset;
         __syncthreads();
