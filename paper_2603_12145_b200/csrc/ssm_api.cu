@@ -40,17 +40,27 @@ bool sizes_ok(int64_t batch, int64_t time)
 }
 
 // The cut of the time axis.  One segment costs one pass over its steps, several cost two, so the cut pays
-// where the rows alone occupy less than half of the `resident` blocks that the device holds; the
-// segments are then as many as fit at once, since a block more would double the time.
+// where the rows alone occupy less than half of the `resident` blocks that the device holds.  The
+// segments then fill one or a few whole rounds of resident blocks, whichever is the shortest.
 void cut_time(ScanShape &s, int64_t blocks_per_segment, int64_t resident)
 {
     s.segments = 1;
     s.segment_steps = s.chunks * kScanChunk;
-    const int64_t most = resident / blocks_per_segment;
-    if (most < 2 || s.chunks < 2) return;
-    const int per = static_cast<int>(div_up(s.chunks, most < s.chunks ? most : s.chunks));
-    s.segments = static_cast<int>(div_up(s.chunks, per));
-    s.segment_steps = per * kScanChunk;
+    if (resident / blocks_per_segment < 2 || s.chunks < 2) return;
+    int64_t best = -1;
+    int best_per = s.chunks;
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+        const int64_t most = rounds * resident / blocks_per_segment;
+        const int64_t per = div_up(s.chunks, most < s.chunks ? most : s.chunks);
+        const int64_t taken = div_up(div_up(s.chunks, per) * blocks_per_segment, resident);
+        const int64_t cost = taken * (4 * per + 1);      // a block's start and end: about a quarter of a chunk
+        if (best < 0 || cost < best) {
+            best = cost;
+            best_per = static_cast<int>(per);
+        }
+    }
+    s.segments = static_cast<int>(div_up(s.chunks, best_per));
+    s.segment_steps = best_per * kScanChunk;
 }
 
 ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
@@ -66,8 +76,10 @@ ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
     s.chunks = static_cast<int>(div_up(time, kScanChunk));
     const int64_t per_block = backward ? 128 : 128 / lanes_of(p->states);
     const int64_t tiles = div_up(s.group_channels, per_block) * s.groups;
-    // blocks per SM by registers (see the kernels' launch bounds)
-    cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * (backward ? 2 : lanes_of(p->states) == 1 ? 4 : 3));
+    // resident blocks per SM: by registers, beyond 16 states backward by shared memory
+    const int lanes = lanes_of(p->states);
+    const int per_sm = backward ? (lanes == 1 ? 2 : 1) : (lanes == 1 ? 4 : 3);
+    cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * per_sm);
     s.slots = 1;
     if (backward) {
         // about four rounds of resident blocks, each with the same number of rows

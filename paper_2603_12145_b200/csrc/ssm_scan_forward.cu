@@ -265,86 +265,113 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
 constexpr int kStepThreads = 256;
 constexpr int kStepRows = 4;    // rows whose states are in flight together
 
+// Four neighbouring elements of a row of b or c, as they lie in memory.
+template <typename T>
+struct alignas(4 * sizeof(T)) Four {
+    T e[4];
+};
+
+// kAligned: states, rows of b and c come in whole, aligned quads.
 template <typename T, int LPC, bool kAligned>
-__global__ void __launch_bounds__(kStepThreads)
+__global__ void __launch_bounds__(kStepThreads, 3)
 k_scan_step(const StepParams p, const T *__restrict__ x, const T *__restrict__ dt, const T *__restrict__ z,
             const T *__restrict__ bv, const T *__restrict__ cv, T *__restrict__ y, const int rows_per_block)
 {
     constexpr int kChannels = kStepThreads / LPC;
     const int part = threadIdx.x % LPC;
     const int c0 = blockIdx.x * kChannels + threadIdx.x / LPC;
-    const bool live = c0 < p.channels;
-    const int d = live ? c0 : p.channels - 1;
-    const int g = d / p.group_channels;
     const int n0 = 4 * part;
+    const bool live = c0 < p.channels;
+    const bool holds = live && n0 < p.states;          // the thread has states
+    const int d = live ? c0 : 0;
+    const int g = d / p.group_channels;
     float a2[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-        a2[e] = n0 + e < p.states ? p.a[static_cast<int64_t>(d) * p.states + n0 + e] * kLog2e : 0.0f;
+        a2[e] = holds && n0 + e < p.states ? p.a[static_cast<int64_t>(d) * p.states + n0 + e] * kLog2e : 0.0f;
     const float bias = p.dt_bias != nullptr ? p.dt_bias[d] : 0.0f;
     const float skip = p.d != nullptr ? p.d[d] : 0.0f;
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * rows_per_block;
     const int64_t r1 = r0 + rows_per_block < p.n ? r0 + rows_per_block : p.n;
+    const int64_t state_row = static_cast<int64_t>(p.channels) * p.states;
     for (int64_t r = r0; r < r1; r += kStepRows) {
-        float h[kStepRows][4];
-        float xv[kStepRows], dv[kStepRows], zv[kStepRows], bb[kStepRows][4], cc[kStepRows][4];
+        // all loads of the rows first
+        float4 h[kStepRows];
+        uint32_t xv[kStepRows], dv[kStepRows], zv[kStepRows];
+        Four<T> bb[kStepRows], cc[kStepRows];
+        uint8_t clear[kStepRows];
 #pragma unroll
         for (int k = 0; k < kStepRows; ++k) {
             const int64_t row = r + k < r1 ? r + k : r1 - 1;
-            const float *src = p.state + (row * p.channels + d) * p.states + n0;
-            const bool clear = p.done != nullptr && p.done[row * p.done_stride] != 0;
-            if (kAligned) {
-                const float4 v = n0 < p.states ? *reinterpret_cast<const float4 *>(src) : make_float4(0, 0, 0, 0);
-                h[k][0] = v.x;
-                h[k][1] = v.y;
-                h[k][2] = v.z;
-                h[k][3] = v.w;
-            } else {
+            const float *src = p.state + row * state_row + static_cast<int64_t>(d) * p.states + n0;
+            const T *b4 = bv + row * p.b_stride + g * p.states + n0, *c4 = cv + row * p.c_stride + g * p.states + n0;
+            h[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[k][e] = n0 + e < p.states ? src[e] : 0.0f;
-            }
-            if (clear) {
+            for (int e = 0; e < 4; ++e) bb[k].e[e] = cc[k].e[e] = from_f32<T>(0.0f);
+            if (holds) {
+                if (kAligned) {
+                    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(h[k].x), "=f"(h[k].y), "=f"(h[k].z), "=f"(h[k].w) : "l"(src));
+                    bb[k] = *reinterpret_cast<const Four<T> *>(b4);
+                    cc[k] = *reinterpret_cast<const Four<T> *>(c4);
+                } else {
+                    float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) h[k][e] = 0.0f;
+                    for (int e = 0; e < 4; ++e) {
+                        const bool in = n0 + e < p.states;
+                        v[e] = in ? src[e] : 0.0f;
+                        if (in) {
+                            bb[k].e[e] = b4[e];
+                            cc[k].e[e] = c4[e];
+                        }
+                    }
+                    h[k] = make_float4(v[0], v[1], v[2], v[3]);
+                }
             }
-            xv[k] = to_f32(x[row * p.x_stride + d]);
-            dv[k] = to_f32(dt[row * p.dt_stride + d]);
-            zv[k] = z != nullptr ? to_f32(z[row * p.z_stride + d]) : 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool in = n0 + e < p.states;
-                bb[k][e] = in ? to_f32(bv[row * p.b_stride + g * p.states + n0 + e]) : 0.0f;
-                cc[k][e] = in ? to_f32(cv[row * p.c_stride + g * p.states + n0 + e]) : 0.0f;
-            }
+            clear[k] = p.done != nullptr ? p.done[row * p.done_stride] : 0;
+            xv[k] = load_bits(x + row * p.x_stride + d);
+            dv[k] = load_bits(dt + row * p.dt_stride + d);
+            zv[k] = z != nullptr ? load_bits(z + row * p.z_stride + d) : 0;
         }
 #pragma unroll
         for (int k = 0; k < kStepRows; ++k) {
-            const float delta = softplus(dv[k] + bias);
-            const float dx = delta * xv[k];
+            if (clear[k]) h[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            const float delta = softplus(from_bits<T>(dv[k]) + bias), xf = from_bits<T>(xv[k]);
+            const float dx = delta * xf;
+            float v[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
             float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                h[k][e] = fmaf(ex2(delta * a2[e]), h[k][e], dx * bb[k][e]);
-                sum = fmaf(cc[k][e], h[k][e], sum);
+                v[e] = fmaf(ex2(delta * a2[e]), v[e], dx * to_f32(bb[k].e[e]));
+                sum = fmaf(to_f32(cc[k].e[e]), v[e], sum);
             }
 #pragma unroll
             for (int m = 1; m < LPC; m *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-            sum = fmaf(skip, xv[k], sum);
-            if (z != nullptr) sum *= zv[k] * sigmoid(zv[k]);
+            sum = fmaf(skip, xf, sum);
+            if (z != nullptr) {
+                const float zf = from_bits<T>(zv[k]);
+                sum *= zf * sigmoid(zf);
+            }
             if (live && r + k < r1) {
                 const int64_t row = r + k;
-                float *dst = p.state_out + (row * p.channels + d) * p.states + n0;
+                float *dst = p.state_out + row * state_row + static_cast<int64_t>(d) * p.states + n0;
                 if (kAligned) {
-                    if (n0 < p.states) *reinterpret_cast<float4 *>(dst) = make_float4(h[k][0], h[k][1], h[k][2], h[k][3]);
+                    if (holds) *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (n0 + e < p.states) dst[e] = h[k][e];
+                        if (n0 + e < p.states) dst[e] = v[e];
                 }
                 if (part == 0) y[row * p.y_stride + d] = from_f32<T>(sum);
             }
         }
     }
+}
+
+template <typename T>
+bool whole_quads(const T *ptr, int64_t stride)
+{
+    return reinterpret_cast<uintptr_t>(ptr) % (4 * sizeof(T)) == 0 && stride % 4 == 0;
 }
 
 template <typename T, int LPC>
@@ -360,7 +387,7 @@ int launch_step(const StepParams &p, const T *x, const T *dt, const T *z, const 
     if (chunks > 65535) chunks = 65535;
     const int64_t rows = (p.n + chunks - 1) / chunks;
     const dim3 grid(tiles, static_cast<unsigned>((p.n + rows - 1) / rows));
-    if (p.states % 4 == 0)
+    if (p.states % 4 == 0 && whole_quads(b, p.b_stride) && whole_quads(c, p.c_stride))
         k_scan_step<T, LPC, true><<<grid, kStepThreads, 0, stream>>>(p, x, dt, z, b, c, y, static_cast<int>(rows));
     else
         k_scan_step<T, LPC, false><<<grid, kStepThreads, 0, stream>>>(p, x, dt, z, b, c, y, static_cast<int>(rows));
