@@ -16,8 +16,8 @@
  *
  * Types.  Everything the caller passes is bfloat16 or binary16, one type per handle.
  * Products run on the tensor cores and accumulate in binary32.  Rounded to the type:
- * results; hidden (an operand of the second product); with a backward pass also g and u
- * (`pre`) and dg and du, which are operands of the products of the backward pass.  The
+ * results; hidden, dg and du, which are operands of further products.  g and u are kept
+ * for the backward pass (`pre`) with the upper 24 bits of their binary32 values.  The
  * activation and its slope are binary32; hidden comes from the unrounded g and u.  The
  * accumulation order inside the tensor cores is not specified; the same call gives the
  * same bits.
@@ -64,8 +64,11 @@ int gated_ffn_set_stream(gated_ffn *p, void *cuda_stream);
 /* Scratch of a forward (backward = 0) or backward (backward = 1) call on n rows. */
 size_t gated_ffn_workspace_bytes(const gated_ffn *p, int64_t n, int backward);
 
-/* hidden[n][hidden] and, if there will be a backward pass, pre[n][2 * hidden] (else NULL) are
- * written: the backward call reads both.  n >= 1. */
+/* Bytes of `pre` for n rows: g and u in a layout of the library's own. */
+size_t gated_ffn_pre_bytes(const gated_ffn *p, int64_t n);
+
+/* hidden[n][hidden] and, if there will be a backward pass, pre (else NULL) are written: the backward
+ * call reads both, with the same n.  n >= 1. */
 int gated_ffn_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in, const void *w_out,
                       void *pre, void *hidden, void *y, int64_t y_stride, void *workspace,
                       size_t workspace_bytes, int64_t n);

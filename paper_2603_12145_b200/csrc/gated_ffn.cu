@@ -13,14 +13,23 @@
 //   kSlope    backward: D = dy W_out; the epilogue reads g and u and writes dg and du.
 //   kStore    the remaining products.
 //
+// A thread's accumulators are one row of the tile, so that its own stores would touch a line each.
+// kGated and kSlope move several times the bytes of their accumulators: there every warp passes
+// blocks of 32 rows x 32 columns through shared memory (swizzled, no bank conflicts) and TMA
+// copies them out, and g and u in.
+//
+// g and u are kept for the backward pass as the upper 24 bits of their binary32 values, in a plane of 16
+// and a plane of 8 bits: rounded to the type they would add an error as large as the result's own
+// rounding to dx and dW_in.
+//
 // Operands lie in memory as they are: where the reduction runs along rows (W_in in dx, W_out in
 // dhidden, both operands of a weight gradient) TMA brings boxes of 64 elements of the row by 64
 // reduction rows and the instruction reads them MN-major; nothing is transposed.
 //
-// Work of kStore: whole rounds of tiles, one tile per pair, and then the tiles of the last one to
-// two rounds as one stretch of 64-element steps cut evenly over the pairs, so that all pairs
-// finish together whatever the number of tiles; a tile that a cut divides goes to scratch in
-// binary32 and k_join adds its pieces in order.
+// Work of kStore: whole rounds of tiles, one tile per pair; the tiles of a last, incomplete round
+// are one stretch of 64-element steps cut evenly over the pairs, so that all pairs finish together
+// whatever the number of tiles; a tile that a cut divides goes to scratch in binary32 and k_join
+// adds its pieces in order.
 //
 // k_rows: up to 32 rows of x, bound by reading the weights.  A block owns 16 rows of the weights
 // (of each projection), its warps split the reduction, and each lane's 16-byte loads of the
@@ -40,7 +49,7 @@ namespace {
 constexpr int kBK = 64;                          // reduction elements per stage
 constexpr int kRowsPerBlock = 128;               // rows of A per block; a pair's tile has twice as many
 constexpr int kTileM = 2 * kRowsPerBlock;
-constexpr int kStages = 6;
+constexpr int kStagesMost = 6;
 constexpr int kABytes = kRowsPerBlock * kBK * 2;
 constexpr int kBBytes = 128 * kBK * 2;           // at most 128 rows of B per block
 constexpr int kStageBytes = kABytes + kBBytes;
@@ -48,10 +57,28 @@ constexpr int kAccCols = 256;
 constexpr int kTmemCols = 2 * kAccCols;
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-constexpr int kSmemBytes = kStages * kStageBytes + 256 + 1024;
+constexpr int kBarrierBytes = 512;
 constexpr int kMinSteps = 4;                     // a piece of a divided tile is at least this long
 
 enum Mode { kStore, kGated, kSlope };
+
+// A block of 32 rows x 32 columns on its way between registers and memory: 16-bit elements 64 bytes per row
+// (64-byte swizzle), 8-bit elements 32 bytes per row (32-byte swizzle).
+constexpr int kBlock16 = 32 * 64;
+constexpr int kBlock8 = 32 * 32;
+constexpr int kPreBytes = 2 * kBlock16 + 2 * kBlock8;    // g and u: upper planes, then lower planes
+
+// Stages of the ring and staging bytes per epilogue warp: kGated holds g and u and the hidden units, kSlope
+// two sets of g and u (one on its way in, one worked on and then overwritten with dg and du).
+__host__ __device__ constexpr int stages_of(int mode) { return mode == kStore ? 6 : mode == kGated ? 5 : 4; }
+__host__ __device__ constexpr int staging_of(int mode) { return mode == kStore ? 0 : mode == kGated ? kPreBytes + kBlock16 : 2 * kPreBytes; }
+__host__ __device__ constexpr int smem_of(int mode)
+{
+    return stages_of(mode) * kStageBytes + kEpilogueWarps * staging_of(mode) + kBarrierBytes + 1024;
+}
+static_assert(smem_of(kStore) <= 227 * 1024 && smem_of(kGated) <= 227 * 1024 && smem_of(kSlope) <= 227 * 1024,
+              "shared memory of a block");
+static_assert(kPreBytes % 1024 == 0 && (kPreBytes + kBlock16) % 1024 == 0, "swizzled blocks need their alignment");
 
 template <typename T>
 struct Type;
@@ -105,9 +132,9 @@ struct Product {
     int steps;              // ceil(k / 64)
     int rounds;             // whole rounds of tiles
     int cuts;               // pairs that share the rest (0: none)
-    void *out;              // kStore: D; kGated: hidden; kSlope: [dg | du]
+    void *out;              // kStore: D
     int64_t out_stride;
-    void *pre;              // kGated: [g | u] or nullptr; kSlope: [g | u], read
+    int keep;               // kGated: write g and u
     float *pieces;          // [cuts][2][256][256]
     int gelu;
     int *err;
@@ -167,35 +194,104 @@ __device__ __forceinline__ void store16(void *row, int c, int width, const uint3
     if (c + 8 < width) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-__device__ __forceinline__ void load16(const void *row, int c, int width, uint32_t (&w)[8])
+// The lane's row of a staged block: 16-byte piece i.
+__device__ __forceinline__ uint32_t piece16(uint32_t block, int lane, int i) { return block + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4); }
+__device__ __forceinline__ uint32_t piece8(uint32_t block, int lane, int i) { return block + lane * 32 + ((i ^ ((lane >> 2) & 1)) << 4); }
+
+__device__ __forceinline__ void put(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
-    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(row) + c);
-    const uint4 a = c < width ? __ldg(src) : make_uint4(0, 0, 0, 0);
-    const uint4 b = c + 8 < width ? __ldg(src + 1) : make_uint4(0, 0, 0, 0);
-    w[0] = a.x;
-    w[1] = a.y;
-    w[2] = a.z;
-    w[3] = a.w;
-    w[4] = b.x;
-    w[5] = b.y;
-    w[6] = b.z;
-    w[7] = b.w;
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+
+__device__ __forceinline__ uint4 get(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Elements [8 i, 8 i + 8) of the lane's row, as the upper 24 bits of binary32 numbers in the two planes.
+__device__ __forceinline__ void put_upper(uint32_t block, int lane, int i, const uint32_t *v)
+{
+    put(piece16(block, lane, i), __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632),
+        __byte_perm(v[4], v[5], 0x7632), __byte_perm(v[6], v[7], 0x7632));
+}
+
+__device__ __forceinline__ uint32_t third_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __byte_perm(__byte_perm(a, b, 0x0051), __byte_perm(c, d, 0x0051), 0x5410);
+}
+
+// Element e (0..3) of a word pair of the upper plane and a word of the lower one.
+__device__ __forceinline__ float join24(uint32_t upper, uint32_t lower, int e)
+{
+    // result bytes, low to high: 0, lower[e], the two bytes of upper's half e & 1
+    const uint32_t shifted = __byte_perm(lower, 0, 0x4404 | (e << 4));           // 0, lower[e], 0, 0
+    return __uint_as_float(__byte_perm(shifted, upper, e & 1 ? 0x7610 : 0x5410));
+}
+
+// A block of one plane (0: g, 1: u) of a [rows][2][columns] array, with this block's own barrier.
+__device__ __forceinline__ void tma_load_plane(uint32_t dst, const CUtensorMap *map, int x, int plane, int y, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(plane), "r"(y), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_store_plane(const CUtensorMap *map, int x, int plane, int y, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x),
+                 "r"(plane), "r"(y), "r"(src)
+                 : "memory");
+}
+
+// 8 consecutive accumulator columns of this thread's lane.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x),
+                 "r"(y), "r"(src)
+                 : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// The copies' reads of shared memory are done.
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// The memory that the epilogues of kGated and kSlope reach by TMA.  [g | u] and [dg | du] are [rows][2][hidden]
+// to the copies: a block at the last columns of one projection must not run into the other.
+struct Maps {
+    CUtensorMap out;            // kGated: hidden units [rows][hidden]; kSlope: [dg | du]
+    CUtensorMap upper, lower;   // planes of [g | u]
+};
 
 template <typename T, int kMode>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
-          const __grid_constant__ Product p)
+          const __grid_constant__ Maps maps, const __grid_constant__ Product p)
 {
+    constexpr int kStages = stages_of(kMode);
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t tiles = (raw + 1023u) & ~1023u;
-    const uint32_t bars = tiles + kStages * kStageBytes;
+    const uint32_t staging = tiles + kStages * kStageBytes;
+    const uint32_t bars = staging + kEpilogueWarps * staging_of(kMode);
     uint8_t *bars_ptr = smem_raw + (bars - raw);
     const uint32_t full0 = bars, empty0 = bars + 8 * kStages;
-    const uint32_t acc_full0 = bars + 16 * kStages, acc_empty0 = acc_full0 + 16;
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars_ptr + 16 * kStages + 32);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(bars_ptr + 16 * kStages + 40);
+    const uint32_t acc_full0 = bars + 16 * kStagesMost, acc_empty0 = acc_full0 + 16;
+    const uint32_t pre_full0 = acc_empty0 + 16;              // two per epilogue warp (kSlope)
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars_ptr + 16 * kStagesMost + 32 + 128);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(bars_ptr + 16 * kStagesMost + 32 + 128 + 8);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_cta_rank();
@@ -212,6 +308,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             mbar_init(acc_full0 + 8 * b, 1);
             mbar_init(acc_empty0 + 8 * b, 2 * kEpilogueWarps);
         }
+        for (int i = 0; i < 2 * kEpilogueWarps; ++i) mbar_init(pre_full0 + 8 * i, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -308,65 +405,131 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
         const int q = warp & 3;
         const int half = (warp - 2) >> 2;                // which half of the columns
         const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
+        const uint32_t stage = staging + (warp - 2) * staging_of(kMode);
+        const uint32_t pre_full = pre_full0 + 16 * (warp - 2);
+        uint32_t pre_phase = 0;                          // bit b: parity of the next arrival in buffer b
         int it = 0;
         for (Walk w(p, pair, pairs); w.next(); ++it) {
             const uint32_t buf = it & 1, use = (it >> 1) & 1;
+            const int row_in_block = q * 32 + lane;
+            const int64_t row = static_cast<int64_t>(w.row_tile()) * kTileM + static_cast<int>(rank) * kRowsPerBlock + row_in_block;
+            const int row0 = static_cast<int>(row) - lane;   // the warp's first row
+            const bool live = row < p.m;
+            const uint32_t t0 = lane_base + buf * kAccCols;
+            // kSlope: set i of the tile's four, columns [f, f + 32) of g and u, into buffer i & 1
+            auto bring = [&](int i) {
+                const int f = w.col_tile() * tile_n + half * (tile_n / 2) + 32 * i;
+                const uint32_t dst = stage + (i & 1) * kPreBytes, bar = pre_full + 8 * (i & 1);
+                mbar_expect_tx(bar, kPreBytes);
+                tma_load_plane(dst, &maps.upper, f, 0, row0, bar);
+                tma_load_plane(dst + kBlock16, &maps.upper, f, 1, row0, bar);
+                tma_load_plane(dst + 2 * kBlock16, &maps.lower, f, 0, row0, bar);
+                tma_load_plane(dst + 2 * kBlock16 + kBlock8, &maps.lower, f, 1, row0, bar);
+            };
+            if (kMode == kSlope && lane == 0) {
+                bulk_wait_read();                        // both buffers: the previous tile's results have left
+                bring(0);
+                bring(1);
+            }
             const bool ready = mbar_wait(acc_full0 + 8 * buf, use, abort_flag);
             if (!__all_sync(0xFFFFFFFFu, ready)) break;
             tc_fence_after_sync();
-            const int row_in_block = q * 32 + lane;
-            const int64_t row = static_cast<int64_t>(w.row_tile()) * kTileM + static_cast<int>(rank) * kRowsPerBlock + row_in_block;
-            const bool live = row < p.m;
-            const uint32_t t0 = lane_base + buf * kAccCols;
             if (kMode == kGated) {
-                const int f0 = w.col_tile() * 128;
-                uint16_t *hrow = static_cast<uint16_t *>(p.out) + (live ? row : 0) * p.out_stride;
-                uint16_t *prow = static_cast<uint16_t *>(p.pre) + (live ? row : 0) * 2 * p.n;
 #pragma unroll 1
-                for (int c = half * 64; c < half * 64 + 64; c += 16) {
-                    uint32_t g[16], u[16];
-                    tmem_ld16(t0 + c, g);
-                    tmem_ld16(t0 + 128 + c, u);
-                    tmem_wait_ld();
-                    uint32_t hw[8], gw[8], uw[8];
+                for (int c = half * 64; c < half * 64 + 64; c += 32) {
+                    const int f = w.col_tile() * 128 + c;
+                    if (lane == 0) bulk_wait_read();     // the blocks staged before have left
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float g0 = __uint_as_float(g[2 * i]), g1 = __uint_as_float(g[2 * i + 1]);
-                        const float u0 = __uint_as_float(u[2 * i]), u1 = __uint_as_float(u[2 * i + 1]);
-                        hw[i] = Type<T>::pack(g0 * act_sigmoid(g0, p.gelu) * u0, g1 * act_sigmoid(g1, p.gelu) * u1);
-                        gw[i] = Type<T>::pack(g0, g1);
-                        uw[i] = Type<T>::pack(u0, u1);
-                    }
-                    if (live) {
-                        store16(hrow, f0 + c, p.n, hw);
-                        if (p.pre != nullptr) {
-                            store16(prow, f0 + c, p.n, gw);
-                            store16(prow + p.n, f0 + c, p.n, uw);
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t g[16], u[16], hw[8];
+                        tmem_ld16(t0 + c + 16 * h, g);
+                        tmem_ld16(t0 + 128 + c + 16 * h, u);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float g0 = __uint_as_float(g[2 * i]), g1 = __uint_as_float(g[2 * i + 1]);
+                            const float u0 = __uint_as_float(u[2 * i]), u1 = __uint_as_float(u[2 * i + 1]);
+                            hw[i] = Type<T>::pack(g0 * act_sigmoid(g0, p.gelu) * u0, g1 * act_sigmoid(g1, p.gelu) * u1);
                         }
+                        put(piece16(stage + kPreBytes, lane, 2 * h), hw[0], hw[1], hw[2], hw[3]);
+                        put(piece16(stage + kPreBytes, lane, 2 * h + 1), hw[4], hw[5], hw[6], hw[7]);
+                        if (p.keep) {
+                            put_upper(stage, lane, 2 * h, g);
+                            put_upper(stage, lane, 2 * h + 1, g + 8);
+                            put_upper(stage + kBlock16, lane, 2 * h, u);
+                            put_upper(stage + kBlock16, lane, 2 * h + 1, u + 8);
+                            put(piece8(stage + 2 * kBlock16, lane, h), third_bytes(g[0], g[1], g[2], g[3]),
+                                third_bytes(g[4], g[5], g[6], g[7]), third_bytes(g[8], g[9], g[10], g[11]),
+                                third_bytes(g[12], g[13], g[14], g[15]));
+                            put(piece8(stage + 2 * kBlock16 + kBlock8, lane, h), third_bytes(u[0], u[1], u[2], u[3]),
+                                third_bytes(u[4], u[5], u[6], u[7]), third_bytes(u[8], u[9], u[10], u[11]),
+                                third_bytes(u[12], u[13], u[14], u[15]));
+                        }
+                    }
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0 && f < p.n && row0 < p.m) {
+                        tma_store(&maps.out, f, row0, stage + kPreBytes);
+                        if (p.keep) {
+                            tma_store_plane(&maps.upper, f, 0, row0, stage);
+                            tma_store_plane(&maps.upper, f, 1, row0, stage + kBlock16);
+                            tma_store_plane(&maps.lower, f, 0, row0, stage + 2 * kBlock16);
+                            tma_store_plane(&maps.lower, f, 1, row0, stage + 2 * kBlock16 + kBlock8);
+                        }
+                        bulk_commit();
                     }
                 }
             } else if (kMode == kSlope) {
-                const int f0 = w.col_tile() * tile_n;
-                const uint16_t *prow = static_cast<const uint16_t *>(p.pre) + (live ? row : 0) * 2 * p.n;
-                uint16_t *orow = static_cast<uint16_t *>(p.out) + (live ? row : 0) * p.out_stride;
+                const int sets = tile_n / 64;
 #pragma unroll 1
-                for (int c = half * (tile_n / 2); c < (half + 1) * (tile_n / 2); c += 16) {
-                    uint32_t d[16], gw[8], uw[8];
-                    tmem_ld16(t0 + c, d);
-                    load16(prow, live ? f0 + c : p.n, p.n, gw);
-                    load16(prow + p.n, live ? f0 + c : p.n, p.n, uw);
-                    tmem_wait_ld();
+                for (int i = 0; i < sets; ++i) {
+                    const int c = half * (tile_n / 2) + 32 * i, f = w.col_tile() * tile_n + c;
+                    const uint32_t pre = stage + (i & 1) * kPreBytes;
+                    const bool here = mbar_wait(pre_full + 8 * (i & 1), (pre_phase >> (i & 1)) & 1, abort_flag);
+                    pre_phase ^= 1u << (i & 1);
+                    if (!__all_sync(0xFFFFFFFFu, here)) break;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float2 g = Type<T>::unpack(gw[i]), u = Type<T>::unpack(uw[i]);
-                        const float d0 = __uint_as_float(d[2 * i]), d1 = __uint_as_float(d[2 * i + 1]);
-                        const float s0 = act_sigmoid(g.x, p.gelu), s1 = act_sigmoid(g.y, p.gelu);
-                        gw[i] = Type<T>::pack(d0 * u.x * act_slope(g.x, s0, p.gelu), d1 * u.y * act_slope(g.y, s1, p.gelu));
-                        uw[i] = Type<T>::pack(d0 * g.x * s0, d1 * g.y * s1);
+                    for (int h = 0; h < 4; ++h) {        // 8 columns at a time
+                        uint32_t d[8];
+                        tmem_ld8(t0 + c + 8 * h, d);
+                        const uint4 gu = get(piece16(pre, lane, h)), uu = get(piece16(pre + kBlock16, lane, h));
+                        const uint4 gl4 = get(piece8(pre + 2 * kBlock16, lane, h >> 1));
+                        const uint4 ul4 = get(piece8(pre + 2 * kBlock16 + kBlock8, lane, h >> 1));
+                        const uint32_t gw[4] = {gu.x, gu.y, gu.z, gu.w}, uw[4] = {uu.x, uu.y, uu.z, uu.w};
+                        const uint32_t gl[2] = {h & 1 ? gl4.z : gl4.x, h & 1 ? gl4.w : gl4.y};
+                        const uint32_t ul[2] = {h & 1 ? ul4.z : ul4.x, h & 1 ? ul4.w : ul4.y};
+                        tmem_wait_ld();
+                        uint32_t og[4], ou[4];
+#pragma unroll
+                        for (int e = 0; e < 8; e += 2) {
+                            float dg[2], du[2];
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) {
+                                const float g = join24(gw[e / 2], gl[e / 4], (e + m) & 3);
+                                const float u = join24(uw[e / 2], ul[e / 4], (e + m) & 3);
+                                const float dh = __uint_as_float(d[e + m]), sg = act_sigmoid(g, p.gelu);
+                                dg[m] = dh * u * act_slope(g, sg, p.gelu);
+                                du[m] = dh * g * sg;
+                            }
+                            og[e / 2] = Type<T>::pack(dg[0], dg[1]);
+                            ou[e / 2] = Type<T>::pack(du[0], du[1]);
+                        }
+                        put(piece16(pre, lane, h), og[0], og[1], og[2], og[3]);
+                        put(piece16(pre + kBlock16, lane, h), ou[0], ou[1], ou[2], ou[3]);
                     }
-                    if (live) {
-                        store16(orow, f0 + c, p.n, gw);
-                        store16(orow + p.n, f0 + c, p.n, uw);
+                    fence_async();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (f < p.n && row0 < p.m) {
+                            tma_store_plane(&maps.out, f, 0, row0, pre);
+                            tma_store_plane(&maps.out, f, 1, row0, pre + kBlock16);
+                        }
+                        bulk_commit();
+                        if (i + 2 < sets) {              // into this buffer, a whole set ahead of its use
+                            bulk_wait_read();
+                            bring(i + 2);
+                        }
                     }
                 }
             } else if (w.piece >= 0) {
@@ -398,6 +561,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_rank(acc_empty0 + 8 * buf, 0));
         }
+        if (kMode != kStore && lane == 0) bulk_wait();
     }
 
     tc_fence_before_sync();
@@ -472,8 +636,11 @@ struct Rows {
     const void *x;
     int64_t x_stride;
     const void *w;              // kGated: [2 * width][k]; else [width][k]
-    void *out, *pre;
+    void *out;
     int64_t out_stride;
+    uint16_t *upper;            // kGated: planes of [g | u], or nullptr
+    uint8_t *lower;
+    int lower_width;
     int n, width, k;            // rows of x, rows of w (one projection), reduction length
     int gelu;
 };
@@ -549,10 +716,13 @@ k_rows(const Rows p)
         T *out = static_cast<T *>(p.out) + r * p.out_stride + f0 + f;
         if constexpr (kGatedRows) {
             *out = static_cast<T>(v[0] * act_sigmoid(v[0], p.gelu) * v[1]);
-            if (p.pre != nullptr) {
-                T *pre = static_cast<T *>(p.pre) + static_cast<int64_t>(r) * 2 * p.width + f0 + f;
-                pre[0] = static_cast<T>(v[0]);
-                pre[p.width] = static_cast<T>(v[1]);
+            if (p.upper != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t bits = __float_as_uint(v[e]);
+                    p.upper[(static_cast<int64_t>(r) * 2 + e) * p.width + f0 + f] = static_cast<uint16_t>(bits >> 16);
+                    p.lower[(static_cast<int64_t>(r) * 2 + e) * p.lower_width + f0 + f] = static_cast<uint8_t>(bits >> 8);
+                }
             }
         } else {
             *out = static_cast<T>(v[0]);
@@ -574,6 +744,35 @@ bool encode(CUtensorMapDataType type, CUtensorMap *m, const void *base, int64_t 
                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// [rows][2][cols] seen by copies of 32 columns of one plane x 32 rows.  pitch: bytes between planes (a row is two).
+bool encode_planes(CUtensorMapDataType type, CUtensorMap *m, const void *base, int64_t rows, int64_t cols, int64_t pitch,
+                   CUtensorMapSwizzle swizzle)
+{
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), 2, static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(pitch), static_cast<cuuint64_t>(2 * pitch)};
+    const cuuint32_t box[3] = {32, 1, 32};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    return tensor_map_encoder()(m, type, 3, const_cast<void *>(base), dims, strides, box, elem_strides,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool encode_blocks(CUtensorMapDataType type, CUtensorMap *m, const void *base, int64_t rows, int64_t cols)
+{
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * 2};
+    const cuuint32_t box[2] = {32, 32};
+    const cuuint32_t elem_strides[2] = {1, 1};
+    return tensor_map_encoder()(m, type, 2, const_cast<void *>(base), dims, strides, box, elem_strides,
+                                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// g and u as the caller keeps them: the upper planes [n][2][hidden] of 16 bits, then, 256-byte aligned, the
+// lower ones [n][2][hidden rounded up to 16] of 8 bits (the copies want rows of whole 16-byte pieces).
+int64_t lower_width(int hidden) { return (hidden + 15) / 16 * 16; }
+size_t upper_bytes(int64_t n, int hidden) { return (static_cast<size_t>(n) * hidden * 4 + 255) & ~static_cast<size_t>(255); }
 
 }  // namespace
 
@@ -618,17 +817,16 @@ Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
     q.m_first = q.m_tiles <= q.n_tiles;
     q.steps = static_cast<int>(div_up(k, kBK));
     const int64_t tiles = static_cast<int64_t>(q.m_tiles) * q.n_tiles;
-    if (mode != kStore) {
-        q.rounds = static_cast<int>(div_up(tiles, p->pairs));
-    } else {
-        q.rounds = static_cast<int>(tiles / p->pairs);
-        if (tiles % p->pairs != 0) {
-            if (q.rounds > 0) --q.rounds;
-            const int64_t rest = tiles - static_cast<int64_t>(q.rounds) * p->pairs;
-            int64_t cuts = rest * q.steps / kMinSteps;
-            if (cuts < rest) cuts = rest;
-            q.cuts = static_cast<int>(cuts < p->pairs ? cuts : p->pairs);
-        }
+    q.rounds = static_cast<int>(tiles / p->pairs);
+    const int64_t rest = tiles % p->pairs;
+    // an incomplete round is cut over all pairs unless it is nearly complete: joining pieces costs
+    // about a sixth of a round
+    if (rest > 0 && (mode != kStore || 6 * rest > 5 * p->pairs)) {
+        ++q.rounds;
+    } else if (rest > 0) {
+        int64_t cuts = rest * q.steps / kMinSteps;
+        if (cuts < rest) cuts = rest;
+        q.cuts = static_cast<int>(cuts < p->pairs ? cuts : p->pairs);
     }
     q.gelu = p->activation == GATED_FFN_GELU;
     q.err = p->err;
@@ -638,7 +836,7 @@ Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
 size_t pieces_bytes(const Product &q) { return static_cast<size_t>(q.cuts) * 2 * kTileM * kAccCols * sizeof(float); }
 
 template <typename T, int kMode>
-int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b)
+int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, const Maps &maps)
 {
     CUtensorMap tm_a, tm_b;
     const CUtensorMapDataType type = Type<T>::kMap;
@@ -659,7 +857,7 @@ int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.dynamicSmemBytes = smem_of(kMode);
     cfg.stream = p->stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -668,7 +866,7 @@ int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b)
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, k_product<T, kMode>, tm_a, tm_b, q) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, k_product<T, kMode>, tm_a, tm_b, maps, q) != cudaSuccess) {
         cudaGetLastError();
         return GATED_FFN_ECUDA;
     }
@@ -697,29 +895,64 @@ int launch_rows(gated_ffn *p, const Rows &r)
     return GATED_FFN_OK;
 }
 
+// The maps of kGated (out: hidden) and kSlope (out: [dg | du]).
+template <typename T>
+bool encode_maps(const gated_ffn *p, Maps *m, bool slope, void *out, const void *pre, int64_t n)
+{
+    const int64_t f = p->hidden;
+    bool ok = slope ? encode_planes(Type<T>::kMap, &m->out, out, n, f, 2 * f, CU_TENSOR_MAP_SWIZZLE_64B)
+                    : encode_blocks(Type<T>::kMap, &m->out, out, n, f);
+    if (pre != nullptr)
+        ok = ok && encode_planes(CU_TENSOR_MAP_DATA_TYPE_UINT16, &m->upper, pre, n, f, 2 * f, CU_TENSOR_MAP_SWIZZLE_64B) &&
+             encode_planes(CU_TENSOR_MAP_DATA_TYPE_UINT8, &m->lower, static_cast<const uint8_t *>(pre) + upper_bytes(n, p->hidden),
+                           n, f, lower_width(p->hidden), CU_TENSOR_MAP_SWIZZLE_32B);
+    return ok;
+}
+
 template <typename T>
 int run_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *pre,
                 void *hidden, void *y, int64_t y_stride, float *scratch, int64_t n)
 {
+    Maps maps = {};
     if (n <= kRowsMax) {
-        Rows r = {x, x_stride, w_in, hidden, pre, p->hidden, static_cast<int>(n), p->hidden, p->model,
-                  p->activation == GATED_FFN_GELU};
+        Rows r = {};
+        r.x = x;
+        r.x_stride = x_stride;
+        r.w = w_in;
+        r.out = hidden;
+        r.out_stride = p->hidden;
+        if (pre != nullptr) {
+            r.upper = static_cast<uint16_t *>(pre);
+            r.lower = static_cast<uint8_t *>(pre) + upper_bytes(n, p->hidden);
+            r.lower_width = static_cast<int>(lower_width(p->hidden));
+        }
+        r.n = static_cast<int>(n);
+        r.width = p->hidden;
+        r.k = p->model;
+        r.gelu = p->activation == GATED_FFN_GELU;
         const int rc = launch_rows<T, true>(p, r);
         if (rc != GATED_FFN_OK) return rc;
-        Rows s = {hidden, p->hidden, w_out, y, nullptr, y_stride, static_cast<int>(n), p->model, p->hidden, 0};
+        Rows s = {};
+        s.x = hidden;
+        s.x_stride = p->hidden;
+        s.w = w_out;
+        s.out = y;
+        s.out_stride = y_stride;
+        s.n = static_cast<int>(n);
+        s.width = p->model;
+        s.k = p->hidden;
         return launch_rows<T, false>(p, s);
     }
     Product q = plan(p, kGated, n, p->hidden, p->model);
-    q.out = hidden;
-    q.out_stride = p->hidden;
-    q.pre = pre;
-    const int rc = launch_product<T, kGated>(p, q, {x, x_stride, 0}, {w_in, p->model, 0});
+    q.keep = pre != nullptr;
+    if (!encode_maps<T>(p, &maps, false, hidden, pre, n)) return GATED_FFN_ECUDA;
+    const int rc = launch_product<T, kGated>(p, q, {x, x_stride, 0}, {w_in, p->model, 0}, maps);
     if (rc != GATED_FFN_OK) return rc;
     Product r = plan(p, kStore, n, p->model, p->hidden);
     r.out = y;
     r.out_stride = y_stride;
     r.pieces = scratch;
-    return launch_product<T, kStore>(p, r, {hidden, p->hidden, 0}, {w_out, p->hidden, 0});
+    return launch_product<T, kStore>(p, r, {hidden, p->hidden, 0}, {w_out, p->hidden, 0}, maps);
 }
 
 struct BackwardPlan {
@@ -753,25 +986,24 @@ int run_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const void *x,
     void *dpre = scratch + b.dpre;
     float *pieces = reinterpret_cast<float *>(scratch + b.pieces);
     const int64_t f = p->hidden, d = p->model;
-    b.slope.out = dpre;
-    b.slope.out_stride = 2 * f;
-    b.slope.pre = const_cast<void *>(pre);
-    int rc = launch_product<T, kSlope>(p, b.slope, {dy, dy_stride, 0}, {w_out, f, 1});
+    Maps maps = {};
+    if (!encode_maps<T>(p, &maps, true, dpre, pre, n)) return GATED_FFN_ECUDA;
+    int rc = launch_product<T, kSlope>(p, b.slope, {dy, dy_stride, 0}, {w_out, f, 1}, maps);
     if (rc != GATED_FFN_OK) return rc;
     b.dx.pieces = b.dw_in.pieces = b.dw_out.pieces = pieces;
     if (dx != nullptr) {
         b.dx.out = dx;
         b.dx.out_stride = dx_stride;
-        rc = launch_product<T, kStore>(p, b.dx, {dpre, 2 * f, 0}, {w_in, d, 1});
+        rc = launch_product<T, kStore>(p, b.dx, {dpre, 2 * f, 0}, {w_in, d, 1}, maps);
         if (rc != GATED_FFN_OK) return rc;
     }
     b.dw_in.out = dw_in;
     b.dw_in.out_stride = d;
-    rc = launch_product<T, kStore>(p, b.dw_in, {dpre, 2 * f, 1}, {x, x_stride, 1});
+    rc = launch_product<T, kStore>(p, b.dw_in, {dpre, 2 * f, 1}, {x, x_stride, 1}, maps);
     if (rc != GATED_FFN_OK) return rc;
     b.dw_out.out = dw_out;
     b.dw_out.out_stride = f;
-    return launch_product<T, kStore>(p, b.dw_out, {dy, dy_stride, 1}, {hidden, f, 1});
+    return launch_product<T, kStore>(p, b.dw_out, {dy, dy_stride, 1}, {hidden, f, 1}, maps);
 }
 
 bool aligned16(const void *v) { return reinterpret_cast<uintptr_t>(v) % 16 == 0; }
@@ -788,15 +1020,14 @@ bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride
 template <typename T>
 bool prepare_kernels(int *pairs, int sms)
 {
-    const void *kernels[3] = {reinterpret_cast<const void *>(k_product<T, kStore>),
-                              reinterpret_cast<const void *>(k_product<T, kGated>),
-                              reinterpret_cast<const void *>(k_product<T, kSlope>)};
-    for (const void *k : kernels)
-        if (!raise_dynamic_smem(k, kSmemBytes)) return false;
+    if (!raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kStore>), smem_of(kStore)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kGated>), smem_of(kGated)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kSlope>), smem_of(kSlope)))
+        return false;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sms & ~1));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.dynamicSmemBytes = smem_of(kStore);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -874,6 +1105,12 @@ size_t gated_ffn_workspace_bytes(const gated_ffn *p, int64_t n, int backward)
     if (p == nullptr || !rows_ok(p, n)) return 0;
     if (backward) return plan_backward(p, n).total;
     return n <= kRowsMax ? 0 : pieces_bytes(plan(p, kStore, n, p->model, p->hidden));
+}
+
+size_t gated_ffn_pre_bytes(const gated_ffn *p, int64_t n)
+{
+    if (p == nullptr || !rows_ok(p, n)) return 0;
+    return upper_bytes(n, p->hidden) + static_cast<size_t>(n) * 2 * lower_width(p->hidden);
 }
 
 int gated_ffn_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in, const void *w_out, void *pre,

@@ -9,7 +9,7 @@ import os
 from . import build as _build
 
 EXPORTS = ("gated_ffn_create", "gated_ffn_destroy", "gated_ffn_set_stream", "gated_ffn_workspace_bytes",
-           "gated_ffn_forward", "gated_ffn_backward", "gated_ffn_status", "gated_ffn_launch_count",
+           "gated_ffn_pre_bytes", "gated_ffn_forward", "gated_ffn_backward", "gated_ffn_status", "gated_ffn_launch_count",
            "gated_ffn_strerror")
 
 ACTIVATIONS = {"silu": 0, "gelu": 1}
@@ -41,6 +41,7 @@ def load(build_if_missing: bool = False):
     L.gated_ffn_destroy.argtypes = [vp]
     L.gated_ffn_set_stream.argtypes = [vp, vp]
     L.gated_ffn_workspace_bytes.argtypes = [vp, i64, i32]
+    L.gated_ffn_pre_bytes.argtypes = [vp, i64]
     L.gated_ffn_forward.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, i64, vp, size, i64]
     L.gated_ffn_backward.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, size, i64]
     L.gated_ffn_status.argtypes = [vp]
@@ -49,6 +50,7 @@ def load(build_if_missing: bool = False):
     for name in EXPORTS:
         getattr(L, name).restype = i32
     L.gated_ffn_workspace_bytes.restype = size
+    L.gated_ffn_pre_bytes.restype = size
     L.gated_ffn_launch_count.restype = i64
     L.gated_ffn_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -151,31 +153,38 @@ class GatedFfn:
 
     def saved(self, n: int):
         """Buffers in which forward() leaves what backward() needs: (pre-activations, hidden)."""
-        return self._empty(n, 2 * self.hidden), self._empty(n, self.hidden)
+        t = self.torch
+        return (t.empty((self._lib.gated_ffn_pre_bytes(self.h, n),), dtype=t.uint8, device=self.device),
+                self._empty(n, self.hidden))
+
+    def _saved(self, saved, n):
+        pre, hidden = saved
+        need = self._lib.gated_ffn_pre_bytes(self.h, n)
+        if pre.dtype is not self.torch.uint8 or pre.shape != (need,) or pre.device != self.device:
+            self._bad("saved[0]", pre, "uint8 (%d,)" % need)
+        return pre.data_ptr(), self._dense("saved[1]", hidden, (n, self.hidden))
 
     def forward(self, x, w_in, w_out, saved=None, out=None):
         n = x.shape[0]
         if out is None:
             out = self._empty(n, self.model)
         if saved is None:
-            pre, hidden = None, self._empty(n, self.hidden)
+            kept = self._empty(n, self.hidden)
+            pre, hidden = None, kept.data_ptr()
         else:
-            pre, hidden = saved
-            self._dense("saved[0]", pre, (n, 2 * self.hidden))
-            self._dense("saved[1]", hidden, (n, self.hidden))
+            pre, hidden = self._saved(saved, n)
         scratch, size = self._scratch(n, 0)
         self._stream()
         _check(self._lib.gated_ffn_forward(
             self.h, self._rows("x", x, n), self._stride(x), self._dense("w_in", w_in, (2 * self.hidden, self.model)),
-            self._dense("w_out", w_out, (self.model, self.hidden)), None if pre is None else pre.data_ptr(),
-            hidden.data_ptr(), self._rows("out", out, n), self._stride(out),
+            self._dense("w_out", w_out, (self.model, self.hidden)), pre, hidden, self._rows("out", out, n), self._stride(out),
             None if scratch is None else scratch.data_ptr(), size, n), "gated_ffn_forward")
         return out
 
     def backward(self, dy, x, w_in, w_out, saved, want_dx: bool = True):
         """(dx, dw_in, dw_out); dx is None unless wanted."""
         n = x.shape[0]
-        pre, hidden = saved
+        pre, hidden = self._saved(saved, n)
         dx = self._empty(n, self.model) if want_dx else None
         dw_in, dw_out = self._empty(2 * self.hidden, self.model), self._empty(self.model, self.hidden)
         scratch, size = self._scratch(n, 1)
@@ -184,8 +193,8 @@ class GatedFfn:
             self.h, self._rows("dy", dy, n), self._stride(dy), self._rows("x", x, n), self._stride(x),
             self._dense("w_in", w_in, (2 * self.hidden, self.model)),
             self._dense("w_out", w_out, (self.model, self.hidden)),
-            self._dense("saved[0]", pre, (n, 2 * self.hidden)), self._dense("saved[1]", hidden, (n, self.hidden)),
-            None if dx is None else dx.data_ptr(), self.model, dw_in.data_ptr(), dw_out.data_ptr(),
+            pre, hidden, None if dx is None else dx.data_ptr(),
+            self.model, dw_in.data_ptr(), dw_out.data_ptr(),
             None if scratch is None else scratch.data_ptr(), size, n), "gated_ffn_backward")
         return dx, dw_in, dw_out
 
