@@ -31,7 +31,7 @@
 // whatever the number of tiles; a tile that a cut divides goes to scratch in binary32 and k_join
 // adds its pieces in order.
 //
-// k_rows: up to 32 rows of x, bound by reading the weights.  A block owns 16 rows of the weights
+// k_rows: up to 64 rows of x, bound by reading the weights.  A block owns 16 rows of the weights
 // (of each projection), its warps split the reduction, and each lane's 16-byte loads of the
 // weights go straight into the operands of warp-wide matrix instructions: a dot product does not
 // care in which order its terms come, so a lane's eight consecutive elements serve as the
@@ -69,9 +69,10 @@ constexpr int kBlock8 = 32 * 32;
 constexpr int kPreBytes = 2 * kBlock16 + 2 * kBlock8;    // g and u: upper planes, then lower planes
 
 // Stages of the ring and staging bytes per epilogue warp: kGated holds g and u and the hidden units, kSlope
-// two sets of g and u (one on its way in, one worked on and then overwritten with dg and du).
-__host__ __device__ constexpr int stages_of(int mode) { return mode == kStore ? 6 : mode == kGated ? 5 : 4; }
-__host__ __device__ constexpr int staging_of(int mode) { return mode == kStore ? 0 : mode == kGated ? kPreBytes + kBlock16 : 2 * kPreBytes; }
+// kSets sets of g and u (one worked on and then overwritten with dg and du, the others on their way in).
+constexpr int kSets = 2;
+__host__ __device__ constexpr int stages_of(int mode) { return mode == kStore ? 6 : mode == kGated ? 5 : 6 - kSets; }
+__host__ __device__ constexpr int staging_of(int mode) { return mode == kStore ? 0 : mode == kGated ? kPreBytes + kBlock16 : kSets * kPreBytes; }
 __host__ __device__ constexpr int smem_of(int mode)
 {
     return stages_of(mode) * kStageBytes + kEpilogueWarps * staging_of(mode) + kBarrierBytes + 1024;
@@ -177,6 +178,11 @@ struct Walk {
     __device__ int row_tile() const { return p.m_first ? tile % p.m_tiles : tile / p.n_tiles; }
     __device__ int col_tile() const { return p.m_first ? tile / p.m_tiles : tile % p.n_tiles; }
 };
+
+// A kernel's start on the device ahead of the end of the one before it: what precedes wait_for_previous() must
+// not touch that one's results.
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // MN-major operand tile with the 128-byte swizzle: boxes of 64 elements (128 bytes) by 64 reduction
 // rows; the next 64 elements are a box (8192 bytes, leading offset) further, the next 8
@@ -313,6 +319,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    if (kMode == kStore) allow_next();       // k_join
     if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
     tc_fence_before_sync();
     cluster_sync_all();
@@ -419,7 +426,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             // kSlope: set i of the tile's four, columns [f, f + 32) of g and u, into buffer i & 1
             auto bring = [&](int i) {
                 const int f = w.col_tile() * tile_n + half * (tile_n / 2) + 32 * i;
-                const uint32_t dst = stage + (i & 1) * kPreBytes, bar = pre_full + 8 * (i & 1);
+                const uint32_t dst = stage + (i % kSets) * kPreBytes, bar = pre_full + 8 * (i % kSets);
                 mbar_expect_tx(bar, kPreBytes);
                 tma_load_plane(dst, &maps.upper, f, 0, row0, bar);
                 tma_load_plane(dst + kBlock16, &maps.upper, f, 1, row0, bar);
@@ -427,9 +434,8 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                 tma_load_plane(dst + 2 * kBlock16 + kBlock8, &maps.lower, f, 1, row0, bar);
             };
             if (kMode == kSlope && lane == 0) {
-                bulk_wait_read();                        // both buffers: the previous tile's results have left
-                bring(0);
-                bring(1);
+                bulk_wait_read();                        // the buffers: the previous tile's results have left
+                for (int i = 0; i < kSets; ++i) bring(i);
             }
             const bool ready = mbar_wait(acc_full0 + 8 * buf, use, abort_flag);
             if (!__all_sync(0xFFFFFFFFu, ready)) break;
@@ -485,9 +491,9 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
 #pragma unroll 1
                 for (int i = 0; i < sets; ++i) {
                     const int c = half * (tile_n / 2) + 32 * i, f = w.col_tile() * tile_n + c;
-                    const uint32_t pre = stage + (i & 1) * kPreBytes;
-                    const bool here = mbar_wait(pre_full + 8 * (i & 1), (pre_phase >> (i & 1)) & 1, abort_flag);
-                    pre_phase ^= 1u << (i & 1);
+                    const uint32_t pre = stage + (i % kSets) * kPreBytes;
+                    const bool here = mbar_wait(pre_full + 8 * (i % kSets), (pre_phase >> (i % kSets)) & 1, abort_flag);
+                    pre_phase ^= 1u << (i % kSets);
                     if (!__all_sync(0xFFFFFFFFu, here)) break;
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {        // 8 columns at a time
@@ -526,9 +532,9 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                             tma_store_plane(&maps.out, f, 1, row0, pre + kBlock16);
                         }
                         bulk_commit();
-                        if (i + 2 < sets) {              // into this buffer, a whole set ahead of its use
+                        if (i + kSets < sets) {          // into this buffer
                             bulk_wait_read();
-                            bring(i + 2);
+                            bring(i + kSets);
                         }
                     }
                 }
@@ -579,7 +585,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
     }
 }
 
-// Adds the pieces of the tiles that were divided: 4 rows of a tile per block, 64 threads per row.
+// Adds the pieces of the tiles that were divided: 16 rows of a tile per block, 64 threads per row, 4 rows each.
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_join(const Product p, const int pairs)
@@ -592,29 +598,40 @@ k_join(const Product p, const int pairs)
     int first = static_cast<int>(lo * p.cuts / rest);
     while (rest * (first + 1) / p.cuts <= lo) ++first;
     while (first > 0 && rest * first / p.cuts > lo) --first;
-    if (rest * first / p.cuts <= lo && rest * (first + 1) / p.cuts >= hi) return;   // one pair did all of it
-    const int row_in_tile = blockIdx.x * 4 + threadIdx.x / 64;
+    int last = first + 1;
+    while (last < p.cuts && rest * last / p.cuts < hi) ++last;
+    if (last == first + 1) return;                       // one pair did all of it
+    const int row0 = blockIdx.x * 16 + threadIdx.x / 64;
     const int c = 4 * (threadIdx.x % 64);
-    const int64_t row = static_cast<int64_t>(p.m_first ? tile % p.m_tiles : tile / p.n_tiles) * kTileM + row_in_tile;
+    const int64_t tile_row = static_cast<int64_t>(p.m_first ? tile % p.m_tiles : tile / p.n_tiles) * kTileM;
     const int col = (p.m_first ? tile / p.m_tiles : tile % p.n_tiles) * p.tile_n + c;
-    if (row >= p.m || c >= p.tile_n || col >= p.n) return;
-    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = first; i < p.cuts && rest * i / p.cuts < hi; ++i) {
+    if (c >= p.tile_n || col >= p.n) return;
+    wait_for_previous();
+    float4 sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int i = first; i < last; ++i) {
         // the slot of its first stretch if that lies in this tile, else of its last
         const int slot = rest * i / p.cuts / p.steps == index ? 0 : 1;
-        const float4 v = *reinterpret_cast<const float4 *>(
-            p.pieces + ((static_cast<int64_t>(i) * 2 + slot) * kTileM + row_in_tile) * kAccCols + c);
-        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        const float *src = p.pieces + (static_cast<int64_t>(i) * 2 + slot) * kTileM * kAccCols + c;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + (row0 + 4 * j) * kAccCols);
+            sum[j] = make_float4(sum[j].x + v.x, sum[j].y + v.y, sum[j].z + v.z, sum[j].w + v.w);
+        }
     }
-    uint32_t out[2] = {Type<T>::pack(sum.x, sum.y), Type<T>::pack(sum.z, sum.w)};
-    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * p.out_stride + col) = make_uint2(out[0], out[1]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t row = tile_row + row0 + 4 * j;
+        if (row < p.m)
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * p.out_stride + col) =
+                make_uint2(Type<T>::pack(sum[j].x, sum[j].y), Type<T>::pack(sum[j].z, sum[j].w));
+    }
 }
 
 // ---- few rows
 
-constexpr int kRowsThreads = 256;
-constexpr int kRowsWarps = kRowsThreads / 32;
-constexpr int kRowsMax = 32;                     // rows of x
+constexpr int kRowsMax = 64;                     // rows of x
 
 template <typename T>
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -645,19 +662,28 @@ struct Rows {
     int gelu;
 };
 
-// NT: groups of 8 rows of x.
+// NT: groups of 8 rows of x.  The warps split the reduction: as many as give enough loads in flight (16 where a
+// block reads one projection, 8 where it reads both) and as the sums of NT = 8 leave room for.
+template <bool kGatedRows, int NT>
+struct RowsShape {
+    static constexpr int kWarps = (kGatedRows ? 8 : 16) / (NT == 8 ? 2 : 1);
+    static constexpr int kDepth = NT <= 2 ? (kGatedRows ? 4 : 8) : 2;    // chunks of 32 reduction elements in flight
+};
+
 template <typename T, bool kGatedRows, int NT>
-__global__ void __launch_bounds__(kRowsThreads)
+__global__ void __launch_bounds__(32 * RowsShape<kGatedRows, NT>::kWarps)
 k_rows(const Rows p)
 {
     constexpr int P = kGatedRows ? 2 : 1;
-    constexpr int kDepth = NT <= 2 ? 4 : 2;      // chunks of 32 reduction elements in flight
-    __shared__ float s_sum[kRowsWarps][P][16][NT * 8 + 1];
+    constexpr int kDepth = RowsShape<kGatedRows, NT>::kDepth, kWarps = RowsShape<kGatedRows, NT>::kWarps;
+    __shared__ float s_sum[kWarps][P][16][NT * 8 + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const int f0 = blockIdx.x * 16;
     const uint16_t *w = static_cast<const uint16_t *>(p.w);
     const uint16_t *x = static_cast<const uint16_t *>(p.x);
+    if (kGatedRows) allow_next();
+    bool waited = kGatedRows;
     float acc[P][NT][4];
 #pragma unroll
     for (int i = 0; i < P; ++i)
@@ -667,11 +693,11 @@ k_rows(const Rows p)
             for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
     const int chunks = (p.k + 31) / 32;
     const uint4 none = make_uint4(0, 0, 0, 0);
-    for (int c0 = warp; c0 < chunks; c0 += kRowsWarps * kDepth) {
+    for (int c0 = warp; c0 < chunks; c0 += kWarps * kDepth) {
         uint4 wv[kDepth][P][2], xv[kDepth][NT];
 #pragma unroll
         for (int s = 0; s < kDepth; ++s) {
-            const int k = (c0 + s * kRowsWarps) * 32 + 8 * t;
+            const int k = (c0 + s * kWarps) * 32 + 8 * t;
 #pragma unroll
             for (int i = 0; i < P; ++i)
 #pragma unroll
@@ -681,10 +707,18 @@ k_rows(const Rows p)
                                       ? __ldg(reinterpret_cast<const uint4 *>(w + (static_cast<int64_t>(i) * p.width + f) * p.k + k))
                                       : none;
                 }
+        }
+        if (!waited) {       // the weights are under way; x is the previous kernel's result
+            wait_for_previous();
+            waited = true;
+        }
+#pragma unroll
+        for (int s = 0; s < kDepth; ++s) {
+            const int k = (c0 + s * kWarps) * 32 + 8 * t;
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int r = 8 * j + g;
-                xv[s][j] = k < p.k && r < p.n ? __ldg(reinterpret_cast<const uint4 *>(x + r * p.x_stride + k)) : none;
+                xv[s][j] = k < p.k && r < p.n ? *reinterpret_cast<const uint4 *>(x + r * p.x_stride + k) : none;
             }
         }
 #pragma unroll
@@ -704,14 +738,15 @@ k_rows(const Rows p)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s_sum[warp][i][g + 8 * (e >> 1)][8 * j + 2 * t + (e & 1)] = acc[i][j][e];
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * NT * 8; i += kRowsThreads) {
+    if (!waited) wait_for_previous();
+    for (int i = threadIdx.x; i < 16 * NT * 8; i += 32 * kWarps) {
         const int f = i % 16, r = i / 16;
         if (r >= p.n || f0 + f >= p.width) continue;
         float v[P];
 #pragma unroll
         for (int e = 0; e < P; ++e) {
             v[e] = 0.0f;
-            for (int k = 0; k < kRowsWarps; ++k) v[e] += s_sum[k][e][f][r];
+            for (int k = 0; k < kWarps; ++k) v[e] += s_sum[k][e][f][r];
         }
         T *out = static_cast<T *>(p.out) + r * p.out_stride + f0 + f;
         if constexpr (kGatedRows) {
@@ -835,6 +870,22 @@ Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
 
 size_t pieces_bytes(const Product &q) { return static_cast<size_t>(q.cuts) * 2 * kTileM * kAccCols * sizeof(float); }
 
+// A launch that may start while the kernel before it on the stream still runs (the kernels say where they wait for it).
+template <typename... Params, typename... Args>
+bool launch_overlapped(cudaStream_t stream, dim3 grid, unsigned threads, void (*kernel)(Params...), Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
+
 template <typename T, int kMode>
 int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, const Maps &maps)
 {
@@ -872,25 +923,37 @@ int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, 
     }
     p->launches += 1;
     if (q.cuts > 1) {
-        const dim3 grid(kTileM / 4, static_cast<unsigned>(tiles - static_cast<int64_t>(q.rounds) * pairs));
-        k_join<T><<<grid, 256, 0, p->stream>>>(q, pairs);
-        if (cudaGetLastError() != cudaSuccess) return GATED_FFN_ECUDA;
+        const dim3 grid(kTileM / 16, static_cast<unsigned>(tiles - static_cast<int64_t>(q.rounds) * pairs));
+        if (!launch_overlapped(p->stream, grid, 256, k_join<T>, q, pairs)) {
+            cudaGetLastError();
+            return GATED_FFN_ECUDA;
+        }
         p->launches += 1;
     }
     return GATED_FFN_OK;
 }
 
+template <typename T, bool kGatedRows, int NT>
+bool launch_rows_of(gated_ffn *p, const Rows &r)
+{
+    const dim3 grid(static_cast<unsigned>(div_up(r.width, 16)));
+    constexpr unsigned kThreadsOf = 32 * RowsShape<kGatedRows, NT>::kWarps;
+    if (!kGatedRows) return launch_overlapped(p->stream, grid, kThreadsOf, k_rows<T, kGatedRows, NT>, r);
+    k_rows<T, kGatedRows, NT><<<grid, kThreadsOf, 0, p->stream>>>(r);
+    return cudaGetLastError() == cudaSuccess;
+}
+
 template <typename T, bool kGatedRows>
 int launch_rows(gated_ffn *p, const Rows &r)
 {
-    const unsigned blocks = static_cast<unsigned>(div_up(r.width, 16));
-    if (r.n <= 8)
-        k_rows<T, kGatedRows, 1><<<blocks, kRowsThreads, 0, p->stream>>>(r);
-    else if (r.n <= 16)
-        k_rows<T, kGatedRows, 2><<<blocks, kRowsThreads, 0, p->stream>>>(r);
-    else
-        k_rows<T, kGatedRows, 4><<<blocks, kRowsThreads, 0, p->stream>>>(r);
-    if (cudaGetLastError() != cudaSuccess) return GATED_FFN_ECUDA;
+    const bool ok = r.n <= 8    ? launch_rows_of<T, kGatedRows, 1>(p, r)
+                    : r.n <= 16 ? launch_rows_of<T, kGatedRows, 2>(p, r)
+                    : r.n <= 32 ? launch_rows_of<T, kGatedRows, 4>(p, r)
+                                : launch_rows_of<T, kGatedRows, 8>(p, r);
+    if (!ok) {
+        cudaGetLastError();
+        return GATED_FFN_ECUDA;
+    }
     p->launches += 1;
     return GATED_FFN_OK;
 }

@@ -104,6 +104,14 @@ class GatedFfn:
             raise ValueError("activation must be one of %s" % (tuple(ACTIVATIONS),))
         self.model, self.hidden, self.activation = int(model), int(hidden), activation
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("device must be a CUDA device")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        # the current stream's handle without building a Stream object: a single token is short
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         with torch.cuda.device(self.device):
             self.h = gated_ffn_create(self.model, self.hidden, ACTIVATIONS[activation], types[self.dtype])
@@ -125,19 +133,19 @@ class GatedFfn:
         return gated_ffn_launch_count(self.h)
 
     def _stream(self):
-        self._lib.gated_ffn_set_stream(self.h, self.torch.cuda.current_stream(self.device).cuda_stream)
+        self._lib.gated_ffn_set_stream(self.h, self._current(self._index))
 
     def _bad(self, name, v, want):
         raise ValueError("%s must be %s on %s, got %s %s on %s with strides %s"
                          % (name, want, self.device, v.dtype, tuple(v.shape), v.device, v.stride()))
 
     def _rows(self, name, v, n):
-        if (v.dtype is not self.dtype or v.shape != (n, self.model) or v.device != self.device or v.stride(1) != 1):
+        if (v.dtype is not self.dtype or v.shape != (n, self.model) or v.get_device() != self._index or v.stride(1) != 1):
             self._bad(name, v, "%s [%d, %d] with a contiguous last dimension" % (self.dtype, n, self.model))
         return v.data_ptr()
 
     def _dense(self, name, v, shape):
-        if v.dtype is not self.dtype or v.shape != shape or v.device != self.device or not v.is_contiguous():
+        if v.dtype is not self.dtype or v.shape != shape or v.get_device() != self._index or not v.is_contiguous():
             self._bad(name, v, "contiguous %s %s" % (self.dtype, shape))
         return v.data_ptr()
 

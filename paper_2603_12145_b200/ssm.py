@@ -128,6 +128,14 @@ class Ssm:
             raise ValueError("dtype must be float32, bfloat16 or float16")
         self.channels, self.states, self.groups, self.width = int(channels), int(states), int(groups), int(width)
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError("device must be a CUDA device")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        # the current stream's handle without building a Stream object: a single token is short
+        self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         with torch.cuda.device(self.device):
             self.h = ssm_create(self.channels, self.states, self.groups, self.width, types[self.dtype])
@@ -148,7 +156,7 @@ class Ssm:
         return ssm_launch_count(self.h)
 
     def _stream(self):
-        self._lib.ssm_set_stream(self.h, self.torch.cuda.current_stream(self.device).cuda_stream)
+        self._lib.ssm_set_stream(self.h, self._current(self._index))
 
     # -- checks: the library sees pointers only
 
@@ -157,25 +165,25 @@ class Ssm:
                          % (name, want, self.device, v.dtype, tuple(v.shape), v.device, v.stride()))
 
     def _seq(self, name, v, batch, time, features):
-        if (v.dtype is not self.dtype or v.shape != (batch, time, features) or v.device != self.device
+        if (v.dtype is not self.dtype or v.shape != (batch, time, features) or v.get_device() != self._index
                 or (features > 1 and v.stride(2) != 1)):
             self._bad(name, v, "%s [%d, %d, %d] with a contiguous last dimension" % (self.dtype, batch, time, features))
         return Seq(v.data_ptr(), v.stride(0), v.stride(1))
 
     def _mask(self, name, v, shape):
-        if v.dtype not in (self.torch.uint8, self.torch.bool) or v.shape != shape or v.device != self.device:
+        if v.dtype not in (self.torch.uint8, self.torch.bool) or v.shape != shape or v.get_device() != self._index:
             self._bad(name, v, "uint8 or bool %s" % (shape,))
         return v
 
     def _row(self, name, v, n, features):
-        if (v.dtype is not self.dtype or v.shape != (n, features) or v.device != self.device
+        if (v.dtype is not self.dtype or v.shape != (n, features) or v.get_device() != self._index
                 or (features > 1 and v.stride(1) != 1)):
             self._bad(name, v, "%s [%d, %d] with a contiguous last dimension" % (self.dtype, n, features))
         return v.data_ptr()
 
     def _dense(self, name, v, shape, dtype=None):
         dtype = self.torch.float32 if dtype is None else dtype
-        if v.dtype is not dtype or v.shape != shape or v.device != self.device or not v.is_contiguous():
+        if v.dtype is not dtype or v.shape != shape or v.get_device() != self._index or not v.is_contiguous():
             self._bad(name, v, "contiguous %s %s" % (dtype, shape))
         return v.data_ptr()
 
