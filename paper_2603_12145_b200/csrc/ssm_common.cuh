@@ -142,6 +142,18 @@ __device__ __forceinline__ float softplus(float v)
     return fmaxf(v, 0.0f) + 2.0f * p;
 }
 
+// ---- sums over lanes
+
+// v[0..3] over the four lanes that share lane >> 2: lane gets the total of v[lane & 3].
+__device__ __forceinline__ float spread4(const float (&v)[4], int lane)
+{
+    const bool b1 = lane & 2, b0 = lane & 1;
+    const float s0 = b1 ? v[0] : v[2], s1 = b1 ? v[1] : v[3];
+    const float k0 = (b1 ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
+    const float k1 = (b1 ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, s1, 2);
+    return (b0 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? k0 : k1, 1);
+}
+
 // ---- pairs of binary32 numbers: one instruction for both
 
 struct Pair {

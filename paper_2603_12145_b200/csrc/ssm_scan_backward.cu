@@ -34,16 +34,6 @@ constexpr int kChunk = kScanChunk;
 
 __device__ __forceinline__ Pair zero_pair() { return Pair{0ull}; }
 
-// v[0..3] over the four lanes that share lane >> 2: lane gets the total of v[lane & 3].
-__device__ __forceinline__ float spread4(const float (&v)[4], int lane)
-{
-    const bool b1 = lane & 2, b0 = lane & 1;
-    const float s0 = b1 ? v[0] : v[2], s1 = b1 ? v[1] : v[3];
-    const float k0 = (b1 ? v[2] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, s0, 2);
-    const float k1 = (b1 ? v[3] : v[1]) + __shfl_xor_sync(0xFFFFFFFFu, s1, 2);
-    return (b0 ? k1 : k0) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? k0 : k1, 1);
-}
-
 // v[0..7] over the eight lanes that share lane & 3: lane gets the total of
 // v[4 * bit 4 + 2 * bit 3 + bit 2 of lane].
 __device__ __forceinline__ float spread8(const float (&v)[8], int lane)

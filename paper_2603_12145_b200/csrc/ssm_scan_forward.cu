@@ -260,25 +260,58 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
 //
 // The state passes through memory once; 4 states make one 16-byte access and neighbouring lanes
 // hold neighbouring quads, so a warp's accesses to the state are contiguous.  A block keeps its
-// channels' parameters and walks rows.
+// channels' parameters and walks rows, four at a time.  What a channel needs once per row (the
+// step's softplus, the gate, the result) is spread over the lanes that share the channel, a row or
+// two for each, and the others' reach it by shuffles: computed by every lane it would be three
+// quarters of the instructions.
 
 constexpr int kStepThreads = 256;
 constexpr int kStepRows = 4;    // rows whose states are in flight together
 
 // Four neighbouring elements of a row of b or c, as they lie in memory.
 template <typename T>
-struct alignas(4 * sizeof(T)) Four {
-    T e[4];
+struct Four {
+    uint32_t w[sizeof(T)];
+    __device__ __forceinline__ float at(int e) const
+    {
+        if (sizeof(T) == 4) return __uint_as_float(w[e]);
+        return from_bits<T>(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xFFFFu);
+    }
 };
+
+template <typename T>
+__device__ __forceinline__ Four<T> load_four(const T *p)     // aligned to its size
+{
+    Four<T> v;
+    if constexpr (sizeof(T) == 4)
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.w[0]), "=r"(v.w[1]), "=r"(v.w[2]), "=r"(v.w[3]) : "l"(p));
+    else
+        asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(v.w[0]), "=r"(v.w[1]) : "l"(p));
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ Four<T> gather_four(const T *p, int count)
+{
+    uint32_t v[4];
+    for (int e = 0; e < 4; ++e) v[e] = e < count ? load_bits(p + e) : 0;
+    Four<T> r;
+    for (int i = 0; i < static_cast<int>(sizeof(T)); ++i) r.w[i] = sizeof(T) == 4 ? v[i] : v[2 * i & 3] | v[(2 * i + 1) & 3] << 16;
+    return r;
+}
 
 // kAligned: states, rows of b and c come in whole, aligned quads.
 template <typename T, int LPC, bool kAligned>
-__global__ void __launch_bounds__(kStepThreads, 3)
+__global__ void __launch_bounds__(kStepThreads, 4)
 k_scan_step(const StepParams p, const T *__restrict__ x, const T *__restrict__ dt, const T *__restrict__ z,
             const T *__restrict__ bv, const T *__restrict__ cv, T *__restrict__ y, const int rows_per_block)
 {
     constexpr int kChannels = kStepThreads / LPC;
+    constexpr int kShare = LPC < kStepRows ? LPC : kStepRows, kOwn = kStepRows / kShare;   // rows whose scalars a lane forms
+    static_assert(kStepRows == 4, "spread4 and the exchanges below");
+    const int lane = threadIdx.x & 31;
     const int part = threadIdx.x % LPC;
+    const int own0 = part % kShare * kOwn;
     const int c0 = blockIdx.x * kChannels + threadIdx.x / LPC;
     const int n0 = 4 * part;
     const bool live = c0 < p.channels;
@@ -294,76 +327,98 @@ k_scan_step(const StepParams p, const T *__restrict__ x, const T *__restrict__ d
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * rows_per_block;
     const int64_t r1 = r0 + rows_per_block < p.n ? r0 + rows_per_block : p.n;
     const int64_t state_row = static_cast<int64_t>(p.channels) * p.states;
+    const int from = holds ? n0 : 0;
+    const T *zs = z != nullptr ? z : x;                // without a gate x stands in for z
+    const int64_t z_stride = z != nullptr ? p.z_stride : p.x_stride;
     for (int64_t r = r0; r < r1; r += kStepRows) {
-        // all loads of the rows first
+        // All loads of the rows first, none of them conditional: lanes without states read the first ones.
         float4 h[kStepRows];
-        uint32_t xv[kStepRows], dv[kStepRows], zv[kStepRows];
+        uint32_t xv[kOwn], dv[kOwn], zv[kOwn];
         Four<T> bb[kStepRows], cc[kStepRows];
         uint8_t clear[kStepRows];
 #pragma unroll
         for (int k = 0; k < kStepRows; ++k) {
             const int64_t row = r + k < r1 ? r + k : r1 - 1;
-            const float *src = p.state + row * state_row + static_cast<int64_t>(d) * p.states + n0;
-            const T *b4 = bv + row * p.b_stride + g * p.states + n0, *c4 = cv + row * p.c_stride + g * p.states + n0;
-            h[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) bb[k].e[e] = cc[k].e[e] = from_f32<T>(0.0f);
-            if (holds) {
-                if (kAligned) {
-                    asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
-                                 : "=f"(h[k].x), "=f"(h[k].y), "=f"(h[k].z), "=f"(h[k].w) : "l"(src));
-                    bb[k] = *reinterpret_cast<const Four<T> *>(b4);
-                    cc[k] = *reinterpret_cast<const Four<T> *>(c4);
-                } else {
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool in = n0 + e < p.states;
-                        v[e] = in ? src[e] : 0.0f;
-                        if (in) {
-                            bb[k].e[e] = b4[e];
-                            cc[k].e[e] = c4[e];
-                        }
-                    }
-                    h[k] = make_float4(v[0], v[1], v[2], v[3]);
-                }
+            const float *src = p.state + row * state_row + static_cast<int64_t>(d) * p.states + from;
+            const T *b4 = bv + row * p.b_stride + g * p.states + from, *c4 = cv + row * p.c_stride + g * p.states + from;
+            if (kAligned) {
+                asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(h[k].x), "=f"(h[k].y), "=f"(h[k].z), "=f"(h[k].w) : "l"(src));
+                bb[k] = load_four(b4);
+                cc[k] = load_four(c4);
+            } else {
+                const int count = min(4, p.states - from);
+                h[k] = make_float4(src[0], count > 1 ? src[1] : 0.0f, count > 2 ? src[2] : 0.0f, count > 3 ? src[3] : 0.0f);
+                bb[k] = gather_four(b4, count);
+                cc[k] = gather_four(c4, count);
             }
             clear[k] = p.done != nullptr ? p.done[row * p.done_stride] : 0;
-            xv[k] = load_bits(x + row * p.x_stride + d);
-            dv[k] = load_bits(dt + row * p.dt_stride + d);
-            zv[k] = z != nullptr ? load_bits(z + row * p.z_stride + d) : 0;
         }
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int64_t row = r + own0 + i < r1 ? r + own0 + i : r1 - 1;
+            xv[i] = load_bits(x + row * p.x_stride + d);
+            dv[i] = load_bits(dt + row * p.dt_stride + d);
+            zv[i] = load_bits(zs + row * z_stride + d);
+        }
+        float delta[kOwn], dx[kOwn];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            delta[i] = softplus(from_bits<T>(dv[i]) + bias);
+            dx[i] = delta[i] * from_bits<T>(xv[i]);
+        }
+        float sum[kStepRows];
 #pragma unroll
         for (int k = 0; k < kStepRows; ++k) {
             if (clear[k]) h[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            const float delta = softplus(from_bits<T>(dv[k]) + bias), xf = from_bits<T>(xv[k]);
-            const float dx = delta * xf;
+            const int source = lane - part + k / kOwn;
+            const float step = kShare > 1 ? __shfl_sync(0xFFFFFFFFu, delta[k % kOwn], source) : delta[k % kOwn];
+            const float input = kShare > 1 ? __shfl_sync(0xFFFFFFFFu, dx[k % kOwn], source) : dx[k % kOwn];
             float v[4] = {h[k].x, h[k].y, h[k].z, h[k].w};
-            float sum = 0.0f;
+            sum[k] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[e] = fmaf(ex2(delta * a2[e]), v[e], dx * to_f32(bb[k].e[e]));
-                sum = fmaf(to_f32(cc[k].e[e]), v[e], sum);
+                v[e] = fmaf(ex2(step * a2[e]), v[e], input * bb[k].at(e));
+                sum[k] = fmaf(cc[k].at(e), v[e], sum[k]);
             }
-#pragma unroll
-            for (int m = 1; m < LPC; m *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, m);
-            sum = fmaf(skip, xf, sum);
-            if (z != nullptr) {
-                const float zf = from_bits<T>(zv[k]);
-                sum *= zf * sigmoid(zf);
-            }
-            if (live && r + k < r1) {
-                const int64_t row = r + k;
-                float *dst = p.state_out + row * state_row + static_cast<int64_t>(d) * p.states + n0;
+            if (!holds) sum[k] = 0.0f;
+            if (holds && r + k < r1) {
+                float *dst = p.state_out + (r + k) * state_row + static_cast<int64_t>(d) * p.states + n0;
                 if (kAligned) {
-                    if (holds) *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (n0 + e < p.states) dst[e] = v[e];
                 }
-                if (part == 0) y[row * p.y_stride + d] = from_f32<T>(sum);
             }
+        }
+#pragma unroll
+        for (int m = kShare; m < LPC; m *= 2)
+#pragma unroll
+            for (int k = 0; k < kStepRows; ++k) sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], m);
+        float mine[kOwn];
+        if constexpr (kShare == 4) {
+            mine[0] = spread4(sum, lane);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                mine[i] = sum[i];
+                if constexpr (kShare == 2) {
+                    const float keep = part & 1 ? sum[2 + i] : sum[i], give = part & 1 ? sum[i] : sum[2 + i];
+                    mine[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, 1);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            float out = fmaf(skip, from_bits<T>(xv[i]), mine[i]);
+            if (z != nullptr) {
+                const float zf = from_bits<T>(zv[i]);
+                out *= zf * sigmoid(zf);
+            }
+            const int64_t row = r + own0 + i;
+            if (live && part < kShare && row < r1) y[row * p.y_stride + d] = from_f32<T>(out);
         }
     }
 }
