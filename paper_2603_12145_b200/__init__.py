@@ -4,4 +4,5 @@
 include/pong.h; `paper_2603_12145_b200.build` compiles it; `inputs` holds the
 seeded synthetic input generators.  Importing the package loads nothing.
 """
-__all__ = ["pong", "cartpole", "build", "inputs", "sharding", "verify"]
+__all__ = ["pong", "cartpole", "gru_policy", "policy_loop", "ssm", "gated_ffn", "ssm_policy", "build", "inputs",
+           "sharding", "verify"]
