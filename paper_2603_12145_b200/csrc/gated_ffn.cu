@@ -127,7 +127,7 @@ struct Product {
     int n;                  // rows of B, columns of D (kGated: hidden units)
     int64_t k;              // reduction length
     int a_rows, b_rows;     // 1: the operand is stored [k][rows] (MN-major), 0: [rows][k]
-    int tile_n;             // columns of D per tile: 256, 192 or 128 (kGated: 128 hidden units)
+    int tile_n;             // columns of D per tile: 256, 192 or 128; kGated: 128 or 64 hidden units, twice as many columns
     int m_tiles, n_tiles;
     int m_first;            // 1: consecutive tiles run down the rows, 0: along the columns
     int steps;              // ceil(k / 64)
@@ -180,7 +180,7 @@ struct Walk {
 };
 
 // A kernel's start on the device ahead of the end of the one before it: what precedes wait_for_previous() must
-// not touch that one's results.
+// not touch that one's results.  Every block waits, so that kernels end in the order of the stream.
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
@@ -190,6 +190,12 @@ __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontr
 __device__ __forceinline__ uint64_t smem_desc_rows(uint32_t addr)
 {
     return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (512ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// Place of a piece's block of 32 rows (0..7) and 16 columns (0..15) in the scratch, in float4.
+__device__ __forceinline__ int64_t piece_at(int pair, int slot, int rows, int cols)
+{
+    return (((static_cast<int64_t>(pair) * 2 + slot) * (kTileM / 32) + rows) * (kAccCols / 16) + cols) * 128;
 }
 
 // Columns [c, c + 16) of a row of `width` columns (a multiple of 8).
@@ -302,7 +308,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_cta_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int tile_n = kMode == kGated ? 256 : p.tile_n;     // accumulator columns
+    const int tile_n = kMode == kGated ? 2 * p.tile_n : p.tile_n;     // accumulator columns
     const int b_half = tile_n / 2;
 
     if (threadIdx.x == 0) {
@@ -319,12 +325,13 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (kMode == kStore) allow_next();       // k_join
+    allow_next();
     if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
     tc_fence_before_sync();
     cluster_sync_all();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
+    wait_for_previous();                     // operands may be its results, and outputs what it still reads
 
     if (warp == 0) {
         if (lane == 0) {
@@ -335,7 +342,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             Walk w(p, pair, pairs);
             while (ok && w.next()) {
                 const int a0 = w.row_tile() * kTileM + static_cast<int>(rank) * kRowsPerBlock;
-                const int b0 = kMode == kGated ? w.col_tile() * 128 + static_cast<int>(rank) * p.n
+                const int b0 = kMode == kGated ? w.col_tile() * p.tile_n + static_cast<int>(rank) * p.n
                                                : w.col_tile() * tile_n + static_cast<int>(rank) * b_half;
                 for (int kc = w.k0; kc < w.k1; ++kc) {
                     if (!mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) {
@@ -442,15 +449,15 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             tc_fence_after_sync();
             if (kMode == kGated) {
 #pragma unroll 1
-                for (int c = half * 64; c < half * 64 + 64; c += 32) {
-                    const int f = w.col_tile() * 128 + c;
+                for (int c = half * (p.tile_n / 2); c < (half + 1) * (p.tile_n / 2); c += 32) {
+                    const int f = w.col_tile() * p.tile_n + c;
                     if (lane == 0) bulk_wait_read();     // the blocks staged before have left
                     __syncwarp();
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t g[16], u[16], hw[8];
                         tmem_ld16(t0 + c + 16 * h, g);
-                        tmem_ld16(t0 + 128 + c + 16 * h, u);
+                        tmem_ld16(t0 + p.tile_n + c + 16 * h, u);
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -539,7 +546,8 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                     }
                 }
             } else if (w.piece >= 0) {
-                float *dst = p.pieces + ((static_cast<int64_t>(pair) * 2 + w.piece) * kTileM + rank * kRowsPerBlock + row_in_block) * kAccCols;
+                // [32 rows][16 columns][4][row][4 columns]: a warp's stores, and k_join's loads, are contiguous
+                float4 *dst = reinterpret_cast<float4 *>(p.pieces) + piece_at(pair, w.piece, static_cast<int>(rank) * 4 + q, 0) + lane;
 #pragma unroll 1
                 for (int c = half * (tile_n / 2); c < (half + 1) * (tile_n / 2); c += 16) {
                     uint32_t d[16];
@@ -547,7 +555,9 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                     tmem_wait_ld();
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        reinterpret_cast<uint4 *>(dst + c)[i] = make_uint4(d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]);
+                        dst[(c / 16) * 128 + 32 * i] =
+                            make_float4(__uint_as_float(d[4 * i]), __uint_as_float(d[4 * i + 1]), __uint_as_float(d[4 * i + 2]),
+                                        __uint_as_float(d[4 * i + 3]));
                 }
             } else {
                 const int c0 = w.col_tile() * tile_n;
@@ -585,11 +595,13 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
     }
 }
 
-// Adds the pieces of the tiles that were divided: 16 rows of a tile per block, 64 threads per row, 4 rows each.
+// Adds the pieces of the tiles that were divided: a warp takes 32 rows x 16 columns, a lane a row.
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_join(const Product p, const int pairs)
 {
+    allow_next();
+    wait_for_previous();                                 // in every block: this kernel must not end before that one
     const int index = blockIdx.y;                        // tile of the shared rest
     const int tile = p.rounds * pairs + index;
     const int64_t rest = static_cast<int64_t>(p.m_tiles * p.n_tiles - p.rounds * pairs) * p.steps;
@@ -601,37 +613,42 @@ k_join(const Product p, const int pairs)
     int last = first + 1;
     while (last < p.cuts && rest * last / p.cuts < hi) ++last;
     if (last == first + 1) return;                       // one pair did all of it
-    const int row0 = blockIdx.x * 16 + threadIdx.x / 64;
-    const int c = 4 * (threadIdx.x % 64);
-    const int64_t tile_row = static_cast<int64_t>(p.m_first ? tile % p.m_tiles : tile / p.n_tiles) * kTileM;
-    const int col = (p.m_first ? tile / p.m_tiles : tile % p.n_tiles) * p.tile_n + c;
-    if (c >= p.tile_n || col >= p.n) return;
-    wait_for_previous();
+    const int part = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int rows = part / (kAccCols / 16), cols = part % (kAccCols / 16);
+    const int c0 = (p.m_first ? tile / p.m_tiles : tile % p.n_tiles) * p.tile_n + 16 * cols;
+    const int64_t row = static_cast<int64_t>(p.m_first ? tile % p.m_tiles : tile / p.n_tiles) * kTileM + rows * 32 + lane;
+    if (16 * cols >= p.tile_n || c0 >= p.n) return;
     float4 sum[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) sum[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int i = first; i < last; ++i) {
         // the slot of its first stretch if that lies in this tile, else of its last
         const int slot = rest * i / p.cuts / p.steps == index ? 0 : 1;
-        const float *src = p.pieces + (static_cast<int64_t>(i) * 2 + slot) * kTileM * kAccCols + c;
+        const float4 *src = reinterpret_cast<const float4 *>(p.pieces) + piece_at(i, slot, rows, cols) + lane;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float4 v = *reinterpret_cast<const float4 *>(src + (row0 + 4 * j) * kAccCols);
+            const float4 v = src[32 * j];
             sum[j] = make_float4(sum[j].x + v.x, sum[j].y + v.y, sum[j].z + v.z, sum[j].w + v.w);
         }
     }
+    if (row >= p.m) return;
+    uint32_t out[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int64_t row = tile_row + row0 + 4 * j;
-        if (row < p.m)
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p.out) + row * p.out_stride + col) =
-                make_uint2(Type<T>::pack(sum[j].x, sum[j].y), Type<T>::pack(sum[j].z, sum[j].w));
+        out[2 * j] = Type<T>::pack(sum[j].x, sum[j].y);
+        out[2 * j + 1] = Type<T>::pack(sum[j].z, sum[j].w);
     }
+    store16(static_cast<uint16_t *>(p.out) + row * p.out_stride, c0, p.n, out);
 }
 
 // ---- few rows
 
-constexpr int kRowsMax = 64;                     // rows of x
+// Rows of x that take k_rows: its blocks read x from L2 once per 16 rows of the weights, k_product's time hardly
+// depends on so few rows.  576 x 1,536: 32 rows 8.6, 64 rows 12.1 against 19.7 us; 2,048 x 8,192: 32 rows 41 against 43,
+// 64 rows 75 against 44 us: up to 32 rows always, up to 64 while model * hidden is below 4 M.
+constexpr int kRowsMax = 64;
+inline bool few_rows(int64_t n, int64_t weights) { return n <= 32 || (n <= kRowsMax && weights <= (int64_t{4} << 20)); }
+
 
 template <typename T>
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -836,14 +853,27 @@ Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
     q.m = m;
     q.n = n;
     q.k = k;
-    // the narrowest total width wins, the widest tile among equals
-    q.tile_n = 256;
-    if (mode == kGated) {
-        q.tile_n = 128;
-    } else {
+    if (mode == kStore) {
+        // an incomplete round is shared by all pairs: the narrowest total width wins, the widest tile among equals
+        q.tile_n = 256;
         const int widths[2] = {192, 128};
         for (int w : widths)
             if (div_up(n, w) * w < div_up(n, q.tile_n) * q.tile_n) q.tile_n = w;
+    } else {
+        // Whole rounds only: the fewest rounds times a tile's cost.  Half the columns cost more than half (the rows of A
+        // are shared by fewer): 0.7 measured (1,003 x 1,000 x 2,504: three rounds of 64 units 24.5 us, two of 128 22.1 us), so a
+        // narrow tile pays where the wide ones are too few for the pairs.
+        const int widths[3] = {256, 192, 128};
+        int64_t best = -1;
+        for (int w : widths) {
+            const int units = mode == kGated ? w / 2 : w;
+            if (mode == kGated && w == 192) continue;      // its halves of 48 units are no multiple of a staged block
+            const int64_t cost = div_up(div_up(m, kTileM) * div_up(n, units), p->pairs) * (w + 192);
+            if (best < 0 || cost < best) {
+                best = cost;
+                q.tile_n = units;
+            }
+        }
     }
     q.m_tiles = static_cast<int>(div_up(m, kTileM));
     q.n_tiles = static_cast<int>(div_up(n, q.tile_n));
@@ -886,13 +916,14 @@ bool launch_overlapped(cudaStream_t stream, dim3 grid, unsigned threads, void (*
     return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
 }
 
+// after_own: the launch before it on the stream is one of this call's, which allow it to start early.
 template <typename T, int kMode>
-int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, const Maps &maps)
+int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, const Maps &maps, bool after_own)
 {
     CUtensorMap tm_a, tm_b;
     const CUtensorMapDataType type = Type<T>::kMap;
     const int64_t b_total = kMode == kGated ? 2 * static_cast<int64_t>(q.n) : q.n;
-    const uint32_t b_box = kMode == kGated ? 128 : q.tile_n / 2;
+    const uint32_t b_box = kMode == kGated ? q.tile_n : q.tile_n / 2;
     q.a_rows = a.by_rows;
     q.b_rows = b.by_rows;
     const bool ok = (a.by_rows ? encode(type, &tm_a, a.ptr, q.k, q.m, a.stride, kBK)
@@ -910,20 +941,22 @@ int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, 
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_of(kMode);
     cfg.stream = p->stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = after_own ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, k_product<T, kMode>, tm_a, tm_b, maps, q) != cudaSuccess) {
         cudaGetLastError();
         return GATED_FFN_ECUDA;
     }
     p->launches += 1;
     if (q.cuts > 1) {
-        const dim3 grid(kTileM / 16, static_cast<unsigned>(tiles - static_cast<int64_t>(q.rounds) * pairs));
+        const dim3 grid((kTileM / 32) * (kAccCols / 16) / 8, static_cast<unsigned>(tiles - static_cast<int64_t>(q.rounds) * pairs));
         if (!launch_overlapped(p->stream, grid, 256, k_join<T>, q, pairs)) {
             cudaGetLastError();
             return GATED_FFN_ECUDA;
@@ -977,7 +1010,7 @@ int run_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in,
                 void *hidden, void *y, int64_t y_stride, float *scratch, int64_t n)
 {
     Maps maps = {};
-    if (n <= kRowsMax) {
+    if (few_rows(n, static_cast<int64_t>(p->model) * p->hidden)) {
         Rows r = {};
         r.x = x;
         r.x_stride = x_stride;
@@ -1009,13 +1042,13 @@ int run_forward(gated_ffn *p, const void *x, int64_t x_stride, const void *w_in,
     Product q = plan(p, kGated, n, p->hidden, p->model);
     q.keep = pre != nullptr;
     if (!encode_maps<T>(p, &maps, false, hidden, pre, n)) return GATED_FFN_ECUDA;
-    const int rc = launch_product<T, kGated>(p, q, {x, x_stride, 0}, {w_in, p->model, 0}, maps);
+    const int rc = launch_product<T, kGated>(p, q, {x, x_stride, 0}, {w_in, p->model, 0}, maps, false);
     if (rc != GATED_FFN_OK) return rc;
     Product r = plan(p, kStore, n, p->model, p->hidden);
     r.out = y;
     r.out_stride = y_stride;
     r.pieces = scratch;
-    return launch_product<T, kStore>(p, r, {hidden, p->hidden, 0}, {w_out, p->hidden, 0}, maps);
+    return launch_product<T, kStore>(p, r, {hidden, p->hidden, 0}, {w_out, p->hidden, 0}, maps, true);
 }
 
 struct BackwardPlan {
@@ -1051,22 +1084,22 @@ int run_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const void *x,
     const int64_t f = p->hidden, d = p->model;
     Maps maps = {};
     if (!encode_maps<T>(p, &maps, true, dpre, pre, n)) return GATED_FFN_ECUDA;
-    int rc = launch_product<T, kSlope>(p, b.slope, {dy, dy_stride, 0}, {w_out, f, 1}, maps);
+    int rc = launch_product<T, kSlope>(p, b.slope, {dy, dy_stride, 0}, {w_out, f, 1}, maps, false);
     if (rc != GATED_FFN_OK) return rc;
     b.dx.pieces = b.dw_in.pieces = b.dw_out.pieces = pieces;
     if (dx != nullptr) {
         b.dx.out = dx;
         b.dx.out_stride = dx_stride;
-        rc = launch_product<T, kStore>(p, b.dx, {dpre, 2 * f, 0}, {w_in, d, 1}, maps);
+        rc = launch_product<T, kStore>(p, b.dx, {dpre, 2 * f, 0}, {w_in, d, 1}, maps, true);
         if (rc != GATED_FFN_OK) return rc;
     }
     b.dw_in.out = dw_in;
     b.dw_in.out_stride = d;
-    rc = launch_product<T, kStore>(p, b.dw_in, {dpre, 2 * f, 1}, {x, x_stride, 1}, maps);
+    rc = launch_product<T, kStore>(p, b.dw_in, {dpre, 2 * f, 1}, {x, x_stride, 1}, maps, true);
     if (rc != GATED_FFN_OK) return rc;
     b.dw_out.out = dw_out;
     b.dw_out.out_stride = f;
-    return launch_product<T, kStore>(p, b.dw_out, {dy, dy_stride, 1}, {hidden, f, 1}, maps);
+    return launch_product<T, kStore>(p, b.dw_out, {dy, dy_stride, 1}, {hidden, f, 1}, maps, true);
 }
 
 bool aligned16(const void *v) { return reinterpret_cast<uintptr_t>(v) % 16 == 0; }
@@ -1167,7 +1200,7 @@ size_t gated_ffn_workspace_bytes(const gated_ffn *p, int64_t n, int backward)
 {
     if (p == nullptr || !rows_ok(p, n)) return 0;
     if (backward) return plan_backward(p, n).total;
-    return n <= kRowsMax ? 0 : pieces_bytes(plan(p, kStore, n, p->model, p->hidden));
+    return few_rows(n, static_cast<int64_t>(p->model) * p->hidden) ? 0 : pieces_bytes(plan(p, kStore, n, p->model, p->hidden));
 }
 
 size_t gated_ffn_pre_bytes(const gated_ffn *p, int64_t n)
