@@ -31,6 +31,16 @@ __device__ __forceinline__ void load_pairs(Pair (&dst)[NP / 2], const float *src
     }
 }
 
+// Minus infinity: the input of a step past the end, whose softplus is zero and leaves the state as it is.
+template <typename T>
+constexpr uint32_t kNoStep = 0;
+template <>
+constexpr uint32_t kNoStep<float> = 0xFF800000u;
+template <>
+constexpr uint32_t kNoStep<__nv_bfloat16> = 0xFF80u;
+template <>
+constexpr uint32_t kNoStep<__half> = 0xFC00u;
+
 template <typename T, int NP, int LN, bool kSummary>
 __global__ void __launch_bounds__(kThreads, LN > 1 ? 3 : 4)
 k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
@@ -39,8 +49,6 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     constexpr int kWidth = (kSummary ? 1 : 2) * NS;               // staged values per step: b (and c)
     constexpr int kStage = (kTile * kWidth + kThreads - 1) / kThreads;
     __shared__ __align__(16) float s_bc[2][kTile][kWidth];
-    __shared__ uint8_t s_reset[2][kTile];
-
     const int tid = threadIdx.x;
     int64_t unit = blockIdx.x;
     const int tile = static_cast<int>(unit % (tiles * s.groups));
@@ -106,7 +114,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
             for (int k = 0; k < kTile; ++k) {
                 const bool in = live && t + k < t1;
                 nx[k] = in ? load_bits(px) : 0;
-                ndt[k] = in ? load_bits(pdt) : 0;
+                ndt[k] = in ? load_bits(pdt) : kNoStep<T>;
                 px += q.x.st;
                 pdt += q.dt.st;
                 if (!kSummary) {
@@ -122,7 +130,9 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
             nbc[k] = pbc[k] != nullptr && t + i / kWidth < t1 ? load_bits(pbc[k]) : 0;
             if (pbc[k] != nullptr) pbc[k] += kTile * st;
         }
-        if (tid < kTile) nreset = q.reset.ptr != nullptr && t + tid < t1 ? *q.reset.row(b, t + tid) : 0;
+        // a lane per step; a ballot shows a tile's resets to the whole warp
+        const int lane = tid & 31;
+        nreset = q.reset.ptr != nullptr && lane < kTile && t + lane < t1 ? *q.reset.row(b, t + lane) : 0;
     };
     fetch(t0);
 
@@ -134,8 +144,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
         float delta[kTile], xv[kTile], gate[kTile];
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            // past the end: delta = 0 leaves the state as it is
-            delta[k] = t + k < t1 ? softplus(from_bits<T>(ndt[k]) + bias) : 0.0f;
+            delta[k] = softplus(from_bits<T>(ndt[k]) + bias);
             xv[k] = from_bits<T>(nx[k]);
             if (!kSummary) {
                 const float z = from_bits<T>(nz[k]);
@@ -147,7 +156,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
             const int i = k * kThreads + tid;
             if (i < kTile * kWidth) (&s_bc[buf][0][0])[i] = from_bits<T>(nbc[k]);
         }
-        if (tid < kTile) s_reset[buf][tid] = nreset;
+        const uint32_t resets = __ballot_sync(0xFFFFFFFFu, nreset != 0);
         __syncthreads();
         if (t + kTile < t1) fetch(t + kTile);
         if (!warp_live) continue;
@@ -162,7 +171,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
         const bool stores = live && part == 0;
 #pragma unroll
         for (int k = 0; k < kTile; ++k) {
-            if (s_reset[buf][k]) {
+            if ((resets >> k) & 1u) {
                 cut = true;
 #pragma unroll
                 for (int i = 0; i < NP / 2; ++i) h[i] = pair(0.0f, 0.0f);
