@@ -216,4 +216,46 @@ __device__ __forceinline__ Pair decay(Pair rate, Pair delta)
     return ex2(fma(rate, delta, pair(kBias, kBias)));
 }
 
+// ---- the scalar functions on pairs (two steps of a channel): the same arithmetic in half the instructions
+
+__device__ __forceinline__ Pair exp_of(Pair v)
+{
+    constexpr float kLog2eLow = 1.9259629911e-8f;
+    const Pair t = mul(v, pair(kLog2e, kLog2e)), minus_t = mul(v, pair(-kLog2e, -kLog2e));
+    const Pair r = fma(v, pair(kLog2eLow, kLog2eLow), fma(v, pair(kLog2e, kLog2e), minus_t));
+    const Pair e = ex2(t);
+    return fma(mul(e, pair(kLn2, kLn2)), r, e);
+}
+
+__device__ __forceinline__ Pair rcp(Pair v) { return pair(rcp(lo(v)), rcp(hi(v))); }
+
+// The gate's sigmoid: for a 16-bit result the exponent's rounding (|v| 2^-24 relative) is far below the result's.
+template <typename T>
+__device__ __forceinline__ Pair gate_sigmoid(Pair v)
+{
+    const Pair one = pair(1.0f, 1.0f);
+    if (sizeof(T) == 2) return rcp(add(ex2(mul(v, pair(-kLog2e, -kLog2e))), one));
+    return rcp(add(exp_of(pair(at_most(-lo(v), 88.0f), at_most(-hi(v), 88.0f))), one));
+}
+
+// softplus, and its slope sigmoid(v) from the same exponential
+__device__ __forceinline__ Pair softplus(Pair v, Pair *slope = nullptr)
+{
+    const Pair e = exp_of(pair(at_least(-fabsf(lo(v)), -104.0f), at_least(-fabsf(hi(v)), -104.0f)));
+    const Pair s = mul(e, rcp(add(e, pair(2.0f, 2.0f))));
+    const Pair q = mul(s, s);
+    Pair p = pair(1.0f / 13.0f, 1.0f / 13.0f);
+    p = fma(p, q, pair(1.0f / 11.0f, 1.0f / 11.0f));
+    p = fma(p, q, pair(1.0f / 9.0f, 1.0f / 9.0f));
+    p = fma(p, q, pair(1.0f / 7.0f, 1.0f / 7.0f));
+    p = fma(p, q, pair(1.0f / 5.0f, 1.0f / 5.0f));
+    p = fma(p, q, pair(1.0f / 3.0f, 1.0f / 3.0f));
+    p = fma(mul(p, q), s, s);
+    if (slope != nullptr) {
+        const Pair r = rcp(add(e, pair(1.0f, 1.0f))), er = mul(e, r);
+        *slope = pair(lo(v) >= 0.0f ? lo(r) : lo(er), hi(v) >= 0.0f ? hi(r) : hi(er));
+    }
+    return fma(p, pair(2.0f, 2.0f), pair(fmaxf(lo(v), 0.0f), fmaxf(hi(v), 0.0f)));
+}
+
 }  // namespace ssm_k

@@ -248,22 +248,29 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                     }
                 }
 #pragma unroll
-                for (int k = 0; k < kChunk; ++k) {
+                for (int k = 0; k < kChunk; k += 2) {
                     float *dst = s_scal + k * 32 + lane;
-                    const bool in = live && k < steps;
-                    const float xv = in ? from_bits<T>(x[k]) : 0.0f, dyv = in ? from_bits<T>(dy[k]) : 0.0f;
-                    const float raw = from_bits<T>(dt[k]) + bias;
-                    const float delta = in ? softplus(raw) : 0.0f;
-                    dst[kDelta * kChunk * 32] = delta;
-                    dst[kDeltaX * kChunk * 32] = delta * xv;
-                    dst[kX * kChunk * 32] = xv;
-                    dst[kSig * kChunk * 32] = sigmoid(raw);
+                    const bool in0 = live && k < steps, in1 = live && k + 1 < steps;
+                    const Pair xv = pair(in0 ? from_bits<T>(x[k]) : 0.0f, in1 ? from_bits<T>(x[k + 1]) : 0.0f);
+                    const Pair dyv = pair(in0 ? from_bits<T>(dy[k]) : 0.0f, in1 ? from_bits<T>(dy[k + 1]) : 0.0f);
+                    Pair sig;
+                    const Pair step = softplus(pair(from_bits<T>(dt[k]) + bias, from_bits<T>(dt[k + 1]) + bias), &sig);
+                    const Pair delta = pair(in0 ? lo(step) : 0.0f, in1 ? hi(step) : 0.0f);
+                    auto keep = [&](int which, Pair v) {
+                        dst[which * kChunk * 32] = lo(v);
+                        dst[which * kChunk * 32 + 32] = hi(v);
+                    };
+                    keep(kDelta, delta);
+                    keep(kDeltaX, mul(delta, xv));
+                    keep(kX, xv);
+                    keep(kSig, sig);
                     if (gated) {
-                        const float zv = in ? from_bits<T>(z[k]) : 0.0f, sg = sigmoid(zv);
-                        dst[kG * kChunk * 32] = dyv * zv * sg;
-                        dst[kW * kChunk * 32] = dyv * fmaf(zv * sg, 1.0f - sg, sg);
+                        const Pair zv = pair(in0 ? from_bits<T>(z[k]) : 0.0f, in1 ? from_bits<T>(z[k + 1]) : 0.0f);
+                        const Pair sg = gate_sigmoid<T>(zv), zs = mul(zv, sg);
+                        keep(kG, mul(dyv, zs));
+                        keep(kW, mul(dyv, fma(zs, fma(sg, pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), sg)));
                     } else {
-                        dst[kG * kChunk * 32] = dyv;
+                        keep(kG, dyv);
                     }
                 }
             }

@@ -143,12 +143,17 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
         // everything that does not wait for the recurrence, for all steps of the tile side by side
         float delta[kTile], xv[kTile], gate[kTile];
 #pragma unroll
-        for (int k = 0; k < kTile; ++k) {
-            delta[k] = softplus(from_bits<T>(ndt[k]) + bias);
+        for (int k = 0; k < kTile; k += 2) {
+            const Pair step = softplus(pair(from_bits<T>(ndt[k]) + bias, from_bits<T>(ndt[k + 1]) + bias));
+            delta[k] = lo(step);
+            delta[k + 1] = hi(step);
             xv[k] = from_bits<T>(nx[k]);
+            xv[k + 1] = from_bits<T>(nx[k + 1]);
             if (!kSummary) {
-                const float z = from_bits<T>(nz[k]);
-                gate[k] = gated ? z * sigmoid(z) : 1.0f;
+                const Pair z = pair(from_bits<T>(nz[k]), from_bits<T>(nz[k + 1]));
+                const Pair f = mul(z, gate_sigmoid<T>(z));
+                gate[k] = gated ? lo(f) : 1.0f;
+                gate[k + 1] = gated ? hi(f) : 1.0f;
             }
         }
 #pragma unroll
