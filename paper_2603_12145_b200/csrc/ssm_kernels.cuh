@@ -22,6 +22,9 @@ struct ScanShape {
 // With 16 states and a 16-bit type the saved states are as much memory as two of the sequences.
 constexpr int kScanChunk = 16;
 
+// Segments whose ends the joining kernels load together.
+constexpr int kAhead = 8;
+
 struct ScanParams {
     const float *a, *d, *dt_bias;
     const float *state;

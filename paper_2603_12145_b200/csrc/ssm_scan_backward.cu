@@ -569,14 +569,26 @@ k_scan_back_carry(const ScanShape s, const ScanParams p)
         a[k] = in ? p.a[static_cast<int64_t>(d) * s.states + n] * kLog2e : 0.0f;
         e[k] = in && p.dstate_out != nullptr ? p.dstate_out[(b * s.channels + d) * s.states + n] : 0.0f;
     }
-    for (int seg = s.segments - 1; seg >= 0; --seg) {
-        float4 *slot = reinterpret_cast<float4 *>(p.carry) + ((b * s.segments + seg) * s.quads + quad) * s.channels + d;
-        const float4 out = seg > 0 ? *slot : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const float span = seg > 0 ? p.span[(b * s.segments + seg) * s.channels + d] : 0.0f;
-        *slot = make_float4(e[0], e[1], e[2], e[3]);
-        const float outs[4] = {out.x, out.y, out.z, out.w};
+    float4 *slots = reinterpret_cast<float4 *>(p.carry) + (b * s.segments * s.quads + quad) * s.channels + d;
+    const float *spans = p.span + b * s.segments * s.channels + d;
+    const int64_t stride = static_cast<int64_t>(s.quads) * s.channels;
+    for (int seg0 = s.segments - 1; seg0 >= 0; seg0 -= kAhead) {
+        float4 out[kAhead];
+        float span[kAhead];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = span < 0.0f ? outs[k] : fmaf(ex2(a[k] * span), e[k], outs[k]);
+        for (int k = 0; k < kAhead; ++k) {               // what leaves the first segment goes to dstate
+            const bool in = seg0 - k > 0;
+            out[k] = in ? slots[(seg0 - k) * stride] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            span[k] = in ? spans[static_cast<int64_t>(seg0 - k) * s.channels] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (seg0 - k < 0) break;
+            slots[(seg0 - k) * stride] = make_float4(e[0], e[1], e[2], e[3]);
+            const float outs[4] = {out[k].x, out[k].y, out[k].z, out[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = span[k] < 0.0f ? outs[i] : fmaf(ex2(a[i] * span[k]), e[i], outs[i]);
+        }
     }
 }
 

@@ -222,7 +222,7 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     }
 }
 
-// Turns the segments' ends (from a zero start) into their starts, in place.
+// Turns the segments' ends (from a zero start) into their starts, in place, kAhead segments' loads in flight together.
 __global__ void __launch_bounds__(256)
 k_scan_carry(const ScanShape s, const ScanParams p)
 {
@@ -240,16 +240,26 @@ k_scan_carry(const ScanShape s, const ScanParams p)
         a[e] = in ? p.a[static_cast<int64_t>(d) * s.states + n] * kLog2e : 0.0f;
         h[e] = in && p.state != nullptr ? p.state[(b * s.channels + d) * s.states + n] : 0.0f;
     }
-    for (int seg = 0; seg < s.segments; ++seg) {
-        const int64_t at = ((b * s.segments + seg) * s.quads + quad) * s.channels + d;
-        float4 *slot = reinterpret_cast<float4 *>(p.carry) + at;
-        const bool last = seg == s.segments - 1;
-        const float4 end = last ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : *slot;
-        const float span = last ? 0.0f : p.span[(b * s.segments + seg) * s.channels + d];
-        *slot = make_float4(h[0], h[1], h[2], h[3]);
-        const float ends[4] = {end.x, end.y, end.z, end.w};
+    float4 *slots = reinterpret_cast<float4 *>(p.carry) + (b * s.segments * s.quads + quad) * s.channels + d;
+    const float *spans = p.span + b * s.segments * s.channels + d;
+    const int64_t stride = static_cast<int64_t>(s.quads) * s.channels;
+    for (int seg0 = 0; seg0 < s.segments; seg0 += kAhead) {
+        float4 end[kAhead];
+        float span[kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = span < 0.0f ? ends[e] : fmaf(ex2(a[e] * span), h[e], ends[e]);
+        for (int k = 0; k < kAhead; ++k) {               // the last segment's end is nobody's start
+            const bool in = seg0 + k < s.segments - 1;
+            end[k] = in ? slots[(seg0 + k) * stride] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            span[k] = in ? spans[static_cast<int64_t>(seg0 + k) * s.channels] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (seg0 + k >= s.segments) break;
+            slots[(seg0 + k) * stride] = make_float4(h[0], h[1], h[2], h[3]);
+            const float ends[4] = {end[k].x, end[k].y, end[k].z, end[k].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = span[k] < 0.0f ? ends[e] : fmaf(ex2(a[e] * span[k]), h[e], ends[e]);
+        }
     }
 }
 
