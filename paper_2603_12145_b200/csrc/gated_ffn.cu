@@ -108,16 +108,18 @@ struct Type<__half> {
 constexpr float kGelu2C = 1.5957691216057308f;   // 2 sqrt(2 / pi)
 constexpr float kGeluK = 0.044715f;
 
-__device__ __forceinline__ float act_sigmoid(float v, int gelu)
+template <bool kGelu>
+__device__ __forceinline__ float act_sigmoid(float v)
 {
-    const float s = gelu ? kGelu2C * fmaf(kGeluK * v * v, v, v) : v;
+    const float s = kGelu ? kGelu2C * fmaf(kGeluK * v * v, v, v) : v;
     return rcp_approx(1.0f + ex2_approx(-kLog2e * s));
 }
 
-__device__ __forceinline__ float act_slope(float v, float sg, int gelu)
+template <bool kGelu>
+__device__ __forceinline__ float act_slope(float v, float sg)
 {
-    const float ds = gelu ? kGelu2C * fmaf(3.0f * kGeluK * v, v, 1.0f) : 1.0f;
-    return fmaf(v * sg * (1.0f - sg), ds, sg);
+    const float rise = v * sg * (1.0f - sg);
+    return kGelu ? fmaf(rise, kGelu2C * fmaf(3.0f * kGeluK * v, v, 1.0f), sg) : sg + rise;
 }
 
 // ---- the product
@@ -136,8 +138,7 @@ struct Product {
     void *out;              // kStore: D
     int64_t out_stride;
     int keep;               // kGated: write g and u
-    float *pieces;          // [cuts][2][256][256]
-    int gelu;
+    float *pieces;          // [cuts][2] tiles in the order of piece_at
     int *err;
 };
 
@@ -287,7 +288,7 @@ struct Maps {
     CUtensorMap upper, lower;   // planes of [g | u]
 };
 
-template <typename T, int kMode>
+template <typename T, int kMode, bool kGelu>
 __global__ void __launch_bounds__(kThreads, 1)
 k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b,
           const __grid_constant__ Maps maps, const __grid_constant__ Product p)
@@ -463,7 +464,7 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                         for (int i = 0; i < 8; ++i) {
                             const float g0 = __uint_as_float(g[2 * i]), g1 = __uint_as_float(g[2 * i + 1]);
                             const float u0 = __uint_as_float(u[2 * i]), u1 = __uint_as_float(u[2 * i + 1]);
-                            hw[i] = Type<T>::pack(g0 * act_sigmoid(g0, p.gelu) * u0, g1 * act_sigmoid(g1, p.gelu) * u1);
+                            hw[i] = Type<T>::pack(g0 * act_sigmoid<kGelu>(g0) * u0, g1 * act_sigmoid<kGelu>(g1) * u1);
                         }
                         put(piece16(stage + kPreBytes, lane, 2 * h), hw[0], hw[1], hw[2], hw[3]);
                         put(piece16(stage + kPreBytes, lane, 2 * h + 1), hw[4], hw[5], hw[6], hw[7]);
@@ -521,8 +522,8 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
                             for (int m = 0; m < 2; ++m) {
                                 const float g = join24(gw[e / 2], gl[e / 4], (e + m) & 3);
                                 const float u = join24(uw[e / 2], ul[e / 4], (e + m) & 3);
-                                const float dh = __uint_as_float(d[e + m]), sg = act_sigmoid(g, p.gelu);
-                                dg[m] = dh * u * act_slope(g, sg, p.gelu);
+                                const float dh = __uint_as_float(d[e + m]), sg = act_sigmoid<kGelu>(g);
+                                dg[m] = dh * u * act_slope<kGelu>(g, sg);
                                 du[m] = dh * g * sg;
                             }
                             og[e / 2] = Type<T>::pack(dg[0], dg[1]);
@@ -767,7 +768,7 @@ k_rows(const Rows p)
         }
         T *out = static_cast<T *>(p.out) + r * p.out_stride + f0 + f;
         if constexpr (kGatedRows) {
-            *out = static_cast<T>(v[0] * act_sigmoid(v[0], p.gelu) * v[1]);
+            *out = static_cast<T>(v[0] * (p.gelu ? act_sigmoid<true>(v[0]) : act_sigmoid<false>(v[0])) * v[1]);
             if (p.upper != nullptr) {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
@@ -893,7 +894,6 @@ Product plan(const gated_ffn *p, int mode, int64_t m, int n, int64_t k)
         if (cuts < rest) cuts = rest;
         q.cuts = static_cast<int>(cuts < p->pairs ? cuts : p->pairs);
     }
-    q.gelu = p->activation == GATED_FFN_GELU;
     q.err = p->err;
     return q;
 }
@@ -950,7 +950,8 @@ int launch_product(gated_ffn *p, Product q, const Operand &a, const Operand &b, 
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = after_own ? 2 : 1;
-    if (cudaLaunchKernelEx(&cfg, k_product<T, kMode>, tm_a, tm_b, maps, q) != cudaSuccess) {
+    auto kernel = kMode != kStore && p->activation == GATED_FFN_GELU ? k_product<T, kMode, kMode != kStore> : k_product<T, kMode, false>;
+    if (cudaLaunchKernelEx(&cfg, kernel, tm_a, tm_b, maps, q) != cudaSuccess) {
         cudaGetLastError();
         return GATED_FFN_ECUDA;
     }
@@ -1116,9 +1117,11 @@ bool stride_ok(int64_t stride, int64_t width) { return stride >= width && stride
 template <typename T>
 bool prepare_kernels(int *pairs, int sms)
 {
-    if (!raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kStore>), smem_of(kStore)) ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kGated>), smem_of(kGated)) ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kSlope>), smem_of(kSlope)))
+    if (!raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kStore, false>), smem_of(kStore)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kGated, false>), smem_of(kGated)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kGated, true>), smem_of(kGated)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kSlope, false>), smem_of(kSlope)) ||
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<T, kSlope, true>), smem_of(kSlope)))
         return false;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(sms & ~1));
@@ -1132,7 +1135,7 @@ bool prepare_kernels(int *pairs, int sms)
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, k_product<T, kStore>, &cfg) != cudaSuccess || clusters < 1) return false;
+    if (cudaOccupancyMaxActiveClusters(&clusters, k_product<T, kStore, false>, &cfg) != cudaSuccess || clusters < 1) return false;
     *pairs = clusters < sms / 2 ? clusters : sms / 2;
     return true;
 }
