@@ -137,3 +137,20 @@ def test_gated_ffn_library_exports_every_declared_symbol():
         assert L.gated_ffn_create(ctypes.byref(h), *bad) == -1
     assert L.gated_ffn_destroy(None) == -2 and L.gated_ffn_status(None) == -2
     assert L.gated_ffn_workspace_bytes(None, 1, 1) == 0
+
+
+def test_sequence_operators_have_no_cpu_fallback():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a CUDA device is present")
+    from paper_2603_12145_b200 import gated_ffn, ssm
+    ssm.load(build_if_missing=True)
+    gated_ffn.load(build_if_missing=True)
+    with pytest.raises(ssm.SsmError) as ei:
+        ssm.ssm_create(64, 16, 1, 4, 1)
+    assert ei.value.code == -4
+    with pytest.raises(gated_ffn.GatedFfnError) as ei:
+        gated_ffn.gated_ffn_create(64, 64, 0, 0)
+    assert ei.value.code == -4
+    with pytest.raises(ValueError):
+        ssm.Ssm(64, device="cpu")

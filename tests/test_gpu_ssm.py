@@ -290,6 +290,95 @@ def test_gradient_against_differences_of_the_kernel(torch):
     del gen
 
 
+def test_offsets_beyond_32_bits(torch):
+    """Rows more than 2^31 elements apart: the same values as from a dense copy, bit for bit."""
+    r = np.random.Generator(np.random.PCG64(11))
+    far = (1 << 31) + 64
+    big = torch.empty((2 * far + 4096,), dtype=torch.bfloat16, device="cuda")
+    dense = [rounded(torch, r.standard_normal((1, 3, w)), "bfloat16")[0] for w in (32, 32, 16, 16)]
+    views, at = [], 0
+    for d in dense:
+        v = big.as_strided((1, 3, d.shape[2]), (0, far, 1), at)
+        v.copy_(d)
+        views.append(v)
+        at += d.shape[2] + 8
+    a = torch.from_numpy(-np.exp(r.standard_normal((32, 16)))).float().cuda()
+    w = torch.from_numpy(r.standard_normal((32, 4))).float().cuda()
+    op = ssm.Ssm(32, 16)
+    out = big.as_strided((1, 3, 32), (3 * far, far, 1), 2048)
+    want_saved, got_saved = op.saved(1, 3), op.saved(1, 3)
+    want = op.scan(dense[0], dense[1], a, dense[2], dense[3], z=dense[1], saved=want_saved)
+    op.scan(views[0], views[1], a, views[2], views[3], z=views[1], out=out, saved=got_saved)
+    assert torch.equal(want, out)
+    one = op.scan_backward(dense[0], dense[0], dense[1], a, dense[2], dense[3], want_saved, z=dense[1])
+    two = op.scan_backward(views[0], views[0], views[1], a, views[2], views[3], got_saved, z=views[1])
+    assert all(one[k] is None or torch.equal(one[k], two[k]) for k in one)
+    want = op.conv(dense[0], w)
+    op.conv(views[0], w, out=out)
+    assert torch.equal(want, out)
+    for x, y in zip(op.conv_backward(dense[1], dense[0], w)[:2], op.conv_backward(views[1], views[0], w)[:2]):
+        assert torch.equal(x, y)
+
+
+def test_nan_and_infinity_stay_in_their_sequence(torch):
+    """A NaN or infinite input spoils its own sequence from its step on, up to the next reset, and nothing else."""
+    dev, _ = make_scan(torch, 21, 3, 40, 64, 16, 1, "bfloat16", "batch", 0, True, True)
+    op = ssm.Ssm(64, 16)
+    reset = torch.zeros((3, 40), dtype=torch.uint8, device="cuda")
+    reset[1, 20] = 1
+    args = dict(d=dev["d"], dt_bias=dev["dt_bias"], reset=reset, state=dev["state"])
+
+    def run(x, dt, z):
+        saved = op.saved(3, 40)
+        y = op.scan(x, dt, dev["a"], dev["b"], dev["c"], z=z, saved=saved, **args)
+        del args["state"]
+        g = op.scan_backward(dev["dy"], x, dt, dev["a"], dev["b"], dev["c"], saved, z=z, want_dstate=True, **args)
+        args["state"] = dev["state"]
+        return y, g
+
+    y, g = run(dev["x"], dev["dt"], dev["z"])
+    x, dt, z = dev["x"].clone(), dev["dt"].clone(), dev["z"].clone()
+    x[1, 7, 5], dt[1, 8, 6], z[1, 9, 8] = float("nan"), float("nan"), float("inf")
+    y2, g2 = run(x, dt, z)
+    for row in (0, 2):
+        assert torch.equal(y[row], y2[row]) and all(torch.equal(g[k][row], g2[k][row]) for k in ("dx", "ddt", "dz", "db", "dc"))
+    assert torch.equal(y[1, 20:], y2[1, 20:]) and torch.equal(y[1, :7], y2[1, :7])
+    others = [c for c in range(64) if c not in (5, 6)]
+    assert torch.equal(y[1, 10:20, others], y2[1, 10:20, others])
+    assert bool(torch.isnan(y2[1, 7:20, 5]).all()) and bool(torch.isnan(y2[1, 8:20, 6]).all())
+    for k in ("dx", "ddt", "dz", "db", "dc"):       # behind the reset nothing flows back from the spoilt part
+        assert torch.equal(g[k][1, 20:], g2[k][1, 20:]), k
+
+
+def test_steps_replay_from_a_cuda_graph(torch):
+    """The single-token forms captured once and replayed on changing inputs, as the policy loop uses them."""
+    n, ch = 37, 96
+    dev, _ = make_scan(torch, 31, n, 4, ch, 16, 1, "bfloat16", "time", 0.2, True, True)
+    op = ssm.Ssm(ch, 16)
+    w = torch.randn((ch, 4), device="cuda")
+    row = {k: dev[k][:, 0].contiguous() for k in ("x", "dt", "b", "c", "z", "reset")}
+    state, history = dev["state"].clone(), op.history(n).zero_()
+    out = torch.empty_like(row["x"])
+
+    def step(r, st, hist, dst):
+        x = op.conv_step(r["x"], hist, w, done=r["reset"])
+        op.scan_step(x, r["dt"], dev["a"], r["b"], r["c"], st, d=dev["d"], z=r["z"], dt_bias=dev["dt_bias"],
+                     done=r["reset"], out=dst)
+
+    step(row, state.clone(), history.clone(), out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(row, state, history, out)
+    want_state, want_history, want = dev["state"].clone(), op.history(n).zero_(), torch.empty_like(out)
+    for t in range(4):
+        for k in row:
+            row[k].copy_(dev[k][:, t])
+        graph.replay()
+        step({k: dev[k][:, t] for k in row}, want_state, want_history, want)
+        assert torch.equal(out, want) and torch.equal(state, want_state) and torch.equal(history, want_history)
+
+
 def test_refusals(torch):
     op = ssm.Ssm(32, 16, dtype=torch.bfloat16)
     x = torch.zeros((2, 4, 32), dtype=torch.bfloat16, device="cuda")
