@@ -31,7 +31,16 @@
 // whatever the number of tiles; a tile that a cut divides goes to scratch in binary32 and k_join
 // adds its pieces in order.
 //
-// k_rows: up to 64 rows of x, bound by reading the weights.  A block owns 16 rows of the weights
+// What bounds it (65,536 x 576 x 1,536 / 8,192 x 2,048 x 8,192, silu, bfloat16, each kernel by itself):
+//     kGated   231 us, 1.00 PFLOP/s / 390 us, 1.41 PFLOP/s   epilogue (1.2 GB/ms written) / tensor cores
+//     kSlope   199 us, 0.58 PFLOP/s / 287 us, 0.96 PFLOP/s   epilogue: 36 instructions per element on 8 warps
+//     kStore   y 110 us, 1.06 / 187 us, 1.47; dx 201 us, 1.15 / 372 us, 1.48; dW_in 250 us, 0.93 / 405 us, 1.36;
+//              dW_out 135 us, 0.86 / 208 us, 1.32 PFLOP/s
+// The products with 576 columns move 57 to 64 KB from L2 per 0.29 us of a tile's arithmetic and run at the
+// 9 to 10 TB/s that L2 gives; wider tiles would need more accumulator columns than there are.
+//
+// k_rows: up to 64 rows of x, bound by reading the weights: one row through 2,048 x 8,192 takes 16.8 us from a
+// graph, 6.0 TB/s.  A block owns 16 rows of the weights
 // (of each projection), its warps split the reduction, and each lane's 16-byte loads of the
 // weights go straight into the operands of warp-wide matrix instructions: a dot product does not
 // care in which order its terms come, so a lane's eight consecutive elements serve as the

@@ -8,6 +8,9 @@
 // resets of a tile; a tile without one, the common case, takes a path that does not look at them.
 // A reset clears the window, which drops every tap from before the episode.
 //
+// 1024 x 128 x 1152 in bfloat16: forward 120 us (5.0 TB/s of 0.6 GB, a copy of the same bytes takes
+// 100 us), backward 222 us (4.1 TB/s of 0.9 GB, schedulers 56 % busy).
+//
 // The backward kernel walks forward too: step t gives dpre_t, which goes into the pending
 // gradients of x_t .. x_{t-width+1} (as far back as the episode reaches); the oldest one is
 // then complete.  Its thread keeps its channels through all its runs, so dw and dbias stay in
