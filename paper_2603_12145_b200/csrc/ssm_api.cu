@@ -74,11 +74,11 @@ ScanShape scan_shape(const ssm *p, int64_t batch, int64_t time, bool backward)
     s.group_channels = p->channels / p->groups;
     s.quads = quads_of(p->states);
     s.chunks = static_cast<int>(div_up(time, kScanChunk));
-    const int64_t per_block = backward ? 128 : 128 / lanes_of(p->states);
+    const int64_t per_block = backward ? scan_back_channels(p->states) : 128 / lanes_of(p->states);
     const int64_t tiles = div_up(s.group_channels, per_block) * s.groups;
-    // resident blocks per SM: by registers, beyond 16 states backward by shared memory
+    // resident blocks per SM: by registers, beyond 32 states backward by shared memory
     const int lanes = lanes_of(p->states);
-    const int per_sm = backward ? (lanes == 1 ? 2 : 1) : (lanes == 1 ? 4 : 3);
+    const int per_sm = backward ? (lanes <= 2 ? 2 : 1) : (lanes == 1 ? 4 : 3);
     cut_time(s, batch * tiles, static_cast<int64_t>(p->sms) * per_sm);
     s.slots = 1;
     if (backward) {
@@ -110,7 +110,7 @@ ScanScratch scan_scratch(const ScanShape &s, bool backward)
         w.dd_part = at;
         at = align16(at + static_cast<size_t>(s.slots) * 2 * s.channels * 4);
         w.dbc_part = at;
-        const size_t tiles = (s.group_channels + 127) / 128;
+        const size_t tiles = div_up(s.group_channels, scan_back_channels(s.states));
         const size_t padded = s.states <= 16 ? 16 : s.states <= 32 ? 32 : 64;
         at += tiles * static_cast<size_t>(s.batch) * s.time * s.groups * 2 * padded * 4;
     }
@@ -171,7 +171,7 @@ template <typename T>
 int run_scan(ssm *p, const ssm_scan_args *a, bool backward)
 {
     const ScanShape s = scan_shape(p, a->batch, a->time, backward);
-    const int64_t per_block = backward ? 128 : 128 / lanes_of(p->states);
+    const int64_t per_block = backward ? scan_back_channels(p->states) : 128 / lanes_of(p->states);
     const int64_t tiles = div_up(s.group_channels, per_block) * s.groups;
     // the grids below have one dimension
     if (s.batch * s.segments * div_up(s.group_channels, 128 / lanes_of(p->states)) * s.groups > kMaxBlocks ||

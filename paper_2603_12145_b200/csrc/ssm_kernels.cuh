@@ -22,6 +22,10 @@ struct ScanShape {
 // With 16 states and a 16-bit type the saved states are as much memory as two of the sequences.
 constexpr int kScanChunk = 16;
 
+// Channels (and threads) of a block of the backward kernel.  Beyond 16 states shared memory limits the blocks: with 32, two
+// of three warps fit on an SM and only one of four (3 x 777 x 330 x 24 states: 69 against 100 us).
+__host__ __device__ constexpr int scan_back_channels(int states) { return states > 16 && states <= 32 ? 96 : 128; }
+
 // Segments whose ends the joining kernels load together.
 constexpr int kAhead = 8;
 

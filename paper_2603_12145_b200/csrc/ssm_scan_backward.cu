@@ -33,8 +33,6 @@
 namespace ssm_k {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
 constexpr int kGroup = 4;      // steps walked backwards out of registers
 constexpr int kChunk = kScanChunk;
 
@@ -71,6 +69,7 @@ enum Scalar { kDelta, kDeltaX, kG, kX, kSig, kW, kScalars };   // kSig: sigmoid(
 template <int SB>
 struct Smem {
     static constexpr int kStates = 16 * SB;
+    static constexpr int kThreads = scan_back_channels(kStates), kWarps = kThreads / 32;
     static constexpr int kBc = kChunk * 2 * kStates * 2;                // floats: every value twice
     static constexpr int kCheck = (kChunk / kGroup) * 16 * 32;          // per warp: h at every fourth step
     static constexpr int kScal = kScalars * kChunk * 32;                // per warp
@@ -136,12 +135,12 @@ __device__ __forceinline__ void turn(Pair (&h)[4][2], const float4 (&v)[4])
 __device__ __forceinline__ void prefetch(const void *ptr) { asm volatile("prefetch.global.L2 [%0];" ::"l"(ptr)); }
 
 template <typename T, int SB>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(Smem<SB>::kThreads, 2)
 k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles)
 {
     using S = Smem<SB>;
-    constexpr int NS = S::kStates;
-    constexpr int kStage = kChunk * 2 * NS / kThreads;   // values of b and c per thread and chunk
+    constexpr int NS = S::kStates, kThreads = S::kThreads, kWarps = S::kWarps;
+    constexpr int kStage = (kChunk * 2 * NS + kThreads - 1) / kThreads;   // values of b and c per thread and chunk
     extern __shared__ __align__(16) float smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     float *s_bc = smem;                                  // [step][b|c][NS][2]
@@ -283,7 +282,8 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
 #pragma unroll
             for (int i = 0; i < kStage; ++i) {
                 const float v = from_bits<T>(bc[i]);
-                *reinterpret_cast<float2 *>(s_bc + 2 * (i * kThreads + tid)) = make_float2(v, v);
+                if (i * kThreads + tid < kChunk * 2 * NS)
+                    *reinterpret_cast<float2 *>(s_bc + 2 * (i * kThreads + tid)) = make_float2(v, v);
             }
             __syncthreads();
 
@@ -430,7 +430,7 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
                     }
                 }
                 __syncthreads();
-                // the block's channels together: warp w takes every fourth step
+                // the block's channels together, the steps spread over the warps
                 for (int k = warp; k < steps; k += kWarps) {
                     float sum = 0.0f;
                     for (int w = 0; w < warps; ++w)
@@ -672,6 +672,7 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
 {
     using S = Smem<SB>;
     static_assert(S::kBytes <= 227 * 1024, "one block's shared memory");
+    constexpr int kThreads = S::kThreads;
     const int tiles = (s.group_channels + kThreads - 1) / kThreads;
     int launched = 3;
     if (cudaFuncSetAttribute(k_scan_backward<T, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) !=
