@@ -80,14 +80,33 @@ __device__ __forceinline__ void widen(Pair (&dst)[(V + 1) / 2], const Vec<T, V> 
     for (int i = 0; i < V; i += 2) dst[i / 2] = pair(to_f32(e[i]), i + 1 < V ? to_f32(e[i + 1 < V ? i + 1 : i]) : 0.0f);
 }
 
+template <typename T>
+__device__ __forceinline__ uint32_t narrow_two(Pair v);     // 16-bit types: both in one conversion
+template <>
+__device__ __forceinline__ uint32_t narrow_two<__nv_bfloat16>(Pair v)
+{
+    const __nv_bfloat162 r = __floats2bfloat162_rn(lo(v), hi(v));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <>
+__device__ __forceinline__ uint32_t narrow_two<__half>(Pair v)
+{
+    const __half2 r = __floats2half2_rn(lo(v), hi(v));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
 template <typename T, int V>
 __device__ __forceinline__ Vec<T, V> narrow(const Pair (&src)[(V + 1) / 2])
 {
-    T e[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = from_f32<T>(i & 1 ? hi(src[i / 2]) : lo(src[i / 2]));
     Vec<T, V> v;
-    memcpy(&v.w, e, sizeof(e));
+    if constexpr (sizeof(T) == 2 && V == 4) {
+        v.w = make_uint2(narrow_two<T>(src[0]), narrow_two<T>(src[1]));
+    } else {
+        T e[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = from_f32<T>(i & 1 ? hi(src[i / 2]) : lo(src[i / 2]));
+        memcpy(&v.w, e, sizeof(e));
+    }
     return v;
 }
 

@@ -113,6 +113,7 @@ class GatedFfn:
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
+        self._on = None                   # the stream that the handle was last given
         with torch.cuda.device(self.device):
             self.h = gated_ffn_create(self.model, self.hidden, ACTIVATIONS[activation], types[self.dtype])
 
@@ -133,7 +134,10 @@ class GatedFfn:
         return gated_ffn_launch_count(self.h)
 
     def _stream(self):
-        self._lib.gated_ffn_set_stream(self.h, self._current(self._index))
+        stream = self._current(self._index)
+        if stream != self._on:
+            self._lib.gated_ffn_set_stream(self.h, stream)
+            self._on = stream
 
     def _bad(self, name, v, want):
         raise ValueError("%s must be %s on %s, got %s %s on %s with strides %s"

@@ -137,6 +137,7 @@ class Ssm:
         self._current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
+        self._on = None                   # the stream that the handle was last given
         with torch.cuda.device(self.device):
             self.h = ssm_create(self.channels, self.states, self.groups, self.width, types[self.dtype])
 
@@ -156,7 +157,10 @@ class Ssm:
         return ssm_launch_count(self.h)
 
     def _stream(self):
-        self._lib.ssm_set_stream(self.h, self._current(self._index))
+        stream = self._current(self._index)
+        if stream != self._on:
+            self._lib.ssm_set_stream(self.h, stream)
+            self._on = stream
 
     # -- checks: the library sees pointers only
 
@@ -262,22 +266,34 @@ class Ssm:
 
     def conv_step(self, x, history, w, bias=None, done=None, history_out=None, out=None):
         """One token of n rows; the history is updated in place unless history_out is given."""
-        n, d = x.shape[0], self.channels
+        t, index, dtype, d = self.torch, self._index, self.dtype, self.channels
+        n = x.shape[0]
         if out is None:
-            out = self.torch.empty((n, d), dtype=self.dtype, device=self.device)
+            out = t.empty((n, d), dtype=dtype, device=self.device)
         if history_out is None:
             history_out = history
-        shape = (n, self.width - 1, d)
+        row, shape, sx, so = (n, d), (n, self.width - 1, d), x.stride(), out.stride()
+        # one look at everything: a single token is short; what does not fit is named below
+        if not (x.dtype is dtype and out.dtype is dtype and history.dtype is dtype and history_out.dtype is dtype
+                and w.dtype is t.float32 and x.shape == row and out.shape == row and history.shape == shape
+                and history_out.shape == shape and w.shape == (d, self.width) and x.get_device() == index
+                and out.get_device() == index and history.get_device() == index and history_out.get_device() == index
+                and w.get_device() == index and sx[1] == 1 and so[1] == 1 and history.is_contiguous()
+                and history_out.is_contiguous() and w.is_contiguous()):
+            self._row("x", x, n, d)
+            self._row("out", out, n, d)
+            self._dense("w", w, (d, self.width))
+            self._dense("history", history, shape, dtype)
+            self._dense("history_out", history_out, shape, dtype)
         if done is not None:
             self._mask("done", done, (n,))
         self._stream()
-        _check(self._lib.ssm_conv_step(
-            self.h, self._row("x", x, n, d), x.stride(0), None if done is None else done.data_ptr(),
-            0 if done is None else done.stride(0), self._dense("w", w, (d, self.width)),
-            None if bias is None else self._dense("bias", bias, (d,)),
-            self._dense("history", history, shape, self.dtype),
-            self._dense("history_out", history_out, shape, self.dtype), self._row("out", out, n, d), out.stride(0),
-            n), "ssm_conv_step")
+        code = self._lib.ssm_conv_step(
+            self.h, x.data_ptr(), sx[0], None if done is None else done.data_ptr(), 0 if done is None else done.stride(0),
+            w.data_ptr(), None if bias is None else self._dense("bias", bias, (d,)), history.data_ptr(),
+            history_out.data_ptr(), out.data_ptr(), so[0], n)
+        if code != 0:
+            raise SsmError(code, "ssm_conv_step")
         return out
 
     # -- scan
@@ -358,22 +374,38 @@ class Ssm:
 
     def scan_step(self, x, dt, a, b, c, state, d=None, z=None, dt_bias=None, done=None, state_out=None, out=None):
         """One token of n rows; the state is updated in place unless state_out is given."""
-        n, ch, narrow = x.shape[0], self.channels, self.groups * self.states
+        t, index, dtype, ch = self.torch, self._index, self.dtype, self.channels
+        n, narrow = x.shape[0], self.groups * self.states
         if out is None:
-            out = self.torch.empty((n, ch), dtype=self.dtype, device=self.device)
+            out = t.empty((n, ch), dtype=dtype, device=self.device)
         if state_out is None:
             state_out = state
-        shape = (n, ch, self.states)
+        row, thin, shape, rates, f32 = (n, ch), (n, narrow), (n, ch, self.states), (ch, self.states), t.float32
+        sx, sdt, sb, sc, so = x.stride(), dt.stride(), b.stride(), c.stride(), out.stride()
+        # one look at everything: a single token is short; what does not fit is named below
+        if not (x.dtype is dtype and dt.dtype is dtype and b.dtype is dtype and c.dtype is dtype and out.dtype is dtype
+                and a.dtype is f32 and state.dtype is f32 and state_out.dtype is f32
+                and x.shape == row and dt.shape == row and out.shape == row and b.shape == thin and c.shape == thin
+                and a.shape == rates and state.shape == shape and state_out.shape == shape
+                and x.get_device() == index and dt.get_device() == index and b.get_device() == index
+                and c.get_device() == index and out.get_device() == index and a.get_device() == index
+                and state.get_device() == index and state_out.get_device() == index
+                and sx[1] == 1 and sdt[1] == 1 and sb[1] == 1 and sc[1] == 1 and so[1] == 1
+                and a.is_contiguous() and state.is_contiguous() and state_out.is_contiguous()):
+            for name, v, features in (("x", x, ch), ("dt", dt, ch), ("b", b, narrow), ("c", c, narrow), ("out", out, ch)):
+                self._row(name, v, n, features)
+            for name, v, want in (("a", a, rates), ("state", state, shape), ("state_out", state_out, shape)):
+                self._dense(name, v, want)
         if done is not None:
             self._mask("done", done, (n,))
         self._stream()
-        _check(self._lib.ssm_scan_step(
-            self.h, self._row("x", x, n, ch), x.stride(0), self._row("dt", dt, n, ch), dt.stride(0),
-            None if z is None else self._row("z", z, n, ch), 0 if z is None else z.stride(0),
-            self._row("b", b, n, narrow), b.stride(0), self._row("c", c, n, narrow), c.stride(0),
-            None if done is None else done.data_ptr(), 0 if done is None else done.stride(0),
-            self._dense("a", a, (ch, self.states)), None if d is None else self._dense("d", d, (ch,)),
-            None if dt_bias is None else self._dense("dt_bias", dt_bias, (ch,)), self._dense("state", state, shape),
-            self._dense("state_out", state_out, shape), self._row("out", out, n, ch), out.stride(0), n),
-            "ssm_scan_step")
+        code = self._lib.ssm_scan_step(
+            self.h, x.data_ptr(), sx[0], dt.data_ptr(), sdt[0], None if z is None else self._row("z", z, n, ch),
+            0 if z is None else z.stride(0), b.data_ptr(), sb[0], c.data_ptr(), sc[0],
+            None if done is None else done.data_ptr(), 0 if done is None else done.stride(0), a.data_ptr(),
+            None if d is None else self._dense("d", d, (ch,)),
+            None if dt_bias is None else self._dense("dt_bias", dt_bias, (ch,)), state.data_ptr(),
+            state_out.data_ptr(), out.data_ptr(), so[0], n)
+        if code != 0:
+            raise SsmError(code, "ssm_scan_step")
         return out
