@@ -250,6 +250,8 @@ template <typename T, int V, int W>
 __global__ void __launch_bounds__(kThreads, 4)
 k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 {
+    allow_next();
+    wait_for_previous();
     constexpr int kTile = 4, P = (V + 1) / 2;
     const int vecs = s.channels / V, tiles = (vecs + 31) / 32;
     const int64_t warp = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) / 32;
@@ -375,6 +377,8 @@ k_conv_backward(const ConvShape s, const ConvParams p, const ConvSeqs<T> q)
 __global__ void __launch_bounds__(256)
 k_conv_params(const ConvShape s, const ConvParams p)
 {
+    allow_next();
+    wait_for_previous();
     __shared__ float part[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
@@ -491,8 +495,8 @@ int launch_conv_backward(const ConvShape &s, const ConvParams &p, const ConvSeqs
         SSM_BY_WIDTH(k_conv_backward, T, 1, blocks, s, p, q);
     }
     const dim3 grid(static_cast<unsigned>((s.channels + 31) / 32), static_cast<unsigned>(s.width + 1));
-    k_conv_params<<<grid, 256, 0, stream>>>(s, p);
-    return cudaGetLastError() == cudaSuccess ? 2 : -1;
+    const bool ok = cudaGetLastError() == cudaSuccess && launch_after(stream, grid, 256, 0, k_conv_params, s, p);
+    return ok ? 2 : -1;
 }
 
 template <typename T>

@@ -5,6 +5,31 @@
 
 namespace ssm_k {
 
+// ---- kernels of one call that follow one another
+//
+// Every kernel begins with allow_next() and wait_for_previous(); those behind the first are launched by
+// launch_after(): their blocks are placed while the kernel before them still runs and wait there for its results,
+// which hides the launch.  Every block waits, so that kernels end in the order of the stream.
+
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+bool launch_after(cudaStream_t stream, dim3 grid, unsigned threads, size_t smem, void (*kernel)(Params...), Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+}
+
 // Sizes of a scan and how its work is cut.
 struct ScanShape {
     int64_t batch;

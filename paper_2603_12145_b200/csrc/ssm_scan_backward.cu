@@ -141,6 +141,8 @@ k_scan_backward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, cons
     using S = Smem<SB>;
     constexpr int NS = S::kStates, kThreads = S::kThreads, kWarps = S::kWarps;
     constexpr int kStage = (kChunk * 2 * NS + kThreads - 1) / kThreads;   // values of b and c per thread and chunk
+    allow_next();
+    wait_for_previous();
     extern __shared__ __align__(16) float smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     float *s_bc = smem;                                  // [step][b|c][NS][2]
@@ -486,6 +488,8 @@ k_scan_back_summary(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, 
     constexpr int NS = NP * LN, kTile = 8;
     __shared__ __align__(16) float s_c[kTile][NS];
     __shared__ uint8_t s_reset[kTile];
+    allow_next();
+    wait_for_previous();
     const int tid = threadIdx.x;
     int64_t unit = blockIdx.x;
     const int tile = static_cast<int>(unit % (tiles * s.groups));
@@ -561,6 +565,8 @@ k_scan_back_summary(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, 
 __global__ void __launch_bounds__(256)
 k_scan_back_carry(const ScanShape s, const ScanParams p)
 {
+    allow_next();
+    wait_for_previous();
     const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
     const int64_t per_row = static_cast<int64_t>(s.quads) * s.channels;
     if (i >= s.batch * per_row) return;
@@ -603,6 +609,8 @@ template <typename T>
 __global__ void __launch_bounds__(256)
 k_scan_dbc(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int tiles, const int padded)
 {
+    allow_next();
+    wait_for_previous();
     const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
     const int64_t rows = s.batch * s.time * s.groups;
     const int n = static_cast<int>(i % padded);
@@ -623,6 +631,8 @@ k_scan_dbc(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const int
 __global__ void __launch_bounds__(256)
 k_scan_params(const ScanShape s, const ScanParams p)
 {
+    allow_next();
+    wait_for_previous();
     __shared__ float4 part[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int d = blockIdx.x * 32 + lane;
@@ -674,10 +684,10 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
     static_assert(S::kBytes <= 227 * 1024, "one block's shared memory");
     constexpr int kThreads = S::kThreads;
     const int tiles = (s.group_channels + kThreads - 1) / kThreads;
-    int launched = 3;
-    if (cudaFuncSetAttribute(k_scan_backward<T, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) !=
-        cudaSuccess)
+    if (cudaFuncSetAttribute(k_scan_backward<T, SB>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes) != cudaSuccess)
         return -1;
+    const dim3 blocks(static_cast<unsigned>(tiles * s.groups) * s.slots);
+    int launched = 3;
     if (s.segments > 1) {
         if (s.states <= 4)
             launch_summary<T, 4, 1>(s, p, q, stream);
@@ -686,15 +696,21 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
         else
             launch_summary<T, 16, SB>(s, p, q, stream);
         const int64_t threads = s.batch * s.quads * s.channels;
-        k_scan_back_carry<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, stream>>>(s, p);
+        if (cudaGetLastError() != cudaSuccess ||
+            !launch_after(stream, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, k_scan_back_carry, s, p) ||
+            !launch_after(stream, blocks, kThreads, S::kBytes, k_scan_backward<T, SB>, s, p, q, tiles))
+            return -1;
         launched += 2;
+    } else {
+        k_scan_backward<T, SB><<<blocks, kThreads, S::kBytes, stream>>>(s, p, q, tiles);
+        if (cudaGetLastError() != cudaSuccess) return -1;
     }
-    k_scan_backward<T, SB><<<static_cast<unsigned>(tiles * s.groups) * s.slots, kThreads, S::kBytes, stream>>>(s, p, q, tiles);
     const int64_t values = s.batch * s.time * s.groups * 2 * S::kStates;
-    k_scan_dbc<T><<<static_cast<unsigned>((values + 255) / 256), 256, 0, stream>>>(s, p, q, tiles, S::kStates);
     const dim3 grid(static_cast<unsigned>((s.channels + 31) / 32), static_cast<unsigned>(s.quads + 1));
-    k_scan_params<<<grid, 256, 0, stream>>>(s, p);
-    return cudaGetLastError() == cudaSuccess ? launched : -1;
+    const bool ok = launch_after(stream, dim3(static_cast<unsigned>((values + 255) / 256)), 256, 0, k_scan_dbc<T>, s, p, q, tiles,
+                                 static_cast<int>(S::kStates)) &&
+                    launch_after(stream, grid, 256, 0, k_scan_params, s, p);
+    return ok ? launched : -1;
 }
 
 }  // namespace

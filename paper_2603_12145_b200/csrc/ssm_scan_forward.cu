@@ -57,6 +57,8 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
     constexpr int kWidth = (kSummary ? 1 : 2) * NS;               // staged values per step: b (and c)
     constexpr int kStage = (kTile * kWidth + kThreads - 1) / kThreads;
     __shared__ __align__(16) float s_bc[2][kTile][kWidth];
+    allow_next();
+    wait_for_previous();
     const int tid = threadIdx.x;
     int64_t unit = blockIdx.x;
     const int tile = static_cast<int>(unit % (tiles * s.groups));
@@ -234,6 +236,8 @@ k_scan_forward(const ScanShape s, const ScanParams p, const ScanSeqs<T> q, const
 __global__ void __launch_bounds__(256)
 k_scan_carry(const ScanShape s, const ScanParams p)
 {
+    allow_next();
+    wait_for_previous();
     const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
     const int64_t per_row = static_cast<int64_t>(s.quads) * s.channels;
     if (i >= s.batch * per_row) return;
@@ -277,15 +281,16 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
     const int per_block = kThreads / LN;
     const int tiles = (s.group_channels + per_block - 1) / per_block;
     const unsigned blocks = static_cast<unsigned>(s.batch * s.segments * s.groups * tiles);
-    int launched = 1;
-    if (s.segments > 1) {
-        k_scan_forward<T, NP, LN, true><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
-        const int64_t threads = s.batch * s.quads * s.channels;
-        k_scan_carry<<<static_cast<unsigned>((threads + 255) / 256), 256, 0, stream>>>(s, p);
-        launched += 2;
+    if (s.segments == 1) {
+        k_scan_forward<T, NP, LN, false><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
+        return cudaGetLastError() == cudaSuccess ? 1 : -1;
     }
-    k_scan_forward<T, NP, LN, false><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
-    return cudaGetLastError() == cudaSuccess ? launched : -1;
+    k_scan_forward<T, NP, LN, true><<<blocks, kThreads, 0, stream>>>(s, p, q, tiles);
+    const int64_t threads = s.batch * s.quads * s.channels;
+    const bool ok = cudaGetLastError() == cudaSuccess &&
+                    launch_after(stream, dim3(static_cast<unsigned>((threads + 255) / 256)), 256, 0, k_scan_carry, s, p) &&
+                    launch_after(stream, dim3(blocks), kThreads, 0, k_scan_forward<T, NP, LN, false>, s, p, q, tiles);
+    return ok ? 3 : -1;
 }
 
 // ---- one token
