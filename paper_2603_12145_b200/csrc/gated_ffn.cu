@@ -33,7 +33,7 @@
 //
 // What bounds it (65,536 x 576 x 1,536 / 8,192 x 2,048 x 8,192, silu, bfloat16, each kernel by itself):
 //     kGated   231 us, 1.00 PFLOP/s / 390 us, 1.41 PFLOP/s   epilogue (1.2 GB/ms written) / tensor cores
-//     kSlope   199 us, 0.58 PFLOP/s / 287 us, 0.96 PFLOP/s   epilogue: 36 instructions per element on 8 warps
+//     kSlope   199 us, 0.58 PFLOP/s / 287 us, 0.96 PFLOP/s   epilogue: slope of the activation on 8 warps
 //     kStore   y 110 us, 1.06 / 187 us, 1.47; dx 201 us, 1.15 / 372 us, 1.48; dW_in 250 us, 0.93 / 405 us, 1.36;
 //              dW_out 135 us, 0.86 / 208 us, 1.32 PFLOP/s
 // The products with 576 columns move 57 to 64 KB from L2 per 0.29 us of a tile's arithmetic and run at the
