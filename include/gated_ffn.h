@@ -25,7 +25,8 @@
  * model and hidden are multiples of 8 (16-byte rows); n is any.  Weights and saved
  * buffers are contiguous; x, y, dy, dx have a row stride in elements (multiple of 8).
  * Pointers are DEVICE pointers owned by the caller, 16-byte aligned; inputs must not
- * overlap outputs.  Calls enqueue on the handle's stream and return
+ * overlap outputs.  Calls enqueue on the handle's stream, on the device that was current when
+ * the handle was created (whichever is current now stays so), and return
  * (gated_ffn_status synchronises).  The library allocates only in gated_ffn_create.
  * Return 0 or a negative GATED_FFN_E* code; no exceptions, aborts, traps or printing;
  * no CPU fallback.

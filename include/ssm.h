@@ -36,7 +36,8 @@
  * DEVICE pointers owned by the caller, aligned to their element.  Inputs must not
  * overlap outputs, except that a step may update its state or history in place.
  *
- * Calls enqueue on the handle's stream and return; nothing is allocated but the
+ * Calls enqueue on the handle's stream, on the device that was current when the handle was
+ * created (whichever is current now stays so), and return; nothing is allocated but the
  * handle.  Return 0 or a negative SSM_E* code; no exceptions, aborts, traps or
  * printing; no CPU fallback.
  */

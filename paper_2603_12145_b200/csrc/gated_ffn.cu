@@ -51,6 +51,7 @@
 #include <cuda_fp16.h>
 
 #include "../../include/gated_ffn.h"
+#include "on_device.cuh"
 #include "sm100.cuh"
 
 namespace {
@@ -1195,6 +1196,7 @@ int gated_ffn_create(gated_ffn **out, int model, int hidden, int activation, int
 int gated_ffn_destroy(gated_ffn *p)
 {
     if (p == nullptr) return GATED_FFN_ENULL;
+    const OnDevice on(p->device);
     cudaStreamSynchronize(p->stream);
     cudaFree(p->err);
     delete p;
@@ -1234,6 +1236,8 @@ int gated_ffn_forward(gated_ffn *p, const void *x, int64_t x_stride, const void 
     const size_t need = gated_ffn_workspace_bytes(p, n, 0);
     if (need > 0 && workspace == nullptr) return GATED_FFN_ENULL;
     if (need > workspace_bytes) return GATED_FFN_ENOMEM;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GATED_FFN_ECUDA;
     float *scratch = static_cast<float *>(workspace);
     return p->type == GATED_FFN_BF16
                ? run_forward<__nv_bfloat16>(p, x, x_stride, w_in, w_out, pre, hidden, y, y_stride, scratch, n)
@@ -1258,6 +1262,8 @@ int gated_ffn_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const vo
                           static_cast<const void *>(workspace)})
         if (!aligned16(v)) return GATED_FFN_EALIGN;
     if (gated_ffn_workspace_bytes(p, n, 1) > workspace_bytes) return GATED_FFN_ENOMEM;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GATED_FFN_ECUDA;
     uint8_t *scratch = static_cast<uint8_t *>(workspace);
     return p->type == GATED_FFN_BF16 ? run_backward<__nv_bfloat16>(p, dy, dy_stride, x, x_stride, w_in, w_out, pre,
                                                                    hidden, dx, dx_stride, dw_in, dw_out, scratch, n)
@@ -1268,7 +1274,8 @@ int gated_ffn_backward(gated_ffn *p, const void *dy, int64_t dy_stride, const vo
 int gated_ffn_status(gated_ffn *p)
 {
     if (p == nullptr) return GATED_FFN_ENULL;
-    if (cudaStreamSynchronize(p->stream) != cudaSuccess) return GATED_FFN_ECUDA;
+    const OnDevice on(p->device);
+    if (!on.ok() || cudaStreamSynchronize(p->stream) != cudaSuccess) return GATED_FFN_ECUDA;
     int flag = 0;
     if (cudaMemcpy(&flag, p->err, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return GATED_FFN_ECUDA;
     if (flag != 0) {

@@ -1,13 +1,14 @@
 // ssm_api.cu -- the C ABI of ssm.h: checks, workspaces, launches.
 #include <new>
 
+#include "on_device.cuh"
 #include "ssm_kernels.cuh"
 
 using namespace ssm_k;
 
 struct ssm {
     int channels = 0, states = 0, groups = 0, width = 0, type = 0;
-    int sms = 0;
+    int device = 0, sms = 0;
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
 };
@@ -233,6 +234,8 @@ int scan(ssm *p, const ssm_scan_args *a, bool backward)
 {
     const int rc = check_scan(p, a, backward);
     if (rc != SSM_OK) return rc;
+    const OnDevice on(p->device);
+    if (!on.ok()) return SSM_ECUDA;
     if (p->type == SSM_F32) return run_scan<float>(p, a, backward);
     return p->type == SSM_BF16 ? run_scan<__nv_bfloat16>(p, a, backward) : run_scan<__half>(p, a, backward);
 }
@@ -322,6 +325,8 @@ int conv(ssm *p, const ssm_conv_args *a, bool backward)
 {
     const int rc = check_conv(p, a, backward);
     if (rc != SSM_OK) return rc;
+    const OnDevice on(p->device);
+    if (!on.ok()) return SSM_ECUDA;
     if (p->type == SSM_F32) return run_conv<float>(p, a, backward);
     return p->type == SSM_BF16 ? run_conv<__nv_bfloat16>(p, a, backward) : run_conv<__half>(p, a, backward);
 }
@@ -350,6 +355,7 @@ int ssm_create(ssm **out, int channels, int states, int groups, int width, int t
     p->groups = groups;
     p->width = width;
     p->type = type;
+    p->device = device;
     p->sms = sms;
     *out = p;
     return SSM_OK;
@@ -397,6 +403,8 @@ int ssm_conv_step(ssm *p, const void *x, int64_t x_stride, const uint8_t *done, 
     s.width = p->width;
     s.sms = p->sms;
     const ConvParams k = {w, bias, nullptr, nullptr, nullptr};
+    const OnDevice on(p->device);
+    if (!on.ok()) return SSM_ECUDA;
     int launched;
     auto call = [&](auto zero) {
         using T = decltype(zero);
@@ -453,6 +461,8 @@ int ssm_scan_step(ssm *p, const void *x, int64_t x_stride, const void *dt, int64
     if (!aligned(state, 16) || !aligned(state_out, 16)) return SSM_EALIGN;
     const StepParams k = {a, d, dt_bias, state, state_out, done, x_stride, dt_stride, z_stride, b_stride, c_stride,
                           y_stride, done_stride, n, p->channels, p->states, p->channels / p->groups, p->sms};
+    const OnDevice on(p->device);
+    if (!on.ok()) return SSM_ECUDA;
     int launched;
     auto call = [&](auto zero) {
         using T = decltype(zero);

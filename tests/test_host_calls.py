@@ -1,0 +1,146 @@
+"""The host side of the C entry points against a stand-in for the CUDA runtime (fake_cudart.c), which
+writes down every call with the device that is current: no GPU, and more devices than a machine has.
+A library is loaded in a process of its own whose libcudart is the stand-in."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    """Directory with the stand-in as libcudart.so.12."""
+    where = tmp_path_factory.mktemp("fake_cudart")
+    (where / "versions").write_text("libcudart.so.12 { global: *; };\n")
+    subprocess.run(["gcc", "-shared", "-fPIC", "-O1", "-I" + os.path.join(CUDA, "include"),
+                    os.path.join(HERE, "fake_cudart.c"), "-o", str(where / "libcudart.so.12"),
+                    "-Wl,-soname,libcudart.so.12", "-Wl,--version-script=" + str(where / "versions")], check=True)
+    return str(where)
+
+
+def child(fake, name):
+    """Runs the function of this file in a process that loads the stand-in."""
+    env = dict(os.environ, LD_LIBRARY_PATH=fake + os.pathsep + os.environ.get("LD_LIBRARY_PATH", ""), PYTHONPATH=ROOT)
+    run = subprocess.run([sys.executable, os.path.abspath(__file__), name, os.path.join(fake, "libcudart.so.12")],
+                         cwd=ROOT, env=env, capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0, run.stdout + run.stderr
+
+
+@pytest.mark.parametrize("library", ["ssm", "gated_ffn"])
+def test_calls_go_to_the_handles_device(fake, library):
+    """A handle of device 1, called while device 0 is current, with the default stream (whose value is 0 on
+    every device) and with another: everything happens on device 1, and device 0 is current again."""
+    child(fake, "device_" + library)
+
+
+# ---- in the child: the libraries' own bindings, addresses instead of tensors ---------
+
+class Fake:
+    def __init__(self, path):
+        self.lib = ctypes.CDLL(path)
+        self.lib.fake_what.restype = ctypes.c_char_p
+        self.lib.fake_stream.restype = ctypes.c_void_p
+        self.lib.fake_stream.argtypes = [ctypes.c_int]
+
+    def current(self):
+        v = ctypes.c_int(-1)
+        self.lib.cudaGetDevice(ctypes.byref(v))
+        return v.value
+
+    def entries(self):
+        L = self.lib
+        return [(L.fake_what(i).decode(), L.fake_device(i), L.fake_stream(i) or 0, L.fake_blocks(i))
+                for i in range(L.fake_count())]
+
+    def on_device_one(self, where, calls, set_stream):
+        """calls: (name, function) each; every one has to do something, all of it on device 1."""
+        for stream in (None, 0x5000):
+            assert set_stream(stream) == 0
+            for name, call in calls:
+                self.lib.cudaSetDevice(0)
+                self.lib.fake_clear()
+                code = call()
+                assert code == 0, (where, name, code)
+                seen = self.entries()
+                assert seen, (where, name, "did nothing")
+                wrong = [e for e in seen if e[1] != 1]
+                assert not wrong, (where, name, "on another device than the handle's", wrong)
+                assert all(e[2] == (stream or 0) for e in seen if e[0] == "launch"), (where, name, seen)
+                assert self.current() == 0, (where, name, "left another device current")
+
+
+def address(i):
+    return 0x40000000 + 0x1000000 * i
+
+
+def scan_args(ssm, op, batch, time, channels, states, groups=1):
+    """A scan's arguments with every tensor present, [batch][time] order."""
+    a = ssm.ScanArgs(batch=batch, time=time)
+    wide = lambda i: ssm.Seq(address(i), time * channels, channels)                          # noqa: E731
+    narrow = lambda i: ssm.Seq(address(i), time * groups * states, groups * states)          # noqa: E731
+    a.x, a.dt, a.z, a.y, a.dy, a.dx, a.ddt, a.dz = [wide(i) for i in range(8)]
+    a.b, a.c, a.db, a.dc = [narrow(i) for i in range(8, 12)]
+    a.reset = ssm.Seq(address(12), time, 1)
+    for i, key in enumerate(("a", "d", "dt_bias", "state", "state_out", "saved", "dstate_out", "da", "dd", "ddt_bias", "dstate")):
+        setattr(a, key, address(13 + i))
+    a.workspace, a.workspace_bytes = address(30), 1 << 40
+    return a
+
+
+def conv_args(ssm, batch, time, channels):
+    a = ssm.ConvArgs(batch=batch, time=time)
+    a.x, a.y, a.dy, a.dx = [ssm.Seq(address(i), time * channels, channels) for i in range(4)]
+    a.reset = ssm.Seq(address(4), time, 1)
+    for i, key in enumerate(("w", "bias", "history", "history_out", "dw", "dbias")):
+        setattr(a, key, address(5 + i))
+    a.workspace, a.workspace_bytes = address(30), 1 << 40
+    return a
+
+
+def device_ssm(fake):
+    from paper_2603_12145_b200 import ssm
+    L = ssm.load()
+    fake.lib.cudaSetDevice(1)
+    h = ssm.ssm_create(96, 16, 1, 4, 1)
+    p = address
+    for batch, time in ((700, 40), (1, 500)):      # uncut, and cut along the time axis: one kernel, and several
+        a, c = scan_args(ssm, h, batch, time, 96, 16), conv_args(ssm, batch, time, 96)
+        step = (h, p(0), 96, p(1), 96, p(2), 96, p(3), 16, p(4), 16, p(5), 1, p(6), p(7), p(8), p(9), p(10), p(11), 96, 5)
+        fake.on_device_one("ssm", [
+            ("scan_forward", lambda: L.ssm_scan_forward(h, ctypes.byref(a))),
+            ("scan_backward", lambda: L.ssm_scan_backward(h, ctypes.byref(a))),
+            ("scan_step", lambda: L.ssm_scan_step(*step)),
+            ("conv_forward", lambda: L.ssm_conv_forward(h, ctypes.byref(c))),
+            ("conv_backward", lambda: L.ssm_conv_backward(h, ctypes.byref(c))),
+            ("conv_step", lambda: L.ssm_conv_step(h, p(0), 96, p(1), 1, p(2), p(3), p(4), p(5), p(6), 96, 5)),
+        ], lambda s: L.ssm_set_stream(h, s))
+
+
+def device_gated_ffn(fake):
+    from paper_2603_12145_b200 import gated_ffn
+    L = gated_ffn.load()
+    p = address
+    for type_ in (0, 1):
+        fake.lib.cudaSetDevice(1)
+        h = gated_ffn.gated_ffn_create(200, 136, type_, type_)
+        calls = []
+        for n in (5, 300):                          # the streaming kernel, and the tiles
+            calls += [("forward %d" % n, lambda n=n: L.gated_ffn_forward(h, p(0), 200, p(1), p(2), p(3), p(4), p(5), 200, p(6),
+                                                                         1 << 30, n)),
+                      ("backward %d" % n, lambda n=n: L.gated_ffn_backward(h, p(7), 200, p(0), 200, p(1), p(2), p(3), p(4), p(5),
+                                                                           200, p(8), p(9), p(6), 1 << 30, n))]
+        fake.on_device_one("gated_ffn", calls + [("status", lambda: L.gated_ffn_status(h))],
+                           lambda s: L.gated_ffn_set_stream(h, s))
+        fake.lib.fake_clear()
+        assert L.gated_ffn_destroy(h) == 0
+        assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
+
+
+if __name__ == "__main__":
+    globals()[sys.argv[1]](Fake(sys.argv[2]))
