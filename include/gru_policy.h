@@ -45,7 +45,8 @@
  * rows = output units, gate blocks of w_ih / w_hh / b_ih / b_hh in the order
  * r, z, n; the library keeps its own device copies.  Every other pointer is a
  * DEVICE pointer owned by the caller; x and h buffers hold bfloat16 [n][H],
- * row-major, 16-byte aligned.  Calls enqueue on the handle's stream and return
+ * row-major, 16-byte aligned.  Calls enqueue on the handle's stream, on the device that
+ * was current when the handle was created (whichever is current now stays so), and return
  * (gru_policy_status synchronises).  The library allocates only in
  * gru_policy_create.  Return 0 or a negative GRU_POLICY_E* code; no exceptions,
  * aborts, traps or printing; no CPU fallback.

@@ -47,6 +47,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/gru_policy.h"
+#include "on_device.cuh"
 #include "sm100.cuh"
 
 namespace {
@@ -826,6 +827,7 @@ int gru_policy_create(gru_policy **out, int hidden, int obs_dim, int n_actions, 
 int gru_policy_destroy(gru_policy *p)
 {
     if (p == nullptr) return GRU_POLICY_ENULL;
+    const OnDevice on(p->device);
     cudaStreamSynchronize(p->stream);
     release(p);
     return GRU_POLICY_OK;
@@ -844,6 +846,8 @@ int gru_policy_encode(gru_policy *p, const float *obs, const uint8_t *done, void
     if (n < 1) return GRU_POLICY_EINVAL;
     if ((reinterpret_cast<uintptr_t>(x_out) | reinterpret_cast<uintptr_t>(h)) % 16 != 0) return GRU_POLICY_EALIGN;
     if (reinterpret_cast<uintptr_t>(obs) % 8 != 0) return GRU_POLICY_EALIGN;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GRU_POLICY_ECUDA;
     const int cols = EncodeTable<GRU_POLICY_MAX_OBS>::cols(p->obs_dim);
     const int threads = encode_threads(p->H, cols);
     EncodeKernel kernel = EncodeTable<GRU_POLICY_MAX_OBS>::get(p->obs_dim);
@@ -883,6 +887,8 @@ static int launch_cell(gru_policy *p, const void *x, const void *h_in, void *h_o
          reinterpret_cast<uintptr_t>(h_out) | reinterpret_cast<uintptr_t>(partial)) % 16 != 0)
         return GRU_POLICY_EALIGN;
     if (h_out == x || h_out == h_in) return GRU_POLICY_EINVAL;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GRU_POLICY_ECUDA;
     TensorMapEncodeFn enc = tensor_map_encoder();
     CUtensorMap tm_x, tm_h;
     if (!encode_operand(enc, &tm_x, x, p->H, n, kBM) || !encode_operand(enc, &tm_h, h_in, p->H, n, kBM))
@@ -941,6 +947,8 @@ int gru_policy_cell_head(gru_policy *p, const void *x, const void *h_in, void *h
 {
     if (p == nullptr || logits == nullptr || workspace == nullptr) return GRU_POLICY_ENULL;
     if (p->A > 4 || cell_smem_bytes(p->H, true) > kMaxSmem) return GRU_POLICY_EINVAL;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GRU_POLICY_ECUDA;
     const int rc = launch_cell(p, x, h_in, h_out, static_cast<float4 *>(workspace), n);
     if (rc != GRU_POLICY_OK) return rc;
     k_head_reduce<<<(n + 255) / 256, 256, 0, p->stream>>>(static_cast<const float4 *>(workspace), logits,
@@ -955,6 +963,8 @@ int gru_policy_head(gru_policy *p, const void *h, float *logits, int n)
     if (p == nullptr || h == nullptr || logits == nullptr) return GRU_POLICY_ENULL;
     if (n < 1) return GRU_POLICY_EINVAL;
     if (reinterpret_cast<uintptr_t>(h) % 16 != 0) return GRU_POLICY_EALIGN;
+    const OnDevice on(p->device);
+    if (!on.ok()) return GRU_POLICY_ECUDA;
     const unsigned blocks = static_cast<unsigned>((n + kHeadRows - 1) / kHeadRows);
     (p->A <= 4 ? k_head<4> : k_head<8>)<<<blocks, kHeadRows, head_smem_bytes(p->A, p->H), p->stream>>>(
         static_cast<const __nv_bfloat16 *>(h), logits, p->head_w, p->head_b, n, p->H, p->A);
@@ -966,7 +976,8 @@ int gru_policy_head(gru_policy *p, const void *h, float *logits, int n)
 int gru_policy_status(gru_policy *p)
 {
     if (p == nullptr) return GRU_POLICY_ENULL;
-    if (cudaStreamSynchronize(p->stream) != cudaSuccess) return GRU_POLICY_ECUDA;
+    const OnDevice on(p->device);
+    if (!on.ok() || cudaStreamSynchronize(p->stream) != cudaSuccess) return GRU_POLICY_ECUDA;
     int flag = 0;
     if (cudaMemcpy(&flag, p->err, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return GRU_POLICY_ECUDA;
     if (flag != 0) {

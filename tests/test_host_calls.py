@@ -32,7 +32,7 @@ def child(fake, name):
     assert run.returncode == 0, run.stdout + run.stderr
 
 
-@pytest.mark.parametrize("library", ["ssm", "gated_ffn"])
+@pytest.mark.parametrize("library", ["ssm", "gated_ffn", "gru_policy"])
 def test_calls_go_to_the_handles_device(fake, library):
     """A handle of device 1, called while device 0 is current, with the default stream (whose value is 0 on
     every device) and with another: everything happens on device 1, and device 0 is current again."""
@@ -140,6 +140,32 @@ def device_gated_ffn(fake):
         fake.lib.fake_clear()
         assert L.gated_ffn_destroy(h) == 0
         assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
+
+
+def host(np, *shape):
+    v = np.zeros(shape, dtype=np.float32)
+    return v, v.ctypes.data
+
+
+def device_gru_policy(fake):
+    import numpy as np
+    from paper_2603_12145_b200 import gru_policy
+    L = gru_policy.load()
+    shapes = {"enc_w": (64, 6), "enc_b": (64,), "w_ih": (192, 64), "w_hh": (192, 64), "b_ih": (192,), "b_hh": (192,),
+              "head_w": (3, 64), "head_b": (3,)}
+    fake.lib.cudaSetDevice(1)
+    h = gru_policy.gru_policy_create(64, 6, 3, {k: np.zeros(v, dtype=np.float32) for k, v in shapes.items()})
+    p = address
+    fake.on_device_one("gru_policy", [
+        ("encode", lambda: L.gru_policy_encode(h, p(0), p(1), p(2), p(3), 300)),
+        ("cell", lambda: L.gru_policy_cell(h, p(0), p(1), p(2), 300)),
+        ("cell_head", lambda: L.gru_policy_cell_head(h, p(0), p(1), p(2), p(3), p(4), 300)),
+        ("head", lambda: L.gru_policy_head(h, p(0), p(1), 300)),
+        ("status", lambda: L.gru_policy_status(h)),
+    ], lambda s: L.gru_policy_set_stream(h, s))
+    fake.lib.fake_clear()
+    assert L.gru_policy_destroy(h) == 0
+    assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
 
 
 if __name__ == "__main__":
