@@ -60,7 +60,8 @@
  *     pong_destroy.
  *   - step / rollout / fill_actions / reset only enqueue work on the handle's
  *     stream and return; episode_stats / get_state / set_state / the *_host
- *     call synchronise that stream.
+ *     call synchronise that stream.  All of it happens on the device that was
+ *     current when the handle was created; whichever is current now stays so.
  *   - Every function returns 0 or a negative PONG_E* code; nothing throws,
  *     aborts, traps or prints.  There is no CPU fallback: without a usable
  *     CUDA device pong_create* fails with PONG_ECUDA.

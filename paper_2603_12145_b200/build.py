@@ -15,8 +15,8 @@ NVCC_FLAGS = ["-std=c++17", "-O3", "-lineinfo",
 # library -> (sources, other files it depends on)
 TARGETS = {
     "libpong_b200.so": (["pong_api.cu", "pong_kernels.cu", "pong_noalloc.cu"],
-                        ["pong_rules.cuh", "pong_kernels.cuh", os.path.join(INCLUDE, "pong.h")]),
-    "libcartpole_b200.so": (["cartpole.cu"], [os.path.join(INCLUDE, "cartpole.h")]),
+                        ["pong_rules.cuh", "pong_kernels.cuh", "on_device.cuh", os.path.join(INCLUDE, "pong.h")]),
+    "libcartpole_b200.so": (["cartpole.cu"], ["on_device.cuh", os.path.join(INCLUDE, "cartpole.h")]),
     "libgru_policy_b200.so": (["gru_policy.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gru_policy.h")]),
     "libgated_ffn_b200.so": (["gated_ffn.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_ffn.h")]),
     "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],

@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include "../../include/cartpole.h"
+#include "on_device.cuh"
 
 namespace cartpole {
 
@@ -383,6 +384,7 @@ struct cartpole_env {
     int n = 0;
     uint64_t seed = 0;
     int env_id_base = 0;
+    int device = 0;
     cudaStream_t stream = nullptr;
     void *block = nullptr;
     float4 *plane_f = nullptr;
@@ -419,6 +421,8 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int do_reset(cartpole_env *h, float *obs_out)
 {
     if (obs_out != nullptr && !aligned16(obs_out)) return CARTPOLE_EALIGN;
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     if (cudaMemsetAsync(h->stats, 0, 2 * sizeof(long long), h->stream) != cudaSuccess) return CARTPOLE_ECUDA;
     h->t = 0;
     cartpole::Args a = base_args(h);
@@ -448,6 +452,8 @@ int check_args(const cartpole_env *h, int T, int mode, const uint8_t *actions, c
 int do_rollout(cartpole_env *h, int T, int mode, const uint8_t *actions, int const_action, float *obs,
                float *reward, uint8_t *done)
 {
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     cartpole::Args a = base_args(h);
     a.T = T;
     a.action_mode = mode;
@@ -519,9 +525,8 @@ int cartpole_create(cartpole_env **out, int n_envs, uint64_t seed, int env_id_ba
     h->seed = seed;
     h->env_id_base = env_id_base;
     {
-        int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess ||
-            cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || h->sms < 1) {
+        if (cudaGetDevice(&h->device) != cudaSuccess ||
+            cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device) != cudaSuccess || h->sms < 1) {
             cudaGetLastError();
             delete h;
             return CARTPOLE_ECUDA;
@@ -554,6 +559,7 @@ int cartpole_create(cartpole_env **out, int n_envs, uint64_t seed, int env_id_ba
 int cartpole_destroy(cartpole_env *h)
 {
     if (h == nullptr) return CARTPOLE_OK;
+    const OnDevice on(h->device);
     int rc = CARTPOLE_OK;
     if (cudaStreamSynchronize(h->stream) != cudaSuccess) rc = CARTPOLE_ECUDA;
     if (h->stage != nullptr && cudaFree(h->stage) != cudaSuccess) rc = CARTPOLE_ECUDA;
@@ -599,6 +605,8 @@ int cartpole_rollout_host(cartpole_env *h, int T, int action_mode, const uint8_t
     int const_action = 0;
     const int rc = check_args(h, T, action_mode, actions_host, obs_host, reward_host, done_host, &const_action);
     if (rc != CARTPOLE_OK) return rc;
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     const size_t tn = (size_t)T * (size_t)h->n;
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
     const size_t off_reward = up(tn * 16), off_done = off_reward + up(tn * 4), off_act = off_done + up(tn);
@@ -638,6 +646,8 @@ int cartpole_rollout_host(cartpole_env *h, int T, int action_mode, const uint8_t
 int cartpole_episode_stats(cartpole_env *h, int64_t *episodes, int64_t *sum_length, int clear)
 {
     if (h == nullptr) return CARTPOLE_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     long long v[2] = {0, 0};
     if (cudaMemcpyAsync(v, h->stats, sizeof(v), cudaMemcpyDeviceToHost, h->stream) != cudaSuccess)
         return CARTPOLE_ECUDA;
@@ -651,6 +661,8 @@ int cartpole_episode_stats(cartpole_env *h, int64_t *episodes, int64_t *sum_leng
 int cartpole_get_state(cartpole_env *h, float *host_f, int32_t *host_i, uint64_t *t)
 {
     if (h == nullptr || host_f == nullptr || host_i == nullptr) return CARTPOLE_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     const size_t n = (size_t)h->n;
     std::vector<float4> f;
     std::vector<int2> i;
@@ -679,6 +691,8 @@ int cartpole_get_state(cartpole_env *h, float *host_f, int32_t *host_i, uint64_t
 int cartpole_set_state(cartpole_env *h, const float *host_f, const int32_t *host_i, uint64_t t)
 {
     if (h == nullptr || host_f == nullptr || host_i == nullptr) return CARTPOLE_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return CARTPOLE_ECUDA;
     const size_t n = (size_t)h->n;
     std::vector<float4> f;
     std::vector<int2> i;

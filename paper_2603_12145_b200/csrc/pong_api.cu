@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "../../include/pong.h"
+#include "on_device.cuh"
 #include "pong_kernels.cuh"
 
 struct pong_env {
@@ -54,6 +55,8 @@ pong::LaunchArgs base_args(const pong_env *h)
 int do_reset(pong_env *h, void *obs_out)
 {
     if (obs_out != nullptr && !aligned(obs_out, 16)) return PONG_EALIGN;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     if (cudaMemsetAsync(h->stats, 0, 3 * sizeof(long long), h->stream) != cudaSuccess) return PONG_ECUDA;
     h->t = 0;
     pong::LaunchArgs a = base_args(h);
@@ -69,6 +72,8 @@ int do_reset(pong_env *h, void *obs_out)
 int do_rollout(pong_env *h, int T, int action_mode, const uint8_t *actions, int const_action,
                void *obs, float *reward, uint8_t *done)
 {
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     pong::LaunchArgs a = base_args(h);
     a.T = T;
     a.action_mode = action_mode;
@@ -169,6 +174,7 @@ int pong_create(pong_env **out, int n_envs, uint64_t seed)
 int pong_destroy(pong_env *h)
 {
     if (h == nullptr) return PONG_OK;
+    const OnDevice on(h->device);
     int rc = PONG_OK;
     if (cudaStreamSynchronize(h->stream) != cudaSuccess) rc = PONG_ECUDA;
     if (h->stage != nullptr && cudaFree(h->stage) != cudaSuccess) rc = PONG_ECUDA;
@@ -224,6 +230,8 @@ int pong_rollout_host(pong_env *h, int T, int action_mode, const uint8_t *action
     const int rc = check_rollout_args(h, T, action_mode, actions_host, obs_host, reward_host,
                                       done_host, &const_action);
     if (rc != PONG_OK) return rc;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     const size_t tn = (size_t)T * (size_t)h->n;
     const bool vec = h->cfg.obs_mode == PONG_OBS_VECTOR;
     const size_t obs_bytes = vec ? tn * 6 * sizeof(float) : (size_t)h->n * 4 * PONG_FRAME_BYTES;
@@ -273,6 +281,8 @@ int pong_fill_actions(pong_env *h, int T, int sticky, uint8_t *actions_out)
 {
     if (h == nullptr || actions_out == nullptr) return PONG_ENULL;
     if (T < 1 || (uint64_t)T * (uint64_t)h->n > (1ull << 40)) return PONG_EINVAL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     pong::LaunchArgs a = base_args(h);
     a.T = T;
     const cudaError_t err = pong::launch_fill_actions(a, sticky != 0, actions_out, h->stream);
@@ -286,6 +296,8 @@ int pong_fill_words(pong_env *h, int T, uint32_t *words_out)
 {
     if (h == nullptr || words_out == nullptr) return PONG_ENULL;
     if (T < 1 || (uint64_t)T * (uint64_t)h->n > (1ull << 40)) return PONG_EINVAL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     pong::LaunchArgs a = base_args(h);
     a.T = T;
     if (pong::launch_fill_words(a, words_out, h->stream) != cudaSuccess) return PONG_ECUDA;
@@ -297,6 +309,8 @@ int pong_fill_words(pong_env *h, int T, uint32_t *words_out)
 int pong_sample_actions(pong_env *h, const float *logits, const uint32_t *words, uint8_t *actions_out)
 {
     if (h == nullptr || logits == nullptr || words == nullptr || actions_out == nullptr) return PONG_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     if (pong::launch_sample_actions(h->n, logits, words, actions_out, h->stream) != cudaSuccess)
         return PONG_ECUDA;
     h->launches += 1;
@@ -321,6 +335,8 @@ int pong_episode_stats(pong_env *h, int64_t *episodes, int64_t *sum_return, int6
                        int clear)
 {
     if (h == nullptr) return PONG_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     long long v[3] = {0, 0, 0};
     if (cudaMemcpyAsync(v, h->stats, sizeof(v), cudaMemcpyDeviceToHost, h->stream) != cudaSuccess)
         return PONG_ECUDA;
@@ -335,6 +351,8 @@ int pong_episode_stats(pong_env *h, int64_t *episodes, int64_t *sum_return, int6
 int pong_get_state(pong_env *h, int32_t *host_soa, uint64_t *t)
 {
     if (h == nullptr || host_soa == nullptr) return PONG_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     const size_t n = (size_t)h->n;
     std::vector<int4> planes;
     try {
@@ -367,6 +385,8 @@ int pong_get_state(pong_env *h, int32_t *host_soa, uint64_t *t)
 int pong_set_state(pong_env *h, const int32_t *s, uint64_t t)
 {
     if (h == nullptr || s == nullptr) return PONG_ENULL;
+    const OnDevice on(h->device);
+    if (!on.ok()) return PONG_ECUDA;
     const size_t n = (size_t)h->n;
     std::vector<int4> planes;
     try {

@@ -32,7 +32,7 @@ def child(fake, name):
     assert run.returncode == 0, run.stdout + run.stderr
 
 
-@pytest.mark.parametrize("library", ["ssm", "gated_ffn", "gru_policy"])
+@pytest.mark.parametrize("library", ["ssm", "gated_ffn", "gru_policy", "pong", "cartpole"])
 def test_calls_go_to_the_handles_device(fake, library):
     """A handle of device 1, called while device 0 is current, with the default stream (whose value is 0 on
     every device) and with another: everything happens on device 1, and device 0 is current again."""
@@ -166,6 +166,64 @@ def device_gru_policy(fake):
     fake.lib.fake_clear()
     assert L.gru_policy_destroy(h) == 0
     assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
+
+
+def device_pong(fake):
+    import numpy as np
+    from paper_2603_12145_b200 import pong
+    L = pong.load()
+    p, n = address, 200
+    for pixels in (0, 1):
+        h = ctypes.c_void_p()
+        fake.lib.cudaSetDevice(1)
+        assert L.pong_create_ex(ctypes.byref(h), n, 7, ctypes.byref(pong._Config(pixels, 1, 0))) == 0
+        keep, obs = host(np, n * 4 * 84 * 84 + 8 * n * 6)
+        rest, reward = host(np, 8 * n)
+        state, got = np.zeros((11, n), dtype=np.int32), np.zeros((11, n), dtype=np.int32)
+        state[2] = 512                               # the ball's speed at a serve
+        fake.on_device_one("pong", [
+            ("reset", lambda: L.pong_reset(h, p(0))),
+            ("step", lambda: L.pong_step(h, p(3), p(0), p(1), p(2))),
+            ("rollout", lambda: L.pong_rollout(h, 8, 0, None, p(0), p(1), p(2))),
+            ("rollout_host", lambda: L.pong_rollout_host(h, 8, 0, None, obs, reward, reward)),
+            ("fill_actions", lambda: L.pong_fill_actions(h, 8, 0, p(0))),
+            ("fill_words", lambda: L.pong_fill_words(h, 8, p(0))),
+            ("sample_actions", lambda: L.pong_sample_actions(h, p(0), p(1), p(2))),
+            ("episode_stats", lambda: L.pong_episode_stats(h, None, None, None, 1)),
+            ("get_state", lambda: L.pong_get_state(h, got.ctypes.data, None)),
+            ("set_state", lambda: L.pong_set_state(h, state.ctypes.data, 0)),
+        ], lambda s: L.pong_set_stream(h, s))
+        fake.lib.fake_clear()
+        assert L.pong_destroy(h) == 0
+        assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
+        del keep, rest
+
+
+def device_cartpole(fake):
+    import numpy as np
+    from paper_2603_12145_b200 import cartpole
+    L = cartpole.load()
+    p = address
+    for n in (200, 65536):                           # blocks, and the balanced chains with their own limit
+        h = ctypes.c_void_p()
+        fake.lib.cudaSetDevice(1)
+        assert L.cartpole_create(ctypes.byref(h), n, 7, 0) == 0
+        keep, obs = host(np, 8 * n * 4)
+        rest, reward = host(np, 8 * n)
+        f, i = np.zeros((4, n), dtype=np.float32), np.zeros((2, n), dtype=np.int32)
+        fake.on_device_one("cartpole", [
+            ("reset", lambda: L.cartpole_reset(h, p(0))),
+            ("step", lambda: L.cartpole_step(h, p(3), p(0), p(1), p(2))),
+            ("rollout", lambda: L.cartpole_rollout(h, 8, 0, None, p(0), p(1), p(2))),
+            ("rollout_host", lambda: L.cartpole_rollout_host(h, 8, 0, None, obs, reward, reward)),
+            ("episode_stats", lambda: L.cartpole_episode_stats(h, None, None, 1)),
+            ("get_state", lambda: L.cartpole_get_state(h, f.ctypes.data, i.ctypes.data, None)),
+            ("set_state", lambda: L.cartpole_set_state(h, f.ctypes.data, i.ctypes.data, 0)),
+        ], lambda s: L.cartpole_set_stream(h, s))
+        fake.lib.fake_clear()
+        assert L.cartpole_destroy(h) == 0
+        assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
+        del keep, rest
 
 
 if __name__ == "__main__":
