@@ -20,11 +20,41 @@ torch.autograd through the Functions below.
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
 
 from . import gated_ffn, pong, ssm
+
+
+class _Refuse(torch.autograd.Function):
+    """A gradient that itself depends on `of` in a way that autograd does not know."""
+
+    @staticmethod
+    def forward(ctx, gradient, *of):
+        return gradient
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise RuntimeError("the sequence operators have first derivatives only: this gradient was asked for its own")
+
+
+def first_order(backward):
+    """For a Function whose backward calls kernels.  With create_graph the gradients would look like constants, and
+    a second derivative would silently lack what goes through the operator; here it raises.  (once_differentiable
+    does so only where the incoming gradient carries a graph, not where the inputs alone do.)"""
+
+    @functools.wraps(backward)
+    def wrapped(ctx, dy):
+        with torch.no_grad():
+            grads = backward(ctx, dy)
+        if not torch.is_grad_enabled():
+            return grads
+        of = [v for v in (dy,) + tuple(ctx.saved_tensors) if v is not None and v.requires_grad]
+        return tuple(_Refuse.apply(g, *of) if g is not None and of else g for g in grads)
+
+    return wrapped
 
 
 class ConvFunction(torch.autograd.Function):
@@ -37,6 +67,7 @@ class ConvFunction(torch.autograd.Function):
         return op.conv(x, w, bias, reset=reset, history=history, history_out=history_out)
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         x, w, bias = ctx.saved_tensors
         dx, dw, dbias = ctx.op.conv_backward(_dense_last(dy), x, w, bias, reset=ctx.reset, history=ctx.history)
@@ -55,6 +86,7 @@ class ScanFunction(torch.autograd.Function):
                        saved=saved)
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         x, dt, a, b, c, d, z, dt_bias, saved = ctx.saved_tensors
         g = ctx.op.scan_backward(_dense_last(dy), x, dt, a, b, c, saved, d=d, z=z, dt_bias=dt_bias, reset=ctx.reset)
@@ -72,6 +104,7 @@ class FfnFunction(torch.autograd.Function):
         return op.forward(x, w_in, w_out, saved=saved)
 
     @staticmethod
+    @first_order
     def backward(ctx, dy):
         x, w_in, w_out = ctx.saved_tensors
         return (None,) + ctx.op.backward(dy.contiguous(), x, w_in, w_out, ctx.kept)
