@@ -24,6 +24,7 @@ import functools
 import math
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import gated_ffn, pong, ssm
 
@@ -62,15 +63,15 @@ class ConvFunction(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, op, x, w, bias, reset, history, history_out):
-        ctx.op, ctx.reset, ctx.history = op, reset, history
-        ctx.save_for_backward(x, w, bias)
+        ctx.op = op
+        ctx.save_for_backward(x, w, bias, reset, history)
         return op.conv(x, w, bias, reset=reset, history=history, history_out=history_out)
 
     @staticmethod
     @first_order
     def backward(ctx, dy):
-        x, w, bias = ctx.saved_tensors
-        dx, dw, dbias = ctx.op.conv_backward(_dense_last(dy), x, w, bias, reset=ctx.reset, history=ctx.history)
+        x, w, bias, reset, history = ctx.saved_tensors
+        dx, dw, dbias = ctx.op.conv_backward(_dense_last(dy), x, w, bias, reset=reset, history=history)
         return None, dx, dw, dbias, None, None, None
 
 
@@ -80,16 +81,16 @@ class ScanFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out):
         saved = op.saved(x.shape[0], x.shape[1])
-        ctx.op, ctx.reset = op, reset
-        ctx.save_for_backward(x, dt, a, b, c, d, z, dt_bias, saved)
+        ctx.op = op
+        ctx.save_for_backward(x, dt, a, b, c, d, z, dt_bias, reset, saved)
         return op.scan(x, dt, a, b, c, d=d, z=z, dt_bias=dt_bias, reset=reset, state=state, state_out=state_out,
                        saved=saved)
 
     @staticmethod
     @first_order
     def backward(ctx, dy):
-        x, dt, a, b, c, d, z, dt_bias, saved = ctx.saved_tensors
-        g = ctx.op.scan_backward(_dense_last(dy), x, dt, a, b, c, saved, d=d, z=z, dt_bias=dt_bias, reset=ctx.reset)
+        x, dt, a, b, c, d, z, dt_bias, reset, saved = ctx.saved_tensors
+        g = ctx.op.scan_backward(_dense_last(dy), x, dt, a, b, c, saved, d=d, z=z, dt_bias=dt_bias, reset=reset)
         return (None, g["dx"], g["ddt"], g["da"], g["db"], g["dc"], g["dd"], g["dz"], g["ddt_bias"], None, None, None)
 
 
@@ -99,15 +100,15 @@ class FfnFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, op, x, w_in, w_out):
         saved = op.saved(x.shape[0])
-        ctx.op, ctx.kept = op, saved
-        ctx.save_for_backward(x, w_in, w_out)
+        ctx.op = op
+        ctx.save_for_backward(x, w_in, w_out, *saved)
         return op.forward(x, w_in, w_out, saved=saved)
 
     @staticmethod
     @first_order
     def backward(ctx, dy):
-        x, w_in, w_out = ctx.saved_tensors
-        return (None,) + ctx.op.backward(dy.contiguous(), x, w_in, w_out, ctx.kept)
+        x, w_in, w_out, pre, hidden = ctx.saved_tensors
+        return (None,) + ctx.op.backward(dy.contiguous(), x, w_in, w_out, (pre, hidden))
 
 
 def _dense_last(v):
@@ -161,6 +162,8 @@ class Layer(torch.nn.Module):
     def step(self, w, h, done, state, history):
         """h [n, model] -> [n, model]; state and history are updated in place."""
         x, z = torch.split(h @ w["w_xz"].t(), [self.inner, self.inner], dim=-1)
+        # a training pass that started from these must not go on with what is written here by address
+        increment_version((state, history))
         x = self.op.conv_step(x, history, self.conv_w, self.conv_b, done=done)
         r, b, c = torch.split(x @ w["w_p"].t(), [self.rank, self.states, self.states], dim=-1)
         y = self.op.scan_step(x, r @ w["w_dt"].t(), w["a"], b, c, state, d=self.skip, z=z, dt_bias=self.dt_bias, done=done)

@@ -37,6 +37,12 @@ class StandIn:
         grads["dx"] = saved * x * dy * (1.0 if reset is None else (reset == 0).unsqueeze(-1))
         return grads
 
+    def conv_step(self, x, history, w, bias=None, done=None):
+        return x
+
+    def scan_step(self, x, dt, a, b, c, state, d=None, z=None, dt_bias=None, done=None):
+        return x
+
     # gated_ffn.GatedFfn
     def forward(self, x, w_in, w_out, saved=None):
         if saved is not None:
@@ -75,3 +81,50 @@ def test_first_derivatives_pass_and_second_ones_are_refused(name):
     (g,) = torch.autograd.grad((scale * through(name, StandIn(), x)).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="first derivatives only"):
         torch.autograd.grad(g.sum(), scale)
+
+
+@pytest.mark.parametrize("name,which", [("conv", "reset"), ("conv", "history"), ("scan", "reset")])
+def test_a_mask_or_history_changed_before_the_backward_pass_is_noticed(name, which):
+    x, reset, history = inputs(), torch.tensor([[0, 1, 0]], dtype=torch.uint8), torch.ones(1, 3, 1)
+    more = {"reset": reset}
+    if name == "conv":
+        more["history"] = history
+    y = through(name, StandIn(), x, **more)
+    y.sum().backward(retain_graph=True)                # as it was
+    more[which].zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+
+
+@pytest.mark.parametrize("name", ["conv", "scan", "ffn"])
+def test_saved_tensor_hooks_see_all_that_the_backward_pass_reads(name):
+    """Under hooks that replace what is kept (to move it elsewhere, say), the gradients come from the replacements."""
+    x, reset, history, kept = inputs(), torch.tensor([[0, 1, 0]], dtype=torch.uint8), torch.full((1, 1, 1), 3.0), []
+
+    def pack(v):
+        kept.append(v.detach().clone())
+        return len(kept) - 1
+
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda i: kept[i]):
+        y = through(name, StandIn(), x, *([] if name == "ffn" else [reset] + ([history] if name == "conv" else [])))
+    with torch.no_grad():
+        reset.fill_(1)
+        history.zero_()
+    y.sum().backward()
+    scale, mask = (3.0 if name == "conv" else 1.0), torch.tensor([1.0, 1.0 if name == "ffn" else 0.0, 1.0]).view(1, 3, 1)
+    assert torch.equal(x.grad, 2 * x.detach() * scale * mask)
+    assert len(kept) >= (5 if name == "ffn" else 4)     # inputs, mask and history, the forward call's buffers
+
+
+def test_an_agent_step_between_forward_and_backward_is_noticed(monkeypatch):
+    """The step writes the history by address, which autograd does not see by itself."""
+    op = StandIn()
+    monkeypatch.setattr(ssm_policy.ssm, "Ssm", lambda *args, **kw: op)
+    monkeypatch.setattr(ssm_policy.gated_ffn, "GatedFfn", lambda *args, **kw: op)
+    layer = ssm_policy.Layer(8, 4, 4, 4, 16, "cpu", 0)
+    state, history = torch.zeros((1, 16, 4)), torch.ones((1, 3, 16), dtype=torch.bfloat16)
+    y = layer.sequence(torch.ones((1, 5, 8), dtype=torch.bfloat16, requires_grad=True), None, state, history)
+    with torch.no_grad():
+        layer.step(layer.weights(), torch.ones((1, 8), dtype=torch.bfloat16), None, state, history)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.float().sum().backward()
