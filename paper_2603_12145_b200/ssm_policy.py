@@ -58,6 +58,10 @@ def first_order(backward):
     return wrapped
 
 
+def _wants_gradient(args):
+    return torch.is_grad_enabled() and any(isinstance(v, torch.Tensor) and v.requires_grad for v in args)
+
+
 class ConvFunction(torch.autograd.Function):
     """ssm.Ssm.conv with its gradients; the history is a constant."""
 
@@ -78,6 +82,13 @@ class ConvFunction(torch.autograd.Function):
 class ScanFunction(torch.autograd.Function):
     """ssm.Ssm.scan with its gradients; the state at the start is a constant."""
 
+    @classmethod
+    def apply(cls, op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out):
+        args = (op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out)
+        if _wants_gradient(args):
+            return super().apply(*args)
+        return op.scan(x, dt, a, b, c, d=d, z=z, dt_bias=dt_bias, reset=reset, state=state, state_out=state_out)
+
     @staticmethod
     def forward(ctx, op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out):
         saved = op.saved(x.shape[0], x.shape[1])
@@ -96,6 +107,10 @@ class ScanFunction(torch.autograd.Function):
 
 class FfnFunction(torch.autograd.Function):
     """gated_ffn.GatedFfn on rows [n, model] with its gradients."""
+
+    @classmethod
+    def apply(cls, op, x, w_in, w_out):
+        return super().apply(op, x, w_in, w_out) if _wants_gradient((x, w_in, w_out)) else op.forward(x, w_in, w_out)
 
     @staticmethod
     def forward(ctx, op, x, w_in, w_out):

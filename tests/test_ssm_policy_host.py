@@ -128,3 +128,13 @@ def test_an_agent_step_between_forward_and_backward_is_noticed(monkeypatch):
         layer.step(layer.weights(), torch.ones((1, 8), dtype=torch.bfloat16), None, state, history)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.float().sum().backward()
+
+
+@pytest.mark.parametrize("name", ["scan", "ffn"])
+def test_nothing_is_kept_where_no_gradient_is_wanted(name):
+    op, x = StandIn(), inputs()
+    want = through(name, op, x)
+    assert want.requires_grad and op.asked == 1
+    with torch.no_grad():
+        assert torch.equal(through(name, op, x), want)
+    assert torch.equal(through(name, op, x.detach()), want) and op.asked == 1
