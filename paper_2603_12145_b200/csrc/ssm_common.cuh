@@ -212,11 +212,14 @@ __device__ __forceinline__ Pair ex2(Pair a) { return pair(ex2(lo(a)), ex2(hi(a))
 // leaves 0.11 either way: 1,000 steps at 0.999 end 1.3e-5 high, the final state of 128 training steps is off by
 // 5.8e-7 (1.3e-6 without the addend; with 0.2 units 1.9e-5 and 8.0e-7).  Where the argument is so large that the
 // addend disappears in its rounding, the state forgets within a few steps.
-__device__ __forceinline__ Pair decay(Pair rate, Pair delta)
-{
-    constexpr float kBias = 0.15f * 1.1920929e-7f * kLog2e;
-    return ex2(fma(rate, delta, pair(kBias, kBias)));
-}
+//
+// Every form of the recurrence uses it, so that a rollout taken in single tokens and its training pass go through
+// the same states.
+constexpr float kDecayBias = 0.15f * 1.1920929e-7f * kLog2e;
+
+__device__ __forceinline__ float decay(float rate, float delta) { return ex2(fmaf(rate, delta, kDecayBias)); }
+
+__device__ __forceinline__ Pair decay(Pair rate, Pair delta) { return ex2(fma(rate, delta, pair(kDecayBias, kDecayBias))); }
 
 // ---- the scalar functions on pairs (two steps of a channel): the same arithmetic in half the instructions
 

@@ -599,7 +599,7 @@ k_scan_back_carry(const ScanShape s, const ScanParams p)
             slots[(seg0 - k) * stride] = make_float4(e[0], e[1], e[2], e[3]);
             const float outs[4] = {out[k].x, out[k].y, out[k].z, out[k].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e[i] = span[k] < 0.0f ? outs[i] : fmaf(ex2(a[i] * span[k]), e[i], outs[i]);
+            for (int i = 0; i < 4; ++i) e[i] = span[k] < 0.0f ? outs[i] : fmaf(decay(a[i], span[k]), e[i], outs[i]);
         }
     }
 }

@@ -270,7 +270,7 @@ k_scan_carry(const ScanShape s, const ScanParams p)
             slots[(seg0 + k) * stride] = make_float4(h[0], h[1], h[2], h[3]);
             const float ends[4] = {end[k].x, end[k].y, end[k].z, end[k].w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = span[k] < 0.0f ? ends[e] : fmaf(ex2(a[e] * span[k]), h[e], ends[e]);
+            for (int e = 0; e < 4; ++e) h[e] = span[k] < 0.0f ? ends[e] : fmaf(decay(a[e], span[k]), h[e], ends[e]);
         }
     }
 }
@@ -416,7 +416,7 @@ k_scan_step(const StepParams p, const T *__restrict__ x, const T *__restrict__ d
             sum[k] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                v[e] = fmaf(ex2(step * a2[e]), v[e], input * bb[k].at(e));
+                v[e] = fmaf(decay(a2[e], step), v[e], input * bb[k].at(e));
                 sum[k] = fmaf(cc[k].at(e), v[e], sum[k]);
             }
             if (!holds) sum[k] = 0.0f;
