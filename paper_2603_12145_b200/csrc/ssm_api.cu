@@ -126,13 +126,30 @@ int check_seq(const ssm_seq &q, size_t bytes)
     return aligned(q.ptr, bytes) ? SSM_OK : SSM_EALIGN;
 }
 
-// Outputs must not share elements: their rows are at least a row apart.
+// Do rows of `row` elements, of which `many` are `step` apart and these in turn `few` times `jump`, stay clear of
+// one another?  They do where a jump passes all the steps; else the i-th jump has to land between two steps.
+bool rows_apart(int64_t row, int64_t many, int64_t step, int64_t few, int64_t jump)
+{
+    if ((many > 1 && step < row) || (few > 1 && jump < row)) return false;
+    if (many == 1 || few == 1) return true;
+    using wide = __int128;
+    if (jump >= static_cast<wide>(many - 1) * step + row || step >= static_cast<wide>(few - 1) * jump + row) return true;
+    for (int64_t i = 1; i < few; ++i) {
+        const wide at = static_cast<wide>(i) * jump, below = at / step;
+        if (below < many && at - below * step < row) return false;
+        if (below + 1 < many && (below + 1) * step - at < row) return false;
+    }
+    return true;
+}
+
+// Outputs must not share elements.
 int check_out(const ssm_seq &q, size_t bytes, int64_t row, int64_t batch, int64_t time)
 {
     const int rc = check_seq(q, bytes);
     if (rc != SSM_OK) return rc;
-    if ((batch > 1 && q.stride_b < row) || (time > 1 && q.stride_t < row)) return SSM_EINVAL;
-    return SSM_OK;
+    const bool apart = batch < time ? rows_apart(row, time, q.stride_t, batch, q.stride_b)
+                                    : rows_apart(row, batch, q.stride_b, time, q.stride_t);
+    return apart ? SSM_OK : SSM_EINVAL;
 }
 
 int check_scan(const ssm *p, const ssm_scan_args *a, bool backward)

@@ -39,6 +39,10 @@ def test_calls_go_to_the_handles_device(fake, library):
     child(fake, "device_" + library)
 
 
+def test_outputs_whose_rows_share_memory_are_refused(fake):
+    child(fake, "shared_rows")
+
+
 # ---- in the child: the libraries' own bindings, addresses instead of tensors ---------
 
 class Fake:
@@ -120,6 +124,44 @@ def device_ssm(fake):
             ("conv_backward", lambda: L.ssm_conv_backward(h, ctypes.byref(c))),
             ("conv_step", lambda: L.ssm_conv_step(h, p(0), 96, p(1), 1, p(2), p(3), p(4), p(5), p(6), 96, 5)),
         ], lambda s: L.ssm_set_stream(h, s))
+
+
+def shared_rows(fake):
+    """Strides of outputs [batch][time][features]: rows of one order, of the other and of wider arrays are
+    taken; two rows at the same place, or running into each other, are not (they would be written in no order)."""
+    from paper_2603_12145_b200 import ssm
+    L = ssm.load()
+    ch, states, batch, time = 96, 16, 3, 5
+    h = ssm.ssm_create(ch, states, 1, 4, 1)
+
+    def strides(row):
+        good = [(time * row, row), (row, batch * row), (time * (row + 5), row + 5), (row + 7, batch * (row + 7)),
+                (7 * time * row, row), (row, 9 * batch * row), ((time - 1) * row + row, row)]
+        bad = [(row, row), (0, row), (row, 0), (2 * row, row), (row, 2 * row), (time * row - 1, row), (row, batch * row - 1),
+               (row - 1, batch * row), (time * row, row - 1), (4 * row, row), (row, 2 * row + 1)]
+        return good, bad
+
+    scan = {"y": (L.ssm_scan_forward, ch), "dx": (L.ssm_scan_backward, ch), "ddt": (L.ssm_scan_backward, ch),
+            "dz": (L.ssm_scan_backward, ch), "db": (L.ssm_scan_backward, states), "dc": (L.ssm_scan_backward, states)}
+    conv = {"y": (L.ssm_conv_forward, ch), "dx": (L.ssm_conv_backward, ch)}
+    for kind, outputs in (("scan", scan), ("conv", conv)):
+        for key, (call, row) in outputs.items():
+            good, bad = strides(row)
+            for taken, pairs in ((0, good), (-1, bad)):
+                for pair in pairs:
+                    a = scan_args(ssm, h, batch, time, ch, states) if kind == "scan" else conv_args(ssm, batch, time, ch)
+                    setattr(a, key, ssm.Seq(address(40), *pair))
+                    assert call(h, ctypes.byref(a)) == taken, (kind, key, row, pair)
+    # neither order's rows lie together, and none share memory: 0, 2, 4 and 3, 5, 7; with a fourth step 6 would meet 3 + 3
+    for b, t, taken in ((2, 3, 0), (3, 4, -1), (3, 2, 0)):
+        a = conv_args(ssm, b, t, ch)
+        a.y = ssm.Seq(address(40), 3 * ch, 2 * ch)
+        assert L.ssm_conv_forward(h, ctypes.byref(a)) == taken, (b, t)
+    # of a single row or step the strides do not matter
+    for b, t, pair in ((1, 5, (0, ch)), (3, 1, (ch, 0)), (1, 1, (0, 0))):
+        a = conv_args(ssm, b, t, ch)
+        a.y = ssm.Seq(address(40), *pair)
+        assert L.ssm_conv_forward(h, ctypes.byref(a)) == 0, (b, t, pair)
 
 
 def device_gated_ffn(fake):
