@@ -43,6 +43,11 @@ def test_outputs_whose_rows_share_memory_are_refused(fake):
     child(fake, "shared_rows")
 
 
+def test_long_cases_are_cut_as_they_say(fake):
+    """The loops that test_gpu_ssm_long.py is about, by the libraries' own launches for 148 SMs."""
+    child(fake, "cuts")
+
+
 # ---- in the child: the libraries' own bindings, addresses instead of tensors ---------
 
 class Fake:
@@ -162,6 +167,56 @@ def shared_rows(fake):
         a = conv_args(ssm, b, t, ch)
         a.y = ssm.Seq(address(40), *pair)
         assert L.ssm_conv_forward(h, ctypes.byref(a)) == 0, (b, t, pair)
+
+
+def up(a, b):
+    return -(-a // b)
+
+
+def cuts(fake):
+    import test_gpu_ssm_long as cases
+    from paper_2603_12145_b200 import ssm
+    L = ssm.load()
+    for batch, time, ch, n, groups, _, _, forward, backward in cases.SCAN:
+        h = ssm.ssm_create(ch, n, groups, 4, 0)
+        lanes, quads = (1 if n <= 16 else 2 if n <= 32 else 4), next(q for q in (1, 2, 4, 8, 16) if 4 * q >= n)
+        chunks = up(time, 16)
+        assert up(chunks, forward[1]) == forward[0] and up(chunks, backward[1]) == backward[0]
+        a = scan_args(ssm, h, batch, time, ch, n, groups)
+        fake.lib.fake_clear()
+        assert L.ssm_scan_forward(h, ctypes.byref(a)) == 0
+        blocks = batch * forward[0] * groups * up(ch // groups, 128 // lanes)
+        assert [e[3] for e in fake.entries() if e[0] == "launch"][-1] == blocks, (batch, time, fake.entries())
+        fake.lib.fake_clear()
+        assert L.ssm_scan_backward(h, ctypes.byref(a)) == 0
+        blocks = backward[2] * groups * up(ch // groups, 96 if 16 < n <= 32 else 128)
+        launches = [e[3] for e in fake.entries() if e[0] == "launch"]
+        assert len(launches) == (3 if backward[0] == 1 else 5) and launches[-3] == blocks, (batch, time, launches, blocks)
+        carry = batch * backward[0] * ch * (16 * quads + 4) if backward[0] > 1 else 0
+        total = L.ssm_scan_workspace_bytes(h, batch, time, 1)
+        parts = up(ch // groups, 96 if 16 < n <= 32 else 128) * batch * time * groups * 2 * max(16, 4 * quads) * 4
+        assert abs(total - carry - backward[2] * ch * (16 * quads + 8) - parts) < 64, (batch, time, total)
+    assert any(c[8][2] < c[0] * c[8][0] for c in cases.SCAN) and any(c[7][0] > 1 and c[7][1] > 1 for c in cases.SCAN)
+    p = address
+    for n, ch, states, groups, _, rows in cases.STEPS:
+        h = ssm.ssm_create(ch, states, groups, 4, 0)
+        fake.lib.fake_clear()
+        assert L.ssm_scan_step(h, p(0), ch, p(1), ch, p(2), ch, p(3), groups * states, p(4), groups * states, p(5), 1, p(6), p(7),
+                               p(8), p(9), p(10), p(11), ch, n) == 0
+        lanes = next(q for q in (1, 2, 4, 8, 16) if 4 * q >= states)
+        assert [e[3] for e in fake.entries()] == [up(ch, 256 // lanes) * up(n, rows)], (n, ch, fake.entries(), rows)
+    assert any(c[5] > 4 for c in cases.STEPS)
+    for batch, time, ch, width, _, _, run, runs in cases.CONV:
+        h = ssm.ssm_create(ch, 16, 1, width, 0)
+        c = conv_args(ssm, batch, time, ch)
+        fake.lib.fake_clear()
+        assert L.ssm_conv_forward(h, ctypes.byref(c)) == 0
+        warps = up(ch // 4, 32) if ch % 4 == 0 else up(ch, 32)
+        units = batch * up(time, run)
+        assert [e[3] for e in fake.entries()] == [up(units * warps, 4)], (batch, time, fake.entries())
+        slots = L.ssm_conv_workspace_bytes(h, batch, time) // (4 * ch * (width + 1))
+        assert up(units, slots) == runs, (batch, time, units, slots)
+    assert any(c[6] > 8 for c in cases.CONV) and all(c[7] > 1 for c in cases.CONV)
 
 
 def device_gated_ffn(fake):
