@@ -44,8 +44,13 @@ def test_outputs_whose_rows_share_memory_are_refused(fake):
 
 
 def test_long_cases_are_cut_as_they_say(fake):
-    """The loops that test_gpu_ssm_long.py is about, by the libraries' own launches for 148 SMs."""
+    """The loops that test_gpu_ssm_long.py is about, by the library's own launches for 148 SMs."""
     child(fake, "cuts")
+
+
+def test_tiles_of_the_block_are_as_the_cases_say(fake):
+    """Of test_gpu_gated_ffn_long.py, with 74 pairs of SMs."""
+    child(fake, "tiles")
 
 
 # ---- in the child: the libraries' own bindings, addresses instead of tensors ---------
@@ -321,6 +326,26 @@ def device_cartpole(fake):
         assert L.cartpole_destroy(h) == 0
         assert fake.entries() and all(e[1] == 1 for e in fake.entries()) and fake.current() == 0, fake.entries()
         del keep, rest
+
+
+def tiles(fake):
+    import test_gpu_gated_ffn_long as cases
+    from paper_2603_12145_b200 import gated_ffn
+    L = gated_ffn.load()
+    p = address
+    for n, model, hidden, activation, _, forward, slope in cases.TILES:
+        h = gated_ffn.gated_ffn_create(model, hidden, 0, 0)
+        fake.lib.fake_clear()
+        assert L.gated_ffn_forward(h, p(0), model, p(1), p(2), p(3), p(4), p(5), model, p(6), 1 << 40, n) == 0
+        grid = fake.entries()[0][3]
+        count = up(n, 256) * up(hidden, 128)
+        assert (grid // 2, up(count, grid // 2)) == forward, (n, hidden, grid, count)
+        fake.lib.fake_clear()
+        assert L.gated_ffn_backward(h, p(0), model, p(1), model, p(2), p(3), p(4), p(5), p(6), model, p(7), p(8), p(9), 1 << 40, n) == 0
+        grid = fake.entries()[0][3]
+        count = up(n, 256) * up(hidden, 192)
+        assert (grid // 2, up(count, grid // 2)) == slope, (n, hidden, grid, count)
+    assert any(c[5][1] > 1 for c in cases.TILES) and any(c[6][1] > 1 for c in cases.TILES)
 
 
 if __name__ == "__main__":
