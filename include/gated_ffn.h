@@ -16,8 +16,10 @@
  *
  * Types.  Everything the caller passes is bfloat16 or binary16, one type per handle.
  * Products run on the tensor cores and accumulate in binary32.  Rounded to the type:
- * results; hidden, dg and du, which are operands of further products.  g and u are kept
- * for the backward pass (`pre`) with the upper 24 bits of their binary32 values.  The
+ * results; hidden, dg and du, which are operands of further products (in binary16 they are
+ * infinite beyond 65,504).  g and u are kept for the backward pass (`pre`) with the upper 24
+ * bits of their binary32 values, cut off: within 2^-15, always towards zero (adding half a unit
+ * first could carry a NaN over into a number), which the rounding of dg and du exceeds by far.  The
  * activation and its slope are binary32; hidden comes from the unrounded g and u.  The
  * accumulation order inside the tensor cores is not specified; the same call gives the
  * same bits.
@@ -27,7 +29,9 @@
  * Pointers are DEVICE pointers owned by the caller, 16-byte aligned; inputs must not
  * overlap outputs.  Calls enqueue on the handle's stream, on the device that was current when
  * the handle was created (whichever is current now stays so), and return
- * (gated_ffn_status synchronises).  The library allocates only in gated_ffn_create.
+ * (gated_ffn_status synchronises).  A handle is not thread-safe (its stream is set by one call
+ * and used by the next): use one handle per host thread or lock.  The library allocates only in
+ * gated_ffn_create.
  * Return 0 or a negative GATED_FFN_E* code; no exceptions, aborts, traps or printing;
  * no CPU fallback.
  */

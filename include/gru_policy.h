@@ -47,8 +47,8 @@
  * DEVICE pointer owned by the caller; x and h buffers hold bfloat16 [n][H],
  * row-major, 16-byte aligned.  Calls enqueue on the handle's stream, on the device that
  * was current when the handle was created (whichever is current now stays so), and return
- * (gru_policy_status synchronises).  The library allocates only in
- * gru_policy_create.  Return 0 or a negative GRU_POLICY_E* code; no exceptions,
+ * (gru_policy_status synchronises).  A handle is not thread-safe: use one per host
+ * thread or lock.  The library allocates only in gru_policy_create.  Return 0 or a negative GRU_POLICY_E* code; no exceptions,
  * aborts, traps or printing; no CPU fallback.
  */
 #ifndef GRU_POLICY_H_

@@ -38,7 +38,8 @@
  *
  * Calls enqueue on the handle's stream, on the device that was current when the handle was
  * created (whichever is current now stays so), and return; nothing is allocated but the
- * handle.  Return 0 or a negative SSM_E* code; no exceptions, aborts, traps or
+ * handle.  A handle is not thread-safe (its stream is set by one call and used by the next): use one
+ * handle per host thread or lock.  Return 0 or a negative SSM_E* code; no exceptions, aborts, traps or
  * printing; no CPU fallback.
  */
 #ifndef SSM_H_

@@ -32,12 +32,15 @@
 // adds its pieces in order.
 //
 // What bounds it (65,536 x 576 x 1,536 / 8,192 x 2,048 x 8,192, silu, bfloat16, each kernel by itself):
-//     kGated   231 us, 1.00 PFLOP/s / 390 us, 1.41 PFLOP/s   epilogue (1.2 GB/ms written) / tensor cores
-//     kSlope   199 us, 0.58 PFLOP/s / 287 us, 0.96 PFLOP/s   epilogue: slope of the activation on 8 warps
+//     kGated   231 us, 1.00 PFLOP/s / 390 us, 1.41 PFLOP/s   epilogue (805 MB written, 3.5 TB/s) / tensor cores
+//     kSlope   199 us, 0.58 PFLOP/s / 287 us, 0.96 PFLOP/s   memory (679 MB read and 403 written, 5.4 TB/s, 0.83 of
+//              a copy: the kept g and u are more than half of it) / epilogue
 //     kStore   y 110 us, 1.06 / 187 us, 1.47; dx 201 us, 1.15 / 372 us, 1.48; dW_in 250 us, 0.93 / 405 us, 1.36;
 //              dW_out 135 us, 0.86 / 208 us, 1.32 PFLOP/s
-// The products with 576 columns move 57 to 64 KB from L2 per 0.29 us of a tile's arithmetic and run at the
-// 9 to 10 TB/s that L2 gives; wider tiles would need more accumulator columns than there are.
+// The products with 576 columns move 57 to 64 KB of operands from L2 per 0.29 us of a tile's arithmetic, 8.5 to 10.5 TB/s
+// (11 to 14 by L2's own count, which has fills and results in it); wider tiles would need more accumulator
+// columns than there are.  dW_out has 576 rows, which three tiles of 256 round up to 768: a quarter of its work is
+// padding (1.15 PFLOP/s with it).
 //
 // k_rows: up to 64 rows of x, bound by reading the weights: one row through 2,048 x 8,192 takes 16.8 us from a
 // graph, 6.0 TB/s.  A block owns 16 rows of the weights

@@ -9,7 +9,9 @@
 // A reset clears the window, which drops every tap from before the episode.
 //
 // 1024 x 128 x 1152 in bfloat16: forward 120 us (5.0 TB/s of 0.6 GB, a copy of the same bytes takes
-// 100 us), backward 222 us (4.1 TB/s of 0.9 GB, schedulers 56 % busy).
+// 100 us), backward 222 us (4.1 TB/s of 0.9 GB, schedulers 56 % busy).  In binary32: forward 199 us (6.1 TB/s),
+// backward 511 us (3.5 TB/s).  Backward, four blocks per SM leave 128 registers: with width 4 some values are
+// spilled (52 bytes of stores per thread in bfloat16, 44 in binary16, 256 in binary32).
 //
 // The backward kernel walks forward too: step t gives dpre_t, which goes into the pending
 // gradients of x_t .. x_{t-width+1} (as far back as the episode reaches); the oldest one is

@@ -300,8 +300,10 @@ int launch(const ScanShape &s, const ScanParams &p, const ScanSeqs<T> &q, cudaSt
 // channels' parameters and walks rows, four at a time.  What a channel needs once per row (the
 // step's softplus, the gate, the result) is spread over the lanes that share the channel, a row or
 // two for each, and the others' reach it by shuffles: computed by every lane it would be three
-// quarters of the instructions.  16,384 rows x 1152 x 16 states: 487 us, 5.3 TB/s of 2.57 GB
-// (0.81 of the measured copy bandwidth; 603 us with the scalars in every lane).
+// quarters of the instructions.  16,384 rows x 1152 x 16 states: 490 us, 5.2 TB/s of 2.57 GB
+// (0.80 of the measured copy bandwidth; 603 us with the scalars in every lane).  64 registers for four blocks per
+// SM: the binary32 form spills (48 bytes of stores per thread) and takes 524 us, 5.2 TB/s of 2.71 GB; without whole
+// vectors (15 states: 132 to 164 bytes) it is 0.80 ms in binary32, 0.97 in bfloat16, 0.92 in binary16.
 
 constexpr int kStepThreads = 256;
 constexpr int kStepRows = 4;    // rows whose states are in flight together

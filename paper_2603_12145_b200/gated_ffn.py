@@ -90,8 +90,8 @@ class GatedFfn:
     """The block for one layer's sizes.  Tensors are torch CUDA tensors of the handle's dtype:
     x, dy [n, model] with a contiguous last dimension and a row stride that is a multiple of 8;
     w_in [2 * hidden, model] (gate rows first) and w_out [model, hidden] contiguous.  Calls
-    enqueue on the current stream of the device.  A tensor that does not fit raises ValueError,
-    a refusal by the library GatedFfnError."""
+    enqueue on the current stream of the device, whichever device is current.  One thread at a
+    time.  A tensor that does not fit raises ValueError, a refusal by the library GatedFfnError."""
 
     def __init__(self, model: int, hidden: int, activation: str = "silu", dtype=None, device: str = "cuda:0"):
         import torch

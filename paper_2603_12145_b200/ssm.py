@@ -115,8 +115,9 @@ class Ssm:
     strides but a contiguous last dimension (a time-major rollout is `v.transpose(0, 1)`);
     single tokens are [n, features].  reset / done are uint8 or bool [batch, time] / [n].
     Parameters and recurrent states are contiguous float32.  Calls enqueue on the current
-    stream of the device; outputs that are not given are allocated.  A tensor that does not
-    fit raises ValueError, a refusal by the library SsmError."""
+    stream of the device, whichever device is current; outputs that are not given are
+    allocated.  One thread at a time.  A tensor that does not fit raises ValueError, a refusal
+    by the library SsmError."""
 
     def __init__(self, channels: int, states: int = 16, groups: int = 1, width: int = 4, dtype=None,
                  device: str = "cuda:0"):
