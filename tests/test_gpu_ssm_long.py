@@ -276,3 +276,28 @@ def test_conv_and_gradients(torch, case):
     for t in range(3):
         step = op.conv_step(dev["x"][:, t].contiguous(), dev["history"], dev["w"], dev["bias"], done=dev["reset"][:, t])
         check("step %d" % t, step, want_y[:, t], EPS * factor * 1.1 * mag_y[:, t], dtype)
+
+
+@pytest.mark.parametrize("rows,dtype", [(300, "float32"), (1, "bfloat16")])
+def test_steps_of_no_length_leave_the_state_as_it_is(torch, rows, dtype):
+    """delta = softplus(-inf) = 0: the state's bits do not change over 1,000 steps, neither as one sequence (uncut, and cut
+    along the time axis) nor as single tokens; nor does a gradient on its way back, and none reaches dt or A."""
+    steps, ch, n = 1000, 128, 16
+    kind = getattr(torch, dtype)
+    gen = torch.Generator("cuda").manual_seed(2)
+    draw = lambda *s: torch.randn(s, device="cuda", generator=gen)      # noqa: E731
+    op = ssm.Ssm(ch, n, dtype=kind)
+    assert (op._lib.ssm_scan_workspace_bytes(op.h, rows, steps, 0) == 0) == (rows == 300)
+    a, h0, x, b = -torch.exp(draw(ch, n)), draw(rows, ch, n), draw(rows, steps, ch).to(kind), draw(rows, steps, n).to(kind)
+    still, out = torch.full((rows, steps, ch), -float("inf"), dtype=kind, device="cuda"), op.state(rows)
+    op.scan(x, still, a, b, b, state=h0, state_out=out)
+    assert torch.equal(out, h0)
+    for t in range(steps):
+        op.scan_step(x[:, t], still[:, t], a, b[:, t], b[:, t], out)
+    assert torch.equal(out, h0)
+    saved = op.saved(rows, steps)
+    op.scan(x, still, a, b, b, state=h0, saved=saved)
+    dy = torch.zeros_like(x)
+    d0 = draw(rows, ch, n)
+    got = op.scan_backward(dy, x, still, a, b, b, saved, dstate_out=d0, want_dstate=True)
+    assert torch.equal(got["dstate"], d0) and bool((got["ddt"] == 0).all()) and bool((got["da"] == 0).all())

@@ -8,6 +8,8 @@ import sys
 
 import pytest
 
+from paper_2603_12145_b200 import build
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
@@ -15,7 +17,8 @@ CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 
 @pytest.fixture(scope="module")
 def fake(tmp_path_factory):
-    """Directory with the stand-in as libcudart.so.12."""
+    """Directory with the stand-in as libcudart.so.12; the libraries are built."""
+    build.build()
     where = tmp_path_factory.mktemp("fake_cudart")
     (where / "versions").write_text("libcudart.so.12 { global: *; };\n")
     subprocess.run(["gcc", "-shared", "-fPIC", "-O1", "-I" + os.path.join(CUDA, "include"),
