@@ -1,0 +1,660 @@
+// layer_norm.cu -- the layer norm of a residual stream behind the C ABI of layer_norm.h.
+//
+// A row stays in the registers of the threads that share it, as the words it was loaded in: the sum, the mean, the
+// variance (from differences to the mean) and the result come from one reading of memory.  A row of up to 128 vectors of
+// 16 bytes belongs to 4 to 32 lanes of a warp, which reduce by shuffles; a wider one to a block, whose warps exchange
+// their sums through shared memory with one barrier per reduction (two alternating slots).  Each thread holds its
+// vectors index lane, lane + R, ... of the R threads, so that a warp's access is contiguous.
+//
+// The backward kernel keeps dw and db of its thread's columns in registers over all its rows; a block's row groups are
+// added in shared memory, blocks leave a row of sums each and k_join adds them, all in a fixed order.
+//
+// Both are bound by memory; the next row's loads are in flight while a row is reduced.
+#include <cmath>
+#include <new>
+#include <type_traits>
+
+#include "../../include/layer_norm.h"
+#include "on_device.cuh"
+#include "vectors.cuh"
+
+namespace {
+
+constexpr int kNarrowThreads = 128;      // block of the kernels whose rows belong to lanes of a warp
+constexpr int kMost = 512;               // threads that share a wide row, at most
+
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename T>
+struct Rows {
+    T *ptr;
+    int64_t stride;
+    __device__ __forceinline__ T *row(int64_t i) const { return ptr + i * stride; }
+};
+
+template <typename T>
+struct Forward {
+    Rows<const T> x, residual;
+    Rows<T> sum, y;
+    const float *w, *b;
+    float2 *saved;
+    int64_t n;
+    int width, lanes;
+    float eps;
+};
+
+template <typename T>
+struct Backward {
+    Rows<const T> dy, s, dsum;
+    Rows<T> dx;
+    const float *w;
+    const float2 *saved;
+    float *part;             // [blocks][2][width], or nullptr: no dw, db
+    int64_t n;
+    int width, lanes;
+};
+
+// Sums over the threads that share a row: R lanes, or the block.
+template <bool kWide>
+struct Team {
+    int size, index;         // threads of the row, and which of them this is
+    int slot = 0;
+    float2 *shared;          // [2][kMost / 32]
+
+    __device__ float2 total(float2 v)
+    {
+        if (kWide) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+                v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+            }
+            float2 *s = shared + slot * (kMost / 32);
+            slot ^= 1;
+            const int lane = index & 31, warps = size >> 5;
+            if (lane == 0) s[index >> 5] = v;
+            __syncthreads();
+            v = lane < warps ? s[lane] : make_float2(0.0f, 0.0f);
+            for (int o = 16; o > 0; o >>= 1) {
+                v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+                v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+            }
+        } else {
+            for (int o = size >> 1; o > 0; o >>= 1) {
+                v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
+                v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
+            }
+        }
+        return v;
+    }
+    __device__ float total(float v)
+    {
+        if constexpr (kWide) {
+            return total(make_float2(v, 0.0f)).x;
+        } else {
+            for (int o = size >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+            return v;
+        }
+    }
+};
+
+// V neighbouring parameters (from L1: every row reads them)
+template <int V>
+__device__ __forceinline__ void load_params(float (&dst)[V], const float *src, float absent)
+{
+    if (src == nullptr) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) dst[e] = absent;
+    } else if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+            const float4 f = __ldg(reinterpret_cast<const float4 *>(src + e));
+            dst[e] = f.x, dst[e + 1] = f.y, dst[e + 2] = f.z, dst[e + 3] = f.w;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) dst[e] = __ldg(src + e);
+    }
+}
+
+// V elements per access, C accesses per thread and row.
+template <typename T, int V, int C, bool kWide>
+__global__ void __launch_bounds__(kWide ? kMost : kNarrowThreads)
+k_forward(const Forward<T> p)
+{
+    __shared__ float2 s_sum[kWide ? 2 * (kMost / 32) : 1];
+    Team<kWide> team;
+    team.size = kWide ? static_cast<int>(blockDim.x) : p.lanes;
+    team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
+    team.shared = s_sum;
+    const int per_block = kWide ? 1 : kNarrowThreads / p.lanes;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * per_block;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block + (kWide ? 0 : threadIdx.x / p.lanes);
+    const int vectors = p.width / V;
+    const float inverse = 1.0f / static_cast<float>(p.width);
+    const bool added = p.residual.ptr != nullptr;
+    Packed<T, V> nx[C], nr[C];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            const bool in = v < vectors && row < p.n;
+            nx[c] = in ? packed_load<T, V>(p.x.row(row) + v * V) : packed_zero<T, V>();
+            if (added) nr[c] = in ? packed_load<T, V>(p.residual.row(row) + v * V) : packed_zero<T, V>();
+        }
+    };
+    fetch(first);
+    // a warp's lanes stay together (its rows are neighbours): all go round while the first of them has a row
+    for (int64_t row = first; row - (kWide ? 0 : (threadIdx.x & 31) / p.lanes) < p.n; row += step) {
+        const bool live = row < p.n;
+        float s[C][V];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[c][e] = packed_get<T, V>(nx[c], e);
+            if (added) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[c][e] += packed_get<T, V>(nr[c], e);
+                const Packed<T, V> rounded = packed_of<T, V>(s[c]);
+                const int v = c * team.size + team.index;
+                if (v < vectors && live) packed_store<T, V>(p.sum.row(row) + v * V, rounded);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[c][e] = packed_get<T, V>(rounded, e);
+            }
+        }
+        fetch(row + step);
+        float sum = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum += s[c][e];
+        const float mean = team.total(sum) * inverse;
+        float square = 0.0f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const bool in = c * team.size + team.index < vectors;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                s[c][e] = in ? s[c][e] - mean : 0.0f;
+                square = fmaf(s[c][e], s[c][e], square);
+            }
+        }
+        const float scale = rsqrtf(fmaf(team.total(square), inverse, p.eps));
+        if (p.saved != nullptr && team.index == 0 && live) p.saved[row] = make_float2(mean, scale);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            if (v < vectors && live) {
+                float w[V], b[V];
+                load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+                load_params<V>(b, p.b != nullptr ? p.b + v * V : nullptr, 0.0f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[c][e] = fmaf(s[c][e] * scale, w[e], b[e]);
+                packed_store<T, V>(p.y.row(row) + v * V, packed_of<T, V>(s[c]));
+            }
+        }
+    }
+}
+
+template <typename T, int V, int C, bool kWide>
+__global__ void __launch_bounds__(kWide ? kMost : kNarrowThreads)
+k_backward(const Backward<T> p)
+{
+    extern __shared__ float s_part[];                      // narrow rows: [2][width] while groups are added
+    __shared__ float2 s_sum[kWide ? 2 * (kMost / 32) : 1];
+    allow_next();
+    Team<kWide> team;
+    team.size = kWide ? static_cast<int>(blockDim.x) : p.lanes;
+    team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
+    team.shared = s_sum;
+    const int per_block = kWide ? 1 : kNarrowThreads / p.lanes;
+    const int group = kWide ? 0 : static_cast<int>(threadIdx.x) / p.lanes;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * per_block;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block + group;
+    const int vectors = p.width / V;
+    const float inverse = 1.0f / static_cast<float>(p.width);
+    const bool added = p.dsum.ptr != nullptr;
+    float dw[C][V], db[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[c][e] = db[c][e] = 0.0f;
+    Packed<T, V> ns[C], ndy[C], nd[C];
+    float2 nstat;
+    auto fetch = [&](int64_t row) {
+        nstat = row < p.n ? __ldg(p.saved + row) : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            const bool in = v < vectors && row < p.n;
+            ns[c] = in ? packed_load<T, V>(p.s.row(row) + v * V) : packed_zero<T, V>();
+            ndy[c] = in ? packed_load<T, V>(p.dy.row(row) + v * V) : packed_zero<T, V>();
+            if (added) nd[c] = in ? packed_load<T, V>(p.dsum.row(row) + v * V) : packed_zero<T, V>();
+        }
+    };
+    fetch(first);
+    for (int64_t row = first; row - (kWide ? 0 : (threadIdx.x & 31) / p.lanes) < p.n; row += step) {
+        const bool live = row < p.n;
+        Packed<T, V> s[C], dy[C], d[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            s[c] = ns[c];
+            dy[c] = ndy[c];
+            if (added) d[c] = nd[c];
+        }
+        const float mean = nstat.x, scale = nstat.y;
+        fetch(row + step);
+        float2 sums = make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            if (v < vectors) {
+                float w[V];
+                load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float z = (packed_get<T, V>(s[c], e) - mean) * scale, g = packed_get<T, V>(dy[c], e);
+                    const float h = g * w[e];
+                    sums.x += h;
+                    sums.y = fmaf(h, z, sums.y);
+                    dw[c][e] = fmaf(g, z, dw[c][e]);
+                    db[c][e] += g;
+                }
+            }
+        }
+        sums = team.total(sums);
+        const float along = -scale * sums.y * inverse, shift = -scale * sums.x * inverse;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            if (v < vectors && live) {
+                float w[V], out[V];
+                load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float z = (packed_get<T, V>(s[c], e) - mean) * scale;
+                    out[e] = fmaf(packed_get<T, V>(dy[c], e) * w[e], scale, fmaf(z, along, shift));
+                    if (added) out[e] += packed_get<T, V>(d[c], e);
+                }
+                packed_store<T, V>(p.dx.row(row) + v * V, packed_of<T, V>(out));
+            }
+        }
+    }
+    if (p.part == nullptr) return;
+    float *part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.width;
+    if constexpr (kWide) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            if (v < vectors) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    part[v * V + e] = dw[c][e];
+                    part[p.width + v * V + e] = db[c][e];
+                }
+            }
+        }
+    } else {
+        for (int g = 0; g < per_block; ++g) {              // the block's row groups one after the other
+            if (g == group) {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int v = c * team.size + team.index;
+                    if (v < vectors) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            float *a = s_part + v * V + e, *b = a + p.width;
+                            *a = g == 0 ? dw[c][e] : *a + dw[c][e];
+                            *b = g == 0 ? db[c][e] : *b + db[c][e];
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < 2 * p.width; i += kNarrowThreads) part[i] = s_part[i];
+    }
+}
+
+// dw and db: a block takes 32 columns of the `rows` rows of sums, eight warps share the rows.
+constexpr int kJoinWarps = 8;
+
+__global__ void __launch_bounds__(32 * kJoinWarps)
+k_join(const float *part, int rows, int width, float *dw, float *db)
+{
+    __shared__ float s[kJoinWarps][32];
+    wait_for_previous();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int column = blockIdx.x * 32 + lane;
+    float sum = 0.0f;
+    if (column < 2 * width) {
+        const float *at = part + column;
+#pragma unroll 8
+        for (int r = warp; r < rows; r += kJoinWarps) sum += at[static_cast<int64_t>(r) * 2 * width];
+    }
+    s[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0 || column >= 2 * width) return;
+#pragma unroll
+    for (int i = 1; i < kJoinWarps; ++i) sum += s[i][lane];
+    if (column < width)
+        dw[column] = sum;
+    else
+        db[column - width] = sum;
+}
+
+// ---------------------------------------------------------------- host side
+
+int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+bool aligned(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
+
+// How a row is shared: `lanes` threads with C accesses each.
+struct Share {
+    int lanes, count;
+    bool wide;
+};
+
+// Vectors of 16 bytes: up to four per lane of a warp, then up to three (four, where that is not enough) per thread of a
+// block.  Single elements: up to 8 per lane, then up to 8 (16) per thread.
+Share share_of(int vectors, bool whole)
+{
+    Share s = {4, 1, false};
+    while (s.lanes < 32 && s.lanes * (whole ? 2 : 4) < vectors) s.lanes *= 2;
+    if (vectors > s.lanes * (whole ? 4 : 8)) {
+        s.wide = true;
+        s.lanes = 64;
+        while (s.lanes < kMost && s.lanes * (whole ? 3 : 8) < vectors) s.lanes *= 2;
+    }
+    s.count = static_cast<int>(div_up(vectors, s.lanes));
+    return s;
+}
+static_assert(kMost * 16 >= LAYER_NORM_MAX_WIDTH && kMost * 3 * 8 >= LAYER_NORM_MAX_WIDTH && kMost * 4 * 4 >= LAYER_NORM_MAX_WIDTH,
+              "the widest row: single elements, vectors of 8, vectors of 4");
+
+template <int N>
+using Count = std::integral_constant<int, N>;
+
+// Calls f with V, C and the form of the kernel for this share.
+template <typename T, typename F>
+bool with_counts(const Share &s, bool whole, F f)
+{
+    using V = Count<16 / sizeof(T)>;
+    using One = Count<1>;
+    if (whole && s.wide) {
+        if (s.count <= 2) return f(V{}, Count<2>{}, std::true_type{});
+        if constexpr (sizeof(T) == 4)
+            if (s.count == 4) return f(V{}, Count<4>{}, std::true_type{});
+        return f(V{}, Count<3>{}, std::true_type{});
+    }
+    if (whole) {
+        if (s.count <= 1) return f(V{}, Count<1>{}, std::false_type{});
+        if (s.count == 2) return f(V{}, Count<2>{}, std::false_type{});
+        if (s.count == 3) return f(V{}, Count<3>{}, std::false_type{});
+        return f(V{}, Count<4>{}, std::false_type{});
+    }
+    if (s.wide) return s.count <= 8 ? f(One{}, Count<8>{}, std::true_type{}) : f(One{}, Count<16>{}, std::true_type{});
+    return s.count <= 4 ? f(One{}, Count<4>{}, std::false_type{}) : f(One{}, Count<8>{}, std::false_type{});
+}
+
+int element_bytes(int type) { return type == LAYER_NORM_F32 ? 4 : 2; }
+
+// Row starts on 16-byte boundaries (of a single row the stride does not matter).
+bool whole_rows(const void *ptr, int64_t stride, int64_t n, int bytes)
+{
+    return ptr == nullptr || (aligned(ptr, 16) && (n == 1 || stride * bytes % 16 == 0));
+}
+
+}  // namespace
+
+struct layer_norm {
+    int width = 0, type = 0;
+    float eps = 0.0f;
+    int device = 0, sms = 0;
+    cudaStream_t stream = nullptr;
+    int64_t launches = 0;
+};
+
+namespace {
+
+// Side by side, blocks of the backward kernel: as many as their registers let an SM hold, at most.
+constexpr int kNarrowBlocks = 4;
+
+// Blocks of the backward kernel (and rows of sums), for either of the kernel's forms.
+int64_t backward_blocks(const layer_norm *p, const Share &s, int64_t n)
+{
+    const int64_t units = s.wide ? n : div_up(n, kNarrowThreads / s.lanes);
+    const int64_t resident = static_cast<int64_t>(p->sms) * (s.wide ? kMost / s.lanes : kNarrowBlocks);
+    return div_up(units, div_up(units, resident));
+}
+
+bool check_in(const void *ptr, int64_t stride, int bytes, int *rc)
+{
+    if (stride < 0) *rc = LAYER_NORM_EINVAL;
+    else if (!aligned(ptr, bytes)) *rc = LAYER_NORM_EALIGN;
+    return *rc == LAYER_NORM_OK;
+}
+
+bool check_out(const void *ptr, int64_t stride, int64_t n, int width, int bytes, int *rc)
+{
+    if (n > 1 && stride < width) *rc = LAYER_NORM_EINVAL;
+    else if (!aligned(ptr, bytes)) *rc = LAYER_NORM_EALIGN;
+    return *rc == LAYER_NORM_OK;
+}
+
+template <typename T>
+Rows<const T> in_rows(const void *ptr, int64_t stride) { return {static_cast<const T *>(ptr), stride}; }
+template <typename T>
+Rows<T> out_rows(void *ptr, int64_t stride) { return {static_cast<T *>(ptr), stride}; }
+
+template <typename T>
+int run_forward(layer_norm *p, Forward<T> f, bool whole)
+{
+    whole = whole && p->width % (16 / sizeof(T)) == 0;
+    const Share s = share_of(whole ? p->width / (16 / sizeof(T)) : p->width, whole);
+    f.lanes = s.lanes;
+    const int64_t units = s.wide ? f.n : div_up(f.n, kNarrowThreads / s.lanes);
+    const int64_t resident = static_cast<int64_t>(p->sms) * (s.wide ? 1024 / s.lanes : 8);
+    const unsigned blocks = static_cast<unsigned>(div_up(units, div_up(units, resident)));
+    const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto wide) {
+        k_forward<T, v.value, c.value, wide.value><<<blocks, s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
+        return cudaGetLastError() == cudaSuccess;
+    });
+    if (!ok) return LAYER_NORM_ECUDA;
+    p->launches += 1;
+    return LAYER_NORM_OK;
+}
+
+template <typename T>
+int run_backward(layer_norm *p, Backward<T> b, bool whole, float *dw, float *db)
+{
+    whole = whole && p->width % (16 / sizeof(T)) == 0;
+    const Share s = share_of(whole ? p->width / (16 / sizeof(T)) : p->width, whole);
+    b.lanes = s.lanes;
+    const int64_t blocks = backward_blocks(p, s, b.n);
+    const size_t smem = s.wide ? 0 : 2 * sizeof(float) * p->width;
+    const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto wide) {
+        k_backward<T, v.value, c.value, wide.value>
+            <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, smem, p->stream>>>(b);
+        return cudaGetLastError() == cudaSuccess;
+    });
+    if (!ok) return LAYER_NORM_ECUDA;
+    p->launches += 1;
+    if (b.part == nullptr) return LAYER_NORM_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(div_up(2 * static_cast<int64_t>(p->width), 32)));
+    cfg.blockDim = dim3(32 * kJoinWarps);
+    cfg.stream = p->stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, k_join, static_cast<const float *>(b.part), static_cast<int>(blocks), p->width, dw, db) !=
+        cudaSuccess) {
+        cudaGetLastError();
+        return LAYER_NORM_ECUDA;
+    }
+    p->launches += 1;
+    return LAYER_NORM_OK;
+}
+
+template <typename T>
+int forward_of(layer_norm *p, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *w,
+               const float *b, void *sum, int64_t sum_stride, void *y, int64_t y_stride, float *saved, int64_t n)
+{
+    Forward<T> f = {};
+    f.x = in_rows<T>(x, x_stride);
+    f.residual = in_rows<T>(residual, residual_stride);
+    f.sum = out_rows<T>(sum, sum_stride);
+    f.y = out_rows<T>(y, y_stride);
+    f.w = w;
+    f.b = b;
+    f.saved = reinterpret_cast<float2 *>(saved);
+    f.n = n;
+    f.width = p->width;
+    f.eps = p->eps;
+    const int e = sizeof(T);
+    const bool whole = whole_rows(x, x_stride, n, e) && whole_rows(residual, residual_stride, n, e) &&
+                       whole_rows(sum, sum_stride, n, e) && whole_rows(y, y_stride, n, e) && aligned(w, 16) && aligned(b, 16);
+    return run_forward<T>(p, f, whole);
+}
+
+template <typename T>
+int backward_of(layer_norm *p, const void *dy, int64_t dy_stride, const void *s, int64_t s_stride, const float *w,
+                const float *saved, const void *dsum, int64_t dsum_stride, void *dx, int64_t dx_stride, float *dw, float *db,
+                void *workspace, int64_t n)
+{
+    Backward<T> f = {};
+    f.dy = in_rows<T>(dy, dy_stride);
+    f.s = in_rows<T>(s, s_stride);
+    f.dsum = in_rows<T>(dsum, dsum_stride);
+    f.dx = out_rows<T>(dx, dx_stride);
+    f.w = w;
+    f.saved = reinterpret_cast<const float2 *>(saved);
+    f.part = dw != nullptr ? static_cast<float *>(workspace) : nullptr;
+    f.n = n;
+    f.width = p->width;
+    const int e = sizeof(T);
+    const bool whole = whole_rows(dy, dy_stride, n, e) && whole_rows(s, s_stride, n, e) && whole_rows(dsum, dsum_stride, n, e) &&
+                       whole_rows(dx, dx_stride, n, e) && aligned(w, 16);
+    return run_backward<T>(p, f, whole, dw, db);
+}
+
+bool rows_ok(int64_t n) { return n >= 1 && n <= 0x7FFFFFFF; }
+
+}  // namespace
+
+extern "C" {
+
+int layer_norm_create(layer_norm **out, int width, float eps, int type)
+{
+    if (out == nullptr) return LAYER_NORM_ENULL;
+    *out = nullptr;
+    if (width < 1 || width > LAYER_NORM_MAX_WIDTH) return LAYER_NORM_EINVAL;
+    if (!(eps > 0.0f) || std::isinf(eps)) return LAYER_NORM_EINVAL;
+    if (type != LAYER_NORM_F32 && type != LAYER_NORM_BF16 && type != LAYER_NORM_F16) return LAYER_NORM_EINVAL;
+    layer_norm *p = new (std::nothrow) layer_norm;
+    if (p == nullptr) return LAYER_NORM_ENOMEM;
+    p->width = width;
+    p->eps = eps;
+    p->type = type;
+    if (cudaGetDevice(&p->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess) {
+        cudaGetLastError();
+        delete p;
+        return LAYER_NORM_ECUDA;
+    }
+    *out = p;
+    return LAYER_NORM_OK;
+}
+
+int layer_norm_destroy(layer_norm *p)
+{
+    if (p == nullptr) return LAYER_NORM_ENULL;
+    delete p;
+    return LAYER_NORM_OK;
+}
+
+int layer_norm_set_stream(layer_norm *p, void *cuda_stream)
+{
+    if (p == nullptr) return LAYER_NORM_ENULL;
+    p->stream = static_cast<cudaStream_t>(cuda_stream);
+    return LAYER_NORM_OK;
+}
+
+int layer_norm_forward(layer_norm *p, const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,
+                       const float *w, const float *b, void *sum, int64_t sum_stride, void *y, int64_t y_stride,
+                       float *saved, int64_t n)
+{
+    if (p == nullptr) return LAYER_NORM_ENULL;
+    if (!rows_ok(n)) return LAYER_NORM_EINVAL;            // first: an empty batch comes without pointers
+    if (x == nullptr || y == nullptr || (residual == nullptr) != (sum == nullptr)) return LAYER_NORM_ENULL;
+    const int e = element_bytes(p->type);
+    int rc = LAYER_NORM_OK;
+    if (!check_in(x, x_stride, e, &rc) || !check_out(y, y_stride, n, p->width, e, &rc)) return rc;
+    if (residual != nullptr &&
+        (!check_in(residual, residual_stride, e, &rc) || !check_out(sum, sum_stride, n, p->width, e, &rc)))
+        return rc;
+    if (!aligned(w, 4) || !aligned(b, 4) || !aligned(saved, 8)) return LAYER_NORM_EALIGN;
+    const OnDevice on(p->device);
+    if (!on.ok()) return LAYER_NORM_ECUDA;
+    auto call = p->type == LAYER_NORM_F32 ? forward_of<float> : p->type == LAYER_NORM_BF16 ? forward_of<__nv_bfloat16> : forward_of<__half>;
+    return call(p, x, x_stride, residual, residual_stride, w, b, sum, sum_stride, y, y_stride, saved, n);
+}
+
+size_t layer_norm_workspace_bytes(const layer_norm *p, int64_t n)
+{
+    if (p == nullptr || !rows_ok(n)) return 0;
+    // rows of whole vectors and others are shared out differently: room for either
+    const int V = 16 / element_bytes(p->type);
+    int64_t rows = backward_blocks(p, share_of(p->width, false), n);
+    if (p->width % V == 0) {
+        const int64_t other = backward_blocks(p, share_of(p->width / V, true), n);
+        if (other > rows) rows = other;
+    }
+    return static_cast<size_t>(rows) * 2 * p->width * sizeof(float);
+}
+
+int layer_norm_backward(layer_norm *p, const void *dy, int64_t dy_stride, const void *s, int64_t s_stride,
+                        const float *w, const float *saved, const void *dsum, int64_t dsum_stride, void *dx,
+                        int64_t dx_stride, float *dw, float *db, void *workspace, size_t workspace_bytes, int64_t n)
+{
+    if (p == nullptr) return LAYER_NORM_ENULL;
+    if (!rows_ok(n)) return LAYER_NORM_EINVAL;
+    if (dy == nullptr || s == nullptr || saved == nullptr || dx == nullptr || (dw == nullptr) != (db == nullptr))
+        return LAYER_NORM_ENULL;
+    const int e = element_bytes(p->type);
+    int rc = LAYER_NORM_OK;
+    if (!check_in(dy, dy_stride, e, &rc) || !check_in(s, s_stride, e, &rc) || !check_out(dx, dx_stride, n, p->width, e, &rc))
+        return rc;
+    if (dsum != nullptr && !check_in(dsum, dsum_stride, e, &rc)) return rc;
+    if (!aligned(w, 4) || !aligned(dw, 4) || !aligned(db, 4) || !aligned(saved, 8) || !aligned(workspace, 16))
+        return LAYER_NORM_EALIGN;
+    if (dw != nullptr) {
+        if (workspace == nullptr) return LAYER_NORM_ENULL;
+        if (layer_norm_workspace_bytes(p, n) > workspace_bytes) return LAYER_NORM_ENOMEM;
+    }
+    const OnDevice on(p->device);
+    if (!on.ok()) return LAYER_NORM_ECUDA;
+    auto call = p->type == LAYER_NORM_F32 ? backward_of<float> : p->type == LAYER_NORM_BF16 ? backward_of<__nv_bfloat16> : backward_of<__half>;
+    return call(p, dy, dy_stride, s, s_stride, w, saved, dsum, dsum_stride, dx, dx_stride, dw, db, workspace, n);
+}
+
+int64_t layer_norm_launch_count(const layer_norm *p) { return p ? p->launches : 0; }
+
+const char *layer_norm_strerror(int code)
+{
+    switch (code) {
+    case LAYER_NORM_OK: return "ok";
+    case LAYER_NORM_EINVAL: return "invalid size, stride, eps or type";
+    case LAYER_NORM_ENULL: return "required pointer is NULL";
+    case LAYER_NORM_EALIGN: return "pointer not aligned to its element";
+    case LAYER_NORM_ECUDA: return "CUDA call or launch failed";
+    case LAYER_NORM_ENOMEM: return "allocation failed, or the workspace is too small";
+    default: return "unknown error";
+    }
+}
+
+}  // extern "C"
