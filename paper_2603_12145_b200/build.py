@@ -20,6 +20,8 @@ TARGETS = {
     "libgru_policy_b200.so": (["gru_policy.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gru_policy.h")]),
     "libgated_ffn_b200.so": (["gated_ffn.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_ffn.h")]),
     "liblayer_norm_b200.so": (["layer_norm.cu"], ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "layer_norm.h")]),
+    "libgated_recurrence_b200.so": (["gated_recurrence.cu"],
+                                    ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_recurrence.h")]),
     "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],
                        ["ssm_common.cuh", "ssm_kernels.cuh", "on_device.cuh", os.path.join(INCLUDE, "ssm.h")]),
 }
@@ -29,6 +31,7 @@ GRU_POLICY_LIB = os.path.join(HERE, "libgru_policy_b200.so")
 SSM_LIB = os.path.join(HERE, "libssm_b200.so")
 GATED_FFN_LIB = os.path.join(HERE, "libgated_ffn_b200.so")
 LAYER_NORM_LIB = os.path.join(HERE, "liblayer_norm_b200.so")
+GATED_RECURRENCE_LIB = os.path.join(HERE, "libgated_recurrence_b200.so")
 
 
 def _nvcc() -> str:
@@ -84,3 +87,4 @@ if __name__ == "__main__":
     print(SSM_LIB)
     print(GATED_FFN_LIB)
     print(LAYER_NORM_LIB)
+    print(GATED_RECURRENCE_LIB)
