@@ -22,6 +22,8 @@ TARGETS = {
     "liblayer_norm_b200.so": (["layer_norm.cu"], ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "layer_norm.h")]),
     "libgated_recurrence_b200.so": (["gated_recurrence.cu"],
                                     ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_recurrence.h")]),
+    "liborthogonal_b200.so": (["orthogonal.cu"],
+                              ["sm100.cuh", "vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "orthogonal.h")]),
     "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],
                        ["ssm_common.cuh", "ssm_kernels.cuh", "on_device.cuh", os.path.join(INCLUDE, "ssm.h")]),
 }
@@ -32,6 +34,7 @@ SSM_LIB = os.path.join(HERE, "libssm_b200.so")
 GATED_FFN_LIB = os.path.join(HERE, "libgated_ffn_b200.so")
 LAYER_NORM_LIB = os.path.join(HERE, "liblayer_norm_b200.so")
 GATED_RECURRENCE_LIB = os.path.join(HERE, "libgated_recurrence_b200.so")
+ORTHOGONAL_LIB = os.path.join(HERE, "liborthogonal_b200.so")
 
 
 def _nvcc() -> str:
@@ -88,3 +91,4 @@ if __name__ == "__main__":
     print(GATED_FFN_LIB)
     print(LAYER_NORM_LIB)
     print(GATED_RECURRENCE_LIB)
+    print(ORTHOGONAL_LIB)
