@@ -5,4 +5,5 @@ include/pong.h; `paper_2603_12145_b200.build` compiles it; `inputs` holds the
 seeded synthetic input generators.  Importing the package loads nothing.
 """
 __all__ = ["pong", "cartpole", "gru_policy", "policy_loop", "ssm", "gated_ffn", "layer_norm",
-           "gated_recurrence", "orthogonal", "ssm_policy", "build", "inputs", "sharding", "verify"]
+           "gated_recurrence", "orthogonal", "optimizers", "ssm_policy", "build", "inputs", "sharding",
+           "verify"]
