@@ -21,7 +21,8 @@ TARGETS = {
     "libgated_ffn_b200.so": (["gated_ffn.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_ffn.h")]),
     "liblayer_norm_b200.so": (["layer_norm.cu"], ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "layer_norm.h")]),
     "libgated_recurrence_b200.so": (["gated_recurrence.cu"],
-                                    ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_recurrence.h")]),
+                                    ["vectors.cuh", "ssm_common.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_recurrence.h"),
+                                     os.path.join(INCLUDE, "ssm.h")]),
     "liborthogonal_b200.so": (["orthogonal.cu"],
                               ["sm100.cuh", "vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "orthogonal.h")]),
     "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],

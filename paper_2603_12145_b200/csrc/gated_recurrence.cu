@@ -18,38 +18,103 @@
 // s and 1 - s with the argument's sign, so that both are at hand to full relative precision.  Per element: three exponentials, two
 // reciprocals, one reciprocal square root.
 #include <new>
+#include <type_traits>
 
 #include "../../include/gated_recurrence.h"
 #include "on_device.cuh"
+#include "ssm_common.cuh"
 #include "vectors.cuh"
 
 namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSteps = 8;                // steps between saved states
+constexpr int kSteps = 8;                // steps of a tile, forward
+constexpr int kSaved = 4;                // steps between saved states, and of a tile, backward
 constexpr int kStepThreads = 256;
 
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// ---- scalar functions
+// ---- V channels' values: a number, or a pair that one instruction works on
+
+using ssm_k::add;
+using ssm_k::ex2;
+using ssm_k::fma;
+using ssm_k::hi;
+using ssm_k::lo;
+using ssm_k::mul;
+using ssm_k::Pair;
+using ssm_k::pair;
+using ssm_k::rcp;
+
+template <int V>
+using Vals = std::conditional_t<V == 1, float, Pair>;
+
+__device__ __forceinline__ float add(float a, float b) { return __fadd_rn(a, b); }
+__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
+__device__ __forceinline__ float fma(float a, float b, float c) { return fmaf(a, b, c); }
+
+template <int V>
+__device__ __forceinline__ Vals<V> all(float v)
+{
+    if constexpr (V == 1)
+        return v;
+    else
+        return pair(v, v);
+}
+
+// f on each channel
+template <typename F>
+__device__ __forceinline__ float each(F f, float a) { return f(a); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a) { return pair(f(lo(a)), f(hi(a))); }
+template <typename F>
+__device__ __forceinline__ float each(F f, float a, float b) { return f(a, b); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a, Pair b) { return pair(f(lo(a), lo(b)), f(hi(a), hi(b))); }
+template <typename F>
+__device__ __forceinline__ float each(F f, float a, float b, float c) { return f(a, b, c); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a, Pair b, Pair c) { return pair(f(lo(a), lo(b), lo(c)), f(hi(a), hi(b), hi(c))); }
+
+template <typename T>
+__device__ __forceinline__ float widen(const Packed<T, 1> &v) { return packed_get<T, 1>(v, 0); }
+template <typename T>
+__device__ __forceinline__ Pair widen(const Packed<T, 2> &v) { return pair(packed_get<T, 2>(v, 0), packed_get<T, 2>(v, 1)); }
+
+template <typename T>
+__device__ __forceinline__ Packed<T, 1> narrow(float v)
+{
+    const float f[1] = {v};
+    return packed_of<T, 1>(f);
+}
+template <typename T>
+__device__ __forceinline__ Packed<T, 2> narrow(Pair v)
+{
+    const float f[2] = {lo(v), hi(v)};
+    return packed_of<T, 2>(f);
+}
+
+template <int V>
+__device__ __forceinline__ Vals<V> load_floats(const float *src)
+{
+    if (src == nullptr) return all<V>(0.0f);
+    if constexpr (V == 1)
+        return src[0];
+    else
+        return pair(src[0], src[1]);
+}
+__device__ __forceinline__ void store_floats(float *dst, float v) { dst[0] = v; }
+__device__ __forceinline__ void store_floats(float *dst, Pair v)
+{
+    dst[0] = lo(v);
+    dst[1] = hi(v);
+}
+
+// ---- the functions of a step
 
 constexpr float kLog2e = 1.4426950408889634f;
-
-__device__ __forceinline__ float ex2(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-
-__device__ __forceinline__ float rcp(float v)
-{
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 
 __device__ __forceinline__ float rsq(float v)
 {
@@ -58,64 +123,71 @@ __device__ __forceinline__ float rsq(float v)
     return r;
 }
 
-// v or the bound, whichever is larger; a NaN stays.
-__device__ __forceinline__ float at_least(float v, float bound)
+// 1 / (1 + e^-v); the exponent's rounding, |v| 2^-24 of the result, is below what matters: where |v| is large, so is the
+// distance to where the sigmoid moves.
+template <typename F>
+__device__ __forceinline__ F sigmoid(F v)
 {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(v), "f"(bound));
-    return r;
+    constexpr int V = sizeof(F) / 4;
+    return each([](float e) { return rcp(e); },
+                add(each([](float e) { return ex2(e); }, mul(v, all<V>(-kLog2e))), all<V>(1.0f)));
 }
 
-// e^v for v in [-104, 0].  v log2 e is formed in two parts: rounded to one binary32 number its error would be that of the
-// exponent, |v| 2^-24 relative in the result.  A 16-bit argument's own step is far coarser: T decides.
-template <typename T>
-__device__ __forceinline__ float exp_of(float v)
+// The same, and 1 - sigmoid(v) to full relative precision.  (Beyond 2^126 the exponential stays there: its product with
+// the sigmoid is one, not infinity times zero.)
+template <typename F>
+__device__ __forceinline__ F sigmoid(F v, F &rest)
 {
-    const float t = v * kLog2e;
-    if (sizeof(T) == 2) return ex2(t);
-    constexpr float kLog2eLow = 1.9259629911e-8f;   // log2 e - float(log2 e)
-    constexpr float kLn2 = 0.6931471805599453f;
-    const float low = fmaf(v, kLog2eLow, fmaf(v, kLog2e, -t));
-    const float e = ex2(t);
-    return fmaf(e * kLn2, low, e);
+    constexpr int V = sizeof(F) / 4;
+    const F e = each([](float x) { return ex2(ssm_k::at_most(x, 126.0f)); }, mul(v, all<V>(-kLog2e)));
+    const F s = each([](float x) { return rcp(x); }, add(e, all<V>(1.0f)));
+    rest = mul(e, s);
+    return s;
 }
 
-// The smaller of sigmoid(v) and 1 - sigmoid(v), with v's sign.
-template <typename T>
-__device__ __forceinline__ float signed_sigmoid(float v)
+// e^L - 1, L <= 0: the series up to L^5 above -1/8 (the next term is under 5e-8 of the sum), else from the exponential, whose
+// error then counts eightfold at most.  (The exponent's own rounding is |L| e^L 2^-24 of one: nothing.)
+template <typename F>
+__device__ __forceinline__ F decay_less_one(F L)
 {
-    const float e = exp_of<T>(at_least(-fabsf(v), -104.0f));
-    return copysignf(e * rcp(1.0f + e), v);
-}
-__device__ __forceinline__ float sigmoid_of(float s) { return __float_as_int(s) < 0 ? -s : 1.0f - s; }
-__device__ __forceinline__ float rest_of(float s) { return __float_as_int(s) < 0 ? 1.0f + s : s; }      // 1 - sigmoid
-
-// e^L - 1, L <= 0: the series up to L^7 below 0.35 (the next term is under 2e-8 of the sum), else from the exponential, whose
-// error then counts at most twofold.
-__device__ __forceinline__ float decay_less_one(float L)
-{
-    float p = 1.0f / 5040.0f;
-    p = fmaf(p, L, 1.0f / 720.0f);
-    p = fmaf(p, L, 1.0f / 120.0f);
-    p = fmaf(p, L, 1.0f / 24.0f);
-    p = fmaf(p, L, 1.0f / 6.0f);
-    p = fmaf(p, L, 0.5f);
-    const float small = fmaf(p * L, L, L), large = exp_of<float>(at_least(L, -104.0f)) - 1.0f;
-    return L > -0.35f ? small : large;
+    constexpr int V = sizeof(F) / 4;
+    F p = fma(L, all<V>(1.0f / 120.0f), all<V>(1.0f / 24.0f));
+    p = fma(p, L, all<V>(1.0f / 6.0f));
+    p = fma(p, L, all<V>(0.5f));
+    p = fma(mul(p, L), L, L);
+    const F large = add(each([](float e) { return ex2(e); }, mul(L, all<V>(kLog2e))), all<V>(-1.0f));
+    return each([](float l, float small, float big) { return l > -0.125f ? small : big; }, L, p, large);
 }
 
 // e^L h from d = e^L - 1, with one rounding; an infinity stays one (d h and h would cancel to a NaN).
-__device__ __forceinline__ float decayed(float d, float h)
+template <typename F>
+__device__ __forceinline__ F decayed(F d, F h)
 {
-    const float v = fmaf(d, h, h);
-    return fabsf(h) == __int_as_float(0x7F800000) ? h : v;
+    return each([](float v, float w) { return fabsf(w) == __int_as_float(0x7F800000) ? w : v; }, fma(d, h, h), h);
 }
 
-// 1 / sqrt(1 - e^(2 L)) from e = e^L - 1; zero where nothing is left of it.
-__device__ __forceinline__ float inverse_gain(float e, float &square)
+// 1 - e^(2 L) = -d (2 + d)
+template <typename F>
+__device__ __forceinline__ F square_gain(F d)
 {
-    square = -e * (2.0f + e);
-    return square < 1.2e-38f ? 0.0f : rsq(square);       // a NaN passes
+    constexpr int V = sizeof(F) / 4;
+    const F minus = mul(d, all<V>(-1.0f));
+    return fma(minus, d, add(minus, minus));
+}
+
+// 1 / sqrt(square); zero where nothing is left of it (a NaN passes)
+template <typename F>
+__device__ __forceinline__ F inverse_root(F square)
+{
+    return each([](float s) { return s < 1.2e-38f ? 0.0f : rsq(s); }, square);
+}
+
+// The state after a step: gates and input of the step, the state before it.
+template <typename F>
+__device__ __forceinline__ F advance(F d, F in, F x, F before)
+{
+    const F square = square_gain(d);
+    return fma(mul(square, inverse_root(square)), mul(in, x), decayed(d, before));
 }
 
 // ---- arguments
@@ -164,145 +236,153 @@ struct Place {
     }
 };
 
-// Steps [t, t + kSteps) that start an episode, as bits.
-template <typename T>
+// Steps [t, t + K) that start an episode, as bits.
+template <int K, typename T>
 __device__ __forceinline__ uint32_t resets_at(const Params<T> &p, int64_t b, int t, int t1)
 {
     if (p.reset.ptr == nullptr) return 0;
     const int lane = threadIdx.x & 31;
-    return __ballot_sync(0xFFFFFFFFu, lane < kSteps && t + lane < t1 && *p.reset.row(b, t + lane) != 0);
+    return __ballot_sync(0xFFFFFFFFu, lane < K && t + lane < t1 && *p.reset.row(b, t + lane) != 0);
 }
 
-template <typename T, int V>
-struct Block {                       // kSteps steps of a sequence
-    Packed<T, V> v[kSteps];
+// K steps of a sequence; steps past the end are zeros.
+template <typename T, int V, int K>
+struct Block {
+    Packed<T, V> v[K];
     __device__ __forceinline__ void load(const Seq<const T> &q, const Place<V> &at, int t)
     {
         const T *ptr = q.row(at.b, t) + at.c;
+        if (t + K <= at.t1) {
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            v[k] = t + k < at.t1 ? packed_load<T, V>(ptr) : packed_zero<T, V>();
-            ptr += q.st;
+            for (int k = 0; k < K; ++k) {
+                v[k] = packed_load<T, V>(ptr);
+                ptr += q.st;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                v[k] = t + k < at.t1 ? packed_load<T, V>(ptr) : packed_zero<T, V>();
+                ptr += q.st;
+            }
         }
     }
 };
-
-template <int V>
-__device__ __forceinline__ void load_floats(float (&dst)[V], const float *src)
-{
-#pragma unroll
-    for (int e = 0; e < V; ++e) dst[e] = src == nullptr ? 0.0f : src[e];
-}
 
 // kEnds: the first pass over segments.
 template <typename T, int V, bool kEnds>
 __global__ void __launch_bounds__(kThreads)
 k_forward(const Shape s, const Params<T> p)
 {
+    using F = Vals<V>;
     allow_next();
     wait_for_previous();
     const int tiles = (s.channels + 32 * V - 1) / (32 * V);
     const int64_t warp = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     if (warp >= s.batch * s.segments * tiles) return;
     const Place<V> at(s, warp / tiles, static_cast<int>(warp % tiles));
-    float a[V], h[V], span[V];
-    load_floats<V>(a, p.a + at.c);
-    if (kEnds || (s.segments == 1 && p.state == nullptr)) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) h[e] = 0.0f;
-    } else {
-        load_floats<V>(h, s.segments > 1 ? p.carry + at.unit * s.channels + at.c : p.state + at.b * s.channels + at.c);
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) span[e] = 0.0f;
-    Block<T, V> nx, nr, ni;
+    const F a = load_floats<V>(p.a + at.c);
+    F h = all<V>(0.0f), span = h;
+    if (!kEnds)
+        h = load_floats<V>(s.segments > 1 ? p.carry + at.unit * s.channels + at.c
+                                          : p.state == nullptr ? nullptr : p.state + at.b * s.channels + at.c);
+    Block<T, V, kSteps> nx, nr, ni;
     nx.load(p.x, at, at.t0);
     nr.load(p.r, at, at.t0);
     ni.load(p.i, at, at.t0);
+    float *saved = nullptr;
+    if (!kEnds && p.saved != nullptr)
+        saved = p.saved + (at.b * ((s.time + kSaved - 1) / kSaved) + at.t0 / kSaved) * s.channels + at.c;
+    T *py = kEnds ? nullptr : p.y.row(at.b, at.t0) + at.c;
     bool cut = false;
     for (int t = at.t0; t < at.t1; t += kSteps) {
-        const Block<T, V> x = nx, r = nr, i = ni;
-        const uint32_t resets = resets_at(p, at.b, t, at.t1);
+        const Block<T, V, kSteps> x = nx, r = nr, i = ni;
+        const uint32_t resets = resets_at<kSteps>(p, at.b, t, at.t1);
         if (t + kSteps < at.t1) {
             nx.load(p.x, at, t + kSteps);
             nr.load(p.r, at, t + kSteps);
             ni.load(p.i, at, t + kSteps);
         }
-        if (!kEnds && p.saved != nullptr && at.live) {
-            float *dst = p.saved + (at.b * ((s.time + kSteps - 1) / kSteps) + t / kSteps) * s.channels + at.c;
+        // Plain: all steps are there and none starts an episode, the common case
+        auto work = [&](auto plain) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) dst[e] = h[e];
-        }
-        T *py = kEnds ? nullptr : p.y.row(at.b, t) + at.c;
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            if (t + k >= at.t1) break;
-            if ((resets >> k) & 1u) {
-                cut = true;
-#pragma unroll
-                for (int e = 0; e < V; ++e) h[e] = 0.0f;
+            for (int k = 0; k < kSteps; ++k) {
+                if (!plain.value) {
+                    if (t + k >= at.t1) break;
+                    if ((resets >> k) & 1u) {
+                        cut = true;
+                        h = all<V>(0.0f);
+                    }
+                }
+                if (!kEnds && k % kSaved == 0 && saved != nullptr) {
+                    if (at.live) store_floats(saved, h);
+                    saved += s.channels;
+                }
+                const F L = mul(a, sigmoid(widen(r.v[k])));
+                h = advance(decay_less_one(L), sigmoid(widen(i.v[k])), widen(x.v[k]), h);
+                if constexpr (kEnds) {
+                    span = add(span, L);
+                } else {
+                    if (at.live) packed_store<T, V>(py, narrow<T>(h));
+                    py += p.y.st;
+                }
             }
-            float out[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float L = a[e] * sigmoid_of(signed_sigmoid<T>(packed_get<T, V>(r.v[k], e)));
-                const float d = decay_less_one(L);
-                float square;
-                const float inverse = inverse_gain(d, square);
-                const float u = sigmoid_of(signed_sigmoid<T>(packed_get<T, V>(i.v[k], e))) * packed_get<T, V>(x.v[k], e);
-                h[e] = fmaf(square * inverse, u, decayed(d, h[e]));
-                out[e] = h[e];
-                if (kEnds) span[e] += L;
-            }
-            if (!kEnds) {
-                if (at.live) packed_store<T, V>(py, packed_of<T, V>(out));
-                py += p.y.st;
-            }
-        }
+        };
+        if (resets == 0 && t + kSteps <= at.t1)
+            work(std::true_type{});
+        else
+            work(std::false_type{});
     }
     if (!at.live) return;
-    if (kEnds) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            p.carry[at.unit * s.channels + at.c + e] = h[e];
-            p.span[at.unit * s.channels + at.c + e] = cut ? 1.0f : span[e];
-        }
+    if constexpr (kEnds) {
+        store_floats(p.carry + at.unit * s.channels + at.c, h);
+        store_floats(p.span + at.unit * s.channels + at.c, cut ? all<V>(1.0f) : span);
     } else if (at.t1 == s.time && p.state_out != nullptr) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) p.state_out[at.b * s.channels + at.c + e] = h[e];
+        store_floats(p.state_out + at.b * s.channels + at.c, h);
     }
 }
 
 // Chains the segments of a row: each end is replaced by the value that enters the segment.  From the first segment on
 // (forward: states) or from the last one back (gradients).
-constexpr int kAhead = 8;
+constexpr int kAhead = 16;
+constexpr int kCarryThreads = 64;
 
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kCarryThreads)
 k_carry(const Shape s, float *carry, const float *span, const float *start, const int backward)
 {
     allow_next();
     wait_for_previous();
-    const int64_t index = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    const int64_t index = static_cast<int64_t>(blockIdx.x) * kCarryThreads + threadIdx.x;
     if (index >= s.batch * s.channels) return;
     const int64_t b = index / s.channels;
     const int c = static_cast<int>(index - b * s.channels);
-    const int64_t base = b * s.segments * s.channels + c;
+    const int64_t step = backward ? -s.channels : s.channels;
+    int64_t at = b * s.segments * s.channels + c + (backward ? static_cast<int64_t>(s.segments - 1) * s.channels : 0);
     float h = start == nullptr ? 0.0f : start[index];
-    for (int g0 = 0; g0 < s.segments; g0 += kAhead) {
-        float end[kAhead], sum[kAhead];
+    float end[2][kAhead], sum[2][kAhead];
+    auto fetch = [&](int from, int64_t first, float (&e)[kAhead], float (&l)[kAhead]) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int g = min(g0 + k, s.segments - 1);
-            const int64_t at = base + static_cast<int64_t>(backward ? s.segments - 1 - g : g) * s.channels;
-            end[k] = carry[at];
-            sum[k] = span[at];
+            const bool in = from + k < s.segments;
+            e[k] = in ? carry[first + k * step] : 0.0f;
+            l[k] = in ? span[first + k * step] : 0.0f;
         }
+    };
+    auto chain = [&](int from, const float (&e)[kAhead], const float (&l)[kAhead]) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (g0 + k >= s.segments) break;
-            carry[base + static_cast<int64_t>(backward ? s.segments - 1 - g0 - k : g0 + k) * s.channels] = h;
-            h = sum[k] > 0.0f ? end[k] : decayed(decay_less_one(sum[k]), h) + end[k];
+            if (from + k >= s.segments) break;
+            carry[at] = h;
+            at += step;
+            const float d = decay_less_one(l[k]);
+            h = l[k] > 0.0f ? e[k] : decayed(d, h) + e[k];
         }
+    };
+    fetch(0, at, end[0], sum[0]);
+    for (int g = 0; g < s.segments; g += 2 * kAhead) {       // the next ones are under way while these are chained
+        fetch(g + kAhead, at + kAhead * step, end[1], sum[1]);
+        chain(g, end[0], sum[0]);
+        fetch(g + 2 * kAhead, at + kAhead * step, end[0], sum[0]);
+        chain(g + kAhead, end[1], sum[1]);
     }
 }
 
@@ -310,6 +390,7 @@ template <typename T, int V, bool kEnds>
 __global__ void __launch_bounds__(kThreads)
 k_backward(const Shape s, const Params<T> p)
 {
+    using F = Vals<V>;
     allow_next();
     wait_for_previous();
     const int tiles = (s.channels + 32 * V - 1) / (32 * V);
@@ -317,131 +398,110 @@ k_backward(const Shape s, const Params<T> p)
     const int64_t units = s.batch * s.segments, slot = warp / tiles, slots = kEnds ? units : s.slots;
     if (slot >= slots) return;
     const int tile = static_cast<int>(warp % tiles);
-    const int chunks = (s.time + kSteps - 1) / kSteps;
-    float a[V], da[V];
+    const int chunks = (s.time + kSaved - 1) / kSaved;
+    const F zero = all<V>(0.0f), one = all<V>(1.0f);
+    F da = zero;
     int c = 0;
     bool live = false;
-#pragma unroll
-    for (int e = 0; e < V; ++e) da[e] = 0.0f;
     for (int64_t unit = slot; unit < units; unit += slots) {
         const Place<V> at(s, unit, tile);
         c = at.c;
         live = at.live;
-        load_floats<V>(a, p.a + c);
-        float g[V], span[V];             // g: what comes from behind the step
-        if (kEnds) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) g[e] = span[e] = 0.0f;
-        } else {
-            load_floats<V>(g, s.segments > 1 ? p.carry + unit * s.channels + c
-                                             : p.dstate_out == nullptr ? nullptr : p.dstate_out + at.b * s.channels + c);
-        }
+        const F a = load_floats<V>(p.a + c);
+        F g = zero, span = zero;         // g: what comes from behind the step
+        if (!kEnds)
+            g = load_floats<V>(s.segments > 1 ? p.carry + unit * s.channels + c
+                                              : p.dstate_out == nullptr ? nullptr : p.dstate_out + at.b * s.channels + c);
         bool cut = false;
-        Block<T, V> nx, nr, ni, ndy;
-        float nh[V];
+        constexpr int K = kSaved;
+        Block<T, V, K> nx, nr, ni, ndy;
+        F nh = zero;
         auto fetch = [&](int t) {
             nr.load(p.r, at, t);
             ndy.load(p.dy, at, t);
             if (!kEnds) {
                 nx.load(p.x, at, t);
                 ni.load(p.i, at, t);
-                load_floats<V>(nh, p.saved + (at.b * chunks + t / kSteps) * s.channels + c);
+                nh = load_floats<V>(p.saved + (at.b * chunks + t / K) * s.channels + c);
             }
         };
-        const int last = at.t0 + (at.t1 - 1 - at.t0) / kSteps * kSteps;
+        const int last = at.t0 + (at.t1 - 1 - at.t0) / K * K;
         fetch(last);
-        for (int t = last; t >= at.t0; t -= kSteps) {
-            const Block<T, V> x = nx, r = nr, i = ni, dy = ndy;
-            const uint32_t resets = resets_at(p, at.b, t, at.t1);
-            float h[V];
-            if (!kEnds) {
+        for (int t = last; t >= at.t0; t -= K) {
+            const Block<T, V, K> x = nx, r = nr, i = ni, dy = ndy;
+            const uint32_t resets = resets_at<K>(p, at.b, t, at.t1);
+            F h = nh;
+            if (t > at.t0) fetch(t - K);
+            auto work = [&](auto plain) {
+                if constexpr (kEnds) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) h[e] = nh[e];
-            }
-            if (t > at.t0) fetch(t - kSteps);
-            if constexpr (kEnds) {
-#pragma unroll
-                for (int k = kSteps - 1; k >= 0; --k) {
-                    if (t + k >= at.t1) continue;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float L = a[e] * sigmoid_of(signed_sigmoid<T>(packed_get<T, V>(r.v[k], e)));
-                        g[e] += packed_get<T, V>(dy.v[k], e);
-                        g[e] = decayed(decay_less_one(L), g[e]);
-                        span[e] += L;
+                    for (int k = K - 1; k >= 0; --k) {
+                        if (!plain.value && t + k >= at.t1) continue;
+                        const F L = mul(a, sigmoid(widen(r.v[k]))), gt = add(g, widen(dy.v[k]));
+                        g = fma(decay_less_one(L), gt, gt);
+                        span = add(span, L);
+                        if (!plain.value && (resets >> k) & 1u) {
+                            cut = true;
+                            g = zero;
+                        }
                     }
-                    if ((resets >> k) & 1u) {
-                        cut = true;
+                } else {
+                    // the steps' gates and the states before them
+                    F gate[K], slope[K], in[K], out[K], d[K], inverse[K], before[K];
 #pragma unroll
-                        for (int e = 0; e < V; ++e) g[e] = 0.0f;
+                    for (int k = 0; k < K; ++k) {
+                        F rest;
+                        gate[k] = sigmoid(widen(r.v[k]), rest);
+                        in[k] = sigmoid(widen(i.v[k]), out[k]);
+                        const F L = mul(a, gate[k]);
+                        slope[k] = mul(L, rest);             // dL / dr
+                        d[k] = decay_less_one(L);
+                        const F square = square_gain(d[k]);
+                        inverse[k] = inverse_root(square);
+                        before[k] = h;
+                        if (!plain.value && (resets >> k) & 1u) before[k] = zero;
+                        h = fma(mul(square, inverse[k]), mul(in[k], widen(x.v[k])), fma(d[k], before[k], before[k]));
                     }
+                    F sum = zero;        // of these steps' terms of da: shorter chains
+                    T *pdx = p.dx.row(at.b, t + K - 1) + c, *pdr = p.dr.row(at.b, t + K - 1) + c, *pdi = p.di.row(at.b, t + K - 1) + c;
+#pragma unroll
+                    for (int k = K - 1; k >= 0; --k) {
+                        if (plain.value || t + k < at.t1) {
+                            const F u = mul(in[k], widen(x.v[k])), gt = add(g, widen(dy.v[k]));
+                            const F into = mul(gt, mul(square_gain(d[k]), inverse[k]));
+                            const F keep = add(d[k], one);
+                            const F dL = mul(mul(gt, keep), fma(mul(u, all<V>(-1.0f)), mul(keep, inverse[k]), before[k]));
+                            sum = fma(dL, gate[k], sum);
+                            g = fma(d[k], gt, gt);
+                            if (!plain.value && (resets >> k) & 1u) g = zero;
+                            if (live) {
+                                packed_store<T, V>(pdx, narrow<T>(mul(into, in[k])));
+                                packed_store<T, V>(pdr, narrow<T>(mul(dL, slope[k])));
+                                packed_store<T, V>(pdi, narrow<T>(mul(mul(into, u), out[k])));
+                            }
+                        }
+                        pdx -= p.dx.st;
+                        pdr -= p.dr.st;
+                        pdi -= p.di.st;
+                    }
+                    da = add(da, sum);
                 }
-            } else {
-                // the steps' gates and the states before them
-                float sr[kSteps][V], si[kSteps][V], d[kSteps][V], inverse[kSteps][V], before[kSteps][V];
-#pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    const bool fresh = (resets >> k) & 1u;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        sr[k][e] = signed_sigmoid<T>(packed_get<T, V>(r.v[k], e));
-                        si[k][e] = signed_sigmoid<T>(packed_get<T, V>(i.v[k], e));
-                        d[k][e] = decay_less_one(a[e] * sigmoid_of(sr[k][e]));
-                        float square;
-                        inverse[k][e] = inverse_gain(d[k][e], square);
-                        before[k][e] = fresh ? 0.0f : h[e];
-                        h[e] = fmaf(square * inverse[k][e], sigmoid_of(si[k][e]) * packed_get<T, V>(x.v[k], e),
-                                    decayed(d[k][e], before[k][e]));
-                    }
-                }
-                float sum[V];                // of these steps' terms of da: shorter chains
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-                T *pdx = p.dx.row(at.b, t) + c, *pdr = p.dr.row(at.b, t) + c, *pdi = p.di.row(at.b, t) + c;
-#pragma unroll
-                for (int k = kSteps - 1; k >= 0; --k) {
-                    if (t + k >= at.t1) continue;
-                    float dx[V], dr[V], di[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float gate = sigmoid_of(sr[k][e]), in = sigmoid_of(si[k][e]), xv = packed_get<T, V>(x.v[k], e);
-                        const float gt = g[e] + packed_get<T, V>(dy.v[k], e);
-                        const float square = -d[k][e] * (2.0f + d[k][e]);
-                        const float gain = gt * (square * inverse[k][e]);
-                        dx[e] = gain * in;
-                        di[e] = dx[e] * xv * rest_of(si[k][e]);
-                        const float decay = 1.0f + d[k][e];
-                        const float dL = gt * decay * (before[k][e] - in * xv * decay * inverse[k][e]);
-                        dr[e] = dL * (a[e] * gate) * rest_of(sr[k][e]);
-                        sum[e] = fmaf(dL, gate, sum[e]);
-                        g[e] = (resets >> k) & 1u ? 0.0f : decayed(d[k][e], gt);
-                    }
-                    if (live) {
-                        packed_store<T, V>(pdx + k * p.dx.st, packed_of<T, V>(dx));
-                        packed_store<T, V>(pdr + k * p.dr.st, packed_of<T, V>(dr));
-                        packed_store<T, V>(pdi + k * p.di.st, packed_of<T, V>(di));
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < V; ++e) da[e] += sum[e];
-            }
+            };
+            if (resets == 0 && t + K <= at.t1)
+                work(std::true_type{});
+            else
+                work(std::false_type{});
         }
         if (!live) continue;
-        if (kEnds) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                p.carry[unit * s.channels + c + e] = g[e];
-                p.span[unit * s.channels + c + e] = cut ? 1.0f : span[e];
-            }
+        if constexpr (kEnds) {
+            store_floats(p.carry + unit * s.channels + c, g);
+            store_floats(p.span + unit * s.channels + c, cut ? one : span);
         } else if (at.segment == 0 && p.dstate != nullptr) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) p.dstate[at.b * s.channels + c + e] = g[e];
+            store_floats(p.dstate + at.b * s.channels + c, g);
         }
     }
     if constexpr (!kEnds) {
-        if (!live) return;
-#pragma unroll
-        for (int e = 0; e < V; ++e) p.part[slot * s.channels + c + e] = da[e];
+        if (live) store_floats(p.part + slot * s.channels + c, da);
     }
 }
 
@@ -495,14 +555,19 @@ k_step(const Step<T> p)
     const Packed<float, V> state = packed_load<float, V>(p.state + n * p.channels + c);
     const bool fresh = p.done != nullptr && p.done[n * p.done_stride] != 0;
     float h[V];
+    if constexpr (V == 1) {
+        h[0] = advance(decay_less_one(mul(__ldg(p.a + c), sigmoid(widen(r)))), sigmoid(widen(i)), widen(x),
+                       fresh ? 0.0f : packed_get<float, 1>(state, 0));
+    } else {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const float before = fresh ? 0.0f : packed_get<float, V>(state, e);
-        const float d = decay_less_one(__ldg(p.a + c + e) * sigmoid_of(signed_sigmoid<T>(packed_get<T, V>(r, e))));
-        float square;
-        const float inverse = inverse_gain(d, square);
-        const float u = sigmoid_of(signed_sigmoid<T>(packed_get<T, V>(i, e))) * packed_get<T, V>(x, e);
-        h[e] = fmaf(square * inverse, u, decayed(d, before));
+        for (int e = 0; e < V; e += 2) {
+            auto two = [&](const auto &v) { return pair(packed_get<T, V>(v, e), packed_get<T, V>(v, e + 1)); };
+            const Pair before = fresh ? pair(0.0f, 0.0f) : pair(packed_get<float, V>(state, e), packed_get<float, V>(state, e + 1));
+            const Pair a = pair(__ldg(p.a + c + e), __ldg(p.a + c + e + 1));
+            const Pair v = advance(decay_less_one(mul(a, sigmoid(two(r)))), sigmoid(two(i)), two(x), before);
+            h[e] = lo(v);
+            h[e + 1] = hi(v);
+        }
     }
     packed_store<float, V>(p.state_out + n * p.channels + c, packed_of<float, V>(h));
     packed_store<T, V>(p.y + n * p.y_stride + c, packed_of<T, V>(h));
@@ -541,7 +606,7 @@ Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool back
     s.time = static_cast<int>(time);
     s.channels = p->channels;
     const int64_t tiles = div_up(p->channels, 64), warps = batch * tiles;
-    const int64_t resident = static_cast<int64_t>(p->sms) * (backward ? 12 : 24);
+    const int64_t resident = static_cast<int64_t>(p->sms) * (backward ? 16 : 20);
     const int64_t chunks = div_up(time, kSteps);
     s.segments = 1;
     s.segment_steps = static_cast<int>(chunks * kSteps);
@@ -669,13 +734,13 @@ int launch(gated_recurrence *p, const Shape &s, const Params<T> &k, bool backwar
 {
     const int64_t tiles = div_up(s.channels, 32 * V), units = s.batch * s.segments;
     const int64_t blocks = div_up(units * tiles, kWarps);
-    if (blocks > kMaxBlocks || div_up(s.batch * s.channels, kThreads) > kMaxBlocks) return GATED_RECURRENCE_EINVAL;
+    if (blocks > kMaxBlocks || div_up(s.batch * s.channels, kCarryThreads) > kMaxBlocks) return GATED_RECURRENCE_EINVAL;
     bool ok = true;
     int launched = 0;
     if (s.segments > 1) {
         ok = backward ? (k_backward<T, V, true><<<static_cast<unsigned>(blocks), kThreads, 0, p->stream>>>(s, k), cudaGetLastError() == cudaSuccess)
                       : (k_forward<T, V, true><<<static_cast<unsigned>(blocks), kThreads, 0, p->stream>>>(s, k), cudaGetLastError() == cudaSuccess);
-        ok = ok && launch_after(p->stream, div_up(s.batch * s.channels, kThreads), kThreads, k_carry, s, k.carry,
+        ok = ok && launch_after(p->stream, div_up(s.batch * s.channels, kCarryThreads), kCarryThreads, k_carry, s, k.carry,
                                 static_cast<const float *>(k.span), backward ? k.dstate_out : k.state, backward ? 1 : 0);
         launched += 2;
     }
@@ -811,7 +876,7 @@ int gated_recurrence_set_stream(gated_recurrence *p, void *cuda_stream)
 size_t gated_recurrence_saved_bytes(const gated_recurrence *p, int64_t batch, int64_t time)
 {
     if (p == nullptr || !sizes_ok(batch, time)) return 0;
-    return static_cast<size_t>(batch) * div_up(time, kSteps) * p->channels * sizeof(float);
+    return static_cast<size_t>(batch) * div_up(time, kSaved) * p->channels * sizeof(float);
 }
 
 size_t gated_recurrence_workspace_bytes(const gated_recurrence *p, int64_t batch, int64_t time, int backward)

@@ -217,7 +217,7 @@ def cuts(fake):                                                                 
             fake.lib.fake_clear()
             assert call(h, ctypes.byref(a)) == 0
             assert len([e for e in fake.entries() if e[0] == "launch"]) == want, (batch, time, fake.entries())
-        assert L.gated_recurrence_saved_bytes(h, batch, time) == batch * -(-time // 8) * 96 * 4
+        assert L.gated_recurrence_saved_bytes(h, batch, time) == batch * -(-time // 4) * 96 * 4
 
 
 if __name__ == "__main__":
