@@ -35,7 +35,7 @@ namespace {
 constexpr int kBK = 64;                          // reduction elements per stage
 constexpr int kRowsPerBlock = 128;               // rows of A per block; a pair's tile has twice as many
 constexpr int kTileM = 2 * kRowsPerBlock;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kABytes = kRowsPerBlock * kBK * 2;
 constexpr int kBBytes = 128 * kBK * 2;           // at most 128 rows of B per block
 constexpr int kStageBytes = kABytes + kBBytes;
@@ -43,39 +43,60 @@ constexpr int kAccCols = 256;
 constexpr int kTmemCols = 2 * kAccCols;
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-constexpr int kSmem = kStages * kStageBytes + 256 + 1024;
-static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+constexpr int kShare = 4;                        // pairs that share a tile's reduction, in a cluster of eight blocks
+constexpr int kShareCols = 128;                  // columns of such a tile, at most
+constexpr int kExchange = (kShare - 1) * kRowsPerBlock * (kShareCols / kShare) * 4;
+constexpr int kBlock = 32 * 64;                  // 32 rows x 32 columns of 16 bits on their way between registers and memory
+constexpr int kSets = 2;                         // per epilogue warp: one worked on, the other on its way in; two planes each
+constexpr int kStaging = 2 * kSets * kBlock;
+// (what pairs exchange and what is staged take turns: a product does one or the other)
+constexpr int kBesides = kEpilogueWarps * kStaging;
+constexpr int kBarrierBytes = 512;
+constexpr int kSmem = kStages * kStageBytes + kBesides + kBarrierBytes + 1024;
+static_assert(kSmem <= 227 * 1024 && kExchange <= kBesides, "shared memory of a block");
 
 constexpr int kRowThreads = 256;                 // blocks of the kernels that read and write rows
-constexpr int kMostParts = 128;                  // partial sums of squares per matrix
+constexpr int kMostParts = 592;                  // partial sums of squares per matrix
 
 // Operands are held times 2^13: an element of a normalised matrix of a million is about 2^-10, of A and B up to 2^2.
 constexpr float kScale = 8192.0f;
 constexpr float kUnscale = 1.0f / kScale;
 
-enum Mode { kGram, kSquare, kApply, kLast };
-
+// A product of the iteration, and how it is cut.
 struct Product {
     int m, n, k;            // rows of A, rows of B, reduction length, of one matrix
-    int batch;
     int a_rows, b_rows;     // 1: the operand is stored [k][rows] (MN-major), 0: [rows][k]
+    int symmetric;          // only tiles with elements on or above the diagonal
     int tile_n;             // columns of D per tile: 256, 128 or 64
     int m_tiles, n_tiles;
     int tiles;              // of one matrix: those that are computed
     int steps;              // ceil(k / 64)
+    int shared;             // 1: the pairs of a cluster share each tile's reduction
+};
+
+struct Iteration {
+    Product gram, square, apply;
+    int batch, steps;
     int tall;               // rows > cols: the diagonal's factors go with columns
+    int share;              // pairs per cluster: 1 or kShare
     int ld;                 // elements between rows of X
     int ldk;                // of O and P
     int dk;                 // elements between the diagonals of two matrices
     float a, b, c;
     __half *o, *p;
     float *d, *e;
-    const __half *hi, *lo;
-    __half *hi_next, *lo_next;
-    __nv_bfloat16 *out;     // kLast
+    __half *hi[2], *lo[2];
+    __nv_bfloat16 *out;
     int64_t out_batch, out_row;
     int out_whole;          // rows of the update start on 16-byte boundaries
+    unsigned *arrived;      // blocks that have finished a product, all products so far
     int *err;
+};
+
+// The operands, by product and by which of X's two places holds it; and blocks of 32 x 32 of what the epilogues read and write.
+struct Maps {
+    CUtensorMap gram_a[2], gram_b[2], square_a, square_b, apply_a[2], apply_b[2];
+    CUtensorMap hi[2], lo[2], o, p, out;
 };
 
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -99,18 +120,27 @@ __device__ __forceinline__ void tma_load_matrix(uint32_t dst, const CUtensorMap 
         : "memory");
 }
 
+// The mbarrier at this shared-memory offset in both blocks of the pair whose first block has rank `leader` in the cluster
+// receives one arrival once every instruction issued so far by this thread is done.
+__device__ __forceinline__ void umma_commit(uint32_t bar, uint32_t leader)
+{
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"(static_cast<uint16_t>(3u << leader))
+        : "memory");
+}
+
 struct Tile {
     int z, row, col;         // matrix, first row and column
 };
 
 // Symmetric products: row block I has the column tiles from the one of its first diagonal element on.
-template <int kMode>
 __device__ __forceinline__ Tile tile_at(const Product &p, int index)
 {
     Tile t;
     t.z = index / p.tiles;
     int i = index - t.z * p.tiles;
-    if (kMode == kGram || kMode == kSquare) {
+    if (p.symmetric) {
         const int per = kTileM / p.tile_n;
         int r = 0;
         while (i >= p.n_tiles - r * per) {
@@ -126,6 +156,21 @@ __device__ __forceinline__ Tile tile_at(const Product &p, int index)
     }
     return t;
 }
+
+// Which tiles a pair works on, and which steps of their reduction.
+struct Walk {
+    int index, step, end, k0, k1;
+    __device__ Walk(const Iteration &q, const Product &p)
+    {
+        const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
+        const int sub = p.shared ? pair % q.share : 0;
+        index = p.shared ? pair / q.share : pair;
+        step = p.shared ? pairs / q.share : pairs;
+        end = p.tiles * q.batch;
+        k0 = p.shared ? p.steps * sub / q.share : 0;
+        k1 = p.shared ? p.steps * (sub + 1) / q.share : p.steps;
+    }
+};
 
 __device__ __forceinline__ uint32_t pack2(float a, float b)
 {
@@ -151,52 +196,252 @@ __device__ __forceinline__ void store16(void *row, int c, int width, const uint3
     if (c + 8 < width) dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// Elements (i, j0 .. j0 + 15) of a symmetric matrix of k rows: those above the diagonal to both places, a zero on it.
-__device__ __forceinline__ void store_symmetric(__half *base, int ldk, int k, int i, int j0, const float (&v)[16])
+// Elements (i, j0 .. j0 + 15) of a symmetric matrix of k rows to their places across the diagonal; neighbouring lanes have
+// neighbouring rows.
+__device__ __forceinline__ void store_mirrored(__half *base, int ldk, int k, int i, int j0, const uint32_t (&w)[8])
 {
-    __half *mirror = base + static_cast<int64_t>(j0) * ldk + i;
-    if (j0 > i) {
-        uint32_t w[8];
+    if (i >= k) return;
+    uint16_t *dst = reinterpret_cast<uint16_t *>(base + static_cast<int64_t>(j0) * ldk + i);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) w[q] = pack2(v[2 * q], v[2 * q + 1]);
-        store16(base + static_cast<int64_t>(i) * ldk, j0, ldk, w);
+    for (int q = 0; q < 16; ++q) {
+        if (j0 + q < k) *dst = static_cast<uint16_t>(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
+        dst += ldk;
+    }
+}
+
+// The lane's row of a staged block (64-byte swizzle): 16-byte piece i.
+__device__ __forceinline__ uint32_t piece16(uint32_t block, int lane, int i) { return block + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4); }
+
+__device__ __forceinline__ void put16(uint32_t block, int lane, int h, const uint32_t (&w)[8])
+{
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            if (j0 + q < k)
-                *reinterpret_cast<uint16_t *>(mirror + static_cast<int64_t>(q) * ldk) =
-                    static_cast<uint16_t>(q & 1 ? w[q / 2] >> 16 : w[q / 2]);
-        }
-    } else if (j0 + 15 >= i) {
+    for (int i = 0; i < 2; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(piece16(block, lane, 2 * h + i)), "r"(w[4 * i]), "r"(w[4 * i + 1]),
+                     "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                     : "memory");
+}
+
+__device__ __forceinline__ void get16(uint32_t block, int lane, int h, uint32_t (&w)[8])
+{
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const int j = j0 + q;
-            if (j < i || j >= k) continue;
-            const __half h = j == i ? __float2half_rn(0.0f) : __float2half_rn(v[q]);
-            base[static_cast<int64_t>(i) * ldk + j] = h;
-            mirror[static_cast<int64_t>(q) * ldk] = h;
+    for (int i = 0; i < 2; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                     : "r"(piece16(block, lane, 2 * h + i))
+                     : "memory");
+}
+
+// A 32 x 32 block of matrix z, with this block's own barrier.
+__device__ __forceinline__ void tma_load_block(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+
+__device__ __forceinline__ void tma_store_block(const CUtensorMap *map, int x, int y, int z, uint32_t src)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
+                 "r"(z), "r"(src)
+                 : "memory");
+}
+
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// The copies' reads of shared memory are done.
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ unsigned load_acquire(const unsigned *p)
+{
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void add_release(unsigned *p)
+{
+    asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
+}
+
+// Waits until `target` blocks have finished; gives up as mbar_wait does.
+__device__ bool wait_arrived(const unsigned *arrived, unsigned target, volatile int *abort_flag)
+{
+    unsigned long long t0 = 0;
+    for (uint32_t spin = 0;; ++spin) {
+        if (load_acquire(arrived) >= target) return true;
+        if ((spin & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const unsigned long long now = global_timer_ns();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                return false;
+            }
         }
     }
 }
 
-template <int kMode>
+__device__ __forceinline__ void mbar_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// What this thread (and those it synchronised with) wrote to the other block's shared memory is there for who waits.
+__device__ __forceinline__ void mbar_arrive_release_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+
+// mbar_wait for a barrier on which other blocks of the cluster arrive, having written to this one's shared memory.
+__device__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag)
+{
+    unsigned long long t0 = 0;
+    for (uint32_t spin = 0;; ++spin) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if ((spin & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const unsigned long long now = global_timer_ns();
+            if (t0 == 0) {
+                t0 = now;
+            } else if (now - t0 > kWaitLimitNs) {
+                *abort_flag = 1;
+                return false;
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ void store_remote(uint32_t cluster_addr, const uint32_t *v)
+{
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+                 : "memory");
+}
+
+__device__ __forceinline__ float4 load_shared4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// ---- epilogues: elements (row, j0 .. j0 + 15) of a product, times 2^26, to what is stored of them.  Rows and columns past
+// the matrix go along; nothing of them is kept.
+
+// A: times 2^13 to O with a zero on the diagonal, which goes to d as it is
+__device__ __forceinline__ void finish_gram(const Iteration &q, int z, int row, int j0, const float (&acc)[16], uint32_t (&w)[8])
+{
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = acc[e] * kUnscale;
+    if (j0 <= row && row < j0 + 16 && row < q.gram.m) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if (j0 + e == row) {
+                q.d[static_cast<int64_t>(z) * q.dk + row] = v[e] * kUnscale;
+                v[e] = 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+}
+
+// B from O's products, O itself and the diagonal d, of which di is the row's: likewise to P and e.  w: O in, P out.
+__device__ __forceinline__ void finish_square(const Iteration &q, int z, int row, int j0, float di, const float (&acc)[16], uint32_t (&w)[8])
+{
+    if (j0 >= q.gram.m) return;
+    const int64_t diagonal = static_cast<int64_t>(z) * q.dk;
+    float v[16], s[16];
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        // (the diagonals are padded to whole pieces of 16)
+        const float4 dj = *reinterpret_cast<const float4 *>(q.d + diagonal + j0 + e);
+        const float2 o0 = unpack2(w[e / 2]), o1 = unpack2(w[e / 2 + 1]);
+        const float o[4] = {o0.x, o0.y, o1.x, o1.y}, ds[4] = {dj.x, dj.y, dj.z, dj.w};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+            s[e + f] = acc[e + f] * kUnscale;
+            v[e + f] = fmaf(q.c, fmaf(di + ds[f], o[f], s[e + f]), q.b * o[f]);
+        }
+    }
+    if (j0 <= row && row < j0 + 16 && row < q.gram.m) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if (j0 + e == row) {
+                q.e[diagonal + row] = fmaf(q.c, fmaf(di, di, s[e] * kUnscale), q.b * di);
+                v[e] = 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
+}
+
+// X' from X = hi + lo in, hi and lo out; of the last product the update instead of hi.  factor: a, and e of the row where the
+// diagonal goes with rows.
+__device__ __forceinline__ void finish_apply(const Iteration &q, bool last, int z, int j0, float factor, const float (&acc)[16],
+                                             uint32_t (&hi)[8], uint32_t (&lo)[8])
+{
+    float v[16];
+    const bool by_columns = q.tall && j0 < q.apply.n;
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+        float f[4] = {factor, factor, factor, factor};
+        if (by_columns) {
+            const float4 ej = *reinterpret_cast<const float4 *>(q.e + static_cast<int64_t>(z) * q.dk + j0 + e);
+            f[0] += ej.x, f[1] += ej.y, f[2] += ej.z, f[3] += ej.w;
+        }
+#pragma unroll
+        for (int g = 0; g < 4; g += 2) {
+            const float2 h = unpack2(hi[(e + g) / 2]), l = unpack2(lo[(e + g) / 2]);
+            v[e + g] = fmaf(f[g], h.x + l.x, acc[e + g] * kUnscale);
+            v[e + g + 1] = fmaf(f[g + 1], h.y + l.y, acc[e + g + 1] * kUnscale);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (last) {
+            hi[e] = pack_bf16(v[2 * e] * kUnscale, v[2 * e + 1] * kUnscale);
+        } else {
+            hi[e] = pack2(v[2 * e], v[2 * e + 1]);
+            const float2 h = unpack2(hi[e]);
+            lo[e] = pack2(v[2 * e] - h.x, v[2 * e + 1] - h.y);
+        }
+    }
+}
+
+// The whole iteration: one block per SM, all at once on the device; blocks wait for one another between products.
 __global__ void __launch_bounds__(kThreads, 1)
-k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const __grid_constant__ Product p)
+k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q)
 {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t stages = (raw + 1023u) & ~1023u;
-    const uint32_t bars = stages + kStages * kStageBytes;
+    const uint32_t besides = stages + kStages * kStageBytes;
+    const uint32_t bars = besides + kBesides;
     uint8_t *bars_ptr = smem_raw + (bars - raw);
     const uint32_t full0 = bars, empty0 = bars + 8 * kStages;
     const uint32_t acc_full0 = bars + 16 * kStages, acc_empty0 = acc_full0 + 16;
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars_ptr + 16 * kStages + 32);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(bars_ptr + 16 * kStages + 32 + 8);
+    const uint32_t ready = acc_empty0 + 16, received = ready + 8, staged0 = received + 8;        // the last: kSets per epilogue warp
+    uint8_t *words = bars_ptr + 16 * kStages + 48 + 8 * kSets * kEpilogueWarps;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(words);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(words + 4);
+    unsigned *finished = reinterpret_cast<unsigned *>(words + 8);     // epilogue warps, all products so far
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_cta_rank();
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int b_half = p.tile_n / 2;
-    const int all = p.tiles * p.batch;
+    const uint32_t cluster_rank = cluster_cta_rank(), rank = cluster_rank & 1;            // pairs are neighbours in the cluster
+    const uint32_t leader = cluster_rank & ~1u;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -207,51 +452,62 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
             mbar_init(acc_full0 + 8 * b, 1);
             mbar_init(acc_empty0 + 8 * b, 2 * kEpilogueWarps);
         }
+        mbar_init(ready, 1);
+        mbar_init(received, (kShare - 1) * kEpilogueWarps / 2);
+        for (int i = 0; i < kSets * kEpilogueWarps; ++i) mbar_init(staged0 + 8 * i, 1);
         *abort_flag = 0;
+        *finished = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    allow_next();
     if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), kTmemCols);
     tc_fence_before_sync();
     cluster_sync_all();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    wait_for_previous();                     // operands are its results, and outputs what it still reads
 
+    const int products = 3 * q.steps;
     if (warp == 0) {
         if (lane == 0) {
-            asm volatile("fence.proxy.async.global;" ::: "memory");    // the previous kernel wrote the operands by plain stores
             uint32_t s = 0, ph = 0;
             bool ok = true;
-            const int b_boxes = (b_half + 63) / 64;
-            const uint32_t bytes = kABytes + (p.b_rows ? b_boxes * 64 * kBK * 2 : b_half * kBK * 2);
-            for (int index = pair; ok && index < all; index += pairs) {
-                const Tile t = tile_at<kMode>(p, index);
-                const int a0 = t.row + static_cast<int>(rank) * kRowsPerBlock, b0 = t.col + static_cast<int>(rank) * b_half;
-                for (int kc = 0; kc < p.steps; ++kc) {
-                    if (!mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t dst = stages + s * kStageBytes;
-                    const uint32_t full = map_to_rank(full0 + 8 * s, 0);
-                    if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * bytes);
-                    if (p.a_rows) {
-                        tma_load_matrix(dst, &tm_a, a0, kc * kBK, t.z, full);
-                        tma_load_matrix(dst + kABytes / 2, &tm_a, a0 + 64, kc * kBK, t.z, full);
-                    } else {
-                        tma_load_matrix(dst, &tm_a, kc * kBK, a0, t.z, full);
-                    }
-                    if (p.b_rows) {
-                        for (int i = 0; i < b_boxes; ++i)
-                            tma_load_matrix(dst + kABytes + i * 64 * kBK * 2, &tm_b, b0 + 64 * i, kc * kBK, t.z, full);
-                    } else {
-                        tma_load_matrix(dst + kABytes, &tm_b, kc * kBK, b0, t.z, full);
-                    }
-                    if (++s == kStages) {
-                        s = 0;
-                        ph ^= 1u;
+            for (int i = 0; ok && i < products; ++i) {
+                const int kind = i % 3, from = i / 3 & 1;
+                const Product &p = kind == 0 ? q.gram : kind == 1 ? q.square : q.apply;
+                const CUtensorMap *tm_a = kind == 0 ? &maps.gram_a[from] : kind == 1 ? &maps.square_a : &maps.apply_a[from];
+                const CUtensorMap *tm_b = kind == 0 ? &maps.gram_b[from] : kind == 1 ? &maps.square_b : &maps.apply_b[from];
+                if (i > 0) ok = wait_arrived(q.arrived, static_cast<unsigned>(i) * gridDim.x, abort_flag);
+                mbar_arrive(ready);
+                asm volatile("fence.proxy.async;" ::: "memory");      // some of the operands were written by plain stores
+                const int b_half = p.tile_n / 2, b_boxes = (b_half + 63) / 64;
+                const uint32_t bytes = kABytes + (p.b_rows ? b_boxes * 64 * kBK * 2 : b_half * kBK * 2);
+                for (Walk w(q, p); ok && w.index < w.end; w.index += w.step) {
+                    const Tile t = tile_at(p, w.index);
+                    const int a0 = t.row + static_cast<int>(rank) * kRowsPerBlock, b0 = t.col + static_cast<int>(rank) * b_half;
+                    for (int kc = w.k0; kc < w.k1; ++kc) {
+                        if (!mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) {
+                            ok = false;
+                            break;
+                        }
+                        const uint32_t dst = stages + s * kStageBytes;
+                        const uint32_t full = map_to_rank(full0 + 8 * s, leader);
+                        if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * bytes);
+                        if (p.a_rows) {
+                            tma_load_matrix(dst, tm_a, a0, kc * kBK, t.z, full);
+                            tma_load_matrix(dst + kABytes / 2, tm_a, a0 + 64, kc * kBK, t.z, full);
+                        } else {
+                            tma_load_matrix(dst, tm_a, kc * kBK, a0, t.z, full);
+                        }
+                        if (p.b_rows) {
+                            for (int b = 0; b < b_boxes; ++b)
+                                tma_load_matrix(dst + kABytes + b * 64 * kBK * 2, tm_b, b0 + 64 * b, kc * kBK, t.z, full);
+                        } else {
+                            tma_load_matrix(dst + kABytes, tm_b, kc * kBK, b0, t.z, full);
+                        }
+                        if (++s == kStages) {
+                            s = 0;
+                            ph ^= 1u;
+                        }
                     }
                 }
             }
@@ -266,163 +522,230 @@ k_product(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUte
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(p.a_rows) << 15) | (static_cast<uint32_t>(p.b_rows) << 16) |
-                                   (static_cast<uint32_t>(p.tile_n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
-            // 16 reduction elements: 32 bytes along a K-major row, 16 rows of 128 bytes MN-major
-            const uint32_t a_step = p.a_rows ? 2048 >> 4 : 32 >> 4, b_step = p.b_rows ? 2048 >> 4 : 32 >> 4;
             uint32_t s = 0, ph = 0;
             bool ok = true;
             int it = 0;
-            for (int index = pair; ok && index < all; index += pairs, ++it) {
-                const uint32_t buf = it & 1, use = (it >> 1) & 1;
-                if (!mbar_wait(acc_empty0 + 8 * buf, use ^ 1u, abort_flag)) break;
-                tc_fence_after_sync();
-                const uint32_t d = tmem_base + buf * kAccCols;
-                for (int kc = 0; kc < p.steps; ++kc) {
-                    if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) {
+            for (int i = 0; ok && i < products; ++i) {
+                const int kind = i % 3;
+                const Product &p = kind == 0 ? q.gram : kind == 1 ? q.square : q.apply;
+                const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(p.a_rows) << 15) | (static_cast<uint32_t>(p.b_rows) << 16) |
+                                       (static_cast<uint32_t>(p.tile_n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
+                // 16 reduction elements: 32 bytes along a K-major row, 16 rows of 128 bytes MN-major
+                const uint32_t a_step = p.a_rows ? 2048 >> 4 : 32 >> 4, b_step = p.b_rows ? 2048 >> 4 : 32 >> 4;
+                for (Walk w(q, p); ok && w.index < w.end; w.index += w.step, ++it) {
+                    const uint32_t buf = it & 1, use = (it >> 1) & 1;
+                    if (!mbar_wait(acc_empty0 + 8 * buf, use ^ 1u, abort_flag)) {
                         ok = false;
                         break;
                     }
                     tc_fence_after_sync();
-                    const uint32_t addr = stages + s * kStageBytes;
-                    const uint64_t ad = p.a_rows ? smem_desc_rows(addr) : smem_desc(addr);
-                    const uint64_t bd = p.b_rows ? smem_desc_rows(addr + kABytes) : smem_desc(addr + kABytes);
+                    const uint32_t d = tmem_base + buf * kAccCols;
+                    for (int kc = w.k0; kc < w.k1; ++kc) {
+                        if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) {
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after_sync();
+                        const uint32_t addr = stages + s * kStageBytes;
+                        const uint64_t ad = p.a_rows ? smem_desc_rows(addr) : smem_desc(addr);
+                        const uint64_t bd = p.b_rows ? smem_desc_rows(addr + kABytes) : smem_desc(addr + kABytes);
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k)
-                        umma_bf16(d, ad + a_step * k, bd + b_step * k, idesc, kc > 0 || k > 0);
-                    umma_commit_pair(empty0 + 8 * s);
-                    if (++s == kStages) {
-                        s = 0;
-                        ph ^= 1u;
+                        for (int k = 0; k < kBK / 16; ++k)
+                            umma_bf16(d, ad + a_step * k, bd + b_step * k, idesc, kc > w.k0 || k > 0);
+                        umma_commit(empty0 + 8 * s, leader);
+                        if (++s == kStages) {
+                            s = 0;
+                            ph ^= 1u;
+                        }
                     }
+                    if (ok) umma_commit(acc_full0 + 8 * buf, leader);
                 }
-                if (ok) umma_commit_pair(acc_full0 + 8 * buf);
             }
         }
     } else {
-        const int q = warp & 3;
+        const int quarter = warp & 3;
         const int half = (warp - 2) >> 2;                // which half of the columns
-        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16);
-        int it = 0;
-        for (int index = pair; index < all; index += pairs, ++it) {
-            const uint32_t buf = it & 1, use = (it >> 1) & 1;
-            const Tile t = tile_at<kMode>(p, index);
-            const int row = t.row + static_cast<int>(rank) * kRowsPerBlock + q * 32 + lane;
-            const bool live = row < p.m;
-            const uint32_t t0 = lane_base + buf * kAccCols;
-            const bool ready = mbar_wait(acc_full0 + 8 * buf, use, abort_flag);
-            if (!__all_sync(0xFFFFFFFFu, ready)) break;
-            tc_fence_after_sync();
-            const int c_end = (half + 1) * (p.tile_n / 2);
-            if (kMode == kGram || kMode == kSquare) {
-                const int64_t square = static_cast<int64_t>(t.z) * p.m * p.ldk;
-                const int64_t diagonal = static_cast<int64_t>(t.z) * p.dk;
-                const float di = kMode == kSquare && live ? p.d[diagonal + row] : 0.0f;
-#pragma unroll 1
-                for (int c = half * (p.tile_n / 2); c < c_end; c += 16) {
-                    const int j0 = t.col + c;
-                    uint32_t acc[16];
-                    tmem_ld16(t0 + c, acc);
-                    if (kMode == kGram) {
-                        tmem_wait_ld();
-                        if (live && j0 < p.n && j0 + 15 >= row) {
-                            float v[16];
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                v[e] = __uint_as_float(acc[e]) * kUnscale;
-                                if (j0 + e == row) p.d[diagonal + row] = v[e] * kUnscale;
-                            }
-                            store_symmetric(p.o + square, p.ldk, p.m, row, j0, v);
+        const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        const int row_in_block = quarter * 32 + lane;
+        const uint32_t stage = besides + (warp - 2) * kStaging, staged = staged0 + 8 * kSets * (warp - 2);
+        uint32_t staged_phase = 0;                       // bit b: parity of the next arrival in set b
+        bool ok = true;
+        int it = 0, exchanges = 0;
+        for (int i = 0; ok && i < products; ++i) {
+            const int kind = i % 3, from = i / 3 & 1;
+            const bool last = i + 1 == products;
+            const Product &p = kind == 0 ? q.gram : kind == 1 ? q.square : q.apply;
+            __half *symmetric = kind == 0 ? q.o : q.p;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(ready, i & 1, abort_flag));
+            if (lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
+            for (Walk w(q, p); ok && w.index < w.end; w.index += w.step, ++it) {
+                const uint32_t buf = it & 1, use = (it >> 1) & 1;
+                const Tile t = tile_at(p, w.index);
+                const int row0 = t.row + static_cast<int>(rank) * kRowsPerBlock + quarter * 32, row = row0 + lane;
+                const bool live = row < p.m;
+                const uint32_t t0 = lane_base + buf * kAccCols;
+                const int64_t diagonal = static_cast<int64_t>(t.z) * q.dk;
+                // the square blocks on the diagonal are computed whole, those above it are written to both places
+                const bool mirrored = kind != 2 && t.col >= t.row + kTileM;
+                const float factor = kind == 1 ? (live ? q.d[diagonal + row] : 0.0f)
+                                               : kind == 2 && !q.tall && live ? q.a + q.e[diagonal + row] : q.a;
+                if (!p.shared) {
+                    const int sets = p.tile_n / 64, first = t.col + half * (p.tile_n / 2);
+                    // set s, columns [first + 32 s, + 32) of what the epilogue reads, into buffer s % kSets
+                    auto bring = [&](int s) {
+                        const uint32_t dst = stage + (s % kSets) * (2 * kBlock), bar = staged + 8 * (s % kSets);
+                        mbar_expect_tx(bar, kind == 1 ? kBlock : 2 * kBlock);
+                        if (kind == 1) {
+                            tma_load_block(dst, &maps.o, first + 32 * s, row0, t.z, bar);
+                        } else {
+                            tma_load_block(dst, &maps.hi[from], first + 32 * s, row0, t.z, bar);
+                            tma_load_block(dst + kBlock, &maps.lo[from], first + 32 * s, row0, t.z, bar);
                         }
-                    } else {
-                        const bool any = live && j0 < p.n && j0 + 15 >= row;
-                        uint32_t ow[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                        if (any) load16(ow, p.o + square + static_cast<int64_t>(row) * p.ldk, j0, p.ldk);
+                    };
+                    if (lane == 0) {
+                        bulk_wait_read();                // the buffers: the previous tile's results have left
+                        if (kind != 0)
+                            for (int s = 0; s < kSets && s < sets; ++s) bring(s);
+                    }
+                    __syncwarp();
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full0 + 8 * buf, use, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after_sync();
+#pragma unroll 1
+                    for (int s = 0; s < sets; ++s) {
+                        const uint32_t block = stage + (s % kSets) * (2 * kBlock);
+                        const int f = first + 32 * s;
+                        if (kind != 0) {
+                            const bool here = mbar_wait(staged + 8 * (s % kSets), (staged_phase >> (s % kSets)) & 1, abort_flag);
+                            staged_phase ^= 1u << (s % kSets);
+                            ok = __all_sync(0xFFFFFFFFu, here);
+                            if (!ok) break;
+                        } else if (s >= kSets) {
+                            if (lane == 0) bulk_wait_read();
+                            __syncwarp();
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t raw_acc[16], u[8], v[8];
+                            tmem_ld16(t0 + half * (p.tile_n / 2) + 32 * s + 16 * h, raw_acc);
+                            if (kind != 0) get16(block, lane, h, u);
+                            if (kind == 2) get16(block + kBlock, lane, h, v);
+                            tmem_wait_ld();
+                            float acc[16];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) acc[e] = __uint_as_float(raw_acc[e]);
+                            const int j0 = f + 16 * h;
+                            if (kind == 0) finish_gram(q, t.z, row, j0, acc, u);
+                            else if (kind == 1) finish_square(q, t.z, row, j0, factor, acc, u);
+                            else finish_apply(q, last, t.z, j0, factor, acc, u, v);
+                            if (last && !q.out_whole) {
+                                __nv_bfloat16 *dst = q.out + t.z * q.out_batch + row * q.out_row;
+                                if (live) {
+#pragma unroll
+                                    for (int e = 0; e < 16; ++e)
+                                        if (j0 + e < p.n)
+                                            *reinterpret_cast<uint16_t *>(dst + j0 + e) = static_cast<uint16_t>(e & 1 ? u[e / 2] >> 16 : u[e / 2]);
+                                }
+                                continue;
+                            }
+                            put16(block, lane, h, u);
+                            if (kind == 2 && !last) put16(block + kBlock, lane, h, v);
+                            if (mirrored) store_mirrored(symmetric + static_cast<int64_t>(t.z) * p.m * q.ldk, q.ldk, p.m, row, j0, u);
+                        }
+                        fence_async();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (f < p.n && row0 < p.m && !(last && !q.out_whole)) {
+                                const CUtensorMap *to = kind == 0 ? &maps.o : kind == 1 ? &maps.p : last ? &maps.out : &maps.hi[from ^ 1];
+                                tma_store_block(to, f, row0, t.z, block);
+                                if (kind == 2 && !last) tma_store_block(&maps.lo[from ^ 1], f, row0, t.z, block + kBlock);
+                            }
+                            bulk_commit();
+                            if (kind != 0 && s + kSets < sets) {     // into this buffer
+                                bulk_wait_read();
+                                bring(s + kSets);
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                } else {
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full0 + 8 * buf, use, abort_flag));
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    // the other pairs' parts go to them: [source][4 columns][row][4], a warp's stores are contiguous
+                    const int part = p.tile_n / kShare, sub = static_cast<int>(cluster_rank >> 1);
+                    for (int c = half * (p.tile_n / 2); c < (half + 1) * (p.tile_n / 2); c += 16) {
+                        const int to = c / part;
+                        if (to == sub) continue;
+                        uint32_t acc[16];
+                        tmem_ld16(t0 + c, acc);
                         tmem_wait_ld();
-                        if (any) {
-                            float v[16];
+                        const int slot = sub < to ? sub : sub - 1;
+                        const uint32_t base = map_to_rank(besides + (slot * (part / 4) + (c - to * part) / 4) * (kRowsPerBlock * 16) + row_in_block * 16,
+                                                          2 * to + rank);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) store_remote(base + e * (kRowsPerBlock * 16), acc + 4 * e);
+                    }
+                    __syncwarp();
+                    if (lane == 0) {
+                        for (int to = 0; to < kShare; ++to) {
+                            // (a part lies in one half of the tile's columns)
+                            if (to != sub && to * part / (p.tile_n / 2) == half)
+                                mbar_arrive_release_cluster(map_to_rank(received, 2 * to + rank));
+                        }
+                    }
+                    const int c0 = sub * part + 16 * half, c1 = (sub + 1) * part;
+                    const int64_t at = static_cast<int64_t>(t.z) * p.m * q.ldk + static_cast<int64_t>(live ? row : 0) * q.ldk;
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(received, exchanges & 1, abort_flag));
+                    ++exchanges;
+                    if (!ok) break;
+#pragma unroll 1
+                    for (int c = c0; c < c1; c += 32) {
+                        const int j0 = t.col + c;
+                        uint32_t raw_acc[16], u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                        tmem_ld16(t0 + c, raw_acc);
+                        if (kind == 1 && live) load16(u, q.o + at, j0, q.ldk);
+                        tmem_wait_ld();
+                        // in the order of the reduction: the parts before this pair's, its own, those after it
+                        float acc[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+                        for (int src = 0; src < kShare; ++src) {
+                            const int slot = src < sub ? src : src - 1;
+                            const uint32_t base = besides + (slot * (part / 4) + (c - sub * part) / 4) * (kRowsPerBlock * 16) + row_in_block * 16;
 #pragma unroll
                             for (int e = 0; e < 16; e += 4) {
-                                // (the diagonals are padded to whole pieces of 16)
-                                const float4 dj = *reinterpret_cast<const float4 *>(p.d + diagonal + j0 + e);
-                                const float2 o0 = unpack2(ow[e / 2]), o1 = unpack2(ow[e / 2 + 1]);
-                                const float o[4] = {o0.x, o0.y, o1.x, o1.y}, ds[4] = {dj.x, dj.y, dj.z, dj.w};
-#pragma unroll
-                                for (int f = 0; f < 4; ++f) {
-                                    const float s = __uint_as_float(acc[e + f]) * kUnscale;
-                                    v[e + f] = fmaf(p.c, fmaf(di + ds[f], o[f], s), p.b * o[f]);
-                                    if (j0 + e + f == row)
-                                        p.e[diagonal + row] = fmaf(p.c, fmaf(di, di, s * kUnscale), p.b * di);
-                                }
+                                const float4 v = src == sub ? make_float4(__uint_as_float(raw_acc[e]), __uint_as_float(raw_acc[e + 1]),
+                                                                          __uint_as_float(raw_acc[e + 2]), __uint_as_float(raw_acc[e + 3]))
+                                                            : load_shared4(base + e / 4 * (kRowsPerBlock * 16));
+                                acc[e] += v.x, acc[e + 1] += v.y, acc[e + 2] += v.z, acc[e + 3] += v.w;
                             }
-                            store_symmetric(p.p + square, p.ldk, p.m, row, j0, v);
                         }
+                        if (kind == 0) finish_gram(q, t.z, row, j0, acc, u);
+                        else finish_square(q, t.z, row, j0, factor, acc, u);
+                        if (live) store16(symmetric + at, j0, q.ldk, u);
+                        if (mirrored) store_mirrored(symmetric + static_cast<int64_t>(t.z) * p.m * q.ldk, q.ldk, p.m, row, j0, u);
                     }
                 }
-            } else {
-                const int64_t diagonal = static_cast<int64_t>(t.z) * p.dk;
-                const int64_t at = (static_cast<int64_t>(t.z) * p.m + (live ? row : 0)) * p.ld;
-                const float factor = p.a + (p.tall || !live ? 0.0f : p.e[diagonal + row]);
-#pragma unroll 1
-                for (int c = half * (p.tile_n / 2); c < c_end; c += 16) {
-                    const int j0 = t.col + c;
-                    uint32_t acc[16], hw[8], lw[8];
-                    tmem_ld16(t0 + c, acc);
-                    const bool any = live && j0 < p.n;
-                    if (any) {
-                        load16(hw, p.hi + at, j0, p.ld);
-                        load16(lw, p.lo + at, j0, p.ld);
-                    }
-                    tmem_wait_ld();
-                    if (!any) continue;
-                    float v[16];
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        float f[4] = {factor, factor, factor, factor};
-                        if (p.tall) {
-                            const float4 ej = *reinterpret_cast<const float4 *>(p.e + diagonal + j0 + e);
-                            f[0] += ej.x, f[1] += ej.y, f[2] += ej.z, f[3] += ej.w;
-                        }
-#pragma unroll
-                        for (int g = 0; g < 4; g += 2) {
-                            const float2 h = unpack2(hw[(e + g) / 2]), l = unpack2(lw[(e + g) / 2]);
-                            v[e + g] = fmaf(f[g], h.x + l.x, __uint_as_float(acc[e + g]) * kUnscale);
-                            v[e + g + 1] = fmaf(f[g + 1], h.y + l.y, __uint_as_float(acc[e + g + 1]) * kUnscale);
-                        }
-                    }
-                    if (kMode == kApply) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            hw[e] = pack2(v[2 * e], v[2 * e + 1]);
-                            const float2 h = unpack2(hw[e]);
-                            lw[e] = pack2(v[2 * e] - h.x, v[2 * e + 1] - h.y);
-                        }
-                        store16(p.hi_next + at, j0, p.ld, hw);
-                        store16(p.lo_next + at, j0, p.ld, lw);
-                    } else {
-                        __nv_bfloat16 *dst = p.out + t.z * p.out_batch + row * p.out_row;
-                        if (p.out_whole) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) hw[e] = pack_bf16(v[2 * e] * kUnscale, v[2 * e + 1] * kUnscale);
-                            store16(dst, j0, p.n, hw);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (j0 + e < p.n) dst[j0 + e] = __float2bfloat16_rn(v[e] * kUnscale);
-                        }
-                    }
-                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(map_to_rank(acc_empty0 + 8 * buf, leader));
             }
-            tc_fence_before_sync();
+            // the block has finished this product when its eighth warp has
+            if (lane == 0) bulk_wait();
+            __threadfence();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(map_to_rank(acc_empty0 + 8 * buf, 0));
+            if (lane == 0 && !last) {
+                if (atomicAdd(finished, 1u) % kEpilogueWarps == kEpilogueWarps - 1) add_release(q.arrived);
+            }
         }
     }
 
     tc_fence_before_sync();
     __syncthreads();
     if (*abort_flag) {
-        if (threadIdx.x == 0) atomicExch(p.err, 1);
+        if (threadIdx.x == 0) atomicExch(q.err, 1);
         const unsigned long long t0 = global_timer_ns();
         while (global_timer_ns() - t0 < kDrainNs) __nanosleep(1000);
     }
@@ -443,6 +766,7 @@ struct Start {
     int64_t g_batch, g_row;
     double eps;
     double *squares;         // [batch][parts]
+    unsigned *arrived;       // the iteration's counter, set to zero here
     __half *hi, *lo;
 };
 
@@ -495,6 +819,7 @@ k_squares(const Start s, const T *g)
 {
     allow_next();
     const int part = blockIdx.x, z = blockIdx.y;
+    if (part == 0 && z == 0 && threadIdx.x == 0) *s.arrived = 0;
     double sum = 0.0;
     each_piece(s, part, [&](int64_t row, int c) {
         float v[8];
@@ -513,7 +838,9 @@ k_start(const Start s, const T *g)
     allow_next();
     wait_for_previous();
     const int part = blockIdx.x, z = blockIdx.y;
-    const double sum = block_sum(threadIdx.x < s.parts ? s.squares[z * s.parts + threadIdx.x] : 0.0);
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < s.parts; i += kRowThreads) sum += s.squares[z * s.parts + i];
+    sum = block_sum(sum);
     const float factor = static_cast<float>(static_cast<double>(kScale) / (sqrt(sum) + s.eps));
     each_piece(s, part, [&](int64_t row, int c) {
         float v[8];
@@ -549,6 +876,18 @@ bool encode(CUtensorMap *m, const __half *base, int64_t batch, int64_t rows, int
                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The same in blocks of 32 x 32; type: of 16 bits, strides in elements.
+bool encode_blocks(CUtensorMap *m, CUtensorMapDataType type, const void *base, int64_t batch, int64_t rows, int64_t cols, int64_t ld, int64_t stack)
+{
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(batch)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(stack) * 2};
+    const cuuint32_t box[3] = {32, 32, 1};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    return tensor_map_encoder()(m, type, 3, const_cast<void *>(base), dims, strides, box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool aligned(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
 
 }  // namespace
@@ -556,7 +895,8 @@ bool aligned(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>
 struct orthogonal {
     int rows = 0, cols = 0, steps = 0, type = 0;
     float a = 0, b = 0, c = 0, eps = 0;
-    int device = 0, sms = 0, pairs = 0;
+    int device = 0, sms = 0;
+    int pairs = 0, clusters = 0;     // of two and of 2 kShare blocks that the device holds at once
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
     int *err = nullptr;
@@ -571,7 +911,7 @@ int64_t pad16(int64_t v) { return div_up(v, 16) * 16; }
 // Everything a call keeps between its kernels.
 struct Layout {
     int64_t ld, ldk, dk;
-    size_t hi[2], lo[2], o, p, d, e, squares, total;
+    size_t hi[2], lo[2], o, p, d, e, squares, arrived, total;
 };
 
 Layout layout_of(const orthogonal *p, int64_t batch)
@@ -597,6 +937,7 @@ Layout layout_of(const orthogonal *p, int64_t batch)
     w.d = take(static_cast<size_t>(batch) * w.dk * 4);
     w.e = take(static_cast<size_t>(batch) * w.dk * 4);
     w.squares = take(static_cast<size_t>(batch) * kMostParts * sizeof(double));
+    w.arrived = take(sizeof(unsigned));
     w.total = at;
     return w;
 }
@@ -611,66 +952,41 @@ int64_t tiles_of(int64_t m, int64_t n, int tile_n, bool symmetric)
     return tiles;
 }
 
-// Rounds of tiles times a tile's cost: half the columns cost more than half, since the rows of A are shared by fewer.
-void choose_tile(const orthogonal *p, Product &q, bool symmetric)
+// Chooses the tiles of a product for `pairs` pairs in clusters of `share` and returns what it costs, in steps of a tile of one
+// column.  Half the columns cost more than half, since the rows of A are shared by fewer; filling the ring and the last
+// tile's epilogue are worth about six steps; exchanging the parts of a shared tile about 1,500.
+int64_t choose_tile(Product &q, int64_t batch, int64_t pairs, int share)
 {
-    const int widths[3] = {256, 128, 64};
+    q.steps = static_cast<int>(div_up(q.k, kBK));
+    q.m_tiles = static_cast<int>(div_up(q.m, kTileM));
     int64_t best = -1;
-    for (int w : widths) {
-        const int64_t tiles = tiles_of(q.m, q.n, w, symmetric);
-        const int64_t cost = div_up(tiles * q.batch, p->pairs) * (w + 128);
-        if (best < 0 || cost < best) {
+    for (int w : {256, 128, 64}) {
+        const int64_t tiles = tiles_of(q.m, q.n, w, q.symmetric);
+        for (int shared = 0; shared <= (share > 1 && q.symmetric && w <= kShareCols ? 1 : 0); ++shared) {
+            // (a shared tile takes all stages of the reduction, and each cluster one)
+            if (shared && (q.steps < kShare || tiles * batch > pairs / share)) continue;
+            const int64_t rounds = shared ? 1 : div_up(tiles * batch, pairs), steps = shared ? div_up(q.steps, kShare) : q.steps;
+            const int64_t cost = (rounds * steps + 6) * (w + 128) + (shared ? 1500 : 0);
+            if (best >= 0 && cost >= best) continue;
             best = cost;
             q.tile_n = w;
             q.tiles = static_cast<int>(tiles);
+            q.shared = shared;
         }
     }
-    q.m_tiles = static_cast<int>(div_up(q.m, kTileM));
     q.n_tiles = static_cast<int>(div_up(q.n, q.tile_n));
-    q.steps = static_cast<int>(div_up(q.k, kBK));
-}
-
-template <typename... Params, typename... Args>
-bool launch_after(cudaStream_t stream, dim3 grid, unsigned threads, size_t smem, bool pairs, void (*kernel)(Params...), const Args &...args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = pairs ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess;
+    return best;
 }
 
 // An operand of a product: a stack of [rows][cols] matrices, read along or across its rows.
 struct Operand {
     const __half *base;
     int64_t rows, cols, ld;
-    int by_rows;             // 1: the reduction runs down the rows
 };
 
-template <int kMode>
-bool launch_product(orthogonal *p, Product q, const Operand &a, const Operand &b)
+bool encode_operand(CUtensorMap *m, const Operand &x, int64_t batch, int by_rows, int box_rows)
 {
-    q.a_rows = a.by_rows;
-    q.b_rows = b.by_rows;
-    CUtensorMap tm_a, tm_b;
-    if (!encode(&tm_a, a.base, q.batch, a.rows, a.cols, a.ld, a.by_rows ? kBK : kRowsPerBlock) ||
-        !encode(&tm_b, b.base, q.batch, b.rows, b.cols, b.ld, b.by_rows ? kBK : q.tile_n / 2))
-        return false;
-    const int64_t all = static_cast<int64_t>(q.tiles) * q.batch;
-    const unsigned pairs = static_cast<unsigned>(all < p->pairs ? all : p->pairs);
-    if (!launch_after(p->stream, dim3(2 * pairs), kThreads, kSmem, true, k_product<kMode>, tm_a, tm_b, q)) return false;
-    p->launches += 1;
-    return true;
+    return encode(m, x.base, batch, x.rows, x.cols, x.ld, by_rows ? kBK : box_rows);
 }
 
 template <typename T>
@@ -687,27 +1003,37 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     s.rows = p->rows;
     s.cols = p->cols;
     s.ld = static_cast<int>(w.ld);
-    // about eight pieces per thread
-    const int64_t parts = div_up(static_cast<int64_t>(p->rows) * (w.ld / 8), 8 * kRowThreads);
+    // a piece per thread where there are few, several where there are many
+    const int64_t parts = div_up(static_cast<int64_t>(p->rows) * (w.ld / 8), kRowThreads);
     s.parts = static_cast<int>(parts < kMostParts ? parts : kMostParts);
     s.g_batch = g_batch;
     s.g_row = g_row;
     s.whole = aligned(g, 16) && (p->rows == 1 || g_row * sizeof(T) % 16 == 0) && (batch == 1 || g_batch * sizeof(T) % 16 == 0);
     s.eps = p->eps;
     s.squares = reinterpret_cast<double *>(base + w.squares);
+    s.arrived = reinterpret_cast<unsigned *>(base + w.arrived);
     s.hi = half(w.hi[0]);
     s.lo = half(w.lo[0]);
     const dim3 grid(static_cast<unsigned>(s.parts), static_cast<unsigned>(batch));
     k_squares<T><<<grid, kRowThreads, 0, p->stream>>>(s, g);
     if (cudaGetLastError() != cudaSuccess) return ORTHOGONAL_ECUDA;
-    if (!launch_after(p->stream, grid, kRowThreads, 0, false, k_start<T>, s, g)) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kRowThreads);
+    cfg.stream = p->stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, k_start<T>, s, g) != cudaSuccess) {
         cudaGetLastError();
         return ORTHOGONAL_ECUDA;
     }
-    p->launches += 2;
 
-    Product q = {};
+    Iteration q = {};
     q.batch = static_cast<int>(batch);
+    q.steps = p->steps;
     q.tall = tall;
     q.ld = static_cast<int>(w.ld);
     q.ldk = static_cast<int>(w.ldk);
@@ -719,37 +1045,82 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     q.p = half(w.p);
     q.d = single(w.d);
     q.e = single(w.e);
+    for (int i = 0; i < 2; ++i) {
+        q.hi[i] = half(w.hi[i]);
+        q.lo[i] = half(w.lo[i]);
+    }
     q.out = out;
     q.out_batch = out_batch;
     q.out_row = out_row;
     q.out_whole = p->cols % 8 == 0 && aligned(out, 16) && (p->rows == 1 || out_row % 8 == 0) && (batch == 1 || out_batch % 8 == 0);
+    q.arrived = s.arrived;
     q.err = p->err;
-    Product gram = q, square = q, apply = q;
-    gram.m = gram.n = square.m = square.n = square.k = k;
-    gram.k = tall ? p->rows : p->cols;
-    apply.m = p->rows;
-    apply.n = p->cols;
-    apply.k = k;
-    choose_tile(p, gram, true);
-    choose_tile(p, square, true);
-    choose_tile(p, apply, false);
-    const Operand o = {q.o, k, k, w.ldk, 0}, pp = {q.p, k, k, w.ldk, 0};
-    for (int i = 0; i < p->steps; ++i) {
-        const __half *hi = half(w.hi[i & 1]);
-        const Operand x = {hi, p->rows, p->cols, w.ld, 0}, xt = {hi, p->rows, p->cols, w.ld, 1};
-        apply.hi = hi;
-        apply.lo = half(w.lo[i & 1]);
-        apply.hi_next = half(w.hi[(i + 1) & 1]);
-        apply.lo_next = half(w.lo[(i + 1) & 1]);
-        const bool last = i + 1 == p->steps;
-        const bool ok = launch_product<kGram>(p, gram, tall ? xt : x, tall ? xt : x) && launch_product<kSquare>(p, square, o, o) &&
-                        (last ? launch_product<kLast>(p, apply, tall ? x : pp, tall ? pp : xt)
-                              : launch_product<kApply>(p, apply, tall ? x : pp, tall ? pp : xt));
-        if (!ok) {
-            cudaGetLastError();
-            return ORTHOGONAL_ECUDA;
-        }
+    q.gram.m = q.gram.n = q.square.m = q.square.n = q.square.k = k;
+    q.gram.k = tall ? p->rows : p->cols;
+    q.gram.symmetric = q.square.symmetric = 1;
+    q.gram.a_rows = q.gram.b_rows = tall;
+    q.apply.m = p->rows;
+    q.apply.n = p->cols;
+    q.apply.k = k;
+    q.apply.b_rows = !tall;
+    // pairs by themselves, or in clusters that can share a reduction: whichever the sum over a step is smaller with
+    Iteration alone = q;
+    auto cost = [&](Iteration &r, int64_t pairs, int share) {
+        r.share = share;
+        return choose_tile(r.gram, batch, pairs, share) + choose_tile(r.square, batch, pairs, share) + choose_tile(r.apply, batch, pairs, share);
+    };
+    const int64_t single_cost = cost(alone, p->pairs, 1);
+    if (p->clusters == 0 || cost(q, static_cast<int64_t>(p->clusters) * kShare, kShare) >= single_cost) q = alone;
+
+    Maps maps;
+    const Operand o = {q.o, k, k, w.ldk}, pp = {q.p, k, k, w.ldk};
+    bool ok = encode_operand(&maps.square_a, o, batch, 0, kRowsPerBlock) && encode_operand(&maps.square_b, o, batch, 0, q.square.tile_n / 2);
+    for (int i = 0; i < 2; ++i) {
+        const Operand x = {q.hi[i], p->rows, p->cols, w.ld};
+        ok = ok && encode_operand(&maps.gram_a[i], x, batch, q.gram.a_rows, kRowsPerBlock) &&
+             encode_operand(&maps.gram_b[i], x, batch, q.gram.b_rows, q.gram.tile_n / 2) &&
+             encode_operand(&maps.apply_a[i], tall ? x : pp, batch, q.apply.a_rows, kRowsPerBlock) &&
+             encode_operand(&maps.apply_b[i], tall ? pp : x, batch, q.apply.b_rows, q.apply.tile_n / 2);
+        for (int low = 0; low < 2; ++low)
+            ok = ok && encode_blocks(low ? &maps.lo[i] : &maps.hi[i], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, low ? q.lo[i] : q.hi[i], batch,
+                                     p->rows, p->cols, w.ld, w.ld * p->rows);
     }
+    for (int b = 0; b < 2; ++b)
+        ok = ok && encode_blocks(b ? &maps.p : &maps.o, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, b ? q.p : q.o, batch, k, k, w.ldk, w.ldk * k);
+    // (of a single row or matrix the stride does not matter, but it has to be one)
+    if (q.out_whole) {
+        const int64_t row = p->rows > 1 ? out_row : p->cols;
+        ok = ok && encode_blocks(&maps.out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, out, batch, p->rows, p->cols, row, batch > 1 ? out_batch : row * p->rows);
+    } else {
+        maps.out = maps.hi[0];
+    }
+    if (!ok) return ORTHOGONAL_ECUDA;
+    // as many blocks as there is work for, in whole clusters
+    auto wanted = [&](const Product &r) {
+        const int64_t tiles = static_cast<int64_t>(r.tiles) * batch;
+        return r.shared ? tiles * q.share : tiles;
+    };
+    int64_t pairs = wanted(q.gram);
+    if (wanted(q.square) > pairs) pairs = wanted(q.square);
+    if (wanted(q.apply) > pairs) pairs = wanted(q.apply);
+    pairs = div_up(pairs, q.share) * q.share;
+    const int64_t most = q.share > 1 ? static_cast<int64_t>(p->clusters) * kShare : p->pairs;
+    if (pairs > most) pairs = most;
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(2 * q.share);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeCooperative;     // all blocks at once: they wait for one another
+    attr[1].val.cooperative = 1;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, k_iterate, maps, q) != cudaSuccess) {
+        cudaGetLastError();
+        return ORTHOGONAL_ECUDA;
+    }
+    p->launches += 3;
     return ORTHOGONAL_OK;
 }
 
@@ -760,28 +1131,26 @@ bool batch_ok(const orthogonal *p, int64_t batch)
            batch * div_up(p->rows, kTileM) * div_up(p->cols, 64) < 0x7FFFFFFF;
 }
 
-bool prepare_kernels(int *pairs, int sms)
+// Clusters of `blocks` blocks of k_iterate that the device holds at once, 0 if none.
+int resident_clusters(int blocks, int sms)
 {
-    if (!raise_dynamic_smem(reinterpret_cast<const void *>(k_product<kGram>), kSmem) ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<kSquare>), kSmem) ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<kApply>), kSmem) ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_product<kLast>), kSmem))
-        return false;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(sms & ~1));
+    cfg.gridDim = dim3(static_cast<unsigned>(sms / blocks * blocks));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(blocks);
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int clusters = 0;
-    if (cudaOccupancyMaxActiveClusters(&clusters, k_product<kGram>, &cfg) != cudaSuccess || clusters < 1) return false;
-    *pairs = clusters < sms / 2 ? clusters : sms / 2;
-    return true;
+    if (cudaOccupancyMaxActiveClusters(&clusters, k_iterate, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        return 0;
+    }
+    return clusters < sms / blocks ? clusters : sms / blocks;
 }
 
 }  // namespace
@@ -809,8 +1178,14 @@ int orthogonal_create(orthogonal **out, int rows, int cols, int steps, float a, 
     p->type = type;
     if (cudaGetDevice(&p->device) != cudaSuccess ||
         cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess ||
-        !prepare_kernels(&p->pairs, p->sms)) {
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_iterate), kSmem)) {
         cudaGetLastError();
+        delete p;
+        return ORTHOGONAL_ECUDA;
+    }
+    p->pairs = resident_clusters(2, p->sms);
+    p->clusters = resident_clusters(2 * kShare, p->sms);
+    if (p->pairs < 1) {
         delete p;
         return ORTHOGONAL_ECUDA;
     }
