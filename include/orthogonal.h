@@ -63,7 +63,7 @@ int orthogonal_create(orthogonal **out, int rows, int cols, int steps, float a, 
 int orthogonal_destroy(orthogonal *p);
 int orthogonal_set_stream(orthogonal *p, void *cuda_stream);
 
-/* Scratch of a call on `batch` matrices. */
+/* Scratch of a call on `batch` matrices; may be 0. */
 size_t orthogonal_workspace_bytes(const orthogonal *p, int64_t batch);
 
 /* batch >= 1 matrices, each by itself. */

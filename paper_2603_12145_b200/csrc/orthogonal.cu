@@ -860,6 +860,461 @@ k_start(const Start s, const T *g)
     });
 }
 
+// ---- a short side of up to 128: the whole iteration on the chip
+//
+// A cluster of up to eight blocks keeps X in shared memory, each block a slice of the long side's columns (a tall matrix is
+// turned while it is read and written).  Of a step only the products X X^T cross blocks: each block sends the rows of its
+// part to the blocks that own them, the owners add them up in order and send A's rows to everyone; A A, B and the slice of B X
+// are each block's own.  Nothing waits for a whole cluster: a block that has received every part of this step knows that all
+// others are past what they read of the last one.
+//
+// Operand tiles are boxes of 64 columns by KP rows with the 128-byte swizzle, as TMA would write them: read along the rows by
+// X X^T, and down the rows (MN-major) by B X.  Instructions have 128 rows; with KP = 64 the upper half of them
+// computes on whatever lies behind the box, and nobody reads it.
+
+constexpr int kSmallThreads = 256;
+constexpr int kSmallWarps = kSmallThreads / 32;
+constexpr int kSmallMost = 8;                            // blocks of a cluster
+constexpr int kGroup = 256;                              // columns of X that one accumulator buffer holds
+
+template <int KP>
+struct Small {
+    static constexpr int kBox = KP * 128;                // 64 columns of KP rows
+    static constexpr int kSquare = KP / 64 * kBox;       // O, P
+    static constexpr int kParts = KP * KP * 4;           // the parts of the rows that a block owns, from everyone
+    static constexpr int kFloats = 2 * KP * 4;           // d, e
+    static constexpr int kRest = 256;                    // barriers
+    // slices: as many boxes as there is room for
+    static constexpr int kBoxes = KP == 64 ? 11 : 3;
+    static constexpr int bytes(int boxes, int blocks)
+    {
+        const int used = 2 * boxes * kBox + 2 * kSquare + (blocks > 1 ? kParts : 0) + kFloats + kRest + 1024;
+        // one block per SM, since each takes all of the tensor memory; and 8 KB behind P for the rows that nobody reads
+        const int least = 120 * 1024;
+        return used + 8192 > least ? (used + 8192 < 227 * 1024 ? used + 8192 : 227 * 1024) : least;
+    }
+};
+static_assert(2 * Small<64>::kBoxes * Small<64>::kBox + 2 * Small<64>::kSquare + Small<64>::kParts + 8192 + 4096 <= 227 * 1024, "64 rows");
+static_assert(2 * Small<128>::kBoxes * Small<128>::kBox + 2 * Small<128>::kSquare + Small<128>::kParts + 2560 <= 227 * 1024, "128 rows");
+
+struct SmallArgs {
+    int k, l;                // short and long side
+    int tall;
+    int boxes;               // of a block's slice
+    int steps;
+    float a, b, c;
+    double eps;
+    int64_t g_batch, g_row;
+    int g_whole;             // runs of eight elements of G's rows start on 16-byte boundaries
+    __nv_bfloat16 *out;
+    int64_t out_batch, out_row;
+    int out_whole;
+    int *err;
+};
+
+__device__ __forceinline__ void umma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+__device__ __forceinline__ void umma_commit_one(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+
+__device__ __forceinline__ void put_piece(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ uint4 get_piece(uint32_t addr)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// Eight columns [8 piece, 8 piece + 8) of a row, in boxes of 64 columns.
+template <int KP>
+__device__ __forceinline__ uint32_t small_piece(uint32_t base, int row, int piece)
+{
+    return base + (piece >> 3) * Small<KP>::kBox + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+}
+
+// Eight neighbours of X in a row, times the factor, to hi and lo.
+__device__ __forceinline__ void split8(const float (&v)[8], float factor, uint32_t (&hw)[4], uint32_t (&lw)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float x = v[2 * e] * factor, y = v[2 * e + 1] * factor;
+        hw[e] = pack2(x, y);
+        const float2 h = unpack2(hw[e]);
+        lw[e] = pack2(x - h.x, y - h.y);
+    }
+}
+
+template <typename T, int KP>
+__global__ void __launch_bounds__(kSmallThreads, 1)
+k_small(const __grid_constant__ SmallArgs p, const T *g)
+{
+    using S = Small<KP>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t hi0 = (raw + 1023u) & ~1023u, lo0 = hi0 + p.boxes * S::kBox;
+    const uint32_t o0 = lo0 + p.boxes * S::kBox, p0 = o0 + S::kSquare;
+    const uint32_t blocks = cluster_size(), rank = cluster_cta_rank();
+    const uint32_t parts0 = p0 + S::kSquare, floats0 = parts0 + (blocks > 1 ? S::kParts : 0);
+    uint8_t *floats_ptr = smem_raw + (floats0 - raw);
+    float *d = reinterpret_cast<float *>(floats_ptr), *e = d + KP;
+    const uint32_t bars = floats0 + S::kFloats;
+    const uint32_t done0 = bars, parts_full = bars + 16, o_full = bars + 24;      // done0: two, one per accumulator buffer
+    double *sums = reinterpret_cast<double *>(floats_ptr + S::kFloats + 32);      // [kSmallWarps], [kSmallMost]
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(floats_ptr + S::kFloats + 32 + 8 * (kSmallWarps + kSmallMost));
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    const int64_t z = blockIdx.x / blocks;
+    const int slice = static_cast<int>(rank) * p.boxes * 64;         // the block's first column
+    const T *gz = g + z * p.g_batch;
+
+    if (threadIdx.x == 0) {
+        mbar_init(done0, 1);
+        mbar_init(done0 + 8, 1);
+        mbar_init(parts_full, kSmallWarps * blocks);
+        mbar_init(o_full, kSmallWarps * blocks);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                         smem_u32(const_cast<uint32_t *>(tmem_slot))),
+                     "r"(512u)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+
+    // The norm.  A unit is eight elements of a row of G: along X's row, or (tall) down eight of them.
+    const int runs = (p.tall ? p.k + 7 : p.boxes * 64) / 8;          // per column of X, or per row
+    const int units = p.tall ? p.boxes * 64 * runs : p.k * runs;
+    auto unit = [&](int u, float (&v)[8], int &r, int &c) {
+        if (p.tall) {
+            r = u / (p.boxes * 64) * 8;
+            c = u % (p.boxes * 64);
+        } else {
+            r = u / runs;
+            c = u % runs * 8;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (slice + c >= p.l) return;
+        if (p.tall)
+            load8<T>(v, gz + (slice + c) * p.g_row, r, p.k, p.g_whole);
+        else
+            load8<T>(v, gz + r * p.g_row, slice + c, p.l, p.g_whole);
+    };
+    double sum = 0.0;
+    for (int u = threadIdx.x; u < units; u += kSmallThreads) {
+        float v[8];
+        int r, c;
+        unit(u, v, r, c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fma(static_cast<double>(v[i]), static_cast<double>(v[i]), sum);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (lane == 0) sums[warp] = sum;
+    // zeros where X has no rows, and (tall) columns are stored element by element
+    for (int i = threadIdx.x; i < 2 * p.boxes * S::kBox / 16; i += kSmallThreads) put_piece(hi0 + 16 * i, 0, 0, 0, 0);
+    if (threadIdx.x < 2 * KP) d[threadIdx.x] = 0.0f;
+    __syncthreads();
+    sum = 0.0;
+    for (int i = 0; i < kSmallWarps; ++i) sum += sums[i];
+    cluster_sync_all();                                              // every block's barriers and memory are there
+    if (blocks > 1) {
+        if (threadIdx.x < blocks) {
+            const uint32_t at = map_to_rank(smem_u32(sums + kSmallWarps + rank), threadIdx.x);
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(sum) : "memory");
+        }
+        cluster_sync_all();
+        sum = 0.0;
+        for (uint32_t i = 0; i < blocks; ++i) sum += sums[kSmallWarps + i];
+    }
+    const float factor = static_cast<float>(static_cast<double>(kScale) / (sqrt(sum) + p.eps));
+    for (int u = threadIdx.x; u < units; u += kSmallThreads) {
+        float v[8];
+        int r, c;
+        unit(u, v, r, c);
+        uint32_t hw[4], lw[4];
+        split8(v, factor, hw, lw);
+        if (!p.tall) {
+            put_piece(small_piece<KP>(hi0, r, c >> 3), hw[0], hw[1], hw[2], hw[3]);
+            put_piece(small_piece<KP>(lo0, r, c >> 3), lw[0], lw[1], lw[2], lw[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (r + i >= p.k) break;
+                const uint32_t at = small_piece<KP>(0, r + i, c >> 3) + 2 * (c & 7);
+                const uint16_t h = static_cast<uint16_t>(i & 1 ? hw[i / 2] >> 16 : hw[i / 2]);
+                const uint16_t l = static_cast<uint16_t>(i & 1 ? lw[i / 2] >> 16 : lw[i / 2]);
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(hi0 + at), "h"(h) : "memory");
+                asm volatile("st.shared.u16 [%0], %1;" ::"r"(lo0 + at), "h"(l) : "memory");
+            }
+        }
+    }
+    fence_async();
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot, lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+
+    // f16 in, f32 out, 128 rows; KP columns along the rows of both, or `n` down the rows of the second operand
+    const uint32_t idesc_square = (1u << 4) | ((KP >> 3) << 17) | ((128u >> 4) << 24);
+    auto idesc_apply = [](int n) { return (1u << 4) | (1u << 16) | (static_cast<uint32_t>(n >> 3) << 17) | ((128u >> 4) << 24); };
+    const int columns = p.boxes * 64, groups = (columns + kGroup - 1) / kGroup;
+    uint32_t done_phase = 0;                                         // bit b: parity of the next commit to buffer b
+    bool ok = true;
+    auto wait_done = [&](int b) {
+        ok = mbar_wait(done0 + 8 * b, (done_phase >> b) & 1, abort_flag) && ok;
+        done_phase ^= 1u << b;
+        tc_fence_after_sync();
+    };
+    auto issue_group = [&](int gr) {                                 // columns [256 gr, + n) of P X into buffer gr & 1
+        const int n = min(kGroup, columns - gr * kGroup);
+        const uint32_t idesc = idesc_apply(n);
+        const uint32_t x = hi0 + gr * (kGroup / 64) * S::kBox;
+        // MN-major: the next 64 columns are a box further, the next 8 rows 1024 bytes
+        const uint64_t bd = static_cast<uint64_t>((x >> 4) & 0x3FFFu) | (static_cast<uint64_t>(S::kBox >> 4) << 16) | (64ull << 32) |
+                            (1ull << 46) | (2ull << 61);
+        for (int i = 0; i < KP / 16; ++i)
+            umma_one(tmem + (gr & 1) * kGroup, smem_desc(p0 + (i >> 2) * S::kBox) + 2 * (i & 3), bd + (2048 >> 4) * i, idesc, i > 0);
+        umma_commit_one(done0 + 8 * (gr & 1));
+    };
+    constexpr int kHalf = KP / 2;                                    // columns of a symmetric product that a warp takes
+    const bool mine = row < KP;
+
+    for (int step = 0; step < p.steps; ++step) {
+        const bool last = step + 1 == p.steps;
+        if (threadIdx.x == 0) {
+            for (int b = 0; b < p.boxes; ++b)
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t x = smem_desc(hi0 + b * S::kBox) + 2 * i;
+                    umma_one(tmem, x, x, idesc_square, b > 0 || i > 0);
+                }
+            umma_commit_one(done0);
+        }
+        wait_done(0);
+        if (blocks == 1) {
+#pragma unroll 1
+            for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+                uint32_t acc[16], w[8];
+                tmem_ld16(lanes + c, acc);
+                tmem_wait_ld();
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    v[i] = __uint_as_float(acc[i]) * kUnscale;
+                    if (c + i == row) {
+                        d[row] = v[i] * kUnscale;
+                        v[i] = 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+                if (mine) {
+                    put_piece(small_piece<KP>(o0, row, c >> 3), w[0], w[1], w[2], w[3]);
+                    put_piece(small_piece<KP>(o0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
+                }
+            }
+        } else {
+            const int own = KP / static_cast<int>(blocks);           // rows that a block adds up
+            // [source][4 columns][row][4]: the rows of an owner lie together
+            const int to = row / own, local = row - to * own;
+            const uint32_t base = mine ? map_to_rank(parts0 + ((rank * (KP / 4)) * own + local) * 16, to) : 0;
+#pragma unroll 1
+            for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+                uint32_t acc[16];
+                tmem_ld16(lanes + c, acc);
+                tmem_wait_ld();
+                if (mine) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) store_remote(base + ((c >> 2) + i) * own * 16, acc + 4 * i);
+                }
+            }
+            __syncwarp();
+            if (lane < blocks) mbar_arrive_release_cluster(map_to_rank(parts_full, lane));
+            ok = mbar_wait_cluster(parts_full, step & 1, abort_flag) && ok;
+            for (int u = threadIdx.x; u < own * (KP / 8); u += kSmallThreads) {
+                const int r = u % own, piece = u / own, i = static_cast<int>(rank) * own + r;
+                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                for (uint32_t src = 0; src < blocks; ++src) {
+                    const uint32_t at = parts0 + ((src * (KP / 4) + 2 * piece) * own + r) * 16;
+                    const float4 x = load_shared4(at), y = load_shared4(at + own * 16);
+                    v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w, v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+                }
+                float diagonal = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] *= kUnscale;
+                    if (8 * piece + j == i) {
+                        diagonal = v[j] * kUnscale;
+                        v[j] = 0.0f;
+                    }
+                }
+                const uint32_t w[4] = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+                for (uint32_t other = 0; other < blocks; ++other) {
+                    store_remote(map_to_rank(small_piece<KP>(o0, i, piece), other), w);
+                    if (piece == i >> 3)
+                        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_rank(smem_u32(d + i), other)), "f"(diagonal) : "memory");
+                }
+            }
+            __syncwarp();
+            if (lane < blocks) mbar_arrive_release_cluster(map_to_rank(o_full, lane));
+            ok = mbar_wait_cluster(o_full, step & 1, abort_flag) && ok;
+        }
+        fence_async();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < KP / 16; ++i) {
+                const uint64_t o = smem_desc(o0 + (i >> 2) * S::kBox) + 2 * (i & 3);
+                umma_one(tmem + kGroup, o, o, idesc_square, i > 0);
+            }
+            umma_commit_one(done0 + 8);
+        }
+        const float di = mine ? d[row] : 0.0f;
+        wait_done(1);
+#pragma unroll 1
+        for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+            uint32_t acc[16], w[8];
+            tmem_ld16(lanes + kGroup + c, acc);
+            const uint4 o_lo = get_piece(small_piece<KP>(o0, row & (KP - 1), c >> 3)), o_hi = get_piece(small_piece<KP>(o0, row & (KP - 1), (c >> 3) + 1));
+            const uint32_t ow[8] = {o_lo.x, o_lo.y, o_lo.z, o_lo.w, o_hi.x, o_hi.y, o_hi.z, o_hi.w};
+            tmem_wait_ld();
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float2 o = unpack2(ow[i / 2]);
+                const float2 dj = *reinterpret_cast<const float2 *>(d + c + i);
+                const float s0 = __uint_as_float(acc[i]) * kUnscale, s1 = __uint_as_float(acc[i + 1]) * kUnscale;
+                v[i] = fmaf(p.c, fmaf(di + dj.x, o.x, s0), p.b * o.x);
+                v[i + 1] = fmaf(p.c, fmaf(di + dj.y, o.y, s1), p.b * o.y);
+                if (c + i == row) {
+                    e[row] = fmaf(p.c, fmaf(di, di, s0 * kUnscale), p.b * di);
+                    v[i] = 0.0f;
+                }
+                if (c + i + 1 == row) {
+                    e[row] = fmaf(p.c, fmaf(di, di, s1 * kUnscale), p.b * di);
+                    v[i + 1] = 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
+            if (mine) {
+                put_piece(small_piece<KP>(p0, row, c >> 3), w[0], w[1], w[2], w[3]);
+                put_piece(small_piece<KP>(p0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
+            }
+        }
+        fence_async();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (threadIdx.x == 0) {
+            issue_group(0);
+            if (groups > 1) issue_group(1);
+        }
+        const float scale = p.a + (mine ? e[row] : 0.0f);
+        for (int gr = 0; gr < groups; ++gr) {
+            const int n = min(kGroup, columns - gr * kGroup);
+            wait_done(gr & 1);
+#pragma unroll 1
+            for (int c = half * (n / 2); c < (half + 1) * (n / 2); c += 16) {
+                uint32_t acc[16];
+                tmem_ld16(lanes + (gr & 1) * kGroup + c, acc);
+                const int piece = (gr * kGroup + c) >> 3;
+                const uint32_t r = row & (KP - 1);
+                const uint4 h0 = get_piece(small_piece<KP>(hi0, r, piece)), h1 = get_piece(small_piece<KP>(hi0, r, piece + 1));
+                const uint4 l0 = get_piece(small_piece<KP>(lo0, r, piece)), l1 = get_piece(small_piece<KP>(lo0, r, piece + 1));
+                const uint32_t hw[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
+                const uint32_t lw[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
+                tmem_wait_ld();
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 h = unpack2(hw[i]), l = unpack2(lw[i]);
+                    v[2 * i] = fmaf(scale, h.x + l.x, __uint_as_float(acc[2 * i]) * kUnscale);
+                    v[2 * i + 1] = fmaf(scale, h.y + l.y, __uint_as_float(acc[2 * i + 1]) * kUnscale);
+                }
+                if (!mine) continue;
+                if (!last) {
+                    uint32_t nh[8], nl[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        nh[i] = pack2(v[2 * i], v[2 * i + 1]);
+                        const float2 h = unpack2(nh[i]);
+                        nl[i] = pack2(v[2 * i] - h.x, v[2 * i + 1] - h.y);
+                    }
+                    put_piece(small_piece<KP>(hi0, row, piece), nh[0], nh[1], nh[2], nh[3]);
+                    put_piece(small_piece<KP>(hi0, row, piece + 1), nh[4], nh[5], nh[6], nh[7]);
+                    put_piece(small_piece<KP>(lo0, row, piece), nl[0], nl[1], nl[2], nl[3]);
+                    put_piece(small_piece<KP>(lo0, row, piece + 1), nl[4], nl[5], nl[6], nl[7]);
+                } else if (row < p.k) {
+                    const int j0 = slice + 8 * piece;
+                    if (p.tall) {                                    // neighbouring lanes have neighbouring columns of the update
+                        __nv_bfloat16 *dst = p.out + z * p.out_batch + j0 * p.out_row + row;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            if (j0 + i < p.l) *dst = __float2bfloat16_rn(v[i] * kUnscale);
+                            dst += p.out_row;
+                        }
+                    } else {
+                        __nv_bfloat16 *dst = p.out + z * p.out_batch + row * p.out_row;
+                        if (p.out_whole) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) w[i] = pack_bf16(v[2 * i] * kUnscale, v[2 * i + 1] * kUnscale);
+                            store16(dst, j0, p.l, w);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (j0 + i < p.l) dst[j0 + i] = __float2bfloat16_rn(v[i] * kUnscale);
+                        }
+                    }
+                }
+            }
+            if (gr + 2 < groups) {                                   // this buffer is free again
+                tc_fence_before_sync();
+                __syncthreads();
+                tc_fence_after_sync();
+                if (threadIdx.x == 0) issue_group(gr + 2);
+            }
+        }
+        fence_async();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+    }
+    if (!ok && lane == 0) atomicExch(p.err, 1);
+    cluster_sync_all();                                              // the others may still write here
+    if (warp == 0) {
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
 // ---------------------------------------------------------------- host side
 
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -907,6 +1362,26 @@ namespace {
 int short_side(const orthogonal *p) { return p->rows < p->cols ? p->rows : p->cols; }
 int64_t pad8(int64_t v) { return div_up(v, 8) * 8; }
 int64_t pad16(int64_t v) { return div_up(v, 16) * 16; }
+
+// How k_small cuts the long side: blocks of a cluster and boxes of 64 columns for each.  A box costs a block about a sixth of
+// what crossing blocks does.  False where the matrix is not for it: a short side over 128, or too long a one.
+bool small_cut(const orthogonal *p, int *blocks, int *boxes)
+{
+    const int k = short_side(p), l = p->rows > p->cols ? p->rows : p->cols;
+    if (k > 128) return false;
+    const int most = k <= 64 ? Small<64>::kBoxes : Small<128>::kBoxes;
+    const int64_t all = div_up(l, 64);
+    int64_t best = -1;
+    for (int n = 1; n <= kSmallMost; n *= 2) {
+        const int64_t each = div_up(all, n);
+        const int64_t cost = each + (n > 1 ? 6 : 0);
+        if (each > most || (best >= 0 && cost >= best)) continue;
+        best = cost;
+        *blocks = n;
+        *boxes = static_cast<int>(each);
+    }
+    return best >= 0;
+}
 
 // Everything a call keeps between its kernels.
 struct Layout {
@@ -999,6 +1474,48 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     auto half = [&](size_t at) { return reinterpret_cast<__half *>(base + at); };
     auto single = [&](size_t at) { return reinterpret_cast<float *>(base + at); };
 
+    const bool out_whole = p->cols % 8 == 0 && aligned(out, 16) && (p->rows == 1 || out_row % 8 == 0) && (batch == 1 || out_batch % 8 == 0);
+    const bool g_whole = aligned(g, 16) && (p->rows == 1 || g_row * sizeof(T) % 16 == 0) && (batch == 1 || g_batch * sizeof(T) % 16 == 0);
+    int blocks, boxes;
+    if (small_cut(p, &blocks, &boxes)) {
+        SmallArgs r = {};
+        r.k = k;
+        r.l = tall ? p->rows : p->cols;
+        r.tall = tall;
+        r.boxes = boxes;
+        r.steps = p->steps;
+        r.a = p->a;
+        r.b = p->b;
+        r.c = p->c;
+        r.eps = p->eps;
+        r.g_batch = g_batch;
+        r.g_row = g_row;
+        r.g_whole = g_whole;
+        r.out = out;
+        r.out_batch = out_batch;
+        r.out_row = out_row;
+        r.out_whole = out_whole;
+        r.err = p->err;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(batch * blocks));
+        cfg.blockDim = dim3(kSmallThreads);
+        cfg.dynamicSmemBytes = k <= 64 ? Small<64>::bytes(boxes, blocks) : Small<128>::bytes(boxes, blocks);
+        cfg.stream = p->stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = static_cast<unsigned>(blocks);
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, k <= 64 ? k_small<T, 64> : k_small<T, 128>, r, g) != cudaSuccess) {
+            cudaGetLastError();
+            return ORTHOGONAL_ECUDA;
+        }
+        p->launches += 1;
+        return ORTHOGONAL_OK;
+    }
+
     Start s = {};
     s.rows = p->rows;
     s.cols = p->cols;
@@ -1008,7 +1525,7 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     s.parts = static_cast<int>(parts < kMostParts ? parts : kMostParts);
     s.g_batch = g_batch;
     s.g_row = g_row;
-    s.whole = aligned(g, 16) && (p->rows == 1 || g_row * sizeof(T) % 16 == 0) && (batch == 1 || g_batch * sizeof(T) % 16 == 0);
+    s.whole = g_whole;
     s.eps = p->eps;
     s.squares = reinterpret_cast<double *>(base + w.squares);
     s.arrived = reinterpret_cast<unsigned *>(base + w.arrived);
@@ -1052,7 +1569,7 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     q.out = out;
     q.out_batch = out_batch;
     q.out_row = out_row;
-    q.out_whole = p->cols % 8 == 0 && aligned(out, 16) && (p->rows == 1 || out_row % 8 == 0) && (batch == 1 || out_batch % 8 == 0);
+    q.out_whole = out_whole;
     q.arrived = s.arrived;
     q.err = p->err;
     q.gram.m = q.gram.n = q.square.m = q.square.n = q.square.k = k;
@@ -1131,6 +1648,13 @@ bool batch_ok(const orthogonal *p, int64_t batch)
            batch * div_up(p->rows, kTileM) * div_up(p->cols, 64) < 0x7FFFFFFF;
 }
 
+template <typename T>
+bool raise_small()
+{
+    return raise_dynamic_smem(reinterpret_cast<const void *>(k_small<T, 64>), 227 * 1024) &&
+           raise_dynamic_smem(reinterpret_cast<const void *>(k_small<T, 128>), 227 * 1024);
+}
+
 // Clusters of `blocks` blocks of k_iterate that the device holds at once, 0 if none.
 int resident_clusters(int blocks, int sms)
 {
@@ -1178,7 +1702,8 @@ int orthogonal_create(orthogonal **out, int rows, int cols, int steps, float a, 
     p->type = type;
     if (cudaGetDevice(&p->device) != cudaSuccess ||
         cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess ||
-        !raise_dynamic_smem(reinterpret_cast<const void *>(k_iterate), kSmem)) {
+        !raise_dynamic_smem(reinterpret_cast<const void *>(k_iterate), kSmem) || !raise_small<float>() ||
+        !raise_small<__nv_bfloat16>() || !raise_small<__half>()) {
         cudaGetLastError();
         delete p;
         return ORTHOGONAL_ECUDA;
@@ -1224,7 +1749,8 @@ int orthogonal_set_stream(orthogonal *p, void *cuda_stream)
 size_t orthogonal_workspace_bytes(const orthogonal *p, int64_t batch)
 {
     if (p == nullptr || !batch_ok(p, batch)) return 0;
-    return layout_of(p, batch).total;
+    int blocks, boxes;
+    return small_cut(p, &blocks, &boxes) ? 0 : layout_of(p, batch).total;
 }
 
 int orthogonal_update(orthogonal *p, const void *g, int64_t g_stride_batch, int64_t g_stride_row, void *update,
@@ -1233,13 +1759,14 @@ int orthogonal_update(orthogonal *p, const void *g, int64_t g_stride_batch, int6
 {
     if (p == nullptr) return ORTHOGONAL_ENULL;
     if (!batch_ok(p, batch)) return ORTHOGONAL_EINVAL;     // first: an empty batch comes without pointers
-    if (g == nullptr || update == nullptr || workspace == nullptr) return ORTHOGONAL_ENULL;
+    const size_t need = orthogonal_workspace_bytes(p, batch);
+    if (g == nullptr || update == nullptr || (need > 0 && workspace == nullptr)) return ORTHOGONAL_ENULL;
     if (g_stride_batch < 0 || g_stride_row < 0) return ORTHOGONAL_EINVAL;
     if (p->rows > 1 && update_stride_row < p->cols) return ORTHOGONAL_EINVAL;
     // the update's matrices one behind the other
     if (batch > 1 && update_stride_batch < (p->rows - 1) * (p->rows > 1 ? update_stride_row : 0) + p->cols) return ORTHOGONAL_EINVAL;
     if (!aligned(g, p->type == ORTHOGONAL_F32 ? 4 : 2) || !aligned(update, 2) || !aligned(workspace, 256)) return ORTHOGONAL_EALIGN;
-    if (orthogonal_workspace_bytes(p, batch) > workspace_bytes) return ORTHOGONAL_ENOMEM;
+    if (need > workspace_bytes) return ORTHOGONAL_ENOMEM;
     const OnDevice on(p->device);
     if (!on.ok()) return ORTHOGONAL_ECUDA;
     __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(update);

@@ -156,9 +156,10 @@ class Orthogonal:
             out = t.empty(shape, dtype=t.bfloat16, device=self.device)
         po, ob, orow = self._matrices("out", out, t.bfloat16, shape)
         size = self._lib.orthogonal_workspace_bytes(self.h, batch)
-        scratch = t.empty((size,), dtype=t.uint8, device=self.device)
+        scratch = t.empty((size,), dtype=t.uint8, device=self.device) if size else None
         self._stream()
-        code = self._lib.orthogonal_update(self.h, pg, gb, gr, po, ob, orow, scratch.data_ptr(), size, batch)
+        code = self._lib.orthogonal_update(self.h, pg, gb, gr, po, ob, orow, None if scratch is None else scratch.data_ptr(),
+                                           size, batch)
         if code != 0:
             raise OrthogonalError(code, "orthogonal_update")
         return out

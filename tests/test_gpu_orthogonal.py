@@ -67,6 +67,23 @@ CASES = [
     (5, 320, 512, "float16", 8, 1.0),
     (1, 2048, 2048, "bfloat16", 64, 0.3),
     (1, 4096, 1000, "float32", 64, 1.0),
+    # short sides of up to 128 in one cluster: one to eight blocks, the last one's slice partly or wholly empty, either
+    # way round, several groups of columns; and those whose long side is too long for it
+    (1, 64, 64, "float32", 4, 1.0),
+    (5, 33, 700, "bfloat16", 4, 0.3),
+    (2, 700, 33, "float16", 4, 0.3),
+    (1, 64, 1024, "float32", 4, 0.1),
+    (1, 1100, 64, "bfloat16", 4, 1.0),
+    (1, 50, 5632, "bfloat16", 4, 1.0),
+    (1, 5601, 17, "float32", 4, 1.0),
+    (1, 20, 6000, "bfloat16", 4, 1.0),
+    (3, 128, 128, "bfloat16", 8, 0.1),
+    (1, 65, 193, "float32", 8, 0.3),
+    (2, 128, 1536, "float16", 8, 1.0),
+    (1, 1441, 100, "bfloat16", 8, 0.1),
+    (1, 90, 400, "float32", 8, 0.03),
+    (1, 2000, 127, "float32", 8, 1.0),
+    (40, 24, 96, "float32", 2, 1.0),
 ]
 
 
