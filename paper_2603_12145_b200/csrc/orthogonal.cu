@@ -35,32 +35,34 @@ namespace {
 constexpr int kBK = 64;                          // reduction elements per stage
 constexpr int kRowsPerBlock = 128;               // rows of A per block; a pair's tile has twice as many
 constexpr int kTileM = 2 * kRowsPerBlock;
-constexpr int kStages = 5;
 constexpr int kABytes = kRowsPerBlock * kBK * 2;
-constexpr int kBBytes = 128 * kBK * 2;           // at most 128 rows of B per block
-constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kRing = 5 * 32 * 1024;             // stages take turns in it: five of 256 columns, up to eight of fewer
+constexpr int kStages = 8;
 constexpr int kAccCols = 256;
 constexpr int kTmemCols = 2 * kAccCols;
 constexpr int kEpilogueWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpilogueWarps;
-constexpr int kShare = 4;                        // pairs that share a tile's reduction, in a cluster of eight blocks
-constexpr int kShareCols = 128;                  // columns of such a tile, at most
-constexpr int kExchange = (kShare - 1) * kRowsPerBlock * (kShareCols / kShare) * 4;
+// Pairs that may share a tile's reduction, in a cluster of four or eight blocks, and the columns of such a tile, at most.
+constexpr int kShares[2] = {2, 4};
+__host__ __device__ constexpr int share_cols(int share) { return share == 2 ? 256 : 128; }
+__host__ __device__ constexpr int exchange_bytes(int share) { return (share - 1) * kRowsPerBlock * (share_cols(share) / share) * 4; }
 constexpr int kBlock = 32 * 64;                  // 32 rows x 32 columns of 16 bits on their way between registers and memory
 constexpr int kSets = 2;                         // per epilogue warp: one worked on, the other on its way in; two planes each
 constexpr int kStaging = 2 * kSets * kBlock;
 // (what pairs exchange and what is staged take turns: a product does one or the other)
 constexpr int kBesides = kEpilogueWarps * kStaging;
 constexpr int kBarrierBytes = 512;
-constexpr int kSmem = kStages * kStageBytes + kBesides + kBarrierBytes + 1024;
-static_assert(kSmem <= 227 * 1024 && kExchange <= kBesides, "shared memory of a block");
+constexpr int kSmem = kRing + kBesides + kBarrierBytes + 1024;
+static_assert(kSmem <= 227 * 1024 && exchange_bytes(2) <= kBesides && exchange_bytes(4) <= kBesides, "shared memory of a block");
 
 constexpr int kRowThreads = 256;                 // blocks of the kernels that read and write rows
 constexpr int kMostParts = 592;                  // partial sums of squares per matrix
 
-// Operands are held times 2^13: an element of a normalised matrix of a million is about 2^-10, of A and B up to 2^2.
+// X is held times 2^13: an element of a normalised matrix of a million is about 2^-10, and hi + lo then has 22 bits of it.  A
+// and B are held as they are (up to 3 in magnitude; what is below binary16's normal numbers, 2^-14, is off by 2^-25 at most).
 constexpr float kScale = 8192.0f;
 constexpr float kUnscale = 1.0f / kScale;
+constexpr float kUnscale2 = kUnscale * kUnscale;
 
 // A product of the iteration, and how it is cut.
 struct Product {
@@ -78,7 +80,7 @@ struct Iteration {
     Product gram, square, apply;
     int batch, steps;
     int tall;               // rows > cols: the diagonal's factors go with columns
-    int share;              // pairs per cluster: 1 or kShare
+    int share;              // pairs per cluster: 1, 2 or 4
     int ld;                 // elements between rows of X
     int ldk;                // of O and P
     int dk;                 // elements between the diagonals of two matrices
@@ -155,6 +157,13 @@ __device__ __forceinline__ Tile tile_at(const Product &p, int index)
         t.col = i / p.m_tiles * p.tile_n;
     }
     return t;
+}
+
+// Bytes of the columns' operand in a stage: whole boxes of 64 columns where the reduction runs along rows.
+__device__ __forceinline__ uint32_t b_bytes(const Product &p)
+{
+    const int half = p.tile_n / 2;
+    return static_cast<uint32_t>(p.b_rows ? (half + 63) / 64 * 64 : half) * kBK * 2;
 }
 
 // Which tiles a pair works on, and which steps of their reduction.
@@ -335,20 +344,20 @@ __device__ __forceinline__ float4 load_shared4(uint32_t addr)
     return v;
 }
 
-// ---- epilogues: elements (row, j0 .. j0 + 15) of a product, times 2^26, to what is stored of them.  Rows and columns past
+// ---- epilogues: elements (row, j0 .. j0 + 15) of a product to what is stored of them.  Rows and columns past
 // the matrix go along; nothing of them is kept.
 
-// A: times 2^13 to O with a zero on the diagonal, which goes to d as it is
+// A from the products of X, to O with a zero on the diagonal, which goes to d
 __device__ __forceinline__ void finish_gram(const Iteration &q, int z, int row, int j0, const float (&acc)[16], uint32_t (&w)[8])
 {
     float v[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = acc[e] * kUnscale;
+    for (int e = 0; e < 16; ++e) v[e] = acc[e] * kUnscale2;
     if (j0 <= row && row < j0 + 16 && row < q.gram.m) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             if (j0 + e == row) {
-                q.d[static_cast<int64_t>(z) * q.dk + row] = v[e] * kUnscale;
+                q.d[static_cast<int64_t>(z) * q.dk + row] = v[e];
                 v[e] = 0.0f;
             }
         }
@@ -362,7 +371,7 @@ __device__ __forceinline__ void finish_square(const Iteration &q, int z, int row
 {
     if (j0 >= q.gram.m) return;
     const int64_t diagonal = static_cast<int64_t>(z) * q.dk;
-    float v[16], s[16];
+    float v[16];
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
         // (the diagonals are padded to whole pieces of 16)
@@ -370,16 +379,13 @@ __device__ __forceinline__ void finish_square(const Iteration &q, int z, int row
         const float2 o0 = unpack2(w[e / 2]), o1 = unpack2(w[e / 2 + 1]);
         const float o[4] = {o0.x, o0.y, o1.x, o1.y}, ds[4] = {dj.x, dj.y, dj.z, dj.w};
 #pragma unroll
-        for (int f = 0; f < 4; ++f) {
-            s[e + f] = acc[e + f] * kUnscale;
-            v[e + f] = fmaf(q.c, fmaf(di + ds[f], o[f], s[e + f]), q.b * o[f]);
-        }
+        for (int f = 0; f < 4; ++f) v[e + f] = fmaf(q.c, fmaf(di + ds[f], o[f], acc[e + f]), q.b * o[f]);
     }
     if (j0 <= row && row < j0 + 16 && row < q.gram.m) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             if (j0 + e == row) {
-                q.e[diagonal + row] = fmaf(q.c, fmaf(di, di, s[e] * kUnscale), q.b * di);
+                q.e[diagonal + row] = fmaf(q.c, fmaf(di, di, acc[e]), q.b * di);
                 v[e] = 0.0f;
             }
         }
@@ -405,8 +411,8 @@ __device__ __forceinline__ void finish_apply(const Iteration &q, bool last, int 
 #pragma unroll
         for (int g = 0; g < 4; g += 2) {
             const float2 h = unpack2(hi[(e + g) / 2]), l = unpack2(lo[(e + g) / 2]);
-            v[e + g] = fmaf(f[g], h.x + l.x, acc[e + g] * kUnscale);
-            v[e + g + 1] = fmaf(f[g + 1], h.y + l.y, acc[e + g + 1] * kUnscale);
+            v[e + g] = fmaf(f[g], h.x + l.x, acc[e + g]);
+            v[e + g + 1] = fmaf(f[g + 1], h.y + l.y, acc[e + g + 1]);
         }
     }
 #pragma unroll
@@ -428,7 +434,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t stages = (raw + 1023u) & ~1023u;
-    const uint32_t besides = stages + kStages * kStageBytes;
+    const uint32_t besides = stages + kRing;
     const uint32_t bars = besides + kBesides;
     uint8_t *bars_ptr = smem_raw + (bars - raw);
     const uint32_t full0 = bars, empty0 = bars + 8 * kStages;
@@ -453,7 +459,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
             mbar_init(acc_empty0 + 8 * b, 2 * kEpilogueWarps);
         }
         mbar_init(ready, 1);
-        mbar_init(received, (kShare - 1) * kEpilogueWarps / 2);
+        mbar_init(received, q.share > 1 ? (q.share - 1) * kEpilogueWarps / 2 : 1);
         for (int i = 0; i < kSets * kEpilogueWarps; ++i) mbar_init(staged0 + 8 * i, 1);
         *abort_flag = 0;
         *finished = 0;
@@ -469,7 +475,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
     const int products = 3 * q.steps;
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t s = 0, ph = 0;
+            uint32_t used = 0;                           // bit s: parity of the stage's uses so far
             bool ok = true;
             for (int i = 0; ok && i < products; ++i) {
                 const int kind = i % 3, from = i / 3 & 1;
@@ -480,16 +486,18 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                 mbar_arrive(ready);
                 asm volatile("fence.proxy.async;" ::: "memory");      // some of the operands were written by plain stores
                 const int b_half = p.tile_n / 2, b_boxes = (b_half + 63) / 64;
-                const uint32_t bytes = kABytes + (p.b_rows ? b_boxes * 64 * kBK * 2 : b_half * kBK * 2);
+                const uint32_t bytes = kABytes + b_bytes(p);
+                const uint32_t depth = min(static_cast<uint32_t>(kStages), kRing / bytes);
+                uint32_t s = 0;                          // (nothing of the last product is in the ring any more)
                 for (Walk w(q, p); ok && w.index < w.end; w.index += w.step) {
                     const Tile t = tile_at(p, w.index);
                     const int a0 = t.row + static_cast<int>(rank) * kRowsPerBlock, b0 = t.col + static_cast<int>(rank) * b_half;
                     for (int kc = w.k0; kc < w.k1; ++kc) {
-                        if (!mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag)) {
+                        if (!mbar_wait(empty0 + 8 * s, ((used >> s) & 1) ^ 1u, abort_flag)) {
                             ok = false;
                             break;
                         }
-                        const uint32_t dst = stages + s * kStageBytes;
+                        const uint32_t dst = stages + s * bytes;
                         const uint32_t full = map_to_rank(full0 + 8 * s, leader);
                         if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * bytes);
                         if (p.a_rows) {
@@ -504,25 +512,17 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                         } else {
                             tma_load_matrix(dst + kABytes, tm_b, kc * kBK, b0, t.z, full);
                         }
-                        if (++s == kStages) {
-                            s = 0;
-                            ph ^= 1u;
-                        }
+                        used ^= 1u << s;
+                        if (++s == depth) s = 0;
                     }
                 }
             }
             // do not leave while the leader's instructions may still read this block's stages
-            for (int i = 0; i < kStages && ok; ++i) {
-                ok = mbar_wait(empty0 + 8 * s, ph ^ 1u, abort_flag);
-                if (++s == kStages) {
-                    s = 0;
-                    ph ^= 1u;
-                }
-            }
+            for (int s = 0; s < kStages && ok; ++s) ok = mbar_wait(empty0 + 8 * s, ((used >> s) & 1) ^ 1u, abort_flag);
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t s = 0, ph = 0;
+            uint32_t used = 0;
             bool ok = true;
             int it = 0;
             for (int i = 0; ok && i < products; ++i) {
@@ -532,6 +532,8 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                                        (static_cast<uint32_t>(p.tile_n >> 3) << 17) | (static_cast<uint32_t>(kTileM >> 4) << 24);
                 // 16 reduction elements: 32 bytes along a K-major row, 16 rows of 128 bytes MN-major
                 const uint32_t a_step = p.a_rows ? 2048 >> 4 : 32 >> 4, b_step = p.b_rows ? 2048 >> 4 : 32 >> 4;
+                const uint32_t bytes = kABytes + b_bytes(p), depth = min(static_cast<uint32_t>(kStages), kRing / bytes);
+                uint32_t s = 0;
                 for (Walk w(q, p); ok && w.index < w.end; w.index += w.step, ++it) {
                     const uint32_t buf = it & 1, use = (it >> 1) & 1;
                     if (!mbar_wait(acc_empty0 + 8 * buf, use ^ 1u, abort_flag)) {
@@ -541,22 +543,20 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                     tc_fence_after_sync();
                     const uint32_t d = tmem_base + buf * kAccCols;
                     for (int kc = w.k0; kc < w.k1; ++kc) {
-                        if (!mbar_wait(full0 + 8 * s, ph, abort_flag)) {
+                        if (!mbar_wait(full0 + 8 * s, (used >> s) & 1, abort_flag)) {
                             ok = false;
                             break;
                         }
                         tc_fence_after_sync();
-                        const uint32_t addr = stages + s * kStageBytes;
+                        const uint32_t addr = stages + s * bytes;
                         const uint64_t ad = p.a_rows ? smem_desc_rows(addr) : smem_desc(addr);
                         const uint64_t bd = p.b_rows ? smem_desc_rows(addr + kABytes) : smem_desc(addr + kABytes);
 #pragma unroll
                         for (int k = 0; k < kBK / 16; ++k)
                             umma_bf16(d, ad + a_step * k, bd + b_step * k, idesc, kc > w.k0 || k > 0);
                         umma_commit(empty0 + 8 * s, leader);
-                        if (++s == kStages) {
-                            s = 0;
-                            ph ^= 1u;
-                        }
+                        used ^= 1u << s;
+                        if (++s == depth) s = 0;
                     }
                     if (ok) umma_commit(acc_full0 + 8 * buf, leader);
                 }
@@ -674,7 +674,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                     if (!ok) break;
                     tc_fence_after_sync();
                     // the other pairs' parts go to them: [source][4 columns][row][4], a warp's stores are contiguous
-                    const int part = p.tile_n / kShare, sub = static_cast<int>(cluster_rank >> 1);
+                    const int part = p.tile_n / q.share, sub = static_cast<int>(cluster_rank >> 1);
                     for (int c = half * (p.tile_n / 2); c < (half + 1) * (p.tile_n / 2); c += 16) {
                         const int to = c / part;
                         if (to == sub) continue;
@@ -689,7 +689,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                     }
                     __syncwarp();
                     if (lane == 0) {
-                        for (int to = 0; to < kShare; ++to) {
+                        for (int to = 0; to < q.share; ++to) {
                             // (a part lies in one half of the tile's columns)
                             if (to != sub && to * part / (p.tile_n / 2) == half)
                                 mbar_arrive_release_cluster(map_to_rank(received, 2 * to + rank));
@@ -711,7 +711,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                         float acc[16];
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-                        for (int src = 0; src < kShare; ++src) {
+                        for (int src = 0; src < q.share; ++src) {
                             const int slot = src < sub ? src : src - 1;
                             const uint32_t base = besides + (slot * (part / 4) + (c - sub * part) / 4) * (kRowsPerBlock * 16) + row_in_block * 16;
 #pragma unroll
@@ -872,7 +872,8 @@ k_start(const Start s, const T *g)
 // X X^T, and down the rows (MN-major) by B X.  Instructions have 128 rows; with KP = 64 the upper half of them
 // computes on whatever lies behind the box, and nobody reads it.
 
-constexpr int kSmallThreads = 256;
+constexpr int kSmallThreads = 512;
+constexpr int kSmallQuads = kSmallThreads / 128;         // warps that share 32 rows: each takes a part of the columns
 constexpr int kSmallWarps = kSmallThreads / 32;
 constexpr int kSmallMost = 8;                            // blocks of a cluster
 constexpr int kGroup = 256;                              // columns of X that one accumulator buffer holds
@@ -883,7 +884,7 @@ struct Small {
     static constexpr int kSquare = KP / 64 * kBox;       // O, P
     static constexpr int kParts = KP * KP * 4;           // the parts of the rows that a block owns, from everyone
     static constexpr int kFloats = 2 * KP * 4;           // d, e
-    static constexpr int kRest = 256;                    // barriers
+    static constexpr int kRest = 512;                    // barriers, sums
     // slices: as many boxes as there is room for
     static constexpr int kBoxes = KP == 64 ? 11 : 3;
     static constexpr int bytes(int boxes, int blocks)
@@ -953,18 +954,6 @@ __device__ __forceinline__ uint32_t small_piece(uint32_t base, int row, int piec
     return base + (piece >> 3) * Small<KP>::kBox + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
 }
 
-// Eight neighbours of X in a row, times the factor, to hi and lo.
-__device__ __forceinline__ void split8(const float (&v)[8], float factor, uint32_t (&hw)[4], uint32_t (&lw)[4])
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float x = v[2 * e] * factor, y = v[2 * e + 1] * factor;
-        hw[e] = pack2(x, y);
-        const float2 h = unpack2(hw[e]);
-        lw[e] = pack2(x - h.x, y - h.y);
-    }
-}
-
 template <typename T, int KP>
 __global__ void __launch_bounds__(kSmallThreads, 1)
 k_small(const __grid_constant__ SmallArgs p, const T *g)
@@ -985,7 +974,7 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    const int quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane;
     const int64_t z = blockIdx.x / blocks;
     const int slice = static_cast<int>(rank) * p.boxes * 64;         // the block's first column
     const T *gz = g + z * p.g_batch;
@@ -1006,39 +995,59 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
 
-    // The norm.  A unit is eight elements of a row of G: along X's row, or (tall) down eight of them.
-    const int runs = (p.tall ? p.k + 7 : p.boxes * 64) / 8;          // per column of X, or per row
-    const int units = p.tall ? p.boxes * 64 * runs : p.k * runs;
-    auto unit = [&](int u, float (&v)[8], int &r, int &c) {
-        if (p.tall) {
-            r = u / (p.boxes * 64) * 8;
-            c = u % (p.boxes * 64);
-        } else {
-            r = u / runs;
-            c = u % runs * 8;
+    // G comes once: its numbers' upper and lower halves lie where hi and lo will, until the norm is known.  A unit is eight
+    // elements of a row of G, along X's row or (tall) down eight of them; several are under way at a time.
+    const int columns = p.boxes * 64;
+    const int units = columns * (KP / 8);
+    for (int i = threadIdx.x; i < 2 * p.boxes * S::kBox / 16; i += kSmallThreads) put_piece(hi0 + 16 * i, 0, 0, 0, 0);
+    if (threadIdx.x < 2 * KP) d[threadIdx.x] = 0.0f;
+    __syncthreads();
+    double sum = 0.0;
+    constexpr int kUnits = 4;
+    for (int u0 = threadIdx.x; u0 < units; u0 += kUnits * kSmallThreads) {
+        float v[kUnits][8];
+        int r[kUnits], c[kUnits];
+#pragma unroll
+        for (int j = 0; j < kUnits; ++j) {
+            const int u = u0 + j * kSmallThreads, box = u / (KP * 8);
+            r[j] = p.tall ? u / 64 % (KP / 8) * 8 : u / 8 % KP;
+            c[j] = box * 64 + (p.tall ? u % 64 : u % 8 * 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+            if (u >= units || r[j] >= p.k || slice + c[j] >= p.l) continue;
+            if (p.tall)
+                load8<T>(v[j], gz + (slice + c[j]) * p.g_row, r[j], p.k, p.g_whole);
+            else
+                load8<T>(v[j], gz + r[j] * p.g_row, slice + c[j], p.l, p.g_whole);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        if (slice + c >= p.l) return;
-        if (p.tall)
-            load8<T>(v, gz + (slice + c) * p.g_row, r, p.k, p.g_whole);
-        else
-            load8<T>(v, gz + r * p.g_row, slice + c, p.l, p.g_whole);
-    };
-    double sum = 0.0;
-    for (int u = threadIdx.x; u < units; u += kSmallThreads) {
-        float v[8];
-        int r, c;
-        unit(u, v, r, c);
+        for (int j = 0; j < kUnits; ++j) {
+            if (u0 + j * kSmallThreads >= units || r[j] >= p.k) continue;
+            uint32_t w[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fma(static_cast<double>(v[i]), static_cast<double>(v[i]), sum);
+            for (int i = 0; i < 8; ++i) {
+                sum = fma(static_cast<double>(v[j][i]), static_cast<double>(v[j][i]), sum);
+                w[i] = __float_as_uint(v[j][i]);
+            }
+            if (!p.tall) {
+                put_piece(small_piece<KP>(hi0, r[j], c[j] >> 3), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632),
+                          __byte_perm(w[4], w[5], 0x7632), __byte_perm(w[6], w[7], 0x7632));
+                put_piece(small_piece<KP>(lo0, r[j], c[j] >> 3), __byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410),
+                          __byte_perm(w[4], w[5], 0x5410), __byte_perm(w[6], w[7], 0x5410));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (r[j] + i >= p.k) break;
+                    const uint32_t at = small_piece<KP>(0, r[j] + i, c[j] >> 3) + 2 * (c[j] & 7);
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(hi0 + at), "h"(static_cast<uint16_t>(w[i] >> 16)) : "memory");
+                    asm volatile("st.shared.u16 [%0], %1;" ::"r"(lo0 + at), "h"(static_cast<uint16_t>(w[i])) : "memory");
+                }
+            }
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
     if (lane == 0) sums[warp] = sum;
-    // zeros where X has no rows, and (tall) columns are stored element by element
-    for (int i = threadIdx.x; i < 2 * p.boxes * S::kBox / 16; i += kSmallThreads) put_piece(hi0 + 16 * i, 0, 0, 0, 0);
-    if (threadIdx.x < 2 * KP) d[threadIdx.x] = 0.0f;
     __syncthreads();
     sum = 0.0;
     for (int i = 0; i < kSmallWarps; ++i) sum += sums[i];
@@ -1053,26 +1062,19 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         for (uint32_t i = 0; i < blocks; ++i) sum += sums[kSmallWarps + i];
     }
     const float factor = static_cast<float>(static_cast<double>(kScale) / (sqrt(sum) + p.eps));
-    for (int u = threadIdx.x; u < units; u += kSmallThreads) {
-        float v[8];
-        int r, c;
-        unit(u, v, r, c);
+    for (int i = threadIdx.x; i < p.boxes * S::kBox / 16; i += kSmallThreads) {
+        const uint4 up = get_piece(hi0 + 16 * i), low = get_piece(lo0 + 16 * i);
+        const uint32_t h[4] = {up.x, up.y, up.z, up.w}, l[4] = {low.x, low.y, low.z, low.w};
         uint32_t hw[4], lw[4];
-        split8(v, factor, hw, lw);
-        if (!p.tall) {
-            put_piece(small_piece<KP>(hi0, r, c >> 3), hw[0], hw[1], hw[2], hw[3]);
-            put_piece(small_piece<KP>(lo0, r, c >> 3), lw[0], lw[1], lw[2], lw[3]);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (r + i >= p.k) break;
-                const uint32_t at = small_piece<KP>(0, r + i, c >> 3) + 2 * (c & 7);
-                const uint16_t h = static_cast<uint16_t>(i & 1 ? hw[i / 2] >> 16 : hw[i / 2]);
-                const uint16_t l = static_cast<uint16_t>(i & 1 ? lw[i / 2] >> 16 : lw[i / 2]);
-                asm volatile("st.shared.u16 [%0], %1;" ::"r"(hi0 + at), "h"(h) : "memory");
-                asm volatile("st.shared.u16 [%0], %1;" ::"r"(lo0 + at), "h"(l) : "memory");
-            }
+        for (int j = 0; j < 4; ++j) {
+            const float x = __uint_as_float(__byte_perm(l[j], h[j], 0x5410)) * factor, y = __uint_as_float(__byte_perm(l[j], h[j], 0x7632)) * factor;
+            hw[j] = pack2(x, y);
+            const float2 f = unpack2(hw[j]);
+            lw[j] = pack2(x - f.x, y - f.y);
         }
+        put_piece(hi0 + 16 * i, hw[0], hw[1], hw[2], hw[3]);
+        put_piece(lo0 + 16 * i, lw[0], lw[1], lw[2], lw[3]);
     }
     fence_async();
     tc_fence_before_sync();
@@ -1083,7 +1085,7 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
     // f16 in, f32 out, 128 rows; KP columns along the rows of both, or `n` down the rows of the second operand
     const uint32_t idesc_square = (1u << 4) | ((KP >> 3) << 17) | ((128u >> 4) << 24);
     auto idesc_apply = [](int n) { return (1u << 4) | (1u << 16) | (static_cast<uint32_t>(n >> 3) << 17) | ((128u >> 4) << 24); };
-    const int columns = p.boxes * 64, groups = (columns + kGroup - 1) / kGroup;
+    const int groups = (columns + kGroup - 1) / kGroup;
     uint32_t done_phase = 0;                                         // bit b: parity of the next commit to buffer b
     bool ok = true;
     auto wait_done = [&](int b) {
@@ -1102,8 +1104,8 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             umma_one(tmem + (gr & 1) * kGroup, smem_desc(p0 + (i >> 2) * S::kBox) + 2 * (i & 3), bd + (2048 >> 4) * i, idesc, i > 0);
         umma_commit_one(done0 + 8 * (gr & 1));
     };
-    constexpr int kHalf = KP / 2;                                    // columns of a symmetric product that a warp takes
-    const bool mine = row < KP;
+    constexpr int kPart = KP / kSmallQuads;                          // columns of a symmetric product that a warp takes
+    const bool mine = quarter * 32 < KP;                             // (whole warps)
 
     for (int step = 0; step < p.steps; ++step) {
         const bool last = step + 1 == p.steps;
@@ -1118,25 +1120,23 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         wait_done(0);
         if (blocks == 1) {
 #pragma unroll 1
-            for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+            for (int c = part * kPart; mine && c < (part + 1) * kPart; c += 16) {
                 uint32_t acc[16], w[8];
                 tmem_ld16(lanes + c, acc);
                 tmem_wait_ld();
                 float v[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    v[i] = __uint_as_float(acc[i]) * kUnscale;
+                    v[i] = __uint_as_float(acc[i]) * kUnscale2;
                     if (c + i == row) {
-                        d[row] = v[i] * kUnscale;
+                        d[row] = v[i];
                         v[i] = 0.0f;
                     }
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
-                if (mine) {
-                    put_piece(small_piece<KP>(o0, row, c >> 3), w[0], w[1], w[2], w[3]);
-                    put_piece(small_piece<KP>(o0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
-                }
+                put_piece(small_piece<KP>(o0, row, c >> 3), w[0], w[1], w[2], w[3]);
+                put_piece(small_piece<KP>(o0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
             }
         } else {
             const int own = KP / static_cast<int>(blocks);           // rows that a block adds up
@@ -1144,14 +1144,12 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             const int to = row / own, local = row - to * own;
             const uint32_t base = mine ? map_to_rank(parts0 + ((rank * (KP / 4)) * own + local) * 16, to) : 0;
 #pragma unroll 1
-            for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+            for (int c = part * kPart; mine && c < (part + 1) * kPart; c += 16) {
                 uint32_t acc[16];
                 tmem_ld16(lanes + c, acc);
                 tmem_wait_ld();
-                if (mine) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) store_remote(base + ((c >> 2) + i) * own * 16, acc + 4 * i);
-                }
+                for (int i = 0; i < 4; ++i) store_remote(base + ((c >> 2) + i) * own * 16, acc + 4 * i);
             }
             __syncwarp();
             if (lane < blocks) mbar_arrive_release_cluster(map_to_rank(parts_full, lane));
@@ -1167,9 +1165,9 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
                 float diagonal = 0.0f;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    v[j] *= kUnscale;
+                    v[j] *= kUnscale2;
                     if (8 * piece + j == i) {
-                        diagonal = v[j] * kUnscale;
+                        diagonal = v[j];
                         v[j] = 0.0f;
                     }
                 }
@@ -1198,10 +1196,10 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         const float di = mine ? d[row] : 0.0f;
         wait_done(1);
 #pragma unroll 1
-        for (int c = half * kHalf; c < (half + 1) * kHalf; c += 16) {
+        for (int c = part * kPart; mine && c < (part + 1) * kPart; c += 16) {
             uint32_t acc[16], w[8];
             tmem_ld16(lanes + kGroup + c, acc);
-            const uint4 o_lo = get_piece(small_piece<KP>(o0, row & (KP - 1), c >> 3)), o_hi = get_piece(small_piece<KP>(o0, row & (KP - 1), (c >> 3) + 1));
+            const uint4 o_lo = get_piece(small_piece<KP>(o0, row, c >> 3)), o_hi = get_piece(small_piece<KP>(o0, row, (c >> 3) + 1));
             const uint32_t ow[8] = {o_lo.x, o_lo.y, o_lo.z, o_lo.w, o_hi.x, o_hi.y, o_hi.z, o_hi.w};
             tmem_wait_ld();
             float v[16];
@@ -1209,24 +1207,22 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             for (int i = 0; i < 16; i += 2) {
                 const float2 o = unpack2(ow[i / 2]);
                 const float2 dj = *reinterpret_cast<const float2 *>(d + c + i);
-                const float s0 = __uint_as_float(acc[i]) * kUnscale, s1 = __uint_as_float(acc[i + 1]) * kUnscale;
+                const float s0 = __uint_as_float(acc[i]), s1 = __uint_as_float(acc[i + 1]);
                 v[i] = fmaf(p.c, fmaf(di + dj.x, o.x, s0), p.b * o.x);
                 v[i + 1] = fmaf(p.c, fmaf(di + dj.y, o.y, s1), p.b * o.y);
                 if (c + i == row) {
-                    e[row] = fmaf(p.c, fmaf(di, di, s0 * kUnscale), p.b * di);
+                    e[row] = fmaf(p.c, fmaf(di, di, s0), p.b * di);
                     v[i] = 0.0f;
                 }
                 if (c + i + 1 == row) {
-                    e[row] = fmaf(p.c, fmaf(di, di, s1 * kUnscale), p.b * di);
+                    e[row] = fmaf(p.c, fmaf(di, di, s1), p.b * di);
                     v[i + 1] = 0.0f;
                 }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
-            if (mine) {
-                put_piece(small_piece<KP>(p0, row, c >> 3), w[0], w[1], w[2], w[3]);
-                put_piece(small_piece<KP>(p0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
-            }
+            put_piece(small_piece<KP>(p0, row, c >> 3), w[0], w[1], w[2], w[3]);
+            put_piece(small_piece<KP>(p0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
         }
         fence_async();
         tc_fence_before_sync();
@@ -1241,13 +1237,12 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             const int n = min(kGroup, columns - gr * kGroup);
             wait_done(gr & 1);
 #pragma unroll 1
-            for (int c = half * (n / 2); c < (half + 1) * (n / 2); c += 16) {
+            for (int c = part * (n / kSmallQuads); mine && c < (part + 1) * (n / kSmallQuads); c += 16) {
                 uint32_t acc[16];
                 tmem_ld16(lanes + (gr & 1) * kGroup + c, acc);
                 const int piece = (gr * kGroup + c) >> 3;
-                const uint32_t r = row & (KP - 1);
-                const uint4 h0 = get_piece(small_piece<KP>(hi0, r, piece)), h1 = get_piece(small_piece<KP>(hi0, r, piece + 1));
-                const uint4 l0 = get_piece(small_piece<KP>(lo0, r, piece)), l1 = get_piece(small_piece<KP>(lo0, r, piece + 1));
+                const uint4 h0 = get_piece(small_piece<KP>(hi0, row, piece)), h1 = get_piece(small_piece<KP>(hi0, row, piece + 1));
+                const uint4 l0 = get_piece(small_piece<KP>(lo0, row, piece)), l1 = get_piece(small_piece<KP>(lo0, row, piece + 1));
                 const uint32_t hw[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
                 const uint32_t lw[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
                 tmem_wait_ld();
@@ -1255,10 +1250,9 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float2 h = unpack2(hw[i]), l = unpack2(lw[i]);
-                    v[2 * i] = fmaf(scale, h.x + l.x, __uint_as_float(acc[2 * i]) * kUnscale);
-                    v[2 * i + 1] = fmaf(scale, h.y + l.y, __uint_as_float(acc[2 * i + 1]) * kUnscale);
+                    v[2 * i] = fmaf(scale, h.x + l.x, __uint_as_float(acc[2 * i]));
+                    v[2 * i + 1] = fmaf(scale, h.y + l.y, __uint_as_float(acc[2 * i + 1]));
                 }
-                if (!mine) continue;
                 if (!last) {
                     uint32_t nh[8], nl[8];
 #pragma unroll
@@ -1351,7 +1345,7 @@ struct orthogonal {
     int rows = 0, cols = 0, steps = 0, type = 0;
     float a = 0, b = 0, c = 0, eps = 0;
     int device = 0, sms = 0;
-    int pairs = 0, clusters = 0;     // of two and of 2 kShare blocks that the device holds at once
+    int pairs = 0, clusters[2] = {0, 0};     // of two blocks, and of 2 kShares[i], that the device holds at once
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
     int *err = nullptr;
@@ -1364,8 +1358,9 @@ int64_t pad8(int64_t v) { return div_up(v, 8) * 8; }
 int64_t pad16(int64_t v) { return div_up(v, 16) * 16; }
 
 // How k_small cuts the long side: blocks of a cluster and boxes of 64 columns for each.  A box costs a block about a sixth of
-// what crossing blocks does.  False where the matrix is not for it: a short side over 128, or too long a one.
-bool small_cut(const orthogonal *p, int *blocks, int *boxes)
+// what crossing blocks does, and matrices that do not fit on the device at once follow one another.  False where the
+// matrix is not for it: a short side over 128, or too long a one.
+bool small_cut(const orthogonal *p, int64_t batch, int *blocks, int *boxes)
 {
     const int k = short_side(p), l = p->rows > p->cols ? p->rows : p->cols;
     if (k > 128) return false;
@@ -1374,7 +1369,7 @@ bool small_cut(const orthogonal *p, int *blocks, int *boxes)
     int64_t best = -1;
     for (int n = 1; n <= kSmallMost; n *= 2) {
         const int64_t each = div_up(all, n);
-        const int64_t cost = each + (n > 1 ? 6 : 0);
+        const int64_t cost = (each + (n > 1 ? 12 : 6)) * div_up(batch, p->sms / n);
         if (each > most || (best >= 0 && cost >= best)) continue;
         best = cost;
         *blocks = n;
@@ -1427,9 +1422,10 @@ int64_t tiles_of(int64_t m, int64_t n, int tile_n, bool symmetric)
     return tiles;
 }
 
-// Chooses the tiles of a product for `pairs` pairs in clusters of `share` and returns what it costs, in steps of a tile of one
-// column.  Half the columns cost more than half, since the rows of A are shared by fewer; filling the ring and the last
-// tile's epilogue are worth about six steps; exchanging the parts of a shared tile about 1,500.
+// Chooses the tiles of a product for `pairs` pairs in clusters of `share` and returns what it costs, in units of 1.6 ns.  A block
+// brings in 128 rows of A and half the columns of B per step, at about 80 KB a microsecond whatever the tile (measured: 0.42 us
+// a step for 256 columns, 0.31 for 128, 0.28 for 64); the wait for the other blocks, the first loads and the last stores come
+// to 3 us, a set of 64 columns in the epilogue to half a microsecond, exchanging the parts of a shared tile to 2 us.
 int64_t choose_tile(Product &q, int64_t batch, int64_t pairs, int share)
 {
     q.steps = static_cast<int>(div_up(q.k, kBK));
@@ -1437,11 +1433,11 @@ int64_t choose_tile(Product &q, int64_t batch, int64_t pairs, int share)
     int64_t best = -1;
     for (int w : {256, 128, 64}) {
         const int64_t tiles = tiles_of(q.m, q.n, w, q.symmetric);
-        for (int shared = 0; shared <= (share > 1 && q.symmetric && w <= kShareCols ? 1 : 0); ++shared) {
-            // (a shared tile takes all stages of the reduction, and each cluster one)
-            if (shared && (q.steps < kShare || tiles * batch > pairs / share)) continue;
-            const int64_t rounds = shared ? 1 : div_up(tiles * batch, pairs), steps = shared ? div_up(q.steps, kShare) : q.steps;
-            const int64_t cost = (rounds * steps + 6) * (w + 128) + (shared ? 1500 : 0);
+        for (int shared = 0; shared <= (share > 1 && q.symmetric && w <= share_cols(share) ? 1 : 0); ++shared) {
+            // (a shared tile takes a step for each pair, and each cluster one tile)
+            if (shared && (q.steps < share || tiles * batch > pairs / share)) continue;
+            const int64_t rounds = shared ? 1 : div_up(tiles * batch, pairs), steps = shared ? div_up(q.steps, share) : q.steps;
+            const int64_t cost = rounds * steps * (w / 2 + 128) + 1800 + w / 64 * 300 + (shared ? 1250 : 0);
             if (best >= 0 && cost >= best) continue;
             best = cost;
             q.tile_n = w;
@@ -1477,7 +1473,7 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     const bool out_whole = p->cols % 8 == 0 && aligned(out, 16) && (p->rows == 1 || out_row % 8 == 0) && (batch == 1 || out_batch % 8 == 0);
     const bool g_whole = aligned(g, 16) && (p->rows == 1 || g_row * sizeof(T) % 16 == 0) && (batch == 1 || g_batch * sizeof(T) % 16 == 0);
     int blocks, boxes;
-    if (small_cut(p, &blocks, &boxes)) {
+    if (small_cut(p, batch, &blocks, &boxes)) {
         SmallArgs r = {};
         r.k = k;
         r.l = tall ? p->rows : p->cols;
@@ -1580,14 +1576,23 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     q.apply.n = p->cols;
     q.apply.k = k;
     q.apply.b_rows = !tall;
-    // pairs by themselves, or in clusters that can share a reduction: whichever the sum over a step is smaller with
-    Iteration alone = q;
+    // pairs by themselves, or in clusters that can share a reduction: whichever a step of the iteration is shortest with
+    int64_t most = p->pairs;                             // pairs on the device
     auto cost = [&](Iteration &r, int64_t pairs, int share) {
         r.share = share;
         return choose_tile(r.gram, batch, pairs, share) + choose_tile(r.square, batch, pairs, share) + choose_tile(r.apply, batch, pairs, share);
     };
-    const int64_t single_cost = cost(alone, p->pairs, 1);
-    if (p->clusters == 0 || cost(q, static_cast<int64_t>(p->clusters) * kShare, kShare) >= single_cost) q = alone;
+    int64_t best = cost(q, most, 1);
+    for (int i = 0; i < 2; ++i) {
+        Iteration other = q;
+        const int64_t pairs = static_cast<int64_t>(p->clusters[i]) * kShares[i];
+        if (pairs == 0) continue;
+        const int64_t c = cost(other, pairs, kShares[i]);
+        if (c >= best) continue;
+        best = c;
+        most = pairs;
+        q = other;
+    }
 
     Maps maps;
     const Operand o = {q.o, k, k, w.ldk}, pp = {q.p, k, k, w.ldk};
@@ -1621,7 +1626,6 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     if (wanted(q.square) > pairs) pairs = wanted(q.square);
     if (wanted(q.apply) > pairs) pairs = wanted(q.apply);
     pairs = div_up(pairs, q.share) * q.share;
-    const int64_t most = q.share > 1 ? static_cast<int64_t>(p->clusters) * kShare : p->pairs;
     if (pairs > most) pairs = most;
     cfg.gridDim = dim3(static_cast<unsigned>(2 * pairs));
     cfg.blockDim = dim3(kThreads);
@@ -1709,7 +1713,7 @@ int orthogonal_create(orthogonal **out, int rows, int cols, int steps, float a, 
         return ORTHOGONAL_ECUDA;
     }
     p->pairs = resident_clusters(2, p->sms);
-    p->clusters = resident_clusters(2 * kShare, p->sms);
+    for (int i = 0; i < 2; ++i) p->clusters[i] = resident_clusters(2 * kShares[i], p->sms);
     if (p->pairs < 1) {
         delete p;
         return ORTHOGONAL_ECUDA;
@@ -1750,7 +1754,7 @@ size_t orthogonal_workspace_bytes(const orthogonal *p, int64_t batch)
 {
     if (p == nullptr || !batch_ok(p, batch)) return 0;
     int blocks, boxes;
-    return small_cut(p, &blocks, &boxes) ? 0 : layout_of(p, batch).total;
+    return small_cut(p, batch, &blocks, &boxes) ? 0 : layout_of(p, batch).total;
 }
 
 int orthogonal_update(orthogonal *p, const void *g, int64_t g_stride_batch, int64_t g_stride_row, void *update,
