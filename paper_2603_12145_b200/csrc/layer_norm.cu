@@ -201,7 +201,7 @@ template <typename T, int V, int C, bool kWide>
 __global__ void __launch_bounds__(kWide ? kMost : kNarrowThreads)
 k_backward(const Backward<T> p)
 {
-    extern __shared__ float s_part[];                      // narrow rows: [2][width] while groups are added
+    extern __shared__ float s_part[];                      // narrow rows: [warps][2][width], the sums of a warp's row groups
     __shared__ float2 s_sum[kWide ? 2 * (kMost / 32) : 1];
     allow_next();
     Team<kWide> team;
@@ -209,9 +209,8 @@ k_backward(const Backward<T> p)
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
     const int per_block = kWide ? 1 : kNarrowThreads / p.lanes;
-    const int group = kWide ? 0 : static_cast<int>(threadIdx.x) / p.lanes;
     const int64_t step = static_cast<int64_t>(gridDim.x) * per_block;
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block + group;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * per_block + (kWide ? 0 : threadIdx.x / p.lanes);
     const int vectors = p.width / V;
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.dsum.ptr != nullptr;
@@ -296,24 +295,38 @@ k_backward(const Backward<T> p)
             }
         }
     } else {
-        for (int g = 0; g < per_block; ++g) {              // the block's row groups one after the other
-            if (g == group) {
+        // a warp's row groups by exchanges, the warps one after the other
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        for (int o = 16; o >= team.size; o >>= 1) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int v = c * team.size + team.index;
-                    if (v < vectors) {
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            float *a = s_part + v * V + e, *b = a + p.width;
-                            *a = g == 0 ? dw[c][e] : *a + dw[c][e];
-                            *b = g == 0 ? db[c][e] : *b + db[c][e];
-                        }
+                for (int e = 0; e < V; ++e) {
+                    dw[c][e] += __shfl_xor_sync(0xFFFFFFFFu, dw[c][e], o);
+                    db[c][e] += __shfl_xor_sync(0xFFFFFFFFu, db[c][e], o);
+                }
+        }
+        if (lane < team.size) {
+            float *mine = s_part + warp * 2 * p.width;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int v = c * team.size + team.index;
+                if (v < vectors) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        mine[v * V + e] = dw[c][e];
+                        mine[p.width + v * V + e] = db[c][e];
                     }
                 }
             }
-            __syncthreads();
         }
-        for (int i = threadIdx.x; i < 2 * p.width; i += kNarrowThreads) part[i] = s_part[i];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * p.width; i += kNarrowThreads) {
+            float sum = s_part[i];
+#pragma unroll
+            for (int w = 1; w < kNarrowThreads / 32; ++w) sum += s_part[w * 2 * p.width + i];
+            part[i] = sum;
+        }
     }
 }
 
@@ -412,21 +425,44 @@ struct layer_norm {
     int width = 0, type = 0;
     float eps = 0.0f;
     int device = 0, sms = 0;
+    int forward_blocks[2] = {0, 0}, backward_blocks[2] = {0, 0};     // that an SM holds; rows of single elements, of vectors
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
 };
 
 namespace {
 
-// Side by side, blocks of the backward kernel: as many as their registers let an SM hold, at most.
-constexpr int kNarrowBlocks = 4;
+Share share_for(const layer_norm *p, bool whole)
+{
+    const int V = 16 / element_bytes(p->type);
+    return share_of(whole ? p->width / V : p->width, whole);
+}
 
-// Blocks of the backward kernel (and rows of sums), for either of the kernel's forms.
-int64_t backward_blocks(const layer_norm *p, const Share &s, int64_t n)
+size_t backward_smem(const layer_norm *p, const Share &s) { return s.wide ? 0 : kNarrowThreads / 32 * 2 * sizeof(float) * p->width; }
+
+// Whole rounds of resident blocks, so that all end together.
+int64_t blocks_for(const layer_norm *p, const Share &s, int64_t n, int per_sm)
 {
     const int64_t units = s.wide ? n : div_up(n, kNarrowThreads / s.lanes);
-    const int64_t resident = static_cast<int64_t>(p->sms) * (s.wide ? kMost / s.lanes : kNarrowBlocks);
-    return div_up(units, div_up(units, resident));
+    return div_up(units, div_up(units, static_cast<int64_t>(p->sms) * per_sm));
+}
+
+template <typename T>
+bool count_blocks(layer_norm *p)
+{
+    for (int whole = 0; whole < 2; ++whole) {
+        if (whole && p->width % (16 / sizeof(T)) != 0) continue;
+        const Share s = share_for(p, whole);
+        const int threads = s.wide ? s.lanes : kNarrowThreads;
+        const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto wide) {
+            return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, wide.value>,
+                                                                 threads, 0) == cudaSuccess &&
+                   cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, wide.value>,
+                                                                 threads, backward_smem(p, s)) == cudaSuccess;
+        });
+        if (!ok || p->forward_blocks[whole] < 1 || p->backward_blocks[whole] < 1) return false;
+    }
+    return true;
 }
 
 bool check_in(const void *ptr, int64_t stride, int bytes, int *rc)
@@ -452,11 +488,9 @@ template <typename T>
 int run_forward(layer_norm *p, Forward<T> f, bool whole)
 {
     whole = whole && p->width % (16 / sizeof(T)) == 0;
-    const Share s = share_of(whole ? p->width / (16 / sizeof(T)) : p->width, whole);
+    const Share s = share_for(p, whole);
     f.lanes = s.lanes;
-    const int64_t units = s.wide ? f.n : div_up(f.n, kNarrowThreads / s.lanes);
-    const int64_t resident = static_cast<int64_t>(p->sms) * (s.wide ? 1024 / s.lanes : 8);
-    const unsigned blocks = static_cast<unsigned>(div_up(units, div_up(units, resident)));
+    const unsigned blocks = static_cast<unsigned>(blocks_for(p, s, f.n, p->forward_blocks[whole]));
     const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto wide) {
         k_forward<T, v.value, c.value, wide.value><<<blocks, s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
         return cudaGetLastError() == cudaSuccess;
@@ -470,10 +504,10 @@ template <typename T>
 int run_backward(layer_norm *p, Backward<T> b, bool whole, float *dw, float *db)
 {
     whole = whole && p->width % (16 / sizeof(T)) == 0;
-    const Share s = share_of(whole ? p->width / (16 / sizeof(T)) : p->width, whole);
+    const Share s = share_for(p, whole);
     b.lanes = s.lanes;
-    const int64_t blocks = backward_blocks(p, s, b.n);
-    const size_t smem = s.wide ? 0 : 2 * sizeof(float) * p->width;
+    const int64_t blocks = blocks_for(p, s, b.n, p->backward_blocks[whole]);
+    const size_t smem = backward_smem(p, s);
     const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto wide) {
         k_backward<T, v.value, c.value, wide.value>
             <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, smem, p->stream>>>(b);
@@ -561,7 +595,8 @@ int layer_norm_create(layer_norm **out, int width, float eps, int type)
     p->eps = eps;
     p->type = type;
     if (cudaGetDevice(&p->device) != cudaSuccess ||
-        cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess) {
+        cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess ||
+        !(type == LAYER_NORM_F32 ? count_blocks<float>(p) : type == LAYER_NORM_BF16 ? count_blocks<__nv_bfloat16>(p) : count_blocks<__half>(p))) {
         cudaGetLastError();
         delete p;
         return LAYER_NORM_ECUDA;
@@ -608,10 +643,9 @@ size_t layer_norm_workspace_bytes(const layer_norm *p, int64_t n)
 {
     if (p == nullptr || !rows_ok(n)) return 0;
     // rows of whole vectors and others are shared out differently: room for either
-    const int V = 16 / element_bytes(p->type);
-    int64_t rows = backward_blocks(p, share_of(p->width, false), n);
-    if (p->width % V == 0) {
-        const int64_t other = backward_blocks(p, share_of(p->width / V, true), n);
+    int64_t rows = blocks_for(p, share_for(p, false), n, p->backward_blocks[0]);
+    if (p->backward_blocks[1] > 0) {
+        const int64_t other = blocks_for(p, share_for(p, true), n, p->backward_blocks[1]);
         if (other > rows) rows = other;
     }
     return static_cast<size_t>(rows) * 2 * p->width * sizeof(float);

@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 from . import build as _build
 
@@ -34,6 +35,8 @@ class Args(ctypes.Structure):
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
+_PACKED = struct.Struct("=%dq" % (ctypes.sizeof(Args) // 8))      # all fields of Args, one after the other
+_NONE = (0, 0, 0)
 _lib = None
 
 
@@ -126,6 +129,7 @@ class GatedRecurrence:
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         self._on = None                   # the stream that the handle was last given
+        self._sizes = {}
         with torch.cuda.device(self.device):
             self.h = gated_recurrence_create(self.channels, types[self.dtype])
 
@@ -156,11 +160,13 @@ class GatedRecurrence:
         raise ValueError("%s must be %s on %s, got %s %s on %s with strides %s"
                          % (name, want, self.device, v.dtype, tuple(v.shape), v.device, v.stride()))
 
-    def _seq(self, name, v, batch, time):
-        if (v.dtype is not self.dtype or v.shape != (batch, time, self.channels) or v.get_device() != self._index
-                or (self.channels > 1 and v.stride(2) != 1)):
-            self._bad(name, v, "%s [%d, %d, %d] with a contiguous last dimension" % (self.dtype, batch, time, self.channels))
-        return Seq(v.data_ptr(), v.stride(0), v.stride(1))
+    def _seq(self, name, v, shape):
+        """(address, stride of the batch, stride of time)."""
+        s = v.stride()
+        if (v.dtype is not self.dtype or v.shape != shape or v.get_device() != self._index
+                or (s[2] != 1 and self.channels > 1)):
+            self._bad(name, v, "%s %s with a contiguous last dimension" % (self.dtype, list(shape)))
+        return v.data_ptr(), s[0], s[1]
 
     def _mask(self, name, v, shape):
         if v.dtype not in (self.torch.uint8, self.torch.bool) or v.shape != shape or v.get_device() != self._index:
@@ -179,10 +185,11 @@ class GatedRecurrence:
 
     def _like(self, v):
         """An output [batch, time, channels] with the order of v's dimensions."""
-        b, t = v.shape[0], v.shape[1]
-        if v.stride(0) < v.stride(1):
+        out = self.torch.empty_like(v)               # keeps the order of what is dense
+        if out.stride(0) > out.stride(1) and v.stride(0) < v.stride(1):
+            b, t = v.shape[0], v.shape[1]
             return self.torch.empty((t, b, self.channels), dtype=self.dtype, device=self.device).transpose(0, 1)
-        return self.torch.empty((b, t, self.channels), dtype=self.dtype, device=self.device)
+        return out
 
     def _f32(self, *shape):
         return self.torch.empty(shape, dtype=self.torch.float32, device=self.device)
@@ -193,73 +200,73 @@ class GatedRecurrence:
         """Buffer for the recurrent state, float32 [n, channels]."""
         return self._f32(n, self.channels)
 
+    def _size(self, batch, time, what):
+        """Bytes of `saved` ("saved"), of the forward (0) and of the backward workspace (1)."""
+        key = (batch, time, what)
+        if key not in self._sizes:
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            self._sizes[key] = (self._lib.gated_recurrence_saved_bytes(self.h, batch, time) if what == "saved" else
+                                self._lib.gated_recurrence_workspace_bytes(self.h, batch, time, what))
+        return self._sizes[key]
+
     def saved(self, batch: int, time: int):
         """Buffer in which sequence() leaves what backward() needs."""
-        return self._f32(int(self._lib.gated_recurrence_saved_bytes(self.h, batch, time)) // 4)
+        return self._f32(self._size(batch, time, "saved") // 4)
 
     # -- sequences
 
-    def _args(self, x, r, i, a, reset):
-        n, t = x.shape[0], x.shape[1]
-        args = Args(batch=n, time=t, x=self._seq("x", x, n, t), r=self._seq("r", r, n, t), i=self._seq("i", i, n, t),
-                    a=self._dense("a", a, (self.channels,)))
+    def _common(self, x, r, i, a, reset):
+        """The shape, and the packed arguments that both passes begin with."""
+        shape = x.shape
+        if len(shape) != 3 or shape[2] != self.channels:
+            self._bad("x", x, "%s [batch, time, %d]" % (self.dtype, self.channels))
+        mask = _NONE
         if reset is not None:
-            self._mask("reset", reset, (n, t))
-            args.reset = Seq(reset.data_ptr(), reset.stride(0), reset.stride(1))
-        return args
+            self._mask("reset", reset, shape[:2])
+            mask = (reset.data_ptr(),) + reset.stride()
+        return shape, (shape[0], shape[1], *self._seq("x", x, shape), *self._seq("r", r, shape), *self._seq("i", i, shape),
+                       *mask, self._dense("a", a, (self.channels,)))
 
-    def _workspace(self, args, backward):
-        size = self._lib.gated_recurrence_workspace_bytes(self.h, args.batch, args.time, backward)
-        if not size:
-            return None
-        scratch = self.torch.empty((size,), dtype=self.torch.uint8, device=self.device)
-        args.workspace, args.workspace_bytes = scratch.data_ptr(), size
-        return scratch
-
-    def _saved(self, saved, args):
-        need = int(self._lib.gated_recurrence_saved_bytes(self.h, args.batch, args.time)) // 4
-        return self._dense("saved", saved, (need,))
+    def _call(self, call, where, *fields):
+        code = call(self.h, _PACKED.pack(*fields))
+        if code != 0:
+            raise GatedRecurrenceError(code, where)
 
     def sequence(self, x, r, i, a, reset=None, state=None, state_out=None, saved=None, out=None):
         """y of the recurrence.  saved (from saved()) is filled for backward()."""
-        args = self._args(x, r, i, a, reset)
+        shape, first = self._common(x, r, i, a, reset)
+        n, t = shape[0], shape[1]
         if out is None:
             out = self._like(x)
-        args.y = self._seq("out", out, args.batch, args.time)
-        shape = (args.batch, self.channels)
-        if state is not None:
-            args.state = self._dense("state", state, shape)
-        if state_out is not None:
-            args.state_out = self._dense("state_out", state_out, shape)
-        if saved is not None:
-            args.saved = self._saved(saved, args)
-        scratch = self._workspace(args, 0)
+        states = (n, self.channels)
+        size = self._size(n, t, 0)
+        scratch = self.torch.empty((size,), dtype=self.torch.uint8, device=self.device) if size else None
         self._stream()
-        _check(self._lib.gated_recurrence_forward(self.h, ctypes.byref(args)), "gated_recurrence_forward")
-        del scratch
+        self._call(self._lib.gated_recurrence_forward, "gated_recurrence_forward", *first,
+                   0 if state is None else self._dense("state", state, states),
+                   0 if state_out is None else self._dense("state_out", state_out, states), *self._seq("out", out, shape),
+                   0 if saved is None else self._dense("saved", saved, (self._size(n, t, "saved") // 4,)),
+                   *_NONE, 0, *_NONE, *_NONE, *_NONE, 0, 0, scratch.data_ptr() if size else 0, size)
         return out
 
     def backward(self, dy, x, r, i, a, saved, reset=None, dstate_out=None, want_dstate=False):
         """Gradients as a dict: dx, dr, di, da, dstate (None where not wanted).  dstate_out: gradient of the state that
         sequence() returned."""
-        args = self._args(x, r, i, a, reset)
-        n, t = args.batch, args.time
-        out = {"dx": self._like(x), "dr": self._like(r), "di": self._like(i), "da": self._f32(self.channels),
-               "dstate": self.state(n) if want_dstate else None}
-        args.dy = self._seq("dy", dy, n, t)
-        args.saved = self._saved(saved, args)
-        for key in ("dx", "dr", "di"):
-            setattr(args, key, self._seq(key, out[key], n, t))
-        args.da = out["da"].data_ptr()
-        if want_dstate:
-            args.dstate = out["dstate"].data_ptr()
-        if dstate_out is not None:
-            args.dstate_out = self._dense("dstate_out", dstate_out, (n, self.channels))
-        scratch = self._workspace(args, 1)
+        shape, first = self._common(x, r, i, a, reset)
+        n, t = shape[0], shape[1]
+        states = (n, self.channels)
+        dx, dr, di, da = self._like(x), self._like(r), self._like(i), self.torch.empty_like(a)
+        dstate = self.state(n) if want_dstate else None
+        size = self._size(n, t, 1)
+        scratch = self.torch.empty((size,), dtype=self.torch.uint8, device=self.device) if size else None
         self._stream()
-        _check(self._lib.gated_recurrence_backward(self.h, ctypes.byref(args)), "gated_recurrence_backward")
-        del scratch
-        return out
+        self._call(self._lib.gated_recurrence_backward, "gated_recurrence_backward", *first, 0, 0, *_NONE,
+                   self._dense("saved", saved, (self._size(n, t, "saved") // 4,)), *self._seq("dy", dy, shape),
+                   0 if dstate_out is None else self._dense("dstate_out", dstate_out, states), dx.data_ptr(), *dx.stride()[:2],
+                   dr.data_ptr(), *dr.stride()[:2], di.data_ptr(), *di.stride()[:2], da.data_ptr(),
+                   0 if dstate is None else dstate.data_ptr(), scratch.data_ptr() if size else 0, size)
+        return {"dx": dx, "dr": dr, "di": di, "da": da, "dstate": dstate}
 
     # -- single tokens
 
@@ -268,7 +275,7 @@ class GatedRecurrence:
         t, index, dtype, ch = self.torch, self._index, self.dtype, self.channels
         n = x.shape[0]
         if out is None:
-            out = t.empty((n, ch), dtype=dtype, device=self.device)
+            out = t.empty_like(x) if x.is_contiguous() else t.empty((n, ch), dtype=dtype, device=self.device)
         if state_out is None:
             state_out = state
         row, f32 = (n, ch), t.float32

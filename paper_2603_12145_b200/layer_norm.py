@@ -105,6 +105,7 @@ class LayerNorm:
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         self._on = None                   # the stream that the handle was last given
+        self._sizes = {}                  # workspace bytes by rows
         with torch.cuda.device(self.device):
             self.h = layer_norm_create(self.width, self.eps, types[self.dtype])
 
@@ -136,20 +137,27 @@ class LayerNorm:
                          % (name, want, self.device, v.dtype, tuple(v.shape), v.device, v.stride()))
 
     def _rows(self, name, v, n):
-        """(address, row stride) of [n, width]."""
-        strides = v.stride()
+        """The address of [n, width]."""
         if (v.dtype is not self.dtype or v.shape != (n, self.width) or v.get_device() != self._index
-                or (self.width > 1 and strides[1] != 1)):
+                or (self.width > 1 and v.stride(1) != 1)):
             self._bad(name, v, "%s [%d, %d] with a contiguous last dimension" % (self.dtype, n, self.width))
-        return v.data_ptr(), strides[0]
+        return v.data_ptr()
 
     def _dense(self, name, v, shape):
         if v.dtype is not self.torch.float32 or v.shape != shape or v.get_device() != self._index or not v.is_contiguous():
             self._bad(name, v, "contiguous torch.float32 %s" % (shape,))
         return v.data_ptr()
 
-    def _empty(self, n):
-        return self.torch.empty((n, self.width), dtype=self.dtype, device=self.device)
+    def _like(self, x):
+        """An output [n, width]."""
+        if x.is_contiguous():
+            return self.torch.empty_like(x)
+        return self.torch.empty((x.shape[0], self.width), dtype=self.dtype, device=self.device)
+
+    def _all_rows(self, n, **rows):
+        for name, v in rows.items():
+            if v is not None:
+                self._rows(name, v, n)
 
     def saved(self, n: int):
         """Buffer in which forward() leaves what backward() needs: float32 [n, 2]."""
@@ -158,25 +166,31 @@ class LayerNorm:
     def forward(self, x, w=None, b=None, residual=None, saved=None, out=None, total=None):
         """The normalised rows; with a residual (rows, total): total = x + residual is the stream as it goes on, and
         may be given as x or residual themselves, to be updated in place."""
+        dtype, index, width = self.dtype, self._index, self.width
         n = x.shape[0]
         if out is None:
-            out = self._empty(n)
-        px, sx = self._rows("x", x, n)
-        po, so = self._rows("out", out, n)
-        pr, sr, pt, st = None, 0, None, 0
+            out = self._like(x)
+        row, sx, so, sr, st = (n, width), x.stride(), out.stride(), (0, 1), (0, 1)
+        # one look at everything: a few rows are short; what does not fit is named below
+        fits = (x.dtype is dtype and out.dtype is dtype and x.shape == row and out.shape == row and x.get_device() == index
+                and out.get_device() == index)
         if residual is not None:
             if total is None:
-                total = self._empty(n)
-            pr, sr = self._rows("residual", residual, n)
-            pt, st = self._rows("total", total, n)
+                total = self._like(x)
+            sr, st = residual.stride(), total.stride()
+            fits = (fits and residual.dtype is dtype and total.dtype is dtype and residual.shape == row and total.shape == row
+                    and residual.get_device() == index and total.get_device() == index)
         elif total is not None:
             raise ValueError("total needs a residual")
-        shape = (self.width,)
-        pw = None if w is None else self._dense("w", w, shape)
-        pb = None if b is None else self._dense("b", b, shape)
-        ps = None if saved is None else self._dense("saved", saved, (n, 2))
+        if not fits or (width > 1 and not sx[1] == so[1] == sr[1] == st[1] == 1):
+            self._all_rows(n, x=x, out=out, residual=residual, total=total)
+        shape = (width,)
         self._stream()
-        code = self._lib.layer_norm_forward(self.h, px, sx, pr, sr, pw, pb, pt, st, po, so, ps, n)
+        code = self._lib.layer_norm_forward(
+            self.h, x.data_ptr(), sx[0], None if residual is None else residual.data_ptr(), sr[0],
+            None if w is None else self._dense("w", w, shape), None if b is None else self._dense("b", b, shape),
+            None if total is None else total.data_ptr(), st[0], out.data_ptr(), so[0],
+            None if saved is None else self._dense("saved", saved, (n, 2)), n)
         if code != 0:
             raise LayerNormError(code, "layer_norm_forward")
         return out if residual is None else (out, total)
@@ -185,26 +199,35 @@ class LayerNorm:
         """(dx, dw, db) for the rows s that were normalised (forward's total, or its x).  dsum: the gradient that
         reaches the stream from behind.  dx is the gradient of x and of the residual alike; dw and db are None unless
         wanted."""
+        dtype, index, width = self.dtype, self._index, self.width
         n = s.shape[0]
-        dx = self._empty(n) if out is None else out
-        pdy, sdy = self._rows("dy", dy, n)
-        ps, ss = self._rows("s", s, n)
-        px, sx = self._rows("out", dx, n)
-        pd, sd = (None, 0) if dsum is None else self._rows("dsum", dsum, n)
-        pw = None if w is None else self._dense("w", w, (self.width,))
+        dx = self._like(s) if out is None else out
+        row, sy, ss, sx, sd = (n, width), dy.stride(), s.stride(), dx.stride(), (0, 1)
+        fits = (dy.dtype is dtype and s.dtype is dtype and dx.dtype is dtype and dy.shape == row and s.shape == row
+                and dx.shape == row and dy.get_device() == index and s.get_device() == index and dx.get_device() == index)
+        if dsum is not None:
+            sd = dsum.stride()
+            fits = fits and dsum.dtype is dtype and dsum.shape == row and dsum.get_device() == index
+        if not fits or (width > 1 and not sy[1] == ss[1] == sx[1] == sd[1] == 1):
+            self._all_rows(n, dy=dy, s=s, out=dx, dsum=dsum)
+        pw = None if w is None else self._dense("w", w, (width,))
         kept = self._dense("saved", saved, (n, 2))
         dw = db = scratch = None
         size = 0
         if want_params:
             t = self.torch
-            both = t.empty((2, self.width), dtype=t.float32, device=self.device)
-            dw, db = both[0], both[1]
-            size = self._lib.layer_norm_workspace_bytes(self.h, n)
+            dw, db = (t.empty((width,), dtype=t.float32, device=self.device) if w is None else t.empty_like(w) for _ in range(2))
+            if n not in self._sizes:
+                if len(self._sizes) > 1000:
+                    self._sizes.clear()
+                self._sizes[n] = self._lib.layer_norm_workspace_bytes(self.h, n)
+            size = self._sizes[n]
             scratch = t.empty((size,), dtype=t.uint8, device=self.device)
         self._stream()
-        code = self._lib.layer_norm_backward(self.h, pdy, sdy, ps, ss, pw, kept, pd, sd, px, sx,
-                                             None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
-                                             None if scratch is None else scratch.data_ptr(), size, n)
+        code = self._lib.layer_norm_backward(
+            self.h, dy.data_ptr(), sy[0], s.data_ptr(), ss[0], pw, kept, None if dsum is None else dsum.data_ptr(), sd[0],
+            dx.data_ptr(), sx[0], None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+            None if scratch is None else scratch.data_ptr(), size, n)
         if code != 0:
             raise LayerNormError(code, "layer_norm_backward")
         return dx, dw, db
