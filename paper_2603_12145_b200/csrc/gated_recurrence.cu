@@ -270,7 +270,7 @@ struct Block {
 
 // kEnds: the first pass over segments.
 template <typename T, int V, bool kEnds>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && !kEnds ? 5 : 1)
 k_forward(const Shape s, const Params<T> p)
 {
     using F = Vals<V>;
@@ -386,8 +386,10 @@ k_carry(const Shape s, float *carry, const float *span, const float *start, cons
     }
 }
 
+// (16-bit types: four blocks per SM, 287 us at 512 x 128 x 1152 against 390 with the two or three that more registers leave;
+// binary32 would spill.)
 template <typename T, int V, bool kEnds>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && !kEnds ? 4 : 1)
 k_backward(const Shape s, const Params<T> p)
 {
     using F = Vals<V>;
@@ -596,9 +598,11 @@ int element_bytes(const gated_recurrence *p) { return p->type == GATED_RECURRENC
 
 bool sizes_ok(int64_t batch, int64_t time) { return batch >= 1 && time >= 1 && batch <= kMaxBlocks && time <= kMaxBlocks / 2; }
 
-// The cut of the time axis, for warps of 64 channels.  One segment costs one pass over its steps, several cost two: the
-// cut pays where the rows alone give less than half of the warps that the device holds.  The segments then fill one or a
-// few whole rounds of them, whichever is the shortest.
+// The cut of the time axis, for warps of 64 channels, by what it would take in nanoseconds.  A warp by itself goes through eight
+// steps in about 1,000 forward and 1,900 backward (800 in the pass that looks for a segment's end); the device through
+// 500 elements a nanosecond forward, 260 backward (700), however they are cut.  Chaining costs two more launches and
+// about 100 per segment.  (3 x 777 x 331 in binary32: forward 69 us uncut, 14.5 in 32 segments, 20.7 in 97; 64 x 512 x 512 in
+// bfloat16: 70 uncut, 80 in 5; backward 134 and 104.)
 Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool backward)
 {
     Shape s = {};
@@ -608,22 +612,29 @@ Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool back
     const int64_t tiles = div_up(p->channels, 64), warps = batch * tiles;
     const int64_t resident = static_cast<int64_t>(p->sms) * (backward ? 16 : 20);
     const int64_t chunks = div_up(time, kSteps);
+    const double elements = static_cast<double>(batch) * time * p->channels;
+    auto passes = [&](int64_t steps8, bool ends) {
+        auto pass = [&](double chain, double rate) {
+            const double alone = chain * steps8, all = elements / rate;
+            return alone > all ? alone + 0.5 * all : all + 0.5 * alone;
+        };
+        return (backward ? pass(1900, 260) : pass(1000, 500)) + (!ends ? 0 : backward ? pass(800, 700) : 0.85 * pass(1000, 500));
+    };
     s.segments = 1;
     s.segment_steps = static_cast<int>(chunks * kSteps);
-    if (resident / warps >= 2 && chunks >= 4) {
-        int64_t best = -1, best_per = chunks;
-        for (int rounds = 1; rounds <= 4; ++rounds) {
-            const int64_t most = rounds * resident / warps;
-            const int64_t per = div_up(chunks, most < chunks ? most : chunks);
-            const int64_t cost = div_up(div_up(chunks, per) * warps, resident) * (2 * per + 1);   // a segment's start: half a chunk
-            if (best < 0 || cost < best) {
-                best = cost;
-                best_per = per;
-            }
-        }
-        s.segments = static_cast<int>(div_up(chunks, best_per));
-        s.segment_steps = static_cast<int>(best_per * kSteps);
-    }
+    double best = passes(chunks * div_up(warps, resident), false);
+    const int64_t round = resident / warps;              // segments that fill the device once
+    auto consider = [&](int64_t n) {
+        if (n < 2 || n > chunks) return;
+        const int64_t per = div_up(chunks, n), segments = div_up(chunks, per);
+        const double cost = passes(per * div_up(segments * warps, resident), true) + 5000 + 100.0 * segments;
+        if (cost >= best) return;
+        best = cost;
+        s.segments = static_cast<int>(segments);
+        s.segment_steps = static_cast<int>(per * kSteps);
+    };
+    for (int64_t n = 2; n < round; n += n / 2) consider(n);
+    for (int64_t n = 1; n <= 4; ++n) consider(n * round);
     const int64_t units = batch * s.segments;
     int64_t slots = div_up(resident, tiles);
     if (slots > units) slots = units;

@@ -331,7 +331,7 @@ k_backward(const Backward<T> p)
 }
 
 // dw and db: a block takes 32 columns of the `rows` rows of sums, eight warps share the rows.
-constexpr int kJoinWarps = 8;
+constexpr int kJoinWarps = 32;
 
 __global__ void __launch_bounds__(32 * kJoinWarps)
 k_join(const float *part, int rows, int width, float *dw, float *db)

@@ -181,15 +181,18 @@ def argument_checks(fake):                                                      
         setattr(a, key, None)
         assert L.gated_recurrence_backward(h, ctypes.byref(a)) == -2
     L = orthogonal.load()
-    h = orthogonal.orthogonal_create(50, 60, 5, 3.4445, -4.775, 2.0315, 1e-7, 1)
+    small = orthogonal.orthogonal_create(50, 160, 5, 3.4445, -4.775, 2.0315, 1e-7, 1)      # stays on the chip: no workspace
+    assert L.orthogonal_workspace_bytes(small, 2) == 0
+    assert L.orthogonal_update(small, p(0), 8000, 160, p(1), 8000, 160, None, 0, 2) == 0
+    h = orthogonal.orthogonal_create(150, 160, 5, 3.4445, -4.775, 2.0315, 1e-7, 1)
     need = L.orthogonal_workspace_bytes(h, 2)
 
-    def update(g=p(0), gb=3000, gr=60, o=p(1), ob=3000, orow=60, ws=p(2), size=need, n=2):
+    def update(g=p(0), gb=24000, gr=160, o=p(1), ob=24000, orow=160, ws=p(2), size=need, n=2):
         return L.orthogonal_update(h, g, gb, gr, o, ob, orow, ws, size, n)
 
     assert update() == 0 and update(gb=0) == 0 and update(n=1, ob=0) == 0
     refused(update, [(-1, dict(n=0)), (-1, dict(n=65536)), (-2, dict(g=None)), (-2, dict(o=None)), (-2, dict(ws=None)), (-1, dict(gr=-1)),
-                     (-1, dict(orow=59)), (-1, dict(ob=2999)), (-3, dict(g=p(0) + 1)), (-3, dict(ws=p(2) + 128)), (-5, dict(size=need - 1))])
+                     (-1, dict(orow=159)), (-1, dict(ob=23999)), (-3, dict(g=p(0) + 1)), (-3, dict(ws=p(2) + 128)), (-5, dict(size=need - 1))])
 
 
 def shared_rows(fake):                                                                   # noqa: F811
@@ -211,7 +214,7 @@ def cuts(fake):                                                                 
     """A call that is cut along the time axis takes two more kernels, one with rows enough does not; workspaces fit."""
     L = gated_recurrence.load()
     h = gated_recurrence.gated_recurrence_create(96, 1)
-    for batch, time, forward, backward in ((5000, 40, 1, 2), (1, 500, 3, 4), (1, 1, 1, 2), (2, 31, 1, 2)):
+    for batch, time, forward, backward in ((5000, 40, 1, 2), (1, 500, 3, 4), (1, 1, 1, 2), (2, 31, 1, 2), (3, 777, 3, 4)):
         a = recurrence_args(batch, time, 96)
         for call, want in ((L.gated_recurrence_forward, forward), (L.gated_recurrence_backward, backward)):
             fake.lib.fake_clear()
