@@ -19,12 +19,14 @@ TARGETS = {
     "libcartpole_b200.so": (["cartpole.cu"], ["on_device.cuh", os.path.join(INCLUDE, "cartpole.h")]),
     "libgru_policy_b200.so": (["gru_policy.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gru_policy.h")]),
     "libgated_ffn_b200.so": (["gated_ffn.cu"], ["sm100.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_ffn.h")]),
-    "liblayer_norm_b200.so": (["layer_norm.cu"], ["vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "layer_norm.h")]),
+    "liblayer_norm_b200.so": (["layer_norm.cu"], ["vectors.cuh", "ssm_common.cuh", "on_device.cuh", os.path.join(INCLUDE, "layer_norm.h"),
+                                                   os.path.join(INCLUDE, "ssm.h")]),
     "libgated_recurrence_b200.so": (["gated_recurrence.cu"],
                                     ["vectors.cuh", "ssm_common.cuh", "on_device.cuh", os.path.join(INCLUDE, "gated_recurrence.h"),
                                      os.path.join(INCLUDE, "ssm.h")]),
     "liborthogonal_b200.so": (["orthogonal.cu"],
-                              ["sm100.cuh", "vectors.cuh", "on_device.cuh", os.path.join(INCLUDE, "orthogonal.h")]),
+                              ["sm100.cuh", "vectors.cuh", "ssm_common.cuh", "on_device.cuh", os.path.join(INCLUDE, "orthogonal.h"),
+                               os.path.join(INCLUDE, "ssm.h")]),
     "libssm_b200.so": (["ssm_api.cu", "ssm_conv.cu", "ssm_scan_forward.cu", "ssm_scan_backward.cu"],
                        ["ssm_common.cuh", "ssm_kernels.cuh", "on_device.cuh", os.path.join(INCLUDE, "ssm.h")]),
 }

@@ -22,7 +22,6 @@
 
 #include "../../include/gated_recurrence.h"
 #include "on_device.cuh"
-#include "ssm_common.cuh"
 #include "vectors.cuh"
 
 namespace {
@@ -35,66 +34,6 @@ constexpr int kStepThreads = 256;
 
 __device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-// ---- V channels' values: a number, or a pair that one instruction works on
-
-using ssm_k::add;
-using ssm_k::ex2;
-using ssm_k::fma;
-using ssm_k::hi;
-using ssm_k::lo;
-using ssm_k::mul;
-using ssm_k::Pair;
-using ssm_k::pair;
-using ssm_k::rcp;
-
-template <int V>
-using Vals = std::conditional_t<V == 1, float, Pair>;
-
-__device__ __forceinline__ float add(float a, float b) { return __fadd_rn(a, b); }
-__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
-__device__ __forceinline__ float fma(float a, float b, float c) { return fmaf(a, b, c); }
-
-template <int V>
-__device__ __forceinline__ Vals<V> all(float v)
-{
-    if constexpr (V == 1)
-        return v;
-    else
-        return pair(v, v);
-}
-
-// f on each channel
-template <typename F>
-__device__ __forceinline__ float each(F f, float a) { return f(a); }
-template <typename F>
-__device__ __forceinline__ Pair each(F f, Pair a) { return pair(f(lo(a)), f(hi(a))); }
-template <typename F>
-__device__ __forceinline__ float each(F f, float a, float b) { return f(a, b); }
-template <typename F>
-__device__ __forceinline__ Pair each(F f, Pair a, Pair b) { return pair(f(lo(a), lo(b)), f(hi(a), hi(b))); }
-template <typename F>
-__device__ __forceinline__ float each(F f, float a, float b, float c) { return f(a, b, c); }
-template <typename F>
-__device__ __forceinline__ Pair each(F f, Pair a, Pair b, Pair c) { return pair(f(lo(a), lo(b), lo(c)), f(hi(a), hi(b), hi(c))); }
-
-template <typename T>
-__device__ __forceinline__ float widen(const Packed<T, 1> &v) { return packed_get<T, 1>(v, 0); }
-template <typename T>
-__device__ __forceinline__ Pair widen(const Packed<T, 2> &v) { return pair(packed_get<T, 2>(v, 0), packed_get<T, 2>(v, 1)); }
-
-template <typename T>
-__device__ __forceinline__ Packed<T, 1> narrow(float v)
-{
-    const float f[1] = {v};
-    return packed_of<T, 1>(f);
-}
-template <typename T>
-__device__ __forceinline__ Packed<T, 2> narrow(Pair v)
-{
-    const float f[2] = {lo(v), hi(v)};
-    return packed_of<T, 2>(f);
-}
 
 template <int V>
 __device__ __forceinline__ Vals<V> load_floats(const float *src)

@@ -75,8 +75,8 @@ struct Team {
             const int lane = index & 31, warps = size >> 5;
             if (lane == 0) s[index >> 5] = v;
             __syncthreads();
-            v = lane < warps ? s[lane] : make_float2(0.0f, 0.0f);
-            for (int o = 16; o > 0; o >>= 1) {
+            v = s[lane & (warps - 1)];               // (their number is a power of two)
+            for (int o = warps >> 1; o > 0; o >>= 1) {
                 v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, o);
                 v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, o);
             }
@@ -99,24 +99,28 @@ struct Team {
     }
 };
 
-// V neighbouring parameters (from L1: every row reads them)
+// V neighbouring parameters (from L1: every row reads them), in units of one or two
 template <int V>
-__device__ __forceinline__ void load_params(float (&dst)[V], const float *src, float absent)
+__device__ __forceinline__ void load_params(Vals<V == 1 ? 1 : 2> (&dst)[(V + 1) / 2], const float *src, float absent)
 {
+    constexpr int W = V == 1 ? 1 : 2;
     if (src == nullptr) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) dst[e] = absent;
-    } else if constexpr (V % 4 == 0) {
-#pragma unroll
-        for (int e = 0; e < V; e += 4) {
-            const float4 f = __ldg(reinterpret_cast<const float4 *>(src + e));
-            dst[e] = f.x, dst[e + 1] = f.y, dst[e + 2] = f.z, dst[e + 3] = f.w;
-        }
+        for (int i = 0; i < (V + 1) / 2; ++i) dst[i] = all<W>(absent);
+    } else if constexpr (V == 1) {
+        dst[0] = __ldg(src);
     } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) dst[e] = __ldg(src + e);
+        for (int i = 0; i < V / 2; i += 2) {
+            const float4 f = __ldg(reinterpret_cast<const float4 *>(src + 2 * i));
+            dst[i] = pair(f.x, f.y);
+            dst[i + 1] = pair(f.z, f.w);
+        }
     }
 }
+
+__device__ __forceinline__ void store_unit(float *dst, float v) { *dst = v; }
+__device__ __forceinline__ void store_unit(float *dst, Pair v) { *reinterpret_cast<float2 *>(dst) = make_float2(lo(v), hi(v)); }
 
 // V elements per access, C accesses per thread and row.
 template <typename T, int V, int C, bool kWide>
@@ -134,6 +138,8 @@ k_forward(const Forward<T> p)
     const int vectors = p.width / V;
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.residual.ptr != nullptr;
+    constexpr int W = V == 1 ? 1 : 2, N = (V + 1) / 2;     // units of a vector
+    using U = Vals<W>;
     Packed<T, V> nx[C], nr[C];
     auto fetch = [&](int64_t row) {
 #pragma unroll
@@ -148,50 +154,49 @@ k_forward(const Forward<T> p)
     // a warp's lanes stay together (its rows are neighbours): all go round while the first of them has a row
     for (int64_t row = first; row - (kWide ? 0 : (threadIdx.x & 31) / p.lanes) < p.n; row += step) {
         const bool live = row < p.n;
-        float s[C][V];
+        U s[C][N], sum = all<W>(0.0f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) s[c][e] = packed_get<T, V>(nx[c], e);
+            const int v = c * team.size + team.index;
             if (added) {
+                Packed<T, V> rounded;
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[c][e] += packed_get<T, V>(nr[c], e);
-                const Packed<T, V> rounded = packed_of<T, V>(s[c]);
-                const int v = c * team.size + team.index;
+                for (int i = 0; i < N; ++i) narrow_at(rounded, i, add(widen_at(nx[c], i), widen_at(nr[c], i)));
                 if (v < vectors && live) packed_store<T, V>(p.sum.row(row) + v * V, rounded);
+                nx[c] = rounded;
+            }
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[c][e] = packed_get<T, V>(rounded, e);
+            for (int i = 0; i < N; ++i) {
+                s[c][i] = widen_at(nx[c], i);
+                sum = add(sum, s[c][i]);
             }
         }
         fetch(row + step);
-        float sum = 0.0f;
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum += s[c][e];
-        const float mean = team.total(sum) * inverse;
-        float square = 0.0f;
+        const float mean = team.total(sum_of(sum)) * inverse;
+        U square = all<W>(0.0f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const bool in = c * team.size + team.index < vectors;
+            if (c * team.size + team.index < vectors) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                s[c][e] = in ? s[c][e] - mean : 0.0f;
-                square = fmaf(s[c][e], s[c][e], square);
+                for (int i = 0; i < N; ++i) {
+                    s[c][i] = add(s[c][i], all<W>(-mean));
+                    square = fma(s[c][i], s[c][i], square);
+                }
             }
         }
-        const float scale = rsqrtf(fmaf(team.total(square), inverse, p.eps));
+        const float scale = rsqrtf(fmaf(team.total(sum_of(square)), inverse, p.eps));
         if (p.saved != nullptr && team.index == 0 && live) p.saved[row] = make_float2(mean, scale);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int v = c * team.size + team.index;
             if (v < vectors && live) {
-                float w[V], b[V];
+                U w[N], b[N];
                 load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
                 load_params<V>(b, p.b != nullptr ? p.b + v * V : nullptr, 0.0f);
+                Packed<T, V> out;
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[c][e] = fmaf(s[c][e] * scale, w[e], b[e]);
-                packed_store<T, V>(p.y.row(row) + v * V, packed_of<T, V>(s[c]));
+                for (int i = 0; i < N; ++i) narrow_at(out, i, fma(mul(s[c][i], all<W>(scale)), w[i], b[i]));
+                packed_store<T, V>(p.y.row(row) + v * V, out);
             }
         }
     }
@@ -214,11 +219,13 @@ k_backward(const Backward<T> p)
     const int vectors = p.width / V;
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.dsum.ptr != nullptr;
-    float dw[C][V], db[C][V];
+    constexpr int W = V == 1 ? 1 : 2, N = (V + 1) / 2;     // units of a vector
+    using U = Vals<W>;
+    U dw[C][N], db[C][N];
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < V; ++e) dw[c][e] = db[c][e] = 0.0f;
+        for (int i = 0; i < N; ++i) dw[c][i] = db[c][i] = all<W>(0.0f);
     Packed<T, V> ns[C], ndy[C], nd[C];
     float2 nstat;
     auto fetch = [&](int64_t row) {
@@ -244,39 +251,41 @@ k_backward(const Backward<T> p)
         }
         const float mean = nstat.x, scale = nstat.y;
         fetch(row + step);
-        float2 sums = make_float2(0.0f, 0.0f);
+        const U q = all<W>(scale);
+        U sum = all<W>(0.0f), along = sum;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int v = c * team.size + team.index;
             if (v < vectors) {
-                float w[V];
+                U w[N];
                 load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float z = (packed_get<T, V>(s[c], e) - mean) * scale, g = packed_get<T, V>(dy[c], e);
-                    const float h = g * w[e];
-                    sums.x += h;
-                    sums.y = fmaf(h, z, sums.y);
-                    dw[c][e] = fmaf(g, z, dw[c][e]);
-                    db[c][e] += g;
+                for (int i = 0; i < N; ++i) {
+                    const U z = mul(add(widen_at(s[c], i), all<W>(-mean)), q), g = widen_at(dy[c], i), h = mul(g, w[i]);
+                    sum = add(sum, h);
+                    along = fma(h, z, along);
+                    dw[c][i] = fma(g, z, dw[c][i]);
+                    db[c][i] = add(db[c][i], g);
                 }
             }
         }
-        sums = team.total(sums);
-        const float along = -scale * sums.y * inverse, shift = -scale * sums.x * inverse;
+        const float2 sums = team.total(make_float2(sum_of(sum), sum_of(along)));
+        const U slope = all<W>(-scale * sums.y * inverse), shift = all<W>(-scale * sums.x * inverse);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int v = c * team.size + team.index;
             if (v < vectors && live) {
-                float w[V], out[V];
+                U w[N];
                 load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+                Packed<T, V> out;
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float z = (packed_get<T, V>(s[c], e) - mean) * scale;
-                    out[e] = fmaf(packed_get<T, V>(dy[c], e) * w[e], scale, fmaf(z, along, shift));
-                    if (added) out[e] += packed_get<T, V>(d[c], e);
+                for (int i = 0; i < N; ++i) {
+                    const U z = mul(add(widen_at(s[c], i), all<W>(-mean)), q);
+                    U x = fma(mul(widen_at(dy[c], i), w[i]), q, fma(z, slope, shift));
+                    if (added) x = add(x, widen_at(d[c], i));
+                    narrow_at(out, i, x);
                 }
-                packed_store<T, V>(p.dx.row(row) + v * V, packed_of<T, V>(out));
+                packed_store<T, V>(p.dx.row(row) + v * V, out);
             }
         }
     }
@@ -288,9 +297,9 @@ k_backward(const Backward<T> p)
             const int v = c * team.size + team.index;
             if (v < vectors) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    part[v * V + e] = dw[c][e];
-                    part[p.width + v * V + e] = db[c][e];
+                for (int i = 0; i < N; ++i) {
+                    store_unit(part + v * V + W * i, dw[c][i]);
+                    store_unit(part + p.width + v * V + W * i, db[c][i]);
                 }
             }
         }
@@ -301,9 +310,9 @@ k_backward(const Backward<T> p)
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    dw[c][e] += __shfl_xor_sync(0xFFFFFFFFu, dw[c][e], o);
-                    db[c][e] += __shfl_xor_sync(0xFFFFFFFFu, db[c][e], o);
+                for (int i = 0; i < N; ++i) {
+                    dw[c][i] = each([&](float x) { return x + __shfl_xor_sync(0xFFFFFFFFu, x, o); }, dw[c][i]);
+                    db[c][i] = each([&](float x) { return x + __shfl_xor_sync(0xFFFFFFFFu, x, o); }, db[c][i]);
                 }
         }
         if (lane < team.size) {
@@ -313,9 +322,9 @@ k_backward(const Backward<T> p)
                 const int v = c * team.size + team.index;
                 if (v < vectors) {
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        mine[v * V + e] = dw[c][e];
-                        mine[p.width + v * V + e] = db[c][e];
+                    for (int i = 0; i < N; ++i) {
+                        store_unit(mine + v * V + W * i, dw[c][i]);
+                        store_unit(mine + p.width + v * V + W * i, db[c][i]);
                     }
                 }
             }

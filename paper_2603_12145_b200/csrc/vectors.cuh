@@ -4,9 +4,13 @@
 
 #include <cstdint>
 
+#include <type_traits>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+
+#include "ssm_common.cuh"
 
 namespace {
 
@@ -112,5 +116,91 @@ __device__ __forceinline__ Packed<T, V> packed_of(const float (&f)[V])
     }
     return v;
 }
+
+// ---- values of one element, or of a pair that one instruction works on
+
+using ssm_k::add;
+using ssm_k::ex2;
+using ssm_k::fma;
+using ssm_k::hi;
+using ssm_k::lo;
+using ssm_k::mul;
+using ssm_k::Pair;
+using ssm_k::pair;
+using ssm_k::rcp;
+
+template <int V>
+using Vals = std::conditional_t<V == 1, float, Pair>;
+
+__device__ __forceinline__ float add(float a, float b) { return __fadd_rn(a, b); }
+__device__ __forceinline__ float mul(float a, float b) { return __fmul_rn(a, b); }
+__device__ __forceinline__ float fma(float a, float b, float c) { return fmaf(a, b, c); }
+
+template <int V>
+__device__ __forceinline__ Vals<V> all(float v)
+{
+    if constexpr (V == 1)
+        return v;
+    else
+        return pair(v, v);
+}
+
+// f on each channel
+template <typename F>
+__device__ __forceinline__ float each(F f, float a) { return f(a); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a) { return pair(f(lo(a)), f(hi(a))); }
+template <typename F>
+__device__ __forceinline__ float each(F f, float a, float b) { return f(a, b); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a, Pair b) { return pair(f(lo(a), lo(b)), f(hi(a), hi(b))); }
+template <typename F>
+__device__ __forceinline__ float each(F f, float a, float b, float c) { return f(a, b, c); }
+template <typename F>
+__device__ __forceinline__ Pair each(F f, Pair a, Pair b, Pair c) { return pair(f(lo(a), lo(b), lo(c)), f(hi(a), hi(b), hi(c))); }
+
+template <typename T>
+__device__ __forceinline__ float widen(const Packed<T, 1> &v) { return packed_get<T, 1>(v, 0); }
+template <typename T>
+__device__ __forceinline__ Pair widen(const Packed<T, 2> &v) { return pair(packed_get<T, 2>(v, 0), packed_get<T, 2>(v, 1)); }
+
+template <typename T>
+__device__ __forceinline__ Packed<T, 1> narrow(float v)
+{
+    const float f[1] = {v};
+    return packed_of<T, 1>(f);
+}
+template <typename T>
+__device__ __forceinline__ Packed<T, 2> narrow(Pair v)
+{
+    const float f[2] = {lo(v), hi(v)};
+    return packed_of<T, 2>(f);
+}
+
+// Of V elements, the i-th pair (of one, the element itself).
+template <typename T, int V>
+__device__ __forceinline__ Vals<V == 1 ? 1 : 2> widen_at(const Packed<T, V> &v, int i)
+{
+    if constexpr (V == 1)
+        return packed_get<T, 1>(v, 0);
+    else
+        return pair(packed_get<T, V>(v, 2 * i), packed_get<T, V>(v, 2 * i + 1));
+}
+
+template <typename T>
+__device__ __forceinline__ void narrow_at(Packed<T, 1> &v, int, float f) { v = narrow<T>(f); }
+template <typename T, int V>
+__device__ __forceinline__ void narrow_at(Packed<T, V> &v, int i, Pair f)
+{
+    if constexpr (sizeof(T) == 4) {
+        v.w[2 * i] = __float_as_uint(lo(f));
+        v.w[2 * i + 1] = __float_as_uint(hi(f));
+    } else {
+        v.w[i] = pack_halves<T>(lo(f), hi(f));
+    }
+}
+
+__device__ __forceinline__ float sum_of(float v) { return v; }
+__device__ __forceinline__ float sum_of(Pair v) { return lo(v) + hi(v); }
 
 }  // namespace
