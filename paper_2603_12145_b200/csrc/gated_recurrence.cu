@@ -26,6 +26,8 @@
 
 namespace {
 
+using namespace vals;
+
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int kSteps = 8;                // steps of a tile, forward

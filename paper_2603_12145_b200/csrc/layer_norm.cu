@@ -20,6 +20,8 @@
 
 namespace {
 
+using namespace vals;
+
 constexpr int kNarrowThreads = 128;      // block of the kernels whose rows belong to lanes of a warp
 constexpr int kMost = 512;               // threads that share a wide row, at most
 
@@ -203,7 +205,7 @@ k_forward(const Forward<T> p)
 }
 
 template <typename T, int V, int C, bool kWide>
-__global__ void __launch_bounds__(kWide ? kMost : kNarrowThreads)
+__global__ void __launch_bounds__(kWide && !(V == 8 && C == 3) ? kMost : kNarrowThreads)
 k_backward(const Backward<T> p)
 {
     extern __shared__ float s_part[];                      // narrow rows: [warps][2][width], the sums of a warp's row groups
@@ -240,6 +242,25 @@ k_backward(const Backward<T> p)
         }
     };
     fetch(first);
+    // A wide row's weights take a third of the accesses if every row fetches them: in registers where there is room (8,192 x
+    // 8,192 in bfloat16 99 against 131 us).
+    constexpr bool kHeld = kWide && sizeof(T) == 2 && V > 1;
+    U held[kHeld ? C : 1][N];
+    if constexpr (kHeld) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int v = c * team.size + team.index;
+            load_params<V>(held[c], p.w != nullptr && v < vectors ? p.w + v * V : nullptr, 1.0f);
+        }
+    }
+    auto weights = [&](U (&w)[N], int c, int v) {
+        if constexpr (kHeld) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = held[c][i];
+        } else {
+            load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+        }
+    };
     for (int64_t row = first; row - (kWide ? 0 : (threadIdx.x & 31) / p.lanes) < p.n; row += step) {
         const bool live = row < p.n;
         Packed<T, V> s[C], dy[C], d[C];
@@ -258,7 +279,7 @@ k_backward(const Backward<T> p)
             const int v = c * team.size + team.index;
             if (v < vectors) {
                 U w[N];
-                load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+                weights(w, c, v);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const U z = mul(add(widen_at(s[c], i), all<W>(-mean)), q), g = widen_at(dy[c], i), h = mul(g, w[i]);
@@ -276,7 +297,7 @@ k_backward(const Backward<T> p)
             const int v = c * team.size + team.index;
             if (v < vectors && live) {
                 U w[N];
-                load_params<V>(w, p.w != nullptr ? p.w + v * V : nullptr, 1.0f);
+                weights(w, c, v);
                 Packed<T, V> out;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
@@ -378,21 +399,22 @@ struct Share {
     bool wide;
 };
 
-// Vectors of 16 bytes: up to four per lane of a warp, then up to three (four, where that is not enough) per thread of a
-// block.  Single elements: up to 8 per lane, then up to 8 (16) per thread.
-Share share_of(int vectors, bool whole)
+// Vectors of 16 bytes: up to four per lane of a warp; then, per thread of a block, up to two of eight elements (three in blocks
+// of up to 128 threads, which have the registers) or four of four.  Single elements: up to 8 per lane, then up to 8 (16 in the
+// largest blocks).
+Share share_of(int vectors, int V)
 {
     Share s = {4, 1, false};
-    while (s.lanes < 32 && s.lanes * (whole ? 2 : 4) < vectors) s.lanes *= 2;
-    if (vectors > s.lanes * (whole ? 4 : 8)) {
+    while (s.lanes < 32 && s.lanes * (V > 1 ? 2 : 4) < vectors) s.lanes *= 2;
+    if (vectors > s.lanes * (V > 1 ? 4 : 8)) {
         s.wide = true;
         s.lanes = 64;
-        while (s.lanes < kMost && s.lanes * (whole ? 3 : 8) < vectors) s.lanes *= 2;
+        while (s.lanes < kMost && s.lanes * (V == 1 ? 8 : V == 4 ? 4 : s.lanes <= kNarrowThreads ? 3 : 2) < vectors) s.lanes *= 2;
     }
     s.count = static_cast<int>(div_up(vectors, s.lanes));
     return s;
 }
-static_assert(kMost * 16 >= LAYER_NORM_MAX_WIDTH && kMost * 3 * 8 >= LAYER_NORM_MAX_WIDTH && kMost * 4 * 4 >= LAYER_NORM_MAX_WIDTH,
+static_assert(kMost * 16 >= LAYER_NORM_MAX_WIDTH && kMost * 2 * 8 >= LAYER_NORM_MAX_WIDTH && kMost * 4 * 4 >= LAYER_NORM_MAX_WIDTH,
               "the widest row: single elements, vectors of 8, vectors of 4");
 
 template <int N>
@@ -405,10 +427,10 @@ bool with_counts(const Share &s, bool whole, F f)
     using V = Count<16 / sizeof(T)>;
     using One = Count<1>;
     if (whole && s.wide) {
-        if (s.count <= 2) return f(V{}, Count<2>{}, std::true_type{});
         if constexpr (sizeof(T) == 4)
-            if (s.count == 4) return f(V{}, Count<4>{}, std::true_type{});
-        return f(V{}, Count<3>{}, std::true_type{});
+            return s.count <= 3 ? f(V{}, Count<3>{}, std::true_type{}) : f(V{}, Count<4>{}, std::true_type{});
+        else
+            return s.count <= 2 ? f(V{}, Count<2>{}, std::true_type{}) : f(V{}, Count<3>{}, std::true_type{});
     }
     if (whole) {
         if (s.count <= 1) return f(V{}, Count<1>{}, std::false_type{});
@@ -444,7 +466,7 @@ namespace {
 Share share_for(const layer_norm *p, bool whole)
 {
     const int V = 16 / element_bytes(p->type);
-    return share_of(whole ? p->width / V : p->width, whole);
+    return whole ? share_of(p->width / V, V) : share_of(p->width, 1);
 }
 
 size_t backward_smem(const layer_norm *p, const Share &s) { return s.wide ? 0 : kNarrowThreads / 32 * 2 * sizeof(float) * p->width; }

@@ -117,7 +117,10 @@ __device__ __forceinline__ Packed<T, V> packed_of(const float (&f)[V])
     return v;
 }
 
-// ---- values of one element, or of a pair that one instruction works on
+// ---- values of one element, or of a pair that one instruction works on.  (In a namespace of their own: among the names of
+// the file that includes this, fma and its like would hide those of binary64.)
+
+namespace vals {
 
 using ssm_k::add;
 using ssm_k::ex2;
@@ -203,4 +206,5 @@ __device__ __forceinline__ void narrow_at(Packed<T, V> &v, int i, Pair f)
 __device__ __forceinline__ float sum_of(float v) { return v; }
 __device__ __forceinline__ float sum_of(Pair v) { return lo(v) + hi(v); }
 
+}  // namespace vals
 }  // namespace

@@ -129,7 +129,8 @@ class GatedRecurrence:
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         self._on = None                   # the stream that the handle was last given
-        self._sizes = {}
+        self._sizes = {}                  # bytes of saved and workspaces by shape
+        self._f32 = torch.empty(0, dtype=torch.float32, device=self.device)     # what new buffers are like
         with torch.cuda.device(self.device):
             self.h = gated_recurrence_create(self.channels, types[self.dtype])
 
@@ -191,14 +192,11 @@ class GatedRecurrence:
             return self.torch.empty((t, b, self.channels), dtype=self.dtype, device=self.device).transpose(0, 1)
         return out
 
-    def _f32(self, *shape):
-        return self.torch.empty(shape, dtype=self.torch.float32, device=self.device)
-
     # -- buffers
 
     def state(self, n: int):
         """Buffer for the recurrent state, float32 [n, channels]."""
-        return self._f32(n, self.channels)
+        return self._f32.new_empty((n, self.channels))
 
     def _size(self, batch, time, what):
         """Bytes of `saved` ("saved"), of the forward (0) and of the backward workspace (1)."""
@@ -212,7 +210,7 @@ class GatedRecurrence:
 
     def saved(self, batch: int, time: int):
         """Buffer in which sequence() leaves what backward() needs."""
-        return self._f32(self._size(batch, time, "saved") // 4)
+        return self._f32.new_empty(self._size(batch, time, "saved") // 4)
 
     # -- sequences
 
@@ -241,7 +239,7 @@ class GatedRecurrence:
             out = self._like(x)
         states = (n, self.channels)
         size = self._size(n, t, 0)
-        scratch = self.torch.empty((size,), dtype=self.torch.uint8, device=self.device) if size else None
+        scratch = self._f32.new_empty(size // 4) if size else None
         self._stream()
         self._call(self._lib.gated_recurrence_forward, "gated_recurrence_forward", *first,
                    0 if state is None else self._dense("state", state, states),
@@ -259,7 +257,7 @@ class GatedRecurrence:
         dx, dr, di, da = self._like(x), self._like(r), self._like(i), self.torch.empty_like(a)
         dstate = self.state(n) if want_dstate else None
         size = self._size(n, t, 1)
-        scratch = self.torch.empty((size,), dtype=self.torch.uint8, device=self.device) if size else None
+        scratch = self._f32.new_empty(size // 4) if size else None
         self._stream()
         self._call(self._lib.gated_recurrence_backward, "gated_recurrence_backward", *first, 0, 0, *_NONE,
                    self._dense("saved", saved, (self._size(n, t, "saved") // 4,)), *self._seq("dy", dy, shape),

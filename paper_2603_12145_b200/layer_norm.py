@@ -106,6 +106,7 @@ class LayerNorm:
         self._lib = load()
         self._on = None                   # the stream that the handle was last given
         self._sizes = {}                  # workspace bytes by rows
+        self._f32 = torch.empty(0, dtype=torch.float32, device=self.device)     # what new buffers are like
         with torch.cuda.device(self.device):
             self.h = layer_norm_create(self.width, self.eps, types[self.dtype])
 
@@ -161,7 +162,7 @@ class LayerNorm:
 
     def saved(self, n: int):
         """Buffer in which forward() leaves what backward() needs: float32 [n, 2]."""
-        return self.torch.empty((n, 2), dtype=self.torch.float32, device=self.device)
+        return self._f32.new_empty((n, 2))
 
     def forward(self, x, w=None, b=None, residual=None, saved=None, out=None, total=None):
         """The normalised rows; with a residual (rows, total): total = x + residual is the stream as it goes on, and
@@ -215,14 +216,13 @@ class LayerNorm:
         dw = db = scratch = None
         size = 0
         if want_params:
-            t = self.torch
-            dw, db = (t.empty((width,), dtype=t.float32, device=self.device) if w is None else t.empty_like(w) for _ in range(2))
+            dw, db = self._f32.new_empty(width), self._f32.new_empty(width)
             if n not in self._sizes:
                 if len(self._sizes) > 1000:
                     self._sizes.clear()
                 self._sizes[n] = self._lib.layer_norm_workspace_bytes(self.h, n)
             size = self._sizes[n]
-            scratch = t.empty((size,), dtype=t.uint8, device=self.device)
+            scratch = self._f32.new_empty(size // 4)
         self._stream()
         code = self._lib.layer_norm_backward(
             self.h, dy.data_ptr(), sy[0], s.data_ptr(), ss[0], pw, kept, None if dsum is None else dsum.data_ptr(), sd[0],

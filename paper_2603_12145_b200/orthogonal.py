@@ -111,6 +111,7 @@ class Orthogonal:
             lambda index: torch.cuda.current_stream(index).cuda_stream)
         self._lib = load()
         self._on = None                   # the stream that the handle was last given
+        self._f32 = torch.empty(0, dtype=torch.float32, device=self.device)     # what new buffers are like
         with torch.cuda.device(self.device):
             self.h = orthogonal_create(self.rows, self.cols, self.steps, a, b, c, self.eps, types[self.dtype])
 
@@ -156,7 +157,7 @@ class Orthogonal:
             out = t.empty(shape, dtype=t.bfloat16, device=self.device)
         po, ob, orow = self._matrices("out", out, t.bfloat16, shape)
         size = self._lib.orthogonal_workspace_bytes(self.h, batch)
-        scratch = t.empty((size,), dtype=t.uint8, device=self.device) if size else None
+        scratch = self._f32.new_empty(size // 4) if size else None
         self._stream()
         code = self._lib.orthogonal_update(self.h, pg, gb, gr, po, ob, orow, None if scratch is None else scratch.data_ptr(),
                                            size, batch)
