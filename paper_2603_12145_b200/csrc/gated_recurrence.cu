@@ -116,11 +116,11 @@ __device__ __forceinline__ F square_gain(F d)
     return fma(minus, d, add(minus, minus));
 }
 
-// 1 / sqrt(square); zero where nothing is left of it (a NaN passes)
+// 1 / sqrt(square); zero where nothing is left of it.  (A NaN passes, and the negative square of a growing state gives one.)
 template <typename F>
 __device__ __forceinline__ F inverse_root(F square)
 {
-    return each([](float s) { return s < 1.2e-38f ? 0.0f : rsq(s); }, square);
+    return each([](float s) { return fabsf(s) < 1.2e-38f ? 0.0f : rsq(s); }, square);
 }
 
 // The state after a step: gates and input of the step, the state before it.

@@ -271,6 +271,24 @@ def test_extreme_gates(torch):
     assert (y[(r[:, 0, 0] > 10) & (i[:, 0, 0] > 50)][:, :, 5] == 1.0).all()    # all decays, all enters
 
 
+@pytest.mark.parametrize("batch,time", [(1, 1), (2, 40), (1, 2000)])
+def test_a_positive_rate_gives_nan_in_its_channel(torch, batch, time):
+    op = gated_recurrence.GatedRecurrence(6, dtype=torch.float32)
+    a = torch.tensor([-0.5, 0.5, -1.0, 30.0, 1e-3, -2.0], device="cuda")
+    x = torch.ones((batch, time, 6), device="cuda")
+    gate = torch.zeros_like(x)
+    saved, last = op.saved(batch, time), op.state(batch)
+    y = op.sequence(x, gate, gate, a, state_out=last, saved=saved)
+    bad = a > 0
+    g = op.backward(x, x, gate, gate, a, saved)
+    for v in (y, last, g["dx"], g["dr"], g["di"], g["da"]):
+        assert torch.isnan(v[..., bad]).all() and torch.isfinite(v[..., ~bad]).all()
+    state = torch.zeros((batch, 6), device="cuda")
+    one = op.step(x[:, 0], gate[:, 0], gate[:, 0], a, state)
+    for v in (one, state):
+        assert torch.isnan(v[..., bad]).all() and torch.isfinite(v[..., ~bad]).all()
+
+
 def test_long_rows_beyond_32_bit_offsets(torch):
     batch, time, ch = 2, 3, 64
     stride = 2 ** 30 + 6
