@@ -759,6 +759,20 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
 
 // ---- the norm, and the first X
 
+// 2^13 / (|G| + eps) as two factors: of a very small matrix it is beyond binary32, and the first, a power of two, is then
+// taken ahead.
+struct Factor {
+    float first, second;
+    __device__ __forceinline__ Factor(double squares, double eps)
+    {
+        const double whole = static_cast<double>(kScale) / (sqrt(squares) + eps);
+        const bool large = whole > 0x1p100;
+        first = large ? 0x1p100f : 1.0f;
+        second = static_cast<float>(large ? whole * 0x1p-100 : whole);
+    }
+    __device__ __forceinline__ float of(float v) const { return v * first * second; }
+};
+
 struct Start {
     int rows, cols, ld;
     int parts;               // blocks per matrix
@@ -841,15 +855,15 @@ k_start(const Start s, const T *g)
     double sum = 0.0;
     for (int i = threadIdx.x; i < s.parts; i += kRowThreads) sum += s.squares[z * s.parts + i];
     sum = block_sum(sum);
-    const float factor = static_cast<float>(static_cast<double>(kScale) / (sqrt(sum) + s.eps));
+    const Factor factor(sum, s.eps);
     each_piece(s, part, [&](int64_t row, int c) {
         float v[8];
         load8<T>(v, g + z * s.g_batch + row * s.g_row, c, s.cols, s.whole);
         uint32_t hw[4], lw[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            v[2 * e] *= factor;
-            v[2 * e + 1] *= factor;
+            v[2 * e] = factor.of(v[2 * e]);
+            v[2 * e + 1] = factor.of(v[2 * e + 1]);
             hw[e] = pack2(v[2 * e], v[2 * e + 1]);
             const float2 h = unpack2(hw[e]);
             lw[e] = pack2(v[2 * e] - h.x, v[2 * e + 1] - h.y);
@@ -1061,14 +1075,14 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         sum = 0.0;
         for (uint32_t i = 0; i < blocks; ++i) sum += sums[kSmallWarps + i];
     }
-    const float factor = static_cast<float>(static_cast<double>(kScale) / (sqrt(sum) + p.eps));
+    const Factor factor(sum, p.eps);
     for (int i = threadIdx.x; i < p.boxes * S::kBox / 16; i += kSmallThreads) {
         const uint4 up = get_piece(hi0 + 16 * i), low = get_piece(lo0 + 16 * i);
         const uint32_t h[4] = {up.x, up.y, up.z, up.w}, l[4] = {low.x, low.y, low.z, low.w};
         uint32_t hw[4], lw[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float x = __uint_as_float(__byte_perm(l[j], h[j], 0x5410)) * factor, y = __uint_as_float(__byte_perm(l[j], h[j], 0x7632)) * factor;
+            const float x = factor.of(__uint_as_float(__byte_perm(l[j], h[j], 0x5410))), y = factor.of(__uint_as_float(__byte_perm(l[j], h[j], 0x7632)));
             hw[j] = pack2(x, y);
             const float2 f = unpack2(hw[j]);
             lw[j] = pack2(x - f.x, y - f.y);

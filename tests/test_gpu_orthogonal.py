@@ -206,6 +206,38 @@ def test_two_handles_side_stream_and_graph(torch):
     b.status()
 
 
+def test_two_streams_at_once(torch):
+    """Updates that take the whole device, on two streams without an order between them."""
+    sizes = ((1728, 576), (1024, 2048), (300, 300), (64, 700))
+    ops = [orthogonal.Orthogonal(m, n) for m, n in sizes]
+    gs = [matrices(torch, 20 + i, 1, m, n, "bfloat16", 8, 0.3)[0] for i, (m, n) in enumerate(sizes)]
+    want = [op.update(g) for op, g in zip(ops, gs)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(w) for w in want] for _ in range(6)]
+    torch.cuda.synchronize()
+    for k, out in enumerate(outs):
+        for i, op in enumerate(ops):
+            with torch.cuda.stream(streams[(i + k) % 2]):
+                op.update(gs[i], out=out[i])
+    torch.cuda.synchronize()
+    for op in ops:
+        op.status()
+    for out in outs:
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("rows,cols", [(100, 60), (200, 300)])
+def test_least_eps(torch, rows, cols):
+    """Norms whose inverse is beyond binary32: no zero times infinity."""
+    op = orthogonal.Orthogonal(rows, cols, dtype=torch.float32, eps=2.0 ** -149)
+    assert (op.update(torch.zeros(rows, cols, device="cuda")) == 0).all()
+    g = matrices(torch, 4, 1, rows, cols, "float32")[0]
+    want = tr.orthogonal(f64(g))
+    assert error(op.update(g), want) <= BOUND
+    small = g * 2.0 ** -124                       # some are subnormal: taken as they are
+    assert error(op.update(small), tr.orthogonal(f64(small), eps=2.0 ** -149)) <= BOUND
+
+
 def test_refusals(torch):
     op = orthogonal.Orthogonal(40, 60)
     g = matrices(torch, 1, 2, 40, 60, "bfloat16")
