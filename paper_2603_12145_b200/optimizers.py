@@ -25,9 +25,17 @@ class OrthogonalMomentum(torch.optim.Optimizer):
         super().__init__(params, dict(lr=lr, momentum=momentum, nesterov=nesterov, weight_decay=weight_decay, steps=steps))
         self._ops = {}
 
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self.__dict__.setdefault("_ops", {})       # a copy has handles of its own
+
     def add_param_group(self, group):
         super().add_param_group(group)
-        for p in self.param_groups[-1]["params"]:
+        params = self.param_groups[-1]["params"]
+        if len(set(map(id, params))) != len(params):
+            self.param_groups.pop()
+            raise ValueError("a parameter appears twice")
+        for p in params:
             if p.dim() != 2 or p.dtype is not torch.float32:
                 self.param_groups.pop()
                 raise ValueError("parameters must be float32 matrices, got %s %s" % (p.dtype, tuple(p.shape)))

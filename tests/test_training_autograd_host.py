@@ -1,5 +1,9 @@
 """What autograd sees of the training operators: the Functions of ssm_policy around stand-ins for the handles (plain torch on
 the CPU), and the optimiser around one for the products; without a GPU."""
+import copy
+import pickle
+import warnings
+
 import pytest
 import torch
 
@@ -154,3 +158,25 @@ def test_orthogonal_momentum_is_its_formula(monkeypatch):
             optimizers.OrthogonalMomentum(bad)
     with pytest.raises(ValueError):
         optimizers.OrthogonalMomentum(p, momentum=1.0)
+
+
+def test_orthogonal_momentum_is_copied_and_takes_no_parameter_twice(monkeypatch):
+    class Whole:
+        def __init__(self, *args, **kw):
+            pass
+
+        def update(self, g):
+            return g.to(torch.bfloat16)
+
+    monkeypatch.setattr(optimizers.orthogonal, "Orthogonal", Whole)
+    p = torch.nn.Parameter(torch.ones(4, 4))
+    opt = optimizers.OrthogonalMomentum([p], lr=0.5, momentum=0.0)
+    for o in (opt, copy.deepcopy(opt), pickle.loads(pickle.dumps(opt))):
+        q = o.param_groups[0]["params"][0]
+        q.grad = torch.ones(4, 4)
+        o.step()
+        assert (q == 0.5).all()
+    with warnings.catch_warnings():
+        warnings.simplefilter("ignore")                # the base class warns
+        with pytest.raises(ValueError):
+            optimizers.OrthogonalMomentum([p, p])
