@@ -142,6 +142,34 @@ def test_forward_and_backward(torch, case):
     assert all(torch.equal(p, q) for p, q in zip(again, (dx, dw, db)))
 
 
+# The widths at which the share of a thread changes: whole rounds of a warp with a rest by twos and fours, up to three
+# vectors per lane (of binary32 four), blocks of 64 threads and more.
+EDGES = [
+    (37, 264, "bfloat16"), (37, 320, "float16"), (45, 384, "bfloat16"), (300, 576, "float16"), (41, 640, "bfloat16"),
+    (40, 768, "bfloat16"), (23, 776, "bfloat16"), (23, 832, "float16"), (19, 1536, "bfloat16"), (19, 1544, "float16"),
+    (11, 4096, "bfloat16"), (9, 4104, "float16"), (31, 256, "float32"), (31, 260, "float32"), (29, 384, "float32"),
+    (29, 388, "float32"), (27, 516, "float32"), (17, 1028, "float32"), (13, 2052, "float32"), (7, 4100, "float32"),
+    (33, 128, "float32"), (21, 129, "bfloat16"), (15, 513, "float32"), (12, 2049, "float16"), (9, 4097, "bfloat16"),
+]
+
+
+@pytest.mark.parametrize("case", EDGES, ids=str)
+def test_widths_between_shares(torch, case):
+    n, width, dtype = case
+    op = layer_norm.LayerNorm(width, eps=1e-5, dtype=getattr(torch, dtype))
+    x, r = make(torch, 1, n, width, dtype), make(torch, 2, n, width, dtype, offset=-0.5)
+    dy, dsum = make(torch, 3, n, width, dtype, offset=0.0), make(torch, 4, n, width, dtype, offset=0.0)
+    w, b = make(torch, 5, 1, width, "float32")[0], make(torch, 6, 1, width, "float32")[0]
+    saved = op.saved(n)
+    y, total = op.forward(x, w, b, residual=r, saved=saved)
+    assert torch.equal(total, x + r)
+    check_forward(f64(total), y, f64(w), f64(b), 1e-5, dtype)
+    dx, dw, db = op.backward(dy, total, w, saved, dsum=dsum)
+    check_backward(f64(total), f64(dy), f64(w), f64(dsum), 1e-5, dtype, dx, dw, db)
+    alone = op.backward(dy, total, w, saved, dsum=dsum, want_params=False)
+    assert torch.equal(alone[0], dx)
+
+
 def test_large_offset_and_constant_rows(torch):
     """Rows far from zero lose nothing to cancellation beyond the mean's rounding; a constant row is all b."""
     op = layer_norm.LayerNorm(576, dtype=torch.float32)
