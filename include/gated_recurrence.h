@@ -18,7 +18,8 @@
  *     dstate = e^(L_0) g_0
  *
  * a = 0 (and a gate that vanishes in binary32) means no decay and no input; the derivative by the rate has no limit there
- * and counts as zero.  A positive a gives NaN.
+ * and counts as zero.  A positive a gives NaN.  A state that has become infinite stays so until a reset; gradients of
+ * steps that meet one are not finite.
  *
  * Types.  x, r, i, y, dy and their gradients are of the handle's type (binary32, bfloat16, binary16).  a, the states and
  * their gradients are binary32, as is all arithmetic; a result is rounded once when it is stored.  The decay enters as
@@ -26,10 +27,11 @@
  * order: the same call gives the same bits.  Sequence and single-token forms go through the same states.
  *
  * Sequences are described by gated_recurrence_seq: element (n, t, c) of a [batch][time][channels] array is
- * ptr[n * stride_b + t * stride_t + c], strides in elements.  A time-major rollout [time][batch][channels] is the same
- * array with the strides exchanged; a column range of a wider projection is one with a larger stride_t.  Pointers are
- * DEVICE pointers owned by the caller, aligned to their element.  Inputs must not overlap outputs, except that a step may
- * update its state in place.  Outputs whose rows would share memory are refused.
+ * ptr[n * stride_b + t * stride_t + c], strides in elements; batch and time are at least 1.  A time-major rollout
+ * [time][batch][channels] is the same array with the strides exchanged; a column range of a wider projection is one with a
+ * larger stride_t.  Pointers are DEVICE pointers owned by the caller, aligned to their element.  Outputs must overlap neither
+ * inputs nor one another, except that a step may update its state in place.  Outputs whose rows would share memory are
+ * refused.
  *
  * Calls enqueue on the handle's stream, on the device that was current when the handle was created (whichever is
  * current now stays so), and return; nothing is allocated but the handle.  A handle is not thread-safe (its stream is

@@ -1,15 +1,19 @@
 // layer_norm.cu -- the layer norm of a residual stream behind the C ABI of layer_norm.h.
 //
 // A row stays in the registers of the threads that share it, as the words it was loaded in: the sum, the mean, the
-// variance (from differences to the mean) and the result come from one reading of memory.  A row of up to 128 vectors of
-// 16 bytes belongs to 4 to 32 lanes of a warp, which reduce by shuffles; a wider one to a block, whose warps exchange
-// their sums through shared memory with one barrier per reduction (two alternating slots).  Each thread holds its
-// vectors index lane, lane + R, ... of the R threads, so that a warp's access is contiguous.
+// variance (from differences to the mean) and the result come from one reading of memory.  A row of up to 96 vectors of
+// 16 bytes (binary32: 128) belongs to 4 to 32 lanes of a warp, which reduce by shuffles; a wider one to a block, whose warps
+// exchange their sums through shared memory with one barrier per reduction (two alternating slots).  Of R threads each holds
+// the vectors index, index + R, ..., so that a warp's access is contiguous.  Blocks go through several rows, as many as fit on
+// the device at once, and the next row's loads are in flight while a row is reduced.
 //
-// The backward kernel keeps dw and db of its thread's columns in registers over all its rows; a block's row groups are
-// added in shared memory, blocks leave a row of sums each and k_join adds them, all in a fixed order.
+// The backward kernel keeps dw and db of its thread's columns in registers over all its rows: per row only the two sums of dx
+// cross threads.  The row groups of a warp are added by exchanges, a block's warps in shared memory, blocks leave a row of
+// sums each and k_join adds them, all in a fixed order.
 //
-// Both are bound by memory; the next row's loads are in flight while a row is reduced.
+// What bounds them: memory, and issue close behind it.  In bfloat16 on a B200, 65,536 x 576 with residual takes 54 us forward
+// (302 MB, 5.6 TB/s) and 59 us backward (5.1 TB/s), 8,192 x 8,192 without takes 70 us (3.8 TB/s: two barriers per row) and 89
+// us (4.5 TB/s); 64 rows take 5 us on the device, less than the call on the host.
 #include <cmath>
 #include <new>
 #include <type_traits>
@@ -22,6 +26,8 @@ namespace {
 
 using namespace vals;
 
+// Who shares a row: lanes of a warp, a block of up to 256 threads, a block of kMost.
+enum Form { kLanes, kBlock, kLargest };
 constexpr int kNarrowThreads = 128;      // block of the kernels whose rows belong to lanes of a warp
 constexpr int kMost = 512;               // threads that share a wide row, at most
 
@@ -127,8 +133,8 @@ __device__ __forceinline__ void store_unit(float *dst, float v) { *dst = v; }
 __device__ __forceinline__ void store_unit(float *dst, Pair v) { *reinterpret_cast<float2 *>(dst) = make_float2(lo(v), hi(v)); }
 
 // A thread's share of a row: C accesses of V elements, index, index + size, ... of the row's `vectors`, and R elements of the rest
-// behind C * size vectors.
-template <typename T, int V, int C, int R>
+// behind C * size vectors.  kAll: every thread has all of its accesses.
+template <typename T, int V, int C, int R, bool kAll>
 struct Mine {
     static constexpr int W = V == 1 ? 1 : 2, N = (V + 1) / 2, kUnits = C * N + R / 2;
     using Unit = Vals<W>;
@@ -161,18 +167,19 @@ struct Mine {
     __device__ __forceinline__ void each_access(F f) const
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) f(c * N, std::integral_constant<int, N>{}, (c * size + index) * V, c * size + index < vectors);
+        for (int c = 0; c < C; ++c) f(c * N, std::integral_constant<int, N>{}, (c * size + index) * V, kAll || c * size + index < vectors);
         if constexpr (R > 0) f(C * N, std::integral_constant<int, R / 2>{}, C * size * V + index * R, true);
     }
-    __device__ __forceinline__ Words load(const T *row, bool live) const
+    // zeros where there is nothing
+    __device__ __forceinline__ Words load(const T *row) const
     {
         Words w;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int i = c * size + index;
-            w.v[c] = live && i < vectors ? packed_load<T, V>(row + i * V) : packed_zero<T, V>();
+            w.v[c] = kAll || i < vectors ? packed_load<T, V>(row + i * V) : packed_zero<T, V>();
         }
-        if constexpr (R > 0) w.rest = live ? packed_load<T, R>(row + C * size * V + index * R) : packed_zero<T, R>();
+        if constexpr (R > 0) w.rest = packed_load<T, R>(row + C * size * V + index * R);
         return w;
     }
     __device__ __forceinline__ void store(T *row, const Words &w) const
@@ -180,7 +187,7 @@ struct Mine {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int i = c * size + index;
-            if (i < vectors) packed_store<T, V>(row + i * V, w.v[c]);
+            if (kAll || i < vectors) packed_store<T, V>(row + i * V, w.v[c]);
         }
         if constexpr (R > 0) packed_store<T, R>(row + C * size * V + index * R, w.rest);
     }
@@ -199,11 +206,14 @@ struct Turns {
     }
 };
 
-template <typename T, int V, int C, int R, bool kWide>
-__global__ void __launch_bounds__(kWide ? kMost : kNarrowThreads)
+// (blocks of 512 threads: two of them on an SM, 8,192 x 8,192 in bfloat16 70 against 80 us; smaller ones lose by the cap on
+// registers, 16,384 x 4,096 92 against 87)
+template <typename T, int V, int C, int R, Form kForm, bool kAll>
+__global__ void __launch_bounds__(kForm == kLargest ? kMost : kForm == kBlock ? kMost / 2 : kNarrowThreads, kForm == kLargest && V == 8 ? 2 : 0)
 k_forward(const Forward<T> p)
 {
-    using M = Mine<T, V, C, R>;
+    constexpr bool kWide = kForm != kLanes;
+    using M = Mine<T, V, C, R, kAll>;
     using U = typename M::Unit;
     constexpr int W = M::W;
     __shared__ float2 s_sum[kWide ? 2 * (kMost / 32) : 1];
@@ -216,11 +226,28 @@ k_forward(const Forward<T> p)
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.residual.ptr != nullptr;
     typename M::Words nx, nr;
-    auto fetch = [&](int64_t row) {
-        nx = mine.load(p.x.row(row), row < p.n);
-        if (added) nr = mine.load(p.residual.row(row), row < p.n);
+    auto fetch = [&](int64_t row) {          // behind the last row that one again: no zeros to be put in place
+        row = row < p.n ? row : p.n - 1;
+        nx = mine.load(p.x.row(row));
+        if (added) nr = mine.load(p.residual.row(row));
     };
     fetch(turns.first);
+    // The parameters of up to 18 elements stay in registers (bfloat16, no residual: 65,536 x 256 14.7 against 18.7 us, x 512
+    // 26.3 against 30.8); of more they cost warps (binary32, 65,536 x 384 39 against 37; 8,192 x 8,192 in bfloat16 103 against 89).
+    constexpr bool kHeld = !kWide && V > 1 && C * V + R <= 18;
+    U held_w[kHeld ? M::kUnits : 1], held_b[kHeld ? M::kUnits : 1];
+    if constexpr (kHeld) {
+        mine.each_access([&](int u0, auto n, int at, bool in) {
+            U w[n.value], b[n.value];
+            load_params<W>(w, p.w != nullptr && in ? p.w + at : nullptr, 1.0f);
+            load_params<W>(b, p.b != nullptr && in ? p.b + at : nullptr, 0.0f);
+#pragma unroll
+            for (int i = 0; i < n.value; ++i) {
+                held_w[u0 + i] = w[i];
+                held_b[u0 + i] = b[i];
+            }
+        });
+    }
     for (int64_t row = turns.first; row - turns.behind < p.n; row += turns.step) {
         const bool live = row < p.n;
         if (added) {
@@ -253,8 +280,16 @@ k_forward(const Forward<T> p)
             if (!in) return;
             Packed<T, W * n.value> out;
             U w[n.value], b[n.value];
-            load_params<W>(w, p.w != nullptr ? p.w + at : nullptr, 1.0f);
-            load_params<W>(b, p.b != nullptr ? p.b + at : nullptr, 0.0f);
+            if constexpr (kHeld) {
+#pragma unroll
+                for (int i = 0; i < n.value; ++i) {
+                    w[i] = held_w[u0 + i];
+                    b[i] = held_b[u0 + i];
+                }
+            } else {
+                load_params<W>(w, p.w != nullptr ? p.w + at : nullptr, 1.0f);
+                load_params<W>(b, p.b != nullptr ? p.b + at : nullptr, 0.0f);
+            }
 #pragma unroll
             for (int i = 0; i < n.value; ++i) narrow_at(out, i, fma(mul(s[u0 + i], all<W>(scale)), w[i], b[i]));
             packed_store<T, W * n.value>(py + at, out);
@@ -262,11 +297,12 @@ k_forward(const Forward<T> p)
     }
 }
 
-template <typename T, int V, int C, int R, bool kWide>
-__global__ void __launch_bounds__(kWide && !(V == 8 && C == 3) ? kMost : kNarrowThreads)
+template <typename T, int V, int C, int R, Form kForm, bool kAll>
+__global__ void __launch_bounds__(kForm == kLanes || (V == 8 && C == 3) ? kNarrowThreads : kForm == kBlock ? kMost / 2 : kMost)
 k_backward(const Backward<T> p)
 {
-    using M = Mine<T, V, C, R>;
+    constexpr bool kWide = kForm != kLanes;
+    using M = Mine<T, V, C, R, kAll>;
     using U = typename M::Unit;
     constexpr int W = M::W;
     extern __shared__ float s_part[];                      // narrow rows: [warps][2][width], the sums of a warp's row groups
@@ -286,15 +322,17 @@ k_backward(const Backward<T> p)
     typename M::Words ns, ndy, nd;
     float2 nstat;
     auto fetch = [&](int64_t row) {
-        nstat = row < p.n ? __ldg(p.saved + row) : make_float2(0.0f, 0.0f);
-        ns = mine.load(p.s.row(row), row < p.n);
-        ndy = mine.load(p.dy.row(row), row < p.n);
-        if (added) nd = mine.load(p.dsum.row(row), row < p.n);
+        row = row < p.n ? row : p.n - 1;
+        nstat = __ldg(p.saved + row);
+        ns = mine.load(p.s.row(row));
+        ndy = mine.load(p.dy.row(row));
+        if (added) nd = mine.load(p.dsum.row(row));
     };
     fetch(turns.first);
-    // A wide row's weights take a third of the accesses if every row fetches them: in registers where there is room (8,192 x
-    // 8,192 in bfloat16 98 against 131 us).
-    constexpr bool kHeld = kWide && sizeof(T) == 2 && V > 1;
+    // The weights take a third of the accesses if every row fetches them: in registers where there is room, that is, not in
+    // blocks for rows of binary32 (bfloat16: 65,536 x 576 61 against 73 us, 8,192 x 8,192 98 against 131; binary32: 32,768 x 512
+    // 49 against 54, but 16,384 x 1,024 75 against 67.)
+    constexpr bool kHeld = V > 1 && (sizeof(T) == 2 || !kWide);
     U held[kHeld ? M::kUnits : 1];
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
@@ -320,7 +358,7 @@ k_backward(const Backward<T> p)
         const U q = all<W>(scale);
         U sum = all<W>(0.0f), along = sum;
         mine.each_access([&](int u0, auto n, int at, bool in) {
-            if (!in) return;
+            if (!in || !live) return;
             U w[n.value];
             weights(w, u0, at);
 #pragma unroll
@@ -388,7 +426,7 @@ k_backward(const Backward<T> p)
     }
 }
 
-// dw and db: a block takes 32 columns of the `rows` rows of sums, eight warps share the rows.
+// dw and db: a block takes 32 columns of the `rows` rows of sums, its warps share the rows.
 constexpr int kJoinWarps = 32;
 
 __global__ void __launch_bounds__(32 * kJoinWarps)
@@ -429,8 +467,9 @@ struct Share {
 };
 
 // Vectors of 16 bytes: up to three (of four elements four) per lane of a warp; then, per thread of a block, up to two of eight
-// elements (three in blocks of up to 128 threads, which have the registers) or four of four.  Single elements: up to 8 per lane, then up to 8 (16 in the
-// largest blocks).
+// elements (three in blocks of up to 128 threads, which have the registers) or four of four.  Single elements: up to 8 per
+// lane, then up to 8 (16 in the largest blocks).  Measured in bfloat16: 32,768 x 1,024 backward 57 us as blocks of 64
+// threads, 74 us as a warp with four vectors per lane.
 Share share_of(int vectors, int V)
 {
     Share s = {4, 1, false, 0};
@@ -455,33 +494,45 @@ static_assert(kMost * 16 >= LAYER_NORM_MAX_WIDTH && kMost * 2 * 8 >= LAYER_NORM_
 template <int N>
 using Count = std::integral_constant<int, N>;
 
-// Calls f with V, C, R and the form of the kernel for this share.
+template <Form kForm>
+using Of = std::integral_constant<Form, kForm>;
+
+// Calls f with V, C, R, the form of the kernel and kAll for this share of a row of `vectors`.  (kAll: bfloat16, 16,384 x 4,096 backward
+// 97 against 104 us.)
 template <typename T, typename F>
-bool with_counts(const Share &s, bool whole, F f)
+bool with_counts(const Share &s, int vectors, bool whole, F f)
 {
     using V = Count<16 / sizeof(T)>;
     using One = Count<1>;
     using None = Count<0>;
-    if (whole && s.wide) {
-        if constexpr (sizeof(T) == 4)
-            return s.count <= 3 ? f(V{}, Count<3>{}, None{}, std::true_type{}) : f(V{}, Count<4>{}, None{}, std::true_type{});
-        else
-            return s.count <= 2 ? f(V{}, Count<2>{}, None{}, std::true_type{}) : f(V{}, Count<3>{}, None{}, std::true_type{});
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const bool largest = s.lanes == kMost;
+    if (!whole) {
+        if (!s.wide) return s.count <= 4 ? f(One{}, Count<4>{}, None{}, Of<kLanes>{}, No{}) : f(One{}, Count<8>{}, None{}, Of<kLanes>{}, No{});
+        if (s.count > 8) return f(One{}, Count<16>{}, None{}, Of<kLargest>{}, No{});
+        return largest ? f(One{}, Count<8>{}, None{}, Of<kLargest>{}, No{}) : f(One{}, Count<8>{}, None{}, Of<kBlock>{}, No{});
     }
-    if (whole) {
-        if constexpr (sizeof(T) == 2) {
-            if (s.rest == 2)
-                return s.count == 1 ? f(V{}, Count<1>{}, Count<2>{}, std::false_type{}) : f(V{}, Count<2>{}, Count<2>{}, std::false_type{});
-            if (s.rest == 4)
-                return s.count == 1 ? f(V{}, Count<1>{}, Count<4>{}, std::false_type{}) : f(V{}, Count<2>{}, Count<4>{}, std::false_type{});
-        } else if (s.count == 4) {
-            return f(V{}, Count<4>{}, None{}, std::false_type{});
+    if constexpr (sizeof(T) == 2) {
+        auto with_rest = [&](auto c) { return s.rest == 2 ? f(V{}, c, Count<2>{}, Of<kLanes>{}, Yes{}) : f(V{}, c, Count<4>{}, Of<kLanes>{}, Yes{}); };
+        if (s.rest > 0) return s.count == 1 ? with_rest(Count<1>{}) : with_rest(Count<2>{});
+    }
+    auto with_count = [&](auto all) {
+        if (s.wide) {
+            if constexpr (sizeof(T) == 4) {
+                if (s.count <= 3) return largest ? f(V{}, Count<3>{}, None{}, Of<kLargest>{}, all) : f(V{}, Count<3>{}, None{}, Of<kBlock>{}, all);
+                return largest ? f(V{}, Count<4>{}, None{}, Of<kLargest>{}, all) : f(V{}, Count<4>{}, None{}, Of<kBlock>{}, all);
+            } else {
+                if (s.count == 3) return f(V{}, Count<3>{}, None{}, Of<kBlock>{}, all);
+                return largest ? f(V{}, Count<2>{}, None{}, Of<kLargest>{}, all) : f(V{}, Count<2>{}, None{}, Of<kBlock>{}, all);
+            }
         }
-        if (s.count <= 1) return f(V{}, Count<1>{}, None{}, std::false_type{});
-        return s.count == 2 ? f(V{}, Count<2>{}, None{}, std::false_type{}) : f(V{}, Count<3>{}, None{}, std::false_type{});
-    }
-    if (s.wide) return s.count <= 8 ? f(One{}, Count<8>{}, None{}, std::true_type{}) : f(One{}, Count<16>{}, None{}, std::true_type{});
-    return s.count <= 4 ? f(One{}, Count<4>{}, None{}, std::false_type{}) : f(One{}, Count<8>{}, None{}, std::false_type{});
+        if constexpr (sizeof(T) == 4)
+            if (s.count == 4) return f(V{}, Count<4>{}, None{}, Of<kLanes>{}, all);
+        if (s.count <= 1) return f(V{}, Count<1>{}, None{}, Of<kLanes>{}, all);
+        return s.count == 2 ? f(V{}, Count<2>{}, None{}, Of<kLanes>{}, all) : f(V{}, Count<3>{}, None{}, Of<kLanes>{}, all);
+    };
+    return vectors == s.lanes * s.count ? with_count(Yes{}) : with_count(No{});
 }
 
 int element_bytes(int type) { return type == LAYER_NORM_F32 ? 4 : 2; }
@@ -527,10 +578,10 @@ bool count_blocks(layer_norm *p)
         if (whole && p->width % (16 / sizeof(T)) != 0) continue;
         const Share s = share_for(p, whole);
         const int threads = s.wide ? s.lanes : kNarrowThreads;
-        const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto r, auto wide) {
-            return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, r.value, wide.value>,
+        const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
+            return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, r.value, form.value, all.value>,
                                                                  threads, 0) == cudaSuccess &&
-                   cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, r.value, wide.value>,
+                   cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, r.value, form.value, all.value>,
                                                                  threads, backward_smem(p, s)) == cudaSuccess;
         });
         if (!ok || p->forward_blocks[whole] < 1 || p->backward_blocks[whole] < 1) return false;
@@ -564,8 +615,8 @@ int run_forward(layer_norm *p, Forward<T> f, bool whole)
     const Share s = share_for(p, whole);
     f.lanes = s.lanes;
     const unsigned blocks = static_cast<unsigned>(blocks_for(p, s, f.n, p->forward_blocks[whole]));
-    const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto r, auto wide) {
-        k_forward<T, v.value, c.value, r.value, wide.value><<<blocks, s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
+    const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
+        k_forward<T, v.value, c.value, r.value, form.value, all.value><<<blocks, s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
         return cudaGetLastError() == cudaSuccess;
     });
     if (!ok) return LAYER_NORM_ECUDA;
@@ -581,8 +632,8 @@ int run_backward(layer_norm *p, Backward<T> b, bool whole, float *dw, float *db)
     b.lanes = s.lanes;
     const int64_t blocks = blocks_for(p, s, b.n, p->backward_blocks[whole]);
     const size_t smem = backward_smem(p, s);
-    const bool ok = with_counts<T>(s, whole, [&](auto v, auto c, auto r, auto wide) {
-        k_backward<T, v.value, c.value, r.value, wide.value>
+    const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
+        k_backward<T, v.value, c.value, r.value, form.value, all.value>
             <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, smem, p->stream>>>(b);
         return cudaGetLastError() == cudaSuccess;
     });
