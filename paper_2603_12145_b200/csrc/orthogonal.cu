@@ -286,6 +286,13 @@ __device__ __forceinline__ void add_release(unsigned *p)
     asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p) : "memory");
 }
 
+__device__ __forceinline__ unsigned add_acq_rel(uint32_t p)
+{
+    unsigned v;
+    asm volatile("atom.acq_rel.cta.shared::cta.add.u32 %0, [%1], 1;" : "=r"(v) : "r"(p) : "memory");
+    return v;
+}
+
 // Waits until `target` blocks have finished; gives up as mbar_wait does.
 __device__ bool wait_arrived(const unsigned *arrived, unsigned target, volatile int *abort_flag)
 {
@@ -496,7 +503,8 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                 const CUtensorMap *tm_b = kind == 0 ? &maps.gram_b[from] : kind == 1 ? &maps.square_b : &maps.apply_b[from];
                 if (i > 0) ok = wait_arrived(q.arrived, static_cast<unsigned>(i) * gridDim.x, abort_flag);
                 mbar_arrive(ready);
-                asm volatile("fence.proxy.async;" ::: "memory");      // some of the operands were written by plain stores
+                // some of the operands were written by plain stores (a fence of all memory: 137 against 130 us)
+                asm volatile("fence.proxy.async.global;" ::: "memory");
                 const int b_half = p.tile_n / 2, b_boxes = (b_half + 63) / 64;
                 const uint32_t bytes = kABytes + b_bytes(p);
                 const uint32_t depth = min(static_cast<uint32_t>(kStages), kRing / bytes);
@@ -589,7 +597,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
             const Product &p = kind == 0 ? q.gram : kind == 1 ? q.square : q.apply;
             __half *symmetric = kind == 0 ? q.o : q.p;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(ready, i & 1, abort_flag));
-            if (lane == 0) asm volatile("fence.proxy.async;" ::: "memory");
+            if (lane == 0) asm volatile("fence.proxy.async.global;" ::: "memory");
             for (Walk w(q, p); ok && w.index < w.end; w.index += w.step, ++it) {
                 const uint32_t buf = it & 1, use = (it >> 1) & 1;
                 const Tile t = tile_at(p, w.index);
@@ -744,12 +752,12 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(map_to_rank(acc_empty0 + 8 * buf, leader));
             }
-            // the block has finished this product when its eighth warp has
-            if (lane == 0) bulk_wait();
-            __threadfence();
+            // The block has finished this product when its eighth warp has: what the others wrote is passed on through the count
+            // (one release for the device instead of one per warp: 1,728 x 576 138 against 144 us).
             __syncwarp();
-            if (lane == 0 && !last) {
-                if (atomicAdd(finished, 1u) % kEpilogueWarps == kEpilogueWarps - 1) add_release(q.arrived);
+            if (lane == 0) {
+                bulk_wait();
+                if (!last && add_acq_rel(smem_u32(finished)) % kEpilogueWarps == kEpilogueWarps - 1) add_release(q.arrived);
             }
         }
     }
