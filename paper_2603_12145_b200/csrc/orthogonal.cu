@@ -17,12 +17,12 @@
 // counter in memory.  k_squares and k_start bring G into X first.  A matrix whose short side is at most 128 takes k_small
 // instead: the whole iteration in the shared memory of one cluster.
 //
-// What bounds it, on a B200 (five steps): 2,048 x 8,192 in bfloat16 takes 650 us, 747 us at the power cap, for 0.56 TFLOP (860
-// and 748 TFLOP/s): a last round of tiles that not all pairs have, epilogues and waits between products.  1,728 x 576 in
-// binary32 takes 144 us: fifteen products of 9 us each, of which the operands' way from L2 (about 80 KB a microsecond into each
+// What bounds it, on a B200 (five steps): 2,048 x 8,192 in bfloat16 takes 630 to 650 us, 720 at the power cap, for 0.56 TFLOP (890
+// and 775 TFLOP/s): a last round of tiles that not all pairs have, epilogues and waits between products.  1,728 x 576 in
+// binary32 takes 131 us: fifteen products of 8 us each, of which the operands' way from L2 (about 80 KB a microsecond into each
 // SM) is a third and the rest is latency: the wait for all blocks 1.3 us, first loads 0.6, epilogue, stores and their
 // fence 3.  As separate launches, each started while the one before ends, it took 181 us (and 855 for 2,048 x 8,192).
-// Eight matrices 384 x 64 take 39 us in k_small.
+// Eight matrices 384 x 64 take 33 us in k_small.
 //
 // Why the diagonals are apart: in the last steps A is near the identity and B near -2.7 of it, so that a X + B X cancels.
 // Rounded to binary16 these diagonals alone put 1e-3 to 3e-3 of error into the result; centred around the polynomial's middle
@@ -904,7 +904,8 @@ k_start(const Start s, const T *g)
 //
 // Operand tiles are boxes of 64 columns by KP rows with the 128-byte swizzle, as TMA would write them: read along the rows by
 // X X^T, and down the rows (MN-major) by B X.  Instructions have 128 rows; with KP = 64 the upper half of them
-// computes on whatever lies behind the box, and nobody reads it.
+// computes on whatever lies behind the box, and nobody reads it, but for P, which is there twice: B X then comes out in all
+// lanes of the tensor memory, and all warps work on it.
 
 constexpr int kSmallThreads = 512;
 constexpr int kSmallQuads = kSmallThreads / 128;         // warps that share 32 rows: each takes a part of the columns
@@ -915,7 +916,8 @@ constexpr int kGroup = 256;                              // columns of X that on
 template <int KP>
 struct Small {
     static constexpr int kBox = KP * 128;                // 64 columns of KP rows
-    static constexpr int kSquare = KP / 64 * kBox;       // O, P
+    static constexpr int kSquare = KP / 64 * kBox;       // O
+    static constexpr int kP = 128 / KP * kSquare;        // P: 128 rows
     static constexpr int kParts = KP * KP * 4;           // the parts of the rows that a block owns, from everyone
     static constexpr int kFloats = 2 * KP * 4;           // d, e
     static constexpr int kRest = 512;                    // barriers, sums
@@ -923,14 +925,12 @@ struct Small {
     static constexpr int kBoxes = KP == 64 ? 11 : 3;
     static constexpr int bytes(int boxes, int blocks)
     {
-        const int used = 2 * boxes * kBox + 2 * kSquare + (blocks > 1 ? kParts : 0) + kFloats + kRest + 1024;
-        // one block per SM, since each takes all of the tensor memory; and 8 KB behind P for the rows that nobody reads
-        const int least = 120 * 1024;
-        return used + 8192 > least ? (used + 8192 < 227 * 1024 ? used + 8192 : 227 * 1024) : least;
+        const int used = 2 * boxes * kBox + kSquare + kP + (blocks > 1 ? kParts : 0) + kFloats + kRest + 1024;
+        const int least = 120 * 1024;                    // one block per SM, since each takes all of the tensor memory
+        return used > least ? used : least;
     }
 };
-static_assert(2 * Small<64>::kBoxes * Small<64>::kBox + 2 * Small<64>::kSquare + Small<64>::kParts + 8192 + 4096 <= 227 * 1024, "64 rows");
-static_assert(2 * Small<128>::kBoxes * Small<128>::kBox + 2 * Small<128>::kSquare + Small<128>::kParts + 2560 <= 227 * 1024, "128 rows");
+static_assert(Small<64>::bytes(Small<64>::kBoxes, 2) <= 227 * 1024 && Small<128>::bytes(Small<128>::kBoxes, 2) <= 227 * 1024, "shared memory of a block");
 
 struct SmallArgs {
     int k, l;                // short and long side
@@ -998,7 +998,7 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
     const uint32_t hi0 = (raw + 1023u) & ~1023u, lo0 = hi0 + p.boxes * S::kBox;
     const uint32_t o0 = lo0 + p.boxes * S::kBox, p0 = o0 + S::kSquare;
     const uint32_t blocks = cluster_size(), rank = cluster_cta_rank();
-    const uint32_t parts0 = p0 + S::kSquare, floats0 = parts0 + (blocks > 1 ? S::kParts : 0);
+    const uint32_t parts0 = p0 + S::kP, floats0 = parts0 + (blocks > 1 ? S::kParts : 0);
     uint8_t *floats_ptr = smem_raw + (floats0 - raw);
     float *d = reinterpret_cast<float *>(floats_ptr), *e = d + KP;
     const uint32_t bars = floats0 + S::kFloats;
@@ -1255,8 +1255,10 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = pack2(v[2 * i], v[2 * i + 1]);
-            put_piece(small_piece<KP>(p0, row, c >> 3), w[0], w[1], w[2], w[3]);
-            put_piece(small_piece<KP>(p0, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
+            for (int copy = 0; copy < S::kP; copy += S::kSquare) {
+                put_piece(small_piece<KP>(p0 + copy, row, c >> 3), w[0], w[1], w[2], w[3]);
+                put_piece(small_piece<KP>(p0 + copy, row, (c >> 3) + 1), w[4], w[5], w[6], w[7]);
+            }
         }
         fence_async();
         tc_fence_before_sync();
@@ -1266,17 +1268,20 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
             issue_group(0);
             if (groups > 1) issue_group(1);
         }
-        const float scale = p.a + (mine ? e[row] : 0.0f);
+        // the row of B X that this lane has, and the runs of 16 columns that are this warp's
+        constexpr int kRuns = kSmallQuads * 128 / KP;
+        const int here = row % KP, run = part * (128 / KP) + row / KP;
+        const float scale = p.a + e[here];
         for (int gr = 0; gr < groups; ++gr) {
             const int n = min(kGroup, columns - gr * kGroup);
             wait_done(gr & 1);
 #pragma unroll 1
-            for (int c = part * (n / kSmallQuads); mine && c < (part + 1) * (n / kSmallQuads); c += 16) {
+            for (int c = 16 * run; c < n; c += 16 * kRuns) {
                 uint32_t acc[16];
                 tmem_ld16(lanes + (gr & 1) * kGroup + c, acc);
                 const int piece = (gr * kGroup + c) >> 3;
-                const uint4 h0 = get_piece(small_piece<KP>(hi0, row, piece)), h1 = get_piece(small_piece<KP>(hi0, row, piece + 1));
-                const uint4 l0 = get_piece(small_piece<KP>(lo0, row, piece)), l1 = get_piece(small_piece<KP>(lo0, row, piece + 1));
+                const uint4 h0 = get_piece(small_piece<KP>(hi0, here, piece)), h1 = get_piece(small_piece<KP>(hi0, here, piece + 1));
+                const uint4 l0 = get_piece(small_piece<KP>(lo0, here, piece)), l1 = get_piece(small_piece<KP>(lo0, here, piece + 1));
                 const uint32_t hw[8] = {h0.x, h0.y, h0.z, h0.w, h1.x, h1.y, h1.z, h1.w};
                 const uint32_t lw[8] = {l0.x, l0.y, l0.z, l0.w, l1.x, l1.y, l1.z, l1.w};
                 tmem_wait_ld();
@@ -1295,21 +1300,21 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
                         const float2 h = unpack2(nh[i]);
                         nl[i] = pack2(v[2 * i] - h.x, v[2 * i + 1] - h.y);
                     }
-                    put_piece(small_piece<KP>(hi0, row, piece), nh[0], nh[1], nh[2], nh[3]);
-                    put_piece(small_piece<KP>(hi0, row, piece + 1), nh[4], nh[5], nh[6], nh[7]);
-                    put_piece(small_piece<KP>(lo0, row, piece), nl[0], nl[1], nl[2], nl[3]);
-                    put_piece(small_piece<KP>(lo0, row, piece + 1), nl[4], nl[5], nl[6], nl[7]);
-                } else if (row < p.k) {
+                    put_piece(small_piece<KP>(hi0, here, piece), nh[0], nh[1], nh[2], nh[3]);
+                    put_piece(small_piece<KP>(hi0, here, piece + 1), nh[4], nh[5], nh[6], nh[7]);
+                    put_piece(small_piece<KP>(lo0, here, piece), nl[0], nl[1], nl[2], nl[3]);
+                    put_piece(small_piece<KP>(lo0, here, piece + 1), nl[4], nl[5], nl[6], nl[7]);
+                } else if (here < p.k) {
                     const int j0 = slice + 8 * piece;
                     if (p.tall) {                                    // neighbouring lanes have neighbouring columns of the update
-                        __nv_bfloat16 *dst = p.out + z * p.out_batch + j0 * p.out_row + row;
+                        __nv_bfloat16 *dst = p.out + z * p.out_batch + j0 * p.out_row + here;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             if (j0 + i < p.l) *dst = __float2bfloat16_rn(v[i] * kUnscale);
                             dst += p.out_row;
                         }
                     } else {
-                        __nv_bfloat16 *dst = p.out + z * p.out_batch + row * p.out_row;
+                        __nv_bfloat16 *dst = p.out + z * p.out_batch + here * p.out_row;
                         if (p.out_whole) {
                             uint32_t w[8];
 #pragma unroll
