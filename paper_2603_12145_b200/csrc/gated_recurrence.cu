@@ -20,7 +20,7 @@
 // sigmoid(v): no cancellation there either.  Per element: three exponentials, two reciprocals, one reciprocal square root.
 //
 // What bounds it: the special-function unit, 6 results per element at 16 per cycle and SM, forward (512 x 128 x 1,152 in
-// bfloat16 146 us, 75.5 M elements: 100 us of it), issue backward (288 us; 41 instructions per pair of elements), HBM in
+// bfloat16 146 us, 75.5 M elements: 100 us of it), issue backward (288 us; 166 instructions per pair of elements), HBM in
 // the single token (16,384 x 1,152 rows 53 us, 302 MB, 5.7 TB/s).  A prompt of 8,192 steps of one row and 2,048 channels
 // takes 82 us, two passes of segments; 64 single tokens take 12 us, the host's part.
 #include <new>
