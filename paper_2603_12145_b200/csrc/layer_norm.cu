@@ -11,9 +11,9 @@
 // cross threads.  The row groups of a warp are added by exchanges, a block's warps in shared memory, blocks leave a row of
 // sums each and k_join adds them, all in a fixed order.
 //
-// What bounds them: memory, and issue close behind it.  In bfloat16 on a B200, 65,536 x 576 with residual takes 54 us forward
-// (302 MB, 5.6 TB/s) and 59 us backward (5.1 TB/s), 8,192 x 8,192 without takes 70 us (3.8 TB/s: two barriers per row) and 89
-// us (4.5 TB/s); 64 rows take 5 us on the device, less than the call on the host.
+// What bounds them: memory, and issue close behind it.  In bfloat16 on a B200, 65,536 x 576 with residual takes 52 us forward
+// (302 MB, 5.8 TB/s) and 58 us backward (5.2 TB/s), 8,192 x 8,192 without takes 51 us (5.2 TB/s) and 89 us (4.5 TB/s: one
+// block per SM, which waits for its row's sums); 64 rows take 5 us on the device, less than the call on the host.
 #include <cmath>
 #include <new>
 #include <type_traits>
@@ -105,7 +105,20 @@ struct Team {
             return v;
         }
     }
+    __device__ void totals(float (&v)[1]) { v[0] = total(v[0]); }
+    __device__ void totals(float (&v)[2])
+    {
+        const float2 t = total(make_float2(v[0], v[1]));
+        v[0] = t.x;
+        v[1] = t.y;
+    }
 };
+
+// Rows that a thread shares at a time, forward: two of few 16-bit elements, which are bound by arithmetic and exchanges, for one
+// round of these and the parameters read once (bfloat16 without residual: 8,192 x 8,192 51 against 70 us, 65,536 x 256
+// 12.4 against 14.4, x 576 30 against 34; binary32 is near memory's rate with one, 65,536 x 512 46 and 47 us).
+template <typename T, int V, int C, int R>
+constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && C * V + R <= 18 ? 2 : 1;
 
 // Units of one or two neighbouring parameters (from L1: every row reads them)
 template <int W, int N>
@@ -198,18 +211,16 @@ struct Turns {
     int64_t first, step;
     int behind;              // which of the warp's rows this lane has: all go round while the first of them is there
     template <bool kWide>
-    static __device__ __forceinline__ Turns of(int lanes)
+    static __device__ __forceinline__ Turns of(int lanes, int rows = 1)
     {
-        const int per_block = kWide ? 1 : kNarrowThreads / lanes;
-        return {static_cast<int64_t>(blockIdx.x) * per_block + (kWide ? 0 : static_cast<int>(threadIdx.x) / lanes),
-                static_cast<int64_t>(gridDim.x) * per_block, kWide ? 0 : static_cast<int>(threadIdx.x & 31) / lanes};
+        const int per_block = kWide ? rows : kNarrowThreads / lanes * rows;
+        return {static_cast<int64_t>(blockIdx.x) * per_block + (kWide ? 0 : static_cast<int>(threadIdx.x) / lanes * rows),
+                static_cast<int64_t>(gridDim.x) * per_block, kWide ? 0 : static_cast<int>(threadIdx.x & 31) / lanes * rows};
     }
 };
 
-// (blocks of 512 threads: two of them on an SM, 8,192 x 8,192 in bfloat16 70 against 80 us; smaller ones lose by the cap on
-// registers, 16,384 x 4,096 92 against 87)
 template <typename T, int V, int C, int R, Form kForm, bool kAll>
-__global__ void __launch_bounds__(kForm == kLargest ? kMost : kForm == kBlock ? kMost / 2 : kNarrowThreads, kForm == kLargest && V == 8 ? 2 : 0)
+__global__ void __launch_bounds__(kForm == kLargest ? kMost : kForm == kBlock ? kMost / 2 : kNarrowThreads)
 k_forward(const Forward<T> p)
 {
     constexpr bool kWide = kForm != kLanes;
@@ -222,19 +233,23 @@ k_forward(const Forward<T> p)
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
     const M mine = {team.size, team.index, p.width / V};
-    const Turns turns = Turns::of<kWide>(p.lanes);
+    constexpr int kRows = kRowsOf<T, V, C, R>;
+    const Turns turns = Turns::of<kWide>(p.lanes, kRows);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.residual.ptr != nullptr;
-    typename M::Words nx, nr;
-    auto fetch = [&](int64_t row) {          // behind the last row that one again: no zeros to be put in place
-        row = row < p.n ? row : p.n - 1;
-        nx = mine.load(p.x.row(row));
-        if (added) nr = mine.load(p.residual.row(row));
+    typename M::Words nx[kRows], nr[kRows];
+    auto fetch = [&](int64_t first) {        // behind the last row that one again: no zeros to be put in place
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int64_t row = first + r < p.n ? first + r : p.n - 1;
+            nx[r] = mine.load(p.x.row(row));
+            if (added) nr[r] = mine.load(p.residual.row(row));
+        }
     };
     fetch(turns.first);
-    // The parameters of up to 18 elements stay in registers (bfloat16, no residual: 65,536 x 256 14.7 against 18.7 us, x 512
-    // 26.3 against 30.8); of more they cost warps (binary32, 65,536 x 384 39 against 37; 8,192 x 8,192 in bfloat16 103 against 89).
-    constexpr bool kHeld = !kWide && V > 1 && C * V + R <= 18;
+    // The parameters stay in registers where there is room (bfloat16, no residual: 65,536 x 256 14.7 against 18.7 us, 32,768 x 1,032 33
+    // against 41); of more elements they cost warps (binary32, 65,536 x 384 39 against 37).
+    constexpr bool kHeld = V > 1 && C * V + R <= (!kWide ? 18 : sizeof(T) == 2 ? 24 : 0);
     U held_w[kHeld ? M::kUnits : 1], held_b[kHeld ? M::kUnits : 1];
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
@@ -249,51 +264,65 @@ k_forward(const Forward<T> p)
         });
     }
     for (int64_t row = turns.first; row - turns.behind < p.n; row += turns.step) {
-        const bool live = row < p.n;
-        if (added) {
+        U s[kRows][M::kUnits];
+        float mean[kRows], scale[kRows];
 #pragma unroll
-            for (int u = 0; u < M::kUnits; ++u) nx.set(u, add(nx.get(u), nr.get(u)));     // rounded to the type
-            if (live) mine.store(p.sum.row(row), nx);
-        }
-        U s[M::kUnits], sum = all<W>(0.0f);
+        for (int r = 0; r < kRows; ++r) {
+            if (added) {
 #pragma unroll
-        for (int u = 0; u < M::kUnits; ++u) {
-            s[u] = nx.get(u);
-            sum = add(sum, s[u]);
+                for (int u = 0; u < M::kUnits; ++u) nx[r].set(u, add(nx[r].get(u), nr[r].get(u)));     // rounded to the type
+                if (row + r < p.n) mine.store(p.sum.row(row + r), nx[r]);
+            }
+            U sum = all<W>(0.0f);
+#pragma unroll
+            for (int u = 0; u < M::kUnits; ++u) {
+                s[r][u] = nx[r].get(u);
+                sum = add(sum, s[r][u]);
+            }
+            mean[r] = sum_of(sum);
         }
         fetch(row + turns.step);
-        const float mean = team.total(sum_of(sum)) * inverse;
-        U square = all<W>(0.0f);
-        mine.each_access([&](int u0, auto n, int, bool in) {
-            if (!in) return;
+        team.totals(mean);
 #pragma unroll
-            for (int i = 0; i < n.value; ++i) {
-                s[u0 + i] = add(s[u0 + i], all<W>(-mean));
-                square = fma(s[u0 + i], s[u0 + i], square);
-            }
-        });
-        const float scale = rsqrtf(fmaf(team.total(sum_of(square)), inverse, p.eps));
-        if (!live) continue;
-        if (p.saved != nullptr && team.index == 0) p.saved[row] = make_float2(mean, scale);
-        T *const py = p.y.row(row);
-        mine.each_access([&](int u0, auto n, int at, bool in) {
-            if (!in) return;
-            Packed<T, W * n.value> out;
-            U w[n.value], b[n.value];
-            if constexpr (kHeld) {
+        for (int r = 0; r < kRows; ++r) {
+            mean[r] *= inverse;
+            U square = all<W>(0.0f);
+            mine.each_access([&](int u0, auto n, int, bool in) {
+                if (!in) return;
 #pragma unroll
                 for (int i = 0; i < n.value; ++i) {
-                    w[i] = held_w[u0 + i];
-                    b[i] = held_b[u0 + i];
+                    s[r][u0 + i] = add(s[r][u0 + i], all<W>(-mean[r]));
+                    square = fma(s[r][u0 + i], s[r][u0 + i], square);
                 }
-            } else {
-                load_params<W>(w, p.w != nullptr ? p.w + at : nullptr, 1.0f);
-                load_params<W>(b, p.b != nullptr ? p.b + at : nullptr, 0.0f);
-            }
+            });
+            scale[r] = sum_of(square);
+        }
+        team.totals(scale);
 #pragma unroll
-            for (int i = 0; i < n.value; ++i) narrow_at(out, i, fma(mul(s[u0 + i], all<W>(scale)), w[i], b[i]));
-            packed_store<T, W * n.value>(py + at, out);
-        });
+        for (int r = 0; r < kRows; ++r) {
+            scale[r] = rsqrtf(fmaf(scale[r], inverse, p.eps));
+            if (row + r >= p.n) continue;
+            if (p.saved != nullptr && team.index == 0) p.saved[row + r] = make_float2(mean[r], scale[r]);
+            T *const py = p.y.row(row + r);
+            mine.each_access([&](int u0, auto n, int at, bool in) {
+                if (!in) return;
+                Packed<T, W * n.value> out;
+                U w[n.value], b[n.value];
+                if constexpr (kHeld) {
+#pragma unroll
+                    for (int i = 0; i < n.value; ++i) {
+                        w[i] = held_w[u0 + i];
+                        b[i] = held_b[u0 + i];
+                    }
+                } else {
+                    load_params<W>(w, p.w != nullptr ? p.w + at : nullptr, 1.0f);
+                    load_params<W>(b, p.b != nullptr ? p.b + at : nullptr, 0.0f);
+                }
+#pragma unroll
+                for (int i = 0; i < n.value; ++i) narrow_at(out, i, fma(mul(s[r][u0 + i], all<W>(scale[r])), w[i], b[i]));
+                packed_store<T, W * n.value>(py + at, out);
+            });
+        }
     }
 }
 
@@ -565,9 +594,9 @@ Share share_for(const layer_norm *p, bool whole)
 size_t backward_smem(const layer_norm *p, const Share &s) { return s.wide ? 0 : kNarrowThreads / 32 * 2 * sizeof(float) * p->width; }
 
 // Whole rounds of resident blocks, so that all end together.
-int64_t blocks_for(const layer_norm *p, const Share &s, int64_t n, int per_sm)
+int64_t blocks_for(const layer_norm *p, const Share &s, int64_t n, int per_sm, int rows = 1)
 {
-    const int64_t units = s.wide ? n : div_up(n, kNarrowThreads / s.lanes);
+    const int64_t units = div_up(n, static_cast<int64_t>(s.wide ? 1 : kNarrowThreads / s.lanes) * rows);
     return div_up(units, div_up(units, static_cast<int64_t>(p->sms) * per_sm));
 }
 
@@ -614,9 +643,10 @@ int run_forward(layer_norm *p, Forward<T> f, bool whole)
     whole = whole && p->width % (16 / sizeof(T)) == 0;
     const Share s = share_for(p, whole);
     f.lanes = s.lanes;
-    const unsigned blocks = static_cast<unsigned>(blocks_for(p, s, f.n, p->forward_blocks[whole]));
     const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-        k_forward<T, v.value, c.value, r.value, form.value, all.value><<<blocks, s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
+        const int64_t blocks = blocks_for(p, s, f.n, p->forward_blocks[whole], kRowsOf<T, v.value, c.value, r.value>);
+        k_forward<T, v.value, c.value, r.value, form.value, all.value>
+            <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
         return cudaGetLastError() == cudaSuccess;
     });
     if (!ok) return LAYER_NORM_ECUDA;
