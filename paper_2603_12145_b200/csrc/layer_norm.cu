@@ -12,7 +12,7 @@
 // sums each and k_join adds them, all in a fixed order.
 //
 // What bounds them: memory, and issue close behind it.  In bfloat16 on a B200, 65,536 x 576 with residual takes 52 us forward
-// (302 MB, 5.8 TB/s) and 58 us backward (5.2 TB/s), 8,192 x 8,192 without takes 51 us (5.2 TB/s) and 89 us (4.5 TB/s: one
+// (302 MB, 5.8 TB/s) and 55 us backward (5.5 TB/s), 8,192 x 8,192 without takes 51 us (5.2 TB/s) and 89 us (4.5 TB/s: one
 // block per SM, which waits for its row's sums); 64 rows take 5 us on the device, less than the call on the host.
 #include <cmath>
 #include <new>
@@ -105,6 +105,17 @@ struct Team {
             return v;
         }
     }
+    __device__ void totals(float2 (&v)[1]) { v[0] = total(v[0]); }
+    __device__ void totals(float2 (&v)[2])              // (lanes of a warp)
+    {
+        for (int o = size >> 1; o > 0; o >>= 1) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                v[r].x += __shfl_xor_sync(0xFFFFFFFFu, v[r].x, o);
+                v[r].y += __shfl_xor_sync(0xFFFFFFFFu, v[r].y, o);
+            }
+        }
+    }
     __device__ void totals(float (&v)[1]) { v[0] = total(v[0]); }
     __device__ void totals(float (&v)[2])
     {
@@ -119,6 +130,10 @@ struct Team {
 // 12.4 against 14.4, x 576 30 against 34; binary32 is near memory's rate with one, 65,536 x 512 46 and 47 us).
 template <typename T, int V, int C, int R>
 constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && C * V + R <= 18 ? 2 : 1;
+// Backward by lanes of a warp likewise (65,536 x 576 with dsum 55.5 against 59.4 us, x 256 24.6 against 26.7); a block's threads
+// have no registers for it.
+template <typename T, int V, int C, int R, Form kForm>
+constexpr int kBackwardRowsOf = kForm == kLanes ? kRowsOf<T, V, C, R> : 1;
 
 // Units of one or two neighbouring parameters (from L1: every row reads them)
 template <int W, int N>
@@ -342,20 +357,24 @@ k_backward(const Backward<T> p)
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
     const M mine = {team.size, team.index, p.width / V};
-    const Turns turns = Turns::of<kWide>(p.lanes);
+    constexpr int kRows = kBackwardRowsOf<T, V, C, R, kForm>;
+    const Turns turns = Turns::of<kWide>(p.lanes, kRows);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.dsum.ptr != nullptr;
     U dw[M::kUnits], db[M::kUnits];
 #pragma unroll
     for (int u = 0; u < M::kUnits; ++u) dw[u] = db[u] = all<W>(0.0f);
-    typename M::Words ns, ndy, nd;
-    float2 nstat;
-    auto fetch = [&](int64_t row) {
-        row = row < p.n ? row : p.n - 1;
-        nstat = __ldg(p.saved + row);
-        ns = mine.load(p.s.row(row));
-        ndy = mine.load(p.dy.row(row));
-        if (added) nd = mine.load(p.dsum.row(row));
+    typename M::Words ns[kRows], ndy[kRows], nd[kRows];
+    float2 nstat[kRows];
+    auto fetch = [&](int64_t first) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const int64_t row = first + r < p.n ? first + r : p.n - 1;
+            nstat[r] = __ldg(p.saved + row);
+            ns[r] = mine.load(p.s.row(row));
+            ndy[r] = mine.load(p.dy.row(row));
+            if (added) nd[r] = mine.load(p.dsum.row(row));
+        }
     };
     fetch(turns.first);
     // The weights take a third of the accesses if every row fetches them: in registers where there is room, that is, not in
@@ -380,45 +399,60 @@ k_backward(const Backward<T> p)
         }
     };
     for (int64_t row = turns.first; row - turns.behind < p.n; row += turns.step) {
-        const bool live = row < p.n;
-        const typename M::Words s = ns, dy = ndy, d = nd;
-        const float mean = nstat.x, scale = nstat.y;
+        typename M::Words s[kRows], dy[kRows], d[kRows];
+        float mean[kRows], scale[kRows];
+        float2 sums[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            s[r] = ns[r];
+            dy[r] = ndy[r];
+            d[r] = nd[r];
+            mean[r] = nstat[r].x;
+            scale[r] = nstat[r].y;
+        }
         fetch(row + turns.step);
-        const U q = all<W>(scale);
-        U sum = all<W>(0.0f), along = sum;
-        mine.each_access([&](int u0, auto n, int at, bool in) {
-            if (!in || !live) return;
-            U w[n.value];
-            weights(w, u0, at);
 #pragma unroll
-            for (int i = 0; i < n.value; ++i) {
-                const int u = u0 + i;
-                const U z = mul(add(s.get(u), all<W>(-mean)), q), g = dy.get(u), h = mul(g, w[i]);
-                sum = add(sum, h);
-                along = fma(h, z, along);
-                dw[u] = fma(g, z, dw[u]);
-                db[u] = add(db[u], g);
-            }
-        });
-        const float2 sums = team.total(make_float2(sum_of(sum), sum_of(along)));
-        if (!live) continue;
-        const U slope = all<W>(-scale * sums.y * inverse), shift = all<W>(-scale * sums.x * inverse);
-        T *const px = p.dx.row(row);
-        mine.each_access([&](int u0, auto n, int at, bool in) {
-            if (!in) return;
-            Packed<T, W * n.value> out;
-            U w[n.value];
-            weights(w, u0, at);
+        for (int r = 0; r < kRows; ++r) {
+            const bool live = row + r < p.n;
+            U sum = all<W>(0.0f), along = sum;
+            mine.each_access([&](int u0, auto n, int at, bool in) {
+                if (!in || !live) return;
+                U w[n.value];
+                weights(w, u0, at);
 #pragma unroll
-            for (int i = 0; i < n.value; ++i) {
-                const int u = u0 + i;
-                const U z = mul(add(s.get(u), all<W>(-mean)), q);
-                U x = fma(mul(dy.get(u), w[i]), q, fma(z, slope, shift));
-                if (added) x = add(x, d.get(u));
-                narrow_at(out, i, x);
-            }
-            packed_store<T, W * n.value>(px + at, out);
-        });
+                for (int i = 0; i < n.value; ++i) {
+                    const int u = u0 + i;
+                    const U z = mul(add(s[r].get(u), all<W>(-mean[r])), all<W>(scale[r])), g = dy[r].get(u), h = mul(g, w[i]);
+                    sum = add(sum, h);
+                    along = fma(h, z, along);
+                    dw[u] = fma(g, z, dw[u]);
+                    db[u] = add(db[u], g);
+                }
+            });
+            sums[r] = make_float2(sum_of(sum), sum_of(along));
+        }
+        team.totals(sums);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (row + r >= p.n) continue;
+            const U slope = all<W>(-scale[r] * sums[r].y * inverse), shift = all<W>(-scale[r] * sums[r].x * inverse);
+            T *const px = p.dx.row(row + r);
+            mine.each_access([&](int u0, auto n, int at, bool in) {
+                if (!in) return;
+                Packed<T, W * n.value> out;
+                U w[n.value];
+                weights(w, u0, at);
+#pragma unroll
+                for (int i = 0; i < n.value; ++i) {
+                    const int u = u0 + i;
+                    const U z = mul(add(s[r].get(u), all<W>(-mean[r])), all<W>(scale[r]));
+                    U x = fma(mul(dy[r].get(u), w[i]), all<W>(scale[r]), fma(z, slope, shift));
+                    if (added) x = add(x, d[r].get(u));
+                    narrow_at(out, i, x);
+                }
+                packed_store<T, W * n.value>(px + at, out);
+            });
+        }
     }
     if (p.part == nullptr) return;
     float *part = p.part + static_cast<int64_t>(blockIdx.x) * 2 * p.width;
@@ -579,6 +613,7 @@ struct layer_norm {
     float eps = 0.0f;
     int device = 0, sms = 0;
     int forward_blocks[2] = {0, 0}, backward_blocks[2] = {0, 0};     // that an SM holds; rows of single elements, of vectors
+    int backward_rows[2] = {1, 1};           // that a thread takes at a time
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
 };
@@ -600,6 +635,11 @@ int64_t blocks_for(const layer_norm *p, const Share &s, int64_t n, int per_sm, i
     return div_up(units, div_up(units, static_cast<int64_t>(p->sms) * per_sm));
 }
 
+int64_t backward_blocks(const layer_norm *p, int64_t n, bool whole)
+{
+    return blocks_for(p, share_for(p, whole), n, p->backward_blocks[whole], p->backward_rows[whole]);
+}
+
 template <typename T>
 bool count_blocks(layer_norm *p)
 {
@@ -608,6 +648,7 @@ bool count_blocks(layer_norm *p)
         const Share s = share_for(p, whole);
         const int threads = s.wide ? s.lanes : kNarrowThreads;
         const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
+            p->backward_rows[whole] = kBackwardRowsOf<T, v.value, c.value, r.value, form.value>;
             return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, r.value, form.value, all.value>,
                                                                  threads, 0) == cudaSuccess &&
                    cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, r.value, form.value, all.value>,
@@ -660,7 +701,7 @@ int run_backward(layer_norm *p, Backward<T> b, bool whole, float *dw, float *db)
     whole = whole && p->width % (16 / sizeof(T)) == 0;
     const Share s = share_for(p, whole);
     b.lanes = s.lanes;
-    const int64_t blocks = blocks_for(p, s, b.n, p->backward_blocks[whole]);
+    const int64_t blocks = backward_blocks(p, b.n, whole);
     const size_t smem = backward_smem(p, s);
     const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
         k_backward<T, v.value, c.value, r.value, form.value, all.value>
@@ -797,9 +838,9 @@ size_t layer_norm_workspace_bytes(const layer_norm *p, int64_t n)
 {
     if (p == nullptr || !rows_ok(n)) return 0;
     // rows of whole vectors and others are shared out differently: room for either
-    int64_t rows = blocks_for(p, share_for(p, false), n, p->backward_blocks[0]);
+    int64_t rows = backward_blocks(p, n, false);
     if (p->backward_blocks[1] > 0) {
-        const int64_t other = blocks_for(p, share_for(p, true), n, p->backward_blocks[1]);
+        const int64_t other = backward_blocks(p, n, true);
         if (other > rows) rows = other;
     }
     return static_cast<size_t>(rows) * 2 * p->width * sizeof(float);
