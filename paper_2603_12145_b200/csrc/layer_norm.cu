@@ -127,13 +127,14 @@ struct Team {
 
 // Rows that a thread shares at a time, forward: two of few 16-bit elements, which are bound by arithmetic and exchanges, for one
 // round of these and the parameters read once (bfloat16 without residual: 8,192 x 8,192 51 against 70 us, 65,536 x 256
-// 12.4 against 14.4, x 576 30 against 34; binary32 is near memory's rate with one, 65,536 x 512 46 and 47 us).
-template <typename T, int V, int C, int R>
-constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && C * V + R <= 18 ? 2 : 1;
+// 12.4 against 14.4, x 576 30 against 34; binary32 is near memory's rate with one, 65,536 x 512 46 and 47 us).  24 elements only
+// where no access is masked and no barrier waits: x 768 41 against 43, but x 696 43 against 40, 32,768 x 1,032 43 against 33.
+template <typename T, int V, int C, int R, Form kForm, bool kAll>
+constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && C * V + R <= (kForm == kLanes && kAll ? 24 : 20) ? 2 : 1;
 // Backward by lanes of a warp likewise (65,536 x 576 with dsum 55.5 against 59.4 us, x 256 24.6 against 26.7); a block's threads
 // have no registers for it.
-template <typename T, int V, int C, int R, Form kForm>
-constexpr int kBackwardRowsOf = kForm == kLanes ? kRowsOf<T, V, C, R> : 1;
+template <typename T, int V, int C, int R, Form kForm, bool kAll>
+constexpr int kBackwardRowsOf = kForm == kLanes ? kRowsOf<T, V, C, R, kForm, kAll> : 1;
 
 // Units of one or two neighbouring parameters (from L1: every row reads them)
 template <int W, int N>
@@ -248,7 +249,7 @@ k_forward(const Forward<T> p)
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
     const M mine = {team.size, team.index, p.width / V};
-    constexpr int kRows = kRowsOf<T, V, C, R>;
+    constexpr int kRows = kRowsOf<T, V, C, R, kForm, kAll>;
     const Turns turns = Turns::of<kWide>(p.lanes, kRows);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.residual.ptr != nullptr;
@@ -263,8 +264,8 @@ k_forward(const Forward<T> p)
     };
     fetch(turns.first);
     // The parameters stay in registers where there is room (bfloat16, no residual: 65,536 x 256 14.7 against 18.7 us, 32,768 x 1,032 33
-    // against 41); of more elements they cost warps (binary32, 65,536 x 384 39 against 37).
-    constexpr bool kHeld = V > 1 && C * V + R <= (!kWide ? 18 : sizeof(T) == 2 ? 24 : 0);
+    // against 41); blocks that share a binary32 row lose warps by it (8,192 x 4,096 51 against 49).
+    constexpr bool kHeld = V > 1 && C * V + R <= (sizeof(T) == 2 ? 24 : kWide ? 0 : 18);
     U held_w[kHeld ? M::kUnits : 1], held_b[kHeld ? M::kUnits : 1];
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
@@ -357,7 +358,7 @@ k_backward(const Backward<T> p)
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
     const M mine = {team.size, team.index, p.width / V};
-    constexpr int kRows = kBackwardRowsOf<T, V, C, R, kForm>;
+    constexpr int kRows = kBackwardRowsOf<T, V, C, R, kForm, kAll>;
     const Turns turns = Turns::of<kWide>(p.lanes, kRows);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.dsum.ptr != nullptr;
@@ -648,7 +649,7 @@ bool count_blocks(layer_norm *p)
         const Share s = share_for(p, whole);
         const int threads = s.wide ? s.lanes : kNarrowThreads;
         const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-            p->backward_rows[whole] = kBackwardRowsOf<T, v.value, c.value, r.value, form.value>;
+            p->backward_rows[whole] = kBackwardRowsOf<T, v.value, c.value, r.value, form.value, all.value>;
             return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, r.value, form.value, all.value>,
                                                                  threads, 0) == cudaSuccess &&
                    cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, r.value, form.value, all.value>,
@@ -685,7 +686,7 @@ int run_forward(layer_norm *p, Forward<T> f, bool whole)
     const Share s = share_for(p, whole);
     f.lanes = s.lanes;
     const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-        const int64_t blocks = blocks_for(p, s, f.n, p->forward_blocks[whole], kRowsOf<T, v.value, c.value, r.value>);
+        const int64_t blocks = blocks_for(p, s, f.n, p->forward_blocks[whole], kRowsOf<T, v.value, c.value, r.value, form.value, all.value>);
         k_forward<T, v.value, c.value, r.value, form.value, all.value>
             <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
         return cudaGetLastError() == cudaSuccess;

@@ -170,6 +170,23 @@ def test_widths_between_shares(torch, case):
     assert torch.equal(alone[0], dx)
 
 
+@pytest.mark.parametrize("width", [8, 64, 256, 576, 768, 1024, 8192])
+@pytest.mark.parametrize("n", [1, 2, 3])
+def test_few_rows(torch, n, width):
+    """Fewer rows than a thread, a warp or a block goes through at a time."""
+    op = layer_norm.LayerNorm(width, eps=1e-5)
+    x, r, dy = (make(torch, seed, n, width, "bfloat16", offset=0.5) for seed in (1, 2, 3))
+    w, b = make(torch, 5, 1, width, "float32")[0], make(torch, 6, 1, width, "float32")[0]
+    room = [torch.full((n + 2, width), 7.0, dtype=x.dtype, device="cuda") for _ in range(3)]
+    saved = op.saved(n)
+    y, total = op.forward(x, w, b, residual=r, saved=saved, out=room[0][:n], total=room[1][:n])
+    assert torch.equal(total, x + r)
+    check_forward(f64(total), y, f64(w), f64(b), 1e-5, "bfloat16")
+    dx, dw, db = op.backward(dy, total, w, saved, out=room[2][:n])
+    check_backward(f64(total), f64(dy), f64(w), None, 1e-5, "bfloat16", dx, dw, db)
+    assert all((v[n:] == 7.0).all() for v in room)
+
+
 def test_large_offset_and_constant_rows(torch):
     """Rows far from zero lose nothing to cancellation beyond the mean's rounding; a constant row is all b."""
     op = layer_norm.LayerNorm(576, dtype=torch.float32)
