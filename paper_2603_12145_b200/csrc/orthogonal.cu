@@ -17,9 +17,9 @@
 // counter in memory.  k_squares and k_start bring G into X first.  A matrix whose short side is at most 128 takes k_small
 // instead: the whole iteration in the shared memory of one cluster.
 //
-// What bounds it, on a B200 (five steps): 2,048 x 8,192 in bfloat16 takes 630 to 650 us, 720 at the power cap, for 0.56 TFLOP (890
+// What bounds it, on a B200 (five steps): 2,048 x 8,192 in bfloat16 takes 630 to 645 us, 720 at the power cap, for 0.56 TFLOP (890
 // and 775 TFLOP/s): a last round of tiles that not all pairs have, epilogues and waits between products.  1,728 x 576 in
-// binary32 takes 131 us: fifteen products of 8 us each, of which the operands' way from L2 (about 80 KB a microsecond into each
+// binary32 takes 127 us: fifteen products of 8 us each, of which the operands' way from L2 (about 80 KB a microsecond into each
 // SM) is a third and the rest is latency: the wait for all blocks 1.3 us, first loads 0.6, epilogue, stores and their
 // fence 3.  As separate launches, each started while the one before ends, it took 181 us (and 855 for 2,048 x 8,192).
 // Eight matrices 384 x 64 take 33 us in k_small.
@@ -64,7 +64,8 @@ constexpr int kStaging = 2 * kSets * kBlock;
 // (what pairs exchange and what is staged take turns: a product does one or the other)
 constexpr int kBesides = kEpilogueWarps * kStaging;
 constexpr int kBarrierBytes = 512;
-constexpr int kSmem = kRing + kBesides + kBarrierBytes + 1024;
+constexpr int kColumns = kEpilogueWarps * 32 * 4;   // per epilogue warp: the diagonal's elements of its 32 columns
+constexpr int kSmem = kRing + kBesides + kBarrierBytes + kColumns + 1024;
 static_assert(kSmem <= 227 * 1024 && exchange_bytes(2) <= kBesides && exchange_bytes(4) <= kBesides, "shared memory of a block");
 
 constexpr int kRowThreads = 256;                 // blocks of the kernels that read and write rows
@@ -261,6 +262,8 @@ __device__ __forceinline__ void tma_load_block(uint32_t dst, const CUtensorMap *
         : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
 __device__ __forceinline__ void tma_store_block(const CUtensorMap *map, int x, int y, int z, uint32_t src)
 {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y),
@@ -385,8 +388,8 @@ __device__ __forceinline__ void finish_gram(const Iteration &q, int z, int row, 
     for (int e = 0; e < 8; ++e) w[e] = pack2(v[2 * e], v[2 * e + 1]);
 }
 
-// B from O's products, O itself and the diagonal d, of which di is the row's: likewise to P and e.  w: O in, P out.
-__device__ __forceinline__ void finish_square(const Iteration &q, int z, int row, int j0, float di, const float (&acc)[16], uint32_t (&w)[8])
+// B from O's products, O itself and the diagonal d, of which di is the row's and d the columns': likewise to P and e.  w: O in, P out.
+__device__ __forceinline__ void finish_square(const Iteration &q, int z, int row, int j0, float di, const float *d, const float (&acc)[16], uint32_t (&w)[8])
 {
     if (j0 >= q.gram.m) return;
     const int64_t diagonal = static_cast<int64_t>(z) * q.dk;
@@ -394,7 +397,7 @@ __device__ __forceinline__ void finish_square(const Iteration &q, int z, int row
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
         // (the diagonals are padded to whole pieces of 16)
-        const float4 dj = *reinterpret_cast<const float4 *>(q.d + diagonal + j0 + e);
+        const float4 dj = *reinterpret_cast<const float4 *>(d + e);
         const float2 o0 = unpack2(w[e / 2]), o1 = unpack2(w[e / 2 + 1]);
         const float o[4] = {o0.x, o0.y, o1.x, o1.y}, ds[4] = {dj.x, dj.y, dj.z, dj.w};
 #pragma unroll
@@ -414,17 +417,16 @@ __device__ __forceinline__ void finish_square(const Iteration &q, int z, int row
 }
 
 // X' from X = hi + lo in, hi and lo out; of the last product the update instead of hi.  factor: a, and e of the row where the
-// diagonal goes with rows.
-__device__ __forceinline__ void finish_apply(const Iteration &q, bool last, int z, int j0, float factor, const float (&acc)[16],
+// diagonal goes with rows; by_columns: e where it goes with columns, else nullptr.
+__device__ __forceinline__ void finish_apply(const Iteration &q, bool last, float factor, const float *by_columns, const float (&acc)[16],
                                              uint32_t (&hi)[8], uint32_t (&lo)[8])
 {
     float v[16];
-    const bool by_columns = q.tall && j0 < q.apply.n;
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
         float f[4] = {factor, factor, factor, factor};
-        if (by_columns) {
-            const float4 ej = *reinterpret_cast<const float4 *>(q.e + static_cast<int64_t>(z) * q.dk + j0 + e);
+        if (by_columns != nullptr) {
+            const float4 ej = *reinterpret_cast<const float4 *>(by_columns + e);
             f[0] += ej.x, f[1] += ej.y, f[2] += ej.z, f[3] += ej.w;
         }
 #pragma unroll
@@ -501,6 +503,8 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                 const Product &p = kind == 0 ? q.gram : kind == 1 ? q.square : q.apply;
                 const CUtensorMap *tm_a = kind == 0 ? &maps.gram_a[from] : kind == 1 ? &maps.square_a : &maps.apply_a[from];
                 const CUtensorMap *tm_b = kind == 0 ? &maps.gram_b[from] : kind == 1 ? &maps.square_b : &maps.apply_b[from];
+                prefetch_map(tm_a);                      // (1 % at the middle sizes)
+                prefetch_map(tm_b);
                 if (i > 0) ok = wait_arrived(q.arrived, static_cast<unsigned>(i) * gridDim.x, abort_flag);
                 mbar_arrive(ready);
                 // some of the operands were written by plain stores (a fence of all memory: 137 against 130 us)
@@ -588,6 +592,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
         const uint32_t lane_base = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         const int row_in_block = quarter * 32 + lane;
         const uint32_t stage = besides + (warp - 2) * kStaging, staged = staged0 + 8 * kSets * (warp - 2);
+        float *columns = reinterpret_cast<float *>(bars_ptr + kBarrierBytes) + 32 * (warp - 2);
         uint32_t staged_phase = 0;                       // bit b: parity of the next arrival in set b
         bool ok = true;
         int it = 0, exchanges = 0;
@@ -622,6 +627,13 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                             tma_load_block(dst + kBlock, &maps.lo[from], first + 32 * s, row0, t.z, bar);
                         }
                     };
+                    // d or e of the columns [first + 32 s, + 32), a set ahead
+                    const float *diagonals = kind == 1 ? q.d + diagonal : kind == 2 && q.tall ? q.e + diagonal : nullptr;
+                    auto fetch_column = [&](int s) {
+                        const int c = first + 32 * s + lane;
+                        return diagonals != nullptr && s < sets && c < p.n ? diagonals[c] : 0.0f;
+                    };
+                    float column = fetch_column(0);
                     if (lane == 0) {
                         bulk_wait_read();                // the buffers: the previous tile's results have left
                         if (kind != 0)
@@ -644,6 +656,11 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                             if (lane == 0) bulk_wait_read();
                             __syncwarp();
                         }
+                        if (diagonals != nullptr) {
+                            columns[lane] = column;
+                            column = fetch_column(s + 1);
+                            __syncwarp();
+                        }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             uint32_t raw_acc[16], u[8], v[8];
@@ -656,8 +673,8 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                             for (int e = 0; e < 16; ++e) acc[e] = __uint_as_float(raw_acc[e]);
                             const int j0 = f + 16 * h;
                             if (kind == 0) finish_gram(q, t.z, row, j0, acc, u);
-                            else if (kind == 1) finish_square(q, t.z, row, j0, factor, acc, u);
-                            else finish_apply(q, last, t.z, j0, factor, acc, u, v);
+                            else if (kind == 1) finish_square(q, t.z, row, j0, factor, columns + 16 * h, acc, u);
+                            else finish_apply(q, last, factor, q.tall ? columns + 16 * h : nullptr, acc, u, v);
                             if (last && !q.out_whole) {
                                 __nv_bfloat16 *dst = q.out + t.z * q.out_batch + row * q.out_row;
                                 if (live) {
@@ -743,7 +760,7 @@ k_iterate(const __grid_constant__ Maps maps, const __grid_constant__ Iteration q
                             }
                         }
                         if (kind == 0) finish_gram(q, t.z, row, j0, acc, u);
-                        else finish_square(q, t.z, row, j0, factor, acc, u);
+                        else finish_square(q, t.z, row, j0, factor, q.d + diagonal + j0, acc, u);
                         if (live) store16(symmetric + at, j0, q.ldk, u);
                         if (mirrored) store_mirrored(symmetric + static_cast<int64_t>(t.z) * p.m * q.ldk, q.ldk, p.m, row, j0, u);
                     }
