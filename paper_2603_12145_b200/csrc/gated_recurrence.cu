@@ -22,7 +22,7 @@
 // What bounds it: the special-function unit, 6 results per element at 16 per cycle and SM, forward (512 x 128 x 1,152 in
 // bfloat16 146 us, 75.5 M elements: 100 us of it), issue backward (288 us; 166 instructions per pair of elements), HBM in
 // the single token (16,384 x 1,152 rows 53 us, 302 MB, 5.7 TB/s).  A prompt of 8,192 steps of one row and 2,048 channels
-// takes 82 us, two passes of segments; 64 single tokens take 12 us, the host's part.
+// takes 75 us, two passes of segments; 64 single tokens take 12 us, the host's part.
 #include <new>
 #include <type_traits>
 
@@ -217,7 +217,7 @@ struct Block {
 
 // kEnds: the first pass over segments.
 template <typename T, int V, bool kEnds>
-__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 && !kEnds ? 5 : 1)
+__global__ void __launch_bounds__(kThreads, sizeof(T) != 2 ? 1 : kEnds ? 4 : 5)
 k_forward(const Shape s, const Params<T> p)
 {
     using F = Vals<V>;
@@ -289,47 +289,68 @@ k_forward(const Shape s, const Params<T> p)
 }
 
 // Chains the segments of a row: each end is replaced by the value that enters the segment.  From the first segment on
-// (forward: states) or from the last one back (gradients).
+// (forward: states) or from the last one back (gradients).  A block takes 32 channels; its warps take a run of segments each, find
+// what it makes of a zero, chain the runs before theirs and go through their own again.
 constexpr int kAhead = 16;
-constexpr int kCarryThreads = 64;
+constexpr int kCarryWarps = 16;          // at most
 
-__global__ void __launch_bounds__(kCarryThreads)
+// The value behind a segment, or a run of them: `end` is what a zero became, L the sum of its logarithms (positive: a reset).
+__device__ __forceinline__ float carried(float h, float end, float L)
+{
+    return L > 0.0f ? end : decayed(decay_less_one(L), h) + end;
+}
+
+__global__ void __launch_bounds__(32 * kCarryWarps)
 k_carry(const Shape s, float *carry, const float *span, const float *start, const int backward)
 {
+    __shared__ float s_end[kCarryWarps][32], s_span[kCarryWarps][32];
     allow_next();
     wait_for_previous();
-    const int64_t index = static_cast<int64_t>(blockIdx.x) * kCarryThreads + threadIdx.x;
-    if (index >= s.batch * s.channels) return;
-    const int64_t b = index / s.channels;
-    const int c = static_cast<int>(index - b * s.channels);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int tiles = (s.channels + 31) / 32;
+    const int64_t b = blockIdx.x / tiles;
+    const int c = static_cast<int>(blockIdx.x % tiles) * 32 + lane;
+    const bool live = c < s.channels;
+    const int64_t index = b * s.channels + (live ? c : 0);
     const int64_t step = backward ? -s.channels : s.channels;
-    int64_t at = b * s.segments * s.channels + c + (backward ? static_cast<int64_t>(s.segments - 1) * s.channels : 0);
-    float h = start == nullptr ? 0.0f : start[index];
-    float end[2][kAhead], sum[2][kAhead];
-    auto fetch = [&](int from, int64_t first, float (&e)[kAhead], float (&l)[kAhead]) {
+    const int64_t base = b * s.segments * s.channels + (live ? c : 0) + (backward ? static_cast<int64_t>(s.segments - 1) * s.channels : 0);
+    const int per = (s.segments + warps - 1) / warps, first = min(warp * per, s.segments), last = min(first + per, s.segments);
+    float end[kAhead] = {}, sum[kAhead] = {};
+    auto fetch = [&](int from) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const bool in = from + k < s.segments;
-            e[k] = in ? carry[first + k * step] : 0.0f;
-            l[k] = in ? span[first + k * step] : 0.0f;
+            const bool in = from + k < last;
+            end[k] = in ? carry[base + (from + k) * step] : 0.0f;
+            sum[k] = in ? span[base + (from + k) * step] : 0.0f;
         }
     };
-    auto chain = [&](int from, const float (&e)[kAhead], const float (&l)[kAhead]) {
+    float h = 0.0f, L = 0.0f;
+    bool cut = false;
+    if (per <= kAhead) fetch(first);
+    if (warp + 1 < warps) {                              // (nobody asks for the last run)
+        for (int g = first; g < last; g += kAhead) {
+            if (per > kAhead) fetch(g);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {           // (a segment that is not there: nothing changes)
+                h = carried(h, end[k], sum[k]);
+                cut = cut || sum[k] > 0.0f;
+                L += sum[k];
+            }
+        }
+    }
+    s_end[warp][lane] = h;
+    s_span[warp][lane] = cut ? 1.0f : L;
+    __syncthreads();
+    h = start == nullptr ? 0.0f : start[index];
+    for (int w = 0; w < warp; ++w) h = carried(h, s_end[w][lane], s_span[w][lane]);
+    for (int g = first; g < last; g += kAhead) {
+        if (per > kAhead) fetch(g);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            if (from + k >= s.segments) break;
-            carry[at] = h;
-            at += step;
-            const float d = decay_less_one(l[k]);
-            h = l[k] > 0.0f ? e[k] : decayed(d, h) + e[k];
+            if (g + k >= last) break;
+            if (live) carry[base + (g + k) * step] = h;
+            h = carried(h, end[k], sum[k]);
         }
-    };
-    fetch(0, at, end[0], sum[0]);
-    for (int g = 0; g < s.segments; g += 2 * kAhead) {       // the next ones are under way while these are chained
-        fetch(g + kAhead, at + kAhead * step, end[1], sum[1]);
-        chain(g, end[0], sum[0]);
-        fetch(g + 2 * kAhead, at + kAhead * step, end[0], sum[0]);
-        chain(g + kAhead, end[1], sum[1]);
     }
 }
 
@@ -548,8 +569,8 @@ bool sizes_ok(int64_t batch, int64_t time) { return batch >= 1 && time >= 1 && b
 // The cut of the time axis, for warps of 64 channels, by what it would take in nanoseconds.  A warp by itself goes through eight
 // steps in about 1,000 forward and 1,900 backward (800 in the pass that looks for a segment's end); the device through
 // 500 elements a nanosecond forward, 260 backward (700), however they are cut.  Chaining costs two more launches and
-// about 100 per segment.  (3 x 777 x 331 in binary32: forward 69 us uncut, 14.5 in 32 segments, 20.7 in 97; 64 x 512 x 512 in
-// bfloat16: 70 uncut, 80 in 5; backward 134 and 104.)
+// about 20 per segment.  (In bfloat16, 1 x 8,192 x 1,024: forward 43 us in 171 segments, 62 in 94; 64 x 512 x 512: 62 uncut,
+// 78 in 5; backward 133 and 104.)
 Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool backward)
 {
     Shape s = {};
@@ -565,7 +586,7 @@ Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool back
             const double alone = chain * steps8, all = elements / rate;
             return alone > all ? alone + 0.5 * all : all + 0.5 * alone;
         };
-        return (backward ? pass(1900, 260) : pass(1000, 500)) + (!ends ? 0 : backward ? pass(800, 700) : 0.85 * pass(1000, 500));
+        return (backward ? pass(1900, 260) : pass(1000, 500)) + (!ends ? 0 : backward ? pass(800, 700) : 0.9 * pass(1000, 500));
     };
     s.segments = 1;
     s.segment_steps = static_cast<int>(chunks * kSteps);
@@ -574,7 +595,7 @@ Shape shape_of(const gated_recurrence *p, int64_t batch, int64_t time, bool back
     auto consider = [&](int64_t n) {
         if (n < 2 || n > chunks) return;
         const int64_t per = div_up(chunks, n), segments = div_up(chunks, per);
-        const double cost = passes(per * div_up(segments * warps, resident), true) + 5000 + 100.0 * segments;
+        const double cost = passes(per * div_up(segments * warps, resident), true) + 6000 + 20.0 * segments;
         if (cost >= best) return;
         best = cost;
         s.segments = static_cast<int>(segments);
@@ -692,13 +713,16 @@ int launch(gated_recurrence *p, const Shape &s, const Params<T> &k, bool backwar
 {
     const int64_t tiles = div_up(s.channels, 32 * V), units = s.batch * s.segments;
     const int64_t blocks = div_up(units * tiles, kWarps);
-    if (blocks > kMaxBlocks || div_up(s.batch * s.channels, kCarryThreads) > kMaxBlocks) return GATED_RECURRENCE_EINVAL;
+    const int64_t chains = s.batch * div_up(s.channels, 32);
+    if (blocks > kMaxBlocks || chains > kMaxBlocks) return GATED_RECURRENCE_EINVAL;
     bool ok = true;
     int launched = 0;
+    // with few segments one warp has them all in its registers
+    const int64_t carry_warps = s.segments <= kAhead ? 1 : s.segments > 8 * kCarryWarps ? kCarryWarps : div_up(s.segments, 8);
     if (s.segments > 1) {
         ok = backward ? (k_backward<T, V, true><<<static_cast<unsigned>(blocks), kThreads, 0, p->stream>>>(s, k), cudaGetLastError() == cudaSuccess)
                       : (k_forward<T, V, true><<<static_cast<unsigned>(blocks), kThreads, 0, p->stream>>>(s, k), cudaGetLastError() == cudaSuccess);
-        ok = ok && launch_after(p->stream, div_up(s.batch * s.channels, kCarryThreads), kCarryThreads, k_carry, s, k.carry,
+        ok = ok && launch_after(p->stream, chains, static_cast<unsigned>(32 * carry_warps), k_carry, s, k.carry,
                                 static_cast<const float *>(k.span), backward ? k.dstate_out : k.state, backward ? 1 : 0);
         launched += 2;
     }

@@ -179,6 +179,15 @@ def test_sequence_and_gradients(torch, case):
     assert all(torch.equal(again[2][k], g[k]) for k in g if g[k] is not None)
 
 
+@pytest.mark.parametrize("case", [(1, 16000, 64, "bfloat16", "batch", 0, True), (1, 16000, 40, "float32", "batch", 0.0005, True),
+                                  (2, 9000, 70, "float16", "time", 0.001, True), (1, 9000, 300, "bfloat16", "wide", 0, False)], ids=str)
+def test_many_segments(torch, case):
+    """Long rows in few channels, cut into so many segments that runs of them are chained, with and without resets."""
+    batch, time, ch, dtype, layout, reset, carry = case
+    dev, val = make(torch, 10 + time, batch, time, ch, dtype, layout, reset, carry)
+    check_all(torch, gated_recurrence.GatedRecurrence(ch, dtype=getattr(torch, dtype)), dev, val, dtype)
+
+
 def test_single_tokens_are_the_sequence(torch):
     """Step by step from the same state, in place, with the flags of the sequence: the same states bit for bit where the
     sequence is in one piece."""
