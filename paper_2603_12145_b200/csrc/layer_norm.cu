@@ -264,8 +264,9 @@ k_forward(const Forward<T> p)
     };
     fetch(turns.first);
     // The parameters stay in registers where there is room (bfloat16, no residual: 65,536 x 256 14.7 against 18.7 us, 32,768 x 1,032 33
-    // against 41); blocks that share a binary32 row lose warps by it (8,192 x 4,096 51 against 49).
-    constexpr bool kHeld = V > 1 && C * V + R <= (sizeof(T) == 2 ? 24 : kWide ? 0 : 18);
+    // against 41; of single elements 65,536 x 577 120 against 157); blocks that share a binary32 row lose warps by it (8,192 x 4,096
+    // 51 against 49).
+    constexpr bool kHeld = V == 1 ? C <= 8 : C * V + R <= (sizeof(T) == 2 ? 24 : kWide ? 0 : 18);
     U held_w[kHeld ? M::kUnits : 1], held_b[kHeld ? M::kUnits : 1];
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
@@ -380,8 +381,8 @@ k_backward(const Backward<T> p)
     fetch(turns.first);
     // The weights take a third of the accesses if every row fetches them: in registers where there is room, that is, not in
     // blocks for rows of binary32 (bfloat16: 65,536 x 576 61 against 73 us, 8,192 x 8,192 98 against 131; binary32: 32,768 x 512
-    // 49 against 54, but 16,384 x 1,024 75 against 67.)
-    constexpr bool kHeld = V > 1 && (sizeof(T) == 2 || !kWide);
+    // 49 against 54, but 16,384 x 1,024 75 against 67; single elements: 16,384 x 1,003 64 against 81.)
+    constexpr bool kHeld = V == 1 ? C <= 8 : sizeof(T) == 2 || !kWide;
     U held[kHeld ? M::kUnits : 1];
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
