@@ -5,7 +5,8 @@
 // 16 bytes (binary32: 128) belongs to 4 to 32 lanes of a warp, which reduce by shuffles; a wider one to a block, whose warps
 // exchange their sums through shared memory with one barrier per reduction (two alternating slots).  Of R threads each holds
 // the vectors index, index + R, ..., so that a warp's access is contiguous.  Blocks go through several rows, as many as fit on
-// the device at once, and the next row's loads are in flight while a row is reduced.
+// the device at once, and the next row's loads are in flight while a row is reduced.  Rows that do not begin on boundaries of
+// 16 bytes are read between these or by single elements (offered()).
 //
 // The backward kernel keeps dw and db of its thread's columns in registers over all its rows: per row only the two sums of dx
 // cross threads.  The row groups of a warp are added by exchanges, a block's warps in shared memory, blocks leave a row of
@@ -28,6 +29,10 @@ using namespace vals;
 
 // Who shares a row: lanes of a warp, a block of up to 256 threads, a block of kMost.
 enum Form { kLanes, kBlock, kLargest };
+// How a row lies in its threads' accesses: some have none in the last round, all have all, or the row begins and ends inside an
+// access (kShifted: at any alignment that all arrays share; the rows of a thread are a multiple of a vector's elements apart, so that
+// all begin alike and its columns stay the same).
+enum Fit { kSome, kAll, kShifted };
 constexpr int kNarrowThreads = 128;      // block of the kernels whose rows belong to lanes of a warp
 constexpr int kMost = 512;               // threads that share a wide row, at most
 
@@ -49,6 +54,7 @@ struct Forward {
     float2 *saved;
     int64_t n;
     int width, lanes;
+    int shift, turn;         // kShifted: elements from a boundary to the first row, and from row to row, modulo a vector
     float eps;
 };
 
@@ -61,6 +67,7 @@ struct Backward {
     float *part;             // [blocks][2][width], or nullptr: no dw, db
     int64_t n;
     int width, lanes;
+    int shift, turn;
 };
 
 // Sums over the threads that share a row: R lanes, or the block.
@@ -129,12 +136,12 @@ struct Team {
 // round of these and the parameters read once (bfloat16 without residual: 8,192 x 8,192 51 against 70 us, 65,536 x 256
 // 12.4 against 14.4, x 576 30 against 34; binary32 is near memory's rate with one, 65,536 x 512 46 and 47 us).  24 elements only
 // where no access is masked and no barrier waits: x 768 41 against 43, but x 696 43 against 40, 32,768 x 1,032 43 against 33.
-template <typename T, int V, int C, int R, Form kForm, bool kAll>
-constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && C * V + R <= (kForm == kLanes && kAll ? 24 : 20) ? 2 : 1;
+template <typename T, int V, int C, int R, Form kForm, Fit kFit>
+constexpr int kRowsOf = sizeof(T) == 2 && V > 1 && kFit != kShifted && C * V + R <= (kForm == kLanes && kFit == kAll ? 24 : 20) ? 2 : 1;
 // Backward by lanes of a warp likewise (65,536 x 576 with dsum 55.5 against 59.4 us, x 256 24.6 against 26.7); a block's threads
 // have no registers for it.
-template <typename T, int V, int C, int R, Form kForm, bool kAll>
-constexpr int kBackwardRowsOf = kForm == kLanes ? kRowsOf<T, V, C, R, kForm, kAll> : 1;
+template <typename T, int V, int C, int R, Form kForm, Fit kFit>
+constexpr int kBackwardRowsOf = kForm == kLanes ? kRowsOf<T, V, C, R, kForm, kFit> : 1;
 
 // Units of one or two neighbouring parameters (from L1: every row reads them)
 template <int W, int N>
@@ -162,8 +169,8 @@ __device__ __forceinline__ void store_unit(float *dst, float v) { *dst = v; }
 __device__ __forceinline__ void store_unit(float *dst, Pair v) { *reinterpret_cast<float2 *>(dst) = make_float2(lo(v), hi(v)); }
 
 // A thread's share of a row: C accesses of V elements, index, index + size, ... of the row's `vectors`, and R elements of the rest
-// behind C * size vectors.  kAll: every thread has all of its accesses.
-template <typename T, int V, int C, int R, bool kAll>
+// behind C * size vectors.
+template <typename T, int V, int C, int R, Fit kFit>
 struct Mine {
     static constexpr int W = V == 1 ? 1 : 2, N = (V + 1) / 2, kUnits = C * N + R / 2;
     using Unit = Vals<W>;
@@ -190,35 +197,89 @@ struct Mine {
     };
 
     int size, index, vectors;
+    int shift, width;                    // (kShifted)
+
+    // The share of the rows that begin `first`, `first` + a multiple of V, ... rows behind the first one.
+    template <typename P>
+    static __device__ __forceinline__ Mine of(int size, int index, const P &p, int64_t first)
+    {
+        if (kFit != kShifted) return {size, index, p.width / V, 0, p.width};
+        const int shift = (p.shift + static_cast<int>(first % V) * p.turn) % V;
+        return {size, index, (shift + p.width + V - 1) / V, shift, p.width};
+    }
+    // The access that begins with element `at` has elements [from, to) of the row.
+    __device__ __forceinline__ int from(int at) const { return kFit == kShifted ? max(0, -at) : 0; }
+    __device__ __forceinline__ int to(int at) const { return kFit == kShifted ? min(V, width - at) : V; }
+    __device__ __forceinline__ bool partial(int at) const { return kFit == kShifted && (at < 0 || at + V > width); }
 
     // f(first unit, how many, the element that they begin with, whether they are there) for each access
     template <typename F>
     __device__ __forceinline__ void each_access(F f) const
     {
 #pragma unroll
-        for (int c = 0; c < C; ++c) f(c * N, std::integral_constant<int, N>{}, (c * size + index) * V, kAll || c * size + index < vectors);
+        for (int c = 0; c < C; ++c)
+            f(c * N, std::integral_constant<int, N>{}, (c * size + index) * V - (kFit == kShifted ? shift : 0), kFit == kAll || c * size + index < vectors);
         if constexpr (R > 0) f(C * N, std::integral_constant<int, R / 2>{}, C * size * V + index * R, true);
     }
-    // zeros where there is nothing
-    __device__ __forceinline__ Words load(const T *row) const
+    // Zeros where there is nothing.  kShifted: what lies beside the row comes along until trim(), but not of the first and the
+    // last row (`outer`), where it may be outside the array.
+    __device__ __forceinline__ Words load(const T *row, bool outer) const
     {
         Words w;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int i = c * size + index;
-            w.v[c] = kAll || i < vectors ? packed_load<T, V>(row + i * V) : packed_zero<T, V>();
+            const int i = c * size + index, at = i * V - (kFit == kShifted ? shift : 0);
+            if (kFit != kAll && i >= vectors) w.v[c] = packed_zero<T, V>();
+            else w.v[c] = one_access(row, at, outer);
         }
         if constexpr (R > 0) w.rest = packed_load<T, R>(row + C * size * V + index * R);
         return w;
+    }
+    __device__ __forceinline__ Packed<T, V> one_access(const T *row, int at, bool outer) const
+    {
+        if constexpr (kFit == kShifted)
+            if (outer && partial(at)) return packed_load_part<T, V>(row + at, from(at), to(at));
+        return packed_load<T, V>(row + at);
+    }
+    __device__ __forceinline__ void trim(Words &w) const
+    {
+        if constexpr (kFit == kShifted) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int at = (c * size + index) * V - shift;
+                if (partial(at)) packed_trim<T, V>(w.v[c], from(at), to(at));
+            }
+        }
     }
     __device__ __forceinline__ void store(T *row, const Words &w) const
     {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int i = c * size + index;
-            if (kAll || i < vectors) packed_store<T, V>(row + i * V, w.v[c]);
+            const int i = c * size + index, at = i * V - (kFit == kShifted ? shift : 0);
+            if (kFit == kAll || i < vectors) store_access(row, at, w.v[c]);
         }
         if constexpr (R > 0) packed_store<T, R>(row + C * size * V + index * R, w.rest);
+    }
+    template <int E>
+    __device__ __forceinline__ void store_access(T *row, int at, const Packed<T, E> &v) const
+    {
+        if constexpr (kFit == kShifted)
+            if (partial(at)) return packed_store_part<T, V>(row + at, v, from(at), to(at));
+        packed_store<T, E>(row + at, v);
+    }
+    // Units of parameters that stay in registers: `absent` where there are none.
+    template <int E>
+    __device__ __forceinline__ void params(Unit (&dst)[E], const float *src, int at, bool in, float absent) const
+    {
+        if constexpr (kFit == kShifted) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                auto one = [&](int e) { return src != nullptr && in && e >= 0 && e < width ? __ldg(src + e) : absent; };
+                dst[i] = pair(one(at + 2 * i), one(at + 2 * i + 1));
+            }
+        } else {
+            load_params<W>(dst, src != nullptr && in ? src + at : nullptr, absent);
+        }
     }
 };
 
@@ -235,12 +296,12 @@ struct Turns {
     }
 };
 
-template <typename T, int V, int C, int R, Form kForm, bool kAll>
+template <typename T, int V, int C, int R, Form kForm, Fit kFit>
 __global__ void __launch_bounds__(kForm == kLargest ? kMost : kForm == kBlock ? kMost / 2 : kNarrowThreads)
 k_forward(const Forward<T> p)
 {
     constexpr bool kWide = kForm != kLanes;
-    using M = Mine<T, V, C, R, kAll>;
+    using M = Mine<T, V, C, R, kFit>;
     using U = typename M::Unit;
     constexpr int W = M::W;
     __shared__ float2 s_sum[kWide ? 2 * (kMost / 32) : 1];
@@ -248,18 +309,20 @@ k_forward(const Forward<T> p)
     team.size = kWide ? static_cast<int>(blockDim.x) : p.lanes;
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
-    const M mine = {team.size, team.index, p.width / V};
-    constexpr int kRows = kRowsOf<T, V, C, R, kForm, kAll>;
+    constexpr int kRows = kRowsOf<T, V, C, R, kForm, kFit>;
     const Turns turns = Turns::of<kWide>(p.lanes, kRows);
+    const M mine = M::of(team.size, team.index, p, turns.first);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.residual.ptr != nullptr;
-    typename M::Words nx[kRows], nr[kRows];
+    typename M::Words nx[kRows] = {}, nr[kRows] = {};
     auto fetch = [&](int64_t first) {        // behind the last row that one again: no zeros to be put in place
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
+            if (kFit == kShifted && first + r >= p.n) return;          // (that one may lie otherwise)
             const int64_t row = first + r < p.n ? first + r : p.n - 1;
-            nx[r] = mine.load(p.x.row(row));
-            if (added) nr[r] = mine.load(p.residual.row(row));
+            const bool outer = row == 0 || row + 1 == p.n;
+            nx[r] = mine.load(p.x.row(row), outer);
+            if (added) nr[r] = mine.load(p.residual.row(row), outer);
         }
     };
     fetch(turns.first);
@@ -271,8 +334,8 @@ k_forward(const Forward<T> p)
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
             U w[n.value], b[n.value];
-            load_params<W>(w, p.w != nullptr && in ? p.w + at : nullptr, 1.0f);
-            load_params<W>(b, p.b != nullptr && in ? p.b + at : nullptr, 0.0f);
+            mine.params(w, p.w, at, in, 1.0f);
+            mine.params(b, p.b, at, in, 0.0f);
 #pragma unroll
             for (int i = 0; i < n.value; ++i) {
                 held_w[u0 + i] = w[i];
@@ -290,6 +353,7 @@ k_forward(const Forward<T> p)
                 for (int u = 0; u < M::kUnits; ++u) nx[r].set(u, add(nx[r].get(u), nr[r].get(u)));     // rounded to the type
                 if (row + r < p.n) mine.store(p.sum.row(row + r), nx[r]);
             }
+            mine.trim(nx[r]);
             U sum = all<W>(0.0f);
 #pragma unroll
             for (int u = 0; u < M::kUnits; ++u) {
@@ -304,13 +368,20 @@ k_forward(const Forward<T> p)
         for (int r = 0; r < kRows; ++r) {
             mean[r] *= inverse;
             U square = all<W>(0.0f);
-            mine.each_access([&](int u0, auto n, int, bool in) {
+            mine.each_access([&](int u0, auto n, int at, bool in) {
                 if (!in) return;
 #pragma unroll
-                for (int i = 0; i < n.value; ++i) {
-                    s[r][u0 + i] = add(s[r][u0 + i], all<W>(-mean[r]));
-                    square = fma(s[r][u0 + i], s[r][u0 + i], square);
+                for (int i = 0; i < n.value; ++i) s[r][u0 + i] = add(s[r][u0 + i], all<W>(-mean[r]));
+                if (mine.partial(at)) {                  // (nothing beside the row)
+                    const int from = mine.from(at), to = mine.to(at);
+                    if constexpr (kFit == kShifted) {
+#pragma unroll
+                        for (int i = 0; i < n.value; ++i)
+                            s[r][u0 + i] = pair(2 * i >= from && 2 * i < to ? lo(s[r][u0 + i]) : 0.0f, 2 * i + 1 >= from && 2 * i + 1 < to ? hi(s[r][u0 + i]) : 0.0f);
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < n.value; ++i) square = fma(s[r][u0 + i], s[r][u0 + i], square);
             });
             scale[r] = sum_of(square);
         }
@@ -337,18 +408,18 @@ k_forward(const Forward<T> p)
                 }
 #pragma unroll
                 for (int i = 0; i < n.value; ++i) narrow_at(out, i, fma(mul(s[r][u0 + i], all<W>(scale[r])), w[i], b[i]));
-                packed_store<T, W * n.value>(py + at, out);
+                mine.store_access(py, at, out);
             });
         }
     }
 }
 
-template <typename T, int V, int C, int R, Form kForm, bool kAll>
+template <typename T, int V, int C, int R, Form kForm, Fit kFit>
 __global__ void __launch_bounds__(kForm == kLanes || (V == 8 && C == 3) ? kNarrowThreads : kForm == kBlock ? kMost / 2 : kMost)
 k_backward(const Backward<T> p)
 {
     constexpr bool kWide = kForm != kLanes;
-    using M = Mine<T, V, C, R, kAll>;
+    using M = Mine<T, V, C, R, kFit>;
     using U = typename M::Unit;
     constexpr int W = M::W;
     extern __shared__ float s_part[];                      // narrow rows: [warps][2][width], the sums of a warp's row groups
@@ -358,24 +429,26 @@ k_backward(const Backward<T> p)
     team.size = kWide ? static_cast<int>(blockDim.x) : p.lanes;
     team.index = static_cast<int>(threadIdx.x) & (team.size - 1);
     team.shared = s_sum;
-    const M mine = {team.size, team.index, p.width / V};
-    constexpr int kRows = kBackwardRowsOf<T, V, C, R, kForm, kAll>;
+    constexpr int kRows = kBackwardRowsOf<T, V, C, R, kForm, kFit>;
     const Turns turns = Turns::of<kWide>(p.lanes, kRows);
+    const M mine = M::of(team.size, team.index, p, turns.first);
     const float inverse = 1.0f / static_cast<float>(p.width);
     const bool added = p.dsum.ptr != nullptr;
     U dw[M::kUnits], db[M::kUnits];
 #pragma unroll
     for (int u = 0; u < M::kUnits; ++u) dw[u] = db[u] = all<W>(0.0f);
-    typename M::Words ns[kRows], ndy[kRows], nd[kRows];
-    float2 nstat[kRows];
+    typename M::Words ns[kRows] = {}, ndy[kRows] = {}, nd[kRows] = {};
+    float2 nstat[kRows] = {};
     auto fetch = [&](int64_t first) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
+            if (kFit == kShifted && first + r >= p.n) return;
             const int64_t row = first + r < p.n ? first + r : p.n - 1;
             nstat[r] = __ldg(p.saved + row);
-            ns[r] = mine.load(p.s.row(row));
-            ndy[r] = mine.load(p.dy.row(row));
-            if (added) nd[r] = mine.load(p.dsum.row(row));
+            const bool outer = row == 0 || row + 1 == p.n;
+            ns[r] = mine.load(p.s.row(row), outer);
+            ndy[r] = mine.load(p.dy.row(row), outer);
+            if (added) nd[r] = mine.load(p.dsum.row(row), outer);
         }
     };
     fetch(turns.first);
@@ -387,7 +460,7 @@ k_backward(const Backward<T> p)
     if constexpr (kHeld) {
         mine.each_access([&](int u0, auto n, int at, bool in) {
             U w[n.value];
-            load_params<W>(w, p.w != nullptr && in ? p.w + at : nullptr, 1.0f);
+            mine.params(w, p.w, at, in, 1.0f);
 #pragma unroll
             for (int i = 0; i < n.value; ++i) held[u0 + i] = w[i];
         });
@@ -409,6 +482,8 @@ k_backward(const Backward<T> p)
             s[r] = ns[r];
             dy[r] = ndy[r];
             d[r] = nd[r];
+            mine.trim(s[r]);
+            mine.trim(dy[r]);
             mean[r] = nstat[r].x;
             scale[r] = nstat[r].y;
         }
@@ -452,7 +527,7 @@ k_backward(const Backward<T> p)
                     if (added) x = add(x, d[r].get(u));
                     narrow_at(out, i, x);
                 }
-                packed_store<T, W * n.value>(px + at, out);
+                mine.store_access(px, at, out);
             });
         }
     }
@@ -463,15 +538,25 @@ k_backward(const Backward<T> p)
             if (!in) return;
 #pragma unroll
             for (int i = 0; i < n.value; ++i) {
-                store_unit(to + at + W * i, dw[u0 + i]);
-                store_unit(to + p.width + at + W * i, db[u0 + i]);
+                if constexpr (kFit == kShifted) {
+                    auto one = [&](int e, float w, float b) {
+                        if (e < 0 || e >= p.width) return;
+                        to[e] = w;
+                        to[p.width + e] = b;
+                    };
+                    one(at + 2 * i, lo(dw[u0 + i]), lo(db[u0 + i]));
+                    one(at + 2 * i + 1, hi(dw[u0 + i]), hi(db[u0 + i]));
+                } else {
+                    store_unit(to + at + W * i, dw[u0 + i]);
+                    store_unit(to + p.width + at + W * i, db[u0 + i]);
+                }
             }
         });
     };
     if constexpr (kWide) {
         leave(part);
     } else {
-        // a warp's row groups by exchanges, the warps one after the other
+        // a warp's row groups by exchanges (kShifted: it has one), the warps one after the other
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         for (int o = 16; o >= team.size; o >>= 1) {
 #pragma unroll
@@ -535,7 +620,7 @@ struct Share {
 // elements (three in blocks of up to 128 threads, which have the registers) or four of four.  Single elements: up to 8 per
 // lane, then up to 8 (16 in the largest blocks).  Measured in bfloat16: 32,768 x 1,024 backward 57 us as blocks of 64
 // threads, 74 us as a warp with four vectors per lane.
-Share share_of(int vectors, int V)
+Share share_of(int vectors, int V, bool with_rest)
 {
     Share s = {4, 1, false, 0};
     while (s.lanes < 32 && s.lanes * (V > 1 ? 2 : 4) < vectors) s.lanes *= 2;
@@ -547,7 +632,7 @@ Share share_of(int vectors, int V)
     s.count = static_cast<int>(div_up(vectors, s.lanes));
     // a warp's last round would leave three or two of four lanes without work: the rest of 64 or 128 elements by twos or fours
     // (65,536 x 576 in bfloat16: 126 against 142 us forward and backward)
-    if (V == 8 && !s.wide && vectors > 32 && (vectors % 32 == 8 || vectors % 32 == 16)) {
+    if (with_rest && V == 8 && !s.wide && vectors > 32 && (vectors % 32 == 8 || vectors % 32 == 16)) {
         s.count = vectors / 32;
         s.rest = vectors % 32 / 4;
     }
@@ -561,19 +646,25 @@ using Count = std::integral_constant<int, N>;
 
 template <Form kForm>
 using Of = std::integral_constant<Form, kForm>;
+template <Fit kFit>
+using As = std::integral_constant<Fit, kFit>;
 
-// Calls f with V, C, R, the form of the kernel and kAll for this share of a row of `vectors`.  (kAll: bfloat16, 16,384 x 4,096 backward
-// 97 against 104 us.)
+// The accesses that a call's arrays allow: single elements, vectors of 16 bytes on their boundaries, or vectors on boundaries that the
+// rows begin and end between.
+enum Access { kSingle, kWhole, kBetween, kAccesses };
+
+// Calls f with V, C, R, the form of the kernel and how rows fit for this share of a row of `vectors`.  (kAll instead of kSome: bfloat16,
+// 16,384 x 4,096 backward 97 against 104 us.)
 template <typename T, typename F>
-bool with_counts(const Share &s, int vectors, bool whole, F f)
+bool with_counts(const Share &s, int vectors, Access access, F f)
 {
     using V = Count<16 / sizeof(T)>;
     using One = Count<1>;
     using None = Count<0>;
-    using Yes = std::true_type;
-    using No = std::false_type;
+    using No = As<kSome>;
+    using Yes = As<kAll>;
     const bool largest = s.lanes == kMost;
-    if (!whole) {
+    if (access == kSingle) {
         if (!s.wide) return s.count <= 4 ? f(One{}, Count<4>{}, None{}, Of<kLanes>{}, No{}) : f(One{}, Count<8>{}, None{}, Of<kLanes>{}, No{});
         if (s.count > 8) return f(One{}, Count<16>{}, None{}, Of<kLargest>{}, No{});
         return largest ? f(One{}, Count<8>{}, None{}, Of<kLargest>{}, No{}) : f(One{}, Count<8>{}, None{}, Of<kBlock>{}, No{});
@@ -597,16 +688,16 @@ bool with_counts(const Share &s, int vectors, bool whole, F f)
         if (s.count <= 1) return f(V{}, Count<1>{}, None{}, Of<kLanes>{}, all);
         return s.count == 2 ? f(V{}, Count<2>{}, None{}, Of<kLanes>{}, all) : f(V{}, Count<3>{}, None{}, Of<kLanes>{}, all);
     };
+    if constexpr (sizeof(T) == 2) {                      // (offered(): by whole warps and small blocks)
+        auto between = [&](auto form) {
+            return s.count <= 2 ? f(V{}, Count<2>{}, None{}, form, As<kShifted>{}) : f(V{}, Count<3>{}, None{}, form, As<kShifted>{});
+        };
+        if (access == kBetween) return s.wide ? between(Of<kBlock>{}) : between(Of<kLanes>{});
+    }
     return vectors == s.lanes * s.count ? with_count(Yes{}) : with_count(No{});
 }
 
 int element_bytes(int type) { return type == LAYER_NORM_F32 ? 4 : 2; }
-
-// Row starts on 16-byte boundaries (of a single row the stride does not matter).
-bool whole_rows(const void *ptr, int64_t stride, int64_t n, int bytes)
-{
-    return ptr == nullptr || (aligned(ptr, 16) && (n == 1 || stride * bytes % 16 == 0));
-}
 
 }  // namespace
 
@@ -614,52 +705,95 @@ struct layer_norm {
     int width = 0, type = 0;
     float eps = 0.0f;
     int device = 0, sms = 0;
-    int forward_blocks[2] = {0, 0}, backward_blocks[2] = {0, 0};     // that an SM holds; rows of single elements, of vectors
-    int backward_rows[2] = {1, 1};           // that a thread takes at a time
+    int forward_blocks[kAccesses] = {}, backward_blocks[kAccesses] = {};     // that an SM holds; none where rows are not read this way
+    int backward_rows[kAccesses] = {};       // that a thread takes at a time
     cudaStream_t stream = nullptr;
     int64_t launches = 0;
 };
 
 namespace {
 
-Share share_for(const layer_norm *p, bool whole)
+int vectors_of(const layer_norm *p, Access access)
 {
     const int V = 16 / element_bytes(p->type);
-    return whole ? share_of(p->width / V, V) : share_of(p->width, 1);
+    return access == kSingle ? p->width : access == kWhole ? p->width / V : (p->width + 2 * (V - 1)) / V;
+}
+
+Share share_for(const layer_norm *p, Access access)
+{
+    return share_of(vectors_of(p, access), access == kSingle ? 1 : 16 / element_bytes(p->type), access == kWhole);
+}
+
+// Whether rows of this width are read this way at all.  Between boundaries 16-bit rows of 257 to about 3,000 elements (65,536 x 577
+// in bfloat16 with residual 95 against 186 us forward, 127 against 223 backward; 32,768 x 1,501 81 and 111 against 198 and 236):
+// shorter ones are as fast by single elements (x 255 71 and 72 against 62 and 74), the backward pass of larger
+// blocks is slower (16,384 x 4,001 399 against 264), binary32 too (65,536 x 255 66 and 80 against 61 and 66).
+bool offered(const layer_norm *p, Access access)
+{
+    if (access == kWhole) return p->width % (16 / element_bytes(p->type)) == 0;
+    return access == kSingle || (p->type != LAYER_NORM_F32 && p->width > 256 && share_for(p, access).lanes <= kNarrowThreads);
 }
 
 size_t backward_smem(const layer_norm *p, const Share &s) { return s.wide ? 0 : kNarrowThreads / 32 * 2 * sizeof(float) * p->width; }
 
-// Whole rounds of resident blocks, so that all end together.
-int64_t blocks_for(const layer_norm *p, const Share &s, int64_t n, int per_sm, int rows = 1)
+// Whole rounds of resident blocks, so that all end together.  Between boundaries, the rows of a thread begin alike: as many blocks as
+// make its rows whole vectors' elements apart, unless it has one row.
+int64_t blocks_for(const layer_norm *p, Access access, int64_t n, int per_sm, int rows)
 {
-    const int64_t units = div_up(n, static_cast<int64_t>(s.wide ? 1 : kNarrowThreads / s.lanes) * rows);
-    return div_up(units, div_up(units, static_cast<int64_t>(p->sms) * per_sm));
+    const Share s = share_for(p, access);
+    const int64_t per_block = static_cast<int64_t>(s.wide ? 1 : kNarrowThreads / s.lanes) * rows;
+    const int64_t units = div_up(n, per_block), blocks = div_up(units, div_up(units, static_cast<int64_t>(p->sms) * per_sm));
+    if (access != kBetween || blocks == units) return blocks;
+    const int64_t V = 16 / element_bytes(p->type), alike = per_block >= V ? 1 : V / per_block;
+    return div_up(blocks, alike) * alike;
 }
 
-int64_t backward_blocks(const layer_norm *p, int64_t n, bool whole)
+int64_t backward_blocks(const layer_norm *p, int64_t n, Access access)
 {
-    return blocks_for(p, share_for(p, whole), n, p->backward_blocks[whole], p->backward_rows[whole]);
+    return blocks_for(p, access, n, p->backward_blocks[access], p->backward_rows[access]);
 }
 
 template <typename T>
 bool count_blocks(layer_norm *p)
 {
-    for (int whole = 0; whole < 2; ++whole) {
-        if (whole && p->width % (16 / sizeof(T)) != 0) continue;
-        const Share s = share_for(p, whole);
+    for (const Access access : {kSingle, kWhole, kBetween}) {
+        if (!offered(p, access)) continue;
+        const Share s = share_for(p, access);
         const int threads = s.wide ? s.lanes : kNarrowThreads;
-        const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-            p->backward_rows[whole] = kBackwardRowsOf<T, v.value, c.value, r.value, form.value, all.value>;
-            return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[whole], k_forward<T, v.value, c.value, r.value, form.value, all.value>,
+        const bool ok = with_counts<T>(s, vectors_of(p, access), access, [&](auto v, auto c, auto r, auto form, auto fit) {
+            p->backward_rows[access] = kBackwardRowsOf<T, v.value, c.value, r.value, form.value, fit.value>;
+            return cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->forward_blocks[access], k_forward<T, v.value, c.value, r.value, form.value, fit.value>,
                                                                  threads, 0) == cudaSuccess &&
-                   cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[whole], k_backward<T, v.value, c.value, r.value, form.value, all.value>,
+                   cudaOccupancyMaxActiveBlocksPerMultiprocessor(&p->backward_blocks[access], k_backward<T, v.value, c.value, r.value, form.value, fit.value>,
                                                                  threads, backward_smem(p, s)) == cudaSuccess;
         });
-        if (!ok || p->forward_blocks[whole] < 1 || p->backward_blocks[whole] < 1) return false;
+        if (!ok || p->forward_blocks[access] < 1 || p->backward_blocks[access] < 1) return false;
     }
     return true;
 }
+
+// How a call's arrays can be read.  add() takes each; single(): a parameter that is not on a boundary.
+struct Lie {
+    const layer_norm *p;
+    int64_t n;
+    int bytes, shift = -1, turn = 0;
+    bool whole = true, alike = true;
+    void add(const void *ptr, int64_t stride)
+    {
+        if (ptr == nullptr) return;
+        const int V = 16 / bytes;
+        const int at = static_cast<int>(reinterpret_cast<uintptr_t>(ptr) / bytes % V), step = n == 1 ? 0 : static_cast<int>(stride % V);
+        whole = whole && at == 0 && step == 0;
+        alike = alike && (n == 1 || stride >= V) && (shift < 0 || (at == shift && step == turn));
+        shift = at;
+        turn = step;
+    }
+    Access access(bool params_whole) const
+    {
+        if (whole && params_whole && offered(p, kWhole)) return kWhole;
+        return alike && offered(p, kBetween) ? kBetween : kSingle;
+    }
+};
 
 bool check_in(const void *ptr, int64_t stride, int bytes, int *rc)
 {
@@ -681,14 +815,13 @@ template <typename T>
 Rows<T> out_rows(void *ptr, int64_t stride) { return {static_cast<T *>(ptr), stride}; }
 
 template <typename T>
-int run_forward(layer_norm *p, Forward<T> f, bool whole)
+int run_forward(layer_norm *p, Forward<T> f, Access access)
 {
-    whole = whole && p->width % (16 / sizeof(T)) == 0;
-    const Share s = share_for(p, whole);
+    const Share s = share_for(p, access);
     f.lanes = s.lanes;
-    const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-        const int64_t blocks = blocks_for(p, s, f.n, p->forward_blocks[whole], kRowsOf<T, v.value, c.value, r.value, form.value, all.value>);
-        k_forward<T, v.value, c.value, r.value, form.value, all.value>
+    const bool ok = with_counts<T>(s, vectors_of(p, access), access, [&](auto v, auto c, auto r, auto form, auto fit) {
+        const int64_t blocks = blocks_for(p, access, f.n, p->forward_blocks[access], kRowsOf<T, v.value, c.value, r.value, form.value, fit.value>);
+        k_forward<T, v.value, c.value, r.value, form.value, fit.value>
             <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, 0, p->stream>>>(f);
         return cudaGetLastError() == cudaSuccess;
     });
@@ -698,15 +831,14 @@ int run_forward(layer_norm *p, Forward<T> f, bool whole)
 }
 
 template <typename T>
-int run_backward(layer_norm *p, Backward<T> b, bool whole, float *dw, float *db)
+int run_backward(layer_norm *p, Backward<T> b, Access access, float *dw, float *db)
 {
-    whole = whole && p->width % (16 / sizeof(T)) == 0;
-    const Share s = share_for(p, whole);
+    const Share s = share_for(p, access);
     b.lanes = s.lanes;
-    const int64_t blocks = backward_blocks(p, b.n, whole);
+    const int64_t blocks = backward_blocks(p, b.n, access);
     const size_t smem = backward_smem(p, s);
-    const bool ok = with_counts<T>(s, whole ? p->width * static_cast<int>(sizeof(T)) / 16 : p->width, whole, [&](auto v, auto c, auto r, auto form, auto all) {
-        k_backward<T, v.value, c.value, r.value, form.value, all.value>
+    const bool ok = with_counts<T>(s, vectors_of(p, access), access, [&](auto v, auto c, auto r, auto form, auto fit) {
+        k_backward<T, v.value, c.value, r.value, form.value, fit.value>
             <<<static_cast<unsigned>(blocks), s.wide ? s.lanes : kNarrowThreads, smem, p->stream>>>(b);
         return cudaGetLastError() == cudaSuccess;
     });
@@ -746,10 +878,14 @@ int forward_of(layer_norm *p, const void *x, int64_t x_stride, const void *resid
     f.n = n;
     f.width = p->width;
     f.eps = p->eps;
-    const int e = sizeof(T);
-    const bool whole = whole_rows(x, x_stride, n, e) && whole_rows(residual, residual_stride, n, e) &&
-                       whole_rows(sum, sum_stride, n, e) && whole_rows(y, y_stride, n, e) && aligned(w, 16) && aligned(b, 16);
-    return run_forward<T>(p, f, whole);
+    Lie lie = {p, n, sizeof(T)};
+    lie.add(x, x_stride);
+    lie.add(residual, residual_stride);
+    lie.add(sum, sum_stride);
+    lie.add(y, y_stride);
+    f.shift = lie.shift;
+    f.turn = lie.turn;
+    return run_forward<T>(p, f, lie.access(aligned(w, 16) && aligned(b, 16)));
 }
 
 template <typename T>
@@ -767,10 +903,14 @@ int backward_of(layer_norm *p, const void *dy, int64_t dy_stride, const void *s,
     f.part = dw != nullptr ? static_cast<float *>(workspace) : nullptr;
     f.n = n;
     f.width = p->width;
-    const int e = sizeof(T);
-    const bool whole = whole_rows(dy, dy_stride, n, e) && whole_rows(s, s_stride, n, e) && whole_rows(dsum, dsum_stride, n, e) &&
-                       whole_rows(dx, dx_stride, n, e) && aligned(w, 16);
-    return run_backward<T>(p, f, whole, dw, db);
+    Lie lie = {p, n, sizeof(T)};
+    lie.add(dy, dy_stride);
+    lie.add(s, s_stride);
+    lie.add(dsum, dsum_stride);
+    lie.add(dx, dx_stride);
+    f.shift = lie.shift;
+    f.turn = lie.turn;
+    return run_backward<T>(p, f, lie.access(aligned(w, 16)), dw, db);
 }
 
 bool rows_ok(int64_t n) { return n >= 1 && n <= 0x7FFFFFFF; }
@@ -839,11 +979,12 @@ int layer_norm_forward(layer_norm *p, const void *x, int64_t x_stride, const voi
 size_t layer_norm_workspace_bytes(const layer_norm *p, int64_t n)
 {
     if (p == nullptr || !rows_ok(n)) return 0;
-    // rows of whole vectors and others are shared out differently: room for either
-    int64_t rows = backward_blocks(p, n, false);
-    if (p->backward_blocks[1] > 0) {
-        const int64_t other = backward_blocks(p, n, true);
-        if (other > rows) rows = other;
+    // rows are shared out by how they lie: room for each way
+    int64_t rows = 0;
+    for (const Access access : {kSingle, kWhole, kBetween}) {
+        if (p->backward_blocks[access] < 1) continue;
+        const int64_t blocks = backward_blocks(p, n, access);
+        if (blocks > rows) rows = blocks;
     }
     return static_cast<size_t>(rows) * 2 * p->width * sizeof(float);
 }

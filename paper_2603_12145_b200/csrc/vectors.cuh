@@ -66,6 +66,36 @@ __device__ __forceinline__ void packed_store(T *p, const Packed<T, V> &v)
         *reinterpret_cast<uint16_t *>(p) = static_cast<uint16_t>(v.w[0]);
 }
 
+// Of runs of 16-bit elements: those [from, to), one by one; the others are neither read (zeros) nor written.
+template <typename T, int V>
+__device__ __forceinline__ Packed<T, V> packed_load_part(const T *p, int from, int to)
+{
+    static_assert(sizeof(T) == 2, "halves of words");
+    Packed<T, V> v = packed_zero<T, V>();
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e >= from && e < to) v.w[e / 2] |= packed_load<T, 1>(p + e).w[0] << (e & 1 ? 16 : 0);
+    return v;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void packed_store_part(T *p, const Packed<T, V> &v, int from, int to)
+{
+    static_assert(sizeof(T) == 2, "halves of words");
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e >= from && e < to) *reinterpret_cast<uint16_t *>(p + e) = static_cast<uint16_t>(v.w[e / 2] >> (e & 1 ? 16 : 0));
+}
+
+// Zeros but for elements [from, to).
+template <typename T, int V>
+__device__ __forceinline__ void packed_trim(Packed<T, V> &v, int from, int to)
+{
+    static_assert(sizeof(T) == 2, "halves of words");
+#pragma unroll
+    for (int e = 0; e < V; ++e) v.w[e / 2] &= e >= from && e < to ? 0xFFFFFFFFu : e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+}
+
 template <typename T>
 __device__ __forceinline__ float half_of(uint32_t w, int upper);
 template <>

@@ -170,6 +170,40 @@ def test_widths_between_shares(torch, case):
     assert torch.equal(alone[0], dx)
 
 
+# Rows that begin and end between boundaries of 16 bytes: many remainders, widths at which the share or the way to read them changes,
+# several rows per thread, and the widest.
+BETWEEN = [
+    (5, 1, "bfloat16"), (9, 2, "float16"), (11, 7, "bfloat16"), (20, 9, "float16"), (40, 33, "bfloat16"), (20000, 65, "bfloat16"),
+    (33, 66, "float16"), (35, 129, "bfloat16"), (37, 250, "bfloat16"), (9000, 255, "bfloat16"), (3000, 577, "float16"),
+    (19, 759, "bfloat16"), (19, 763, "bfloat16"), (23, 1001, "float16"), (1300, 2001, "bfloat16"), (17, 2045, "bfloat16"),
+    (15, 3067, "float16"), (1000, 5001, "bfloat16"), (9, 8177, "float16"), (9, 8179, "bfloat16"), (7, 8191, "float16"),
+    (20000, 35, "float32"), (31, 1, "float32"), (31, 5, "float32"), (3000, 131, "float32"), (33, 254, "float32"),
+    (2000, 509, "float32"), (21, 511, "float32"),
+]
+
+
+@pytest.mark.parametrize("layout", ["dense", "wide"])
+@pytest.mark.parametrize("case", BETWEEN, ids=str)
+def test_rows_between_boundaries(torch, case, layout):
+    n, width, dtype = case
+    op = layer_norm.LayerNorm(width, eps=1e-5, dtype=getattr(torch, dtype))
+    x, r, dy, dsum = (make(torch, seed, n, width, dtype, layout, offset=0.5) for seed in (1, 2, 3, 4))
+    w, b = make(torch, 5, 1, width, "float32")[0], make(torch, 6, 1, width, "float32")[0]
+    room = [make(torch, 7, n, width, dtype, layout) for _ in range(3)]
+    saved = op.saved(n)
+    y, total = op.forward(x, w, b, residual=r, saved=saved, out=room[0], total=room[1])
+    assert torch.equal(total, x + r)
+    check_forward(f64(total), y, f64(w), f64(b), 1e-5, dtype)
+    dx, dw, db = op.backward(dy, total, w, saved, dsum=dsum, out=room[2])
+    check_backward(f64(total), f64(dy), f64(w), f64(dsum), 1e-5, dtype, dx, dw, db)
+    if layout == "wide":                      # nothing beside the columns
+        for v in room:
+            whole = v._base
+            assert torch.isnan(whole[:, :3]).all() and torch.isnan(whole[:, 3 + width:]).all()
+    again = op.backward(dy, total, w, saved, dsum=dsum, out=make(torch, 7, n, width, dtype, layout))
+    assert all(torch.equal(p, q) for p, q in zip(again, (dx, dw, db)))
+
+
 @pytest.mark.parametrize("width", [8, 64, 256, 576, 768, 1024, 8192])
 @pytest.mark.parametrize("n", [1, 2, 3])
 def test_few_rows(torch, n, width):
