@@ -18,8 +18,8 @@
  * Types.  x, residual, s, y, dy, dsum, dx are of the handle's type (binary32, bfloat16, binary16).  w, b, the saved
  * statistics and dw, db are binary32, as is all arithmetic; a result is rounded once when it is stored.  The variance
  * is summed from differences to the mean, which are formed first.  Every sum has a fixed order: the same call gives the
- * same bits (on arrays of the same strides and alignment).  A row with a NaN or an infinity in it gives NaN in that row (and in dw, db), and in no other.  Where the
- * variance is beyond binary32 (differences of 1e19), q is zero and y is b.
+ * same bits (on arrays of the same strides and alignment).  A row with a NaN or an infinity in it gives NaN in that row
+ * (and in dw, db), and in no other.  Where the variance is beyond binary32 (differences of 1e19), q is zero and y is b.
  *
  * Rows are contiguous, `width` elements, with a row stride in elements (inputs: >= 0, so that one row can serve for all;
  * outputs: >= width).  Any width and alignment to the element is taken; rows of whole 16-byte pieces are faster.
