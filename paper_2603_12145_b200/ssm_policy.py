@@ -32,6 +32,7 @@ import functools
 import math
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.graph import increment_version
 
 from . import gated_ffn, gated_recurrence, layer_norm, optimizers, pong, ssm
@@ -66,8 +67,14 @@ def first_order(backward):
     return wrapped
 
 
-def _wants_gradient(args):
-    return torch.is_grad_enabled() and any(isinstance(v, torch.Tensor) and v.requires_grad for v in args)
+def _differentiated(args):
+    """Whether autograd has to see the call: an input that requires a gradient, or one with a forward-mode tangent, which the
+    kernels would drop (a Function without a rule for it raises)."""
+    tensors = [v for v in args if isinstance(v, torch.Tensor)]
+    if torch.is_grad_enabled() and any(v.requires_grad for v in tensors):
+        return True
+    # (without an open level nothing carries one: 2 us less per call)
+    return getattr(forward_ad, "_current_level", 0) >= 0 and any(forward_ad.unpack_dual(v).tangent is not None for v in tensors)
 
 
 class ConvFunction(torch.autograd.Function):
@@ -93,7 +100,7 @@ class ScanFunction(torch.autograd.Function):
     @classmethod
     def apply(cls, op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out):
         args = (op, x, dt, a, b, c, d, z, dt_bias, reset, state, state_out)
-        if _wants_gradient(args):
+        if _differentiated(args):
             return super().apply(*args)
         return op.scan(x, dt, a, b, c, d=d, z=z, dt_bias=dt_bias, reset=reset, state=state, state_out=state_out)
 
@@ -118,7 +125,7 @@ class FfnFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, op, x, w_in, w_out):
-        return super().apply(op, x, w_in, w_out) if _wants_gradient((x, w_in, w_out)) else op.forward(x, w_in, w_out)
+        return super().apply(op, x, w_in, w_out) if _differentiated((x, w_in, w_out)) else op.forward(x, w_in, w_out)
 
     @staticmethod
     def forward(ctx, op, x, w_in, w_out):
@@ -140,7 +147,7 @@ class NormFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, op, x, residual, w, b):
-        if _wants_gradient((x, residual, w, b)):
+        if _differentiated((x, residual, w, b)):
             return super().apply(op, x, residual, w, b)
         return op.forward(x, w, b, residual=residual)
 
@@ -170,7 +177,7 @@ class RecurrenceFunction(torch.autograd.Function):
 
     @classmethod
     def apply(cls, op, x, r, i, a, reset, state, state_out):
-        if _wants_gradient((x, r, i, a, state)):
+        if _differentiated((x, r, i, a, state)):
             return super().apply(op, x, r, i, a, reset, state, state_out)
         return op.sequence(x, r, i, a, reset=reset, state=state, state_out=state_out)
 

@@ -1,0 +1,68 @@
+"""What the Functions of ssm_policy do with inputs that carry a forward-mode tangent, around stand-ins for the handles (plain
+torch on the CPU); without a GPU.  The handles read tensors by address, so that a tangent has nowhere to go: the call has to
+raise, as the Functions' own forward-mode rule does, and not to return a result that looks constant."""
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+from paper_2603_12145_b200 import ssm_policy
+
+
+class StandIn:
+    """A result of plain torch operations on the detached values: what reading by address sees."""
+
+    def saved(self, *sizes):
+        return (torch.zeros(1), torch.zeros(1)) if len(sizes) == 1 and self.pair else torch.zeros(1)
+
+    def __init__(self, pair=False):
+        self.pair = pair
+
+    def forward(self, x, *args, residual=None, saved=None):
+        y = x.detach() * 2.0
+        return y if residual is None else (y, x.detach() + residual.detach())
+
+    def sequence(self, x, *args, **kw):
+        return x.detach() * 2.0
+
+    scan = sequence
+
+
+def call(name, v):
+    """A Function's call with v its tensors by name; what is not there is a constant."""
+    x = torch.ones(1, 3, 2) if name in ("scan", "recurrence") else torch.ones(3, 2)
+    w = torch.ones(2)
+    at = lambda key, other: v.get(key, other)                                              # noqa: E731
+    if name == "norm":
+        return ssm_policy.NormFunction.apply(StandIn(), at("x", x), None, at("w", w), at("b", w))
+    if name == "added":
+        return ssm_policy.NormFunction.apply(StandIn(), at("x", x), at("residual", x), at("w", w), at("b", w))[0]
+    if name == "recurrence":
+        return ssm_policy.RecurrenceFunction.apply(StandIn(), at("x", x), at("r", x), at("i", x), at("a", -w), None,
+                                                   at("state", torch.ones(1, 2)), None)
+    if name == "scan":
+        return ssm_policy.ScanFunction.apply(StandIn(), at("x", x), at("dt", x), at("a", -torch.ones(2, 4)), at("b", torch.ones(1, 3, 4)),
+                                             torch.ones(1, 3, 4), w, x, w, None, None, None)
+    return ssm_policy.FfnFunction.apply(StandIn(pair=True), at("x", x), at("w_in", torch.ones(4, 2)), torch.ones(2, 2))
+
+
+TENSORS = {"norm": {"x": (3, 2), "w": (2,), "b": (2,)}, "added": {"x": (3, 2), "residual": (3, 2), "w": (2,)},
+           "recurrence": {"x": (1, 3, 2), "r": (1, 3, 2), "a": (2,), "state": (1, 2)},
+           "scan": {"x": (1, 3, 2), "dt": (1, 3, 2), "b": (1, 3, 4)}, "ffn": {"x": (3, 2), "w_in": (4, 2)}}
+
+
+@pytest.mark.parametrize("grad", [False, True])
+@pytest.mark.parametrize("name,key", [(n, k) for n, keys in TENSORS.items() for k in keys])
+def test_a_tangent_is_refused(name, key, grad):
+    with forward_ad.dual_level(), torch.set_grad_enabled(grad):
+        v = torch.full(TENSORS[name][key], -1.0 if key == "a" else 1.0)
+        with pytest.raises(NotImplementedError):
+            call(name, {key: forward_ad.make_dual(v, torch.ones_like(v))})
+
+
+@pytest.mark.parametrize("name", list(TENSORS))
+def test_without_one_the_call_goes_through(name):
+    want = call(name, {})
+    with forward_ad.dual_level():                    # nobody carries one
+        assert torch.equal(call(name, {}), want)
+        with torch.no_grad():
+            assert torch.equal(call(name, {}), want)
