@@ -173,7 +173,8 @@ class NormFunction(torch.autograd.Function):
 
 
 class RecurrenceFunction(torch.autograd.Function):
-    """gated_recurrence.GatedRecurrence.sequence with its gradients; the state at the start is a constant."""
+    """gated_recurrence.GatedRecurrence.sequence with its gradients, that of the state at the start among them.  state_out is
+    filled by address: what is computed from it is a constant here."""
 
     @classmethod
     def apply(cls, op, x, r, i, a, reset, state, state_out):
@@ -185,15 +186,16 @@ class RecurrenceFunction(torch.autograd.Function):
     def forward(ctx, op, x, r, i, a, reset, state, state_out):
         saved = op.saved(x.shape[0], x.shape[1])
         ctx.op = op
-        ctx.save_for_backward(x, r, i, a, reset, saved)
+        # (the kernels do not read the state again; the gradients depend on it)
+        ctx.save_for_backward(x, r, i, a, reset, saved, state if ctx.needs_input_grad[6] else None)
         return op.sequence(x, r, i, a, reset=reset, state=state, state_out=state_out, saved=saved)
 
     @staticmethod
     @first_order
     def backward(ctx, dy):
-        x, r, i, a, reset, saved = ctx.saved_tensors
-        g = ctx.op.backward(_dense_last(dy), x, r, i, a, saved, reset=reset)
-        return None, g["dx"], g["dr"], g["di"], g["da"], None, None, None
+        x, r, i, a, reset, saved, _ = ctx.saved_tensors
+        g = ctx.op.backward(_dense_last(dy), x, r, i, a, saved, reset=reset, want_dstate=ctx.needs_input_grad[6])
+        return None, g["dx"], g["dr"], g["di"], g["da"], None, g["dstate"], None
 
 
 def _dense_last(v):

@@ -66,3 +66,46 @@ def test_without_one_the_call_goes_through(name):
         assert torch.equal(call(name, {}), want)
         with torch.no_grad():
             assert torch.equal(call(name, {}), want)
+
+
+class Recurrence(StandIn):
+    """y_t = x_t + state (where no episode starts at the first step), and its gradients."""
+
+    def sequence(self, x, r, i, a, reset=None, state=None, state_out=None, saved=None):
+        return x.detach() + (0.0 if state is None else self.kept(reset) * state.detach().unsqueeze(1))
+
+    def kept(self, reset):
+        return 1.0 if reset is None else (reset[:, :1] == 0).unsqueeze(-1).float()
+
+    def backward(self, dy, x, r, i, a, saved, reset=None, dstate_out=None, want_dstate=False):
+        self.wanted = want_dstate
+        zero = torch.zeros_like(x)
+        return {"dx": dy.clone(), "dr": zero, "di": zero, "da": torch.zeros_like(a),
+                "dstate": (self.kept(reset) * dy).sum(1) if want_dstate else None}
+
+
+@pytest.mark.parametrize("alone", [False, True])
+@pytest.mark.parametrize("reset", [None, 0, 1])
+def test_the_state_at_the_start_has_its_gradient(alone, reset):
+    """With or without another input that requires one; none is formed where none is wanted."""
+    op, x, a = Recurrence(), torch.ones(2, 3, 4, requires_grad=not alone), -torch.ones(4)
+    state = torch.ones(2, 4, requires_grad=True)
+    mask = None if reset is None else torch.tensor([[reset, 0, 0], [0, 1, 0]], dtype=torch.uint8)
+    weight = torch.arange(24.0).view(2, 3, 4)
+    (weight * ssm_policy.RecurrenceFunction.apply(op, x, x, x, a, mask, state, None)).sum().backward()
+    want = weight.sum(1)
+    if reset:
+        want[0] = 0.0
+    assert torch.equal(state.grad, want)
+    if not alone:
+        ssm_policy.RecurrenceFunction.apply(op, x, x, x, a, mask, state.detach(), None).sum().backward()
+        assert op.wanted is False
+
+
+def test_a_second_derivative_by_the_state_is_refused():
+    op, x = Recurrence(), torch.ones(2, 3, 4, requires_grad=True)
+    state = torch.ones(2, 4, requires_grad=True)
+    (g,) = torch.autograd.grad(ssm_policy.RecurrenceFunction.apply(op, x, x, x, -torch.ones(4), None, state, None).sum(), x,
+                               create_graph=True)
+    with pytest.raises(RuntimeError, match="first derivatives only"):
+        torch.autograd.grad(g.sum(), state)
