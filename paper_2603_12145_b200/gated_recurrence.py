@@ -187,6 +187,8 @@ class GatedRecurrence:
     def _like(self, v):
         """An output [batch, time, channels] with the order of v's dimensions."""
         out = self.torch.empty_like(v)               # keeps the order of what is dense
+        if out.stride(2) != 1 and self.channels > 1:                     # (of overlapping rows the channels' place too)
+            out = self.torch.empty(v.shape, dtype=self.dtype, device=self.device)
         if out.stride(0) > out.stride(1) and v.stride(0) < v.stride(1):
             b, t = v.shape[0], v.shape[1]
             return self.torch.empty((t, b, self.channels), dtype=self.dtype, device=self.device).transpose(0, 1)

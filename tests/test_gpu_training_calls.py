@@ -50,3 +50,17 @@ def test_the_state_at_the_start_has_its_gradient(torch, batch, time, reset):
     size = tr.recurrence_grad(*v, mask.cpu().numpy(), f64(state.detach()), magnitude=True)["dstate"]
     assert (np.abs(f64(got) - want) <= 2.0 ** -12 * size).all()
     assert np.abs(want).max() > 0.1
+
+
+def test_overlapping_windows_as_input(torch):
+    """x, r and i as windows into a series, a step or a row apart: what dense copies give."""
+    batch, time, ch = 6, 30, 24
+    op = gated_recurrence.GatedRecurrence(ch, dtype=torch.float32)
+    a, dy = -torch.exp(normal(torch, 1, ch)), normal(torch, 2, batch, time, ch)
+    for strides in ((time, 1, 1), (1, batch, 1), (1, 1, 1), (0, ch, 1), (0, 0, 1)):
+        x, r, i = (normal(torch, 3 + k, 1000).as_strided((batch, time, ch), strides) for k in range(3))
+        dense = [v.contiguous() for v in (x, r, i)]
+        saved, kept = op.saved(batch, time), op.saved(batch, time)
+        assert torch.equal(op.sequence(x, r, i, a, saved=saved), op.sequence(*dense, a, saved=kept))
+        got, want = op.backward(dy, x, r, i, a, saved), op.backward(dy, *dense, a, kept)
+        assert all(torch.equal(got[k], want[k]) for k in ("dx", "dr", "di", "da"))

@@ -5,7 +5,7 @@ import pytest
 import torch
 from torch.autograd import forward_ad
 
-from paper_2603_12145_b200 import ssm_policy
+from paper_2603_12145_b200 import gated_recurrence, ssm_policy
 
 
 class StandIn:
@@ -109,3 +109,18 @@ def test_a_second_derivative_by_the_state_is_refused():
                                create_graph=True)
     with pytest.raises(RuntimeError, match="first derivatives only"):
         torch.autograd.grad(g.sum(), state)
+
+
+# ---- the recurrence's outputs ---------------------------------------------------------------
+
+
+@pytest.mark.parametrize("strides", [(40, 8, 1), (8, 32, 1), (0, 8, 1), (8, 0, 1), (0, 0, 1), (5, 1, 1), (1, 5, 1), (1, 1, 1), (100, 3, 1),
+                                     (3, 100, 1)], ids=str)
+def test_outputs_have_contiguous_rows_that_lie_apart(strides):
+    """Whatever the strides of the input: expanded ones and overlapping windows among them."""
+    op = object.__new__(gated_recurrence.GatedRecurrence)
+    op.torch, op.dtype, op.channels, op.device, op.h = torch, torch.float32, 8, torch.device("cpu"), None
+    v = torch.zeros(1000).as_strided((4, 5, 8), strides)
+    out = op._like(v)
+    assert out.shape == v.shape and out.stride(2) == 1 and out.is_contiguous() == (strides[0] >= strides[1])
+    assert out.is_contiguous() or out.transpose(0, 1).is_contiguous()
