@@ -70,23 +70,40 @@ __device__ __forceinline__ float rsq(float v)
     return r;
 }
 
-// 1 / (1 + e^-v); the exponent's rounding, |v| 2^-24 of the result, is below what matters: where |v| is large, so is the
-// distance to where the sigmoid moves.
+// e^-v of binary32 gates, `most` bounding -v: the exponent carries its low part, without which its rounding would be |v| 2^-24 of
+// the result (gates down to -80: 62 units of 2^-24 where 4 remain; 256 x 128 x 1,152 forward 113 against 109 us).  Below e^-104
+// nothing is left, and an infinite exponent has no low part.  Gates of 16 bits do without: their own rounding moves the result by
+// more.
 template <typename F>
+__device__ __forceinline__ F exp_minus(F v, float most)
+{
+    return ssm_k::exp_of(each([&](float e) { return ssm_k::at_least(ssm_k::at_most(-e, most), -104.0f); }, v));
+}
+
+// 1 / (1 + e^-v), T the type that v comes in.  (Beyond e^88 the reciprocal is below the normal numbers: zero.)
+template <typename T, typename F>
 __device__ __forceinline__ F sigmoid(F v)
 {
     constexpr int V = sizeof(F) / 4;
-    return each([](float e) { return rcp(e); },
-                add(each([](float e) { return ex2(e); }, mul(v, all<V>(-kLog2e))), all<V>(1.0f)));
+    F e;
+    if constexpr (sizeof(T) == 4)
+        e = exp_minus(v, 88.0f);
+    else
+        e = each([](float x) { return ex2(x); }, mul(v, all<V>(-kLog2e)));
+    return each([](float x) { return rcp(x); }, add(e, all<V>(1.0f)));
 }
 
-// The same, and 1 - sigmoid(v) to full relative precision.  (Beyond 2^126 the exponential stays there: its product with
+// The same, and 1 - sigmoid(v) to full relative precision.  (The exponential stays within 2^126: its product with
 // the sigmoid is one, not infinity times zero.)
-template <typename F>
+template <typename T, typename F>
 __device__ __forceinline__ F sigmoid(F v, F &rest)
 {
     constexpr int V = sizeof(F) / 4;
-    const F e = each([](float x) { return ex2(ssm_k::at_most(x, 126.0f)); }, mul(v, all<V>(-kLog2e)));
+    F e;
+    if constexpr (sizeof(T) == 4)
+        e = exp_minus(v, 87.3f);
+    else
+        e = each([](float x) { return ex2(ssm_k::at_most(x, 126.0f)); }, mul(v, all<V>(-kLog2e)));
     const F s = each([](float x) { return rcp(x); }, add(e, all<V>(1.0f)));
     rest = mul(e, s);
     return s;
@@ -264,8 +281,8 @@ k_forward(const Shape s, const Params<T> p)
                     if (at.live) store_floats(saved, h);
                     saved += s.channels;
                 }
-                const F L = mul(a, sigmoid(widen(r.v[k])));
-                h = advance(decay_less_one(L), sigmoid(widen(i.v[k])), widen(x.v[k]), h);
+                const F L = mul(a, sigmoid<T>(widen(r.v[k])));
+                h = advance(decay_less_one(L), sigmoid<T>(widen(i.v[k])), widen(x.v[k]), h);
                 if constexpr (kEnds) {
                     span = add(span, L);
                 } else {
@@ -407,7 +424,7 @@ k_backward(const Shape s, const Params<T> p)
 #pragma unroll
                     for (int k = K - 1; k >= 0; --k) {
                         if (!plain.value && t + k >= at.t1) continue;
-                        const F L = mul(a, sigmoid(widen(r.v[k]))), gt = add(g, widen(dy.v[k]));
+                        const F L = mul(a, sigmoid<T>(widen(r.v[k]))), gt = add(g, widen(dy.v[k]));
                         g = fma(decay_less_one(L), gt, gt);
                         span = add(span, L);
                         if (!plain.value && (resets >> k) & 1u) {
@@ -421,8 +438,8 @@ k_backward(const Shape s, const Params<T> p)
 #pragma unroll
                     for (int k = 0; k < K; ++k) {
                         F rest;
-                        gate[k] = sigmoid(widen(r.v[k]), rest);
-                        in[k] = sigmoid(widen(i.v[k]), out[k]);
+                        gate[k] = sigmoid<T>(widen(r.v[k]), rest);
+                        in[k] = sigmoid<T>(widen(i.v[k]), out[k]);
                         const F L = mul(a, gate[k]);
                         slope[k] = mul(L, rest);             // dL / dr
                         d[k] = decay_less_one(L);
@@ -526,7 +543,7 @@ k_step(const Step<T> p)
     const bool fresh = p.done != nullptr && p.done[n * p.done_stride] != 0;
     float h[V];
     if constexpr (V == 1) {
-        h[0] = advance(decay_less_one(mul(__ldg(p.a + c), sigmoid(widen(r)))), sigmoid(widen(i)), widen(x),
+        h[0] = advance(decay_less_one(mul(__ldg(p.a + c), sigmoid<T>(widen(r)))), sigmoid<T>(widen(i)), widen(x),
                        fresh ? 0.0f : packed_get<float, 1>(state, 0));
     } else {
 #pragma unroll
@@ -534,7 +551,7 @@ k_step(const Step<T> p)
             auto two = [&](const auto &v) { return pair(packed_get<T, V>(v, e), packed_get<T, V>(v, e + 1)); };
             const Pair before = fresh ? pair(0.0f, 0.0f) : pair(packed_get<float, V>(state, e), packed_get<float, V>(state, e + 1));
             const Pair a = pair(__ldg(p.a + c + e), __ldg(p.a + c + e + 1));
-            const Pair v = advance(decay_less_one(mul(a, sigmoid(two(r)))), sigmoid(two(i)), two(x), before);
+            const Pair v = advance(decay_less_one(mul(a, sigmoid<T>(two(r)))), sigmoid<T>(two(i)), two(x), before);
             h[e] = lo(v);
             h[e + 1] = hi(v);
         }

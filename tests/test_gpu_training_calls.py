@@ -64,3 +64,39 @@ def test_overlapping_windows_as_input(torch):
         assert torch.equal(op.sequence(x, r, i, a, saved=saved), op.sequence(*dense, a, saved=kept))
         got, want = op.backward(dy, x, r, i, a, saved), op.backward(dy, *dense, a, kept)
         assert all(torch.equal(got[k], want[k]) for k in ("dx", "dr", "di", "da"))
+
+
+@pytest.mark.parametrize("ch", [64, 33])
+def test_binary32_gates_keep_their_relative_precision(torch, ch):
+    """Input gates from all but closed (e^-80) to all but open, with a decay that is nothing (a = -50, its gate open), so that y is
+    the gate itself times x = 1.  In units of 2^-24 a sigmoid has 8 (four of the exponential, one of 1 + e, two of the reciprocal,
+    one of the exponent's low part), the gain's root 4, the products and the last rounding one each: 16; its derivative a sigmoid
+    and the exponential more: 32.  The exponent rounded to one number would be off by 62 at -80."""
+    n = 2000
+    op = gated_recurrence.GatedRecurrence(ch, dtype=torch.float32)
+    gate = torch.linspace(-80.0, 80.0, n * ch, device="cuda").view(n, 1, ch)
+    x, r, a = torch.ones_like(gate), torch.full_like(gate, 60.0), torch.full((ch,), -50.0, device="cuda")
+    si = tr.sigmoid(f64(gate))
+    saved = op.saved(n, 1)
+    got = op.sequence(x, r, gate, a, saved=saved)
+    g = op.backward(x, x, r, gate, a, saved)
+    one = op.step(x[:, 0], r[:, 0], gate[:, 0], a, torch.zeros((n, ch), device="cuda"))
+    slope = si * tr.sigmoid(-f64(gate))
+    for name, v, want, units in (("y", got, si, 16), ("step", one[:, None], si, 16), ("dx", g["dx"], si, 16), ("di", g["di"], slope, 32)):
+        err = np.abs(f64(v) / want - 1.0).max() / U
+        assert err <= units, (name, err)
+
+
+def test_binary32_gates_of_any_size(torch):
+    """Infinite, huge and vanishing gates, and one that is no number, in its channel alone."""
+    v = torch.tensor([float("-inf"), -3e38, -104.0, -88.5, -87.4, 0.0, 90.0, 3e38, float("inf"), float("nan")], device="cuda")
+    op = gated_recurrence.GatedRecurrence(10, dtype=torch.float32)
+    x, a = torch.ones((3, 5, 10), device="cuda"), torch.full((10,), -1.0, device="cuda")
+    open_ = torch.full_like(x, 60.0)
+    gate = v.expand(3, 5, 10).contiguous()
+    for r, i in ((open_, gate), (gate, open_)):
+        saved = op.saved(3, 5)
+        y = op.sequence(x, r, i, a, state=torch.ones((3, 10), device="cuda"), saved=saved)
+        g = op.backward(x, x, r, i, a, saved)
+        for out in (y, g["dx"], g["dr"], g["di"]):
+            assert torch.isfinite(out[..., :9]).all() and torch.isnan(out[..., 9]).all()
