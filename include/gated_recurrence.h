@@ -25,8 +25,9 @@
  * their gradients are binary32, as is all arithmetic; a result is rounded once when it is stored.  The decay enters as
  * h + (e^L - 1) h with e^L - 1 to full relative precision, so that slow channels gather no bias; of a fast one e^L is off by
  * 2^-25 of one.  The gates' sigmoids are exact to some units of 2^-24 relative in binary32, in the 16-bit types
- * to the rounding of their argument.  Every sum has a fixed order: the same call gives the same bits.  Sequence and single-token forms
- * go through the same states.
+ * to the rounding of their argument.  Every sum has a fixed order: the same call gives the same bits.  Single tokens go
+ * through the states of the sequence bit for bit where it is taken in one piece (a forward workspace of 0 bytes); a row whose time is
+ * cut starts its pieces from chained values, which agree but for roundings.
  *
  * Sequences are described by gated_recurrence_seq: element (n, t, c) of a [batch][time][channels] array is
  * ptr[n * stride_b + t * stride_t + c], strides in elements; batch and time are at least 1.  A time-major rollout
