@@ -1357,7 +1357,7 @@ k_small(const __grid_constant__ SmallArgs p, const T *g)
         __syncthreads();
         tc_fence_after_sync();
     }
-    if (!ok && lane == 0) atomicExch(p.err, 1);
+    if (!ok) atomicExch(p.err, 1);                                   // (whichever thread gave up)
     cluster_sync_all();                                              // the others may still write here
     if (warp == 0) {
         __syncwarp();
