@@ -772,7 +772,9 @@ bool count_blocks(layer_norm *p)
     return true;
 }
 
-// How a call's arrays can be read.  add() takes each; single(): a parameter that is not on a boundary.
+// How a call's arrays can be read: add() takes each, access() decides.  Whole vectors need the parameters (params_whole) and all rows on
+// boundaries; between boundaries the rows have to lie alike and the width has to be offered, the parameters lie as they like (whole
+// rows with other parameters come here too); else single elements.
 struct Lie {
     const layer_norm *p;
     int64_t n;

@@ -94,7 +94,6 @@ struct Iteration {
     int batch, steps;
     int tall;               // rows > cols: the diagonal's factors go with columns
     int share;              // pairs per cluster: 1, 2 or 4
-    int ld;                 // elements between rows of X
     int ldk;                // of O and P
     int dk;                 // elements between the diagonals of two matrices
     float a, b, c;
@@ -1604,7 +1603,6 @@ int run(orthogonal *p, const T *g, int64_t g_batch, int64_t g_row, __nv_bfloat16
     q.batch = static_cast<int>(batch);
     q.steps = p->steps;
     q.tall = tall;
-    q.ld = static_cast<int>(w.ld);
     q.ldk = static_cast<int>(w.ldk);
     q.dk = static_cast<int>(w.dk);
     q.a = p->a;
