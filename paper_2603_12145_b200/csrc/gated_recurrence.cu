@@ -70,14 +70,17 @@ __device__ __forceinline__ float rsq(float v)
     return r;
 }
 
-// e^-v of binary32 gates, `most` bounding -v: the exponent carries its low part, without which its rounding would be |v| 2^-24 of
-// the result (gates down to -80: 62 units of 2^-24 where 4 remain; 256 x 128 x 1,152 forward 113 against 109 us).  Below e^-104
-// nothing is left, and an infinite exponent has no low part.  Gates of 16 bits do without: their own rounding moves the result by
-// more.
+// e^-v of binary32 gates, `most` bounding -v = n.  The rounded exponent t = n log2 e alone would be off by |v| 2^-24 of the result (62
+// units of 2^-24 for gates down to -80): 2^t is multiplied by 1 + (n - t ln 2), which leaves t times ln 2's own rounding, 2e-9 (6
+// units in all; 256 x 128 x 1,152 forward 110 against 109 us).  Below e^-104 nothing is left, and an infinite exponent has no
+// difference.  Gates of 16 bits do without: their own rounding moves the result by more.
 template <typename F>
 __device__ __forceinline__ F exp_minus(F v, float most)
 {
-    return ssm_k::exp_of(each([&](float e) { return ssm_k::at_least(ssm_k::at_most(-e, most), -104.0f); }, v));
+    constexpr int V = sizeof(F) / 4;
+    const F n = each([&](float e) { return ssm_k::at_least(ssm_k::at_most(-e, most), -104.0f); }, v);
+    const F t = mul(n, all<V>(kLog2e)), e = each([](float x) { return ex2(x); }, t);
+    return fma(e, fma(t, all<V>(-ssm_k::kLn2), n), e);
 }
 
 // 1 / (1 + e^-v), T the type that v comes in.  (Beyond e^88 the reciprocal is below the normal numbers: zero.)
@@ -232,9 +235,10 @@ struct Block {
     }
 };
 
-// kEnds: the first pass over segments.
+// kEnds: the first pass over segments.  (Binary32 in three blocks per SM: 1 x 4,096 x 2,048 53 us, 62 with the two that 206 registers
+// leave.)
 template <typename T, int V, bool kEnds>
-__global__ void __launch_bounds__(kThreads, sizeof(T) != 2 ? 1 : kEnds ? 4 : 5)
+__global__ void __launch_bounds__(kThreads, sizeof(T) != 2 ? 3 : kEnds ? 4 : 5)
 k_forward(const Shape s, const Params<T> p)
 {
     using F = Vals<V>;

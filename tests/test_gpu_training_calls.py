@@ -73,9 +73,9 @@ def test_overlapping_windows_as_input(torch):
 @pytest.mark.parametrize("ch", [64, 33])
 def test_binary32_gates_keep_their_relative_precision(torch, ch):
     """Input gates from all but closed (e^-80) to all but open, with a decay that is nothing (a = -50, its gate open), so that y is
-    the gate itself times x = 1.  In units of 2^-24 a sigmoid has 8 (four of the exponential, one of 1 + e, two of the reciprocal,
-    one of the exponent's low part), the gain's root 4, the products and the last rounding one each: 16; its derivative a sigmoid
-    and the exponential more: 32.  The exponent rounded to one number would be off by 62 at -80."""
+    the gate itself times x = 1.  In units of 2^-24 a sigmoid has at most 12 (four of the exponential, 115 * 2e-9 / 2^-24 = 4 of its
+    exponent, one of 1 + e, two of the reciprocal, one of a product), the products and the last rounding one each: 16; its derivative a
+    sigmoid and the exponential more: 32.  The exponent rounded to one number would be off by 62 at -80."""
     n = 2000
     op = gated_recurrence.GatedRecurrence(ch, dtype=torch.float32)
     gate = torch.linspace(-80.0, 80.0, n * ch, device="cuda").view(n, 1, ch)
