@@ -18,7 +18,7 @@
  * size of the whole result late in the iteration, are binary32 and enter the products as exact row or column factors.
  * Against binary64 the update is off by its own rounding (1.7e-3 relative, root mean square) and 2e-4 to 8e-4 more; an
  * exactly rank-deficient G by up to 2e-3 more (the directions that are not there take up rounding errors).  So an evaluation
- * in binary32 differs from it by 1.2e-3 (root mean square; elements by one step of bfloat16 at most), whatever the type of G.  X is held
+ * in binary32 differs from it by 1.2e-3 (root mean square), whatever the type of G.  X is held
  * times 2^13 and stays finite as long as none of its elements exceeds 7 in magnitude, which the usual coefficients
  * keep; other ones are the caller's choice.  The same call gives the same bits.  An infinity or NaN in a
  * matrix gives NaN in its update, and in no other matrix's.
